@@ -148,6 +148,135 @@ MOE_API void attn_destroy(attn_ctx *ctx);
  * failing attn_init on this thread. */
 MOE_API const char *attn_last_error(const attn_ctx *ctx);
 
+/* ------------------------------------------------------------ paged cache --
+ * The cache of many sequences at once, handed out in pages, for a server that
+ * generates for a batch of them (the single-sequence cache above is one run of
+ * positions).  A sequence's position p lies in page table[p / page_size] at
+ * slot p % page_size; which pages are whose is the caller's business.  Two
+ * operators work on it, each on the batch that attn_paged_set_batch set:
+ *
+ *   attn_paged_append  rotates the new tokens' queries and keys by their
+ *                      positions (as attn_forward: pairs i and i + head_dim/2,
+ *                      angle pos * theta^(-2i/head_dim)), writes the queries
+ *                      out as bf16 and the keys and values to their pages;
+ *   attn_paged_attend  o_j = bf16( softmax_p(q_j . k_p / sqrt(head_dim)) v_p ),
+ *                      p over the token's sequence's positions up to its own;
+ *                      query head j uses key/value head j / (n_heads /
+ *                      n_kv_heads).
+ *
+ * attn_forward_paged is the attention block on top of them.
+ *
+ * Pages hold bf16, or with ATTN_PAGED_E4M3 one byte per element: e4m3 (1 sign,
+ * 4 exponent, 3 mantissa bits, bias 7, largest value 448, no infinities) times
+ * a scale per page and key/value head, keys and values apart.  A scale is a
+ * power of two, so a stored value is code * scale exactly and exactly a bf16.
+ * Append sets it to 2^e, e the least integer >= -100 such that 448 * 2^e is no
+ * less than any finite new value of the page.  Where the page already
+ * holds earlier tokens of the sequence (the first new slot is not slot 0), the
+ * scale never falls, and where it grows the earlier codes are rounded again to
+ * the new one (which changes only values below 2^-6 of the new scale).  Codes
+ * are rounded to nearest, ties to even, once, from the fp32 value.
+ *
+ * Values that are not finite: bf16 pages keep them; e4m3 pages store them as
+ * NaN.  A row that sees one is not finite in that dimension (in all, if it is
+ * a key); rows that do not see it are untouched by it, and so are all rows by
+ * what slots behind a sequence's last token hold. */
+
+typedef struct attn_paged_ctx attn_paged_ctx;
+
+#define ATTN_PAGED_E4M3 0x1 /* pages of e4m3 with a scale per page and key/value head */
+
+/*   n_heads, n_kv_heads, head_dim : as attn_config, with at most 16 query
+ *                heads per key/value head and n_heads * head_dim at most 65536.
+ *   page_size  : positions per page, 16, 32, 64, 128 or 256.
+ *   n_pages    : pages in each layer's pool, at most 2^24 (a page number means
+ *                the same page of every layer).
+ *   n_layers   : layers in the cache, 1 .. 1024.
+ *   max_seqs   : most sequences of a batch, 1 .. 4096.
+ *   max_tokens : most new tokens of a batch, all sequences together, 1 .. 32768.
+ *   max_blocks : most pages of one sequence, 1 .. 65536 (max_blocks *
+ *                page_size positions at most 2^24); max_seqs * max_blocks at
+ *                most 2^26.
+ *   rope_theta : base of the rotary frequencies (> 1).
+ *   flags      : 0 or ATTN_PAGED_E4M3. */
+typedef struct {
+    int32_t n_heads, n_kv_heads, head_dim, page_size;
+    int32_t n_pages, n_layers, max_seqs, max_tokens, max_blocks;
+    float rope_theta;
+    int32_t flags;
+} attn_paged_config;
+
+/* Bytes of the caller-allocated cache and workspace; 0 if cfg is invalid.
+ * Cache layout, per layer: K, then V, each [n_pages][n_kv_heads][page_size]
+ * [head_dim] of bf16 or e4m3 codes, then with ATTN_PAGED_E4M3 the scales of K
+ * and of V, each fp32 [n_pages][n_kv_heads] padded to 256 B.  A caller may
+ * write pages there directly (scales: powers of two from 2^-100 to 2^120). */
+MOE_API size_t attn_paged_cache_bytes(const attn_paged_config *cfg);
+MOE_API size_t attn_paged_workspace_bytes(const attn_paged_config *cfg);
+
+/* Validates cfg and records the two caller-allocated device buffers (256-byte
+ * aligned, kept until attn_paged_destroy).  Allocates only the host-side
+ * context.  Errors as attn_init; the message is readable through
+ * attn_paged_last_error(NULL). */
+MOE_API moe_status attn_paged_init(const attn_paged_config *cfg, void *cache, void *workspace,
+                                   attn_paged_ctx **out);
+
+/* Sets the batch that the calls after it work on (one per generation step,
+ * for all layers).  All arrays are host memory, read before the call returns:
+ * n_new and pos0 int32 [n_seqs], sequence s having n_new[s] >= 0 new tokens
+ * behind pos0[s] >= 0 cached ones; table int32 [n_seqs][ld], its row s the
+ * sequence's pages (ceil((pos0 + n_new) / page_size) entries are read).  The
+ * batch's tokens are the sequences' new tokens in order, T = sum of n_new.
+ * A table entry of -1 is no page: its positions are left out of the
+ * attention (a row that sees no position gives zeros).
+ * Enqueues one small kernel on stream that hands the batch to the device;
+ * allocates no device memory (the first calls allocate pinned host memory).
+ * Errors, the previous batch then staying set: MOE_E_ARG (a NULL array,
+ * negative counts, ld too small, an entry outside -1 .. n_pages - 1, a new
+ * token without a page, a page that two sequences or two blocks of one would
+ * write), MOE_E_CAPACITY (n_seqs, T or a sequence's length beyond the
+ * config's), MOE_E_STATE (stream is capturing a graph), MOE_E_HIP.
+ * A graph captured over append and attend calls replays on the batch that is
+ * set when it is replayed, which must have as many sequences and the same
+ * n_new as the one set at its capture (positions and pages may differ). */
+MOE_API moe_status attn_paged_set_batch(attn_paged_ctx *ctx, int32_t n_seqs, const int32_t *n_new,
+                                        const int32_t *pos0, const int32_t *table, int32_t ld,
+                                        moe_stream_t stream);
+
+/* Types of attn_paged_append's q | k | v. */
+typedef enum { ATTN_QKV_F32 = 0, ATTN_QKV_BF16 = 1 } attn_qkv_type;
+
+/* q | k | v of the batch's T tokens (rows of (n_heads + 2 n_kv_heads) head_dim
+ * elements, ld elements apart, rows 16-byte aligned) in; q out bf16 [T][n_heads
+ * head_dim]; keys and values to the pages of layer `layer`; slots of other
+ * positions keep their values (see above for scales that grow).  q may not
+ * overlap qkv.  Requires a batch (MOE_E_STATE); T == 0 is a no-op. */
+MOE_API moe_status attn_paged_append(attn_paged_ctx *ctx, int32_t layer, const void *qkv, int64_t ld,
+                                     int32_t type, uint16_t *q, moe_stream_t stream);
+
+/* Attention of the batch's T tokens, q bf16 [T][n_heads head_dim] (rotated),
+ * over their sequences' positions up to their own in layer `layer`'s pages,
+ * which must hold them; out bf16 [T][n_heads head_dim] (not q). */
+MOE_API moe_status attn_paged_attend(attn_paged_ctx *ctx, int32_t layer, const uint16_t *q, uint16_t *out,
+                                     moe_stream_t stream);
+
+/* Frees the host-side context and its pinned memory (never the caller's
+ * buffers); waits for a batch still on its way to the device. */
+MOE_API void attn_paged_destroy(attn_paged_ctx *ctx);
+
+/* Message of the last failing call on ctx; with ctx == NULL, of the last
+ * failing attn_paged_init on this thread. */
+MOE_API const char *attn_paged_last_error(const attn_paged_ctx *ctx);
+
+/* attn_forward on a paged cache: the block on the T tokens of the batch set on
+ * `cache`, x and y bf16 [T, d] (y may be x), layer `layer` of both contexts;
+ * with z not NULL also z = norm2(y), as attn_forward_norm.  The contexts must
+ * agree in n_heads, n_kv_heads, head_dim and rope_theta (MOE_E_SHAPE) and
+ * share one device; T <= max_tokens of ctx, whose own cache is not used.  Errors as
+ * attn_forward and attn_forward_norm; MOE_E_STATE without a batch. */
+MOE_API moe_status attn_forward_paged(attn_ctx *ctx, int32_t layer, attn_paged_ctx *cache, const uint16_t *x,
+                                      uint16_t *y, uint16_t *z, moe_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

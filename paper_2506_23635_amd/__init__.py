@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libmoe.so")
 
 MOE_OK = 0
 MOE_PARTIAL_F32 = 0x1   # moe_config.flags: y of moe_forward is fp32 [T, d]
+ATTN_PAGED_E4M3 = 0x1   # attn_paged_config.flags: pages of e4m3 with scales
+QKV_F32, QKV_BF16 = 0, 1   # attn_qkv_type
 DIAG_MAX_WG = 512    # MOE_DIAG_MAX_WG of include/moe.h
 WS_REGIONS = ["route_partials", "logits", "topk_idx", "topk_w", "counts", "offsets", "pair_row",
               "row_token", "active", "tiles", "n_tiles", "h", "o"]   # moe_ws_region order
@@ -34,7 +36,10 @@ EXPORTED = ["moe_weight_bytes", "moe_workspace_bytes", "moe_workspace_map", "moe
             "attn_weight_bytes", "attn_cache_bytes", "attn_workspace_bytes", "attn_init",
             "attn_load_layer", "attn_load_post_norm", "attn_forward", "attn_forward_norm",
             "attn_intermediates", "attn_profile_enable", "attn_profile_read", "attn_destroy",
-            "attn_last_error"]
+            "attn_last_error",
+            "attn_paged_cache_bytes", "attn_paged_workspace_bytes", "attn_paged_init",
+            "attn_paged_set_batch", "attn_paged_append", "attn_paged_attend", "attn_paged_destroy",
+            "attn_paged_last_error", "attn_forward_paged"]
 
 ATTN_KERNEL_KINDS = ["norm", "qkv", "score", "combine", "out", "pack", "rope", "residual",
                      "post_norm"]
@@ -65,6 +70,15 @@ class AttnConfig(ctypes.Structure):
                 ("n_layers", ctypes.c_int32), ("max_seq", ctypes.c_int32),
                 ("max_tokens", ctypes.c_int32), ("rope_theta", ctypes.c_float),
                 ("norm_eps", ctypes.c_float), ("flags", ctypes.c_int32)]
+
+
+class PagedConfig(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_layers", ctypes.c_int32),
+                ("max_seqs", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("max_blocks", ctypes.c_int32), ("rope_theta", ctypes.c_float),
+                ("flags", ctypes.c_int32)]
 
 
 class MoeError(RuntimeError):
@@ -131,8 +145,23 @@ def lib():
         L.attn_destroy.restype = None
         L.attn_last_error.argtypes = [P]
         L.attn_last_error.restype = ctypes.c_char_p
+        pcfg = ctypes.POINTER(PagedConfig)
+        for fn in ("attn_paged_cache_bytes", "attn_paged_workspace_bytes"):
+            getattr(L, fn).argtypes = [pcfg]
+            getattr(L, fn).restype = ctypes.c_size_t
+        L.attn_paged_init.argtypes = [pcfg, P, P, ctypes.POINTER(P)]
+        L.attn_paged_set_batch.argtypes = [P, I, P, P, P, I, P]
+        L.attn_paged_append.argtypes = [P, I, P, ctypes.c_int64, I, P, P]
+        L.attn_paged_attend.argtypes = [P, I, P, P, P]
+        L.attn_paged_destroy.argtypes = [P]
+        L.attn_paged_destroy.restype = None
+        L.attn_paged_last_error.argtypes = [P]
+        L.attn_paged_last_error.restype = ctypes.c_char_p
+        L.attn_forward_paged.argtypes = [P, I, P, P, P, P, P]
         for fn in ("attn_init", "attn_load_layer", "attn_load_post_norm", "attn_forward",
-                   "attn_forward_norm", "attn_intermediates",
+                   "attn_forward_norm", "attn_intermediates", "attn_paged_init",
+                   "attn_paged_set_batch", "attn_paged_append", "attn_paged_attend",
+                   "attn_forward_paged",
                    "attn_profile_enable", "attn_profile_read"):
             getattr(L, fn).restype = ctypes.c_int
         for fn in ("moe_init", "moe_load_expert", "moe_load_router", "moe_route", "moe_forward",
@@ -636,6 +665,17 @@ class AttnLayer:
                           _tensor_ptr(y, "y", n, bf, self.device),
                           _tensor_ptr(z, "z", n, bf, self.device), T, pos0, self.stream)
 
+    def forward_paged(self, layer, cache, x, y, z=None):
+        """attn_forward_paged: the block on the T tokens of the batch set on `cache` (a
+        PagedCache of the same device); z, if given: the post-attention norm of y."""
+        if cache.device != self.device:
+            raise MoeError(-1, f"the cache is on {cache.device}, expected {self.device}")
+        n, bf = cache.tokens * self.cfg.d_model, _bf16_types(self.torch)
+        with self.torch.cuda.device(self.device):
+            attn_forward_paged(self.ctx, layer, cache.ctx, _tensor_ptr(x, "x", n, bf, self.device),
+                               _tensor_ptr(y, "y", n, bf, self.device),
+                               None if z is None else _tensor_ptr(z, "z", n, bf, self.device), self.stream)
+
     def intermediates(self, T):
         """Copies of the last forward's h, qkv, q, a, o (numpy; bf16 as uint16)."""
         import numpy as np
@@ -654,3 +694,171 @@ class AttnLayer:
             a = t.cpu().numpy()
             out.append(a.view(np.uint16) if dt == torch.int16 else a)
         return dict(zip(["h", "qkv", "q", "a", "o"], out))
+
+
+# ------------------------------------------------------------ paged cache --
+
+def _pcheck(ctx, status: int):
+    if status != MOE_OK:
+        raise MoeError(status, lib().attn_paged_last_error(ctx).decode())
+
+
+def make_paged_config(n_heads, n_kv_heads, head_dim, page_size=64, n_pages=1, n_layers=1, max_seqs=1,
+                      max_tokens=16, max_blocks=64, rope_theta=5e5, flags=0) -> PagedConfig:
+    return PagedConfig(n_heads, n_kv_heads, head_dim, page_size, n_pages, n_layers, max_seqs, max_tokens,
+                       max_blocks, rope_theta, flags)
+
+
+def attn_paged_cache_bytes(cfg: PagedConfig) -> int:
+    return int(lib().attn_paged_cache_bytes(ctypes.byref(cfg)))
+
+
+def attn_paged_workspace_bytes(cfg: PagedConfig) -> int:
+    return int(lib().attn_paged_workspace_bytes(ctypes.byref(cfg)))
+
+
+def attn_paged_init(cfg: PagedConfig, cache_ptr: int, workspace_ptr: int) -> int:
+    out = ctypes.c_void_p()
+    _pcheck(None, lib().attn_paged_init(ctypes.byref(cfg), cache_ptr, workspace_ptr, ctypes.byref(out)))
+    return out.value
+
+
+def attn_paged_set_batch(ctx, n_seqs, n_new_ptr, pos0_ptr, table_ptr, ld, stream=0):
+    _pcheck(ctx, lib().attn_paged_set_batch(ctx, n_seqs, n_new_ptr, pos0_ptr, table_ptr, ld, stream))
+
+
+def attn_paged_append(ctx, layer, qkv_ptr, ld, qkv_type, q_ptr, stream=0):
+    _pcheck(ctx, lib().attn_paged_append(ctx, layer, qkv_ptr, ld, qkv_type, q_ptr, stream))
+
+
+def attn_paged_attend(ctx, layer, q_ptr, out_ptr, stream=0):
+    _pcheck(ctx, lib().attn_paged_attend(ctx, layer, q_ptr, out_ptr, stream))
+
+
+def attn_forward_paged(ctx, layer, cache_ctx, x_ptr, y_ptr, z_ptr, stream=0):
+    _acheck(ctx, lib().attn_forward_paged(ctx, layer, cache_ctx, x_ptr, y_ptr, z_ptr, stream))
+
+
+class PagedCache:
+    """Owns a paged key/value cache's context plus its torch-allocated pages and
+    workspace on one GPU (argument marshalling only)."""
+
+    def __init__(self, cfg: PagedConfig, device="cuda", cache=None, workspace=None):
+        """cache / workspace: caller-owned uint8 device tensors of at least
+        attn_paged_cache_bytes / attn_paged_workspace_bytes (allocated here if None)."""
+        import torch
+        self.torch = torch
+        self.cfg = cfg
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise MoeError(-1, f"the cache lives on a GPU, not on {self.device}")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        cb, sb = attn_paged_cache_bytes(cfg), attn_paged_workspace_bytes(cfg)
+        if not (cb and sb):
+            raise MoeError(-2, "invalid paged-cache config")
+
+        def buf(t, n, name):
+            if t is None:
+                return torch.empty(n, dtype=torch.uint8, device=self.device)
+            _tensor_ptr(t, name, n, (torch.uint8,), self.device)
+            return t
+        self.cache = buf(cache, cb, "cache")
+        self.workspace = buf(workspace, sb, "workspace")
+        self.tokens = 0      # of the batch set
+        self.ctx = attn_paged_init(cfg, self.cache.data_ptr(), self.workspace.data_ptr())
+
+    @property
+    def stream(self) -> int:
+        return self.torch.cuda.current_stream(self.device).cuda_stream
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            lib().attn_paged_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def views(self, layer):
+        """(K, V, K scales, V scales) of a layer: pages [n_pages, n_kv_heads, page_size, head_dim]
+        as bfloat16 or float8_e4m3fn, scales fp32 [n_pages, n_kv_heads] (None with bf16 pages)."""
+        c, torch = self.cfg, self.torch
+        if not 0 <= layer < c.n_layers:
+            raise MoeError(-1, "layer out of range")
+        e4m3 = bool(c.flags & ATTN_PAGED_E4M3)
+        shape = (c.n_pages, c.n_kv_heads, c.page_size, c.head_dim)
+        data = shape[0] * shape[1] * shape[2] * shape[3] * (1 if e4m3 else 2)
+        n = c.n_pages * c.n_kv_heads * 4
+        scales = (n + 255) // 256 * 256 if e4m3 else 0
+        at = layer * 2 * (data + scales)
+        dt = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+        k, v = (self.cache[at + i * data:at + (i + 1) * data].view(dt).view(shape) for i in (0, 1))
+        if not e4m3:
+            return k, v, None, None
+        at += 2 * data
+        ks, vs = (self.cache[at + i * scales:at + i * scales + n].view(torch.float32).view(shape[:2]) for i in (0, 1))
+        return k, v, ks, vs
+
+    def set_batch(self, n_new, pos0, table):
+        """attn_paged_set_batch: n_new and pos0 are sequences of ints, table [n_seqs, blocks]
+        (lists of equal length, or an integer tensor or array), all on the host."""
+        def host(a, name):
+            if isinstance(a, self.torch.Tensor):
+                if a.device.type != "cpu":
+                    raise MoeError(-1, f"{name} must be on the host")
+                a = a.numpy()
+            return _int32(a, name)
+        n, p, tb = host(n_new, "n_new"), host(pos0, "pos0"), host(table, "table")
+        if n.ndim != 1 or p.shape != n.shape:
+            raise MoeError(-1, "n_new and pos0 must be one-dimensional and equally long")
+        if n.size == 0:
+            tb = tb.reshape(0, 0)
+        if tb.ndim != 2 or tb.shape[0] != n.size:
+            raise MoeError(-1, "table must be [n_seqs, blocks]")
+        with self.torch.cuda.device(self.device):
+            attn_paged_set_batch(self.ctx, n.size, n.ctypes.data, p.ctypes.data, tb.ctypes.data, tb.shape[1], self.stream)
+        self.tokens = int(n.sum())
+
+    def append(self, layer, qkv, q):
+        """attn_paged_append: qkv [T, (n_heads + 2 n_kv_heads) head_dim] fp32 or bf16 (bfloat16 or
+        its bits), rows apart by any stride of whole 16 bytes; q (out) bf16 [T, n_heads head_dim]."""
+        c, torch, T = self.cfg, self.torch, self.tokens
+        nqkv = (c.n_heads + 2 * c.n_kv_heads) * c.head_dim
+        bf = _bf16_types(torch)
+        if qkv.dtype not in bf + (torch.float32,):
+            raise MoeError(-1, f"qkv has dtype {qkv.dtype}, expected float32 or bfloat16")
+        if qkv.device != self.device:
+            raise MoeError(-1, f"qkv is on {qkv.device}, expected {self.device}")
+        if qkv.dim() != 2 or qkv.shape[0] < T or qkv.shape[1] != nqkv:
+            raise MoeError(-2, f"qkv has shape {tuple(qkv.shape)}, the call uses [{T}, {nqkv}]")
+        if qkv.stride(1) != 1 and T:
+            raise MoeError(-1, "the rows of qkv must be contiguous")
+        ld = qkv.stride(0) if T > 1 else nqkv
+        with torch.cuda.device(self.device):
+            attn_paged_append(self.ctx, layer, qkv.data_ptr(), ld, QKV_F32 if qkv.dtype == torch.float32 else QKV_BF16,
+                              _tensor_ptr(q, "q", T * c.n_heads * c.head_dim, bf, self.device), self.stream)
+
+    def attend(self, layer, q, out):
+        """attn_paged_attend: out = attention of q (both bf16 [T, n_heads head_dim])."""
+        c, bf = self.cfg, _bf16_types(self.torch)
+        n = self.tokens * c.n_heads * c.head_dim
+        with self.torch.cuda.device(self.device):
+            attn_paged_attend(self.ctx, layer, _tensor_ptr(q, "q", n, bf, self.device),
+                              _tensor_ptr(out, "out", n, bf, self.device), self.stream)
+
+
+def _int32(a, name):
+    """A contiguous int32 numpy array of integers that fit."""
+    import numpy as np
+    a = np.asarray(a)
+    if a.size == 0:
+        return np.zeros(a.shape, np.int32)
+    if a.dtype.kind not in "iu":
+        raise MoeError(-1, f"{name} must hold integers")
+    if a.min() < -2 ** 31 or a.max() >= 2 ** 31:
+        raise MoeError(-1, f"{name} must fit in 32 bits")
+    return np.ascontiguousarray(a, dtype=np.int32)

@@ -37,7 +37,7 @@ def _compile(src):
 
 def build(force: bool = True) -> str:
     srcs = sources()
-    headers = glob.glob(os.path.join(CSRC, "*.h")) + [os.path.join(ROOT, "include", "moe.h")]
+    headers = glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(ROOT, "include", "*.h"))
     if not force and os.path.exists(LIB):
         newest = max(os.path.getmtime(p) for p in srcs + headers)
         if os.path.getmtime(LIB) >= newest:

@@ -162,7 +162,8 @@ struct GemvArgs {
     int K, N, T;
 };
 
-template <int kS>
+// kRes false: y32 alone.
+template <int kS, bool kRes = true>
 __global__ __launch_bounds__(64 * kSplit) void gemv_kernel(GemvArgs a)
 {
     __shared__ f32x4_t s_red[kS][kSplit * 64];
@@ -180,7 +181,8 @@ __global__ __launch_bounds__(64 * kSplit) void gemv_kernel(GemvArgs a)
     // token j; other lanes read token 0's)
     const int c = min(w, kS - 1);
     const int64_t o = (int64_t)(has_tok ? j : 0) * a.N + (q + c) * kTileRows + g * 4;
-    const uint2 r = *reinterpret_cast<const uint2*>(a.res + o);
+    uint2 r{};
+    if constexpr (kRes) r = *reinterpret_cast<const uint2*>(a.res + o);
     stream_batches<kS>(pw, slab, px, KT, w, has_tok, acc, [] {});
 #pragma unroll
     for (int i = 0; i < kS; ++i) s_red[i][w * 64 + lane] = acc[i];
@@ -190,6 +192,7 @@ __global__ __launch_bounds__(64 * kSplit) void gemv_kernel(GemvArgs a)
     for (int i = 1; i < kSplit; ++i) sum += s_red[c][i * 64 + lane];
     if (!has_tok) return;
     *reinterpret_cast<float4*>(a.y32 + o) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+    if constexpr (!kRes) return;
     const float r0 = __uint_as_float(r.x << 16), r1 = __uint_as_float(r.x & 0xFFFF0000u);
     const float r2 = __uint_as_float(r.y << 16), r3 = __uint_as_float(r.y & 0xFFFF0000u);
     const uint32_t lo = (uint32_t)moe::f32_to_bf16(r0 + sum[0]) |
@@ -1335,6 +1338,16 @@ hipError_t attn_launch_out(const void* w, const uint16_t* x, int T, int K, int N
     const dim3 block(64 * attn::kSplit);
     if (two_tiles(tiles, K, T)) hipLaunchKernelGGL(attn::gemv_kernel<2>, dim3(tiles / 2), block, 0, s, a);
     else hipLaunchKernelGGL(attn::gemv_kernel<1>, dim3(tiles), block, 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t attn_launch_product(const void* w, const uint16_t* x, int T, int K, int N, float* y32, hipStream_t s)
+{
+    attn::GemvArgs a{static_cast<const uint8_t*>(w), x, y32, nullptr, nullptr, K, N, T};
+    const int tiles = N / moe::kTileRows;
+    const dim3 block(64 * attn::kSplit);
+    if (two_tiles(tiles, K, T)) hipLaunchKernelGGL((attn::gemv_kernel<2, false>), dim3(tiles / 2), block, 0, s, a);
+    else hipLaunchKernelGGL((attn::gemv_kernel<1, false>), dim3(tiles), block, 0, s, a);
     return hipGetLastError();
 }
 

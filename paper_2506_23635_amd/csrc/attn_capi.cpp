@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "../../include/attn.h"
+#include "attn_paged.h"
 #include "moe_common.h"
 
 namespace {
@@ -344,6 +345,55 @@ moe_status forward_impl(attn_ctx* ctx, int32_t layer, const uint16_t* x, uint16_
     return MOE_OK;
 }
 
+// The block over a paged cache: the projection's sums stay fp32, in packed row
+// order, and append rotates, rounds and stores them; the output projection as
+// in forward_impl and prefill.
+moe_status paged_impl(attn_ctx* ctx, int32_t layer, attn_paged_ctx* cache, const uint16_t* x, uint16_t* y, int T,
+                      hipStream_t s)
+{
+    const attn_config& c = ctx->cfg;
+    const Layout& L = ctx->L;
+    uint8_t* w = layer_w(ctx, layer);
+    uint16_t* h = reinterpret_cast<uint16_t*>(ctx->ws + L.h_off);
+    float* qkv = reinterpret_cast<float*>(ctx->ws + L.qkv_off);
+    uint16_t* q = reinterpret_cast<uint16_t*>(ctx->ws + L.q_off);
+    uint16_t* a = reinterpret_cast<uint16_t*>(ctx->ws + L.a_off);
+    float* o = reinterpret_cast<float*>(ctx->ws + L.o_off);
+    const int d = c.d_model;
+    const bool few = T <= kDecodeTokens;
+    float* part = few ? nullptr : reinterpret_cast<float*>(ctx->ws + L.split_off);
+    const int sq = few ? 1 : moe_gemm_plain_split(T, L.nqkv), so = few ? 1 : moe_gemm_plain_split(T, d);
+    hipError_t e = timed(ctx, ATTN_K_NORM, s, [&] {
+        return attn_launch_norm(x, reinterpret_cast<const float*>(w), T, d, c.norm_eps, h, nullptr, nullptr, 0, 0, s);
+    });
+    if (e != hipSuccess) return hip_fail(ctx, e, "norm kernel launch");
+    float* sums = sq > 1 ? part : qkv;
+    e = timed(ctx, ATTN_K_QKV, s, [&] {
+        if (few) return attn_launch_product(w + L.wqkv_off, h, T, d, L.nqkv, sums, s);
+        moe::GemmArgs g = product(w + L.wqkv_off, h, d, L.nqkv, sums, T, sq);
+        return moe_launch_gemm_down(&g, s);
+    });
+    if (e != hipSuccess) return hip_fail(ctx, e, "projection launch");
+    const paged::Source src{sums, L.nqkv, (int64_t)T * L.nqkv, sq, 0, 1};
+    e = timed(ctx, ATTN_K_ROPE, s, [&] { return attn_paged_run_append(cache, layer, &src, q, s); });
+    if (e != hipSuccess) return hip_fail(ctx, e, "append kernel launch");
+    e = timed(ctx, ATTN_K_SCORE, s, [&] { return attn_paged_run_attend(cache, layer, q, a, s); });
+    if (e != hipSuccess) return hip_fail(ctx, e, "attention kernel launch");
+    e = timed(ctx, ATTN_K_OUT, s, [&] {
+        if (few) return attn_launch_out(w + L.wo_off, a, T, L.nq, d, o, x, y, s);
+        moe::GemmArgs g = product(w + L.wo_off, a, L.nq, d, so > 1 ? part : o, T, so);
+        g.res = x;
+        g.y16 = y;
+        return so > 1 ? moe_launch_gemm_down(&g, s) : moe_launch_gemm_out(&g, s);
+    });
+    if (e != hipSuccess) return hip_fail(ctx, e, "output projection launch");
+    if (so > 1) {
+        e = timed(ctx, ATTN_K_RESIDUAL, s, [&] { return attn_launch_residual(x, part, so, o, y, (int64_t)T * d, s); });
+        if (e != hipSuccess) return hip_fail(ctx, e, "residual kernel launch");
+    }
+    return MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -489,6 +539,36 @@ moe_status attn_forward_norm(attn_ctx* ctx, int32_t layer, const uint16_t* x, ui
     const float* gamma2 = reinterpret_cast<const float*>(layer_w(ctx, layer) + ctx->L.gamma2_off);
     const hipError_t e = timed(ctx, ATTN_K_POST_NORM, s, [&] {
         return attn_launch_norm(y, gamma2, T, ctx->cfg.d_model, ctx->cfg.norm_eps, z, nullptr, nullptr, 0, 0, s);
+    });
+    if (e != hipSuccess) return hip_fail(ctx, e, "post-attention norm launch");
+    return MOE_OK;
+}
+
+moe_status attn_forward_paged(attn_ctx* ctx, int32_t layer, attn_paged_ctx* cache, const uint16_t* x, uint16_t* y,
+                              uint16_t* z, moe_stream_t stream)
+{
+    if (!ctx) return MOE_E_ARG;
+    if (!cache) return fail(ctx, MOE_E_ARG, "cache is NULL");
+    const attn_config& c = ctx->cfg;
+    const attn_paged_config& p = *attn_paged_cfg(cache);
+    if (p.n_heads != c.n_heads || p.n_kv_heads != c.n_kv_heads || p.head_dim != c.head_dim ||
+        p.rope_theta != c.rope_theta)
+        return fail(ctx, MOE_E_SHAPE, "the cache's heads, head_dim or rope_theta are not the block's");
+    if (layer < 0 || layer >= c.n_layers || layer >= p.n_layers) return fail(ctx, MOE_E_ARG, "layer out of range");
+    if (!attn_paged_has_batch(cache)) return fail(ctx, MOE_E_STATE, "no batch set on the cache");
+    const int32_t T = attn_paged_tokens(cache);
+    if (T > c.max_tokens) return fail(ctx, MOE_E_CAPACITY, "the batch's tokens exceed max_tokens");
+    if (!ctx->loaded[layer]) return fail(ctx, MOE_E_STATE, "layer weights not loaded");
+    if (z && !ctx->post_loaded[layer]) return fail(ctx, MOE_E_STATE, "post-attention norm not loaded");
+    if (T == 0) return MOE_OK;
+    if (!x || !y) return fail(ctx, MOE_E_ARG, "x or y is NULL");
+    if (misaligned(x) || misaligned(y) || misaligned(z)) return fail(ctx, MOE_E_ALIGN, "x, y and z must be 16-byte aligned");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const moe_status st = paged_impl(ctx, layer, cache, x, y, T, s);
+    if (st != MOE_OK || !z) return st;
+    const float* gamma2 = reinterpret_cast<const float*>(layer_w(ctx, layer) + ctx->L.gamma2_off);
+    const hipError_t e = timed(ctx, ATTN_K_POST_NORM, s, [&] {
+        return attn_launch_norm(y, gamma2, T, c.d_model, c.norm_eps, z, nullptr, nullptr, 0, 0, s);
     });
     if (e != hipSuccess) return hip_fail(ctx, e, "post-attention norm launch");
     return MOE_OK;

@@ -1,0 +1,993 @@
+// attn_paged.hip -- kernels of the paged cache (include/attn.h): appending a
+// batch's keys and values with the rotation, and causal attention over pages.
+//
+//   unpack_kernel  a batch's arrays from pinned host memory to the workspace
+//   append_kernel  q rotated to bf16; bf16 pages: k rotated and v to their slots
+//   code_kernel    e4m3 pages: k rotated and v to their slots, the pages' scales
+//   few_kernel     attention of up to 16 query rows per key/value head
+//   tile_kernel    attention of blocks of 128 or 64 query rows
+//   merge_kernel   adds the partial sums of rows whose positions were shared out
+#include <cmath>
+
+#include "attn_paged.h"
+#include "moe_common.h"
+
+namespace paged {
+
+using moe::f32x4_t;
+using moe::u32x4_t;
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
+
+__device__ inline u32x4_t ld16(const void* p) { return *reinterpret_cast<const u32x4_t*>(p); }
+
+__device__ inline f32x16_t mfma32x32x16(const u32x4_t a, const u32x4_t b, f32x16_t c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(moe::bf16x8_t, a),
+                                                   __builtin_bit_cast(moe::bf16x8_t, b), c, 0, 0, 0);
+}
+
+// barrier for LDS traffic only: global loads stay in flight across it
+__device__ __forceinline__ void lds_barrier()
+{
+    constexpr int kWaitLgkm = 0xC07F;   // lgkmcnt 0; vmcnt and expcnt at their maxima
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kWaitLgkm);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// ------------------------------------------------------------------ batch --
+
+__global__ __launch_bounds__(256) void unpack_kernel(Unpack u)
+{
+    for (int s = 0; s < kSegments; ++s) {
+        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(u.src + u.seg[s].src);
+        u32x4_t* dst = reinterpret_cast<u32x4_t*>(u.dst + u.seg[s].dst);
+        const uint64_t n = u.seg[s].bytes / 16;
+        for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) dst[i] = src[i];
+    }
+}
+
+// ----------------------------------------------------------------- append --
+
+// cos and sin of pos * inv_freq, the angle formed and reduced modulo 2 pi in
+// fp64 (2 pi in two parts, Cody and Waite): sincosf sees [-pi, pi] only
+__device__ inline float2 rotation(int pos, double inv_freq)
+{
+    constexpr double kTwoPiHi = 6.28318530717958623200e+00;   // 2 pi rounded to fp64
+    constexpr double kTwoPiLo = 2.44929359829470635445e-16;   // 2 pi - kTwoPiHi
+    constexpr double kInvTwoPi = 1.59154943091895335769e-01;
+    const double ang = (double)pos * inv_freq;
+    const double k = rint(ang * kInvTwoPi);
+    const double r = fma(-k, kTwoPiLo, fma(-k, kTwoPiHi, ang));
+    float c, s;
+    sincosf((float)r, &s, &c);
+    return make_float2(c, s);
+}
+
+// Four consecutive features f .. f + 3 (f a multiple of 4) of head `head` of
+// token t.  Packed rows hold a query or key head's features f and f + hd/2
+// eight apart in tiles of 16 (moe::rope_row).
+template <bool kPacked>
+__device__ inline float4 load4(const Source& x, int t, int head, int f, int hd, int n_rotated)
+{
+    if constexpr (kPacked) {
+        const int n = head * hd + f;
+        const float* src = static_cast<const float*>(x.x) + t * x.ld + (head < n_rotated ? moe::rope_row(n, hd) : n);
+        float4 v = *reinterpret_cast<const float4*>(src);
+        for (int k = 1; k < x.n_split; ++k) {
+            const float4 p = *reinterpret_cast<const float4*>(src + k * x.stride);
+            v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+        }
+        return v;
+    } else {
+        const int64_t i = t * x.ld + head * hd + f;
+        if (!x.bf16) return *reinterpret_cast<const float4*>(static_cast<const float*>(x.x) + i);
+        const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(x.x) + i);
+        return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u),
+                           __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u));
+    }
+}
+
+__device__ inline uint2 pack_bf16x4(const float* v)
+{
+    return make_uint2(moe::cvt_pk_bf16(v[0], v[1]), moe::cvt_pk_bf16(v[2], v[3]));
+}
+
+// Eight values of one head: a piece of four rotation pairs (lo: features f ..
+// f + 3, hi: their partners), or of a value head eight features f .. f + 7.
+struct Piece {
+    float lo[4], hi[4];
+};
+
+template <bool kPacked>
+__device__ inline Piece load_piece(const Source& x, int t, int head, int f, int hd, int n_rotated, bool turn)
+{
+    const float4 a = load4<kPacked>(x, t, head, f, hd, n_rotated);
+    const float4 b = load4<kPacked>(x, t, head, turn ? f + hd / 2 : f + 4, hd, n_rotated);
+    return Piece{{a.x, a.y, a.z, a.w}, {b.x, b.y, b.z, b.w}};
+}
+
+__device__ inline void turn_pair(float& a, float& b, float2 cs)
+{
+    const float x = a, y = b;
+    a = x * cs.x - y * cs.y;
+    b = y * cs.x + x * cs.y;
+}
+
+// q of every token (and with bf16 pages k and v): blockIdx.x is the token,
+// blockIdx.y a run of 256 pieces of it.  The token's rotations, one per
+// frequency, are formed once per workgroup.
+template <bool kPacked>
+__global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t* __restrict__ q)
+{
+    __shared__ float2 s_cs[64];
+    const int t = blockIdx.x;
+    const Token tok = a.tok[t];
+    const int hd = a.hd, half = hd / 2, P = hd / 8;      // pieces per head
+    if ((int)threadIdx.x < half) s_cs[threadIdx.x] = rotation(tok.pos, a.freq[threadIdx.x]);
+    const int e = blockIdx.y * 256 + threadIdx.x;
+    const int head = e / P, n_rotated = a.H + a.G;
+    const bool live = head < (a.e4m3 ? a.H : a.H + 2 * a.G);
+    const bool turn = head < n_rotated;
+    const int f = turn ? e % P * 4 : e % P * 8;
+    Piece v{};
+    if (live) v = load_piece<kPacked>(x, t, head, f, hd, n_rotated, turn);
+    __syncthreads();
+    if (!live) return;
+    if (turn) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) turn_pair(v.lo[i], v.hi[i], s_cs[f + i]);
+    }
+    uint16_t* dst;
+    if (head < a.H) {
+        dst = q + ((int64_t)t * a.H + head) * hd;
+    } else {
+        const int g = turn ? head - a.H : head - n_rotated;
+        const int64_t row = ((int64_t)tok.page * a.G + g) << a.shift | (tok.pos & ((1 << a.shift) - 1));
+        dst = reinterpret_cast<uint16_t*>(turn ? a.k : a.v) + row * hd;
+    }
+    *reinterpret_cast<uint2*>(dst + f) = pack_bf16x4(v.lo);
+    *reinterpret_cast<uint2*>(dst + f + (turn ? half : 4)) = pack_bf16x4(v.hi);
+}
+
+// The least exponent e >= kExpMin with amax <= 448 * 2^e = 1.75 * 2^(e + 8),
+// from the bits of a finite amax >= 0: the carry of the addition is 1 where
+// the mantissa is past 1.75.
+__device__ inline int scale_exponent(float amax)
+{
+    const int e = (int)((__float_as_uint(amax) + (0x7FFFFFu - 0x600000u)) >> 23) - 127 - 8;
+    return max(e, kExpMin);
+}
+
+__device__ inline float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+__device__ inline bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
+
+// four values times 2^-e as e4m3 codes; what is not finite becomes NaN
+__device__ inline uint32_t code4(const float* v, float inv)
+{
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = finite(v[i]) ? v[i] * inv : NAN;
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(w[0], w[1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(w[2], w[3], c, true);
+    return (uint32_t)c;
+}
+
+// codes rounded again for a scale that grew: value * ratio, ratio a power of two
+__device__ inline uint32_t recode4(uint32_t c, float ratio)
+{
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false);
+    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(lo[0] * ratio, lo[1] * ratio, 0, false);
+    r = __builtin_amdgcn_cvt_pk_fp8_f32(hi[0] * ratio, hi[1] * ratio, r, true);
+    return (uint32_t)r;
+}
+
+// e4m3 pages: one workgroup per page with new tokens, key/value head and K or
+// V, so that the page's scale has one writer and needs no atomics.  The new
+// values' maximum gives the scale; up to kHold passes of tokens stay in
+// registers between the two uses, more are read and rotated again.
+constexpr int kHold = 4;
+
+template <bool kPacked>
+__global__ __launch_bounds__(256) void code_kernel(Args a, Source x)
+{
+    __shared__ float s_max[4];
+    const int G = a.G, hd = a.hd, P = hd / 8;
+    const int per_pass = 256 / P;
+    const int tj = threadIdx.x / P, pc = threadIdx.x % P;
+    const int n_tasks = a.hdr->n_pages * G * 2;
+    for (int task = blockIdx.x; task < n_tasks; task += gridDim.x) {
+        const PageWork w = a.pages[task / (2 * G)];
+        const int g = task / 2 % G;
+        const bool turn = task % 2 == 0;
+        const int head = a.H + g + (turn ? 0 : G), f = pc * (turn ? 4 : 8);
+        const int64_t pg = (int64_t)w.page * G + g;
+        uint8_t* base = (turn ? a.k : a.v) + (pg << a.shift) * hd;
+        float* scale = (turn ? a.k_scale : a.v_scale) + pg;
+        int e_old = kExpMin;
+        if (w.slot0 > 0) e_old = min(max((int)(__float_as_uint(*scale) >> 23 & 255u) - 127, kExpMin), kExpMax);
+        Piece v[kHold];
+        auto load = [&](int j0) {
+#pragma unroll
+            for (int u = 0; u < kHold; ++u) {
+                const int j = j0 + u * per_pass + tj;
+                if (j >= w.n) {
+                    v[u] = Piece{};
+                    continue;
+                }
+                v[u] = load_piece<kPacked>(x, w.tok0 + j, head, f, hd, a.H + G, turn);
+                if (turn) {
+                    const int pos = a.tok[w.tok0 + j].pos;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) turn_pair(v[u].lo[i], v[u].hi[i], rotation(pos, a.freq[f + i]));
+                }
+            }
+        };
+        const int chunk = kHold * per_pass;
+        float amax = 0.f;
+        for (int j0 = 0; j0 < w.n; j0 += chunk) {
+            load(j0);
+#pragma unroll
+            for (int u = 0; u < kHold; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (finite(v[u].lo[i])) amax = fmaxf(amax, fabsf(v[u].lo[i]));
+                    if (finite(v[u].hi[i])) amax = fmaxf(amax, fabsf(v[u].hi[i]));
+                }
+        }
+        for (int off = 32; off >= 1; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
+        if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = amax;
+        __syncthreads();
+        amax = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+        const int e = max(e_old, scale_exponent(amax));
+        if (threadIdx.x == 0) *scale = exp2i(e);
+        if (w.slot0 > 0 && e > e_old) {
+            const float ratio = exp2i(max(e_old - e, -126));
+            for (int i = threadIdx.x; i < w.slot0 * hd / 16; i += 256) {
+                u32x4_t c = ld16(base + i * 16);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[k] = recode4(c[k], ratio);
+                *reinterpret_cast<u32x4_t*>(base + i * 16) = c;
+            }
+        }
+        const float inv = exp2i(-e);
+        for (int j0 = 0; j0 < w.n; j0 += chunk) {
+            if (w.n > chunk) load(j0);
+#pragma unroll
+            for (int u = 0; u < kHold; ++u) {
+                const int j = j0 + u * per_pass + tj;
+                if (j >= w.n) continue;
+                uint8_t* dst = base + (w.slot0 + j) * hd + f;
+                *reinterpret_cast<uint32_t*>(dst) = code4(v[u].lo, inv);
+                *reinterpret_cast<uint32_t*>(dst + (turn ? hd / 2 : 4)) = code4(v[u].hi, inv);
+            }
+        }
+        __syncthreads();                                 // s_max is written again
+    }
+}
+
+// ----------------------------------------------------------------- attend --
+
+// A maximum in base 2, with the product's one rounding everywhere: p, the
+// rescaling and the merges then refer to the same value.
+__device__ inline float base2(float m, float scale2)
+{
+#pragma clang fp contract(off)
+    return m * scale2;
+}
+
+// eight e4m3 codes as eight bf16 of code * scale (exact: a power of two)
+__device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
+{
+    return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, true)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, false)),
+                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
+}
+
+// of two bf16: bits all ones in the halves that are not finite
+__device__ inline uint32_t bad_halves(uint32_t w)
+{
+    return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+
+constexpr uint32_t kOnes = 0x3F803F80u;      // two bf16 ones
+
+// few_kernel: up to 16 query rows (tokens of a sequence times the heads of
+// one key/value head) over one range of positions, 4 waves taking the range's
+// 32-position steps in turn, each with a maximum and sums of its own, merged
+// through LDS at the end.
+//
+// Everything stays in registers.  Scores transposed, S^T = K Q^T, with
+// v_mfma_f32_16x16x32_bf16: lane (r, g) = (lane % 16, lane / 16) supplies K of
+// position r and Q of row r, and ends with the scores of row r at positions
+// 16 s + 4 g + i of sub-block s.  O^T += V^T P^T takes them as they are: its B
+// operand wants eight positions per lane, in any order that V follows, and
+// gets {4 g + i, 16 + 4 g + i}; the lane loads V of those eight positions at
+// dims D r .. D r + D - 1 (D = hd / 16, whole rows per 16 lanes) and output
+// block i takes dim D r + i for row r: an 8 x D transposition inside the lane.
+// P enters as two bf16 terms (the second the rounding of what the first left:
+// 16 bits), since the matrix cores have time: the loads bound the kernel.
+template <int HD, bool kE4m3>
+__global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __restrict__ q,
+                                                     uint16_t* __restrict__ out, float scale2)
+{
+    constexpr int NC = HD / 32;              // MFMA K steps of the scores
+    constexpr int D = HD / 16;               // dims per lane of V
+    constexpr int ES = kE4m3 ? 1 : 2;
+    constexpr int KW = kE4m3 ? HD / 64 : NC; // 16-byte loads per K row and lane
+    constexpr int VW = D * ES / 4;           // words per V row and lane
+    constexpr int ROW = HD + 4;
+    __shared__ __attribute__((aligned(16))) float s_o[4][kFewRows][ROW];
+    __shared__ float s_m[4][kFewRows], s_l[4][kFewRows];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int group = a.H / a.G, P = 1 << a.shift;
+    const int n_items = a.hdr->n_few;
+    for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+        const Item im = a.few[it];
+        const int32_t* table = a.table + im.table;
+        const int R = im.rows, kvh = im.kvh, n_pos = im.n_pos;
+        const bool row_ok = r < R;
+        const int t = (row_ok ? r : 0) / group, j = kvh * group + (row_ok ? r : 0) % group;
+        const int lim = row_ok ? im.pos0 + t : n_pos;    // the row's last position
+        u32x4_t qf[NC];
+        {
+            const uint16_t* qr = q + ((int64_t)(im.tok0 + t) * a.H + j) * HD;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                const int d = kE4m3 ? c / 2 * 64 + g * 16 + c % 2 * 8 : c * 32 + g * 8;
+                const u32x4_t v = ld16(qr + d);
+                qf[c] = row_ok ? v : u32x4_t{0u, 0u, 0u, 0u};
+            }
+        }
+        f32x4_t o[D];
+#pragma unroll
+        for (int i = 0; i < D; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        float m = -INFINITY, l = 0.f;
+        // One set of registers for the loads: the next step's K is loaded into
+        // them as soon as the scores are formed, its V once V is transposed.
+        u32x4_t kr[2][KW];
+        uint32_t vr[8][VW];
+        float ksc[2], vsc[2];
+        // pages of the step at p0; a sub-block past the sequence's end reads
+        // the end's page
+        auto pages = [&](int p0, int (&pg)[2]) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) pg[s] = table[min(p0 + 16 * s, n_pos - 1) >> a.shift];
+        };
+        // rows past the sequence's last position read that position (masked
+        // for every row); a sub-block without a page reads page 0 and is
+        // cleared before use
+        auto fetch_k = [&](int p0, const int (&pg)[2]) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int pb = min(p0 + 16 * s, (n_pos - 1) & ~15);
+                const int64_t head = (int64_t)max(pg[s], 0) * a.G + kvh;
+                const int64_t row = (head << a.shift) + (pb & (P - 1)) + min(r, n_pos - 1 - pb);
+                const uint8_t* kb = a.k + row * (HD * ES) + g * 16;
+#pragma unroll
+                for (int c = 0; c < KW; ++c) kr[s][c] = ld16(kb + c * 64);
+                if constexpr (kE4m3) ksc[s] = a.k_scale[head];
+            }
+        };
+        auto fetch_v = [&](int p0, const int (&pg)[2]) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int pb = min(p0 + 16 * s, (n_pos - 1) & ~15);
+                const int64_t head = (int64_t)max(pg[s], 0) * a.G + kvh;
+                const uint8_t* vb = a.v + ((head << a.shift) + (pb & (P - 1))) * (HD * ES) + r * (D * ES);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint8_t* src = vb + min(4 * g + i, n_pos - 1 - pb) * (HD * ES);
+                    uint32_t* dst = vr[s * 4 + i];
+                    if constexpr (VW == 4) {
+                        const u32x4_t u = ld16(src);
+                        dst[0] = u[0]; dst[1] = u[1]; dst[2] = u[2]; dst[3] = u[3];
+                    } else if constexpr (VW == 2) {
+                        const uint2 u = *reinterpret_cast<const uint2*>(src);
+                        dst[0] = u.x; dst[1] = u.y;
+                    } else {
+                        dst[0] = *reinterpret_cast<const uint32_t*>(src);
+                    }
+                }
+                if constexpr (kE4m3) vsc[s] = a.v_scale[head];
+            }
+        };
+        // two dims of the lane's position i, as bf16
+        auto dims = [&](int i, int k) -> uint32_t {
+            if constexpr (kE4m3) {
+                const uint32_t c = vr[i][k / 2];
+                return __builtin_bit_cast(uint32_t, k % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, vsc[i / 4], true)
+                                                          : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, vsc[i / 4], false));
+            } else {
+                return vr[i][k];
+            }
+        };
+        constexpr int step = 4 * kTile;
+        int p0 = im.begin + w * kTile;
+        int pg[2], pn[2];
+        if (p0 < im.end) {
+            pages(p0, pg);
+            fetch_k(p0, pg);
+            fetch_v(p0, pg);
+            pages(p0 + step, pn);
+        }
+        for (; p0 < im.end; p0 += step) {
+            const bool more = p0 + step < im.end;
+            f32x4_t sc[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                sc[s] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    u32x4_t kf;
+                    if constexpr (kE4m3) kf = decode8(kr[s][c / 2][c % 2 * 2], kr[s][c / 2][c % 2 * 2 + 1], ksc[s]);
+                    else kf = kr[s][c];
+                    sc[s] = moe::mfma16x16x32(kf, qf[c], sc[s]);
+                }
+            }
+            if (more) fetch_k(p0 + step, pn);
+            const bool masked = p0 + kTile - 1 > im.pos0 || pg[0] < 0 || pg[1] < 0;
+            if (masked) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (pg[s] < 0 || p0 + 16 * s + 4 * g + i > lim) sc[s][i] = -INFINITY;
+            }
+            float mx = m;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[s][i]);
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
+            if (__ballot(mx != m)) {
+                const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
+                l *= alpha;
+#pragma unroll
+                for (int i = 0; i < D; ++i) o[i] *= alpha;
+                m = mx;
+            }
+            u32x4_t p1, p2;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const float pa = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i], scale2, -ms));
+                    const float pb = __builtin_amdgcn_exp2f(fmaf(sc[s][2 * i + 1], scale2, -ms));
+                    l += pa + pb;
+                    const uint32_t hw = moe::cvt_pk_bf16(pa, pb);
+                    p1[2 * s + i] = hw;
+                    p2[2 * s + i] = moe::cvt_pk_bf16(pa - __uint_as_float(hw << 16), pb - __uint_as_float(hw & 0xFFFF0000u));
+                }
+            // dim D r + i of the lane's eight positions
+            u32x4_t vt[D];
+#pragma unroll
+            for (int k = 0; k < D / 2; ++k)
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const uint32_t lo = dims(2 * n, k), hi = dims(2 * n + 1, k);
+                    vt[2 * k][n] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+                    vt[2 * k + 1][n] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+                }
+            if (more) fetch_v(p0 + step, pn);
+            if (masked) {
+                // values without a page are zeros; and a value that is not
+                // finite among positions that some rows do not see is taken
+                // out, since 0 times it would still reach those, while the
+                // rows that see it (counted by a product of zeros and ones)
+                // get a NaN
+                uint32_t bad = 0u;
+#pragma unroll
+                for (int i = 0; i < D; ++i)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        if (pg[n / 2] < 0) vt[i][n] = 0u;
+                        bad |= bad_halves(vt[i][n]);
+                    }
+                if (__ballot(bad != 0u)) {
+                    u32x4_t seen;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            seen[2 * s + i] = (sc[s][2 * i] == -INFINITY ? 0u : kOnes & 0xFFFFu) |
+                                              (sc[s][2 * i + 1] == -INFINITY ? 0u : kOnes & 0xFFFF0000u);
+#pragma unroll
+                    for (int i = 0; i < D; ++i) {
+                        u32x4_t ind;
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            const uint32_t x = bad_halves(vt[i][n]);
+                            ind[n] = x & kOnes;
+                            vt[i][n] &= ~x;
+                        }
+                        const f32x4_t count = moe::mfma16x16x32(ind, seen, f32x4_t{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (count[e] > 0.f) o[i][e] = NAN;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] = moe::mfma16x16x32(vt[i], p1, o[i]);
+#pragma unroll
+            for (int i = 0; i < D; ++i) o[i] = moe::mfma16x16x32(vt[i], p2, o[i]);
+            pg[0] = pn[0];
+            pg[1] = pn[1];
+            if (more) pages(p0 + 2 * step, pn);
+        }
+        l += __shfl_xor(l, 16, 64);
+        l += __shfl_xor(l, 32, 64);
+        if (row_ok) {
+            if (g == 0) {
+                s_m[w][r] = m;
+                s_l[w][r] = l;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < D; i += 4)
+                    *reinterpret_cast<float4*>(&s_o[w][r][D * (4 * g + e) + i]) =
+                        make_float4(o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]);
+        }
+        __syncthreads();
+        // the waves' sums in wave order: thread (row, eight or four dims)
+        const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * D;
+        if (row < R) {
+            float M = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
+            const float Ms = M == -INFINITY ? 0.f : base2(M, scale2);
+            float L = 0.f, v[D];
+#pragma unroll
+            for (int i = 0; i < D; ++i) v[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float mk = s_m[k][row];
+                const float f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(mk, scale2) - Ms);
+                if (mk == -INFINITY) continue;
+                L = fmaf(s_l[k][row], f, L);
+#pragma unroll
+                for (int i = 0; i < D; ++i) v[i] = fmaf(s_o[k][row][d0 + i], f, v[i]);
+            }
+            if (im.slot >= 0) {
+                float* dst = a.few_part + ((int64_t)im.slot * kFewRows + row) * (HD + kPartPad);
+#pragma unroll
+                for (int i = 0; i < D; i += 4)
+                    *reinterpret_cast<float4*>(dst + d0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                if (d0 == 0) {
+                    dst[HD] = M == -INFINITY ? -INFINITY : Ms;
+                    dst[HD + 1] = L;
+                }
+            } else {
+                const int tt = row / group, jj = kvh * group + row % group;
+                uint16_t* dst = out + ((int64_t)(im.tok0 + tt) * a.H + jj) * HD + d0;
+                const float inv = M == -INFINITY ? 0.f : 1.0f / L;
+#pragma unroll
+                for (int i = 0; i < D; ++i) v[i] *= inv;
+#pragma unroll
+                for (int i = 0; i < D; i += 4) *reinterpret_cast<uint2*>(dst + i) = pack_bf16x4(v + i);
+            }
+        }
+        __syncthreads();                                 // the LDS sums are written again
+    }
+}
+
+// tile_kernel: blocks of 128 or 64 query rows (kPG = 1 or 2 position groups:
+// the 4 / kPG waves of a group own 32 rows each) over one range of positions
+// in steps of 64, K rows and V transposed staged in LDS as bf16 (e4m3 codes
+// are decoded on the way).  v_mfma_f32_32x32x16_bf16: S^T = K Q^T leaves lane
+// (c, h) = (lane % 32, lane / 32) the scores of row c at positions 8 i + 4 h +
+// e of a 32-position block, which O^T += V^T P^T takes from the registers, V^T
+// being read in the same order.  P enters rounded to one bf16 (relative error
+// 2^-8 at most per weight, random in sign; the output's own rounding is as
+// large): a second term would cost half as many matrix instructions again.
+constexpr int tile_rows(int pg) { return 128 / pg; }
+
+template <int HD, bool kE4m3, int kPG>
+__global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __restrict__ items, int which,
+                                                      const uint16_t* __restrict__ q,
+                                                      uint16_t* __restrict__ out, float scale2)
+{
+    constexpr int KQ = HD / 16;              // 16-dim K steps of the score MFMAs
+    constexpr int DB = HD / 32;              // 32-dim blocks of the output
+    constexpr int kP = kStep;
+    constexpr int NB = kP / 32 / kPG;        // 32-position blocks per wave and step
+    constexpr int kRowWaves = 4 / kPG;       // waves on different rows
+    constexpr int KROW = HD + 8;             // padded K row in LDS (bf16)
+    constexpr int VROW = kP + 4;             // padded V^T row in LDS (bf16)
+    constexpr int ES = kE4m3 ? 1 : 2;
+    constexpr int kQBytes = tile_rows(kPG) * KROW * 2;
+    constexpr int kStageBytes = kP * KROW * 2 + HD * VROW * 2 + kQBytes;
+    constexpr int kMergeBytes = (4 - kRowWaves) * (DB * 16 + 2) * 64 * 4;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kStageBytes > kMergeBytes ? kStageBytes : kMergeBytes];
+    __shared__ uint32_t s_bad[2];
+    uint16_t* ks = reinterpret_cast<uint16_t*>(lds);
+    uint32_t* vt32 = reinterpret_cast<uint32_t*>(lds + kP * KROW * 2);
+    uint16_t* qs = reinterpret_cast<uint16_t*>(lds + kP * KROW * 2 + HD * VROW * 2);
+    const int group = a.H / a.G, P = 1 << a.shift;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 31, h = lane >> 5;
+    const int pg = w / kRowWaves;                        // the wave's position group
+    const int n_items = a.hdr->n_tile[which];
+    const u32x4_t zero = {0u, 0u, 0u, 0u};
+    for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+        const Item im = items[it];
+        const int32_t* table = a.table + im.table;
+        const int kvh = im.kvh, n_pos = im.n_pos, R = im.rows;
+        const int row_w0 = w % kRowWaves * 32;           // the wave's first row in the block
+        const int row = row_w0 + c;
+        const bool wave_ok = row_w0 < R, row_ok = row < R;
+        const int gr = im.row0 + (row_ok ? row : 0);     // the lane's row of the sequence
+        const int t = gr / group, j = kvh * group + gr % group;
+        const int lim = im.pos0 + t;
+        const int lim_w0 = im.pos0 + (im.row0 + row_w0) / group;
+        const int lim_b0 = im.pos0 + im.row0 / group;    // last position of the block's first row
+        __syncthreads();                                 // the last item's LDS reads are done
+        const uint16_t* qw = qs + row * KROW + h * 8;
+        if (pg == 0) {
+            const uint16_t* qrow = q + ((int64_t)(im.tok0 + t) * a.H + j) * HD + h * 8;
+#pragma unroll
+            for (int k = 0; k < KQ; ++k) {
+                const u32x4_t v = ld16(qrow + k * 16);
+                *reinterpret_cast<u32x4_t*>(const_cast<uint16_t*>(qw) + k * 16) = row_ok ? v : zero;
+            }
+        }
+        if (threadIdx.x < 2) s_bad[threadIdx.x] = 0u;
+        f32x16_t o[DB];
+#pragma unroll
+        for (int b = 0; b < DB; ++b) o[b] = f32x16_t{};
+        float m = -INFINITY, l = 0.f;
+        constexpr int KL = kP * (HD / 8) / 256;          // K pieces of 8 dims per thread
+        constexpr int VL = (kP / 2) * (HD / 8) / 256;    // pairs of V pieces per thread
+        constexpr int RW = 2 * ES;                       // words of a piece
+        uint32_t kr[KL][RW], va[VL][RW], vb[VL][RW];
+        float kscale[KL], vscale;
+        int kpage[KL], vpage;                            // of the pieces fetched next
+        int kpage_now[KL], vpage_now;                    // of the pieces in registers
+        // rows past the sequence's end are the last row (masked for all)
+        const int kp0 = threadIdx.x / (HD / 8), k8k = threadIdx.x % (HD / 8);
+        const int vp0 = threadIdx.x % (kP / 2) * 2;
+        auto pages = [&](int p0) {
+#pragma unroll
+            for (int i = 0; i < KL; ++i) kpage[i] = table[min(p0 + kp0 + i * (2048 / HD), n_pos - 1) >> a.shift];
+            vpage = table[min(p0 + vp0, n_pos - 1) >> a.shift];
+        };
+        auto ld_piece = [&](const uint8_t* src, uint32_t (&dst)[RW]) {
+            if constexpr (kE4m3) {
+                const uint2 v = *reinterpret_cast<const uint2*>(src);
+                dst[0] = v.x; dst[1] = v.y;
+            } else {
+                const u32x4_t v = ld16(src);
+                dst[0] = v[0]; dst[1] = v[1]; dst[2] = v[2]; dst[3] = v[3];
+            }
+        };
+        auto fetch = [&](int p0) {
+#pragma unroll
+            for (int i = 0; i < KL; ++i) {
+                const int p = min(p0 + kp0 + i * (2048 / HD), n_pos - 1);
+                const int64_t head = (int64_t)max(kpage[i], 0) * a.G + kvh;
+                ld_piece(a.k + ((head << a.shift) + (p & (P - 1))) * (HD * ES) + k8k * 8 * ES, kr[i]);
+                if constexpr (kE4m3) kscale[i] = a.k_scale[head];
+                kpage_now[i] = kpage[i];
+            }
+            const int64_t head = (int64_t)max(vpage, 0) * a.G + kvh;
+            const int pa = min(p0 + vp0, n_pos - 1), pb = min(p0 + vp0 + 1, n_pos - 1);
+            if constexpr (kE4m3) vscale = a.v_scale[head];
+            vpage_now = vpage;
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const int k8 = threadIdx.x / (kP / 2) + i * (512 / kP);
+                // an even position and the next one share a page of 16 or more
+                ld_piece(a.v + ((head << a.shift) + (pa & (P - 1))) * (HD * ES) + k8 * 8 * ES, va[i]);
+                ld_piece(a.v + ((head << a.shift) + (pb & (P - 1))) * (HD * ES) + k8 * 8 * ES, vb[i]);
+            }
+        };
+        auto piece = [&](const uint32_t (&src)[RW], float scale, bool mapped) {
+            u32x4_t v;
+            if constexpr (kE4m3) v = decode8(src[0], src[1], scale);
+            else v = u32x4_t{src[0], src[1], src[2], src[3]};
+            return mapped ? v : zero;
+        };
+        const int first = im.begin, end = im.end;
+        if (first < end) {
+            pages(first);
+            fetch(first);
+            pages(first + kP);
+        }
+        for (int p0 = first; p0 < end; p0 += kP) {
+            const bool block_masked = p0 + kP - 1 > lim_b0;
+            lds_barrier();                               // the last step's LDS reads are done
+            const int parity = (p0 - first) / kP & 1;
+#pragma unroll
+            for (int i = 0; i < KL; ++i)
+                *reinterpret_cast<u32x4_t*>(&ks[(kp0 + i * (2048 / HD)) * KROW + k8k * 8]) =
+                    piece(kr[i], kE4m3 ? kscale[i] : 0.f, kpage_now[i] >= 0);
+            uint32_t bad = 0u;
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const int pp = threadIdx.x % (kP / 2), k8 = threadIdx.x / (kP / 2) + i * (512 / kP);
+                const u32x4_t xa = piece(va[i], kE4m3 ? vscale : 0.f, vpage_now >= 0);
+                const u32x4_t xb = piece(vb[i], kE4m3 ? vscale : 0.f, vpage_now >= 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    vt32[((k8 * 8 + 2 * e) * VROW) / 2 + pp] = __builtin_amdgcn_perm(xb[e], xa[e], 0x05040100u);
+                    vt32[((k8 * 8 + 2 * e + 1) * VROW) / 2 + pp] = __builtin_amdgcn_perm(xb[e], xa[e], 0x07060302u);
+                    if (block_masked) bad |= bad_halves(xa[e]) | bad_halves(xb[e]);
+                }
+            }
+            if (block_masked && bad) s_bad[parity] = 1u;
+            if (threadIdx.x == 0) s_bad[parity ^ 1] = 0u;
+            uint32_t holes = 0u;                         // runs of 16 positions without a page
+            if (im.holes) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (table[min(p0 + 16 * i, n_pos - 1) >> a.shift] < 0) holes |= 1u << i;
+            }
+            if (p0 + kP < end) {
+                fetch(p0 + kP);
+                pages(p0 + 2 * kP);
+            }
+            lds_barrier();
+            const bool any_bad = s_bad[parity] != 0u;
+            if (!wave_ok) continue;
+            f32x16_t sc[NB];
+#pragma unroll
+            for (int pb = 0; pb < NB; ++pb) sc[pb] = f32x16_t{};
+#pragma unroll
+            for (int k = 0; k < KQ; ++k) {
+                const u32x4_t qf = *reinterpret_cast<const u32x4_t*>(qw + k * 16);
+#pragma unroll
+                for (int pb = 0; pb < NB; ++pb) {
+                    const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(
+                        &ks[((pg * NB + pb) * 32 + c) * KROW + k * 16 + h * 8]);
+                    sc[pb] = mfma32x32x16(kf, qf, sc[pb]);
+                }
+            }
+            const int pw0 = p0 + pg * NB * 32;           // the wave's first position
+            float mx = m;
+            const bool masked = pw0 + NB * 32 - 1 > lim_w0 || holes;
+            if (masked) {
+#pragma unroll
+                for (int pb = 0; pb < NB; ++pb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at = pb * 32 + 8 * (i / 4) + 4 * h + (i % 4);
+                        if (pw0 + at > lim || (holes >> ((pg * NB * 32 + at) / 16) & 1u)) sc[pb][i] = -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int pb = 0; pb < NB; ++pb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[pb][i]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
+            if (__ballot(mx != m)) {
+                const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
+                l *= alpha;
+#pragma unroll
+                for (int b = 0; b < DB; ++b) o[b] *= alpha;
+                m = mx;
+            }
+#pragma unroll
+            for (int pb = 0; pb < NB; ++pb)
+#pragma unroll
+                for (int sx = 0; sx < 2; ++sx) {
+                    u32x4_t bt, seen;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float s0 = sc[pb][sx * 8 + 2 * i], s1 = sc[pb][sx * 8 + 2 * i + 1];
+                        const float pa = __builtin_amdgcn_exp2f(fmaf(s0, scale2, -ms));
+                        const float pb2 = __builtin_amdgcn_exp2f(fmaf(s1, scale2, -ms));
+                        l += pa + pb2;
+                        bt[i] = moe::cvt_pk_bf16(pa, pb2);
+                        seen[i] = (s0 == -INFINITY ? 0u : kOnes & 0xFFFFu) | (s1 == -INFINITY ? 0u : kOnes & 0xFFFF0000u);
+                    }
+                    u32x4_t av[DB];
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) {
+                        const uint32_t* vr = vt32 + ((b * 32 + c) * VROW + (pg * NB + pb) * 32 + sx * 16 + 4 * h) / 2;
+                        const uint2 v0 = *reinterpret_cast<const uint2*>(vr);
+                        const uint2 v1 = *reinterpret_cast<const uint2*>(vr + 4);
+                        av[b] = u32x4_t{v0.x, v0.y, v1.x, v1.y};
+                    }
+                    if (any_bad) {
+                        // as in few_kernel: values that are not finite are
+                        // taken out, and rows that see them get a NaN
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) {
+                            u32x4_t ind;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t x = bad_halves(av[b][i]);
+                                ind[i] = x & kOnes;
+                                av[b][i] &= ~x;
+                            }
+                            const f32x16_t n = mfma32x32x16(ind, seen, f32x16_t{});
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (n[e] > 0.f) o[b][e] = NAN;
+                        }
+                    }
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) o[b] = mfma32x32x16(av[b], bt, o[b]);
+                }
+        }
+        l += __shfl_xor(l, 32, 64);
+        if constexpr (kPG > 1) {
+            // the other position group's sums, merged by group 0
+            float* mg = reinterpret_cast<float*>(lds);
+            __syncthreads();
+            if (pg > 0) {
+                float* dst = mg + (w - kRowWaves) * (DB * 16 + 2) * 64 + lane;
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dst[(b * 16 + i) * 64] = o[b][i];
+                dst[DB * 16 * 64] = m;
+                dst[(DB * 16 + 1) * 64] = l;
+            }
+            __syncthreads();
+            if (pg > 0) continue;
+#pragma unroll
+            for (int k = 1; k < kPG; ++k) {
+                const float* src = mg + ((k - 1) * kRowWaves + w) * (DB * 16 + 2) * 64 + lane;
+                const float m2 = src[DB * 16 * 64], l2 = src[(DB * 16 + 1) * 64];
+                const float mn = fmaxf(m, m2);
+                const float ms = mn == -INFINITY ? 0.f : base2(mn, scale2);
+                const float f1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
+                const float f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m2, scale2) - ms);
+#pragma unroll
+                for (int b = 0; b < DB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[b][i] = fmaf(src[(b * 16 + i) * 64], f2, o[b][i] * f1);
+                l = fmaf(l2, f2, l * f1);
+                m = mn;
+            }
+        }
+        if (!row_ok) continue;
+        // lane: dims 32 b + 8 i + 4 h + e of its row (register 4 i + e)
+        if (im.slot >= 0) {
+            float* dst = a.tile_part + ((int64_t)im.slot * 128 + row) * (HD + kPartPad);
+#pragma unroll
+            for (int b = 0; b < DB; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<float4*>(dst + b * 32 + 8 * i + 4 * h) =
+                        make_float4(o[b][4 * i], o[b][4 * i + 1], o[b][4 * i + 2], o[b][4 * i + 3]);
+            if (h == 0) {
+                dst[HD] = m == -INFINITY ? -INFINITY : base2(m, scale2);
+                dst[HD + 1] = l;
+            }
+            continue;
+        }
+        const float inv = m == -INFINITY ? 0.f : 1.0f / l;
+        uint16_t* dst = out + ((int64_t)(im.tok0 + t) * a.H + j) * HD + 4 * h;
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v[4] = {o[b][4 * i] * inv, o[b][4 * i + 1] * inv, o[b][4 * i + 2] * inv, o[b][4 * i + 3] * inv};
+                *reinterpret_cast<uint2*>(dst + b * 32 + 8 * i) = pack_bf16x4(v);
+            }
+    }
+}
+
+// merge_kernel: one wave per row, lane i taking dims i HD/64 ..; the partial
+// sums of the row's slots are added in slot order, weighted by their maxima.
+template <int HD>
+__global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict__ out)
+{
+    constexpr int D = HD / 64;
+    const int group = a.H / a.G, lane = threadIdx.x & 63;
+    const int n_items = a.hdr->n_merge;
+    for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+        const Merge mg = a.merge[it];
+        const int stride = (mg.tile ? 128 : kFewRows) * (HD + kPartPad);
+        for (int row = blockIdx.y * 4 + (threadIdx.x >> 6); row < mg.rows; row += gridDim.y * 4) {
+            const float* base = (mg.tile ? a.tile_part : a.few_part) + (int64_t)mg.slot0 * stride + row * (HD + kPartPad);
+            float M = -INFINITY;
+            for (int s = lane; s < mg.n; s += 64) M = fmaxf(M, base[(int64_t)s * stride + HD]);
+            for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+            float L = 0.f, acc[D];
+#pragma unroll
+            for (int e = 0; e < D; ++e) acc[e] = 0.f;
+            if (M != -INFINITY) {
+#pragma unroll 4
+                for (int s = 0; s < mg.n; ++s) {
+                    const float* pc = base + (int64_t)s * stride;
+                    const float mk = pc[HD];
+                    if (mk == -INFINITY) continue;
+                    const float f = __builtin_amdgcn_exp2f(mk - M);
+                    L = fmaf(pc[HD + 1], f, L);
+#pragma unroll
+                    for (int e = 0; e < D; ++e) acc[e] = fmaf(pc[lane * D + e], f, acc[e]);
+                }
+            }
+            const float inv = M == -INFINITY ? 0.f : 1.0f / L;
+            const int gr = mg.row0 + row, t = gr / group, j = mg.kvh * group + gr % group;
+            uint16_t* dst = out + ((int64_t)(mg.tok0 + t) * a.H + j) * HD + lane * D;
+            if constexpr (D == 2)
+                *reinterpret_cast<uint32_t*>(dst) = moe::cvt_pk_bf16(acc[0] * inv, acc[1] * inv);
+            else
+                dst[0] = moe::f32_to_bf16(acc[0] * inv);
+        }
+    }
+}
+
+}  // namespace paged
+
+extern "C" {
+
+hipError_t attn_paged_launch_unpack(const paged::Unpack* u, hipStream_t s)
+{
+    uint64_t most = 0;
+    for (const paged::Segment& g : u->seg) most = g.bytes > most ? g.bytes : most;
+    const uint64_t blocks = (most / 16 + 255) / 256;
+    hipLaunchKernelGGL(paged::unpack_kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks > 256 ? 256 : blocks)), dim3(256), 0, s, *u);
+    return hipGetLastError();
+}
+
+hipError_t attn_paged_launch_append(const paged::Args* a, const paged::Source* x, uint16_t* q, int T,
+                                    int n_pages, hipStream_t s)
+{
+    const int pieces = (a->e4m3 ? a->H : a->H + 2 * a->G) * a->hd / 8;
+    const dim3 grid(T, (pieces + 255) / 256);
+    if (x->packed) hipLaunchKernelGGL(paged::append_kernel<true>, grid, dim3(256), 0, s, *a, *x, q);
+    else hipLaunchKernelGGL(paged::append_kernel<false>, grid, dim3(256), 0, s, *a, *x, q);
+    if (a->e4m3) {
+        const dim3 tasks(n_pages * a->G * 2);
+        if (x->packed) hipLaunchKernelGGL(paged::code_kernel<true>, tasks, dim3(256), 0, s, *a, *x);
+        else hipLaunchKernelGGL(paged::code_kernel<false>, tasks, dim3(256), 0, s, *a, *x);
+    }
+    return hipGetLastError();
+}
+
+static float scale2(int hd) { return (float)(1.4426950408889634 / sqrt((double)hd)); }
+
+hipError_t attn_paged_launch_few(const paged::Args* a, const uint16_t* q, uint16_t* out, int grid, hipStream_t s)
+{
+#define FEW(HD, E) hipLaunchKernelGGL((paged::few_kernel<HD, E>), dim3(grid), dim3(256), 0, s, *a, q, out, scale2(HD))
+    if (a->hd == 128) {
+        if (a->e4m3) FEW(128, true);
+        else FEW(128, false);
+    } else {
+        if (a->e4m3) FEW(64, true);
+        else FEW(64, false);
+    }
+#undef FEW
+    return hipGetLastError();
+}
+
+hipError_t attn_paged_launch_tile(const paged::Args* a, const uint16_t* q, uint16_t* out, int kind, int grid,
+                                  hipStream_t s)
+{
+#define TILE(HD, E, PG) \
+    hipLaunchKernelGGL((paged::tile_kernel<HD, E, PG>), dim3(grid), dim3(256), 0, s, *a, a->tile[kind], kind, q, out, scale2(HD))
+    if (a->hd == 128) {
+        if (a->e4m3) { if (kind) TILE(128, true, 2); else TILE(128, true, 1); }
+        else { if (kind) TILE(128, false, 2); else TILE(128, false, 1); }
+    } else {
+        if (a->e4m3) { if (kind) TILE(64, true, 2); else TILE(64, true, 1); }
+        else { if (kind) TILE(64, false, 2); else TILE(64, false, 1); }
+    }
+#undef TILE
+    return hipGetLastError();
+}
+
+hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, hipStream_t s)
+{
+    const dim3 g(grid, (rows + 3) / 4);
+    if (a->hd == 128) hipLaunchKernelGGL(paged::merge_kernel<128>, g, dim3(256), 0, s, *a, out);
+    else hipLaunchKernelGGL(paged::merge_kernel<64>, g, dim3(256), 0, s, *a, out);
+    return hipGetLastError();
+}
+
+}  // extern "C"

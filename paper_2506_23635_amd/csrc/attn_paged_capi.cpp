@@ -1,0 +1,576 @@
+// attn_paged_capi.cpp -- the C-ABI of the paged cache (include/attn.h):
+// configuration checks, the carve-up of the caller's cache and workspace, a
+// batch's checks and its division into workgroups' shares, and the launches.
+// Nothing here allocates device memory.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <string>
+#include <utility>
+#include <vector>
+
+#include "attn_paged.h"
+
+using paged::Item;
+using paged::Merge;
+
+namespace {
+
+constexpr size_t kAlign = 256;
+constexpr int kStages = 4;             // batches on their way to the device at once
+constexpr int kXcds = 8;
+constexpr int64_t kFewItems = 2048;    // at most about so many shares of few_kernel ...
+constexpr int64_t kTileItems = 512;    // ... and of tile_kernel come from dividing positions
+
+size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+struct Layout {
+    size_t data_bytes, scale_bytes, layer_bytes, cache_bytes;   // K or V of a layer; its scales
+    size_t hdr, freq, tok, pages, few, tile[2], merge, table, few_part, tile_part, ws_bytes;
+    size_t max_few, max_tile[2], max_merge, few_slots, tile_slots;
+    int shift;
+};
+
+const char* check_config(const attn_paged_config* c)
+{
+    if (!c) return "config is NULL";
+    if (c->head_dim != 64 && c->head_dim != 128) return "head_dim must be 64 or 128";
+    if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads) return "n_kv_heads must divide n_heads";
+    if (c->n_heads / c->n_kv_heads > paged::kFewRows) return "at most 16 query heads per key/value head";
+    if ((int64_t)c->n_heads * c->head_dim > 65536) return "n_heads * head_dim too large";
+    if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)))
+        return "page_size must be 16, 32, 64, 128 or 256";
+    if (c->n_pages < 1 || c->n_pages > (1 << 24)) return "n_pages must be in [1, 2^24]";
+    if (c->n_layers < 1 || c->n_layers > 1024) return "n_layers must be in [1, 1024]";
+    if (c->max_seqs < 1 || c->max_seqs > 4096) return "max_seqs must be in [1, 4096]";
+    if (c->max_tokens < 1 || c->max_tokens > 32768) return "max_tokens must be in [1, 32768]";
+    if (c->max_blocks < 1 || c->max_blocks > 65536) return "max_blocks must be in [1, 65536]";
+    if ((int64_t)c->max_blocks * c->page_size > (1 << 24)) return "max_blocks * page_size must be at most 2^24";
+    if ((int64_t)c->max_seqs * c->max_blocks > (1 << 26)) return "max_seqs * max_blocks must be at most 2^26";
+    if (!(c->rope_theta > 1.0f) || !std::isfinite(c->rope_theta)) return "rope_theta must be > 1";
+    if (c->flags & ~ATTN_PAGED_E4M3) return "flags must be 0 or ATTN_PAGED_E4M3";
+    return nullptr;
+}
+
+Layout make_layout(const attn_paged_config* c)
+{
+    Layout L{};
+    const size_t G = c->n_kv_heads, hd = c->head_dim, H = c->n_heads, group = H / G;
+    const bool e4m3 = c->flags & ATTN_PAGED_E4M3;
+    for (L.shift = 4; (1 << L.shift) < c->page_size; ++L.shift) {}
+    L.data_bytes = (size_t)c->n_pages * G * c->page_size * hd * (e4m3 ? 1 : 2);
+    L.scale_bytes = e4m3 ? align_up((size_t)c->n_pages * G * 4, kAlign) : 0;
+    L.layer_bytes = 2 * L.data_bytes + 2 * L.scale_bytes;
+    L.cache_bytes = L.layer_bytes * c->n_layers;
+    // Shares: every sequence and key/value head has one, every row block of
+    // tile_kernel, and divided positions add at most twice the division's aim
+    // (a range is at least half as long as the common length).
+    const size_t S = c->max_seqs, T = c->max_tokens, rows = T * group;
+    const size_t few_seqs = std::min(S, T), tile_seqs = std::min(S, rows / (paged::kFewRows + 1) + 1);
+    L.max_few = few_seqs * G + 2 * kFewItems;
+    // (no more ranges than steps)
+    const size_t few_steps = few_seqs * G * (((size_t)c->max_blocks * c->page_size + 127) / 128);
+    L.few_slots = std::min<size_t>(2 * kFewItems, few_steps);
+    const bool tiles = rows > (size_t)paged::kFewRows;
+    for (int k = 0; k < 2; ++k)
+        L.max_tile[k] = tiles ? (rows / (128 >> k) + tile_seqs) * G + 2 * kTileItems : 0;
+    L.tile_slots = tiles ? 2 * kTileItems : 0;
+    L.max_merge = kFewItems + 2 * (tiles ? kTileItems : 0);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, kAlign); return o; };
+    L.hdr = take(sizeof(paged::Header));
+    L.freq = take(hd / 2 * 8);
+    L.tok = take(T * sizeof(paged::Token) + 16);
+    L.pages = take(T * sizeof(paged::PageWork));
+    L.few = take(L.max_few * sizeof(Item));
+    L.tile[0] = take(L.max_tile[0] * sizeof(Item));
+    L.tile[1] = take(L.max_tile[1] * sizeof(Item));
+    L.merge = take(L.max_merge * sizeof(Merge));
+    L.table = take(S * c->max_blocks * 4 + 16);
+    L.few_part = take(L.few_slots * paged::kFewRows * (hd + paged::kPartPad) * 4);
+    L.tile_part = take(L.tile_slots * 128 * (hd + paged::kPartPad) * 4);
+    L.ws_bytes = off;
+    return L;
+}
+
+thread_local std::string g_init_error;
+
+struct Stage {
+    uint8_t* mem = nullptr;            // pinned host memory
+    size_t bytes = 0;
+    hipEvent_t done = nullptr;
+    bool busy = false;
+};
+
+// A batch as the host keeps it.
+struct Batch {
+    std::vector<paged::Token> tok;
+    std::vector<paged::PageWork> pages;
+    std::vector<Item> few, tile[2];
+    std::vector<Merge> merge;
+    std::vector<int32_t> table;
+    int merge_rows = 0;
+};
+
+}  // namespace
+
+struct attn_paged_ctx {
+    attn_paged_config cfg;
+    Layout L;
+    uint8_t *cache, *ws;
+    std::vector<double> freq;
+    std::vector<int32_t> written;      // per page: the call that last had it written, for set_batch
+    int32_t call;
+    bool set;
+    int32_t T, n_pages, n_few, n_tile[2], n_merge, merge_rows;
+    Stage stage[kStages];
+    int next_stage;
+    std::string err;
+};
+
+namespace {
+
+moe_status fail(attn_paged_ctx* ctx, moe_status s, const char* msg)
+{
+    try {
+        (ctx ? ctx->err : g_init_error) = msg;
+    } catch (...) {
+    }
+    return s;
+}
+
+moe_status hip_fail(attn_paged_ctx* ctx, hipError_t e, const char* what)
+{
+    try {
+        ctx->err = std::string(what) + ": " + hipGetErrorString(e);
+    } catch (...) {
+    }
+    return MOE_E_HIP;
+}
+
+bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
+
+// Divides `steps` steps from `begin` on into n ranges that differ by one at most.
+void ranges(std::vector<Item>& out, Item it, int n, int step, int& slot)
+{
+    const int64_t steps = (it.end - it.begin + step - 1) / step;
+    const int begin = it.begin, end = it.end;
+    for (int i = 0; i < n; ++i) {
+        it.begin = begin + (int)(steps * i / n) * step;
+        it.end = std::min<int64_t>(end, begin + steps * (i + 1) / n * step);
+        it.slot = n > 1 ? slot++ : -1;
+        out.push_back(it);
+    }
+}
+
+// The common length of a range: `total` steps in about `aim` shares.
+int64_t range_steps(int64_t total, int64_t aim, int64_t least)
+{
+    return std::max(least, (total + aim - 1) / aim);
+}
+
+// Longest shares first: the workgroups are handed out in order.
+bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.begin; }
+
+// One list for eight XCDs, workgroup b going to XCD b % 8: the shares in
+// order (those of one sequence and key/value head together, so that an L2
+// reads its keys and values once) cut into eight runs of about equal work,
+// each run's longest first, and the runs interleaved.
+void by_xcd(std::vector<Item>& v)
+{
+    if (v.size() <= 1) return;
+    int64_t total = 0;
+    auto cost = [](const Item& it) { return (int64_t)(it.end - it.begin) + 2 * paged::kStep; };
+    for (const Item& it : v) total += cost(it);
+    std::vector<Item> run[kXcds];
+    int64_t at = 0;
+    for (const Item& it : v) {
+        const int64_t mid = at + cost(it) / 2;
+        run[std::min<int64_t>(kXcds - 1, mid * kXcds / total)].push_back(it);
+        at += cost(it);
+    }
+    for (auto& r : run) std::stable_sort(r.begin(), r.end(), longer);
+    // a run that is used up goes on with the last of the longest one left
+    std::vector<Item> out;
+    out.reserve(v.size());
+    size_t next[kXcds] = {};
+    while (out.size() < v.size()) {
+        auto left = [&](int x) { return run[x].size() - next[x]; };
+        const int x = (int)(out.size() % kXcds);
+        if (left(x) > 0) {
+            out.push_back(run[x][next[x]++]);
+            continue;
+        }
+        int y = 0;
+        for (int k = 1; k < kXcds; ++k)
+            if (left(k) > left(y)) y = k;
+        out.push_back(run[y].back());
+        run[y].pop_back();
+    }
+    v = std::move(out);
+}
+
+void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, const int32_t* pos0, int n_seqs,
+            const std::vector<uint8_t>& holes, Batch& b)
+{
+    const int G = c.n_kv_heads, group = c.n_heads / G;
+    auto blocks_of = [&](int s) { return (int)(((int64_t)pos0[s] + n_new[s] + c.page_size - 1) >> L.shift); };
+    // few rows: every wave takes steps of 32 positions, a workgroup 128
+    constexpr int kFewStep = 4 * paged::kTile;
+    int64_t few_total = 0, tile_total = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+        const int64_t R = (int64_t)n_new[s] * group, n_pos = (int64_t)pos0[s] + n_new[s];
+        if (R == 0) continue;
+        if (R <= paged::kFewRows) {
+            few_total += (n_pos + kFewStep - 1) / kFewStep * G;
+        } else {
+            const int rows = R <= 64 ? 64 : 128;
+            for (int64_t r0 = 0; r0 < R; r0 += rows)
+                tile_total += (pos0[s] + (std::min(r0 + rows, R) - 1) / group + paged::kStep) / paged::kStep * G;
+        }
+    }
+    const int64_t few_len = range_steps(few_total, kFewItems, 1), tile_len = range_steps(tile_total, kTileItems, 4);
+    int few_slot = 0, tile_slot = 0, tok0 = 0, table = 0;
+    for (int s = 0; s < n_seqs; ++s) {
+        const int R = n_new[s] * group, n_pos = pos0[s] + n_new[s];
+        Item it{};
+        it.tok0 = tok0;
+        it.pos0 = pos0[s];
+        it.n_pos = n_pos;
+        it.table = table;
+        it.holes = holes[s];
+        if (R > 0 && R <= paged::kFewRows) {
+            it.rows = R;
+            it.end = n_pos;
+            const int64_t steps = (n_pos + kFewStep - 1) / kFewStep;
+            const int n = (int)((steps + few_len - 1) / few_len);
+            for (it.kvh = 0; it.kvh < G; ++it.kvh) {
+                if (n > 1) {
+                    b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, 0, 0});
+                    b.merge_rows = std::max(b.merge_rows, R);
+                }
+                ranges(b.few, it, n, kFewStep, few_slot);
+            }
+        } else if (R > 0) {
+            const int kind = R <= 64, rows = 128 >> kind;
+            for (it.kvh = 0; it.kvh < G; ++it.kvh)
+                for (int r0 = 0; r0 < R; r0 += rows) {
+                    it.row0 = r0;
+                    it.rows = std::min(rows, R - r0);
+                    it.begin = 0;
+                    it.end = pos0[s] + (r0 + it.rows - 1) / group + 1;
+                    const int64_t steps = (it.end + paged::kStep - 1) / paged::kStep;
+                    const int n = (int)((steps + tile_len - 1) / tile_len);
+                    if (n > 1) {
+                        b.merge.push_back(Merge{tok0, r0, it.rows, it.kvh, tile_slot, n, 1, 0});
+                        b.merge_rows = std::max(b.merge_rows, (int)it.rows);
+                    }
+                    ranges(b.tile[kind], it, n, paged::kStep, tile_slot);
+                }
+        }
+        tok0 += n_new[s];
+        table += n_new[s] > 0 ? blocks_of(s) : 0;
+    }
+    std::stable_sort(b.few.begin(), b.few.end(), longer);
+    by_xcd(b.tile[0]);
+    by_xcd(b.tile[1]);
+}
+
+paged::Args layer_args(attn_paged_ctx* c, int layer)
+{
+    const Layout& L = c->L;
+    paged::Args a{};
+    a.hdr = reinterpret_cast<const paged::Header*>(c->ws + L.hdr);
+    a.freq = reinterpret_cast<const double*>(c->ws + L.freq);
+    a.tok = reinterpret_cast<const paged::Token*>(c->ws + L.tok);
+    a.pages = reinterpret_cast<const paged::PageWork*>(c->ws + L.pages);
+    a.few = reinterpret_cast<const Item*>(c->ws + L.few);
+    for (int k = 0; k < 2; ++k) a.tile[k] = reinterpret_cast<const Item*>(c->ws + L.tile[k]);
+    a.merge = reinterpret_cast<const Merge*>(c->ws + L.merge);
+    a.table = reinterpret_cast<const int32_t*>(c->ws + L.table);
+    a.few_part = reinterpret_cast<float*>(c->ws + L.few_part);
+    a.tile_part = reinterpret_cast<float*>(c->ws + L.tile_part);
+    uint8_t* base = c->cache + (size_t)layer * L.layer_bytes;
+    a.k = base;
+    a.v = base + L.data_bytes;
+    a.k_scale = reinterpret_cast<float*>(base + 2 * L.data_bytes);
+    a.v_scale = reinterpret_cast<float*>(base + 2 * L.data_bytes + L.scale_bytes);
+    a.H = c->cfg.n_heads;
+    a.G = c->cfg.n_kv_heads;
+    a.hd = c->cfg.head_dim;
+    a.shift = L.shift;
+    a.e4m3 = (c->cfg.flags & ATTN_PAGED_E4M3) != 0;
+    return a;
+}
+
+// Waits until the stage's last batch has left it, and makes it large enough.
+hipError_t ready(Stage& st, size_t bytes)
+{
+    hipError_t e = hipSuccess;
+    if (st.busy) {
+        e = hipEventSynchronize(st.done);
+        if (e != hipSuccess) return e;
+        st.busy = false;
+    }
+    if (!st.done) {
+        e = hipEventCreateWithFlags(&st.done, hipEventDisableTiming);
+        if (e != hipSuccess) { st.done = nullptr; return e; }
+    }
+    if (st.bytes < bytes) {
+        if (st.mem) (void)hipHostFree(st.mem);
+        st.mem = nullptr;
+        st.bytes = 0;
+        void* p = nullptr;
+        const size_t want = align_up(bytes + bytes / 2, 4096);
+        e = hipHostMalloc(&p, want, hipHostMallocDefault);
+        if (e != hipSuccess) return e;
+        st.mem = static_cast<uint8_t*>(p);
+        st.bytes = want;
+    }
+    return hipSuccess;
+}
+
+moe_status check_call(attn_paged_ctx* ctx, int32_t layer)
+{
+    if (layer < 0 || layer >= ctx->cfg.n_layers) return fail(ctx, MOE_E_ARG, "layer out of range");
+    if (!ctx->set) return fail(ctx, MOE_E_STATE, "no batch set");
+    return MOE_OK;
+}
+
+bool capturing(hipStream_t s)
+{
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    return hipStreamIsCapturing(s, &st) == hipSuccess && st != hipStreamCaptureStatusNone;
+}
+
+moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, const int32_t* pos0,
+                     const int32_t* table, int32_t ld, hipStream_t s)
+{
+    const attn_paged_config& c = ctx->cfg;
+    const Layout& L = ctx->L;
+    if (n_seqs < 0) return fail(ctx, MOE_E_ARG, "n_seqs is negative");
+    if (n_seqs > c.max_seqs) return fail(ctx, MOE_E_CAPACITY, "n_seqs exceeds max_seqs");
+    if (n_seqs > 0 && (!n_new || !pos0 || !table)) return fail(ctx, MOE_E_ARG, "n_new, pos0 or table is NULL");
+    if (n_seqs > 0 && ld < 1) return fail(ctx, MOE_E_ARG, "ld must be at least 1");
+    int64_t T = 0;
+    for (int i = 0; i < n_seqs; ++i) {
+        if (n_new[i] < 0 || pos0[i] < 0) return fail(ctx, MOE_E_ARG, "n_new and pos0 must be non-negative");
+        T += n_new[i];
+    }
+    if (T > c.max_tokens) return fail(ctx, MOE_E_CAPACITY, "the batch's tokens exceed max_tokens");
+    Batch b;
+    std::vector<uint8_t> holes(n_seqs, 0);
+    b.tok.reserve(T);
+    if (ctx->call == INT32_MAX) {
+        std::fill(ctx->written.begin(), ctx->written.end(), 0);
+        ctx->call = 0;
+    }
+    const int32_t call = ++ctx->call;
+    for (int i = 0; i < n_seqs; ++i) {
+        const int64_t n_pos = (int64_t)pos0[i] + n_new[i], blocks = (n_pos + c.page_size - 1) >> L.shift;
+        if (blocks > c.max_blocks) return fail(ctx, MOE_E_CAPACITY, "a sequence exceeds max_blocks pages");
+        if (blocks > ld) return fail(ctx, MOE_E_ARG, "ld is smaller than a sequence's pages");
+        const int32_t* row = table + (int64_t)i * ld;
+        for (int64_t k = 0; k < blocks; ++k) {
+            if (row[k] < -1 || row[k] >= c.n_pages) return fail(ctx, MOE_E_ARG, "a table entry is outside -1 .. n_pages - 1");
+            if (row[k] < 0) holes[i] = 1;
+        }
+        if (n_new[i] == 0) continue;
+        b.table.insert(b.table.end(), row, row + blocks);
+        for (int64_t k = pos0[i] >> L.shift; k < blocks; ++k) {
+            const int32_t page = row[k];
+            if (page < 0) return fail(ctx, MOE_E_ARG, "a new token has no page");
+            if (ctx->written[page] == call) return fail(ctx, MOE_E_ARG, "a page would be written twice");
+            ctx->written[page] = call;
+            const int64_t lo = std::max<int64_t>(pos0[i], k << L.shift), hi = std::min(n_pos, (k + 1) << L.shift);
+            b.pages.push_back(paged::PageWork{page, (int32_t)(lo - (k << L.shift)), (int32_t)(hi - lo), (int32_t)b.tok.size()});
+            for (int64_t p = lo; p < hi; ++p) b.tok.push_back(paged::Token{(int32_t)p, page});
+        }
+    }
+    divide(c, L, n_new, pos0, n_seqs, holes, b);
+    if (b.few.size() > L.max_few || b.tile[0].size() > L.max_tile[0] || b.tile[1].size() > L.max_tile[1] ||
+        b.merge.size() > L.max_merge)
+        return fail(ctx, MOE_E_CAPACITY, "the batch has more shares than the workspace holds");
+    if (T > 0) {
+        paged::Header h{};
+        h.T = (int32_t)T;
+        h.n_pages = (int32_t)b.pages.size();
+        h.n_few = (int32_t)b.few.size();
+        for (int k = 0; k < 2; ++k) h.n_tile[k] = (int32_t)b.tile[k].size();
+        h.n_merge = (int32_t)b.merge.size();
+        const struct { size_t dst; const void* src; size_t bytes; } parts[paged::kSegments] = {
+            {L.hdr, &h, sizeof h},
+            {L.freq, ctx->freq.data(), ctx->freq.size() * 8},
+            {L.tok, b.tok.data(), b.tok.size() * sizeof(paged::Token)},
+            {L.pages, b.pages.data(), b.pages.size() * sizeof(paged::PageWork)},
+            {L.few, b.few.data(), b.few.size() * sizeof(Item)},
+            {L.tile[0], b.tile[0].data(), b.tile[0].size() * sizeof(Item)},
+            {L.tile[1], b.tile[1].data(), b.tile[1].size() * sizeof(Item)},
+            {L.merge, b.merge.data(), b.merge.size() * sizeof(Merge)},
+            {L.table, b.table.data(), b.table.size() * 4}};
+        size_t bytes = 0;
+        for (const auto& p : parts) bytes += align_up(p.bytes, 16);
+        if (capturing(s)) return fail(ctx, MOE_E_STATE, "a batch cannot be set while the stream captures a graph");
+        Stage& st = ctx->stage[ctx->next_stage];
+        hipError_t e = ready(st, bytes);
+        if (e != hipSuccess) return hip_fail(ctx, e, "pinned memory for the batch");
+        paged::Unpack u{};
+        u.src = st.mem;
+        u.dst = ctx->ws;
+        size_t at = 0;
+        for (int k = 0; k < paged::kSegments; ++k) {
+            const size_t n = align_up(parts[k].bytes, 16);
+            if (parts[k].bytes) std::memcpy(st.mem + at, parts[k].src, parts[k].bytes);
+            if (n > parts[k].bytes) std::memset(st.mem + at + parts[k].bytes, 0, n - parts[k].bytes);
+            u.seg[k] = paged::Segment{parts[k].dst, at, n};
+            at += n;
+        }
+        e = attn_paged_launch_unpack(&u, s);
+        if (e != hipSuccess) return hip_fail(ctx, e, "batch kernel launch");
+        e = hipEventRecord(st.done, s);
+        if (e != hipSuccess) return hip_fail(ctx, e, "batch event");
+        st.busy = true;
+        ctx->next_stage = (ctx->next_stage + 1) % kStages;
+    }
+    ctx->T = (int32_t)T;
+    ctx->n_pages = (int32_t)b.pages.size();
+    ctx->n_few = (int32_t)b.few.size();
+    for (int k = 0; k < 2; ++k) ctx->n_tile[k] = (int32_t)b.tile[k].size();
+    ctx->n_merge = (int32_t)b.merge.size();
+    ctx->merge_rows = b.merge_rows;
+    ctx->set = true;
+    return MOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t attn_paged_tokens(const attn_paged_ctx* ctx) { return ctx->T; }
+const attn_paged_config* attn_paged_cfg(const attn_paged_ctx* ctx) { return &ctx->cfg; }
+int attn_paged_has_batch(const attn_paged_ctx* ctx) { return ctx->set; }
+
+hipError_t attn_paged_run_append(attn_paged_ctx* ctx, int32_t layer, const paged::Source* x, uint16_t* q,
+                                 hipStream_t s)
+{
+    const paged::Args a = layer_args(ctx, layer);
+    return attn_paged_launch_append(&a, x, q, ctx->T, ctx->n_pages, s);
+}
+
+hipError_t attn_paged_run_attend(attn_paged_ctx* ctx, int32_t layer, const uint16_t* q, uint16_t* out,
+                                 hipStream_t s)
+{
+    const paged::Args a = layer_args(ctx, layer);
+    // a graph may replay on a longer batch: its launches have room for the
+    // shares that one may have, and the merge is there
+    const bool graph = capturing(s);
+    auto grid = [&](int n) { return graph ? std::max(n, 512) : n; };
+    hipError_t e = hipSuccess;
+    for (int k = 0; k < 2 && e == hipSuccess; ++k)
+        if (ctx->n_tile[k]) e = attn_paged_launch_tile(&a, q, out, k, grid(ctx->n_tile[k]), s);
+    if (e == hipSuccess && ctx->n_few) e = attn_paged_launch_few(&a, q, out, grid(ctx->n_few), s);
+    if (e == hipSuccess && (ctx->n_merge || graph))
+        e = attn_paged_launch_merge(&a, out, graph ? std::max(ctx->n_merge, 64) : ctx->n_merge,
+                                    std::max(ctx->merge_rows, graph ? paged::kFewRows : 1), s);
+    return e;
+}
+
+size_t attn_paged_cache_bytes(const attn_paged_config* cfg)
+{
+    return check_config(cfg) ? 0 : make_layout(cfg).cache_bytes;
+}
+
+size_t attn_paged_workspace_bytes(const attn_paged_config* cfg)
+{
+    return check_config(cfg) ? 0 : make_layout(cfg).ws_bytes;
+}
+
+moe_status attn_paged_init(const attn_paged_config* cfg, void* cache, void* workspace, attn_paged_ctx** out)
+{
+    if (!out) return fail(nullptr, MOE_E_ARG, "out is NULL");
+    *out = nullptr;
+    if (const char* why = check_config(cfg)) return fail(nullptr, MOE_E_SHAPE, why);
+    if (!cache || !workspace) return fail(nullptr, MOE_E_ARG, "cache or workspace is NULL");
+    if (((uintptr_t)cache | (uintptr_t)workspace) & (kAlign - 1))
+        return fail(nullptr, MOE_E_ALIGN, "cache and workspace must be 256-byte aligned");
+    attn_paged_ctx* c = new (std::nothrow) attn_paged_ctx();
+    if (!c) return fail(nullptr, MOE_E_ARG, "out of host memory");
+    c->cfg = *cfg;
+    c->L = make_layout(cfg);
+    c->cache = static_cast<uint8_t*>(cache);
+    c->ws = static_cast<uint8_t*>(workspace);
+    try {
+        c->freq.resize(cfg->head_dim / 2);
+        c->written.assign(cfg->n_pages, 0);
+    } catch (...) {
+        delete c;
+        return fail(nullptr, MOE_E_ARG, "out of host memory");
+    }
+    for (int f = 0; f < cfg->head_dim / 2; ++f) c->freq[f] = std::pow((double)cfg->rope_theta, -2.0 * f / cfg->head_dim);
+    *out = c;
+    return MOE_OK;
+}
+
+moe_status attn_paged_set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, const int32_t* pos0,
+                                const int32_t* table, int32_t ld, moe_stream_t stream)
+{
+    if (!ctx) return MOE_E_ARG;
+    try {
+        return set_batch(ctx, n_seqs, n_new, pos0, table, ld, static_cast<hipStream_t>(stream));
+    } catch (...) {
+        return fail(ctx, MOE_E_ARG, "out of host memory for the batch");
+    }
+}
+
+moe_status attn_paged_append(attn_paged_ctx* ctx, int32_t layer, const void* qkv, int64_t ld, int32_t type,
+                             uint16_t* q, moe_stream_t stream)
+{
+    if (!ctx) return MOE_E_ARG;
+    const moe_status st = check_call(ctx, layer);
+    if (st != MOE_OK) return st;
+    const attn_paged_config& c = ctx->cfg;
+    if (type != ATTN_QKV_F32 && type != ATTN_QKV_BF16) return fail(ctx, MOE_E_ARG, "unknown type of q | k | v");
+    const int64_t n = (int64_t)(c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
+    if (ld < n || ld > (INT64_MAX >> 20)) return fail(ctx, MOE_E_ARG, "ld is smaller than a row of q | k | v, or too large");
+    if (ld % (type == ATTN_QKV_BF16 ? 8 : 4)) return fail(ctx, MOE_E_ALIGN, "the rows of q | k | v must be 16-byte aligned");
+    if (ctx->T == 0) return MOE_OK;
+    if (!qkv || !q) return fail(ctx, MOE_E_ARG, "qkv or q is NULL");
+    if (misaligned(qkv) || misaligned(q)) return fail(ctx, MOE_E_ALIGN, "qkv and q must be 16-byte aligned");
+    const paged::Source x{qkv, ld, 0, 1, type == ATTN_QKV_BF16, 0};
+    const hipError_t e = attn_paged_run_append(ctx, layer, &x, q, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e, "append kernel launch");
+    return MOE_OK;
+}
+
+moe_status attn_paged_attend(attn_paged_ctx* ctx, int32_t layer, const uint16_t* q, uint16_t* out,
+                             moe_stream_t stream)
+{
+    if (!ctx) return MOE_E_ARG;
+    const moe_status st = check_call(ctx, layer);
+    if (st != MOE_OK) return st;
+    if (ctx->T == 0) return MOE_OK;
+    if (!q || !out) return fail(ctx, MOE_E_ARG, "q or out is NULL");
+    if (q == out) return fail(ctx, MOE_E_ARG, "out may not be q");
+    if (misaligned(q) || misaligned(out)) return fail(ctx, MOE_E_ALIGN, "q and out must be 16-byte aligned");
+    const hipError_t e = attn_paged_run_attend(ctx, layer, q, out, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e, "attention kernel launch");
+    return MOE_OK;
+}
+
+void attn_paged_destroy(attn_paged_ctx* ctx)
+{
+    if (!ctx) return;
+    for (Stage& st : ctx->stage) {
+        if (st.busy) (void)hipEventSynchronize(st.done);
+        if (st.done) (void)hipEventDestroy(st.done);
+        if (st.mem) (void)hipHostFree(st.mem);
+    }
+    delete ctx;
+}
+
+const char* attn_paged_last_error(const attn_paged_ctx* ctx) { return ctx ? ctx->err.c_str() : g_init_error.c_str(); }
+
+}  // extern "C"

@@ -194,6 +194,8 @@ hipError_t attn_launch_qkv(const void* w, uint16_t* h, const uint16_t* x, const 
                            int max_seq, int pos0, hipStream_t s);
 hipError_t attn_launch_out(const void* w, const uint16_t* x, int T, int K, int N, float* y32,
                            const uint16_t* res, uint16_t* y16, hipStream_t s);
+hipError_t attn_launch_product(const void* w, const uint16_t* x, int T, int K, int N, float* y32,
+                               hipStream_t s);
 hipError_t attn_launch_rope(const float* qkvp, const float* cos_sin, float* qkv, uint16_t* q,
                             uint16_t* kc, uint16_t* vc, int T, int H, int G, int hd, int max_seq,
                             int pos0, int n_split, hipStream_t s);
