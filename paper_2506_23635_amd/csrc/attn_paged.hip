@@ -8,6 +8,7 @@
 //   tile_kernel    attention of blocks of 128 or 64 query rows
 //   merge_kernel   adds the partial sums of rows whose positions were shared out
 #include <cmath>
+#include <type_traits>
 
 #include "attn_paged.h"
 #include "moe_common.h"
@@ -25,6 +26,41 @@ __device__ inline f32x16_t mfma32x32x16(const u32x4_t a, const u32x4_t b, f32x16
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(moe::bf16x8_t, a),
                                                    __builtin_bit_cast(moe::bf16x8_t, b), c, 0, 0, 0);
+}
+
+// A load through the scalar cache, of what no kernel writes while this one
+// runs and whose address is the same for the whole wave.  (Left to the
+// compiler these are vector loads, as the kernel also stores, and the wait for
+// a page number becomes a wait for every key and value in flight.)
+template <class T>
+__device__ __forceinline__ T uniform_load(const T* p)
+{
+    return *(const __attribute__((address_space(4))) T*)p;
+}
+
+template <class T>
+__device__ __forceinline__ T uniform_struct(const T* p)
+{
+    static_assert(sizeof(T) % 16 == 0);
+    T r;
+    u32x4_t* d = reinterpret_cast<u32x4_t*>(&r);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(T) / 16); ++i) d[i] = uniform_load(reinterpret_cast<const u32x4_t*>(p) + i);
+    return r;
+}
+
+// The maximum over lanes l, l ^ 32 and over l, l ^ 16 (halves and rows
+// swapped between two registers: no LDS)
+__device__ __forceinline__ float max32(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float max16(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
 // barrier for LDS traffic only: global loads stay in flight across it
@@ -199,9 +235,9 @@ __global__ __launch_bounds__(256) void code_kernel(Args a, Source x)
     const int G = a.G, hd = a.hd, P = hd / 8;
     const int per_pass = 256 / P;
     const int tj = threadIdx.x / P, pc = threadIdx.x % P;
-    const int n_tasks = a.hdr->n_pages * G * 2;
+    const int n_tasks = uniform_load(&a.hdr->n_pages) * G * 2;
     for (int task = blockIdx.x; task < n_tasks; task += gridDim.x) {
-        const PageWork w = a.pages[task / (2 * G)];
+        const PageWork w = uniform_struct(a.pages + task / (2 * G));
         const int g = task / 2 % G;
         const bool turn = task % 2 == 0;
         const int head = a.H + g + (turn ? 0 : G), f = pc * (turn ? 4 : 8);
@@ -327,9 +363,9 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int group = a.H / a.G, P = 1 << a.shift;
-    const int n_items = a.hdr->n_few;
+    const int n_items = uniform_load(&a.hdr->n_few);
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        const Item im = a.few[it];
+        const Item im = uniform_struct(a.few + it);
         const int32_t* table = a.table + im.table;
         const int R = im.rows, kvh = im.kvh, n_pos = im.n_pos;
         const bool row_ok = r < R;
@@ -358,7 +394,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
         // the end's page
         auto pages = [&](int p0, int (&pg)[2]) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) pg[s] = table[min(p0 + 16 * s, n_pos - 1) >> a.shift];
+            for (int s = 0; s < 2; ++s) pg[s] = uniform_load(table + (min(p0 + 16 * s, n_pos - 1) >> a.shift));
         };
         // rows past the sequence's last position read that position (masked
         // for every row); a sub-block without a page reads page 0 and is
@@ -372,7 +408,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
                 const uint8_t* kb = a.k + row * (HD * ES) + g * 16;
 #pragma unroll
                 for (int c = 0; c < KW; ++c) kr[s][c] = ld16(kb + c * 64);
-                if constexpr (kE4m3) ksc[s] = a.k_scale[head];
+                if constexpr (kE4m3) ksc[s] = uniform_load(a.k_scale + head);
             }
         };
         auto fetch_v = [&](int p0, const int (&pg)[2]) {
@@ -395,7 +431,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
                         dst[0] = *reinterpret_cast<const uint32_t*>(src);
                     }
                 }
-                if constexpr (kE4m3) vsc[s] = a.v_scale[head];
+                if constexpr (kE4m3) vsc[s] = uniform_load(a.v_scale + head);
             }
         };
         // two dims of the lane's position i, as bf16
@@ -411,14 +447,12 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
         constexpr int step = 4 * kTile;
         int p0 = im.begin + w * kTile;
         int pg[2], pn[2];
-        if (p0 < im.end) {
-            pages(p0, pg);
-            fetch_k(p0, pg);
-            fetch_v(p0, pg);
-            pages(p0 + step, pn);
-        }
-        for (; p0 < im.end; p0 += step) {
-            const bool more = p0 + step < im.end;
+        // One step: scores, softmax, P V.  kMore: the next step's loads are
+        // issued on the way (static: loads behind a branch would make every
+        // wait for V a wait for the next K too).  kMasked: some row does not
+        // see some position of the step, or a page is missing.
+        auto advance = [&](auto more, auto mask) {
+            constexpr bool kMore = decltype(more)::value, kMasked = decltype(mask)::value;
             f32x4_t sc[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -431,9 +465,8 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
                     sc[s] = moe::mfma16x16x32(kf, qf[c], sc[s]);
                 }
             }
-            if (more) fetch_k(p0 + step, pn);
-            const bool masked = p0 + kTile - 1 > im.pos0 || pg[0] < 0 || pg[1] < 0;
-            if (masked) {
+            if constexpr (kMore) fetch_k(p0 + step, pn);
+            if constexpr (kMasked) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -445,8 +478,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[s][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            mx = max32(max16(mx));
             const float ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
             if (__ballot(mx != m)) {
                 const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
@@ -477,8 +509,8 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
                     vt[2 * k][n] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
                     vt[2 * k + 1][n] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
                 }
-            if (more) fetch_v(p0 + step, pn);
-            if (masked) {
+            if constexpr (kMore) fetch_v(p0 + step, pn);
+            if constexpr (kMasked) {
                 // values without a page are zeros; and a value that is not
                 // finite among positions that some rows do not see is taken
                 // out, since 0 times it would still reach those, while the
@@ -520,9 +552,28 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
             for (int i = 0; i < D; ++i) o[i] = moe::mfma16x16x32(vt[i], p1, o[i]);
 #pragma unroll
             for (int i = 0; i < D; ++i) o[i] = moe::mfma16x16x32(vt[i], p2, o[i]);
-            pg[0] = pn[0];
-            pg[1] = pn[1];
-            if (more) pages(p0 + 2 * step, pn);
+        };
+        // steps that every row sees whole, one after another without a pause;
+        // then the sequence's last ones (and all of one with missing pages)
+        const int clean = im.holes ? 0 : min(im.end, im.pos0 + 1) - kTile;   // the last start of such a step
+        if (p0 <= clean) {
+            pages(p0, pg);
+            pages(p0 + step, pn);
+            fetch_k(p0, pg);
+            fetch_v(p0, pg);
+            for (; p0 + step <= clean; p0 += step) {
+                advance(std::true_type{}, std::false_type{});
+                pages(p0 + 2 * step, pn);
+            }
+            advance(std::false_type{}, std::false_type{});
+            p0 += step;
+        }
+        for (; p0 < im.end; p0 += step) {
+            pages(p0, pg);
+            if (pg[0] < 0 && pg[1] < 0) continue;
+            fetch_k(p0, pg);
+            fetch_v(p0, pg);
+            advance(std::false_type{}, std::true_type{});
         }
         l += __shfl_xor(l, 16, 64);
         l += __shfl_xor(l, 32, 64);
@@ -615,10 +666,10 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, h = lane >> 5;
     const int pg = w / kRowWaves;                        // the wave's position group
-    const int n_items = a.hdr->n_tile[which];
+    const int n_items = uniform_load(&a.hdr->n_tile[which]);
     const u32x4_t zero = {0u, 0u, 0u, 0u};
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        const Item im = items[it];
+        const Item im = uniform_struct(items + it);
         const int32_t* table = a.table + im.table;
         const int kvh = im.kvh, n_pos = im.n_pos, R = im.rows;
         const int row_w0 = w % kRowWaves * 32;           // the wave's first row in the block
@@ -728,7 +779,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
             if (im.holes) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (table[min(p0 + 16 * i, n_pos - 1) >> a.shift] < 0) holes |= 1u << i;
+                    if (uniform_load(table + (min(p0 + 16 * i, n_pos - 1) >> a.shift)) < 0) holes |= 1u << i;
             }
             if (p0 + kP < end) {
                 fetch(p0 + kP);
@@ -766,7 +817,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
             for (int pb = 0; pb < NB; ++pb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[pb][i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            mx = max32(mx);
             const float ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
             if (__ballot(mx != m)) {
                 const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
@@ -887,9 +938,9 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
 {
     constexpr int D = HD / 64;
     const int group = a.H / a.G, lane = threadIdx.x & 63;
-    const int n_items = a.hdr->n_merge;
+    const int n_items = uniform_load(&a.hdr->n_merge);
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        const Merge mg = a.merge[it];
+        const Merge mg = uniform_struct(a.merge + it);
         const int stride = (mg.tile ? 128 : kFewRows) * (HD + kPartPad);
         for (int row = blockIdx.y * 4 + (threadIdx.x >> 6); row < mg.rows; row += gridDim.y * 4) {
             const float* base = (mg.tile ? a.tile_part : a.few_part) + (int64_t)mg.slot0 * stride + row * (HD + kPartPad);
