@@ -105,7 +105,7 @@ hipError_t attn_paged_launch_append(const paged::Args* a, const paged::Source* x
 hipError_t attn_paged_launch_few(const paged::Args* a, const uint16_t* q, uint16_t* out, int grid, hipStream_t s);
 hipError_t attn_paged_launch_tile(const paged::Args* a, const uint16_t* q, uint16_t* out, int kind, int grid,
                                   hipStream_t s);
-hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, hipStream_t s);
+hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, int slots, hipStream_t s);
 
 // The batch of a paged context as the attention block needs it.
 int32_t attn_paged_tokens(const attn_paged_ctx* ctx);

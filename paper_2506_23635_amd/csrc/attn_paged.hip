@@ -2,8 +2,8 @@
 // batch's keys and values with the rotation, and causal attention over pages.
 //
 //   unpack_kernel  a batch's arrays from pinned host memory to the workspace
-//   append_kernel  q rotated to bf16; bf16 pages: k rotated and v to their slots
-//   code_kernel    e4m3 pages: k rotated and v to their slots, the pages' scales
+//   append_kernel  q rotated to bf16, k rotated and v to their slots (of e4m3
+//                  pages the scales too)
 //   few_kernel     attention of up to 16 query rows per key/value head
 //   tile_kernel    attention of blocks of 128 or 64 query rows
 //   merge_kernel   adds the partial sums of rows whose positions were shared out
@@ -21,6 +21,10 @@ using moe::u32x4_t;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 
 __device__ inline u32x4_t ld16(const void* p) { return *reinterpret_cast<const u32x4_t*>(p); }
+
+typedef __attribute__((__vector_size__(2 * sizeof(uint32_t)))) uint32_t u32x2_t;
+__device__ inline u32x4_t ld16_nt(const void* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)); }
+__device__ inline u32x2_t ld8_nt(const void* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(p)); }
 
 __device__ inline f32x16_t mfma32x32x16(const u32x4_t a, const u32x4_t b, f32x16_t c)
 {
@@ -152,18 +156,17 @@ __device__ inline void turn_pair(float& a, float& b, float2 cs)
     b = y * cs.x + x * cs.y;
 }
 
-// q of every token (and with bf16 pages k and v): blockIdx.x is the token,
-// blockIdx.y a run of 256 pieces of it.  The token's rotations, one per
-// frequency, are formed once per workgroup.
+// q of a token t (and with bf16 pages its k and v): one workgroup per run of
+// 256 pieces.  The token's rotations, one per frequency, are formed once per
+// workgroup.
 template <bool kPacked>
-__global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t* __restrict__ q)
+__device__ __forceinline__ void append_rows(const Args& a, const Source& x, uint16_t* __restrict__ q, int t, int run)
 {
     __shared__ float2 s_cs[64];
-    const int t = blockIdx.x;
     const Token tok = a.tok[t];
     const int hd = a.hd, half = hd / 2, P = hd / 8;      // pieces per head
     if ((int)threadIdx.x < half) s_cs[threadIdx.x] = rotation(tok.pos, a.freq[threadIdx.x]);
-    const int e = blockIdx.y * 256 + threadIdx.x;
+    const int e = run * 256 + threadIdx.x;
     const int head = e / P, n_rotated = a.H + a.G;
     const bool live = head < (a.e4m3 ? a.H : a.H + 2 * a.G);
     const bool turn = head < n_rotated;
@@ -229,14 +232,14 @@ __device__ inline uint32_t recode4(uint32_t c, float ratio)
 constexpr int kHold = 4;
 
 template <bool kPacked>
-__global__ __launch_bounds__(256) void code_kernel(Args a, Source x)
+__device__ __forceinline__ void append_codes(const Args& a, const Source& x, int n_blocks)
 {
     __shared__ float s_max[4];
     const int G = a.G, hd = a.hd, P = hd / 8;
     const int per_pass = 256 / P;
     const int tj = threadIdx.x / P, pc = threadIdx.x % P;
     const int n_tasks = uniform_load(&a.hdr->n_pages) * G * 2;
-    for (int task = blockIdx.x; task < n_tasks; task += gridDim.x) {
+    for (int task = blockIdx.x; task < n_tasks; task += n_blocks) {
         const PageWork w = uniform_struct(a.pages + task / (2 * G));
         const int g = task / 2 % G;
         const bool turn = task % 2 == 0;
@@ -306,6 +309,17 @@ __global__ __launch_bounds__(256) void code_kernel(Args a, Source x)
     }
 }
 
+// The first n_code workgroups code pages (longer work first), the others take
+// the tokens' runs, n_runs each.
+template <bool kPacked>
+__global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t* __restrict__ q, int n_code,
+                                                     int n_runs)
+{
+    const int b = (int)blockIdx.x - n_code;
+    if (b < 0) append_codes<kPacked>(a, x, n_code);
+    else append_rows<kPacked>(a, x, q, b / n_runs, b % n_runs);
+}
+
 // ----------------------------------------------------------------- attend --
 
 // A maximum in base 2, with the product's one rounding everywhere: p, the
@@ -323,6 +337,35 @@ __device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, true)),
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, false)),
                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
+}
+
+// Four rows of 16 dims, 16-bit, transposed on their way from LDS: lane n of
+// each 16 supplies the address of dims 4 (n % 4) .. + 3 of row n / 4 and gets
+// dim n of the four rows.
+__device__ __forceinline__ uint2 transposed(const uint8_t* p)
+{
+    typedef short s16x4_t __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                         (__attribute__((address_space(3))) s16x4_t*)const_cast<uint8_t*>(p)));
+}
+
+// 16 bytes a lane from base + offset (below `bytes`, a wave's range) straight
+// to LDS, lane after lane from dst on.  In assembly, because after the
+// compiler's builtin the next LDS read, whatever it reads, waits for the load;
+// it writes no register, the caller waits for it (vmcnt) before the barrier
+// that hands the rows on, and the LDS address passed in tells the compiler
+// that the memory changes.  (m0 is the compiler's to use as well, but nothing
+// here makes it keep a value there.)
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t bytes, uint8_t* dst, int offset)
+{
+    const uint64_t b = (uint64_t)(uintptr_t)base;
+    // buffer descriptor: base, no stride, its size, raw dword data (gfx9 family)
+    const u32x4_t d = {(uint32_t)b, (uint32_t)(b >> 32) & 0xFFFFu, bytes, 0x00020000u};
+    const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)dst;
+    // (the pause: a scalar register that a vector instruction has just written)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(offset), "s"(d));
 }
 
 // of two bf16: bits all ones in the halves that are not finite
@@ -363,9 +406,12 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int group = a.H / a.G, P = 1 << a.shift;
+    // (the first share is read along with the count, not after it: the list
+    // has room for every workgroup of the grid)
+    Item im = uniform_struct(a.few + blockIdx.x);
     const int n_items = uniform_load(&a.hdr->n_few);
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        const Item im = uniform_struct(a.few + it);
+        if (it != (int)blockIdx.x) im = uniform_struct(a.few + it);
         const int32_t* table = a.table + im.table;
         const int R = im.rows, kvh = im.kvh, n_pos = im.n_pos;
         const bool row_ok = r < R;
@@ -407,7 +453,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
                 const int64_t row = (head << a.shift) + (pb & (P - 1)) + min(r, n_pos - 1 - pb);
                 const uint8_t* kb = a.k + row * (HD * ES) + g * 16;
 #pragma unroll
-                for (int c = 0; c < KW; ++c) kr[s][c] = ld16(kb + c * 64);
+                for (int c = 0; c < KW; ++c) kr[s][c] = ld16_nt(kb + c * 64);
                 if constexpr (kE4m3) ksc[s] = uniform_load(a.k_scale + head);
             }
         };
@@ -422,11 +468,11 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
                     const uint8_t* src = vb + min(4 * g + i, n_pos - 1 - pb) * (HD * ES);
                     uint32_t* dst = vr[s * 4 + i];
                     if constexpr (VW == 4) {
-                        const u32x4_t u = ld16(src);
+                        const u32x4_t u = ld16_nt(src);
                         dst[0] = u[0]; dst[1] = u[1]; dst[2] = u[2]; dst[3] = u[3];
                     } else if constexpr (VW == 2) {
-                        const uint2 u = *reinterpret_cast<const uint2*>(src);
-                        dst[0] = u.x; dst[1] = u.y;
+                        const u32x2_t u = ld8_nt(src);
+                        dst[0] = u[0]; dst[1] = u[1];
                     } else {
                         dst[0] = *reinterpret_cast<const uint32_t*>(src);
                     }
@@ -632,14 +678,28 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
 
 // tile_kernel: blocks of 128 or 64 query rows (kPG = 1 or 2 position groups:
 // the 4 / kPG waves of a group own 32 rows each) over one range of positions
-// in steps of 64, K rows and V transposed staged in LDS as bf16 (e4m3 codes
-// are decoded on the way).  v_mfma_f32_32x32x16_bf16: S^T = K Q^T leaves lane
-// (c, h) = (lane % 32, lane / 32) the scores of row c at positions 8 i + 4 h +
-// e of a 32-position block, which O^T += V^T P^T takes from the registers, V^T
-// being read in the same order.  P enters rounded to one bf16 (relative error
-// 2^-8 at most per weight, random in sign; the output's own rounding is as
-// large): a second term would cost half as many matrix instructions again.
+// in steps of 64, whose K and V rows are in LDS as bf16, two steps in turn, so
+// that one barrier a step is enough; the query rows stay in registers.
+// v_mfma_f32_32x32x16_bf16: S^T = K Q^T leaves lane (c, h) = (lane % 32,
+// lane / 32) the scores of row c at positions 8 i + 4 h + e of a 32-position
+// block, which O^T += V^T P^T takes from the registers, V^T being read in the
+// same order by transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read four
+// rows of 16 dims, and lane n ends with dim n of the four).
+//
+// Rows go through registers, a step ahead (e4m3 codes are decoded on the way).
+// (Straight from memory to LDS the compiler made every transposing read wait
+// for the next step's rows.)  A row's 16-byte chunks are swapped about by its
+// number, so that neither the 32 rows of a K read nor the 8 of a V read meet
+// in the same banks.
+//
+// P enters rounded to one bf16 (relative error 2^-8 at most per weight, random
+// in sign; the output's own rounding is as large): a second term would cost
+// half as many matrix instructions again.  The exponent's reference m only
+// follows the maximum when some score is more than 2^kLazy above it: the
+// weights are then at most 2^kLazy, which changes nothing in fp32 or bf16, and
+// most steps need no rescaling and no exchange between lanes.
 constexpr int tile_rows(int pg) { return 128 / pg; }
+constexpr float kLazy = 8.f;
 
 template <int HD, bool kE4m3, int kPG>
 __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __restrict__ items, int which,
@@ -651,25 +711,40 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     constexpr int kP = kStep;
     constexpr int NB = kP / 32 / kPG;        // 32-position blocks per wave and step
     constexpr int kRowWaves = 4 / kPG;       // waves on different rows
-    constexpr int KROW = HD + 8;             // padded K row in LDS (bf16)
-    constexpr int VROW = kP + 4;             // padded V^T row in LDS (bf16)
+    constexpr int RB = HD * 2;               // bytes of a row in LDS
     constexpr int ES = kE4m3 ? 1 : 2;
-    constexpr int kQBytes = tile_rows(kPG) * KROW * 2;
-    constexpr int kStageBytes = kP * KROW * 2 + HD * VROW * 2 + kQBytes;
+    constexpr int kHalf = kP * RB;           // K or V of a step
+    constexpr int kBuf = 2 * kHalf;
     constexpr int kMergeBytes = (4 - kRowWaves) * (DB * 16 + 2) * 64 * 4;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kStageBytes > kMergeBytes ? kStageBytes : kMergeBytes];
-    __shared__ uint32_t s_bad[2];
-    uint16_t* ks = reinterpret_cast<uint16_t*>(lds);
-    uint32_t* vt32 = reinterpret_cast<uint32_t*>(lds + kP * KROW * 2);
-    uint16_t* qs = reinterpret_cast<uint16_t*>(lds + kP * KROW * 2 + HD * VROW * 2);
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBuf > kMergeBytes ? 2 * kBuf : kMergeBytes];
+    __shared__ uint32_t s_bad;               // a value of V that is not finite, where it is masked for some rows
     const int group = a.H / a.G, P = 1 << a.shift;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, h = lane >> 5;
     const int pg = w / kRowWaves;                        // the wave's position group
+    Item im = uniform_struct(items + blockIdx.x);
     const int n_items = uniform_load(&a.hdr->n_tile[which]);
     const u32x4_t zero = {0u, 0u, 0u, 0u};
+    // chunk of row r is at chunk ^ k_key(r) of K, ^ v_key(r) of V (rows of 64
+    // dims: two share the 256 bytes of all banks)
+    auto k_key = [](int r) { return HD == 128 ? r & 15 : r >> 1 & 7; };
+    auto v_key = [](int r) { return HD == 128 ? (r & 7) * 2 : (r >> 1 & 3) * 2; };
+    const int k_off = (pg * NB * 32 + c) * RB + (h ^ k_key(c)) * 16;          // K step k: ^ k * 32
+    const int vrow = 4 * h + (c & 15) / 4;               // the lane's V row of 8
+    int v_off[DB];
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+        v_off[b] = kHalf + (pg * NB * 32 + vrow) * RB +
+                   ((b * 4 + c / 16 * 2 + (c >> 1 & 1)) ^ v_key(vrow)) * 16 + (c & 1) * 8;
+    constexpr int CL = HD * ES / 64;                     // 16-byte pieces of K per lane and step
+    constexpr int LR = 1024 / (HD * ES);                 // rows per 64 pieces
+    constexpr int PR = HD * ES / 16;                     // pieces per row
+    constexpr int DC = kE4m3 ? 2 : 1;                    // LDS chunks per piece
+    const int k_in = (lane % PR * DC ^ k_key(lane / PR)) * 16, v_in = (lane % PR * DC ^ v_key(lane / PR)) * 16;
+    u32x4_t kc[CL], vc[CL];                              // e4m3: the next step's codes
+    float ksc = 0.f, vsc = 0.f;
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        const Item im = uniform_struct(items + it);
+        if (it != (int)blockIdx.x) im = uniform_struct(items + it);
         const int32_t* table = a.table + im.table;
         const int kvh = im.kvh, n_pos = im.n_pos, R = im.rows;
         const int row_w0 = w % kRowWaves * 32;           // the wave's first row in the block
@@ -680,195 +755,216 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
         const int lim = im.pos0 + t;
         const int lim_w0 = im.pos0 + (im.row0 + row_w0) / group;
         const int lim_b0 = im.pos0 + im.row0 / group;    // last position of the block's first row
-        __syncthreads();                                 // the last item's LDS reads are done
-        const uint16_t* qw = qs + row * KROW + h * 8;
-        if (pg == 0) {
+        u32x4_t qf[KQ];
+        {
             const uint16_t* qrow = q + ((int64_t)(im.tok0 + t) * a.H + j) * HD + h * 8;
 #pragma unroll
             for (int k = 0; k < KQ; ++k) {
                 const u32x4_t v = ld16(qrow + k * 16);
-                *reinterpret_cast<u32x4_t*>(const_cast<uint16_t*>(qw) + k * 16) = row_ok ? v : zero;
+                qf[k] = row_ok ? v : zero;
             }
         }
-        if (threadIdx.x < 2) s_bad[threadIdx.x] = 0u;
         f32x16_t o[DB];
 #pragma unroll
         for (int b = 0; b < DB; ++b) o[b] = f32x16_t{};
-        float m = -INFINITY, l = 0.f;
-        constexpr int KL = kP * (HD / 8) / 256;          // K pieces of 8 dims per thread
-        constexpr int VL = (kP / 2) * (HD / 8) / 256;    // pairs of V pieces per thread
-        constexpr int RW = 2 * ES;                       // words of a piece
-        uint32_t kr[KL][RW], va[VL][RW], vb[VL][RW];
-        float kscale[KL], vscale;
-        int kpage[KL], vpage;                            // of the pieces fetched next
-        int kpage_now[KL], vpage_now;                    // of the pieces in registers
-        // rows past the sequence's end are the last row (masked for all)
-        const int kp0 = threadIdx.x / (HD / 8), k8k = threadIdx.x % (HD / 8);
-        const int vp0 = threadIdx.x % (kP / 2) * 2;
-        auto pages = [&](int p0) {
-#pragma unroll
-            for (int i = 0; i < KL; ++i) kpage[i] = table[min(p0 + kp0 + i * (2048 / HD), n_pos - 1) >> a.shift];
-            vpage = table[min(p0 + vp0, n_pos - 1) >> a.shift];
-        };
-        auto ld_piece = [&](const uint8_t* src, uint32_t (&dst)[RW]) {
+        float m = -INFINITY, ms = 0.f, thr = -INFINITY, l = 0.f;
+        // Wave w brings rows 16 w .. + 15 of the next step, which lie in one
+        // page.  Positions past the sequence's end are its last one (masked
+        // for every row); without a page they are zeros.
+        auto bring = [&](int p0, int to) {
+            const int pb = min(p0 + 16 * w, (n_pos - 1) & ~15), last = n_pos - 1 - pb;
+            const int page = uniform_load(table + (pb >> a.shift));
+            const int64_t head = (int64_t)max(page, 0) * a.G + kvh;
+            const int64_t at = ((head << a.shift) + (pb & (P - 1))) * (HD * ES);
             if constexpr (kE4m3) {
-                const uint2 v = *reinterpret_cast<const uint2*>(src);
-                dst[0] = v.x; dst[1] = v.y;
+                // into registers (`decode` takes them on); rows past the end
+                // and without a page: see above
+#pragma unroll
+                for (int i = 0; i < CL; ++i) {
+                    const int src = min(i * LR + lane / PR, last) * HD + lane % PR * 16;
+                    kc[i] = ld16(a.k + at + src);
+                    vc[i] = ld16(a.v + at + src);
+                }
+                ksc = uniform_load(a.k_scale + head);
+                vsc = uniform_load(a.v_scale + head);
+                if (page < 0) {
+#pragma unroll
+                    for (int i = 0; i < CL; ++i) kc[i] = vc[i] = zero;
+                }
             } else {
-                const u32x4_t v = ld16(src);
-                dst[0] = v[0]; dst[1] = v[1]; dst[2] = v[2]; dst[3] = v[3];
+                uint8_t* dst = lds + to + w * 16 * RB;
+                if (page < 0) {
+#pragma unroll
+                    for (int i = 0; i < CL; ++i) {
+                        *reinterpret_cast<u32x4_t*>(dst + i * 1024 + lane * 16) = zero;
+                        *reinterpret_cast<u32x4_t*>(dst + kHalf + i * 1024 + lane * 16) = zero;
+                    }
+                    return;
+                }
+#pragma unroll
+                for (int i = 0; i < CL; ++i) {
+                    const int r = min(i * LR + lane / PR, last) * RB;
+                    load_to_lds(a.k + at, 16 * RB, dst + i * 1024, r + (k_in ^ k_key(i * LR) * 16));
+                    load_to_lds(a.v + at, 16 * RB, dst + kHalf + i * 1024, r + (v_in ^ v_key(i * LR) * 16));
+                }
             }
         };
-        auto fetch = [&](int p0) {
+        // piece i of the lane: row i LR + lane / PR, whose key is that of
+        // lane / PR ^ that of i LR
+        auto decode = [&](int to) {
 #pragma unroll
-            for (int i = 0; i < KL; ++i) {
-                const int p = min(p0 + kp0 + i * (2048 / HD), n_pos - 1);
-                const int64_t head = (int64_t)max(kpage[i], 0) * a.G + kvh;
-                ld_piece(a.k + ((head << a.shift) + (p & (P - 1))) * (HD * ES) + k8k * 8 * ES, kr[i]);
-                if constexpr (kE4m3) kscale[i] = a.k_scale[head];
-                kpage_now[i] = kpage[i];
+            for (int i = 0; i < CL; ++i) {
+                uint8_t* dst = lds + to + (w * 16 + i * LR + lane / PR) * RB;
+                const int ko = k_in ^ k_key(i * LR) * 16, vo = v_in ^ v_key(i * LR) * 16;
+                *reinterpret_cast<u32x4_t*>(dst + ko) = decode8(kc[i][0], kc[i][1], ksc);
+                *reinterpret_cast<u32x4_t*>(dst + (ko ^ 16)) = decode8(kc[i][2], kc[i][3], ksc);
+                *reinterpret_cast<u32x4_t*>(dst + kHalf + vo) = decode8(vc[i][0], vc[i][1], vsc);
+                *reinterpret_cast<u32x4_t*>(dst + kHalf + (vo ^ 16)) = decode8(vc[i][2], vc[i][3], vsc);
             }
-            const int64_t head = (int64_t)max(vpage, 0) * a.G + kvh;
-            const int pa = min(p0 + vp0, n_pos - 1), pb = min(p0 + vp0 + 1, n_pos - 1);
-            if constexpr (kE4m3) vscale = a.v_scale[head];
-            vpage_now = vpage;
-#pragma unroll
-            for (int i = 0; i < VL; ++i) {
-                const int k8 = threadIdx.x / (kP / 2) + i * (512 / kP);
-                // an even position and the next one share a page of 16 or more
-                ld_piece(a.v + ((head << a.shift) + (pa & (P - 1))) * (HD * ES) + k8 * 8 * ES, va[i]);
-                ld_piece(a.v + ((head << a.shift) + (pb & (P - 1))) * (HD * ES) + k8 * 8 * ES, vb[i]);
-            }
-        };
-        auto piece = [&](const uint32_t (&src)[RW], float scale, bool mapped) {
-            u32x4_t v;
-            if constexpr (kE4m3) v = decode8(src[0], src[1], scale);
-            else v = u32x4_t{src[0], src[1], src[2], src[3]};
-            return mapped ? v : zero;
         };
         const int first = im.begin, end = im.end;
+        // a step that some row of the block does not see whole
+        auto partly_seen = [&](int p0) { return p0 + kP - 1 > lim_b0 || im.holes; };
+        __syncthreads();                                 // the last item's LDS reads are done
+        if (threadIdx.x == 0) s_bad = 0u;
+        __syncthreads();
         if (first < end) {
-            pages(first);
-            fetch(first);
-            pages(first + kP);
-        }
-        for (int p0 = first; p0 < end; p0 += kP) {
-            const bool block_masked = p0 + kP - 1 > lim_b0;
-            lds_barrier();                               // the last step's LDS reads are done
-            const int parity = (p0 - first) / kP & 1;
-#pragma unroll
-            for (int i = 0; i < KL; ++i)
-                *reinterpret_cast<u32x4_t*>(&ks[(kp0 + i * (2048 / HD)) * KROW + k8k * 8]) =
-                    piece(kr[i], kE4m3 ? kscale[i] : 0.f, kpage_now[i] >= 0);
-            uint32_t bad = 0u;
-#pragma unroll
-            for (int i = 0; i < VL; ++i) {
-                const int pp = threadIdx.x % (kP / 2), k8 = threadIdx.x / (kP / 2) + i * (512 / kP);
-                const u32x4_t xa = piece(va[i], kE4m3 ? vscale : 0.f, vpage_now >= 0);
-                const u32x4_t xb = piece(vb[i], kE4m3 ? vscale : 0.f, vpage_now >= 0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    vt32[((k8 * 8 + 2 * e) * VROW) / 2 + pp] = __builtin_amdgcn_perm(xb[e], xa[e], 0x05040100u);
-                    vt32[((k8 * 8 + 2 * e + 1) * VROW) / 2 + pp] = __builtin_amdgcn_perm(xb[e], xa[e], 0x07060302u);
-                    if (block_masked) bad |= bad_halves(xa[e]) | bad_halves(xb[e]);
-                }
+            bring(first, 0);
+            if constexpr (kE4m3) {
+                decode(0);
+                if (first + kP < end) bring(first + kP, 0);
             }
-            if (block_masked && bad) s_bad[parity] = 1u;
-            if (threadIdx.x == 0) s_bad[parity ^ 1] = 0u;
-            uint32_t holes = 0u;                         // runs of 16 positions without a page
-            if (im.holes) {
+        }
+        // The step's start, the same for every wave: its rows have arrived
+        // from every wave, every wave is done with the last step's, and the
+        // next one's are on their way.  Of a step that is only partly seen,
+        // values of V that are not finite are taken out (0 times one would
+        // still reach the rows that do not see it).
+        auto begin_step = [&](int p0, int buf) {
+            __builtin_amdgcn_s_waitcnt(kE4m3 ? 0xC07F : 0x0070);   // lgkmcnt 0, and vmcnt 0 where LDS is loaded
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (partly_seen(p0)) {
+                uint32_t bad = 0u;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (uniform_load(table + (min(p0 + 16 * i, n_pos - 1) >> a.shift)) < 0) holes |= 1u << i;
+                for (int i = 0; i < 16 * RB / 1024; ++i) {
+                    u32x4_t* d = reinterpret_cast<u32x4_t*>(lds + buf + kHalf + w * 16 * RB + i * 1024 + lane * 16);
+                    u32x4_t v = *d;
+                    uint32_t any = 0u;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t x = bad_halves(v[k]);
+                        any |= x;
+                        v[k] &= ~x;
+                    }
+                    if (any) *d = v;
+                    bad |= any;
+                }
+                if (bad) s_bad = 1u;
+                lds_barrier();
             }
             if (p0 + kP < end) {
-                fetch(p0 + kP);
-                pages(p0 + 2 * kP);
-            }
-            lds_barrier();
-            const bool any_bad = s_bad[parity] != 0u;
-            if (!wave_ok) continue;
-            f32x16_t sc[NB];
-#pragma unroll
-            for (int pb = 0; pb < NB; ++pb) sc[pb] = f32x16_t{};
-#pragma unroll
-            for (int k = 0; k < KQ; ++k) {
-                const u32x4_t qf = *reinterpret_cast<const u32x4_t*>(qw + k * 16);
-#pragma unroll
-                for (int pb = 0; pb < NB; ++pb) {
-                    const u32x4_t kf = *reinterpret_cast<const u32x4_t*>(
-                        &ks[((pg * NB + pb) * 32 + c) * KROW + k * 16 + h * 8]);
-                    sc[pb] = mfma32x32x16(kf, qf, sc[pb]);
+                if constexpr (kE4m3) {
+                    decode(buf ^ kBuf);
+                    if (p0 + 2 * kP < end) bring(p0 + 2 * kP, 0);
+                } else {
+                    bring(p0 + kP, buf ^ kBuf);
                 }
             }
-            const int pw0 = p0 + pg * NB * 32;           // the wave's first position
-            float mx = m;
-            const bool masked = pw0 + NB * 32 - 1 > lim_w0 || holes;
-            if (masked) {
+        };
+        int buf = 0;
+        if (!wave_ok) {                                  // no rows: this wave only brings its share
+            for (int p0 = first; p0 < end; p0 += kP, buf ^= kBuf) begin_step(p0, buf);
+        } else {
+            for (int p0 = first; p0 < end; p0 += kP, buf ^= kBuf) {
+                begin_step(p0, buf);
+                const uint8_t* kb = lds + buf;
+                f32x16_t sc[NB];
+#pragma unroll
+                for (int pb = 0; pb < NB; ++pb) sc[pb] = f32x16_t{};
+#pragma unroll
+                for (int k = 0; k < KQ; ++k)
+#pragma unroll
+                    for (int pb = 0; pb < NB; ++pb)
+                        sc[pb] = mfma32x32x16(*reinterpret_cast<const u32x4_t*>(kb + (k_off ^ (k * 32)) + pb * 32 * RB), qf[k], sc[pb]);
+                const int pw0 = p0 + pg * NB * 32;       // the wave's first position
+                if (pw0 + NB * 32 - 1 > lim_w0 || im.holes) {
+                    uint32_t holes = 0u;                 // runs of 16 positions without a page
+                    if (im.holes) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (uniform_load(table + (min(p0 + 16 * i, n_pos - 1) >> a.shift)) < 0) holes |= 1u << i;
+                    }
+#pragma unroll
+                    for (int pb = 0; pb < NB; ++pb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int at = pb * 32 + 8 * (i / 4) + 4 * h + i % 4;
+                            if (pw0 + at > lim || (holes >> ((pg * NB * 32 + at) / 16) & 1u)) sc[pb][i] = -INFINITY;
+                        }
+                }
+                float mx = -INFINITY;
 #pragma unroll
                 for (int pb = 0; pb < NB; ++pb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int at = pb * 32 + 8 * (i / 4) + 4 * h + (i % 4);
-                        if (pw0 + at > lim || (holes >> ((pg * NB * 32 + at) / 16) & 1u)) sc[pb][i] = -INFINITY;
-                    }
-            }
+                    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[pb][i]);
+                if (__ballot(mx > thr)) {
+                    mx = fmaxf(m, max32(mx));
+                    const float mn = mx == -INFINITY ? 0.f : base2(mx, scale2);
+                    const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - mn);
+                    l *= alpha;
 #pragma unroll
-            for (int pb = 0; pb < NB; ++pb)
+                    for (int b = 0; b < DB; ++b) o[b] *= alpha;
+                    m = mx;
+                    ms = mn;
+                    thr = mx + kLazy / scale2;
+                }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[pb][i]);
-            mx = max32(mx);
-            const float ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
-            if (__ballot(mx != m)) {
-                const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
-                l *= alpha;
+                for (int pb = 0; pb < NB; ++pb)
 #pragma unroll
-                for (int b = 0; b < DB; ++b) o[b] *= alpha;
-                m = mx;
-            }
-#pragma unroll
-            for (int pb = 0; pb < NB; ++pb)
-#pragma unroll
-                for (int sx = 0; sx < 2; ++sx) {
-                    u32x4_t bt, seen;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float s0 = sc[pb][sx * 8 + 2 * i], s1 = sc[pb][sx * 8 + 2 * i + 1];
-                        const float pa = __builtin_amdgcn_exp2f(fmaf(s0, scale2, -ms));
-                        const float pb2 = __builtin_amdgcn_exp2f(fmaf(s1, scale2, -ms));
-                        l += pa + pb2;
-                        bt[i] = moe::cvt_pk_bf16(pa, pb2);
-                        seen[i] = (s0 == -INFINITY ? 0u : kOnes & 0xFFFFu) | (s1 == -INFINITY ? 0u : kOnes & 0xFFFF0000u);
-                    }
-                    u32x4_t av[DB];
-#pragma unroll
-                    for (int b = 0; b < DB; ++b) {
-                        const uint32_t* vr = vt32 + ((b * 32 + c) * VROW + (pg * NB + pb) * 32 + sx * 16 + 4 * h) / 2;
-                        const uint2 v0 = *reinterpret_cast<const uint2*>(vr);
-                        const uint2 v1 = *reinterpret_cast<const uint2*>(vr + 4);
-                        av[b] = u32x4_t{v0.x, v0.y, v1.x, v1.y};
-                    }
-                    if (any_bad) {
-                        // as in few_kernel: values that are not finite are
-                        // taken out, and rows that see them get a NaN
+                    for (int sx = 0; sx < 2; ++sx) {
+                        u32x4_t av[DB];
 #pragma unroll
                         for (int b = 0; b < DB; ++b) {
-                            u32x4_t ind;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t x = bad_halves(av[b][i]);
-                                ind[i] = x & kOnes;
-                                av[b][i] &= ~x;
-                            }
-                            const f32x16_t n = mfma32x32x16(ind, seen, f32x16_t{});
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (n[e] > 0.f) o[b][e] = NAN;
+                            const uint8_t* p = kb + v_off[b] + (pb * 32 + sx * 16) * RB;
+                            const uint2 v0 = transposed(p), v1 = transposed(p + 8 * RB);
+                            av[b] = u32x4_t{v0.x, v0.y, v1.x, v1.y};
                         }
-                    }
+                        u32x4_t bt;
 #pragma unroll
-                    for (int b = 0; b < DB; ++b) o[b] = mfma32x32x16(av[b], bt, o[b]);
+                        for (int i = 0; i < 4; ++i) {
+                            const float pa = __builtin_amdgcn_exp2f(fmaf(sc[pb][sx * 8 + 2 * i], scale2, -ms));
+                            const float pb2 = __builtin_amdgcn_exp2f(fmaf(sc[pb][sx * 8 + 2 * i + 1], scale2, -ms));
+                            l += pa + pb2;
+                            bt[i] = moe::cvt_pk_bf16(pa, pb2);
+                        }
+#pragma unroll
+                        for (int b = 0; b < DB; ++b) o[b] = mfma32x32x16(av[b], bt, o[b]);
+                    }
+            }
+        }
+        __syncthreads();
+        if (s_bad) {
+            // the rows that see a value that was taken out get a NaN in its dim
+            for (int p0 = first; p0 < end; p0 += kP) {
+                if (!partly_seen(p0)) continue;
+                for (int p = p0; p < min(p0 + kP, end); ++p) {
+                    const int pgv = uniform_load(table + (p >> a.shift));
+                    if (pgv < 0) continue;
+                    const uint8_t* vrow = a.v + ((((int64_t)pgv * a.G + kvh) << a.shift) + (p & (P - 1))) * (HD * ES);
+#pragma unroll
+                    for (int b = 0; b < DB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int d = b * 32 + 8 * (i / 4) + 4 * h + i % 4;
+                            bool bad;
+                            if constexpr (kE4m3) bad = (vrow[d] & 0x7F) == 0x7F;
+                            else bad = (reinterpret_cast<const uint16_t*>(vrow)[d] & 0x7F80) == 0x7F80;
+                            if (bad && p <= lim) o[b][i] = NAN;
+                        }
                 }
+            }
         }
         l += __shfl_xor(l, 32, 64);
         if constexpr (kPG > 1) {
@@ -931,44 +1027,97 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     }
 }
 
-// merge_kernel: one wave per row, lane i taking dims i HD/64 ..; the partial
-// sums of the row's slots are added in slot order, weighted by their maxima.
+// merge_kernel: the partial sums of a row's slots, weighted by their maxima,
+// added in slot order.  Up to kWaveSlots slots a wave takes a row (lane s the
+// maximum and weight of slot s, then every lane its dims of all slots); more,
+// a workgroup does, wave w adding slots w, w + 4, ..., the waves' sums in wave
+// order.  A slot without weight holds zeros.
+constexpr int kWaveSlots = 16;
+constexpr int kMaxSlots = 4096;
+
 template <int HD>
 __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict__ out)
 {
     constexpr int D = HD / 64;
-    const int group = a.H / a.G, lane = threadIdx.x & 63;
+    __shared__ float s_f[kMaxSlots], s_red[2][4], s_sum[4][HD];
+    const int group = a.H / a.G, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n_items = uniform_load(&a.hdr->n_merge);
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
         const Merge mg = uniform_struct(a.merge + it);
-        const int stride = (mg.tile ? 128 : kFewRows) * (HD + kPartPad);
-        for (int row = blockIdx.y * 4 + (threadIdx.x >> 6); row < mg.rows; row += gridDim.y * 4) {
-            const float* base = (mg.tile ? a.tile_part : a.few_part) + (int64_t)mg.slot0 * stride + row * (HD + kPartPad);
-            float M = -INFINITY;
-            for (int s = lane; s < mg.n; s += 64) M = fmaxf(M, base[(int64_t)s * stride + HD]);
-            for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-            float L = 0.f, acc[D];
-#pragma unroll
-            for (int e = 0; e < D; ++e) acc[e] = 0.f;
-            if (M != -INFINITY) {
-#pragma unroll 4
-                for (int s = 0; s < mg.n; ++s) {
-                    const float* pc = base + (int64_t)s * stride;
-                    const float mk = pc[HD];
-                    if (mk == -INFINITY) continue;
-                    const float f = __builtin_amdgcn_exp2f(mk - M);
-                    L = fmaf(pc[HD + 1], f, L);
-#pragma unroll
-                    for (int e = 0; e < D; ++e) acc[e] = fmaf(pc[lane * D + e], f, acc[e]);
-                }
+        const int n = mg.n, stride = (mg.tile ? 128 : kFewRows) * (HD + kPartPad);
+        const float* base = (mg.tile ? a.tile_part : a.few_part) + (int64_t)mg.slot0 * stride;
+        auto add = [&](const float* row, int s, float f, float (&acc)[D]) {
+            const float* pc = row + (int64_t)s * stride + lane * D;
+            if constexpr (D == 2) {
+                const float2 v = *reinterpret_cast<const float2*>(pc);
+                acc[0] = fmaf(v.x, f, acc[0]);
+                acc[1] = fmaf(v.y, f, acc[1]);
+            } else {
+                acc[0] = fmaf(pc[0], f, acc[0]);
             }
-            const float inv = M == -INFINITY ? 0.f : 1.0f / L;
+        };
+        auto write = [&](int row, const float (&acc)[D], float L) {
+            const float inv = L > 0.f || L != L ? 1.0f / L : 0.f;      // no weight at all: zeros
             const int gr = mg.row0 + row, t = gr / group, j = mg.kvh * group + gr % group;
             uint16_t* dst = out + ((int64_t)(mg.tok0 + t) * a.H + j) * HD + lane * D;
-            if constexpr (D == 2)
-                *reinterpret_cast<uint32_t*>(dst) = moe::cvt_pk_bf16(acc[0] * inv, acc[1] * inv);
-            else
-                dst[0] = moe::f32_to_bf16(acc[0] * inv);
+            if constexpr (D == 2) *reinterpret_cast<uint32_t*>(dst) = moe::cvt_pk_bf16(acc[0] * inv, acc[1] * inv);
+            else dst[0] = moe::f32_to_bf16(acc[0] * inv);
+        };
+        if (n <= kWaveSlots) {
+            for (int row = blockIdx.y * 4 + w; row < mg.rows; row += gridDim.y * 4) {
+                const float* pr = base + row * (HD + kPartPad);
+                float2 ml = make_float2(-INFINITY, 0.f);
+                if (lane < n) ml = *reinterpret_cast<const float2*>(pr + (int64_t)lane * stride + HD);
+                float M = ml.x;
+                for (int off = kWaveSlots / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+                const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+                float L = ml.y * f;
+                for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
+                L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
+                float acc[D] = {};
+#pragma unroll
+                for (int s = 0; s < kWaveSlots; ++s)                   // (past n: slot 0 with factor 0)
+                    add(pr, s < n ? s : 0, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s)), acc);
+                write(row, acc, L);
+            }
+            continue;
+        }
+        for (int row = blockIdx.y; row < mg.rows; row += gridDim.y) {
+            const float* pr = base + row * (HD + kPartPad);
+            float M = -INFINITY, L = 0.f;
+            for (int s = threadIdx.x; s < n; s += 256) M = fmaxf(M, pr[(int64_t)s * stride + HD]);
+            for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+            if (lane == 0) s_red[0][w] = M;
+            __syncthreads();
+            M = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+            for (int s = threadIdx.x; s < n; s += 256) {
+                const float2 ml = *reinterpret_cast<const float2*>(pr + (int64_t)s * stride + HD);
+                const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+                s_f[s] = f;
+                L = fmaf(ml.y, f, L);
+            }
+            for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
+            if (lane == 0) s_red[1][w] = L;
+            __syncthreads();
+            L = ((s_red[1][0] + s_red[1][1]) + s_red[1][2]) + s_red[1][3];
+            float acc[D] = {};
+            int s = w;
+            for (; s + 28 < n; s += 32)
+#pragma unroll
+                for (int u = 0; u < 8; ++u) add(pr, s + 4 * u, s_f[s + 4 * u], acc);
+            for (; s < n; s += 4) add(pr, s, s_f[s], acc);
+#pragma unroll
+            for (int e = 0; e < D; ++e) s_sum[w][lane * D + e] = acc[e];
+            __syncthreads();
+            if (w == 0) {
+#pragma unroll
+                for (int e = 0; e < D; ++e) {
+                    const int d = lane * D + e;
+                    acc[e] = ((s_sum[0][d] + s_sum[1][d]) + s_sum[2][d]) + s_sum[3][d];
+                }
+                write(row, acc, L);
+            }
+            __syncthreads();                             // the LDS sums are written again
         }
     }
 }
@@ -989,15 +1138,11 @@ hipError_t attn_paged_launch_unpack(const paged::Unpack* u, hipStream_t s)
 hipError_t attn_paged_launch_append(const paged::Args* a, const paged::Source* x, uint16_t* q, int T,
                                     int n_pages, hipStream_t s)
 {
-    const int pieces = (a->e4m3 ? a->H : a->H + 2 * a->G) * a->hd / 8;
-    const dim3 grid(T, (pieces + 255) / 256);
-    if (x->packed) hipLaunchKernelGGL(paged::append_kernel<true>, grid, dim3(256), 0, s, *a, *x, q);
-    else hipLaunchKernelGGL(paged::append_kernel<false>, grid, dim3(256), 0, s, *a, *x, q);
-    if (a->e4m3) {
-        const dim3 tasks(n_pages * a->G * 2);
-        if (x->packed) hipLaunchKernelGGL(paged::code_kernel<true>, tasks, dim3(256), 0, s, *a, *x);
-        else hipLaunchKernelGGL(paged::code_kernel<false>, tasks, dim3(256), 0, s, *a, *x);
-    }
+    const int pieces = (a->e4m3 ? a->H : a->H + 2 * a->G) * a->hd / 8, runs = (pieces + 255) / 256;
+    const int codes = a->e4m3 ? n_pages * a->G * 2 : 0;
+    const dim3 grid(codes + T * runs);
+    if (x->packed) hipLaunchKernelGGL(paged::append_kernel<true>, grid, dim3(256), 0, s, *a, *x, q, codes, runs);
+    else hipLaunchKernelGGL(paged::append_kernel<false>, grid, dim3(256), 0, s, *a, *x, q, codes, runs);
     return hipGetLastError();
 }
 
@@ -1033,9 +1178,11 @@ hipError_t attn_paged_launch_tile(const paged::Args* a, const uint16_t* q, uint1
     return hipGetLastError();
 }
 
-hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, hipStream_t s)
+hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, int slots, hipStream_t s)
 {
-    const dim3 g(grid, (rows + 3) / 4);
+    // (a workgroup takes four rows, or one where some row has many slots)
+    const bool few = slots <= paged::kWaveSlots;
+    const dim3 g(grid, few ? (rows + 3) / 4 : rows);
     if (a->hd == 128) hipLaunchKernelGGL(paged::merge_kernel<128>, g, dim3(256), 0, s, *a, out);
     else hipLaunchKernelGGL(paged::merge_kernel<64>, g, dim3(256), 0, s, *a, out);
     return hipGetLastError();

@@ -7,7 +7,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
+#include <queue>
 #include <string>
 #include <utility>
 #include <vector>
@@ -22,8 +24,9 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kStages = 4;             // batches on their way to the device at once
 constexpr int kXcds = 8;
-constexpr int64_t kFewItems = 2048;    // at most about so many shares of few_kernel ...
-constexpr int64_t kTileItems = 512;    // ... and of tile_kernel come from dividing positions
+constexpr int64_t kFewItems = 1024;    // at most about so many shares of few_kernel ...
+constexpr int64_t kTileItems = 768;    // ... and half as many of tile_kernel, come from dividing positions
+constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -70,7 +73,7 @@ Layout make_layout(const attn_paged_config* c)
     // (a range is at least half as long as the common length).
     const size_t S = c->max_seqs, T = c->max_tokens, rows = T * group;
     const size_t few_seqs = std::min(S, T), tile_seqs = std::min(S, rows / (paged::kFewRows + 1) + 1);
-    L.max_few = few_seqs * G + 2 * kFewItems;
+    L.max_few = few_seqs * G + 2 * kFewItems;            // at least kGraphGrid, as below
     // (no more ranges than steps)
     const size_t few_steps = few_seqs * G * (((size_t)c->max_blocks * c->page_size + 127) / 128);
     L.few_slots = std::min<size_t>(2 * kFewItems, few_steps);
@@ -112,7 +115,7 @@ struct Batch {
     std::vector<Item> few, tile[2];
     std::vector<Merge> merge;
     std::vector<int32_t> table;
-    int merge_rows = 0;
+    int merge_rows = 0, merge_slots = 0;   // most of one entry
 };
 
 }  // namespace
@@ -125,7 +128,7 @@ struct attn_paged_ctx {
     std::vector<int32_t> written;      // per page: the call that last had it written, for set_batch
     int32_t call;
     bool set;
-    int32_t T, n_pages, n_few, n_tile[2], n_merge, merge_rows;
+    int32_t T, n_pages, n_few, n_tile[2], n_merge, merge_rows, merge_slots;
     Stage stage[kStages];
     int next_stage;
     std::string err;
@@ -166,10 +169,54 @@ void ranges(std::vector<Item>& out, Item it, int n, int step, int& slot)
     }
 }
 
-// The common length of a range: `total` steps in about `aim` shares.
-int64_t range_steps(int64_t total, int64_t aim, int64_t least)
+// A row block of tile_kernel: the steps of 64 positions that it needs.
+struct Block {
+    int steps, rows;
+};
+
+// The length of the ranges, in steps, that the row blocks' positions are
+// divided into: the least estimated time over the division of the longest
+// block into 1 .. kMostRanges ranges (a block of `steps` steps has
+// ceil(steps / length) of them).  The workgroups are handed out longest first,
+// two per CU; that is played through for one key/value head and its share of
+// the places.  Measured on 128 x 64 steps at head_dim 128: a step 2.2 us, where
+// a CU has one workgroup 1.6; about one and a half more per workgroup; the
+// partial sums written and read at about 4.5 TB/s, the merge's launch 4 us.
+int range_steps(const std::vector<Block>& blocks, int G)
 {
-    return std::max(least, (total + aim - 1) / aim);
+    constexpr int kPlaces = 512, kCus = 256, kMostRanges = 16;
+    int longest = 0;
+    for (const Block& b : blocks) longest = std::max(longest, b.steps);
+    const int places = std::max(1, kPlaces / G);
+    int best = std::max(1, longest);
+    double best_us = 0.0;
+    std::vector<double> items;
+    for (int n = 1; n <= kMostRanges && n <= longest; ++n) {
+        const int len = (longest + n - 1) / n;
+        items.clear();
+        int64_t slots = 0, rows = 0;
+        for (const Block& b : blocks) {
+            const int k = (b.steps + len - 1) / len;
+            for (int i = 0; i < k; ++i) items.push_back((b.steps + k - 1) / k + 1.5);
+            if (k > 1) { slots += k; rows += (int64_t)k * b.rows; }
+        }
+        if (slots * G > 2 * kTileItems) break;
+        std::sort(items.begin(), items.end(), std::greater<double>());
+        std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
+        double end = 0.0;
+        for (double it : items) {
+            if ((int)busy.size() == places) {
+                it += busy.top();
+                busy.pop();
+            }
+            busy.push(it);
+            end = std::max(end, it);
+        }
+        double us = end * ((int64_t)items.size() * G <= kCus ? 1.6 : 2.2);
+        if (slots) us += 4.0 + (double)rows * G * 132 * 4 * 2 / 4.5e6;
+        if (n == 1 || us < 0.97 * best_us) { best = len; best_us = us; }
+    }
+    return best;
 }
 
 // Longest shares first: the workgroups are handed out in order.
@@ -220,19 +267,23 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
     auto blocks_of = [&](int s) { return (int)(((int64_t)pos0[s] + n_new[s] + c.page_size - 1) >> L.shift); };
     // few rows: every wave takes steps of 32 positions, a workgroup 128
     constexpr int kFewStep = 4 * paged::kTile;
-    int64_t few_total = 0, tile_total = 0;
+    int64_t few_total = 0;
+    std::vector<Block> blocks;                           // of one key/value head
     for (int s = 0; s < n_seqs; ++s) {
         const int64_t R = (int64_t)n_new[s] * group, n_pos = (int64_t)pos0[s] + n_new[s];
         if (R == 0) continue;
         if (R <= paged::kFewRows) {
             few_total += (n_pos + kFewStep - 1) / kFewStep * G;
-        } else {
-            const int rows = R <= 64 ? 64 : 128;
-            for (int64_t r0 = 0; r0 < R; r0 += rows)
-                tile_total += (pos0[s] + (std::min(r0 + rows, R) - 1) / group + paged::kStep) / paged::kStep * G;
+            continue;
+        }
+        const int rows = R <= 64 ? 64 : 128;
+        for (int64_t r0 = 0; r0 < R; r0 += rows) {
+            const int64_t last = std::min(r0 + rows, R);
+            blocks.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0)});
         }
     }
-    const int64_t few_len = range_steps(few_total, kFewItems, 1), tile_len = range_steps(tile_total, kTileItems, 4);
+    const int64_t few_len = std::max<int64_t>(1, (few_total + kFewItems - 1) / kFewItems);
+    const int tile_len = range_steps(blocks, G);
     int few_slot = 0, tile_slot = 0, tok0 = 0, table = 0;
     for (int s = 0; s < n_seqs; ++s) {
         const int R = n_new[s] * group, n_pos = pos0[s] + n_new[s];
@@ -251,6 +302,7 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
                 if (n > 1) {
                     b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, 0, 0});
                     b.merge_rows = std::max(b.merge_rows, R);
+                    b.merge_slots = std::max(b.merge_slots, n);
                 }
                 ranges(b.few, it, n, kFewStep, few_slot);
             }
@@ -267,6 +319,7 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
                     if (n > 1) {
                         b.merge.push_back(Merge{tok0, r0, it.rows, it.kvh, tile_slot, n, 1, 0});
                         b.merge_rows = std::max(b.merge_rows, (int)it.rows);
+                        b.merge_slots = std::max(b.merge_slots, n);
                     }
                     ranges(b.tile[kind], it, n, paged::kStep, tile_slot);
                 }
@@ -441,6 +494,7 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
     for (int k = 0; k < 2; ++k) ctx->n_tile[k] = (int32_t)b.tile[k].size();
     ctx->n_merge = (int32_t)b.merge.size();
     ctx->merge_rows = b.merge_rows;
+    ctx->merge_slots = b.merge_slots;
     ctx->set = true;
     return MOE_OK;
 }
@@ -467,14 +521,15 @@ hipError_t attn_paged_run_attend(attn_paged_ctx* ctx, int32_t layer, const uint1
     // a graph may replay on a longer batch: its launches have room for the
     // shares that one may have, and the merge is there
     const bool graph = capturing(s);
-    auto grid = [&](int n) { return graph ? std::max(n, 512) : n; };
+    auto grid = [&](int n) { return graph ? std::max(n, kGraphGrid) : n; };
     hipError_t e = hipSuccess;
     for (int k = 0; k < 2 && e == hipSuccess; ++k)
         if (ctx->n_tile[k]) e = attn_paged_launch_tile(&a, q, out, k, grid(ctx->n_tile[k]), s);
     if (e == hipSuccess && ctx->n_few) e = attn_paged_launch_few(&a, q, out, grid(ctx->n_few), s);
     if (e == hipSuccess && (ctx->n_merge || graph))
         e = attn_paged_launch_merge(&a, out, graph ? std::max(ctx->n_merge, 64) : ctx->n_merge,
-                                    std::max(ctx->merge_rows, graph ? paged::kFewRows : 1), s);
+                                    std::max(ctx->merge_rows, graph ? paged::kFewRows : 1),
+                                    graph ? INT32_MAX : ctx->merge_slots, s);
     return e;
 }
 
