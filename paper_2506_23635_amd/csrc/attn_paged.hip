@@ -91,19 +91,34 @@ __global__ __launch_bounds__(256) void unpack_kernel(Unpack u)
 
 // ----------------------------------------------------------------- append --
 
-// cos and sin of pos * inv_freq, the angle formed and reduced modulo 2 pi in
-// fp64 (2 pi in two parts, Cody and Waite): sincosf sees [-pi, pi] only
+// cos and sin of pos * inv_freq.  The angle is formed and reduced to the
+// nearest multiple k of pi / 2 in fp64 (pi / 2 in two parts; k below 2^25);
+// what is left, r in [-pi / 4, pi / 4], goes through the Taylor series to r^9
+// and r^10 in fp32, which leave out less than 2^-28 and 2^-33: the result is
+// within 2 ulp of fp32.  (With the library's sincosf, and the new values held
+// in registers between the scale and the codes, pieces of six prompts of 200 to
+// 900 tokens took 24.3 us into e4m3 pages; so they take 17.7.)
 __device__ inline float2 rotation(int pos, double inv_freq)
 {
-    constexpr double kTwoPiHi = 6.28318530717958623200e+00;   // 2 pi rounded to fp64
-    constexpr double kTwoPiLo = 2.44929359829470635445e-16;   // 2 pi - kTwoPiHi
-    constexpr double kInvTwoPi = 1.59154943091895335769e-01;
+    constexpr double kHalfPiHi = 1.57079632679489655800e+00;   // pi / 2 rounded to fp64
+    constexpr double kHalfPiLo = 6.12323399573676603587e-17;   // pi / 2 - kHalfPiHi
+    constexpr double kInvHalfPi = 6.36619772367581382433e-01;
     const double ang = (double)pos * inv_freq;
-    const double k = rint(ang * kInvTwoPi);
-    const double r = fma(-k, kTwoPiLo, fma(-k, kTwoPiHi, ang));
-    float c, s;
-    sincosf((float)r, &s, &c);
-    return make_float2(c, s);
+    const double k = rint(ang * kInvHalfPi);
+    const float r = (float)fma(-k, kHalfPiLo, fma(-k, kHalfPiHi, ang));
+    const int quarter = (int)k;
+    const float x = r * r;
+    float s = fmaf(x, 1.0f / 362880.0f, -1.0f / 5040.0f);
+    s = fmaf(x, s, 1.0f / 120.0f);
+    s = fmaf(x, s, -1.0f / 6.0f);
+    s = fmaf(r * x, s, r);
+    float c = fmaf(x, -1.0f / 3628800.0f, 1.0f / 40320.0f);
+    c = fmaf(x, c, -1.0f / 720.0f);
+    c = fmaf(x, c, 1.0f / 24.0f);
+    c = fmaf(x, c, -0.5f);
+    c = fmaf(x, c, 1.0f);
+    const float cq = quarter & 1 ? s : c, sq = quarter & 1 ? c : s;
+    return make_float2((quarter + 1) & 2 ? -cq : cq, quarter & 2 ? -sq : sq);
 }
 
 // Four consecutive features f .. f + 3 (f a multiple of 4) of head `head` of
@@ -227,10 +242,10 @@ __device__ inline uint32_t recode4(uint32_t c, float ratio)
 
 // e4m3 pages: one workgroup per page with new tokens, key/value head and K or
 // V, so that the page's scale has one writer and needs no atomics.  The new
-// values' maximum gives the scale; up to kHold passes of tokens stay in
-// registers between the two uses, more are read and rotated again.
-constexpr int kHold = 4;
-
+// values' maximum gives the scale, then they are coded.  A thread takes a
+// piece of a token; more tokens than one pass takes (16 at 128 dims) are read
+// and rotated a second time (held in registers instead, they left the queries'
+// workgroups half of the waves per CU).
 template <bool kPacked>
 __device__ __forceinline__ void append_codes(const Args& a, const Source& x, int n_blocks)
 {
@@ -249,34 +264,24 @@ __device__ __forceinline__ void append_codes(const Args& a, const Source& x, int
         float* scale = (turn ? a.k_scale : a.v_scale) + pg;
         int e_old = kExpMin;
         if (w.slot0 > 0) e_old = min(max((int)(__float_as_uint(*scale) >> 23 & 255u) - 127, kExpMin), kExpMax);
-        Piece v[kHold];
-        auto load = [&](int j0) {
+        auto load = [&](int j) {
+            Piece v = load_piece<kPacked>(x, w.tok0 + j, head, f, hd, a.H + G, turn);
+            if (turn) {
+                const int pos = a.tok[w.tok0 + j].pos;
 #pragma unroll
-            for (int u = 0; u < kHold; ++u) {
-                const int j = j0 + u * per_pass + tj;
-                if (j >= w.n) {
-                    v[u] = Piece{};
-                    continue;
-                }
-                v[u] = load_piece<kPacked>(x, w.tok0 + j, head, f, hd, a.H + G, turn);
-                if (turn) {
-                    const int pos = a.tok[w.tok0 + j].pos;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) turn_pair(v[u].lo[i], v[u].hi[i], rotation(pos, a.freq[f + i]));
-                }
+                for (int i = 0; i < 4; ++i) turn_pair(v.lo[i], v.hi[i], rotation(pos, a.freq[f + i]));
             }
+            return v;
         };
-        const int chunk = kHold * per_pass;
+        Piece v{};
         float amax = 0.f;
-        for (int j0 = 0; j0 < w.n; j0 += chunk) {
-            load(j0);
+        for (int j = tj; j < w.n; j += per_pass) {
+            v = load(j);
 #pragma unroll
-            for (int u = 0; u < kHold; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (finite(v[u].lo[i])) amax = fmaxf(amax, fabsf(v[u].lo[i]));
-                    if (finite(v[u].hi[i])) amax = fmaxf(amax, fabsf(v[u].hi[i]));
-                }
+            for (int i = 0; i < 4; ++i) {
+                if (finite(v.lo[i])) amax = fmaxf(amax, fabsf(v.lo[i]));
+                if (finite(v.hi[i])) amax = fmaxf(amax, fabsf(v.hi[i]));
+            }
         }
         for (int off = 32; off >= 1; off >>= 1) amax = fmaxf(amax, __shfl_xor(amax, off, 64));
         if ((threadIdx.x & 63) == 0) s_max[threadIdx.x >> 6] = amax;
@@ -294,16 +299,11 @@ __device__ __forceinline__ void append_codes(const Args& a, const Source& x, int
             }
         }
         const float inv = exp2i(-e);
-        for (int j0 = 0; j0 < w.n; j0 += chunk) {
-            if (w.n > chunk) load(j0);
-#pragma unroll
-            for (int u = 0; u < kHold; ++u) {
-                const int j = j0 + u * per_pass + tj;
-                if (j >= w.n) continue;
-                uint8_t* dst = base + (w.slot0 + j) * hd + f;
-                *reinterpret_cast<uint32_t*>(dst) = code4(v[u].lo, inv);
-                *reinterpret_cast<uint32_t*>(dst + (turn ? hd / 2 : 4)) = code4(v[u].hi, inv);
-            }
+        for (int j = tj; j < w.n; j += per_pass) {
+            if (w.n > per_pass) v = load(j);
+            uint8_t* dst = base + (w.slot0 + j) * hd + f;
+            *reinterpret_cast<uint32_t*>(dst) = code4(v.lo, inv);
+            *reinterpret_cast<uint32_t*>(dst + (turn ? hd / 2 : 4)) = code4(v.hi, inv);
         }
         __syncthreads();                                 // s_max is written again
     }
@@ -311,12 +311,12 @@ __device__ __forceinline__ void append_codes(const Args& a, const Source& x, int
 
 // The first n_code workgroups code pages (longer work first), the others take
 // the tokens' runs, n_runs each.
-template <bool kPacked>
+template <bool kPacked, bool kE4m3>
 __global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t* __restrict__ q, int n_code,
                                                      int n_runs)
 {
-    const int b = (int)blockIdx.x - n_code;
-    if (b < 0) append_codes<kPacked>(a, x, n_code);
+    const int b = (int)blockIdx.x - (kE4m3 ? n_code : 0);
+    if (kE4m3 && b < 0) append_codes<kPacked>(a, x, n_code);
     else append_rows<kPacked>(a, x, q, b / n_runs, b % n_runs);
 }
 
@@ -366,6 +366,13 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t bytes,
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
                  : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(offset), "s"(d));
+}
+
+// the same into registers
+__device__ __forceinline__ u32x4_t load_16(const uint8_t* base, uint32_t bytes, int offset)
+{
+    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)bytes, 0x00020000);
+    return __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(d, offset, 0, 0));
 }
 
 // of two bf16: bits all ones in the halves that are not finite
@@ -689,8 +696,8 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
 // Rows go through registers, a step ahead (e4m3 codes are decoded on the way).
 // (Straight from memory to LDS the compiler made every transposing read wait
 // for the next step's rows.)  A row's 16-byte chunks are swapped about by its
-// number, so that neither the 32 rows of a K read nor the 8 of a V read meet
-// in the same banks.
+// number, so that neither the 32 rows of a K read nor the four of a V read
+// meet in the same banks.
 //
 // P enters rounded to one bf16 (relative error 2^-8 at most per weight, random
 // in sign; the output's own rounding is as large): a second term would cost
@@ -728,7 +735,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     // chunk of row r is at chunk ^ k_key(r) of K, ^ v_key(r) of V (rows of 64
     // dims: two share the 256 bytes of all banks)
     auto k_key = [](int r) { return HD == 128 ? r & 15 : r >> 1 & 7; };
-    auto v_key = [](int r) { return HD == 128 ? (r & 7) * 2 : (r >> 1 & 3) * 2; };
+    auto v_key = [](int r) { return HD == 128 ? (r & 3) * 4 : (r >> 1 & 1) * 4; };
     const int k_off = (pg * NB * 32 + c) * RB + (h ^ k_key(c)) * 16;          // K step k: ^ k * 32
     const int vrow = 4 * h + (c & 15) / 4;               // the lane's V row of 8
     int v_off[DB];
@@ -736,13 +743,14 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     for (int b = 0; b < DB; ++b)
         v_off[b] = kHalf + (pg * NB * 32 + vrow) * RB +
                    ((b * 4 + c / 16 * 2 + (c >> 1 & 1)) ^ v_key(vrow)) * 16 + (c & 1) * 8;
-    constexpr int CL = HD * ES / 64;                     // 16-byte pieces of K per lane and step
+    constexpr int RW = kP / 4;                           // rows of a step that a wave brings
+    constexpr int CL = RW * HD * ES / 1024;              // 16-byte pieces of K per lane and step
     constexpr int LR = 1024 / (HD * ES);                 // rows per 64 pieces
     constexpr int PR = HD * ES / 16;                     // pieces per row
     constexpr int DC = kE4m3 ? 2 : 1;                    // LDS chunks per piece
-    const int k_in = (lane % PR * DC ^ k_key(lane / PR)) * 16, v_in = (lane % PR * DC ^ v_key(lane / PR)) * 16;
+    const int k_in = (lane % PR * DC ^ k_key(RW * w) ^ k_key(lane / PR)) * 16, v_in = (lane % PR * DC ^ v_key(lane / PR)) * 16;
     u32x4_t kc[CL], vc[CL];                              // e4m3: the next step's codes
-    float ksc = 0.f, vsc = 0.f;
+    float ksc = 0.f, vsc = 0.f, ksc_in = 0.f, vsc_in = 0.f;
     for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
         if (it != (int)blockIdx.x) im = uniform_struct(items + it);
         const int32_t* table = a.table + im.table;
@@ -768,88 +776,89 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
 #pragma unroll
         for (int b = 0; b < DB; ++b) o[b] = f32x16_t{};
         float m = -INFINITY, ms = 0.f, thr = -INFINITY, l = 0.f;
-        // Wave w brings rows 16 w .. + 15 of the next step, which lie in one
-        // page.  Positions past the sequence's end are its last one (masked
-        // for every row); without a page they are zeros.
-        auto bring = [&](int p0, int to) {
-            const int pb = min(p0 + 16 * w, (n_pos - 1) & ~15), last = n_pos - 1 - pb;
+        // Wave w brings RW rows of a later step from RW w on, which lie in one
+        // page, piece by piece between its matrix products: K's pieces, then
+        // V's.  Positions past the sequence's end are its last one (masked for
+        // every row); without a page they are zeros.
+        const uint8_t *kb_in = nullptr, *vb_in = nullptr;
+        uint32_t in_bytes = 0;
+        int last = 0;
+        auto locate = [&](int p0) {
+            const int pb = min(p0 + RW * w, (n_pos - 1) & ~(RW - 1));
+            last = n_pos - 1 - pb;
             const int page = uniform_load(table + (pb >> a.shift));
             const int64_t head = (int64_t)max(page, 0) * a.G + kvh;
             const int64_t at = ((head << a.shift) + (pb & (P - 1))) * (HD * ES);
+            kb_in = a.k + at;
+            vb_in = a.v + at;
+            in_bytes = page < 0 ? 0u : RW * HD * ES;     // (a read past the size gives zero)
             if constexpr (kE4m3) {
-                // into registers (`decode` takes them on); rows past the end
-                // and without a page: see above
-#pragma unroll
-                for (int i = 0; i < CL; ++i) {
-                    const int src = min(i * LR + lane / PR, last) * HD + lane % PR * 16;
-                    kc[i] = ld16(a.k + at + src);
-                    vc[i] = ld16(a.v + at + src);
-                }
-                ksc = uniform_load(a.k_scale + head);
-                vsc = uniform_load(a.v_scale + head);
-                if (page < 0) {
-#pragma unroll
-                    for (int i = 0; i < CL; ++i) kc[i] = vc[i] = zero;
-                }
-            } else {
-                uint8_t* dst = lds + to + w * 16 * RB;
-                if (page < 0) {
-#pragma unroll
-                    for (int i = 0; i < CL; ++i) {
-                        *reinterpret_cast<u32x4_t*>(dst + i * 1024 + lane * 16) = zero;
-                        *reinterpret_cast<u32x4_t*>(dst + kHalf + i * 1024 + lane * 16) = zero;
-                    }
-                    return;
-                }
-#pragma unroll
-                for (int i = 0; i < CL; ++i) {
-                    const int r = min(i * LR + lane / PR, last) * RB;
-                    load_to_lds(a.k + at, 16 * RB, dst + i * 1024, r + (k_in ^ k_key(i * LR) * 16));
-                    load_to_lds(a.v + at, 16 * RB, dst + kHalf + i * 1024, r + (v_in ^ v_key(i * LR) * 16));
-                }
+                ksc_in = uniform_load(a.k_scale + head);
+                vsc_in = uniform_load(a.v_scale + head);
             }
         };
-        // piece i of the lane: row i LR + lane / PR, whose key is that of
-        // lane / PR ^ that of i LR
-        auto decode = [&](int to) {
+        // bf16: piece i of the located step straight to LDS
+        auto load_piece = [&](int i, int to) {
+            const bool v = i >= CL;
+            const int x = i % CL;
+            const int off = min(x * LR + lane / PR, last) * RB + (v ? v_in ^ v_key(x * LR) * 16 : k_in ^ k_key(x * LR) * 16);
+            load_to_lds(v ? vb_in : kb_in, in_bytes, lds + to + (v ? kHalf : 0) + w * RW * RB + x * 1024, off);
+        };
+        // e4m3: the located step's codes into registers, and from there
+        // (piece i: row i LR + lane / PR, whose key is that of lane / PR ^ that
+        // of i LR) to LDS
+        auto load_codes = [&] {
 #pragma unroll
             for (int i = 0; i < CL; ++i) {
-                uint8_t* dst = lds + to + (w * 16 + i * LR + lane / PR) * RB;
-                const int ko = k_in ^ k_key(i * LR) * 16, vo = v_in ^ v_key(i * LR) * 16;
-                *reinterpret_cast<u32x4_t*>(dst + ko) = decode8(kc[i][0], kc[i][1], ksc);
-                *reinterpret_cast<u32x4_t*>(dst + (ko ^ 16)) = decode8(kc[i][2], kc[i][3], ksc);
-                *reinterpret_cast<u32x4_t*>(dst + kHalf + vo) = decode8(vc[i][0], vc[i][1], vsc);
-                *reinterpret_cast<u32x4_t*>(dst + kHalf + (vo ^ 16)) = decode8(vc[i][2], vc[i][3], vsc);
+                const int off = min(i * LR + lane / PR, last) * HD + lane % PR * 16;
+                kc[i] = load_16(kb_in, in_bytes, off);
+                vc[i] = load_16(vb_in, in_bytes, off);
             }
+            ksc = ksc_in;
+            vsc = vsc_in;
+        };
+        auto decode_piece = [&](int i, int to) {
+            const bool v = i >= CL;
+            const int x = i % CL;
+            uint8_t* dst = lds + to + (v ? kHalf : 0) + (w * RW + x * LR + lane / PR) * RB;
+            const int off = v ? v_in ^ v_key(x * LR) * 16 : k_in ^ k_key(x * LR) * 16;
+            const u32x4_t& c = v ? vc[x] : kc[x];
+            const float scale = v ? vsc : ksc;
+            *reinterpret_cast<u32x4_t*>(dst + off) = decode8(c[0], c[1], scale);
+            *reinterpret_cast<u32x4_t*>(dst + (off ^ 16)) = decode8(c[2], c[3], scale);
         };
         const int first = im.begin, end = im.end;
+        const int p_last = first + (end - first - 1) / kP * kP;   // the last step; past it, it is brought again
         // a step that some row of the block does not see whole
         auto partly_seen = [&](int p0) { return p0 + kP - 1 > lim_b0 || im.holes; };
         __syncthreads();                                 // the last item's LDS reads are done
         if (threadIdx.x == 0) s_bad = 0u;
-        __syncthreads();
-        if (first < end) {
-            bring(first, 0);
-            if constexpr (kE4m3) {
-                decode(0);
-                if (first + kP < end) bring(first + kP, 0);
-            }
+        locate(first);
+        if constexpr (kE4m3) {
+            load_codes();
+#pragma unroll
+            for (int i = 0; i < 2 * CL; ++i) decode_piece(i, 0);
+            locate(min(first + kP, p_last));
+            load_codes();
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * CL; ++i) load_piece(i, 0);
         }
         // The step's start, the same for every wave: its rows have arrived
-        // from every wave, every wave is done with the last step's, and the
-        // next one's are on their way.  Of a step that is only partly seen,
-        // values of V that are not finite are taken out (0 times one would
-        // still reach the rows that do not see it).
+        // from every wave, and every wave is done with the last step's.  Of a
+        // step that is only partly seen, values of V that are not finite are
+        // taken out (0 times one would still reach the rows that do not see it).
         auto begin_step = [&](int p0, int buf) {
             __builtin_amdgcn_s_waitcnt(kE4m3 ? 0xC07F : 0x0070);   // lgkmcnt 0, and vmcnt 0 where LDS is loaded
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
+            locate(min(p0 + (kE4m3 ? 2 : 1) * kP, p_last));
             if (partly_seen(p0)) {
                 uint32_t bad = 0u;
 #pragma unroll
-                for (int i = 0; i < 16 * RB / 1024; ++i) {
-                    u32x4_t* d = reinterpret_cast<u32x4_t*>(lds + buf + kHalf + w * 16 * RB + i * 1024 + lane * 16);
+                for (int i = 0; i < RW * RB / 1024; ++i) {
+                    u32x4_t* d = reinterpret_cast<u32x4_t*>(lds + buf + kHalf + w * RW * RB + i * 1024 + lane * 16);
                     u32x4_t v = *d;
                     uint32_t any = 0u;
 #pragma unroll
@@ -864,44 +873,79 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
                 if (bad) s_bad = 1u;
                 lds_barrier();
             }
-            if (p0 + kP < end) {
-                if constexpr (kE4m3) {
-                    decode(buf ^ kBuf);
-                    if (p0 + 2 * kP < end) bring(p0 + 2 * kP, 0);
-                } else {
-                    bring(p0 + kP, buf ^ kBuf);
-                }
+        };
+        // what is brought beside K step k of the scores
+        auto bring = [&](int k, int to) {
+            if constexpr (kE4m3) {
+#pragma unroll
+                for (int i = 0; i < 2 * CL; ++i)
+                    if (i * (KQ - 1) / (2 * CL) == k) decode_piece(i, to);
+                if (k == KQ - 1) load_codes();
+            } else {
+#pragma unroll
+                for (int i = 0; i < 2 * CL; ++i)
+                    if (i * KQ / (2 * CL) == k) load_piece(i, to);
             }
         };
         int buf = 0;
         if (!wave_ok) {                                  // no rows: this wave only brings its share
-            for (int p0 = first; p0 < end; p0 += kP, buf ^= kBuf) begin_step(p0, buf);
+            for (int p0 = first; p0 < end; p0 += kP, buf ^= kBuf) {
+                begin_step(p0, buf);
+#pragma unroll
+                for (int k = 0; k < KQ; ++k) bring(k, buf ^ kBuf);
+            }
         } else {
             for (int p0 = first; p0 < end; p0 += kP, buf ^= kBuf) {
                 begin_step(p0, buf);
                 const uint8_t* kb = lds + buf;
+                // K fragments are read kAhead K steps before their products, an
+                // LDS access taking as long as several of these
                 f32x16_t sc[NB];
-#pragma unroll
-                for (int pb = 0; pb < NB; ++pb) sc[pb] = f32x16_t{};
-#pragma unroll
-                for (int k = 0; k < KQ; ++k)
+                constexpr int kAhead = KQ < 4 ? KQ : 4;
+                u32x4_t kf[kAhead][NB];
+                auto read_k = [&](int k) {
 #pragma unroll
                     for (int pb = 0; pb < NB; ++pb)
-                        sc[pb] = mfma32x32x16(*reinterpret_cast<const u32x4_t*>(kb + (k_off ^ (k * 32)) + pb * 32 * RB), qf[k], sc[pb]);
+                        kf[k % kAhead][pb] = *reinterpret_cast<const u32x4_t*>(kb + (k_off ^ (k * 32)) + pb * 32 * RB);
+                };
+#pragma unroll
+                for (int k = 0; k < kAhead; ++k) read_k(k);
+                // V of the first 16 positions, and then always 16 ahead
+                u32x4_t av[2][DB];
+                auto read_v = [&](int i) {
+#pragma unroll
+                    for (int b = 0; b < DB; ++b) {
+                        const uint8_t* p = kb + v_off[b] + i * 16 * RB;
+                        const uint2 v0 = transposed(p), v1 = transposed(p + 8 * RB);
+                        av[i % 2][b] = u32x4_t{v0.x, v0.y, v1.x, v1.y};
+                    }
+                };
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int k = 0; k < KQ; ++k) {
+#pragma unroll
+                    for (int pb = 0; pb < NB; ++pb)
+                        sc[pb] = mfma32x32x16(kf[k % kAhead][pb], qf[k], k ? sc[pb] : f32x16_t{});
+                    if (k + kAhead < KQ) read_k(k + kAhead);
+                    else if (k == KQ - 1) read_v(0);
+                    bring(k, buf ^ kBuf);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
                 const int pw0 = p0 + pg * NB * 32;       // the wave's first position
                 if (pw0 + NB * 32 - 1 > lim_w0 || im.holes) {
                     uint32_t holes = 0u;                 // runs of 16 positions without a page
                     if (im.holes) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < kP / 16; ++i)
                             if (uniform_load(table + (min(p0 + 16 * i, n_pos - 1) >> a.shift)) < 0) holes |= 1u << i;
                     }
+                    const int seen = lim - pw0 - 4 * h;
 #pragma unroll
                     for (int pb = 0; pb < NB; ++pb)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            const int at = pb * 32 + 8 * (i / 4) + 4 * h + i % 4;
-                            if (pw0 + at > lim || (holes >> ((pg * NB * 32 + at) / 16) & 1u)) sc[pb][i] = -INFINITY;
+                            const int at = pb * 32 + 8 * (i / 4) + i % 4;
+                            if (at > seen || (holes >> (pg * NB * 2 + at / 16) & 1u)) sc[pb][i] = -INFINITY;
                         }
                 }
                 float mx = -INFINITY;
@@ -920,30 +964,35 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
                     ms = mn;
                     thr = mx + kLazy / scale2;
                 }
+                // the weights of 16 positions are formed beside the products
+                // of the 16 before, two scores to a product
+                u32x4_t bt[2];
+                auto weights = [&](int i, int e) {
+                    const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e], scale2, -ms));
+                    const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e + 1], scale2, -ms));
+                    l += pa + pb;
+                    bt[i % 2][e] = moe::cvt_pk_bf16(pa, pb);
+                };
 #pragma unroll
-                for (int pb = 0; pb < NB; ++pb)
+                for (int e = 0; e < 4; ++e) weights(0, e);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int sx = 0; sx < 2; ++sx) {
-                        u32x4_t av[DB];
+                for (int i = 0; i < 2 * NB; ++i) {
+                    if (i + 1 < 2 * NB) read_v(i + 1);
 #pragma unroll
-                        for (int b = 0; b < DB; ++b) {
-                            const uint8_t* p = kb + v_off[b] + (pb * 32 + sx * 16) * RB;
-                            const uint2 v0 = transposed(p), v1 = transposed(p + 8 * RB);
-                            av[b] = u32x4_t{v0.x, v0.y, v1.x, v1.y};
+                    for (int b = 0; b < DB; ++b) {
+                        o[b] = mfma32x32x16(av[i % 2][b], bt[i % 2], o[b]);
+                        if (i + 1 < 2 * NB) {
+#pragma unroll
+                            for (int e = b * 4 / DB; e < (b + 1) * 4 / DB; ++e) weights(i + 1, e);
                         }
-                        u32x4_t bt;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float pa = __builtin_amdgcn_exp2f(fmaf(sc[pb][sx * 8 + 2 * i], scale2, -ms));
-                            const float pb2 = __builtin_amdgcn_exp2f(fmaf(sc[pb][sx * 8 + 2 * i + 1], scale2, -ms));
-                            l += pa + pb2;
-                            bt[i] = moe::cvt_pk_bf16(pa, pb2);
-                        }
-#pragma unroll
-                        for (int b = 0; b < DB; ++b) o[b] = mfma32x32x16(av[b], bt, o[b]);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                }
             }
         }
+        // (what was brought again is done with the LDS)
+        __builtin_amdgcn_s_waitcnt(0x0070);
         __syncthreads();
         if (s_bad) {
             // the rows that see a value that was taken out get a NaN in its dim
@@ -1075,9 +1124,15 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
                 for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
                 L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
                 float acc[D] = {};
+                auto add_all = [&](auto most) {                         // (past n: slot 0 with factor 0)
 #pragma unroll
-                for (int s = 0; s < kWaveSlots; ++s)                   // (past n: slot 0 with factor 0)
-                    add(pr, s < n ? s : 0, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s)), acc);
+                    for (int s = 0; s < decltype(most)::value; ++s)
+                        add(pr, s < n ? s : 0, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s)), acc);
+                };
+                if (n <= 2) add_all(std::integral_constant<int, 2>{});
+                else if (n <= 5) add_all(std::integral_constant<int, 5>{});
+                else if (n <= 8) add_all(std::integral_constant<int, 8>{});
+                else add_all(std::integral_constant<int, kWaveSlots>{});
                 write(row, acc, L);
             }
             continue;
@@ -1141,8 +1196,15 @@ hipError_t attn_paged_launch_append(const paged::Args* a, const paged::Source* x
     const int pieces = (a->e4m3 ? a->H : a->H + 2 * a->G) * a->hd / 8, runs = (pieces + 255) / 256;
     const int codes = a->e4m3 ? n_pages * a->G * 2 : 0;
     const dim3 grid(codes + T * runs);
-    if (x->packed) hipLaunchKernelGGL(paged::append_kernel<true>, grid, dim3(256), 0, s, *a, *x, q, codes, runs);
-    else hipLaunchKernelGGL(paged::append_kernel<false>, grid, dim3(256), 0, s, *a, *x, q, codes, runs);
+#define APPEND(PACKED, E) hipLaunchKernelGGL((paged::append_kernel<PACKED, E>), grid, dim3(256), 0, s, *a, *x, q, codes, runs)
+    if (x->packed) {
+        if (a->e4m3) APPEND(true, true);
+        else APPEND(true, false);
+    } else {
+        if (a->e4m3) APPEND(false, true);
+        else APPEND(false, false);
+    }
+#undef APPEND
     return hipGetLastError();
 }
 

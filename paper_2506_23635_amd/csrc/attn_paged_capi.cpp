@@ -24,8 +24,9 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kStages = 4;             // batches on their way to the device at once
 constexpr int kXcds = 8;
-constexpr int64_t kFewItems = 1024;    // at most about so many shares of few_kernel ...
-constexpr int64_t kTileItems = 768;    // ... and half as many of tile_kernel, come from dividing positions
+// Dividing positions makes at most twice as many shares (and partial sums)
+constexpr int64_t kFewItems = 1024;    // of few_kernel
+constexpr int64_t kTileItems = 768;    // of tile_kernel
 constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -156,51 +157,73 @@ moe_status hip_fail(attn_paged_ctx* ctx, hipError_t e, const char* what)
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
-// Divides `steps` steps from `begin` on into n ranges that differ by one at most.
-void ranges(std::vector<Item>& out, Item it, int n, int step, int& slot)
+// Appends the shares of `it` that end after the given steps (the last: all of them).
+void add_ranges(std::vector<Item>& out, Item it, const std::vector<int>& cuts, int step, int& slot)
 {
-    const int64_t steps = (it.end - it.begin + step - 1) / step;
     const int begin = it.begin, end = it.end;
-    for (int i = 0; i < n; ++i) {
-        it.begin = begin + (int)(steps * i / n) * step;
-        it.end = std::min<int64_t>(end, begin + steps * (i + 1) / n * step);
-        it.slot = n > 1 ? slot++ : -1;
+    const bool several = cuts.size() > 1;
+    int from = 0;
+    for (int to : cuts) {
+        it.begin = begin + from * step;
+        it.end = (int)std::min<int64_t>(end, begin + (int64_t)to * step);
+        it.slot = several ? slot++ : -1;
         out.push_back(it);
+        from = to;
     }
+}
+
+// n ranges of `steps` steps that differ by one at most
+void even_cuts(int64_t steps, int64_t n, std::vector<int>& cuts)
+{
+    cuts.clear();
+    for (int64_t i = 1; i <= n; ++i) cuts.push_back((int)(steps * i / n));
 }
 
 // A row block of tile_kernel: the steps of 64 positions that it needs.
 struct Block {
     int steps, rows;
+    std::vector<int> cuts;
 };
 
-// The length of the ranges, in steps, that the row blocks' positions are
-// divided into: the least estimated time over the division of the longest
-// block into 1 .. kMostRanges ranges (a block of `steps` steps has
-// ceil(steps / length) of them).  The workgroups are handed out longest first,
-// two per CU; that is played through for one key/value head and its share of
-// the places.  Measured on 128 x 64 steps at head_dim 128: a step 2.2 us, where
-// a CU has one workgroup 1.6; about one and a half more per workgroup; the
-// partial sums written and read at about 4.5 TB/s, the merge's launch 4 us.
-int range_steps(const std::vector<Block>& blocks, int G)
+// Divides the row blocks' positions into ranges: the longest block's into 1 ..
+// kMostRanges, and every block then has ranges of about that length; by the
+// least estimated time.  The workgroups are handed out longest first, two per
+// CU; that is played through for one key/value head and its share of the
+// places.  Measured at head_dim 128: a step 2.2 us, where a CU has one
+// workgroup 1.6; about one and a half more per share; the partial sums written
+// and read at about 4.5 TB/s, the merge's launch 4 us.  (512 tokens after 8000
+// positions, bf16: 1 range 191 us, 2 145, 5 117, and the merge 6 to 16.  Cutting
+// all blocks' steps in a row into one equal run per place instead: 123.)
+void divide_blocks(std::vector<Block>& blocks, int G)
 {
-    constexpr int kPlaces = 512, kCus = 256, kMostRanges = 16;
+    constexpr int kPlaces = 512, kCus = 256, kMostRanges = 12;
     int longest = 0;
-    for (const Block& b : blocks) longest = std::max(longest, b.steps);
+    for (Block& b : blocks) {
+        even_cuts(b.steps, 1, b.cuts);
+        longest = std::max(longest, b.steps);
+    }
     const int places = std::max(1, kPlaces / G);
-    int best = std::max(1, longest);
-    double best_us = 0.0;
+    if (blocks.size() >= 4 * (size_t)places) return;     // enough without
+    std::vector<Block> trial = blocks;
     std::vector<double> items;
+    double best_us = 0.0;
     for (int n = 1; n <= kMostRanges && n <= longest; ++n) {
         const int len = (longest + n - 1) / n;
+        for (Block& b : trial) even_cuts(b.steps, (b.steps + len - 1) / len, b.cuts);
         items.clear();
         int64_t slots = 0, rows = 0;
-        for (const Block& b : blocks) {
-            const int k = (b.steps + len - 1) / len;
-            for (int i = 0; i < k; ++i) items.push_back((b.steps + k - 1) / k + 1.5);
-            if (k > 1) { slots += k; rows += (int64_t)k * b.rows; }
+        for (const Block& b : trial) {
+            int from = 0;
+            for (int c : b.cuts) {
+                items.push_back(c - from + 1.5);
+                from = c;
+            }
+            if (b.cuts.size() > 1) {
+                slots += (int64_t)b.cuts.size();
+                rows += (int64_t)b.cuts.size() * b.rows;
+            }
         }
-        if (slots * G > 2 * kTileItems) break;
+        if (slots * G > 2 * kTileItems) continue;
         std::sort(items.begin(), items.end(), std::greater<double>());
         std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
         double end = 0.0;
@@ -214,9 +237,11 @@ int range_steps(const std::vector<Block>& blocks, int G)
         }
         double us = end * ((int64_t)items.size() * G <= kCus ? 1.6 : 2.2);
         if (slots) us += 4.0 + (double)rows * G * 132 * 4 * 2 / 4.5e6;
-        if (n == 1 || us < 0.97 * best_us) { best = len; best_us = us; }
+        if (n == 1 || us < 0.97 * best_us) {
+            best_us = us;
+            for (size_t i = 0; i < blocks.size(); ++i) blocks[i].cuts = trial[i].cuts;
+        }
     }
-    return best;
 }
 
 // Longest shares first: the workgroups are handed out in order.
@@ -279,11 +304,13 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
         const int rows = R <= 64 ? 64 : 128;
         for (int64_t r0 = 0; r0 < R; r0 += rows) {
             const int64_t last = std::min(r0 + rows, R);
-            blocks.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0)});
+            blocks.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0), {}});
         }
     }
     const int64_t few_len = std::max<int64_t>(1, (few_total + kFewItems - 1) / kFewItems);
-    const int tile_len = range_steps(blocks, G);
+    divide_blocks(blocks, G);
+    std::vector<int> cuts;
+    size_t block = 0;                                    // the sequence's first of `blocks`
     int few_slot = 0, tile_slot = 0, tok0 = 0, table = 0;
     for (int s = 0; s < n_seqs; ++s) {
         const int R = n_new[s] * group, n_pos = pos0[s] + n_new[s];
@@ -298,31 +325,33 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
             it.end = n_pos;
             const int64_t steps = (n_pos + kFewStep - 1) / kFewStep;
             const int n = (int)((steps + few_len - 1) / few_len);
+            even_cuts(steps, n, cuts);
             for (it.kvh = 0; it.kvh < G; ++it.kvh) {
                 if (n > 1) {
                     b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, 0, 0});
                     b.merge_rows = std::max(b.merge_rows, R);
                     b.merge_slots = std::max(b.merge_slots, n);
                 }
-                ranges(b.few, it, n, kFewStep, few_slot);
+                add_ranges(b.few, it, cuts, kFewStep, few_slot);
             }
         } else if (R > 0) {
-            const int kind = R <= 64, rows = 128 >> kind;
+            const int kind = R <= 64, rows = 128 >> kind, n_blocks = (R + rows - 1) / rows;
             for (it.kvh = 0; it.kvh < G; ++it.kvh)
-                for (int r0 = 0; r0 < R; r0 += rows) {
-                    it.row0 = r0;
-                    it.rows = std::min(rows, R - r0);
+                for (int k = 0; k < n_blocks; ++k) {
+                    const Block& bl = blocks[block + k];
+                    const int n = (int)bl.cuts.size();
+                    it.row0 = k * rows;
+                    it.rows = bl.rows;
                     it.begin = 0;
-                    it.end = pos0[s] + (r0 + it.rows - 1) / group + 1;
-                    const int64_t steps = (it.end + paged::kStep - 1) / paged::kStep;
-                    const int n = (int)((steps + tile_len - 1) / tile_len);
+                    it.end = pos0[s] + (it.row0 + it.rows - 1) / group + 1;
                     if (n > 1) {
-                        b.merge.push_back(Merge{tok0, r0, it.rows, it.kvh, tile_slot, n, 1, 0});
+                        b.merge.push_back(Merge{tok0, it.row0, it.rows, it.kvh, tile_slot, n, 1, 0});
                         b.merge_rows = std::max(b.merge_rows, (int)it.rows);
                         b.merge_slots = std::max(b.merge_slots, n);
                     }
-                    ranges(b.tile[kind], it, n, paged::kStep, tile_slot);
+                    add_ranges(b.tile[kind], it, bl.cuts, paged::kStep, tile_slot);
                 }
+            block += n_blocks;
         }
         tok0 += n_new[s];
         table += n_new[s] > 0 ? blocks_of(s) : 0;
