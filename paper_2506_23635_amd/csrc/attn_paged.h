@@ -9,9 +9,10 @@
 
 namespace paged {
 
-constexpr int kFewRows = 16;       // query rows of one key/value head that few_kernel takes at once
-constexpr int kTile = 32;          // positions of a few_kernel wave's step
-constexpr int kStep = 64;          // positions of a tile_kernel workgroup's step
+constexpr int kXcds = 8;
+constexpr int kFewRows = 16;       // query rows of one key/value head that few() takes at once
+constexpr int kTile = 32;          // positions of a step of one wave of few()
+constexpr int kStep = 64;          // positions of a workgroup's step of tile()
 constexpr int kPartPad = 4;        // maximum, weight and padding behind the hd sums of a partial row
 constexpr int kExpMin = -100;      // exponents of an e4m3 page's scale
 constexpr int kExpMax = 120;
@@ -48,15 +49,16 @@ struct Item {
 struct Merge {
     int32_t tok0, row0, rows, kvh;
     int32_t slot0, n;
-    int32_t tile;      // 0: few_kernel's slots, 1: tile_kernel's
+    int32_t tile;      // 0: few()'s slots, 1: tile()'s
     int32_t pad;
 };
 
 // Counts that the kernels read on the device, so that a captured launch
 // follows a batch set after the capture.
 struct Header {
-    int32_t T, n_pages, n_few, n_tile[2], n_merge;
-    int32_t pad[2];
+    int32_t T, n_pages, n_few, n_tile[2];
+    int32_t n_merge[2];        // few()'s entries, then tile()'s
+    int32_t pad;
 };
 
 // Device pointers and sizes of a context's batch.
@@ -102,10 +104,11 @@ extern "C" {
 hipError_t attn_paged_launch_unpack(const paged::Unpack* u, hipStream_t s);
 hipError_t attn_paged_launch_append(const paged::Args* a, const paged::Source* x, uint16_t* q, int T,
                                     int n_pages, hipStream_t s);
-hipError_t attn_paged_launch_few(const paged::Args* a, const uint16_t* q, uint16_t* out, int grid, hipStream_t s);
-hipError_t attn_paged_launch_tile(const paged::Args* a, const uint16_t* q, uint16_t* out, int kind, int grid,
-                                  hipStream_t s);
-hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, int slots, hipStream_t s);
+// n: workgroups for few()'s shares, for tile()'s blocks of 128 rows and of 64
+hipError_t attn_paged_launch_attend(const paged::Args* a, const uint16_t* q, uint16_t* out, const int* n, hipStream_t s);
+// n, slots: few()'s and tile()'s entries at once, and the most slots of one
+hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, const int* n, const int* slots, int few_rows,
+                                   hipStream_t s);
 
 // The batch of a paged context as the attention block needs it.
 int32_t attn_paged_tokens(const attn_paged_ctx* ctx);

@@ -4,8 +4,8 @@
 //   unpack_kernel  a batch's arrays from pinned host memory to the workspace
 //   append_kernel  q rotated to bf16, k rotated and v to their slots (of e4m3
 //                  pages the scales too)
-//   few_kernel     attention of up to 16 query rows per key/value head
-//   tile_kernel    attention of blocks of 128 or 64 query rows
+//   attend_kernel  attention: few() of up to 16 query rows per key/value head,
+//                  tile() of blocks of 128 or 64
 //   merge_kernel   adds the partial sums of rows whose positions were shared out
 #include <cmath>
 #include <type_traits>
@@ -383,7 +383,7 @@ __device__ inline uint32_t bad_halves(uint32_t w)
 
 constexpr uint32_t kOnes = 0x3F803F80u;      // two bf16 ones
 
-// few_kernel: up to 16 query rows (tokens of a sequence times the heads of
+// few(): up to 16 query rows (tokens of a sequence times the heads of
 // one key/value head) over one range of positions, 4 waves taking the range's
 // 32-position steps in turn, each with a maximum and sums of its own, merged
 // through LDS at the end.
@@ -398,27 +398,31 @@ constexpr uint32_t kOnes = 0x3F803F80u;      // two bf16 ones
 // block i takes dim D r + i for row r: an 8 x D transposition inside the lane.
 // P enters as two bf16 terms (the second the rounding of what the first left:
 // 16 bits), since the matrix cores have time: the loads bound the kernel.
+// b, nb: this workgroup among those that take such shares, and their number.
+template <int HD>
+struct FewLds {
+    float o[4][kFewRows][HD + 4];            // the waves' sums, maxima and weights
+    float m[4][kFewRows], l[4][kFewRows];
+};
+
 template <int HD, bool kE4m3>
-__global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __restrict__ q,
-                                                     uint16_t* __restrict__ out, float scale2)
+__device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
+                                    float scale2, FewLds<HD>& lds, int b, int nb)
 {
     constexpr int NC = HD / 32;              // MFMA K steps of the scores
     constexpr int D = HD / 16;               // dims per lane of V
     constexpr int ES = kE4m3 ? 1 : 2;
     constexpr int KW = kE4m3 ? HD / 64 : NC; // 16-byte loads per K row and lane
     constexpr int VW = D * ES / 4;           // words per V row and lane
-    constexpr int ROW = HD + 4;
-    __shared__ __attribute__((aligned(16))) float s_o[4][kFewRows][ROW];
-    __shared__ float s_m[4][kFewRows], s_l[4][kFewRows];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int group = a.H / a.G, P = 1 << a.shift;
     // (the first share is read along with the count, not after it: the list
     // has room for every workgroup of the grid)
-    Item im = uniform_struct(a.few + blockIdx.x);
+    Item im = uniform_struct(a.few + b);
     const int n_items = uniform_load(&a.hdr->n_few);
-    for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        if (it != (int)blockIdx.x) im = uniform_struct(a.few + it);
+    for (int it = b; it < n_items; it += nb) {
+        if (it != b) im = uniform_struct(a.few + it);
         const int32_t* table = a.table + im.table;
         const int R = im.rows, kvh = im.kvh, n_pos = im.n_pos;
         const bool row_ok = r < R;
@@ -632,33 +636,33 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
         l += __shfl_xor(l, 32, 64);
         if (row_ok) {
             if (g == 0) {
-                s_m[w][r] = m;
-                s_l[w][r] = l;
+                lds.m[w][r] = m;
+                lds.l[w][r] = l;
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int i = 0; i < D; i += 4)
-                    *reinterpret_cast<float4*>(&s_o[w][r][D * (4 * g + e) + i]) =
+                    *reinterpret_cast<float4*>(&lds.o[w][r][D * (4 * g + e) + i]) =
                         make_float4(o[i][e], o[i + 1][e], o[i + 2][e], o[i + 3][e]);
         }
         __syncthreads();
         // the waves' sums in wave order: thread (row, eight or four dims)
         const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * D;
         if (row < R) {
-            float M = fmaxf(fmaxf(s_m[0][row], s_m[1][row]), fmaxf(s_m[2][row], s_m[3][row]));
+            float M = fmaxf(fmaxf(lds.m[0][row], lds.m[1][row]), fmaxf(lds.m[2][row], lds.m[3][row]));
             const float Ms = M == -INFINITY ? 0.f : base2(M, scale2);
             float L = 0.f, v[D];
 #pragma unroll
             for (int i = 0; i < D; ++i) v[i] = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float mk = s_m[k][row];
+                const float mk = lds.m[k][row];
                 const float f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(mk, scale2) - Ms);
                 if (mk == -INFINITY) continue;
-                L = fmaf(s_l[k][row], f, L);
+                L = fmaf(lds.l[k][row], f, L);
 #pragma unroll
-                for (int i = 0; i < D; ++i) v[i] = fmaf(s_o[k][row][d0 + i], f, v[i]);
+                for (int i = 0; i < D; ++i) v[i] = fmaf(lds.o[k][row][d0 + i], f, v[i]);
             }
             if (im.slot >= 0) {
                 float* dst = a.few_part + ((int64_t)im.slot * kFewRows + row) * (HD + kPartPad);
@@ -683,7 +687,7 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
     }
 }
 
-// tile_kernel: blocks of 128 or 64 query rows (kPG = 1 or 2 position groups:
+// tile(): blocks of 128 or 64 query rows (kPG = 1 or 2 position groups:
 // the 4 / kPG waves of a group own 32 rows each) over one range of positions
 // in steps of 64, whose K and V rows are in LDS as bf16, two steps in turn, so
 // that one barrier a step is enough; the query rows stay in registers.
@@ -708,10 +712,15 @@ __global__ __launch_bounds__(256, 2) void few_kernel(Args a, const uint16_t* __r
 constexpr int tile_rows(int pg) { return 128 / pg; }
 constexpr float kLazy = 8.f;
 
+template <int HD>
+struct TileLds {
+    uint8_t rows[4 * kStep * HD * 2];        // K and V of two steps; then the other position group's sums
+    uint32_t bad;                            // a value of V is not finite, where it is masked for some rows
+};
+
 template <int HD, bool kE4m3, int kPG>
-__global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __restrict__ items, int which,
-                                                      const uint16_t* __restrict__ q,
-                                                      uint16_t* __restrict__ out, float scale2)
+__device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
+                                     float scale2, TileLds<HD>& shared, int wg, int n_wg)
 {
     constexpr int KQ = HD / 16;              // 16-dim K steps of the score MFMAs
     constexpr int DB = HD / 32;              // 32-dim blocks of the output
@@ -723,14 +732,15 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     constexpr int kHalf = kP * RB;           // K or V of a step
     constexpr int kBuf = 2 * kHalf;
     constexpr int kMergeBytes = (4 - kRowWaves) * (DB * 16 + 2) * 64 * 4;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kBuf > kMergeBytes ? 2 * kBuf : kMergeBytes];
-    __shared__ uint32_t s_bad;               // a value of V that is not finite, where it is masked for some rows
+    static_assert(sizeof shared.rows >= 2 * kBuf && sizeof shared.rows >= kMergeBytes);
+    uint8_t* lds = shared.rows;
     const int group = a.H / a.G, P = 1 << a.shift;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 31, h = lane >> 5;
     const int pg = w / kRowWaves;                        // the wave's position group
-    Item im = uniform_struct(items + blockIdx.x);
-    const int n_items = uniform_load(&a.hdr->n_tile[which]);
+    const Item* items = a.tile[kPG - 1];
+    Item im = uniform_struct(items + wg);
+    const int n_items = uniform_load(&a.hdr->n_tile[kPG - 1]);
     const u32x4_t zero = {0u, 0u, 0u, 0u};
     // chunk of row r is at chunk ^ k_key(r) of K, ^ v_key(r) of V (rows of 64
     // dims: two share the 256 bytes of all banks)
@@ -751,8 +761,8 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     const int k_in = (lane % PR * DC ^ k_key(RW * w) ^ k_key(lane / PR)) * 16, v_in = (lane % PR * DC ^ v_key(lane / PR)) * 16;
     u32x4_t kc[CL], vc[CL];                              // e4m3: the next step's codes
     float ksc = 0.f, vsc = 0.f, ksc_in = 0.f, vsc_in = 0.f;
-    for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
-        if (it != (int)blockIdx.x) im = uniform_struct(items + it);
+    for (int it = wg; it < n_items; it += n_wg) {
+        if (it != wg) im = uniform_struct(items + it);
         const int32_t* table = a.table + im.table;
         const int kvh = im.kvh, n_pos = im.n_pos, R = im.rows;
         const int row_w0 = w % kRowWaves * 32;           // the wave's first row in the block
@@ -832,7 +842,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
         // a step that some row of the block does not see whole
         auto partly_seen = [&](int p0) { return p0 + kP - 1 > lim_b0 || im.holes; };
         __syncthreads();                                 // the last item's LDS reads are done
-        if (threadIdx.x == 0) s_bad = 0u;
+        if (threadIdx.x == 0) shared.bad = 0u;
         locate(first);
         if constexpr (kE4m3) {
             load_codes();
@@ -870,7 +880,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
                     if (any) *d = v;
                     bad |= any;
                 }
-                if (bad) s_bad = 1u;
+                if (bad) shared.bad = 1u;
                 lds_barrier();
             }
         };
@@ -994,7 +1004,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
         // (what was brought again is done with the LDS)
         __builtin_amdgcn_s_waitcnt(0x0070);
         __syncthreads();
-        if (s_bad) {
+        if (shared.bad) {
             // the rows that see a value that was taken out get a NaN in its dim
             for (int p0 = first; p0 < end; p0 += kP) {
                 if (!partly_seen(p0)) continue;
@@ -1076,22 +1086,76 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(Args a, const Item* __rest
     }
 }
 
+// The attention's launch.  kKinds: the kinds of shares that the batch has, 1
+// few(), 2 and 4 tile() on blocks of 128 and 64 rows; with several kinds the
+// workgroups that take them come in turn, eight at a time (one per XCD), so
+// that the ones that wait for memory and the ones that multiply share the CUs.
+struct Split {
+    int few, tile[2];                        // workgroups / 8 of each kind
+};
+
+template <int HD, bool kE4m3, int kKinds>
+__global__ __launch_bounds__(256, 2) void attend_kernel(Args a, const uint16_t* __restrict__ q,
+                                                        uint16_t* __restrict__ out, float scale2, Split n)
+{
+    union Lds {
+        FewLds<HD> few;
+        TileLds<HD> tile;
+    };
+    __shared__ __attribute__((aligned(1024)))
+    uint8_t mem[kKinds == 1 ? sizeof(FewLds<HD>) : kKinds == 7 ? sizeof(Lds) : sizeof(TileLds<HD>)];
+    FewLds<HD>& fl = *reinterpret_cast<FewLds<HD>*>(mem);
+    TileLds<HD>& tl = *reinterpret_cast<TileLds<HD>*>(mem);
+    const int b = blockIdx.x, nb = gridDim.x;
+    if constexpr (kKinds == 1) {
+        few<HD, kE4m3>(a, q, out, scale2, fl, b, nb);
+    } else if constexpr (kKinds == 2) {
+        tile<HD, kE4m3, 1>(a, q, out, scale2, tl, b, nb);
+    } else if constexpr (kKinds == 4) {
+        tile<HD, kE4m3, 2>(a, q, out, scale2, tl, b, nb);
+    } else {
+        const int x = b / kXcds, tiles = n.tile[0] + n.tile[1], all = tiles + n.few;
+        const int before = (int)((int64_t)x * tiles / all);
+        if ((int)((int64_t)(x + 1) * tiles / all) == before)
+            few<HD, kE4m3>(a, q, out, scale2, fl, (x - before) * kXcds + b % kXcds, n.few * kXcds);
+        else if (before < n.tile[0])
+            tile<HD, kE4m3, 1>(a, q, out, scale2, tl, before * kXcds + b % kXcds, n.tile[0] * kXcds);
+        else
+            tile<HD, kE4m3, 2>(a, q, out, scale2, tl, (before - n.tile[0]) * kXcds + b % kXcds, n.tile[1] * kXcds);
+    }
+}
+
 // merge_kernel: the partial sums of a row's slots, weighted by their maxima,
 // added in slot order.  Up to kWaveSlots slots a wave takes a row (lane s the
 // maximum and weight of slot s, then every lane its dims of all slots); more,
 // a workgroup does, wave w adding slots w, w + 4, ..., the waves' sums in wave
 // order.  A slot without weight holds zeros.
 constexpr int kWaveSlots = 16;
-constexpr int kMaxSlots = 4096;
+constexpr int kMaxSlots = 2 * 1024;          // kFewItems' most of one row
+
+//
+// A workgroup takes up to four rows of an entry, `chunks` workgroups an entry
+// (four rows, or one, of up to 16 of few()'s; of up to 128 of tile()'s).
+struct MergeGrid {
+    int few, few_chunks, tile_chunks;        // workgroups / few_chunks for few()'s entries
+    int few_rows, tile_rows;                 // rows of a workgroup, 4 or 1
+};
 
 template <int HD>
-__global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict__ out)
+__global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict__ out, MergeGrid g)
 {
     constexpr int D = HD / 64;
     __shared__ float s_f[kMaxSlots], s_red[2][4], s_sum[4][HD];
     const int group = a.H / a.G, lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n_items = uniform_load(&a.hdr->n_merge);
-    for (int it = blockIdx.x; it < n_items; it += gridDim.x) {
+    const int b = blockIdx.x, few_wgs = g.few * g.few_chunks;
+    const bool tiles = b >= few_wgs;
+    const int chunks = tiles ? g.tile_chunks : g.few_chunks, rows = tiles ? g.tile_rows : g.few_rows;
+    const int x = tiles ? b - few_wgs : b;
+    const int entries = tiles ? ((int)gridDim.x - few_wgs) / chunks : g.few;   // taken at once
+    const int row0 = x % chunks * rows;
+    const int n_few = uniform_load(&a.hdr->n_merge[0]);
+    const int first = tiles ? n_few : 0, last = tiles ? n_few + uniform_load(&a.hdr->n_merge[1]) : n_few;
+    for (int it = first + x / chunks; it < last; it += entries) {
         const Merge mg = uniform_struct(a.merge + it);
         const int n = mg.n, stride = (mg.tile ? 128 : kFewRows) * (HD + kPartPad);
         const float* base = (mg.tile ? a.tile_part : a.few_part) + (int64_t)mg.slot0 * stride;
@@ -1113,7 +1177,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
             else dst[0] = moe::f32_to_bf16(acc[0] * inv);
         };
         if (n <= kWaveSlots) {
-            for (int row = blockIdx.y * 4 + w; row < mg.rows; row += gridDim.y * 4) {
+            for (int row = row0 + w; row < min(mg.rows, row0 + rows); row += 4) {
                 const float* pr = base + row * (HD + kPartPad);
                 float2 ml = make_float2(-INFINITY, 0.f);
                 if (lane < n) ml = *reinterpret_cast<const float2*>(pr + (int64_t)lane * stride + HD);
@@ -1137,7 +1201,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
             }
             continue;
         }
-        for (int row = blockIdx.y; row < mg.rows; row += gridDim.y) {
+        for (int row = row0; row < min(mg.rows, row0 + rows); ++row) {
             const float* pr = base + row * (HD + kPartPad);
             float M = -INFINITY, L = 0.f;
             for (int s = threadIdx.x; s < n; s += 256) M = fmaxf(M, pr[(int64_t)s * stride + HD]);
@@ -1210,43 +1274,48 @@ hipError_t attn_paged_launch_append(const paged::Args* a, const paged::Source* x
 
 static float scale2(int hd) { return (float)(1.4426950408889634 / sqrt((double)hd)); }
 
-hipError_t attn_paged_launch_few(const paged::Args* a, const uint16_t* q, uint16_t* out, int grid, hipStream_t s)
+hipError_t attn_paged_launch_attend(const paged::Args* a, const uint16_t* q, uint16_t* out, const int* n, hipStream_t s)
 {
-#define FEW(HD, E) hipLaunchKernelGGL((paged::few_kernel<HD, E>), dim3(grid), dim3(256), 0, s, *a, q, out, scale2(HD))
+    auto groups = [](int v) { return (v + paged::kXcds - 1) / paged::kXcds; };
+    const paged::Split sp{groups(n[0]), {groups(n[1]), groups(n[2])}};
+    const int kinds = (n[0] ? 1 : 0) | (n[1] ? 2 : 0) | (n[2] ? 4 : 0);
+    if (!kinds) return hipSuccess;
+    const bool one = kinds == 1 || kinds == 2 || kinds == 4;
+    const int grid = one ? n[0] + n[1] + n[2] : (sp.few + sp.tile[0] + sp.tile[1]) * paged::kXcds;
+#define ATTEND(HD, E, K) hipLaunchKernelGGL((paged::attend_kernel<HD, E, K>), dim3(grid), dim3(256), 0, s, *a, q, out, scale2(HD), sp)
+#define ATTEND_ALL(HD, E) \
+    do { \
+        if (kinds == 1) ATTEND(HD, E, 1); \
+        else if (kinds == 2) ATTEND(HD, E, 2); \
+        else if (kinds == 4) ATTEND(HD, E, 4); \
+        else ATTEND(HD, E, 7); \
+    } while (0)
     if (a->hd == 128) {
-        if (a->e4m3) FEW(128, true);
-        else FEW(128, false);
+        if (a->e4m3) ATTEND_ALL(128, true);
+        else ATTEND_ALL(128, false);
     } else {
-        if (a->e4m3) FEW(64, true);
-        else FEW(64, false);
+        if (a->e4m3) ATTEND_ALL(64, true);
+        else ATTEND_ALL(64, false);
     }
-#undef FEW
+#undef ATTEND_ALL
+#undef ATTEND
     return hipGetLastError();
 }
 
-hipError_t attn_paged_launch_tile(const paged::Args* a, const uint16_t* q, uint16_t* out, int kind, int grid,
-                                  hipStream_t s)
+hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, const int* n, const int* slots, int few_rows,
+                                   hipStream_t s)
 {
-#define TILE(HD, E, PG) \
-    hipLaunchKernelGGL((paged::tile_kernel<HD, E, PG>), dim3(grid), dim3(256), 0, s, *a, a->tile[kind], kind, q, out, scale2(HD))
-    if (a->hd == 128) {
-        if (a->e4m3) { if (kind) TILE(128, true, 2); else TILE(128, true, 1); }
-        else { if (kind) TILE(128, false, 2); else TILE(128, false, 1); }
-    } else {
-        if (a->e4m3) { if (kind) TILE(64, true, 2); else TILE(64, true, 1); }
-        else { if (kind) TILE(64, false, 2); else TILE(64, false, 1); }
-    }
-#undef TILE
-    return hipGetLastError();
-}
-
-hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, int grid, int rows, int slots, hipStream_t s)
-{
-    // (a workgroup takes four rows, or one where some row has many slots)
-    const bool few = slots <= paged::kWaveSlots;
-    const dim3 g(grid, few ? (rows + 3) / 4 : rows);
-    if (a->hd == 128) hipLaunchKernelGGL(paged::merge_kernel<128>, g, dim3(256), 0, s, *a, out);
-    else hipLaunchKernelGGL(paged::merge_kernel<64>, g, dim3(256), 0, s, *a, out);
+    // four rows to a workgroup, or one where some row has many slots
+    paged::MergeGrid g{};
+    g.few_rows = slots[0] <= paged::kWaveSlots ? 4 : 1;
+    g.tile_rows = slots[1] <= paged::kWaveSlots ? 4 : 1;
+    g.few = n[0];
+    g.few_chunks = (few_rows + g.few_rows - 1) / g.few_rows;
+    g.tile_chunks = 128 / g.tile_rows;
+    const dim3 grid(g.few * g.few_chunks + n[1] * g.tile_chunks);
+    if (grid.x == 0) return hipSuccess;
+    if (a->hd == 128) hipLaunchKernelGGL(paged::merge_kernel<128>, grid, dim3(256), 0, s, *a, out, g);
+    else hipLaunchKernelGGL(paged::merge_kernel<64>, grid, dim3(256), 0, s, *a, out, g);
     return hipGetLastError();
 }
 

@@ -23,11 +23,12 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int kStages = 4;             // batches on their way to the device at once
-constexpr int kXcds = 8;
+using paged::kXcds;
 // Dividing positions makes at most twice as many shares (and partial sums)
 constexpr int64_t kFewItems = 1024;    // of few_kernel
 constexpr int64_t kTileItems = 768;    // of tile_kernel
-constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least
+constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least of a kind,
+constexpr int kGraphMerge = 16;        // and entries of its merge at once
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -74,13 +75,14 @@ Layout make_layout(const attn_paged_config* c)
     // (a range is at least half as long as the common length).
     const size_t S = c->max_seqs, T = c->max_tokens, rows = T * group;
     const size_t few_seqs = std::min(S, T), tile_seqs = std::min(S, rows / (paged::kFewRows + 1) + 1);
-    L.max_few = few_seqs * G + 2 * kFewItems;            // at least kGraphGrid, as below
+    // (at least kGraphGrid, and eight more, as a launch's workgroups are a multiple of eight)
+    L.max_few = few_seqs * G + 2 * kFewItems + kXcds;
     // (no more ranges than steps)
     const size_t few_steps = few_seqs * G * (((size_t)c->max_blocks * c->page_size + 127) / 128);
     L.few_slots = std::min<size_t>(2 * kFewItems, few_steps);
     const bool tiles = rows > (size_t)paged::kFewRows;
     for (int k = 0; k < 2; ++k)
-        L.max_tile[k] = tiles ? (rows / (128 >> k) + tile_seqs) * G + 2 * kTileItems : 0;
+        L.max_tile[k] = tiles ? (rows / (128 >> k) + tile_seqs) * G + 2 * kTileItems + kXcds : 0;
     L.tile_slots = tiles ? 2 * kTileItems : 0;
     L.max_merge = kFewItems + 2 * (tiles ? kTileItems : 0);
     size_t off = 0;
@@ -114,9 +116,9 @@ struct Batch {
     std::vector<paged::Token> tok;
     std::vector<paged::PageWork> pages;
     std::vector<Item> few, tile[2];
-    std::vector<Merge> merge;
+    std::vector<Merge> merge, tile_merge;   // tile()'s behind few()'s
     std::vector<int32_t> table;
-    int merge_rows = 0, merge_slots = 0;   // most of one entry
+    int slots[2] = {0, 0};                 // most of one entry of few()'s, of tile()'s
 };
 
 }  // namespace
@@ -129,7 +131,8 @@ struct attn_paged_ctx {
     std::vector<int32_t> written;      // per page: the call that last had it written, for set_batch
     int32_t call;
     bool set;
-    int32_t T, n_pages, n_few, n_tile[2], n_merge, merge_rows, merge_slots;
+    int32_t T, n_pages, n_few, n_tile[2], n_merge[2];
+    int slots[2];                      // the most of one merge entry
     Stage stage[kStages];
     int next_stage;
     std::string err;
@@ -329,8 +332,7 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
             for (it.kvh = 0; it.kvh < G; ++it.kvh) {
                 if (n > 1) {
                     b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, 0, 0});
-                    b.merge_rows = std::max(b.merge_rows, R);
-                    b.merge_slots = std::max(b.merge_slots, n);
+                    b.slots[0] = std::max(b.slots[0], n);
                 }
                 add_ranges(b.few, it, cuts, kFewStep, few_slot);
             }
@@ -345,9 +347,8 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
                     it.begin = 0;
                     it.end = pos0[s] + (it.row0 + it.rows - 1) / group + 1;
                     if (n > 1) {
-                        b.merge.push_back(Merge{tok0, it.row0, it.rows, it.kvh, tile_slot, n, 1, 0});
-                        b.merge_rows = std::max(b.merge_rows, (int)it.rows);
-                        b.merge_slots = std::max(b.merge_slots, n);
+                        b.tile_merge.push_back(Merge{tok0, it.row0, it.rows, it.kvh, tile_slot, n, 1, 0});
+                        b.slots[1] = std::max(b.slots[1], n);
                     }
                     add_ranges(b.tile[kind], it, bl.cuts, paged::kStep, tile_slot);
                 }
@@ -474,7 +475,7 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
     }
     divide(c, L, n_new, pos0, n_seqs, holes, b);
     if (b.few.size() > L.max_few || b.tile[0].size() > L.max_tile[0] || b.tile[1].size() > L.max_tile[1] ||
-        b.merge.size() > L.max_merge)
+        b.merge.size() + b.tile_merge.size() > L.max_merge)
         return fail(ctx, MOE_E_CAPACITY, "the batch has more shares than the workspace holds");
     if (T > 0) {
         paged::Header h{};
@@ -482,7 +483,9 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         h.n_pages = (int32_t)b.pages.size();
         h.n_few = (int32_t)b.few.size();
         for (int k = 0; k < 2; ++k) h.n_tile[k] = (int32_t)b.tile[k].size();
-        h.n_merge = (int32_t)b.merge.size();
+        h.n_merge[0] = (int32_t)b.merge.size();
+        h.n_merge[1] = (int32_t)b.tile_merge.size();
+        b.merge.insert(b.merge.end(), b.tile_merge.begin(), b.tile_merge.end());
         const struct { size_t dst; const void* src; size_t bytes; } parts[paged::kSegments] = {
             {L.hdr, &h, sizeof h},
             {L.freq, ctx->freq.data(), ctx->freq.size() * 8},
@@ -521,9 +524,9 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
     ctx->n_pages = (int32_t)b.pages.size();
     ctx->n_few = (int32_t)b.few.size();
     for (int k = 0; k < 2; ++k) ctx->n_tile[k] = (int32_t)b.tile[k].size();
-    ctx->n_merge = (int32_t)b.merge.size();
-    ctx->merge_rows = b.merge_rows;
-    ctx->merge_slots = b.merge_slots;
+    ctx->n_merge[1] = (int32_t)b.tile_merge.size();
+    ctx->n_merge[0] = (int32_t)b.merge.size() - (T > 0 ? ctx->n_merge[1] : 0);
+    for (int k = 0; k < 2; ++k) ctx->slots[k] = b.slots[k];
     ctx->set = true;
     return MOE_OK;
 }
@@ -547,19 +550,22 @@ hipError_t attn_paged_run_attend(attn_paged_ctx* ctx, int32_t layer, const uint1
                                  hipStream_t s)
 {
     const paged::Args a = layer_args(ctx, layer);
-    // a graph may replay on a longer batch: its launches have room for the
-    // shares that one may have, and the merge is there
+    // A graph may replay on a longer batch: its launches have room for the
+    // shares that one may have, and the merge is there (its entries: a
+    // sequence's and key/value head's rows, a row block's).
     const bool graph = capturing(s);
-    auto grid = [&](int n) { return graph ? std::max(n, kGraphGrid) : n; };
-    hipError_t e = hipSuccess;
-    for (int k = 0; k < 2 && e == hipSuccess; ++k)
-        if (ctx->n_tile[k]) e = attn_paged_launch_tile(&a, q, out, k, grid(ctx->n_tile[k]), s);
-    if (e == hipSuccess && ctx->n_few) e = attn_paged_launch_few(&a, q, out, grid(ctx->n_few), s);
-    if (e == hipSuccess && (ctx->n_merge || graph))
-        e = attn_paged_launch_merge(&a, out, graph ? std::max(ctx->n_merge, 64) : ctx->n_merge,
-                                    std::max(ctx->merge_rows, graph ? paged::kFewRows : 1),
-                                    graph ? INT32_MAX : ctx->merge_slots, s);
-    return e;
+    int n[3] = {ctx->n_few, ctx->n_tile[0], ctx->n_tile[1]};
+    int m[2] = {ctx->n_merge[0], ctx->n_merge[1]}, slots[2] = {ctx->slots[0], ctx->slots[1]};
+    if (graph) {
+        for (int& v : n)
+            if (v) v = std::max(v, kGraphGrid);
+        m[0] = n[0] ? std::max(m[0], kGraphMerge) : 0;
+        m[1] = n[1] || n[2] ? std::max(m[1], kGraphMerge) : 0;
+        slots[0] = slots[1] = INT32_MAX;
+    }
+    const hipError_t e = attn_paged_launch_attend(&a, q, out, n, s);
+    if (e != hipSuccess || (m[0] == 0 && m[1] == 0)) return e;
+    return attn_paged_launch_merge(&a, out, m, slots, paged::kFewRows, s);
 }
 
 size_t attn_paged_cache_bytes(const attn_paged_config* cfg)
