@@ -170,8 +170,9 @@ MOE_API const char *attn_last_error(const attn_ctx *ctx);
  * 4 exponent, 3 mantissa bits, bias 7, largest value 448, no infinities) times
  * a scale per page and key/value head, keys and values apart.  A scale is a
  * power of two, so a stored value is code * scale exactly and exactly a bf16.
- * Append sets it to 2^e, e the least integer >= -100 such that 448 * 2^e is no
- * less than any finite new value of the page.  Where the page already
+ * Append sets it to 2^e, e the least integer from -100 on such that 448 * 2^e is
+ * no less than any finite new value of the page (at most 119: values past 448 *
+ * 2^119 are stored as that).  Where the page already
  * holds earlier tokens of the sequence (the first new slot is not slot 0), the
  * scale never falls, and where it grows the earlier codes are rounded again to
  * the new one (which changes only values below 2^-6 of the new scale).  Codes
@@ -210,7 +211,7 @@ typedef struct {
  * Cache layout, per layer: K, then V, each [n_pages][n_kv_heads][page_size]
  * [head_dim] of bf16 or e4m3 codes, then with ATTN_PAGED_E4M3 the scales of K
  * and of V, each fp32 [n_pages][n_kv_heads] padded to 256 B.  A caller may
- * write pages there directly (scales: powers of two from 2^-100 to 2^120). */
+ * write pages there directly (scales: powers of two from 2^-100 to 2^119). */
 MOE_API size_t attn_paged_cache_bytes(const attn_paged_config *cfg);
 MOE_API size_t attn_paged_workspace_bytes(const attn_paged_config *cfg);
 
@@ -228,14 +229,17 @@ MOE_API moe_status attn_paged_init(const attn_paged_config *cfg, void *cache, vo
  * sequence's pages (ceil((pos0 + n_new) / page_size) entries are read).  The
  * batch's tokens are the sequences' new tokens in order, T = sum of n_new.
  * A table entry of -1 is no page: its positions are left out of the
- * attention (a row that sees no position gives zeros).
+ * attention (a row that sees no position gives zeros); append refuses a batch
+ * whose new tokens do not all have pages.
  * Enqueues one small kernel on stream that hands the batch to the device;
  * allocates no device memory (the first calls allocate pinned host memory).
  * Errors, the previous batch then staying set: MOE_E_ARG (a NULL array,
- * negative counts, ld too small, an entry outside -1 .. n_pages - 1, a new
- * token without a page, a page that two sequences or two blocks of one would
- * write), MOE_E_CAPACITY (n_seqs, T or a sequence's length beyond the
- * config's), MOE_E_STATE (stream is capturing a graph), MOE_E_HIP.
+ * negative counts, ld too small, an entry outside -1 .. n_pages - 1, a page
+ * that two sequences or two blocks of one would write), MOE_E_CAPACITY (n_seqs,
+ * T or a sequence's length beyond the config's), MOE_E_STATE (stream is
+ * capturing a graph); after MOE_E_HIP no batch is set.
+ * The calls on a context share its workspace: they go to one stream, or the
+ * caller orders them.
  * A graph captured over append and attend calls replays on the batch that is
  * set when it is replayed, which must have as many sequences and the same
  * n_new as the one set at its capture (positions and pages may differ). */
@@ -250,13 +254,14 @@ typedef enum { ATTN_QKV_F32 = 0, ATTN_QKV_BF16 = 1 } attn_qkv_type;
  * elements, ld elements apart, rows 16-byte aligned) in; q out bf16 [T][n_heads
  * head_dim]; keys and values to the pages of layer `layer`; slots of other
  * positions keep their values (see above for scales that grow).  q may not
- * overlap qkv.  Requires a batch (MOE_E_STATE); T == 0 is a no-op. */
+ * overlap qkv.  Requires a batch whose new tokens all have pages (MOE_E_STATE);
+ * T == 0 is a no-op. */
 MOE_API moe_status attn_paged_append(attn_paged_ctx *ctx, int32_t layer, const void *qkv, int64_t ld,
                                      int32_t type, uint16_t *q, moe_stream_t stream);
 
 /* Attention of the batch's T tokens, q bf16 [T][n_heads head_dim] (rotated),
  * over their sequences' positions up to their own in layer `layer`'s pages,
- * which must hold them; out bf16 [T][n_heads head_dim] (not q). */
+ * which must hold them; out bf16 [T][n_heads head_dim] may not overlap q. */
 MOE_API moe_status attn_paged_attend(attn_paged_ctx *ctx, int32_t layer, const uint16_t *q, uint16_t *out,
                                      moe_stream_t stream);
 

@@ -555,7 +555,8 @@ moe_status attn_forward_paged(attn_ctx* ctx, int32_t layer, attn_paged_ctx* cach
         p.rope_theta != c.rope_theta)
         return fail(ctx, MOE_E_SHAPE, "the cache's heads, head_dim or rope_theta are not the block's");
     if (layer < 0 || layer >= c.n_layers || layer >= p.n_layers) return fail(ctx, MOE_E_ARG, "layer out of range");
-    if (!attn_paged_has_batch(cache)) return fail(ctx, MOE_E_STATE, "no batch set on the cache");
+    if (!attn_paged_can_append(cache))
+        return fail(ctx, MOE_E_STATE, "no batch set on the cache, or one with a token that has no page");
     const int32_t T = attn_paged_tokens(cache);
     if (T > c.max_tokens) return fail(ctx, MOE_E_CAPACITY, "the batch's tokens exceed max_tokens");
     if (!ctx->loaded[layer]) return fail(ctx, MOE_E_STATE, "layer weights not loaded");

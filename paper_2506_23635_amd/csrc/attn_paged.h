@@ -15,9 +15,9 @@ constexpr int kTile = 32;          // positions of a step of one wave of few()
 constexpr int kStep = 64;          // positions of a workgroup's step of tile()
 constexpr int kPartPad = 4;        // maximum, weight and padding behind the hd sums of a partial row
 constexpr int kExpMin = -100;      // exponents of an e4m3 page's scale
-constexpr int kExpMax = 120;
+constexpr int kExpMax = 119;        // 448 * 2^119 is the largest such that is a bf16
 
-// A token: its position and its page (the slot is position % page_size).
+// A token: its position and its page (the slot is position % page_size), or -1.
 struct Token {
     int32_t pos, page;
 };
@@ -49,15 +49,14 @@ struct Item {
 struct Merge {
     int32_t tok0, row0, rows, kvh;
     int32_t slot0, n;
-    int32_t tile;      // 0: few()'s slots, 1: tile()'s
-    int32_t pad;
+    int32_t pad[2];
 };
 
 // Counts that the kernels read on the device, so that a captured launch
 // follows a batch set after the capture.
 struct Header {
     int32_t T, n_pages, n_few, n_tile[2];
-    int32_t n_merge[2];        // few()'s entries, then tile()'s
+    int32_t n_merge[2];        // few()'s entries, tile()'s
     int32_t pad;
 };
 
@@ -69,7 +68,7 @@ struct Args {
     const PageWork* pages;     // [n_pages]
     const Item* few;
     const Item* tile[2];       // row blocks of 128, of 64
-    const Merge* merge;
+    const Merge* merge[2];     // few()'s entries, tile()'s
     const int32_t* table;
     float* few_part;           // [slot][16][hd + kPartPad]
     float* tile_part;          // [slot][128][hd + kPartPad]
@@ -91,7 +90,7 @@ struct Source {
 struct Segment {
     uint64_t dst, src, bytes;   // bytes a multiple of 16
 };
-constexpr int kSegments = 9;
+constexpr int kSegments = 10;
 struct Unpack {
     const uint8_t* src;        // pinned host memory
     uint8_t* dst;              // the workspace
@@ -113,7 +112,7 @@ hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, const in
 // The batch of a paged context as the attention block needs it.
 int32_t attn_paged_tokens(const attn_paged_ctx* ctx);
 const attn_paged_config* attn_paged_cfg(const attn_paged_ctx* ctx);
-int attn_paged_has_batch(const attn_paged_ctx* ctx);
+int attn_paged_can_append(const attn_paged_ctx* ctx);   // a batch is set, and all its tokens have pages
 hipError_t attn_paged_run_append(attn_paged_ctx* ctx, int32_t layer, const paged::Source* x, uint16_t* q,
                                  hipStream_t s);
 hipError_t attn_paged_run_attend(attn_paged_ctx* ctx, int32_t layer, const uint16_t* q, uint16_t* out,

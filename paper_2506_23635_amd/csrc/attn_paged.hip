@@ -198,6 +198,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Source& x, uint
     if (head < a.H) {
         dst = q + ((int64_t)t * a.H + head) * hd;
     } else {
+        if (tok.page < 0) return;            // (a graph replayed on a batch that append itself refuses)
         const int g = turn ? head - a.H : head - n_rotated;
         const int64_t row = ((int64_t)tok.page * a.G + g) << a.shift | (tok.pos & ((1 << a.shift) - 1));
         dst = reinterpret_cast<uint16_t*>(turn ? a.k : a.v) + row * hd;
@@ -206,13 +207,13 @@ __device__ __forceinline__ void append_rows(const Args& a, const Source& x, uint
     *reinterpret_cast<uint2*>(dst + f + (turn ? half : 4)) = pack_bf16x4(v.hi);
 }
 
-// The least exponent e >= kExpMin with amax <= 448 * 2^e = 1.75 * 2^(e + 8),
-// from the bits of a finite amax >= 0: the carry of the addition is 1 where
-// the mantissa is past 1.75.
+// The least exponent e of kExpMin .. kExpMax with amax <= 448 * 2^e = 1.75 *
+// 2^(e + 8), from the bits of a finite amax >= 0: the carry of the addition is
+// 1 where the mantissa is past 1.75.  (Past kExpMax values end at 448.)
 __device__ inline int scale_exponent(float amax)
 {
     const int e = (int)((__float_as_uint(amax) + (0x7FFFFFu - 0x600000u)) >> 23) - 127 - 8;
-    return max(e, kExpMin);
+    return min(max(e, kExpMin), kExpMax);
 }
 
 __device__ inline float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
@@ -224,7 +225,7 @@ __device__ inline uint32_t code4(const float* v, float inv)
 {
     float w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = finite(v[i]) ? v[i] * inv : NAN;
+    for (int i = 0; i < 4; ++i) w[i] = finite(v[i]) ? fminf(fmaxf(v[i] * inv, -448.f), 448.f) : NAN;
     int c = __builtin_amdgcn_cvt_pk_fp8_f32(w[0], w[1], 0, false);
     c = __builtin_amdgcn_cvt_pk_fp8_f32(w[2], w[3], c, true);
     return (uint32_t)c;
@@ -612,7 +613,7 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
         };
         // steps that every row sees whole, one after another without a pause;
         // then the sequence's last ones (and all of one with missing pages)
-        const int clean = im.holes ? 0 : min(im.end, im.pos0 + 1) - kTile;   // the last start of such a step
+        const int clean = im.holes ? -1 : min(im.end, im.pos0 + 1) - kTile;   // the last start of such a step
         if (p0 <= clean) {
             pages(p0, pg);
             pages(p0 + step, pn);
@@ -658,8 +659,8 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float mk = lds.m[k][row];
+                // (a wave that has seen only NaN has no maximum, and NaN sums)
                 const float f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(mk, scale2) - Ms);
-                if (mk == -INFINITY) continue;
                 L = fmaf(lds.l[k][row], f, L);
 #pragma unroll
                 for (int i = 0; i < D; ++i) v[i] = fmaf(lds.o[k][row][d0 + i], f, v[i]);
@@ -697,11 +698,11 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 // same order by transposing LDS reads (ds_read_b64_tr_b16: 16 lanes read four
 // rows of 16 dims, and lane n ends with dim n of the four).
 //
-// Rows go through registers, a step ahead (e4m3 codes are decoded on the way).
-// (Straight from memory to LDS the compiler made every transposing read wait
-// for the next step's rows.)  A row's 16-byte chunks are swapped about by its
-// number, so that neither the 32 rows of a K read nor the four of a V read
-// meet in the same banks.
+// Rows are brought piece by piece beside the matrix products: bf16 rows of the
+// next step straight from memory to LDS, e4m3 codes of the step after that to
+// registers, decoded to LDS a step later.  A row's 16-byte chunks are swapped
+// about by its number, so that neither the 32 rows of a K read nor the four of
+// a V read meet in the same banks.
 //
 // P enters rounded to one bf16 (relative error 2^-8 at most per weight, random
 // in sign; the output's own rounding is as large): a second term would cost
@@ -709,7 +710,6 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 // follows the maximum when some score is more than 2^kLazy above it: the
 // weights are then at most 2^kLazy, which changes nothing in fp32 or bf16, and
 // most steps need no rescaling and no exchange between lanes.
-constexpr int tile_rows(int pg) { return 128 / pg; }
 constexpr float kLazy = 8.f;
 
 template <int HD>
@@ -1130,12 +1130,12 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(Args a, const uint16_t* 
 // maximum and weight of slot s, then every lane its dims of all slots); more,
 // a workgroup does, wave w adding slots w, w + 4, ..., the waves' sums in wave
 // order.  A slot without weight holds zeros.
-constexpr int kWaveSlots = 16;
-constexpr int kMaxSlots = 2 * 1024;          // kFewItems' most of one row
-
 //
 // A workgroup takes up to four rows of an entry, `chunks` workgroups an entry
 // (four rows, or one, of up to 16 of few()'s; of up to 128 of tile()'s).
+constexpr int kWaveSlots = 16;
+constexpr int kMaxSlots = 2 * 1024;          // kFewItems' most of one row
+
 struct MergeGrid {
     int few, few_chunks, tile_chunks;        // workgroups / few_chunks for few()'s entries
     int few_rows, tile_rows;                 // rows of a workgroup, 4 or 1
@@ -1153,12 +1153,15 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
     const int x = tiles ? b - few_wgs : b;
     const int entries = tiles ? ((int)gridDim.x - few_wgs) / chunks : g.few;   // taken at once
     const int row0 = x % chunks * rows;
-    const int n_few = uniform_load(&a.hdr->n_merge[0]);
-    const int first = tiles ? n_few : 0, last = tiles ? n_few + uniform_load(&a.hdr->n_merge[1]) : n_few;
-    for (int it = first + x / chunks; it < last; it += entries) {
-        const Merge mg = uniform_struct(a.merge + it);
-        const int n = mg.n, stride = (mg.tile ? 128 : kFewRows) * (HD + kPartPad);
-        const float* base = (mg.tile ? a.tile_part : a.few_part) + (int64_t)mg.slot0 * stride;
+    const Merge* list = a.merge[tiles];
+    const float* part = tiles ? a.tile_part : a.few_part;
+    const int stride = (tiles ? 128 : kFewRows) * (HD + kPartPad);
+    Merge mg = uniform_struct(list + x / chunks);
+    const int last = uniform_load(&a.hdr->n_merge[tiles]);
+    for (int it = x / chunks; it < last; it += entries) {
+        if (it != x / chunks) mg = uniform_struct(list + it);
+        const int n = mg.n;
+        const float* base = part + (int64_t)mg.slot0 * stride;
         auto add = [&](const float* row, int s, float f, float (&acc)[D]) {
             const float* pc = row + (int64_t)s * stride + lane * D;
             if constexpr (D == 2) {
@@ -1203,14 +1206,17 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
         }
         for (int row = row0; row < min(mg.rows, row0 + rows); ++row) {
             const float* pr = base + row * (HD + kPartPad);
-            float M = -INFINITY, L = 0.f;
-            for (int s = threadIdx.x; s < n; s += 256) M = fmaxf(M, pr[(int64_t)s * stride + HD]);
+            // thread s: slot s (and s + 256, ..., which are read twice)
+            auto ml_of = [&](int s) { return *reinterpret_cast<const float2*>(pr + (int64_t)s * stride + HD); };
+            const float2 own = (int)threadIdx.x < n ? ml_of(threadIdx.x) : make_float2(-INFINITY, 0.f);
+            float M = own.x, L = 0.f;
+            for (int s = threadIdx.x + 256; s < n; s += 256) M = fmaxf(M, ml_of(s).x);
             for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
             if (lane == 0) s_red[0][w] = M;
             __syncthreads();
             M = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
             for (int s = threadIdx.x; s < n; s += 256) {
-                const float2 ml = *reinterpret_cast<const float2*>(pr + (int64_t)s * stride + HD);
+                const float2 ml = s < 256 ? own : ml_of(s);
                 const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
                 s_f[s] = f;
                 L = fmaf(ml.y, f, L);
@@ -1220,11 +1226,15 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
             __syncthreads();
             L = ((s_red[1][0] + s_red[1][1]) + s_red[1][2]) + s_red[1][3];
             float acc[D] = {};
-            int s = w;
-            for (; s + 28 < n; s += 32)
+            // sixteen slots of a wave at a time, all loads together (past n:
+            // slot 0 with factor 0)
+            for (int s = w; s < n; s += 64) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) add(pr, s + 4 * u, s_f[s + 4 * u], acc);
-            for (; s < n; s += 4) add(pr, s, s_f[s], acc);
+                for (int u = 0; u < 16; ++u) {
+                    const int z = s + 4 * u;
+                    add(pr, z < n ? z : 0, z < n ? s_f[z] : 0.f, acc);
+                }
+            }
 #pragma unroll
             for (int e = 0; e < D; ++e) s_sum[w][lane * D + e] = acc[e];
             __syncthreads();

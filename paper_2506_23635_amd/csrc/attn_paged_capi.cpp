@@ -25,8 +25,8 @@ constexpr size_t kAlign = 256;
 constexpr int kStages = 4;             // batches on their way to the device at once
 using paged::kXcds;
 // Dividing positions makes at most twice as many shares (and partial sums)
-constexpr int64_t kFewItems = 1024;    // of few_kernel
-constexpr int64_t kTileItems = 768;    // of tile_kernel
+constexpr int64_t kFewItems = 1024;    // of few()
+constexpr int64_t kTileItems = 768;    // of tile()
 constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least of a kind,
 constexpr int kGraphMerge = 16;        // and entries of its merge at once
 
@@ -34,8 +34,8 @@ size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 struct Layout {
     size_t data_bytes, scale_bytes, layer_bytes, cache_bytes;   // K or V of a layer; its scales
-    size_t hdr, freq, tok, pages, few, tile[2], merge, table, few_part, tile_part, ws_bytes;
-    size_t max_few, max_tile[2], max_merge, few_slots, tile_slots;
+    size_t hdr, freq, tok, pages, few, tile[2], merge[2], table, few_part, tile_part, ws_bytes;
+    size_t max_few, max_tile[2], max_merge[2], few_slots, tile_slots;
     int shift;
 };
 
@@ -71,7 +71,7 @@ Layout make_layout(const attn_paged_config* c)
     L.layer_bytes = 2 * L.data_bytes + 2 * L.scale_bytes;
     L.cache_bytes = L.layer_bytes * c->n_layers;
     // Shares: every sequence and key/value head has one, every row block of
-    // tile_kernel, and divided positions add at most twice the division's aim
+    // tile(), and divided positions add at most twice the division's aim
     // (a range is at least half as long as the common length).
     const size_t S = c->max_seqs, T = c->max_tokens, rows = T * group;
     const size_t few_seqs = std::min(S, T), tile_seqs = std::min(S, rows / (paged::kFewRows + 1) + 1);
@@ -84,7 +84,8 @@ Layout make_layout(const attn_paged_config* c)
     for (int k = 0; k < 2; ++k)
         L.max_tile[k] = tiles ? (rows / (128 >> k) + tile_seqs) * G + 2 * kTileItems + kXcds : 0;
     L.tile_slots = tiles ? 2 * kTileItems : 0;
-    L.max_merge = kFewItems + 2 * (tiles ? kTileItems : 0);
+    L.max_merge[0] = std::max<size_t>(kFewItems, kGraphMerge);
+    L.max_merge[1] = tiles ? kTileItems : 0;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, kAlign); return o; };
     L.hdr = take(sizeof(paged::Header));
@@ -94,7 +95,8 @@ Layout make_layout(const attn_paged_config* c)
     L.few = take(L.max_few * sizeof(Item));
     L.tile[0] = take(L.max_tile[0] * sizeof(Item));
     L.tile[1] = take(L.max_tile[1] * sizeof(Item));
-    L.merge = take(L.max_merge * sizeof(Merge));
+    L.merge[0] = take(L.max_merge[0] * sizeof(Merge));
+    L.merge[1] = take(L.max_merge[1] * sizeof(Merge));
     L.table = take(S * c->max_blocks * 4 + 16);
     L.few_part = take(L.few_slots * paged::kFewRows * (hd + paged::kPartPad) * 4);
     L.tile_part = take(L.tile_slots * 128 * (hd + paged::kPartPad) * 4);
@@ -116,8 +118,9 @@ struct Batch {
     std::vector<paged::Token> tok;
     std::vector<paged::PageWork> pages;
     std::vector<Item> few, tile[2];
-    std::vector<Merge> merge, tile_merge;   // tile()'s behind few()'s
+    std::vector<Merge> merge, tile_merge;   // of few(), of tile()
     std::vector<int32_t> table;
+    bool unplaced = false;                 // a new token has no page
     int slots[2] = {0, 0};                 // most of one entry of few()'s, of tile()'s
 };
 
@@ -130,7 +133,7 @@ struct attn_paged_ctx {
     std::vector<double> freq;
     std::vector<int32_t> written;      // per page: the call that last had it written, for set_batch
     int32_t call;
-    bool set;
+    bool set, unplaced;
     int32_t T, n_pages, n_few, n_tile[2], n_merge[2];
     int slots[2];                      // the most of one merge entry
     Stage stage[kStages];
@@ -182,7 +185,7 @@ void even_cuts(int64_t steps, int64_t n, std::vector<int>& cuts)
     for (int64_t i = 1; i <= n; ++i) cuts.push_back((int)(steps * i / n));
 }
 
-// A row block of tile_kernel: the steps of 64 positions that it needs.
+// A row block of tile(): the steps of 64 positions that it needs.
 struct Block {
     int steps, rows;
     std::vector<int> cuts;
@@ -331,7 +334,7 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
             even_cuts(steps, n, cuts);
             for (it.kvh = 0; it.kvh < G; ++it.kvh) {
                 if (n > 1) {
-                    b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, 0, 0});
+                    b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, {}});
                     b.slots[0] = std::max(b.slots[0], n);
                 }
                 add_ranges(b.few, it, cuts, kFewStep, few_slot);
@@ -347,7 +350,7 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
                     it.begin = 0;
                     it.end = pos0[s] + (it.row0 + it.rows - 1) / group + 1;
                     if (n > 1) {
-                        b.tile_merge.push_back(Merge{tok0, it.row0, it.rows, it.kvh, tile_slot, n, 1, 0});
+                        b.tile_merge.push_back(Merge{tok0, it.row0, it.rows, it.kvh, tile_slot, n, {}});
                         b.slots[1] = std::max(b.slots[1], n);
                     }
                     add_ranges(b.tile[kind], it, bl.cuts, paged::kStep, tile_slot);
@@ -372,7 +375,7 @@ paged::Args layer_args(attn_paged_ctx* c, int layer)
     a.pages = reinterpret_cast<const paged::PageWork*>(c->ws + L.pages);
     a.few = reinterpret_cast<const Item*>(c->ws + L.few);
     for (int k = 0; k < 2; ++k) a.tile[k] = reinterpret_cast<const Item*>(c->ws + L.tile[k]);
-    a.merge = reinterpret_cast<const Merge*>(c->ws + L.merge);
+    for (int k = 0; k < 2; ++k) a.merge[k] = reinterpret_cast<const Merge*>(c->ws + L.merge[k]);
     a.table = reinterpret_cast<const int32_t*>(c->ws + L.table);
     a.few_part = reinterpret_cast<float*>(c->ws + L.few_part);
     a.tile_part = reinterpret_cast<float*>(c->ws + L.tile_part);
@@ -465,17 +468,18 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         b.table.insert(b.table.end(), row, row + blocks);
         for (int64_t k = pos0[i] >> L.shift; k < blocks; ++k) {
             const int32_t page = row[k];
-            if (page < 0) return fail(ctx, MOE_E_ARG, "a new token has no page");
-            if (ctx->written[page] == call) return fail(ctx, MOE_E_ARG, "a page would be written twice");
-            ctx->written[page] = call;
+            if (page >= 0 && ctx->written[page] == call) return fail(ctx, MOE_E_ARG, "a page would be written twice");
+            if (page >= 0) ctx->written[page] = call;
+            else b.unplaced = true;
             const int64_t lo = std::max<int64_t>(pos0[i], k << L.shift), hi = std::min(n_pos, (k + 1) << L.shift);
-            b.pages.push_back(paged::PageWork{page, (int32_t)(lo - (k << L.shift)), (int32_t)(hi - lo), (int32_t)b.tok.size()});
+            if (page >= 0)
+                b.pages.push_back(paged::PageWork{page, (int32_t)(lo - (k << L.shift)), (int32_t)(hi - lo), (int32_t)b.tok.size()});
             for (int64_t p = lo; p < hi; ++p) b.tok.push_back(paged::Token{(int32_t)p, page});
         }
     }
     divide(c, L, n_new, pos0, n_seqs, holes, b);
     if (b.few.size() > L.max_few || b.tile[0].size() > L.max_tile[0] || b.tile[1].size() > L.max_tile[1] ||
-        b.merge.size() + b.tile_merge.size() > L.max_merge)
+        b.merge.size() > L.max_merge[0] || b.tile_merge.size() > L.max_merge[1])
         return fail(ctx, MOE_E_CAPACITY, "the batch has more shares than the workspace holds");
     if (T > 0) {
         paged::Header h{};
@@ -485,7 +489,6 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         for (int k = 0; k < 2; ++k) h.n_tile[k] = (int32_t)b.tile[k].size();
         h.n_merge[0] = (int32_t)b.merge.size();
         h.n_merge[1] = (int32_t)b.tile_merge.size();
-        b.merge.insert(b.merge.end(), b.tile_merge.begin(), b.tile_merge.end());
         const struct { size_t dst; const void* src; size_t bytes; } parts[paged::kSegments] = {
             {L.hdr, &h, sizeof h},
             {L.freq, ctx->freq.data(), ctx->freq.size() * 8},
@@ -494,7 +497,8 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
             {L.few, b.few.data(), b.few.size() * sizeof(Item)},
             {L.tile[0], b.tile[0].data(), b.tile[0].size() * sizeof(Item)},
             {L.tile[1], b.tile[1].data(), b.tile[1].size() * sizeof(Item)},
-            {L.merge, b.merge.data(), b.merge.size() * sizeof(Merge)},
+            {L.merge[0], b.merge.data(), b.merge.size() * sizeof(Merge)},
+            {L.merge[1], b.tile_merge.data(), b.tile_merge.size() * sizeof(Merge)},
             {L.table, b.table.data(), b.table.size() * 4}};
         size_t bytes = 0;
         for (const auto& p : parts) bytes += align_up(p.bytes, 16);
@@ -513,6 +517,7 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
             u.seg[k] = paged::Segment{parts[k].dst, at, n};
             at += n;
         }
+        ctx->set = false;                                // (until the new one is on its way)
         e = attn_paged_launch_unpack(&u, s);
         if (e != hipSuccess) return hip_fail(ctx, e, "batch kernel launch");
         e = hipEventRecord(st.done, s);
@@ -525,8 +530,9 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
     ctx->n_few = (int32_t)b.few.size();
     for (int k = 0; k < 2; ++k) ctx->n_tile[k] = (int32_t)b.tile[k].size();
     ctx->n_merge[1] = (int32_t)b.tile_merge.size();
-    ctx->n_merge[0] = (int32_t)b.merge.size() - (T > 0 ? ctx->n_merge[1] : 0);
+    ctx->n_merge[0] = (int32_t)b.merge.size();
     for (int k = 0; k < 2; ++k) ctx->slots[k] = b.slots[k];
+    ctx->unplaced = b.unplaced;
     ctx->set = true;
     return MOE_OK;
 }
@@ -537,7 +543,7 @@ extern "C" {
 
 int32_t attn_paged_tokens(const attn_paged_ctx* ctx) { return ctx->T; }
 const attn_paged_config* attn_paged_cfg(const attn_paged_ctx* ctx) { return &ctx->cfg; }
-int attn_paged_has_batch(const attn_paged_ctx* ctx) { return ctx->set; }
+int attn_paged_can_append(const attn_paged_ctx* ctx) { return ctx->set && !ctx->unplaced; }
 
 hipError_t attn_paged_run_append(attn_paged_ctx* ctx, int32_t layer, const paged::Source* x, uint16_t* q,
                                  hipStream_t s)
@@ -626,6 +632,7 @@ moe_status attn_paged_append(attn_paged_ctx* ctx, int32_t layer, const void* qkv
     const int64_t n = (int64_t)(c.n_heads + 2 * c.n_kv_heads) * c.head_dim;
     if (ld < n || ld > (INT64_MAX >> 20)) return fail(ctx, MOE_E_ARG, "ld is smaller than a row of q | k | v, or too large");
     if (ld % (type == ATTN_QKV_BF16 ? 8 : 4)) return fail(ctx, MOE_E_ALIGN, "the rows of q | k | v must be 16-byte aligned");
+    if (ctx->unplaced) return fail(ctx, MOE_E_STATE, "a new token of the batch has no page");
     if (ctx->T == 0) return MOE_OK;
     if (!qkv || !q) return fail(ctx, MOE_E_ARG, "qkv or q is NULL");
     if (misaligned(qkv) || misaligned(q)) return fail(ctx, MOE_E_ALIGN, "qkv and q must be 16-byte aligned");

@@ -13,11 +13,10 @@ E4M3[[127, 255]] = np.nan
 
 
 def e4m3_codes(v):
-    """The code of the nearest e4m3 value (ties to the even code) of v, |v| <= 448, NaN to 0x7f."""
+    """The code of the nearest e4m3 value (ties to the even code; past 448: 448) of v, NaN to 0x7f."""
     v = np.asarray(v, np.float64)
     pos = E4M3[:127]
-    a = np.abs(np.where(np.isnan(v), 0.0, v))
-    assert a.max(initial=0.0) <= 448.0
+    a = np.minimum(np.abs(np.where(np.isnan(v), 0.0, v)), 448.0)
     hi = np.clip(np.searchsorted(pos, a), 1, 126)
     lo = hi - 1
     mid = (pos[lo] + pos[hi]) / 2
@@ -28,9 +27,9 @@ def e4m3_codes(v):
 
 
 def scale_exponent(amax):
-    """The least e >= -100 with amax <= 448 * 2^e."""
+    """The least e of -100 .. 119 with amax <= 448 * 2^e (119, if none is)."""
     e = -100
-    while amax > 448.0 * 2.0 ** e:
+    while amax > 448.0 * 2.0 ** e and e < 119:
         e += 1
     return e
 

@@ -48,7 +48,7 @@ class Case:
                                     flags=moe.ATTN_PAGED_E4M3 if e4m3 else 0)
         self.cfg = cfg
         self.cache = moe.PagedCache(cfg)
-        self.cache.cache.fill_(0x7F)     # NaN codes, and large bf16 values, wherever nothing is written
+        self.cache.cache.fill_(0xFF)     # NaN, as bf16, as a code and as a scale, wherever nothing is written
         self.pool = ref.Pool(n_pages, G, P, hd, e4m3)
 
     def set_batch(self):
@@ -227,3 +227,587 @@ def test_append_the_shape_of_the_model(torch):
         c.cache.append(0, qkv, q)
         torch.cuda.synchronize()
         check_append(c, qkv, q, before)
+
+
+# ------------------------------------------------------------- e4m3 values --
+
+def test_every_code_is_read_exactly(torch):
+    """One position a sequence: its weight is 1 and the output its value, code * scale, exactly
+    (under 2^120, which append never sets, the codes whose values no bf16 holds are not finite)."""
+    hd, P, exps = 128, 16, [-100, -60, -9, -1, 0, 3, 50, 119, 120]
+    codes = np.array([c for c in range(256) if c & 0x7F != 0x7F])
+    per = 2 * len(exps)                       # 254 codes in two rows of 127
+    c = Case(torch, 2, 1, hd, P, True, [(0, 1)] * per, seed=1)
+    K, V, ks, vs = c.cache.views(0)
+    want = np.zeros((per, hd))
+    for s in range(per):
+        row = np.zeros(hd, np.uint8)
+        row[:127] = codes[s % 2 * 127:s % 2 * 127 + 127]
+        pg, e = int(c.table[s, 0]), exps[s // 2]
+        V.view(torch.uint8)[pg, 0, 0] = torch.from_numpy(row).cuda()
+        K.view(torch.uint8)[pg, 0, 0] = 0
+        vs[pg, 0], ks[pg, 0] = 2.0 ** e, 1.0
+        want[s] = ref.E4M3[row] * 2.0 ** e
+    c.set_batch()
+    q = c.queries()
+    out = torch.empty_like(q)
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    got = f64(out).reshape(per, 2, hd)
+    is_bf16 = np.abs(want) < 2.0 ** 128                   # 2^128 - 2^120 is the largest
+    for j in (0, 1):
+        assert np.array_equal(got[:, j][is_bf16], want[is_bf16]) and not np.isfinite(got[:, j][~is_bf16]).any()
+    assert (~is_bf16).any()
+
+
+def test_every_rounding_to_a_code(torch):
+    """Values at, half way between and next to half way between all codes, under several scales
+    (a row's 448 * 2^e sets its page's)."""
+    hd, P, exps = 128, 16, [-100, -30, 0, 7, 111]
+    pos = ref.E4M3[:127]
+    mid = (pos[:-1] + pos[1:]) / 2
+    grid = np.concatenate([pos, mid, np.nextafter(mid.astype(np.float32), np.float32(0)).astype(np.float64),
+                           np.nextafter(mid.astype(np.float32), np.float32(1e9)).astype(np.float64)])
+    grid = np.concatenate([grid, -grid])
+    rows = np.zeros((-(-grid.size // (hd - 1)), hd))
+    rows[:, 0] = 448.0
+    rows[:, 1:].flat[:grid.size] = grid
+    n = rows.shape[0]
+    c = Case(torch, 1, 1, hd, P, True, [(0, n)] * len(exps), seed=2)
+    c.set_batch()
+    qkv = np.zeros((c.T, 3, hd))
+    for i, e in enumerate(exps):
+        qkv[i * n:(i + 1) * n, 2] = rows * 2.0 ** e
+    x = torch.from_numpy(qkv.reshape(c.T, 3 * hd)).float().cuda()
+    assert np.array_equal(f64(x).reshape(qkv.shape), qkv)                    # all of them fp32 values
+    c.cache.append(0, x, torch.empty((c.T, hd), dtype=torch.bfloat16, device="cuda"))
+    torch.cuda.synchronize()
+    _, V, _, vs = c.cache.views(0)
+    V, vs = V.view(torch.uint8).cpu().numpy(), vs.cpu().numpy()
+    for i, e in enumerate(exps):
+        want = ref.e4m3_codes(rows)
+        for t in range(n):
+            pg = c.table[i, t // P]
+            assert vs[pg, 0] == 2.0 ** e
+            assert np.array_equal(ref.E4M3[V[pg, 0, t % P]], ref.E4M3[want[t]]), (e, t)
+
+
+def test_values_that_are_not_finite_are_stored_as_nan_and_set_no_scale(torch):
+    c = Case(torch, 2, 1, 64, 16, True, [(3, 4)], seed=3)
+    c.fill_context(sigma=0.01)
+    c.set_batch()
+    x = torch.randn((4, 4 * 64), device="cuda")
+    x[1, 3 * 64 + 5], x[2, 3 * 64 + 6], x[3, 3 * 64 + 7], x[0, 2 * 64 + 9] = float("inf"), float("-inf"), float("nan"), float("nan")
+    c.cache.append(0, x, torch.empty((4, 128), dtype=torch.bfloat16, device="cuda"))
+    torch.cuda.synchronize()
+    K, V, ks, vs = (t.cpu() for t in c.cache.views(0))
+    pg = int(c.table[0, 0])
+    v = f64(V)[pg, 0, 3:7]
+    bad = np.zeros_like(v, bool)
+    bad[1, 5] = bad[2, 6] = bad[3, 7] = True
+    assert np.array_equal(np.isnan(v), bad)
+    xs = f64(x)[:, 3 * 64:]
+    assert float(vs[pg, 0]) == 2.0 ** ref.scale_exponent(np.abs(xs[~bad]).max())
+    k = f64(K)[pg, 0, 3:7]
+    assert np.isnan(k[0, [9, 41]]).all() and np.isnan(k).sum() == 2          # the pair of the rotation
+    assert np.isfinite(float(ks[pg, 0]))
+
+
+def test_the_largest_values(torch):
+    """Past 448 * 2^119 values are stored as that, which a bf16 still holds."""
+    c = Case(torch, 1, 1, 64, 16, True, [(0, 3)], seed=8)
+    c.set_batch()
+    x = torch.zeros((3, 3 * 64), device="cuda")
+    x[:, 2 * 64:2 * 64 + 4] = torch.tensor([3.4e38, -3.4e38, 448 * 2.0 ** 119, 2.0 ** 119], device="cuda")
+    c.cache.append(0, x, torch.empty((3, 64), dtype=torch.bfloat16, device="cuda"))
+    _, V, _, vs = c.cache.views(0)
+    pg = int(c.table[0, 0])
+    assert float(vs[pg, 0]) == 2.0 ** 119
+    assert np.array_equal(f64(V)[pg, 0, :3, :4], np.tile([448.0, -448.0, 448.0, 1.0], (3, 1)))
+
+
+def test_zeros_and_tiny_values(torch):
+    c = Case(torch, 1, 1, 64, 16, True, [(0, 2), (0, 2)], seed=4)
+    c.set_batch()
+    x = torch.zeros((4, 3 * 64), device="cuda")
+    x[2:, 64:] = 1e-40
+    c.cache.append(0, x, torch.empty((4, 64), dtype=torch.bfloat16, device="cuda"))
+    K, V, ks, vs = c.cache.views(0)
+    for s in range(2):
+        pg = int(c.table[s, 0])
+        assert float(ks[pg, 0]) == float(vs[pg, 0]) == 2.0 ** -100
+        assert (f64(K)[pg, 0, :2] == 0).all() and (f64(V)[pg, 0, :2] == 0).all()
+
+
+# ---------------------------------------------------------------- masks --
+
+HOLED = [(100, 1), (64, 70), (30, 3), (200, 17), (0, 1)]
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("P", [16, 32, 64])
+@pytest.mark.parametrize("shape", [(4, 2, 64), (6, 1, 128)], ids=lambda s: "%d-%d-%d" % s)
+def test_pages_that_are_missing(torch, shape, P, e4m3):
+    """Positions without a page are left out (one sequence has none but its last page)."""
+    c = Case(torch, *shape, P, e4m3, HOLED, seed=P)
+    c.fill_context(new_too=True)
+    rng = np.random.default_rng(P)
+    table = c.table.copy()
+    for s, (p0, n) in enumerate(HOLED):
+        for b in range(p0 // P):
+            if s == 0 or rng.random() < 0.5:
+                table[s, b] = -1
+    c.table = table
+    c.set_batch()
+    q = c.queries()
+    out = torch.full_like(q, 7.0)
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    c.check_attend(q, out)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(32, 1)], [(0, 2), (40, 1)], [(16, 40)], [(0, 130), (600, 1), (9, 9)]], ids=str)
+@pytest.mark.parametrize("shape", [(4, 2, 64), (6, 1, 128)], ids=lambda s: "%d-%d-%d" % s)
+def test_rows_that_see_nothing_are_zero(torch, shape, lens, e4m3):
+    """Without any page, or without the first ones: rows before the first page are zeros, the others
+    right.  Such a batch is for reading: append refuses it."""
+    c = Case(torch, *shape, 16, e4m3, lens, seed=len(lens))
+    c.fill_context(new_too=True)
+    for keep in (0, 1):                                   # the last page of each sequence, or none
+        table = np.full_like(c.table, -1)
+        for s, (p0, n) in enumerate(lens):
+            last = (p0 + n - 1) // 16
+            if keep:
+                table[s, last] = c.table[s, last]
+        whole, c.table = c.table, table
+        c.set_batch()
+        q = c.queries()
+        out = torch.full_like(q, 7.0)
+        c.cache.attend(0, q, out)
+        torch.cuda.synchronize()
+        c.check_attend(q, out)
+        if not keep:
+            assert (out == 0).all()
+        if not keep or any((p0 + n - 1) // 16 != p0 // 16 for p0, n in lens):
+            before = c.cache.cache.clone()
+            with pytest.raises(moe.MoeError) as e:
+                c.cache.append(0, rows_of(c, torch.float32), q)
+            assert e.value.status == -5
+            assert torch.equal(before, c.cache.cache)
+        c.table = whole
+
+
+def test_a_replayed_append_leaves_out_tokens_without_a_page(torch):
+    for e4m3 in (False, True):
+        c = Case(torch, 4, 2, 64, 16, e4m3, [(20, 2), (5, 1)], seed=9)
+        c.fill_context()
+        c.set_batch()
+        qkv = rows_of(c, torch.float32)
+        q = torch.empty((c.T, 256), dtype=torch.bfloat16, device="cuda")
+        c.cache.append(0, qkv, q)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.cache.append(0, qkv, q)
+        table = c.table.copy()
+        table[0] = -1
+        c.cache.set_batch([2, 1], [20, 5], table)
+        before = c.cache.cache.clone()
+        pg = int(c.table[1, 0])
+        for t in c.cache.views(0)[:2]:
+            t.view(torch.uint8 if e4m3 else torch.int16)[pg, :, 5] = 0
+        for _ in range(3):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(before, c.cache.cache)     # sequence 1 is written as before, 0 is not
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(20, 3)], [(20, 8)], [(70, 40)], [(0, 130)], [(90, 2), (10, 50)]], ids=str)
+@pytest.mark.parametrize("shape", [(4, 2, 64), (6, 1, 128)], ids=lambda s: "%d-%d-%d" % s)
+def test_a_value_that_is_not_finite_stays_with_the_rows_that_see_it(torch, shape, lens, e4m3):
+    """NaN and infinities in some new tokens' values (one dim) and one key: rows before them are
+    right, rows that see a value are not finite in its dim and right in the others, rows that see
+    the key are not finite at all."""
+    H, G, hd = shape
+    c = Case(torch, H, G, hd, 16, e4m3, lens, seed=7)
+    c.fill_context(new_too=True)
+    c.set_batch()
+    q = c.queries()
+    K, V, _, _ = c.cache.views(0)
+    clean = torch.empty_like(q)
+    c.cache.attend(0, q, clean)
+    bits = 0x7F if e4m3 else None
+    where = {}                                            # sequence -> (position of the value, of the key)
+    for s, (p0, n) in enumerate(lens):
+        pv, pk = p0 + n // 2, p0 + n - 1
+        where[s] = (pv, pk)
+        for t, p, d in ((V, pv, 5), (K, pk, 3)):
+            row = t[int(c.table[s, p // 16]), 0, p % 16]
+            if e4m3:
+                row.view(torch.uint8)[d] = bits
+            else:
+                row[d] = float("inf") if d == 5 else float("nan")
+    out = torch.full_like(q, 7.0)
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    a, b = f64(clean).reshape(-1, H, hd), f64(out).reshape(-1, H, hd)
+    at = 0
+    for s, (p0, n) in enumerate(lens):
+        for i in range(n):
+            for j in range(H):
+                x, y = a[at + i, j], b[at + i, j]
+                if j >= H // G:                           # another key/value head
+                    assert np.array_equal(x, y)
+                elif p0 + i >= where[s][1]:
+                    assert not np.isfinite(y).any()
+                elif p0 + i >= where[s][0]:
+                    assert not np.isfinite(y[5]) and np.array_equal(np.delete(x, 5), np.delete(y, 5))
+                else:
+                    assert np.array_equal(x, y), (s, i, j)
+        at += n
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")], ids=str)
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(700, 1), (9, 1)], [(20, 6)], [(70, 40)], [(300, 1), (40, 40), (10, 8)]], ids=str)
+def test_a_query_that_is_not_finite_spoils_its_own_row(torch, lens, e4m3, bad):
+    c = Case(torch, 6, 1, 128, 16, e4m3, lens, seed=15)
+    c.fill_context(new_too=True)
+    c.set_batch()
+    q = c.queries()
+    clean, out = torch.empty_like(q), torch.empty_like(q)
+    c.cache.attend(0, q, clean)
+    at = 0
+    for _, n in lens:                                     # head 2 of each sequence's last token
+        at += n
+        q[at - 1, 2 * 128 + 17] = bad
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    a, b = f64(clean).reshape(-1, 6, 128), f64(out).reshape(-1, 6, 128)
+    spoiled = np.zeros(a.shape[:2], bool)
+    spoiled[np.cumsum([n for _, n in lens]) - 1, 2] = True
+    assert np.isnan(b[spoiled]).all() and np.array_equal(a[~spoiled], b[~spoiled])
+
+
+# ------------------------------------------------------------- together --
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("shape,P", [((4, 2, 64), 16), ((6, 1, 128), 32), ((48, 8, 128), 64)], ids=str)
+def test_prompts_then_generation(torch, shape, P, e4m3):
+    """As a server runs them: prompts of several sequences, then single tokens of all of them,
+    pieces and tokens mixed, a sequence that ends and another that takes its pages; append and
+    attend on two layers, each step checked against the fp64 pages."""
+    H, G, hd = shape
+    steps = [[(0, 37), (0, 5), (0, 0)], [(37, 1), (5, 1), (0, 20)], [(38, 1), (6, 1), (20, 33)],
+             [(39, 3), (7, 1), (53, 1)], [(42, 1), (0, 18), (54, 1)]]          # the last: sequence 1 anew
+    c = Case(torch, H, G, hd, P, e4m3, [(42, 1), (0, 18), (54, 1)], seed=11, n_layers=2, max_tokens=64)
+    pools = [ref.Pool(c.cfg.n_pages, G, P, hd, e4m3) for _ in range(2)]
+    for lens in steps:
+        c.lens, c.T = lens, sum(n for _, n in lens)
+        c.set_batch()
+        for layer in range(2):
+            c.pool = pools[layer]
+            qkv = rows_of(c, torch.float32)
+            before = [t.clone() for t in c.cache.views(layer)[:2]]
+            q = torch.empty((c.T, H * hd), dtype=torch.bfloat16, device="cuda")
+            out = torch.empty_like(q)
+            c.cache.append(layer, qkv, q)
+            c.cache.attend(layer, q, out)
+            torch.cuda.synchronize()
+            check_append(c, qkv, q, before, layer)
+            # the attention is held to the pages as they are (a key's code may be the other neighbour)
+            K, V, ks, vs = c.cache.views(layer)
+            if e4m3:
+                c.pool.kc[:] = K.view(torch.uint8).cpu().numpy()
+            else:
+                c.pool.k[:] = np.where(np.isnan(f64(K)), c.pool.k, f64(K))
+            c.check_attend(q, out)
+
+
+def attn_block(torch, wl, max_tokens, heads=None):
+    cfg = moe.make_attn_config(wl.d, wl.n_heads, wl.n_kv, wl.hd, n_layers=1, max_seq=wl.max_seq, max_tokens=max_tokens,
+                               rope_theta=wl.theta, norm_eps=wl.eps)
+    att = moe.AttnLayer(cfg)
+    gamma, wqkv, wo = wl.gamma(), wl.wqkv(), wl.wo()
+    att.load_layer(0, torch.from_numpy(gamma), torch.from_numpy(wqkv.view(np.int16)), torch.from_numpy(wo.view(np.int16)))
+    return att, gamma, wqkv, wo
+
+
+def block_on_codes(c, s, x, gamma, wqkv, wo, wl):
+    """The fp64 block of sequence s (roundings as the block defines them) with its attention over
+    the device's e4m3 pages, whose new entries are checked against the block's keys and values."""
+    p0, n = c.lens[s]
+    H, G, hd = wl.n_heads, wl.n_kv, wl.hd
+    w64 = [mi.bf16_bits_to_f32(w).astype(np.float64) for w in (wqkv, wo)]
+    h = ref.bf16_round((x - x.mean(1, keepdims=True)) / np.sqrt(x.var(1, keepdims=True) + wl.eps) * gamma)
+    qkv = (h @ w64[0].reshape(wl.d, -1)).reshape(n, H + 2 * G, hd)
+    pos = np.arange(p0, p0 + n)
+    q = ref.bf16_round(ref.rotate(qkv[:, :H], pos, wl.theta))
+    K, V, ks, vs = c.cache.views(0)
+    pool = ref.Pool(c.cfg.n_pages, G, c.P, hd, True)
+    pool.kc[:], pool.vc[:] = (t.view(c.torch.uint8).cpu().numpy() for t in (K, V))
+    for dst, src in ((pool.ks, ks), (pool.vs, vs)):
+        v = src.cpu().numpy()
+        ok = np.isfinite(v) & (v > 0)
+        dst[ok] = np.log2(v[ok])
+    new = (ref.rotate(qkv[:, H:H + G], pos, wl.theta), qkv[:, H + G:])
+    for i in range(n):
+        pg, slot = c.table[s, (p0 + i) // c.P], (p0 + i) % c.P
+        for which in (0, 1):
+            for g in range(G):
+                v, e = new[which][i, g], (pool.ks, pool.vs)[which][pg, g]
+                step = np.maximum(np.abs(v), 2.0 ** (e - 6.0)) * 2.0 ** -3
+                # (h may be its other neighbour in places: a relative 2^-8 of some terms)
+                assert (np.abs(pool.value(which, pg, g)[slot] - v) <= step + 2e-2 * np.abs(v).max()).all()
+    a = ref.bf16_round(ref.attend(q, pool, p0, c.table[s])[0]).reshape(n, H * hd)
+    return x + a @ w64[1].reshape(H * hd, wl.d)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(29, 1)], [(29, 4)], [(0, 3), (17, 1), (40, 12)], [(0, 20), (31, 1)], [(5, 200), (64, 30)]], ids=str)
+def test_the_block_on_pages(torch, lens, e4m3):
+    """attn_forward_paged against the fp64 block of each sequence by itself, within the block's
+    end-to-end bars; rows of other sequences never matter.  On e4m3 pages the block is put together
+    from its parts, its attention over the pages as they are, and the pages hold the parts' keys
+    and values within a code's step."""
+    wl = mi.ATTN_WORKLOADS["attn_tiny"]
+    T = sum(n for _, n in lens)
+    c = Case(torch, wl.n_heads, wl.n_kv, wl.hd, 16, e4m3, lens, seed=5)
+    cfg = moe.make_paged_config(wl.n_heads, wl.n_kv, wl.hd, page_size=16, n_pages=c.cfg.n_pages, max_seqs=len(lens),
+                                max_tokens=T, max_blocks=c.blocks, rope_theta=wl.theta,
+                                flags=moe.ATTN_PAGED_E4M3 if e4m3 else 0)
+    c.cache = moe.PagedCache(cfg)
+    c.fill_context(sigma=1.0)
+    c.set_batch()
+    att, gamma, wqkv, wo = attn_block(torch, wl, max(T, 16))
+    x = torch.from_numpy(c.rng.standard_normal((T, wl.d))).to(torch.bfloat16).cuda()
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    g2 = 1 + 0.1 * c.rng.standard_normal(wl.d).astype(np.float32)
+    with pytest.raises(moe.MoeError):                     # no post norm loaded
+        att.forward_paged(0, c.cache, x, y, z)
+    att.forward_paged(0, c.cache, x, y)
+    first = y.clone()
+    att.load_post_norm(0, torch.from_numpy(g2))
+    att.forward_paged(0, c.cache, x, y, z)
+    torch.cuda.synchronize()
+    assert torch.equal(first.view(torch.int16), y.view(torch.int16))
+    at = 0
+    for s, (p0, n) in enumerate(lens):
+        kc, vc = np.zeros((wl.max_seq + 300, wl.n_kv, wl.hd), np.uint16), np.zeros((wl.max_seq + 300, wl.n_kv, wl.hd), np.uint16)
+        for p in range(p0):
+            for which, dst in ((0, kc), (1, vc)):
+                v = np.stack([c.pool.value(which, c.table[s, p // 16], g)[p % 16] for g in range(wl.n_kv)])
+                dst[p] = (v.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)
+        xs = x[at:at + n].cpu().view(torch.int16).numpy().view(np.uint16)
+        if e4m3:
+            want = block_on_codes(c, s, f64(x[at:at + n]), gamma, wqkv, wo, wl)
+        else:
+            want = oracle.attention_block(xs, gamma, wqkv, wo, kc, vc, p0, wl.n_heads, wl.n_kv, wl.eps, wl.theta)["y64"]
+        got = f64(y[at:at + n])
+        rel = np.linalg.norm(got - want) / np.linalg.norm(want)
+        assert rel <= 2e-3 and np.abs(got - want).max() <= 1e-2 * max(1.0, np.abs(want).max()), (s, p0, n)
+        at += n
+    zr = f64(y)
+    zr = (zr - zr.mean(1, keepdims=True)) / np.sqrt(zr.var(1, keepdims=True) + wl.eps) * g2
+    assert (np.abs(f64(z) - zr) <= ref.BF16 * np.abs(zr) * 2 + 1e-5).all()
+
+
+def test_a_sequence_alone_and_in_a_batch_give_the_same_block(torch):
+    """One token each: the projections and the attention of a sequence do not see the others (the
+    position ranges, and with them the last bits, may differ: the bf16 outputs by a step)."""
+    wl = mi.ATTN_WORKLOADS["attn_tiny"]
+    lens = [(20, 1), (3, 1), (47, 1)]
+    c = Case(torch, wl.n_heads, wl.n_kv, wl.hd, 16, False, lens, seed=6)
+    cfg = moe.make_paged_config(wl.n_heads, wl.n_kv, wl.hd, page_size=16, n_pages=c.cfg.n_pages, max_seqs=3, max_tokens=3,
+                                max_blocks=c.blocks, rope_theta=wl.theta)
+    c.cache = moe.PagedCache(cfg)
+    c.fill_context()
+    att, *_ = attn_block(torch, wl, 16)
+    x = torch.randn((3, wl.d), device="cuda").to(torch.bfloat16)
+    c.set_batch()
+    y = torch.empty_like(x)
+    att.forward_paged(0, c.cache, x, y)
+    for s in range(3):
+        c.cache.set_batch([1], [lens[s][0]], c.table[s:s + 1])
+        ys = torch.empty_like(x[:1])
+        att.forward_paged(0, c.cache, x[s:s + 1].contiguous(), ys)
+        d = np.abs(f64(ys) - f64(y[s:s + 1]))
+        assert (d <= 2 * ref.BF16 * np.abs(f64(ys)) + 1e-6).all()
+
+
+# ------------------------------------------------ graphs, streams, memory --
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [1, 40, 2]], ids=str)
+def test_graph_replays_follow_the_batch(torch, new, e4m3):
+    """append and attend captured once, replayed on the batches of five steps (longer contexts,
+    more ranges, other pages), eager work in between: the eager results, bit for bit."""
+    H, G, hd, P = 6, 1, 128, 16
+    ctx = [[10, 3, 50], [300, 31, 900], [301, 0, 16], [2000, 700, 5], [5000, 64, 3000]]
+    last = [(max(s[i] for s in ctx), new[i]) for i in range(3)]
+    c = Case(torch, H, G, hd, P, e4m3, last, seed=13)
+    c.fill_context()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    T = sum(new)
+    nqkv = (H + 2 * G) * hd
+    qkv = torch.empty((T, nqkv), device="cuda")
+    q, out = (torch.full((T, H * hd), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    start = c.cache.cache.clone()
+
+    def batch(i):
+        c.cache.set_batch(new, ctx[i], c.table)
+        qkv.copy_(torch.randn((T, nqkv), generator=g, device="cuda"))
+
+    batch(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.cache.append(0, qkv, q)
+        c.cache.attend(0, q, out)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.append(0, qkv, q)
+        c.cache.attend(0, q, out)
+        with pytest.raises(moe.MoeError) as e:
+            c.cache.set_batch(new, ctx[0], c.table)
+        assert e.value.status == -5
+    for i in [0, 1, 2, 3, 4, 4, 1]:
+        batch(i)
+        c.cache.cache.copy_(start)
+        c.cache.append(0, qkv, q)
+        c.cache.attend(0, q, out)
+        torch.cuda.synchronize()
+        want = [q.clone(), out.clone(), c.cache.cache.clone()]
+        c.cache.cache.copy_(start)
+        q.fill_(7.0)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, [q, out, c.cache.cache]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
+        torch.randn(1000, device="cuda").sum().item()
+
+
+def test_two_contexts_on_two_streams(torch):
+    """Two caches, each on a stream of its own at the same time, many steps: as one after the other."""
+    cases = [Case(torch, 4, 2, 64, 16, e, [(500, 1), (37, 20)], seed=s) for s, e in ((21, False), (22, True))]
+    streams = [torch.cuda.Stream() for _ in cases]
+    data = []
+    for c in cases:
+        c.fill_context()
+        data.append((rows_of(c, torch.float32), *(torch.empty((c.T, 256), dtype=torch.bfloat16, device="cuda") for _ in range(2))))
+
+    def step(c, x, q, out):
+        c.set_batch()
+        c.cache.append(0, x, q)
+        c.cache.attend(0, q, out)
+    want = []
+    for c, d in zip(cases, data):
+        step(c, *d)
+        torch.cuda.synchronize()
+        want.append(d[2].clone())
+        d[2].zero_()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c, d, st in zip(cases, data, streams):
+            with torch.cuda.stream(st):
+                step(c, *d)
+    torch.cuda.synchronize()
+    for d, w in zip(data, want):
+        assert torch.equal(d[2].view(torch.int16), w.view(torch.int16))
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_nothing_is_written_outside(torch, e4m3):
+    """Cache, workspace, q and out inside patterned margins."""
+    H, G, hd, P, lens = 48, 8, 128, 16, [(900, 1), (30, 100), (0, 2), (333, 9)]
+    c = Case(torch, H, G, hd, P, e4m3, lens, seed=31)
+    cb, wb = moe.attn_paged_cache_bytes(c.cfg), moe.attn_paged_workspace_bytes(c.cfg)
+    pad = 1 << 16
+
+    def guarded(n):
+        t = torch.full((n + 2 * pad,), 0xA5, dtype=torch.uint8, device="cuda")
+        return t, t[pad:pad + n]
+    (call, cin), (wall, win) = guarded(cb), guarded(wb)
+    qall, qin = guarded(c.T * H * hd * 2)
+    oall, oin = guarded(c.T * H * hd * 2)
+    c.cache = moe.PagedCache(c.cfg, cache=cin, workspace=win)
+    c.fill_context()
+    c.set_batch()
+    q, out = (t.view(torch.bfloat16).view(c.T, H * hd) for t in (qin, oin))
+    c.cache.append(0, rows_of(c, torch.float32), q)
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    for t in (call, wall, qall, oall):
+        assert (t[:pad] == 0xA5).all() and (t[-pad:] == 0xA5).all()
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_pages_behind_four_gigabytes(torch, e4m3):
+    """A pool whose keys alone pass 2^32 bytes and 2^31 elements; a sequence on its last pages."""
+    H, G, hd, P = 48, 8, 128, 256
+    n_pages = (1 << 32) // (G * P * hd * (1 if e4m3 else 2)) + 64
+    cfg = moe.make_paged_config(H, G, hd, page_size=P, n_pages=n_pages, max_seqs=2, max_tokens=64, max_blocks=4,
+                                rope_theta=THETA, flags=moe.ATTN_PAGED_E4M3 if e4m3 else 0)
+    lens = [(300, 1), (10, 30)]
+    c = Case(torch, H, G, hd, P, e4m3, lens, seed=41)
+    big = {int(p): n_pages - 1 - i for i, p in enumerate(c.table[c.table >= 0])}
+    pool = c.pool
+    c.cache = moe.PagedCache(cfg)
+    small = c.table.copy()
+    c.fill_context_at = None
+    K, V, ks, vs = c.cache.views(0)
+    for s, (p0, n) in enumerate(lens):
+        k, v = (c.rng.standard_normal((p0, G, hd)) for _ in range(2))
+        pool.append(k, v, 0, small[s])
+    for p, b in big.items():
+        if e4m3:
+            K.view(torch.uint8)[b] = torch.from_numpy(pool.kc[p]).cuda()
+            V.view(torch.uint8)[b] = torch.from_numpy(pool.vc[p]).cuda()
+            ks[b] = torch.from_numpy(2.0 ** pool.ks[p].astype(np.float64)).float().cuda()
+            vs[b] = torch.from_numpy(2.0 ** pool.vs[p].astype(np.float64)).float().cuda()
+        else:
+            K[b] = torch.from_numpy(pool.k[p]).to(torch.bfloat16).cuda()
+            V[b] = torch.from_numpy(pool.v[p]).to(torch.bfloat16).cuda()
+    table = np.array([[big.get(int(p), -1) for p in row] for row in small], np.int32)
+    c.cache.set_batch([n for _, n in lens], [p for p, _ in lens], table)
+    qkv = rows_of(c, torch.float32)
+    q = torch.empty((c.T, H * hd), dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    c.cache.append(0, qkv, q)
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    x = f64(qkv).reshape(-1, H + 2 * G, hd)
+    pos = np.concatenate([np.arange(p, p + n) for p, n in lens])
+    turned = ref.rotate(x[:, :H + G], pos, THETA)
+    at = 0
+    for s, (p0, n) in enumerate(lens):
+        pool.append(turned[at:at + n, H:], x[at:at + n, H + G:], p0, small[s])
+        at += n
+    for p, b in big.items():                              # the keys as they are stored
+        if e4m3:
+            assert (K.view(torch.uint8)[b].cpu().numpy() != pool.kc[p]).mean() <= 1e-3
+            pool.kc[p] = K.view(torch.uint8)[b].cpu().numpy()
+        else:
+            pool.k[p] = f64(K[b])
+    c.table = small
+    c.check_attend(q, out)
+
+
+def test_a_batch_of_nothing(torch):
+    c = Case(torch, 4, 2, 64, 16, False, [(3, 1), (0, 0)], seed=51)
+    q = torch.full((1, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(moe.MoeError) as e:
+        c.cache.attend(0, q, torch.empty_like(q))
+    assert e.value.status == -5                           # no batch yet
+    for lens in ([], [(5, 0), (0, 0)]):
+        c.cache.set_batch([n for _, n in lens], [p for p, _ in lens], c.table[:0] if not lens else np.zeros((2, 1), np.int32))
+        out = torch.full_like(q, 7.0)
+        c.cache.append(0, torch.empty((0, 512), device="cuda"), q)
+        c.cache.attend(0, q, out)
+        torch.cuda.synchronize()
+        assert (out == 7.0).all() and (q == 7.0).all()
