@@ -27,6 +27,7 @@ using paged::kXcds;
 // Dividing positions makes at most twice as many shares (and partial sums)
 constexpr int64_t kFewItems = 1024;    // of few()
 constexpr int64_t kTileItems = 768;    // of tile()
+constexpr int kFewStep = 4 * paged::kTile;   // positions of a workgroup's step of few()
 constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least of a kind,
 constexpr int kGraphMerge = 16;        // and entries of its merge at once
 
@@ -78,7 +79,7 @@ Layout make_layout(const attn_paged_config* c)
     // (at least kGraphGrid, and eight more, as a launch's workgroups are a multiple of eight)
     L.max_few = few_seqs * G + 2 * kFewItems + kXcds;
     // (no more ranges than steps)
-    const size_t few_steps = few_seqs * G * (((size_t)c->max_blocks * c->page_size + 127) / 128);
+    const size_t few_steps = few_seqs * G * (((size_t)c->max_blocks * c->page_size + kFewStep - 1) / kFewStep);
     L.few_slots = std::min<size_t>(2 * kFewItems, few_steps);
     const bool tiles = rows > (size_t)paged::kFewRows;
     for (int k = 0; k < 2; ++k)
@@ -250,6 +251,30 @@ void divide_blocks(std::vector<Block>& blocks, int G)
     }
 }
 
+// The length in steps of 128 positions of few()'s shares: one that makes
+// kFewItems of them, unless whole sequences take no longer.  Whole, they are
+// played through as sharing the memory's rate, each of them at one step per
+// 1.1 us at the most; divided, all shares end together, and the merge comes
+// after them.  (One token after 256, 511, 1023 and 2047 positions: whole 7.0,
+// 8.4, 12.5 and 25 us, divided 10.2, 10.6, 10.6 and 10.8; 8 sequences of 300 to
+// 1000: 16.9 and 12.6, 32 of them: 21.4 and 25.2; 64 of 300 to 3000: 86 and 81.)
+int64_t few_length(std::vector<int>& steps, int G, double step_bytes)
+{
+    constexpr double kStepUs = 1.1, kMergeUs = 4.5, kRate = 6.4e6;
+    if (steps.empty()) return 1;
+    std::sort(steps.begin(), steps.end());
+    int64_t total = 0;
+    double whole = 0.0;
+    for (size_t i = 0; i < steps.size(); ++i) {
+        total += (int64_t)steps[i] * G;
+        const double active = (double)(steps.size() - i) * G;
+        whole += (steps[i] - (i ? steps[i - 1] : 0)) * std::max(kStepUs, active * step_bytes / kRate);
+    }
+    const int64_t len = (total + kFewItems - 1) / kFewItems;
+    const double divided = std::max(len * kStepUs, total * step_bytes / kRate) + kMergeUs;
+    return whole < 0.9 * divided ? steps.back() : len;   // (the tail is slower than played through)
+}
+
 // Longest shares first: the workgroups are handed out in order.
 bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.begin; }
 
@@ -296,15 +321,13 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
 {
     const int G = c.n_kv_heads, group = c.n_heads / G;
     auto blocks_of = [&](int s) { return (int)(((int64_t)pos0[s] + n_new[s] + c.page_size - 1) >> L.shift); };
-    // few rows: every wave takes steps of 32 positions, a workgroup 128
-    constexpr int kFewStep = 4 * paged::kTile;
-    int64_t few_total = 0;
+    std::vector<int> few_steps;                          // of each sequence
     std::vector<Block> blocks;                           // of one key/value head
     for (int s = 0; s < n_seqs; ++s) {
         const int64_t R = (int64_t)n_new[s] * group, n_pos = (int64_t)pos0[s] + n_new[s];
         if (R == 0) continue;
         if (R <= paged::kFewRows) {
-            few_total += (n_pos + kFewStep - 1) / kFewStep * G;
+            few_steps.push_back((int)((n_pos + kFewStep - 1) / kFewStep));
             continue;
         }
         const int rows = R <= 64 ? 64 : 128;
@@ -313,7 +336,7 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
             blocks.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0), {}});
         }
     }
-    const int64_t few_len = std::max<int64_t>(1, (few_total + kFewItems - 1) / kFewItems);
+    const int64_t few_len = few_length(few_steps, G, (double)kFewStep * c.head_dim * (c.flags & ATTN_PAGED_E4M3 ? 2 : 4));
     divide_blocks(blocks, G);
     std::vector<int> cuts;
     size_t block = 0;                                    // the sequence's first of `blocks`
