@@ -715,6 +715,10 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 // follows the maximum when some score is more than 2^kLazy above it: the
 // weights are then at most 2^kLazy, which changes nothing in fp32 or bf16, and
 // most steps need no rescaling and no exchange between lanes.
+//
+// A wave in its matrix products goes before its SIMD's other wave, so that the
+// two fall out of step and one's softmax runs beside the other's products (a
+// prompt of 2048 tokens: 66.7 us, at equal priority 70.3).
 constexpr float kLazy = 8.f;
 
 template <int HD>
@@ -925,6 +929,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                 };
 #pragma unroll
                 for (int k = 0; k < kAhead; ++k) read_k(k);
+                __builtin_amdgcn_s_setprio(1);
                 // V of the first 16 positions, and then always 16 ahead
                 u32x4_t av[2][DB];
                 auto read_v = [&](int i) {
@@ -946,6 +951,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                     bring(k, buf ^ kBuf);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                __builtin_amdgcn_s_setprio(0);
                 const int pw0 = p0 + pg * NB * 32;       // the wave's first position
                 if (pw0 + NB * 32 - 1 > lim_w0 || im.holes) {
                     uint32_t holes = 0u;                 // runs of 16 positions without a page
@@ -991,6 +997,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
 #pragma unroll
                 for (int e = 0; e < 4; ++e) weights(0, e);
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int i = 0; i < 2 * NB; ++i) {
                     if (i + 1 < 2 * NB) read_v(i + 1);
@@ -1004,6 +1011,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
+                __builtin_amdgcn_s_setprio(0);
             }
         }
         // (what was brought again is done with the LDS)
