@@ -415,11 +415,6 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
     constexpr int ES = kE4m3 ? 1 : 2;
     constexpr int KW = kE4m3 ? HD / 64 : NC; // 16-byte loads per K row and lane
     constexpr int VW = D * ES / 4;           // words per V row and lane
-    // Nothing is read twice, so loads pass the caches by; but a K row of 128
-    // e4m3 dims is one cache line that two loads take half each (one token
-    // after 131071 positions: 48.8 us with its lines kept, 52.4 without; bf16
-    // rows, two lines: 64 sequences of 300 to 3000 positions 87 and 83).
-    constexpr bool kKeepK = kE4m3 && HD == 128;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int group = a.H / a.G, P = 1 << a.shift;
@@ -470,7 +465,7 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
                 const int64_t row = (head << a.shift) + (pb & (P - 1)) + min(r, n_pos - 1 - pb);
                 const uint8_t* kb = a.k + row * (HD * ES) + g * 16;
 #pragma unroll
-                for (int c = 0; c < KW; ++c) kr[s][c] = kKeepK ? ld16(kb + c * 64) : ld16_nt(kb + c * 64);
+                for (int c = 0; c < KW; ++c) kr[s][c] = ld16_nt(kb + c * 64);
                 if constexpr (kE4m3) ksc[s] = uniform_load(a.k_scale + head);
             }
         };

@@ -255,9 +255,10 @@ void divide_blocks(std::vector<Block>& blocks, int G)
 // kFewItems of them, unless whole sequences take no longer.  Whole, they are
 // played through as sharing the memory's rate, each of them at one step per
 // 1.1 us at the most; divided, all shares end together, and the merge comes
-// after them.  (One token after 256, 511, 1023 and 2047 positions: whole 7.0,
-// 8.4, 12.5 and 25 us, divided 10.2, 10.6, 10.6 and 10.8; 8 sequences of 300 to
-// 1000: 16.9 and 12.6, 32 of them: 21.4 and 25.2; 64 of 300 to 3000: 86 and 81.)
+// after them.  (bf16, from memory: one token after 256, 511, 1023 and 2047
+// positions whole 8.0, 10.9, 17.5 and 31 us, divided 11.0, 11.1, 11.5 and 12.0;
+// 8 sequences of 300 to 1000 whole 17.5, divided 13.5; 32 of them 21.9 and
+// 25.9; 64 of 300 to 3000 88 and 82.)
 int64_t few_length(std::vector<int>& steps, int G, double step_bytes)
 {
     constexpr double kStepUs = 1.1, kMergeUs = 4.5, kRate = 6.4e6;
