@@ -277,8 +277,10 @@ MOE_API const char *attn_paged_last_error(const attn_paged_ctx *ctx);
  * `cache`, x and y bf16 [T, d] (y may be x), layer `layer` of both contexts;
  * with z not NULL also z = norm2(y), as attn_forward_norm.  The contexts must
  * agree in n_heads, n_kv_heads, head_dim and rope_theta (MOE_E_SHAPE) and
- * share one device; T <= max_tokens of ctx, whose own cache is not used.  Errors as
- * attn_forward and attn_forward_norm; MOE_E_STATE without a batch. */
+ * share one device; T <= max_tokens of ctx, whose own cache is not used.
+ * (attn_intermediates then finds no q | k | v in the order it names.)  Errors
+ * as attn_forward and attn_forward_norm; MOE_E_STATE without a batch that
+ * append takes. */
 MOE_API moe_status attn_forward_paged(attn_ctx *ctx, int32_t layer, attn_paged_ctx *cache, const uint16_t *x,
                                       uint16_t *y, uint16_t *z, moe_stream_t stream);
 

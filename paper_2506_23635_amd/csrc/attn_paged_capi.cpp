@@ -123,6 +123,7 @@ struct Batch {
     std::vector<int32_t> table;
     bool unplaced = false;                 // a new token has no page
     int slots[2] = {0, 0};                 // most of one entry of few()'s, of tile()'s
+    int all_slots[2] = {0, 0};
 };
 
 }  // namespace
@@ -384,6 +385,8 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
         tok0 += n_new[s];
         table += n_new[s] > 0 ? blocks_of(s) : 0;
     }
+    b.all_slots[0] = few_slot;
+    b.all_slots[1] = tile_slot;
     std::stable_sort(b.few.begin(), b.few.end(), longer);
     by_xcd(b.tile[0]);
     by_xcd(b.tile[1]);
@@ -503,7 +506,8 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
     }
     divide(c, L, n_new, pos0, n_seqs, holes, b);
     if (b.few.size() > L.max_few || b.tile[0].size() > L.max_tile[0] || b.tile[1].size() > L.max_tile[1] ||
-        b.merge.size() > L.max_merge[0] || b.tile_merge.size() > L.max_merge[1])
+        b.merge.size() > L.max_merge[0] || b.tile_merge.size() > L.max_merge[1] ||
+        (size_t)b.all_slots[0] > L.few_slots || (size_t)b.all_slots[1] > L.tile_slots)
         return fail(ctx, MOE_E_CAPACITY, "the batch has more shares than the workspace holds");
     if (T > 0) {
         paged::Header h{};

@@ -637,6 +637,117 @@ def test_a_sequence_alone_and_in_a_batch_give_the_same_block(torch):
         assert (d <= 2 * ref.BF16 * np.abs(f64(ys)) + 1e-6).all()
 
 
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(29, 1), (8, 2)], [(0, 20), (31, 1)]], ids=str)
+def test_the_block_in_place_and_captured(torch, lens, e4m3):
+    """y may be x; and the block replays on the batches of later steps."""
+    wl = mi.ATTN_WORKLOADS["attn_tiny"]
+    T, ends = sum(n for _, n in lens), [(p + 40, n) for p, n in lens]
+    c = Case(torch, wl.n_heads, wl.n_kv, wl.hd, 16, e4m3, ends, seed=8)
+    c.cache = moe.PagedCache(moe.make_paged_config(wl.n_heads, wl.n_kv, wl.hd, page_size=16, n_pages=c.cfg.n_pages,
+                                                   max_seqs=2, max_tokens=T, max_blocks=c.blocks, rope_theta=wl.theta,
+                                                   flags=moe.ATTN_PAGED_E4M3 if e4m3 else 0))
+    c.fill_context(sigma=1.0)
+    att, *_ = attn_block(torch, wl, 16 if T <= 16 else 32)
+    new = [n for _, n in lens]
+    start = c.cache.cache.clone()
+    x = torch.from_numpy(c.rng.standard_normal((T, wl.d))).to(torch.bfloat16).cuda()
+    buf, y = x.clone(), torch.empty_like(x)
+    c.cache.set_batch(new, [p for p, _ in lens], c.table)
+    att.forward_paged(0, c.cache, x, y)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        att.forward_paged(0, c.cache, buf, buf)
+    for more in (0, 1, 17, 40, 3):
+        c.cache.set_batch(new, [p + more for p, _ in lens], c.table)
+        c.cache.cache.copy_(start)
+        att.forward_paged(0, c.cache, x, y)
+        want = c.cache.cache.clone()
+        c.cache.cache.copy_(start)
+        buf.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(buf.view(torch.int16), y.view(torch.int16)) and torch.equal(want, c.cache.cache), more
+
+
+def test_the_block_refuses_a_batch_it_has_no_room_for(torch):
+    wl = mi.ATTN_WORKLOADS["attn_tiny"]
+    c = Case(torch, wl.n_heads, wl.n_kv, wl.hd, 16, False, [(0, 17)], seed=10)
+    cache = moe.PagedCache(moe.make_paged_config(wl.n_heads, wl.n_kv, wl.hd, page_size=16, n_pages=c.cfg.n_pages,
+                                                 max_tokens=32, max_blocks=c.blocks, rope_theta=wl.theta))
+    att, *_ = attn_block(torch, wl, 16)
+    x = torch.zeros((17, wl.d), dtype=torch.bfloat16, device="cuda")
+    for new, table, status in ((17, c.table, -4), (16, np.full_like(c.table, -1), -5)):
+        cache.set_batch([new], [0], table)
+        with pytest.raises(moe.MoeError) as e:
+            att.forward_paged(0, cache, x, torch.empty_like(x))
+        assert e.value.status == status
+
+
+def test_calls_with_the_wrong_tensors_are_refused(torch):
+    c = Case(torch, 4, 2, 64, 16, False, [(3, 2)], seed=12)
+    c.set_batch()
+    q, out = (torch.zeros((2, 256), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    qkv = torch.zeros((2, 512), device="cuda")
+    before = c.cache.cache.clone()
+    for bad in (qkv.half(), qkv.cpu(), qkv[:1], qkv[:, :504], torch.zeros((2, 1024), device="cuda")[:, ::2],
+                torch.zeros((2, 514), device="cuda")[:, :512], torch.zeros(1025, device="cuda")[1:].view(2, 512)):
+        with pytest.raises(moe.MoeError):
+            c.cache.append(0, bad, q)
+    for bad in (q.float(), q.cpu(), q[:1], torch.zeros((256, 2), dtype=torch.bfloat16, device="cuda").t()):
+        with pytest.raises(moe.MoeError):
+            c.cache.append(0, qkv, bad)
+        with pytest.raises(moe.MoeError):
+            c.cache.attend(0, bad, out)
+        with pytest.raises(moe.MoeError):
+            c.cache.attend(0, q, bad)
+    with pytest.raises(moe.MoeError):
+        c.cache.attend(0, q, q)
+    with pytest.raises(moe.MoeError):
+        c.cache.set_batch([1], [0], torch.zeros((1, 1), dtype=torch.int32, device="cuda"))
+    for n_new, pos0, table in (([1, 1], [0], [[0], [0]]), ([1], [0], [0]), ([[1]], [[0]], [[0]]), ([1], [0], [[0], [1]])):
+        with pytest.raises(moe.MoeError):
+            c.cache.set_batch(n_new, pos0, table)
+    torch.cuda.synchronize()
+    assert torch.equal(before, c.cache.cache)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [2, 40])
+def test_the_last_positions(torch, n, e4m3):
+    """The largest positions that a config allows, 2^24 - 256 on, in a sequence whose other pages
+    are missing: the rotation by them, and attention over the last page alone."""
+    H, G, hd, P, blocks = 4, 2, 64, 256, 65536
+    p0 = blocks * P - P
+    cache = moe.PagedCache(moe.make_paged_config(H, G, hd, page_size=P, n_pages=3, max_tokens=n, max_blocks=blocks,
+                                                 rope_theta=THETA, flags=moe.ATTN_PAGED_E4M3 if e4m3 else 0))
+    cache.cache.fill_(0xFF)
+    table = np.full((1, blocks), -1, np.int32)
+    table[0, -1] = 2
+    cache.set_batch([n], [p0], table)
+    c = Case(torch, H, G, hd, P, e4m3, [(0, n)], seed=14)
+    c.cache, c.table, c.pool = cache, np.array([[2]], np.int32), ref.Pool(3, G, P, hd, e4m3)
+    qkv = rows_of(c, torch.float32)
+    q = torch.empty((n, H * hd), dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    cache.append(0, qkv, q)
+    cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    x = f64(qkv).reshape(n, H + 2 * G, hd)
+    turned, err = ref.rotate(x[:, :H + G], p0 + np.arange(n), THETA), ref.rotation_error(x[:, :H + G])
+    assert (np.abs(f64(q).reshape(n, H, hd) - turned[:, :H]) <= ref.BF16 * np.abs(turned[:, :H]) + (1 + ref.BF16) * err[:, :H] + 1e-37).all()
+    c.pool.append(turned[:, H:], x[:, H + G:], 0, [2])
+    K, V, ks, vs = cache.views(0)
+    if e4m3:
+        assert (K.view(torch.uint8)[2, :, :n].cpu().numpy() != c.pool.kc[2, :, :n]).mean() <= 1e-3
+        c.pool.kc[2] = K.view(torch.uint8)[2].cpu().numpy()
+    else:
+        assert (np.abs(f64(K)[2, :, :n] - c.pool.k[2, :, :n]) <= (ref.BF16 * 2 * np.abs(c.pool.k[2, :, :n]) + (1 + ref.BF16) * err[:, H:].transpose(1, 0, 2) + 1e-37)).all()
+        c.pool.k[2, :, :n] = f64(K)[2, :, :n]
+    c.check_attend(q, out)
+
+
 # ------------------------------------------------ graphs, streams, memory --
 
 @pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
