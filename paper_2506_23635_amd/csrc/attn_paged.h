@@ -87,13 +87,16 @@ struct Source {
     int n_split, bf16, packed;
 };
 
+// A batch's arrays lie one after another in pinned host memory, each from a
+// multiple of 16 bytes on, and go to places of their own in the workspace.
 struct Segment {
-    uint64_t dst, src, bytes;   // bytes a multiple of 16
+    uint64_t dst, src;
 };
 constexpr int kSegments = 10;
 struct Unpack {
-    const uint8_t* src;        // pinned host memory
-    uint8_t* dst;              // the workspace
+    const uint8_t* src;
+    uint8_t* dst;
+    uint64_t bytes;            // of all, a multiple of 16
     Segment seg[kSegments];
 };
 

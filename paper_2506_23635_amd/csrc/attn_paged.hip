@@ -81,11 +81,12 @@ __device__ __forceinline__ void lds_barrier()
 
 __global__ __launch_bounds__(256) void unpack_kernel(Unpack u)
 {
-    for (int s = 0; s < kSegments; ++s) {
-        const u32x4_t* src = reinterpret_cast<const u32x4_t*>(u.src + u.seg[s].src);
-        u32x4_t* dst = reinterpret_cast<u32x4_t*>(u.dst + u.seg[s].dst);
-        const uint64_t n = u.seg[s].bytes / 16;
-        for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) dst[i] = src[i];
+    for (uint64_t at = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 16; at < u.bytes; at += (uint64_t)gridDim.x * 4096) {
+        uint64_t dst = 0;                    // of the last segment that begins at or before it
+#pragma unroll
+        for (int s = 0; s < kSegments; ++s)
+            if (u.seg[s].src <= at) dst = u.seg[s].dst + (at - u.seg[s].src);
+        *reinterpret_cast<u32x4_t*>(u.dst + dst) = ld16(u.src + at);
     }
 }
 
@@ -1170,14 +1171,14 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
         if (it != x / chunks) mg = uniform_struct(list + it);
         const int n = mg.n;
         const float* base = part + (int64_t)mg.slot0 * stride;
-        auto add = [&](const float* row, int s, float f, float (&acc)[D]) {
-            const float* pc = row + (int64_t)s * stride + lane * D;
+        auto load = [&](const float* row, int s, float (&v)[D]) {
+            const float* p = row + (int64_t)s * stride + lane * D;
             if constexpr (D == 2) {
-                const float2 v = *reinterpret_cast<const float2*>(pc);
-                acc[0] = fmaf(v.x, f, acc[0]);
-                acc[1] = fmaf(v.y, f, acc[1]);
+                const float2 t = *reinterpret_cast<const float2*>(p);
+                v[0] = t.x;
+                v[1] = t.y;
             } else {
-                acc[0] = fmaf(pc[0], f, acc[0]);
+                v[0] = p[0];
             }
         };
         auto write = [&](int row, const float (&acc)[D], float L) {
@@ -1188,28 +1189,37 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
             else dst[0] = moe::f32_to_bf16(acc[0] * inv);
         };
         if (n <= kWaveSlots) {
-            for (int row = row0 + w; row < min(mg.rows, row0 + rows); row += 4) {
-                const float* pr = base + row * (HD + kPartPad);
-                float2 ml = make_float2(-INFINITY, 0.f);
-                if (lane < n) ml = *reinterpret_cast<const float2*>(pr + (int64_t)lane * stride + HD);
-                float M = ml.x;
-                for (int off = kWaveSlots / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-                const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
-                float L = ml.y * f;
-                for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
-                L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
-                float acc[D] = {};
-                auto add_all = [&](auto most) {                         // (past n: slot 0 with factor 0)
+            // `most` slots (past n: slot 0 with factor 0), their sums loaded
+            // along with the maxima
+            auto add_all = [&](auto most) {
+                constexpr int kMost = decltype(most)::value;
+                for (int row = row0 + w; row < min(mg.rows, row0 + rows); row += 4) {
+                    const float* pr = base + row * (HD + kPartPad);
+                    float2 ml = make_float2(-INFINITY, 0.f);
+                    if (lane < n) ml = *reinterpret_cast<const float2*>(pr + (int64_t)lane * stride + HD);
+                    float v[kMost][D];
 #pragma unroll
-                    for (int s = 0; s < decltype(most)::value; ++s)
-                        add(pr, s < n ? s : 0, __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s)), acc);
-                };
-                if (n <= 2) add_all(std::integral_constant<int, 2>{});
-                else if (n <= 5) add_all(std::integral_constant<int, 5>{});
-                else if (n <= 8) add_all(std::integral_constant<int, 8>{});
-                else add_all(std::integral_constant<int, kWaveSlots>{});
-                write(row, acc, L);
-            }
+                    for (int s = 0; s < kMost; ++s) load(pr, s < n ? s : 0, v[s]);
+                    float M = ml.x;
+                    for (int off = kWaveSlots / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+                    const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+                    float L = ml.y * f;
+                    for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
+                    L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
+                    float acc[D] = {};
+#pragma unroll
+                    for (int s = 0; s < kMost; ++s) {
+                        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+#pragma unroll
+                        for (int e = 0; e < D; ++e) acc[e] = fmaf(v[s][e], fs, acc[e]);
+                    }
+                    write(row, acc, L);
+                }
+            };
+            if (n <= 2) add_all(std::integral_constant<int, 2>{});
+            else if (n <= 5) add_all(std::integral_constant<int, 5>{});
+            else if (n <= 8) add_all(std::integral_constant<int, 8>{});
+            else add_all(std::integral_constant<int, kWaveSlots>{});
             continue;
         }
         for (int row = row0; row < min(mg.rows, row0 + rows); ++row) {
@@ -1240,7 +1250,10 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
 #pragma unroll
                 for (int u = 0; u < 16; ++u) {
                     const int z = s + 4 * u;
-                    add(pr, z < n ? z : 0, z < n ? s_f[z] : 0.f, acc);
+                    float v[D];
+                    load(pr, z < n ? z : 0, v);
+#pragma unroll
+                    for (int e = 0; e < D; ++e) acc[e] = fmaf(v[e], z < n ? s_f[z] : 0.f, acc[e]);
                 }
             }
 #pragma unroll
@@ -1265,9 +1278,7 @@ extern "C" {
 
 hipError_t attn_paged_launch_unpack(const paged::Unpack* u, hipStream_t s)
 {
-    uint64_t most = 0;
-    for (const paged::Segment& g : u->seg) most = g.bytes > most ? g.bytes : most;
-    const uint64_t blocks = (most / 16 + 255) / 256;
+    const uint64_t blocks = (u->bytes / 16 + 255) / 256;
     hipLaunchKernelGGL(paged::unpack_kernel, dim3((unsigned)(blocks < 1 ? 1 : blocks > 256 ? 256 : blocks)), dim3(256), 0, s, *u);
     return hipGetLastError();
 }

@@ -542,9 +542,10 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
             const size_t n = align_up(parts[k].bytes, 16);
             if (parts[k].bytes) std::memcpy(st.mem + at, parts[k].src, parts[k].bytes);
             if (n > parts[k].bytes) std::memset(st.mem + at + parts[k].bytes, 0, n - parts[k].bytes);
-            u.seg[k] = paged::Segment{parts[k].dst, at, n};
+            u.seg[k] = paged::Segment{parts[k].dst, at};
             at += n;
         }
+        u.bytes = at;
         ctx->set = false;                                // (until the new one is on its way)
         e = attn_paged_launch_unpack(&u, s);
         if (e != hipSuccess) return hip_fail(ctx, e, "batch kernel launch");
