@@ -11,6 +11,7 @@ namespace paged {
 
 constexpr int kXcds = 8;
 constexpr int kFewRows = 16;       // query rows of one key/value head that few() takes at once
+constexpr int kFewRuns = 512;      // workgroups that divided positions of few() go to: two per CU
 constexpr int kTile = 32;          // positions of a step of one wave of few()
 constexpr int kStep = 64;          // positions of a workgroup's step of tile()
 constexpr int kPartPad = 4;        // maximum, weight and padding behind the hd sums of a partial row
@@ -41,7 +42,7 @@ struct Item {
     int32_t table;     // its pages, from here in the table
     int32_t slot;      // where the unnormalised sums go, or -1: all of the positions, result to out
     int32_t holes;     // whether some of its table entries are -1
-    int32_t pad;
+    int32_t next;      // of few()'s: the workgroup's next share in the list, or -1
 };
 
 // Rows whose positions several items share: their partial sums are slots

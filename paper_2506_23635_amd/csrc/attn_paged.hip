@@ -404,10 +404,11 @@ constexpr uint32_t kOnes = 0x3F803F80u;      // two bf16 ones
 // block i takes dim D r + i for row r: an 8 x D transposition inside the lane.
 // P enters as two bf16 terms (the second the rounding of what the first left:
 // 16 bits), since the matrix cores have time: the loads bound the kernel (64
-// sequences of 8000 to 16000 positions in bf16 495 us, 6.4 TB/s, where a plain
-// read does 7.1; one token after 131071 in e4m3 47 us, 5.7: a share takes some 3
-// us to its first scores, and only two workgroups' registers fit a CU).
-// b, nb: this workgroup among those that take such shares, and their number.
+// sequences of 8000 to 16000 positions in bf16 484 us, 6.5 TB/s, where a plain
+// read does 7.1; one token after 131071 in e4m3 45 us, 6.0: a share takes some 3
+// us to its first scores).
+// b, nb: this workgroup among those that take such shares, and their number (it
+// takes the runs of shares that begin with shares b, b + nb, ... of the list).
 template <int HD>
 struct FewLds {
     float o[4][kFewRows][HD + 4];            // the waves' sums, maxima and weights
@@ -429,8 +430,8 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
     // (the first share is read along with the count, not after it: the list
     // has room for every workgroup of the grid)
     Item im = uniform_struct(a.few + b);
-    const int n_items = uniform_load(&a.hdr->n_few);
-    for (int it = b; it < n_items; it += nb) {
+    const int n_first = uniform_load(&a.hdr->n_few);
+    for (int it = b, first = b; it < n_first || it != first;) {
         if (it != b) im = uniform_struct(a.few + it);
         const int32_t* table = a.table + im.table;
         const int R = im.rows, kvh = im.kvh, n_pos = im.n_pos;
@@ -693,6 +694,8 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
             }
         }
         __syncthreads();                                 // the LDS sums are written again
+        if (im.next < 0) first += nb;
+        it = im.next < 0 ? first : im.next;
     }
 }
 
@@ -1161,7 +1164,7 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(Args a, const uint16_t* 
 // slots, by latency, 3.7 to 5.
 constexpr int kWaveSlots = 16;
 constexpr int kTileRows = 2;                 // rows of tile()'s that a wave takes at once
-constexpr int kMaxSlots = 2 * 1024;          // kFewItems' most of one row
+constexpr int kMaxSlots = kFewRuns;          // the most of one row
 
 struct MergeGrid {
     int few, few_chunks, tile_chunks;        // workgroups / few_chunks for few()'s entries

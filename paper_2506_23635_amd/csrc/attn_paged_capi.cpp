@@ -24,9 +24,9 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kStages = 4;             // batches on their way to the device at once
 using paged::kXcds;
-// Dividing positions makes at most twice as many shares (and partial sums)
-constexpr int64_t kFewItems = 1024;    // of few()
-constexpr int64_t kTileItems = 768;    // of tile()
+using paged::kFewRuns;
+// Dividing positions makes at most twice as many shares (and partial sums) of tile()
+constexpr int64_t kTileItems = 768;
 constexpr int kFewStep = 4 * paged::kTile;   // positions of a workgroup's step of few()
 constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least of a kind,
 constexpr int kGraphMerge = 16;        // and entries of its merge at once
@@ -72,20 +72,21 @@ Layout make_layout(const attn_paged_config* c)
     L.layer_bytes = 2 * L.data_bytes + 2 * L.scale_bytes;
     L.cache_bytes = L.layer_bytes * c->n_layers;
     // Shares: every sequence and key/value head has one, every row block of
-    // tile(), and divided positions add at most twice the division's aim
-    // (a range is at least half as long as the common length).
+    // tile(), and divided positions add one for each end of a run of few(), and
+    // of tile() at most twice the division's aim (a range is at least half as
+    // long as the common length).
     const size_t S = c->max_seqs, T = c->max_tokens, rows = T * group;
     const size_t few_seqs = std::min(S, T), tile_seqs = std::min(S, rows / (paged::kFewRows + 1) + 1);
     // (at least kGraphGrid, and eight more, as a launch's workgroups are a multiple of eight)
-    L.max_few = few_seqs * G + 2 * kFewItems + kXcds;
-    // (no more ranges than steps)
+    L.max_few = few_seqs * G + kFewRuns + kXcds;
+    // (every end of a run makes a share, and its neighbour, two of several; no more than steps)
     const size_t few_steps = few_seqs * G * (((size_t)c->max_blocks * c->page_size + kFewStep - 1) / kFewStep);
-    L.few_slots = std::min<size_t>(2 * kFewItems, few_steps);
+    L.few_slots = std::min<size_t>(2 * kFewRuns, few_steps);
     const bool tiles = rows > (size_t)paged::kFewRows;
     for (int k = 0; k < 2; ++k)
         L.max_tile[k] = tiles ? (rows / (128 >> k) + tile_seqs) * G + 2 * kTileItems + kXcds : 0;
     L.tile_slots = tiles ? 2 * kTileItems : 0;
-    L.max_merge[0] = std::max<size_t>(kFewItems, kGraphMerge);
+    L.max_merge[0] = std::max<size_t>(kFewRuns, kGraphMerge);
     L.max_merge[1] = tiles ? kTileItems : 0;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off = align_up(off + bytes, kAlign); return o; };
@@ -122,6 +123,7 @@ struct Batch {
     std::vector<Merge> merge, tile_merge;   // of few(), of tile()
     std::vector<int32_t> table;
     bool unplaced = false;                 // a new token has no page
+    int n_runs = 0;                        // of few()
     int slots[2] = {0, 0};                 // most of one entry of few()'s, of tile()'s
     int all_slots[2] = {0, 0};
 };
@@ -252,33 +254,92 @@ void divide_blocks(std::vector<Block>& blocks, int G)
     }
 }
 
-// The length in steps of 128 positions of few()'s shares: one that makes
-// kFewItems of them, unless whole sequences take no longer.  Whole, they are
-// played through as sharing the memory's rate, each of them at one step per
-// 1.1 us at the most; divided, all shares end together, and the merge comes
-// after them.  (bf16, from memory: one token after 256, 511, 1023 and 2047
-// positions whole 8.0, 10.9, 17.5 and 31 us, divided 11.0, 11.1, 11.5 and 12.0;
-// 8 sequences of 300 to 1000 whole 17.5, divided 13.5; 32 of them 21.9 and
-// 25.9; 64 of 300 to 3000 88 and 82.)
-int64_t few_length(std::vector<int>& steps, int G, double step_bytes)
-{
-    constexpr double kStepUs = 1.1, kMergeUs = 4.5, kRate = 6.4e6;
-    if (steps.empty()) return 1;
-    std::sort(steps.begin(), steps.end());
-    int64_t total = 0;
-    double whole = 0.0;
-    for (size_t i = 0; i < steps.size(); ++i) {
-        total += (int64_t)steps[i] * G;
-        const double active = (double)(steps.size() - i) * G;
-        whole += (steps[i] - (i ? steps[i - 1] : 0)) * std::max(kStepUs, active * step_bytes / kRate);
-    }
-    const int64_t len = (total + kFewItems - 1) / kFewItems;
-    const double divided = std::max(len * kStepUs, total * step_bytes / kRate) + kMergeUs;
-    return whole < 0.9 * divided ? steps.back() : len;   // (the tail is slower than played through)
-}
-
 // Longest shares first: the workgroups are handed out in order.
 bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.begin; }
+
+// Divides the shares of few(), given as whole sequences (one per sequence and
+// key/value head), into the runs of kFewRuns workgroups, equal in steps: a CU
+// holds about 64 KB of loads in flight, whether of one workgroup or of two, so
+// that the positions of every CU have to be as many (320 equal sequences and
+// heads, one or two a CU, stream 4.7 TB/s; 256 and 512 6.3).  A run takes the
+// sequences one after another, long and short ones in turn, each start counted
+// as kStart steps; a sequence that runs share is added up by the merge.
+// Sequences stay whole, a workgroup each, where that is estimated to take no
+// longer: a CU does a step in step_us at least, or all of them stream at kRate;
+// divided, a merge comes after them.  (bf16, from memory: one token after 256,
+// 511, 1023 and 2047 positions whole 7.9, 10.9, 17.5 and 31 us, divided 11.0,
+// 10.2, 10.4 and 11.0; 32 sequences of 300 to 1000 whole 21.8, 25.9 in equal
+// ranges; 64 of 300 to 3000 whole 87, in equal ranges of each sequence 81, in
+// runs 78; 8 of 3000 to 8000 45.3 and 42.2.)
+void divide_few(std::vector<Item>& whole, double step_bytes, Batch& b, int& slot)
+{
+    constexpr double kStart = 0.5, kCus = 256.0, kRate = 6.3e6, kMergeUs = 4.5;
+    const double step_us = std::max(0.65, 1.68 * step_bytes / 65536);
+    auto steps = [](const Item& it) { return (it.end + kFewStep - 1) / kFewStep; };
+    std::stable_sort(whole.begin(), whole.end(), longer);
+    int64_t total = 0;
+    for (const Item& it : whole) total += steps(it);
+    b.n_runs = (int)whole.size();
+    b.few = whole;
+    if (whole.empty() || whole.size() >= 4 * kFewRuns) return;   // (so many even out)
+    const int longest = steps(whole[0]);
+    const double stream_us = total * step_bytes / kRate, mean = total / kCus;
+    const double busiest = whole.size() <= kCus ? longest : std::max((double)longest, 1.28 * (mean + longest / 4.0));
+    const double whole_us = std::max(stream_us, step_us * busiest);
+    const double divided_us = std::max(stream_us, step_us * std::ceil(mean)) + kMergeUs;
+    if (whole_us < 0.9 * divided_us) return;
+    std::vector<int> first;                              // of each run
+    for (double room_all = std::max(kStart + 1.0, (total + kStart * (whole.size() + kFewRuns)) / kFewRuns);; room_all *= 1.02) {
+        b.few.clear();
+        b.merge.clear();
+        first.assign(1, 0);
+        slot = b.slots[0] = 0;
+        double room = room_all;
+        for (size_t i = 0; i < whole.size(); ++i) {
+            Item it = whole[i % 2 ? whole.size() - 1 - i / 2 : i / 2];
+            const int end = it.end, n = steps(it);
+            const size_t at = b.few.size();
+            for (int from = 0; from < n;) {
+                int k = n - from;
+                if (k + kStart > room + std::min(1.0, room_all / 8)) {   // (rather a little longer than one more start)
+                    k = (int)(room - kStart);
+                    if (k < 1 || (k < 2 && room < room_all)) {
+                        first.push_back((int)b.few.size());
+                        room = room_all;
+                        continue;
+                    }
+                }
+                it.begin = from * kFewStep;
+                it.end = std::min(end, (from + k) * kFewStep);
+                b.few.push_back(it);
+                from += k;
+                room -= k + kStart;
+            }
+            const int pieces = (int)(b.few.size() - at);
+            if (pieces == 1) continue;
+            b.merge.push_back(Merge{it.tok0, 0, it.rows, it.kvh, slot, pieces, {}});
+            b.slots[0] = std::max(b.slots[0], pieces);
+            for (int k = 0; k < pieces; ++k) b.few[at + k].slot = slot++;
+        }
+        if (first.size() <= (size_t)kFewRuns) break;
+    }
+    // the list: the runs' first shares, then the others
+    std::vector<Item> shares(b.few.size());
+    const int runs = (int)first.size();
+    int more = runs;
+    first.push_back((int)b.few.size());
+    for (int r = 0; r < runs; ++r) {
+        int to = r;
+        for (int i = first[r]; i < first[r + 1]; ++i) {
+            shares[to] = b.few[i];
+            const int next = i + 1 < first[r + 1] ? more++ : -1;
+            shares[to].next = next;
+            to = next;
+        }
+    }
+    b.few = std::move(shares);
+    b.n_runs = runs;
+}
 
 // One list for eight XCDs, workgroup b going to XCD b % 8: the shares in
 // order (those of one sequence and key/value head together, so that an L2
@@ -323,24 +384,18 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
 {
     const int G = c.n_kv_heads, group = c.n_heads / G;
     auto blocks_of = [&](int s) { return (int)(((int64_t)pos0[s] + n_new[s] + c.page_size - 1) >> L.shift); };
-    std::vector<int> few_steps;                          // of each sequence
     std::vector<Block> blocks;                           // of one key/value head
     for (int s = 0; s < n_seqs; ++s) {
-        const int64_t R = (int64_t)n_new[s] * group, n_pos = (int64_t)pos0[s] + n_new[s];
-        if (R == 0) continue;
-        if (R <= paged::kFewRows) {
-            few_steps.push_back((int)((n_pos + kFewStep - 1) / kFewStep));
-            continue;
-        }
+        const int64_t R = (int64_t)n_new[s] * group;
+        if (R <= paged::kFewRows) continue;
         const int rows = R <= 64 ? 64 : 128;
         for (int64_t r0 = 0; r0 < R; r0 += rows) {
             const int64_t last = std::min(r0 + rows, R);
             blocks.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0), {}});
         }
     }
-    const int64_t few_len = few_length(few_steps, G, (double)kFewStep * c.head_dim * (c.flags & ATTN_PAGED_E4M3 ? 2 : 4));
     divide_blocks(blocks, G);
-    std::vector<int> cuts;
+    std::vector<Item> whole;                             // of few()
     size_t block = 0;                                    // the sequence's first of `blocks`
     int few_slot = 0, tile_slot = 0, tok0 = 0, table = 0;
     for (int s = 0; s < n_seqs; ++s) {
@@ -354,16 +409,8 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
         if (R > 0 && R <= paged::kFewRows) {
             it.rows = R;
             it.end = n_pos;
-            const int64_t steps = (n_pos + kFewStep - 1) / kFewStep;
-            const int n = (int)((steps + few_len - 1) / few_len);
-            even_cuts(steps, n, cuts);
-            for (it.kvh = 0; it.kvh < G; ++it.kvh) {
-                if (n > 1) {
-                    b.merge.push_back(Merge{tok0, 0, R, it.kvh, few_slot, n, {}});
-                    b.slots[0] = std::max(b.slots[0], n);
-                }
-                add_ranges(b.few, it, cuts, kFewStep, few_slot);
-            }
+            it.slot = it.next = -1;
+            for (it.kvh = 0; it.kvh < G; ++it.kvh) whole.push_back(it);
         } else if (R > 0) {
             const int kind = R <= 64, rows = 128 >> kind, n_blocks = (R + rows - 1) / rows;
             for (it.kvh = 0; it.kvh < G; ++it.kvh)
@@ -385,9 +432,9 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
         tok0 += n_new[s];
         table += n_new[s] > 0 ? blocks_of(s) : 0;
     }
+    divide_few(whole, (double)kFewStep * c.head_dim * (c.flags & ATTN_PAGED_E4M3 ? 2 : 4), b, few_slot);
     b.all_slots[0] = few_slot;
     b.all_slots[1] = tile_slot;
-    std::stable_sort(b.few.begin(), b.few.end(), longer);
     by_xcd(b.tile[0]);
     by_xcd(b.tile[1]);
 }
@@ -513,7 +560,7 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         paged::Header h{};
         h.T = (int32_t)T;
         h.n_pages = (int32_t)b.pages.size();
-        h.n_few = (int32_t)b.few.size();
+        h.n_few = b.n_runs;
         for (int k = 0; k < 2; ++k) h.n_tile[k] = (int32_t)b.tile[k].size();
         h.n_merge[0] = (int32_t)b.merge.size();
         h.n_merge[1] = (int32_t)b.tile_merge.size();
@@ -556,7 +603,7 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
     }
     ctx->T = (int32_t)T;
     ctx->n_pages = (int32_t)b.pages.size();
-    ctx->n_few = (int32_t)b.few.size();
+    ctx->n_few = b.n_runs;
     for (int k = 0; k < 2; ++k) ctx->n_tile[k] = (int32_t)b.tile[k].size();
     ctx->n_merge[1] = (int32_t)b.tile_merge.size();
     ctx->n_merge[0] = (int32_t)b.merge.size();
