@@ -1157,18 +1157,17 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(Args a, const uint16_t* 
 // a workgroup does, wave w adding slots w, w + 4, ..., the waves' sums in wave
 // order.  A slot without weight holds zeros.
 //
-// A workgroup takes four rows of an entry of few()'s, eight of tile()'s, or one
-// where some row has many slots; `chunks` workgroups an entry of 16 or 128
+// A workgroup takes four rows of an entry of few()'s, or one where some row has
+// many slots, and eight of tile()'s (sixteen with two slots); `chunks` workgroups an entry of 16 or 128
 // rows.  Bound by its reads, which mostly come from the last-level cache: five
 // ranges of 500 tokens' rows, 65 MB, take 13.4 us (one row a wave 15.4); few
 // slots, by latency, 3.7 to 5.
 constexpr int kWaveSlots = 16;
-constexpr int kTileRows = 2;                 // rows of tile()'s that a wave takes at once
 constexpr int kMaxSlots = kFewRuns;          // the most of one row
 
 struct MergeGrid {
     int few, few_chunks, tile_chunks;        // workgroups / few_chunks for few()'s entries
-    int few_rows, tile_rows;                 // rows of a workgroup, 4 or 8, or 1
+    int few_rows, tile_rows;                 // rows of a workgroup
 };
 
 template <int HD>
@@ -1212,47 +1211,53 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
         if (n <= kWaveSlots) {
             // `most` slots (past n: slot 0 with factor 0), their sums loaded
             // along with the maxima
-            auto add_all = [&](auto most, auto pairs) {
-                constexpr int kMost = decltype(most)::value, kPairs = decltype(pairs)::value;
+            auto add_all = [&](auto most, auto rows_at_once) {
+                constexpr int kMost = decltype(most)::value, kRows = decltype(rows_at_once)::value;
                 const int end = min(mg.rows, row0 + rows);
-                if (row0 + w >= end) return;
-                float2 ml[kPairs];
-                float v[kPairs][kMost][D];
+                for (int r0 = row0 + w; r0 < end; r0 += 4 * kRows) {
+                    float2 ml[kRows];
+                    float v[kRows][kMost][D];
 #pragma unroll
-                for (int k = 0; k < kPairs; ++k) {                      // (past the end: row0 + w again)
-                    const int row = row0 + w + 4 * k < end ? row0 + w + 4 * k : row0 + w;
-                    const float* pr = base + row * (HD + kPartPad);
-                    ml[k] = make_float2(-INFINITY, 0.f);
-                    if (lane < n) ml[k] = *reinterpret_cast<const float2*>(pr + (int64_t)lane * stride + HD);
+                    for (int k = 0; k < kRows; ++k) {                      // (past the end: r0 again)
+                        const int row = r0 + 4 * k < end ? r0 + 4 * k : r0;
+                        const float* pr = base + row * (HD + kPartPad);
+                        ml[k] = make_float2(-INFINITY, 0.f);
+                        if (lane < n) ml[k] = *reinterpret_cast<const float2*>(pr + (int64_t)lane * stride + HD);
 #pragma unroll
-                    for (int s = 0; s < kMost; ++s) load(pr, s < n ? s : 0, v[k][s]);
-                }
-#pragma unroll
-                for (int k = 0; k < kPairs; ++k) {
-                    float M = ml[k].x;
-                    for (int off = kWaveSlots / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-                    const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - M);
-                    float L = ml[k].y * f;
-                    for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
-                    L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
-                    float acc[D] = {};
-#pragma unroll
-                    for (int s = 0; s < kMost; ++s) {
-                        const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
-#pragma unroll
-                        for (int e = 0; e < D; ++e) acc[e] = fmaf(v[k][s][e], fs, acc[e]);
+                        for (int s = 0; s < kMost; ++s) load(pr, s < n ? s : 0, v[k][s]);
                     }
-                    if (row0 + w + 4 * k < end) write(row0 + w + 4 * k, acc, L);
+#pragma unroll
+                    for (int k = 0; k < kRows; ++k) {
+                        float M = ml[k].x;
+                        for (int off = kWaveSlots / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
+                        const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - M);
+                        float L = ml[k].y * f;
+                        for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
+                        L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
+                        float acc[D] = {};
+#pragma unroll
+                        for (int s = 0; s < kMost; ++s) {
+                            const float fs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s));
+#pragma unroll
+                            for (int e = 0; e < D; ++e) acc[e] = fmaf(v[k][s][e], fs, acc[e]);
+                        }
+                        if (r0 + 4 * k < end) write(r0 + 4 * k, acc, L);
+                    }
                 }
             };
-            auto add_any = [&](auto pairs) {
-                if (n <= 2) add_all(std::integral_constant<int, 2>{}, pairs);
-                else if (n <= 5) add_all(std::integral_constant<int, 5>{}, pairs);
-                else if (n <= 8) add_all(std::integral_constant<int, 8>{}, pairs);
-                else add_all(std::integral_constant<int, kWaveSlots>{}, pairs);
-            };
-            if (tiles) add_any(std::integral_constant<int, kTileRows>{});
-            else add_any(std::integral_constant<int, 1>{});
+            using std::integral_constant;
+            if (!tiles) {                                // four rows for four waves
+                if (n <= 5) add_all(integral_constant<int, 5>{}, integral_constant<int, 1>{});
+                else add_all(integral_constant<int, kWaveSlots>{}, integral_constant<int, 1>{});
+            } else if (n <= 2) {
+                add_all(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+            } else if (n <= 5) {
+                add_all(integral_constant<int, 5>{}, integral_constant<int, 2>{});
+            } else if (n <= 8) {
+                add_all(integral_constant<int, 8>{}, integral_constant<int, 2>{});
+            } else {
+                add_all(integral_constant<int, kWaveSlots>{}, integral_constant<int, 1>{});
+            }
             continue;
         }
         for (int row = row0; row < min(mg.rows, row0 + rows); ++row) {
@@ -1370,7 +1375,7 @@ hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, const in
     // four rows to a workgroup, or one where some row has many slots
     paged::MergeGrid g{};
     g.few_rows = slots[0] <= paged::kWaveSlots ? 4 : 1;
-    g.tile_rows = slots[1] <= paged::kWaveSlots ? 4 * paged::kTileRows : 1;
+    g.tile_rows = slots[1] <= 2 ? 16 : 8;
     g.few = n[0];
     g.few_chunks = (few_rows + g.few_rows - 1) / g.few_rows;
     g.tile_chunks = 128 / g.tile_rows;

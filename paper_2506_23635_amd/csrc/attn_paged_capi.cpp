@@ -28,6 +28,7 @@ using paged::kFewRuns;
 // Dividing positions makes at most twice as many shares (and partial sums) of tile()
 constexpr int64_t kTileItems = 768;
 constexpr int kFewStep = 4 * paged::kTile;   // positions of a workgroup's step of few()
+constexpr double kStreamRate = 6.3e6;  // bytes/us that few() reads where every CU has its share
 constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least of a kind,
 constexpr int kGraphMerge = 16;        // and entries of its merge at once
 
@@ -189,69 +190,114 @@ void even_cuts(int64_t steps, int64_t n, std::vector<int>& cuts)
     for (int64_t i = 1; i <= n; ++i) cuts.push_back((int)(steps * i / n));
 }
 
-// A row block of tile(): the steps of 64 positions that it needs.
+// A row block of tile(): the steps of 64 positions that it needs, and the
+// number of ranges that they are divided into.
 struct Block {
-    int steps, rows;
-    std::vector<int> cuts;
+    int steps, rows, ranges;
 };
+
+// How long workgroups take together, their times alone on a CU given longest
+// first: handed out in that order, one to each CU, then a second, then to
+// whichever has one done; two on a CU each take `slow` times as long.
+double play(const std::vector<double>& times, int cus, double slow)
+{
+    struct Cu {
+        double left[2], at;
+        int n;
+        unsigned version;                                // of its event in the queue
+    };
+    typedef std::pair<double, std::pair<int, unsigned>> Event;
+    std::vector<Cu> cu(cus, Cu{});
+    std::priority_queue<Event, std::vector<Event>, std::greater<Event>> events;
+    size_t next = 0;
+    double end = 0.0;
+    auto fill = [&](Cu& c) {
+        if (next < times.size()) c.left[c.n++] = times[next++];
+    };
+    auto schedule = [&](int x) {
+        Cu& c = cu[x];
+        ++c.version;
+        if (c.n == 1) events.push({c.at + c.left[0], {x, c.version}});
+        if (c.n == 2) events.push({c.at + std::min(c.left[0], c.left[1]) * slow, {x, c.version}});
+    };
+    for (int k = 0; k < 2; ++k)
+        for (Cu& c : cu) fill(c);
+    for (int x = 0; x < cus; ++x) schedule(x);
+    while (!events.empty()) {
+        const Event e = events.top();
+        events.pop();
+        Cu& c = cu[e.second.first];
+        if (e.second.second != c.version) continue;
+        const double done = (e.first - c.at) / (c.n == 2 ? slow : 1.0);
+        c.at = end = e.first;
+        int n = 0;
+        for (int k = 0; k < c.n; ++k)
+            if (c.left[k] - done > 1e-9) c.left[n++] = c.left[k] - done;
+        for (int gone = c.n - n; c.n = n, gone > 0; --gone, n = c.n) fill(c);
+        schedule(e.second.first);
+    }
+    return end;
+}
 
 // Divides the row blocks' positions into ranges: the longest block's into 1 ..
 // kMostRanges, and every block then has ranges of about that length; by the
-// least estimated time.  The workgroups are handed out longest first, two per
-// CU; that is played through for one key/value head and its share of the
-// places.  Measured at head_dim 128: a step 2.2 us, where a CU has one
-// workgroup 1.6; about one and a half more per share; the partial sums written
-// and read at about 4.5 TB/s, the merge's launch 4 us.  (512 tokens after 8000
-// positions, bf16: 1 range 191 us, 2 145, 5 117, and the merge 6 to 16.  Cutting
-// all blocks' steps in a row into one equal run per place instead: 123.)
-void divide_blocks(std::vector<Block>& blocks, int G)
+// least estimated time, which it returns.  The workgroups are played through
+// for one key/value head and its share of the CUs.  Measured at head_dim 128:
+// a step of 128 rows 1.25 us, where a CU has two workgroups 2.2, of 64 rows 0.9
+// and 1.35; 1.5 and 2.5 steps more per share, and one for the masks of a block's
+// last; the partial sums written and read at about 9 TB/s, the merge 5 us.  (512
+// tokens after 8000 positions, bf16: 1 range 161 us, 2 140, 5 130.  Cutting all
+// blocks' steps in a row into one equal run per place instead: 5 % slower than
+// the best.)  Beside few()'s shares, which take few_us by themselves, the longest
+// has a neighbour for as long, and the work adds up (24 single tokens and two
+// pieces: 1, 2, 3, 4 ranges 63.4, 58.3, 61.1, 65.3 us; the pieces alone 45, 48,
+// 48, 39.6).
+double divide_blocks(std::vector<Block>& blocks, int G, int head_dim, bool wide, double few_us)
 {
-    constexpr int kPlaces = 512, kCus = 256, kMostRanges = 12;
+    constexpr int kCus = 256, kMostRanges = 16;          // (the merge's waves take a row of 16 slots)
+    const double step_us = (wide ? 1.25 : 0.9) * (head_dim == 128 ? 1.0 : 0.66), slow = wide ? 1.76 : 1.5, start = wide ? 1.5 : 2.5;
+    const int cus = std::max(1, kCus / G);
     int longest = 0;
+    double all = 0.0;
     for (Block& b : blocks) {
-        even_cuts(b.steps, 1, b.cuts);
+        b.ranges = 1;
         longest = std::max(longest, b.steps);
+        all += (b.steps + start + 1.0) * step_us;
     }
-    const int places = std::max(1, kPlaces / G);
-    if (blocks.size() >= 4 * (size_t)places) return;     // enough without
-    std::vector<Block> trial = blocks;
-    std::vector<double> items;
+    if (blocks.size() >= 8 * (size_t)cus) return all * slow / (2 * cus);   // enough without
+    std::vector<double> times;
     double best_us = 0.0;
-    for (int n = 1; n <= kMostRanges && n <= longest; ++n) {
+    int best_len = longest;
+    for (int n = 1; n <= kMostRanges && n <= longest; n += n < 6 ? 1 : 2) {
         const int len = (longest + n - 1) / n;
-        for (Block& b : trial) even_cuts(b.steps, (b.steps + len - 1) / len, b.cuts);
-        items.clear();
         int64_t slots = 0, rows = 0;
-        for (const Block& b : trial) {
-            int from = 0;
-            for (int c : b.cuts) {
-                items.push_back(c - from + 1.5);
-                from = c;
-            }
-            if (b.cuts.size() > 1) {
-                slots += (int64_t)b.cuts.size();
-                rows += (int64_t)b.cuts.size() * b.rows;
+        times.clear();
+        for (const Block& b : blocks) {
+            const int ranges = (b.steps + len - 1) / len;
+            for (int64_t i = 0; i < ranges; ++i)
+                times.push_back(((b.steps * (i + 1) / ranges - b.steps * i / ranges) + start + (i + 1 < ranges ? 0.0 : 1.0)) * step_us);
+            if (ranges > 1) {
+                slots += ranges;
+                rows += (int64_t)ranges * b.rows;
             }
         }
-        if (slots * G > 2 * kTileItems) continue;
-        std::sort(items.begin(), items.end(), std::greater<double>());
-        std::priority_queue<double, std::vector<double>, std::greater<double>> busy;
-        double end = 0.0;
-        for (double it : items) {
-            if ((int)busy.size() == places) {
-                it += busy.top();
-                busy.pop();
-            }
-            busy.push(it);
-            end = std::max(end, it);
+        if (slots * G > 2 * kTileItems || (n > 1 && times.size() > 8 * (size_t)cus)) break;
+        std::sort(times.begin(), times.end(), std::greater<double>());
+        double us = play(times, cus, slow);
+        if (few_us > 0.0) {
+            double work = 0.0;
+            for (double t : times) work += t;
+            const double beside = std::min(times[0] * slow, times[0] + few_us);
+            us = std::max({us, beside, few_us + work * slow / (2 * cus)});
         }
-        double us = end * ((int64_t)items.size() * G <= kCus ? 1.6 : 2.2);
-        if (slots) us += 4.0 + (double)rows * G * 132 * 4 * 2 / 4.5e6;
+        if (slots) us += 5.0 + (double)rows * G * (head_dim + paged::kPartPad) * 4 * 2 / 9e6;
         if (n == 1 || us < 0.97 * best_us) {
             best_us = us;
-            for (size_t i = 0; i < blocks.size(); ++i) blocks[i].cuts = trial[i].cuts;
+            best_len = len;
         }
     }
+    for (Block& b : blocks) b.ranges = (b.steps + best_len - 1) / best_len;
+    return best_us;
 }
 
 // Longest shares first: the workgroups are handed out in order.
@@ -265,7 +311,7 @@ bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.b
 // sequences one after another, long and short ones in turn, each start counted
 // as kStart steps; a sequence that runs share is added up by the merge.
 // Sequences stay whole, a workgroup each, where that is estimated to take no
-// longer: a CU does a step in step_us at least, or all of them stream at kRate;
+// longer: a CU does a step in step_us at least, or all of them stream at kStreamRate;
 // divided, a merge comes after them.  (bf16, from memory: one token after 256,
 // 511, 1023 and 2047 positions whole 7.9, 10.9, 17.5 and 31 us, divided 11.0,
 // 10.2, 10.4 and 11.0; 32 sequences of 300 to 1000 whole 21.8, 25.9 in equal
@@ -273,7 +319,7 @@ bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.b
 // runs 78; 8 of 3000 to 8000 45.3 and 42.2.)
 void divide_few(std::vector<Item>& whole, double step_bytes, Batch& b, int& slot)
 {
-    constexpr double kStart = 0.5, kCus = 256.0, kRate = 6.3e6, kMergeUs = 4.5;
+    constexpr double kStart = 0.5, kCus = 256.0, kMergeUs = 4.5;
     const double step_us = std::max(0.65, 1.68 * step_bytes / 65536);
     auto steps = [](const Item& it) { return (it.end + kFewStep - 1) / kFewStep; };
     std::stable_sort(whole.begin(), whole.end(), longer);
@@ -283,7 +329,7 @@ void divide_few(std::vector<Item>& whole, double step_bytes, Batch& b, int& slot
     b.few = whole;
     if (whole.empty() || whole.size() >= 4 * kFewRuns) return;   // (so many even out)
     const int longest = steps(whole[0]);
-    const double stream_us = total * step_bytes / kRate, mean = total / kCus;
+    const double stream_us = total * step_bytes / kStreamRate, mean = total / kCus;
     const double busiest = whole.size() <= kCus ? longest : std::max((double)longest, 1.28 * (mean + longest / 4.0));
     const double whole_us = std::max(stream_us, step_us * busiest);
     const double divided_us = std::max(stream_us, step_us * std::ceil(mean)) + kMergeUs;
@@ -384,17 +430,44 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
 {
     const int G = c.n_kv_heads, group = c.n_heads / G;
     auto blocks_of = [&](int s) { return (int)(((int64_t)pos0[s] + n_new[s] + c.page_size - 1) >> L.shift); };
-    std::vector<Block> blocks;                           // of one key/value head
-    for (int s = 0; s < n_seqs; ++s) {
-        const int64_t R = (int64_t)n_new[s] * group;
-        if (R <= paged::kFewRows) continue;
-        const int rows = R <= 64 ? 64 : 128;
-        for (int64_t r0 = 0; r0 < R; r0 += rows) {
-            const int64_t last = std::min(r0 + rows, R);
-            blocks.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0), {}});
+    // Row blocks of one key/value head: of 128 rows (64 where a sequence has no
+    // more), or of 64 all of them where that is estimated to be quicker: twice as
+    // many shares, and shorter steps, but a third more work.  (Prompts of 300, 1000
+    // and 2048 tokens: 14.3, 31.2 and 65 us in blocks of 128, 12.4, 29.4 and 80 of
+    // 64; four of 200 to 400 20.3 and 23.7.)  Not beside few()'s shares, where the
+    // CUs are busy anyway (19 single tokens and a piece of 200 to 300: 46.9, and
+    // 52.6 in blocks of 64).
+    auto block_rows = [](int64_t R, bool wide) { return wide && R > 64 ? 128 : 64; };
+    auto blocks_with = [&](bool wide) {
+        std::vector<Block> v;
+        for (int s = 0; s < n_seqs; ++s) {
+            const int64_t R = (int64_t)n_new[s] * group;
+            if (R <= paged::kFewRows) continue;
+            const int rows = block_rows(R, wide);
+            for (int64_t r0 = 0; r0 < R; r0 += rows) {
+                const int64_t last = std::min(r0 + rows, R);
+                v.push_back(Block{(int)((pos0[s] + (last - 1) / group + paged::kStep) / paged::kStep), (int)(last - r0), 1});
+            }
+        }
+        return v;
+    };
+    const double few_bytes = (double)kFewStep * c.head_dim * (c.flags & ATTN_PAGED_E4M3 ? 2 : 4);   // of a step
+    double few_us = 0.0;
+    for (int s = 0; s < n_seqs; ++s)
+        if (n_new[s] > 0 && (int64_t)n_new[s] * group <= paged::kFewRows)
+            few_us += ((int64_t)pos0[s] + n_new[s]) * G * few_bytes / kFewStep / kStreamRate;
+    std::vector<Block> blocks = blocks_with(true);
+    bool wide = false;
+    for (const Block& bl : blocks) wide |= bl.rows > 64;
+    const double us = divide_blocks(blocks, G, c.head_dim, wide, few_us);
+    if (wide && few_us == 0.0) {
+        std::vector<Block> narrow = blocks_with(false);
+        if (divide_blocks(narrow, G, c.head_dim, false, few_us) < us) {
+            blocks = std::move(narrow);
+            wide = false;
         }
     }
-    divide_blocks(blocks, G);
+    std::vector<int> cuts;
     std::vector<Item> whole;                             // of few()
     size_t block = 0;                                    // the sequence's first of `blocks`
     int few_slot = 0, tile_slot = 0, tok0 = 0, table = 0;
@@ -412,11 +485,11 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
             it.slot = it.next = -1;
             for (it.kvh = 0; it.kvh < G; ++it.kvh) whole.push_back(it);
         } else if (R > 0) {
-            const int kind = R <= 64, rows = 128 >> kind, n_blocks = (R + rows - 1) / rows;
+            const int rows = block_rows(R, wide), kind = rows == 64, n_blocks = (R + rows - 1) / rows;
             for (it.kvh = 0; it.kvh < G; ++it.kvh)
                 for (int k = 0; k < n_blocks; ++k) {
                     const Block& bl = blocks[block + k];
-                    const int n = (int)bl.cuts.size();
+                    const int n = bl.ranges;
                     it.row0 = k * rows;
                     it.rows = bl.rows;
                     it.begin = 0;
@@ -425,14 +498,15 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
                         b.tile_merge.push_back(Merge{tok0, it.row0, it.rows, it.kvh, tile_slot, n, {}});
                         b.slots[1] = std::max(b.slots[1], n);
                     }
-                    add_ranges(b.tile[kind], it, bl.cuts, paged::kStep, tile_slot);
+                    even_cuts(bl.steps, n, cuts);
+                    add_ranges(b.tile[kind], it, cuts, paged::kStep, tile_slot);
                 }
             block += n_blocks;
         }
         tok0 += n_new[s];
         table += n_new[s] > 0 ? blocks_of(s) : 0;
     }
-    divide_few(whole, (double)kFewStep * c.head_dim * (c.flags & ATTN_PAGED_E4M3 ? 2 : 4), b, few_slot);
+    divide_few(whole, few_bytes, b, few_slot);
     b.all_slots[0] = few_slot;
     b.all_slots[1] = tile_slot;
     by_xcd(b.tile[0]);
@@ -633,14 +707,15 @@ hipError_t attn_paged_run_attend(attn_paged_ctx* ctx, int32_t layer, const uint1
 {
     const paged::Args a = layer_args(ctx, layer);
     // A graph may replay on a longer batch: its launches have room for the
-    // shares that one may have, and the merge is there (its entries: a
-    // sequence's and key/value head's rows, a row block's).
+    // shares that one may have, of row blocks of either kind, and the merge is
+    // there (its entries: a sequence's and key/value head's rows, a row block's).
     const bool graph = capturing(s);
     int n[3] = {ctx->n_few, ctx->n_tile[0], ctx->n_tile[1]};
     int m[2] = {ctx->n_merge[0], ctx->n_merge[1]}, slots[2] = {ctx->slots[0], ctx->slots[1]};
     if (graph) {
-        for (int& v : n)
-            if (v) v = std::max(v, kGraphGrid);
+        if (n[0]) n[0] = std::max(n[0], kGraphGrid);
+        if (n[1] || n[2])
+            for (int k = 1; k <= 2; ++k) n[k] = std::max(n[k], kGraphGrid);
         m[0] = n[0] ? std::max(m[0], kGraphMerge) : 0;
         m[1] = n[1] || n[2] ? std::max(m[1], kGraphMerge) : 0;
         slots[0] = slots[1] = INT32_MAX;
