@@ -281,7 +281,7 @@ double divide_blocks(std::vector<Block>& blocks, int G, int head_dim, bool wide,
                 rows += (int64_t)ranges * b.rows;
             }
         }
-        if (slots * G > 2 * kTileItems || (n > 1 && times.size() > 8 * (size_t)cus)) break;
+        if (slots * G > 2 * kTileItems || (n > 1 && times.size() > 4 * (size_t)cus)) break;
         std::sort(times.begin(), times.end(), std::greater<double>());
         double us = play(times, cus, slow);
         if (few_us > 0.0) {
