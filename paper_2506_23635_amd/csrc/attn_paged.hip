@@ -1115,7 +1115,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
 // workgroups that take them come in turn, eight at a time (one per XCD), so
 // that the ones that wait for memory and the ones that multiply share the CUs
 // (24 sequences with one token and two with 150 to 300, after up to 3000
-// positions: 63 to 66 us with the merge; as two calls 36 and 40).
+// positions: 59 to 60 us with the merge; as two calls 36 and 38).
 struct Split {
     int few, tile[2];                        // workgroups / 8 of each kind
 };
