@@ -652,6 +652,7 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         size_t bytes = 0;
         for (const auto& p : parts) bytes += align_up(p.bytes, 16);
         if (capturing(s)) return fail(ctx, MOE_E_STATE, "a batch cannot be set while the stream captures a graph");
+        ctx->set = false;                                // (until the new one is on its way)
         Stage& st = ctx->stage[ctx->next_stage];
         hipError_t e = ready(st, bytes);
         if (e != hipSuccess) return hip_fail(ctx, e, "pinned memory for the batch");
@@ -667,7 +668,6 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
             at += n;
         }
         u.bytes = at;
-        ctx->set = false;                                // (until the new one is on its way)
         e = attn_paged_launch_unpack(&u, s);
         if (e != hipSuccess) return hip_fail(ctx, e, "batch kernel launch");
         e = hipEventRecord(st.done, s);

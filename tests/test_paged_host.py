@@ -1,6 +1,8 @@
 """The paged cache's C-ABI and binding on the host: sizes, refusals before anything is launched, the
 fp64 reference's own pins, and that its bounds fail planted errors."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -219,3 +221,19 @@ def test_the_bound_fails_planted_errors(one_term, L):
             other.k, other.v = pool.k, np.roll(pool.v, 1, axis=3)
             bad, _, _ = ref.attend(q, other, L - n, table)
         assert (np.abs(bad - o) > bound).any(), plant
+
+
+def test_batches_are_divided_into_shares_once_each(tmp_path):
+    """paged_divide.cpp, under the address and undefined-behaviour sanitizers."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    exe = str(tmp_path / "paged_divide")
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    "-D__HIP_PLATFORM_AMD__", "-I", rocm + "/include", os.path.join(here, "paged_divide.cpp"), "-o", exe,
+                    "-L", rocm + "/lib", "-lamdhip64", "-Wl,-rpath," + rocm + "/lib"], check=True)
+    for seed in (1, 2):
+        r = subprocess.run([exe, str(seed), "700"], capture_output=True, text=True,
+                           env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"))
+        assert r.returncode == 0, r.stdout + r.stderr
+        few, tile = map(int, r.stdout.split())
+        assert few > 100 and tile > 50                    # divided batches of both kinds were among them
