@@ -228,11 +228,11 @@ double play(const std::vector<double>& times, int cus, double slow)
         events.pop();
         Cu& c = cu[e.second.first];
         if (e.second.second != c.version) continue;
-        const double done = (e.first - c.at) / (c.n == 2 ? slow : 1.0);
+        const double done = c.n == 2 ? std::min(c.left[0], c.left[1]) : c.left[0];
         c.at = end = e.first;
         int n = 0;
         for (int k = 0; k < c.n; ++k)
-            if (c.left[k] - done > 1e-9) c.left[n++] = c.left[k] - done;
+            if (c.left[k] > done) c.left[n++] = c.left[k] - done;
         for (int gone = c.n - n; c.n = n, gone > 0; --gone, n = c.n) fill(c);
         schedule(e.second.first);
     }
@@ -311,8 +311,8 @@ bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.b
 // sequences one after another, long and short ones in turn, each start counted
 // as kStart steps; a sequence that runs share is added up by the merge.
 // Sequences stay whole, a workgroup each, where that is estimated to take no
-// longer: a CU does a step in step_us at least, or all of them stream at kStreamRate;
-// divided, a merge comes after them.  (bf16, from memory: one token after 256,
+// longer: a CU does a step in step_us at least, or all of them stream at
+// kStreamRate; divided, a merge comes after them.  (bf16, from memory: one token after 256,
 // 511, 1023 and 2047 positions whole 7.9, 10.9, 17.5 and 31 us, divided 11.0,
 // 10.2, 10.4 and 11.0; 32 sequences of 300 to 1000 whole 21.8, 25.9 in equal
 // ranges; 64 of 300 to 3000 whole 87, in equal ranges of each sequence 81, in
