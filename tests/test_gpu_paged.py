@@ -126,6 +126,25 @@ def test_attend(torch, shape, P, lens, e4m3):
     c.check_attend(q, out[:c.T])
 
 
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+@pytest.mark.parametrize("lens", [[(2000, 300)], [(0, 130)] * 24, [(0, 1200)], [(3000, 8)]],
+                         ids=["piece", "prompts", "prompt", "few-tokens"])
+@pytest.mark.parametrize("shape", [(4, 2, 64), (6, 1, 128), (16, 1, 64)], ids=lambda s: "%d-%d-%d" % s)
+def test_attend_many_rows(torch, shape, lens, e4m3):
+    """Enough rows, or positions, that both kinds of row blocks appear, whole and divided."""
+    c = Case(torch, *shape, 64, e4m3, lens, seed=17)
+    c.fill_context(new_too=True)
+    c.set_batch()
+    q = c.queries()
+    out = torch.full_like(q, 7.0)
+    c.cache.attend(0, q, out)
+    first = out.clone()
+    c.cache.attend(0, q, out)
+    torch.cuda.synchronize()
+    assert torch.equal(first.view(torch.int16), out.view(torch.int16))
+    c.check_attend(q, out)
+
+
 def check_append(c, qkv, q, before, layer=0):
     """Queries, pages and scales after an append; `before`: the pages' bytes before it."""
     torch = c.torch
@@ -800,6 +819,33 @@ def test_graph_replays_follow_the_batch(torch, new, e4m3):
         for a, b in zip(want, [q, out, c.cache.cache]):
             assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), i
         torch.randn(1000, device="cuda").sum().item()
+
+
+@pytest.mark.parametrize("order", [[0, 2000, 500, 4000, 0], [2000, 0, 4000, 100]], ids=str)
+@pytest.mark.parametrize("e4m3", [False, True], ids=["bf16", "e4m3"])
+def test_graph_replays_take_the_blocks_of_a_later_batch(torch, e4m3, order):
+    """A prompt's pieces, captured at one length and replayed at others, for which the rows are
+    divided into blocks of the other kind, and positions into ranges."""
+    H, G, hd, P, n = 16, 1, 64, 64, 300
+    c = Case(torch, H, G, hd, P, e4m3, [(max(order), n)], seed=19)
+    c.fill_context(new_too=True)
+    q = c.queries()
+    want, out = torch.empty_like(q), torch.empty_like(q)
+    c.cache.set_batch([n], order[:1], c.table)
+    c.cache.attend(0, q, want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.cache.attend(0, q, out)
+    for p0 in order:
+        c.cache.set_batch([n], [p0], c.table)
+        c.cache.attend(0, q, want)
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(want.view(torch.int16), out.view(torch.int16)), p0
+        c.lens = [(p0, n)]
+        c.check_attend(q, out)
 
 
 def test_two_contexts_on_two_streams(torch):
