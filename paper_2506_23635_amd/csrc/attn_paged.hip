@@ -715,21 +715,22 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 // about by its number, so that neither the 32 rows of a K read nor the four of
 // a V read meet in the same banks.
 //
-// P enters rounded to one bf16 (relative error 2^-8 at most per weight, random
-// in sign; the output's own rounding is as large): a second term would cost
-// half as many matrix instructions again.  The exponent's reference m only
+// P enters as two bf16 terms, as in few(): a weight is off by 2^-16 of itself at
+// most.  (One term, off by 2^-8, would save a third of the matrix instructions,
+// a prompt of 2048 tokens 85 -> 67 us, but the result's error would then be half
+// as large again as its own rounding, and change with the kind of share that a
+// row happens to be in.)  The exponent's reference m only
 // follows the maximum when some score is more than 2^kLazy above it: the
 // weights are then at most 2^kLazy, which changes nothing in fp32 or bf16, and
 // most steps need no rescaling and no exchange between lanes.
 //
 // A wave in its matrix products goes before its SIMD's other wave, so that the
 // two fall out of step and one's softmax runs beside the other's products (a
-// prompt of 2048 tokens: 66.7 us, at equal priority 70.3).
+// prompt of 2048 tokens, with one term: 66.7 us, at equal priority 70.3).
 //
-// Bound by what does not run beside the products: the matrix cores are busy in
-// 46 % of the cycles.  A prompt of 2048 tokens at 48 heads of 128 takes 61 to 63
-// us (820 to 840 TFLOP/s of the 51.6 GFLOP below the diagonal), 500 tokens after
-// 7001 on e4m3 pages 108 (825), and the merge of its five ranges 13.4.
+// Bound by what does not run beside the products.  A prompt of 2048 tokens at 48
+// heads of 128 takes 80 to 85 us (610 to 645 TFLOP/s of the 51.6 GFLOP below the
+// diagonal), 500 tokens after 7001 on e4m3 pages 140 to 147 with their merge.
 constexpr float kLazy = 8.f;
 
 template <int HD>
@@ -998,12 +999,14 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                 }
                 // the weights of 16 positions are formed beside the products
                 // of the 16 before, two scores to a product
-                u32x4_t bt[2];
+                u32x4_t bt[2], rt[2];
                 auto weights = [&](int i, int e) {
                     const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e], scale2, -ms));
                     const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e + 1], scale2, -ms));
                     l += pa + pb;
-                    bt[i % 2][e] = moe::cvt_pk_bf16(pa, pb);
+                    const uint32_t hw = moe::cvt_pk_bf16(pa, pb);
+                    bt[i % 2][e] = hw;
+                    rt[i % 2][e] = moe::cvt_pk_bf16(pa - __uint_as_float(hw << 16), pb - __uint_as_float(hw & 0xFFFF0000u));
                 };
 #pragma unroll
                 for (int e = 0; e < 4; ++e) weights(0, e);
@@ -1015,6 +1018,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
 #pragma unroll
                     for (int b = 0; b < DB; ++b) {
                         o[b] = mfma32x32x16(av[i % 2][b], bt[i % 2], o[b]);
+                        o[b] = mfma32x32x16(av[i % 2][b], rt[i % 2], o[b]);
                         if (i + 1 < 2 * NB) {
 #pragma unroll
                             for (int e = b * 4 / DB; e < (b + 1) * 4 / DB; ++e) weights(i + 1, e);

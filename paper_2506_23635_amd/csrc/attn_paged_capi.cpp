@@ -242,9 +242,12 @@ double play(const std::vector<double>& times, int cus, double slow)
 // Divides the row blocks' positions into ranges: the longest block's into 1 ..
 // kMostRanges, and every block then has ranges of about that length; by the
 // least estimated time, which it returns.  The workgroups are played through
-// for one key/value head and its share of the CUs.  Measured at head_dim 128:
-// a step of 128 rows 1.25 us, where a CU has two workgroups 2.2, of 64 rows 0.9
-// and 1.35; 1.5 and 2.5 steps more per share, and one for the masks of a block's
+// for one key/value head and its share of the CUs.  Measured at head_dim 128,
+// with weights of one bf16 term: a step of 128 rows 1.25 us, where a CU has two
+// workgroups 2.2, of 64 rows 0.9 and 1.35 (with the two terms that tile() takes
+// 1.55, 2.65, 1.0 and 1.55; but planned with these, 500-token prompts took 20.5
+// -> 17.6 us, 16 sequences of 8 tokens 41 -> 46, 20 tokens and a piece 50.8 ->
+// 54.1, and the other 22 batches the same); 1.5 and 2.5 steps more per share, and one for the masks of a block's
 // last; the partial sums written and read at about 9 TB/s, the merge 5 us.  (512
 // tokens after 8000 positions, bf16: 1 range 161 us, 2 140, 5 130.  Cutting all
 // blocks' steps in a row into one equal run per place instead: 5 % slower than
