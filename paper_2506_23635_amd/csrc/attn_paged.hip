@@ -328,12 +328,46 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t*
 
 // ----------------------------------------------------------------- attend --
 
-// A maximum in base 2, with the product's one rounding everywhere: p, the
-// rescaling and the merges then refer to the same value.
+// A weight is 2^(s scale2 - M), M a base-2 maximum of the row, in one fused
+// multiply-add: M is m * scale2 with the product's one rounding, everywhere,
+// so that p, the rescaling and the merges refer to the same value, and what
+// the rounding left out is a factor that all of the row's weights share.  From
+// |M| = 2^31 on that factor alone can leave fp32's range, so from kFar on M is
+// m * scale2 exactly, in two parts (base2, base2_rest), and the weights are
+// 2^((s - m) scale2) (far_scores): the difference first.
 __device__ inline float base2(float m, float scale2)
 {
 #pragma clang fp contract(off)
     return m * scale2;
+}
+
+constexpr float kFar = 16777216.f;           // 2^24: below, the factor is in [2^-1/2, 2^1/2]
+
+__device__ inline float base2_rest(float m, float scale2)
+{
+    const float b = base2(m, scale2);
+    return fabsf(b) < kFar ? 0.f : fmaf(m, scale2, -b);
+}
+
+// 2^(M' - M) of the maxima m <= mx: what sums that refer to m are multiplied by
+__device__ __forceinline__ float decay(float m, float mx, float scale2)
+{
+    if (m == -INFINITY) return 0.f;
+    return __builtin_amdgcn_exp2f((base2(m, scale2) - base2(mx, scale2)) + (base2_rest(m, scale2) - base2_rest(mx, scale2)));
+}
+
+// Scores of rows whose maximum m is far, less m; and what is to be subtracted
+// from their product with scale2 (ms = base2(m), or 0 where m is -inf).
+template <class Vec, int N>
+__device__ __forceinline__ float far_scores(Vec (&sc)[N], float m, float ms)
+{
+    if (!__ballot(!(fabsf(ms) < kFar))) return ms;
+    const bool far = !(fabsf(ms) < kFar);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < (int)(sizeof(Vec) / 4); ++e) sc[i][e] -= far ? m : 0.f;
+    return far ? 0.f : ms;
 }
 
 // eight e4m3 codes as eight bf16 of code * scale (exact: a power of two)
@@ -546,14 +580,14 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, sc[s][i]);
             mx = max32(max16(mx));
-            const float ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
             if (__ballot(mx != m)) {
-                const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
+                const float alpha = decay(m, mx, scale2);
                 l *= alpha;
 #pragma unroll
                 for (int i = 0; i < D; ++i) o[i] *= alpha;
                 m = mx;
             }
+            const float ms = far_scores(sc, m, m == -INFINITY ? 0.f : base2(m, scale2));
             u32x4_t p1, p2;
 #pragma unroll
             for (int s = 0; s < 2; ++s)
@@ -661,7 +695,6 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
         const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * D;
         if (row < R) {
             float M = fmaxf(fmaxf(lds.m[0][row], lds.m[1][row]), fmaxf(lds.m[2][row], lds.m[3][row]));
-            const float Ms = M == -INFINITY ? 0.f : base2(M, scale2);
             float L = 0.f, v[D];
 #pragma unroll
             for (int i = 0; i < D; ++i) v[i] = 0.f;
@@ -669,7 +702,7 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
             for (int k = 0; k < 4; ++k) {
                 const float mk = lds.m[k][row];
                 // (a wave that has seen only NaN has no maximum, and NaN sums)
-                const float f = mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(mk, scale2) - Ms);
+                const float f = decay(mk, M, scale2);
                 L = fmaf(lds.l[k][row], f, L);
 #pragma unroll
                 for (int i = 0; i < D; ++i) v[i] = fmaf(lds.o[k][row][d0 + i], f, v[i]);
@@ -680,7 +713,7 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
                 for (int i = 0; i < D; i += 4)
                     *reinterpret_cast<float4*>(dst + d0 + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                 if (d0 == 0) {
-                    dst[HD] = M == -INFINITY ? -INFINITY : Ms;
+                    dst[HD] = M;
                     dst[HD + 1] = L;
                 }
             } else {
@@ -988,21 +1021,21 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                     for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[pb][i]);
                 if (__ballot(mx > thr)) {
                     mx = fmaxf(m, max32(mx));
-                    const float mn = mx == -INFINITY ? 0.f : base2(mx, scale2);
-                    const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - mn);
+                    const float alpha = decay(m, mx, scale2);
                     l *= alpha;
 #pragma unroll
                     for (int b = 0; b < DB; ++b) o[b] *= alpha;
                     m = mx;
-                    ms = mn;
+                    ms = mx == -INFINITY ? 0.f : base2(mx, scale2);
                     thr = mx + kLazy / scale2;
                 }
+                const float ref = far_scores(sc, m, ms);
                 // the weights of 16 positions are formed beside the products
                 // of the 16 before, two scores to a product
                 u32x4_t bt[2], rt[2];
                 auto weights = [&](int i, int e) {
-                    const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e], scale2, -ms));
-                    const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e + 1], scale2, -ms));
+                    const float pa = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e], scale2, -ref));
+                    const float pb = __builtin_amdgcn_exp2f(fmaf(sc[i / 2][i % 2 * 8 + 2 * e + 1], scale2, -ref));
                     l += pa + pb;
                     const uint32_t hw = moe::cvt_pk_bf16(pa, pb);
                     bt[i % 2][e] = hw;
@@ -1074,9 +1107,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                 const float* src = mg + ((k - 1) * kRowWaves + w) * (DB * 16 + 2) * 64 + lane;
                 const float m2 = src[DB * 16 * 64], l2 = src[(DB * 16 + 1) * 64];
                 const float mn = fmaxf(m, m2);
-                const float ms = mn == -INFINITY ? 0.f : base2(mn, scale2);
-                const float f1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, scale2) - ms);
-                const float f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m2, scale2) - ms);
+                const float f1 = decay(m, mn, scale2), f2 = decay(m2, mn, scale2);
 #pragma unroll
                 for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -1097,7 +1128,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
                     *reinterpret_cast<float4*>(dst + b * 32 + 8 * i + 4 * h) =
                         make_float4(o[b][4 * i], o[b][4 * i + 1], o[b][4 * i + 2], o[b][4 * i + 3]);
             if (h == 0) {
-                dst[HD] = m == -INFINITY ? -INFINITY : base2(m, scale2);
+                dst[HD] = m;
                 dst[HD + 1] = l;
             }
             continue;
@@ -1175,7 +1206,7 @@ struct MergeGrid {
 };
 
 template <int HD>
-__global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict__ out, MergeGrid g)
+__global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict__ out, float scale2, MergeGrid g)
 {
     constexpr int D = HD / 64;
     __shared__ float s_f[kMaxSlots], s_red[2][4], s_sum[4][HD];
@@ -1234,7 +1265,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
                     for (int k = 0; k < kRows; ++k) {
                         float M = ml[k].x;
                         for (int off = kWaveSlots / 2; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-                        const float f = ml[k].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[k].x - M);
+                        const float f = decay(ml[k].x, M, scale2);
                         float L = ml[k].y * f;
                         for (int off = kWaveSlots / 2; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
                         L = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(L)));
@@ -1277,7 +1308,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
             M = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
             for (int s = threadIdx.x; s < n; s += 256) {
                 const float2 ml = s < 256 ? own : ml_of(s);
-                const float f = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+                const float f = decay(ml.x, M, scale2);
                 s_f[s] = f;
                 L = fmaf(ml.y, f, L);
             }
@@ -1385,8 +1416,8 @@ hipError_t attn_paged_launch_merge(const paged::Args* a, uint16_t* out, const in
     g.tile_chunks = 128 / g.tile_rows;
     const dim3 grid(g.few * g.few_chunks + n[1] * g.tile_chunks);
     if (grid.x == 0) return hipSuccess;
-    if (a->hd == 128) hipLaunchKernelGGL(paged::merge_kernel<128>, grid, dim3(256), 0, s, *a, out, g);
-    else hipLaunchKernelGGL(paged::merge_kernel<64>, grid, dim3(256), 0, s, *a, out, g);
+    if (a->hd == 128) hipLaunchKernelGGL(paged::merge_kernel<128>, grid, dim3(256), 0, s, *a, out, scale2(128), g);
+    else hipLaunchKernelGGL(paged::merge_kernel<64>, grid, dim3(256), 0, s, *a, out, scale2(64), g);
     return hipGetLastError();
 }
 
