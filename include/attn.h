@@ -179,9 +179,18 @@ MOE_API const char *attn_last_error(const attn_ctx *ctx);
  * are rounded to nearest, ties to even, once, from the fp32 value.
  *
  * Values that are not finite: bf16 pages keep them; e4m3 pages store them as
- * NaN.  A row that sees one is not finite in that dimension (in all, if it is
- * a key); rows that do not see it are untouched by it, and so are all rows by
- * what slots behind a sequence's last token hold. */
+ * NaN.  A row that sees such a value is not finite in its dimension, whatever
+ * its weight; a key counts by its score q . k: NaN or +inf, and the row is not
+ * finite in any dimension; -inf, and the position weighs nothing (a row all of
+ * whose scores are -inf gives zeros, as one that sees no position).  Rows that
+ * do not see it are untouched by it, and so are all rows by what slots behind a
+ * sequence's last token hold.
+ *
+ * Numbers: scores are sums in fp32 (a row is not finite where the sum of |q_i
+ * k_i| passes its range), the weights' maximum and sum are fp32, each weight
+ * enters its product with v as two bf16 terms (16 bits), the sums are fp32, and
+ * the result is rounded to bf16 once.  The order of the sums, and with it the
+ * last bits, depends on how a batch's positions are divided. */
 
 typedef struct attn_paged_ctx attn_paged_ctx;
 

@@ -567,12 +567,13 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
                 }
             }
             if constexpr (kMore) fetch_k(p0 + step, pn);
+            auto unseen = [&](int s, int i) { return pg[s] < 0 || p0 + 16 * s + 4 * g + i > lim; };
             if constexpr (kMasked) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (pg[s] < 0 || p0 + 16 * s + 4 * g + i > lim) sc[s][i] = -INFINITY;
+                        if (unseen(s, i)) sc[s][i] = -INFINITY;
             }
             float mx = m;
 #pragma unroll
@@ -631,8 +632,8 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
                     for (int s = 0; s < 2; ++s)
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
-                            seen[2 * s + i] = (sc[s][2 * i] == -INFINITY ? 0u : kOnes & 0xFFFFu) |
-                                              (sc[s][2 * i + 1] == -INFINITY ? 0u : kOnes & 0xFFFF0000u);
+                            seen[2 * s + i] = (unseen(s, 2 * i) ? 0u : kOnes & 0xFFFFu) |
+                                              (unseen(s, 2 * i + 1) ? 0u : kOnes & 0xFFFF0000u);
 #pragma unroll
                     for (int i = 0; i < D; ++i) {
                         u32x4_t ind;
