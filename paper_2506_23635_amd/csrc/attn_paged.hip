@@ -392,10 +392,12 @@ __device__ __forceinline__ uint2 transposed(const uint8_t* p)
 // 16 bytes a lane from base + offset (below `bytes`, a wave's range) straight
 // to LDS, lane after lane from dst on.  In assembly, because after the
 // compiler's builtin the next LDS read, whatever it reads, waits for the load;
-// it writes no register, the caller waits for it (vmcnt) before the barrier
-// that hands the rows on, and the LDS address passed in tells the compiler
-// that the memory changes.  (m0 is the compiler's to use as well, but nothing
-// here makes it keep a value there.)
+// it writes no register, and the caller waits for it (vmcnt) before the barrier
+// that hands the rows on.  m0 and memory are declared as changed (m0 is a register
+// that the compiler never hands out and only sets for instructions that read it,
+// of which a warning reminds; none here do).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t bytes, uint8_t* dst, int offset)
 {
     const uint64_t b = (uint64_t)(uintptr_t)base;
@@ -405,8 +407,10 @@ __device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t bytes,
     // (the pause: a scalar register that a vector instruction has just written)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
-                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(offset), "s"(d));
+                 : "s"(__builtin_amdgcn_readfirstlane(at)), "v"(offset), "s"(d)
+                 : "m0", "memory");
 }
+#pragma clang diagnostic pop
 
 // the same into registers
 __device__ __forceinline__ u32x4_t load_16(const uint8_t* base, uint32_t bytes, int offset)
