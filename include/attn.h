@@ -263,14 +263,16 @@ typedef enum { ATTN_QKV_F32 = 0, ATTN_QKV_BF16 = 1 } attn_qkv_type;
  * elements, ld elements apart, rows 16-byte aligned) in; q out bf16 [T][n_heads
  * head_dim]; keys and values to the pages of layer `layer`; slots of other
  * positions keep their values (see above for scales that grow).  q may not
- * overlap qkv.  Requires a batch whose new tokens all have pages (MOE_E_STATE);
- * T == 0 is a no-op. */
+ * overlap what lies between qkv's first element and its last (MOE_E_ARG).
+ * Requires a batch whose new tokens all have pages (MOE_E_STATE); T == 0 is a
+ * no-op. */
 MOE_API moe_status attn_paged_append(attn_paged_ctx *ctx, int32_t layer, const void *qkv, int64_t ld,
                                      int32_t type, uint16_t *q, moe_stream_t stream);
 
 /* Attention of the batch's T tokens, q bf16 [T][n_heads head_dim] (rotated),
  * over their sequences' positions up to their own in layer `layer`'s pages,
- * which must hold them; out bf16 [T][n_heads head_dim] may not overlap q. */
+ * which must hold them; out bf16 [T][n_heads head_dim] may not overlap q
+ * (MOE_E_ARG). */
 MOE_API moe_status attn_paged_attend(attn_paged_ctx *ctx, int32_t layer, const uint16_t *q, uint16_t *out,
                                      moe_stream_t stream);
 

@@ -168,6 +168,15 @@ moe_status hip_fail(attn_paged_ctx* ctx, hipError_t e, const char* what)
 
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
+bool overlap(const void* a, uint64_t a_bytes, const void* b, uint64_t b_bytes)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return x < y ? y - x < a_bytes : x - y < b_bytes;
+}
+
+// of the batch's queries, or of their results
+uint64_t q_bytes(const attn_paged_ctx* c) { return (uint64_t)c->T * c->cfg.n_heads * c->cfg.head_dim * 2; }
+
 // Appends the shares of `it` that end after the given steps (the last: all of them).
 void add_ranges(std::vector<Item>& out, Item it, const std::vector<int>& cuts, int step, int& slot)
 {
@@ -790,6 +799,8 @@ moe_status attn_paged_append(attn_paged_ctx* ctx, int32_t layer, const void* qkv
     if (ctx->T == 0) return MOE_OK;
     if (!qkv || !q) return fail(ctx, MOE_E_ARG, "qkv or q is NULL");
     if (misaligned(qkv) || misaligned(q)) return fail(ctx, MOE_E_ALIGN, "qkv and q must be 16-byte aligned");
+    const uint64_t qkv_bytes = ((uint64_t)(ctx->T - 1) * ld + n) * (type == ATTN_QKV_BF16 ? 2 : 4);
+    if (overlap(qkv, qkv_bytes, q, q_bytes(ctx))) return fail(ctx, MOE_E_ARG, "q may not overlap qkv");
     const paged::Source x{qkv, ld, 0, 1, type == ATTN_QKV_BF16, 0};
     const hipError_t e = attn_paged_run_append(ctx, layer, &x, q, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e, "append kernel launch");
@@ -804,7 +815,7 @@ moe_status attn_paged_attend(attn_paged_ctx* ctx, int32_t layer, const uint16_t*
     if (st != MOE_OK) return st;
     if (ctx->T == 0) return MOE_OK;
     if (!q || !out) return fail(ctx, MOE_E_ARG, "q or out is NULL");
-    if (q == out) return fail(ctx, MOE_E_ARG, "out may not be q");
+    if (overlap(q, q_bytes(ctx), out, q_bytes(ctx))) return fail(ctx, MOE_E_ARG, "out may not overlap q");
     if (misaligned(q) || misaligned(out)) return fail(ctx, MOE_E_ALIGN, "q and out must be 16-byte aligned");
     const hipError_t e = attn_paged_run_attend(ctx, layer, q, out, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e, "attention kernel launch");
