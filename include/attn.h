@@ -240,7 +240,8 @@ MOE_API moe_status attn_paged_init(const attn_paged_config *cfg, void *cache, vo
  * A table entry of -1 is no page: its positions are left out of the
  * attention (a row that sees no position gives zeros); append refuses a batch
  * whose new tokens do not all have pages.
- * Enqueues one small kernel on stream that hands the batch to the device;
+ * Enqueues one small kernel on stream that hands the batch to the device (not
+ * where neither it nor the batch before has a token);
  * allocates no device memory (the first calls allocate pinned host memory).
  * Errors, the previous batch then staying set: MOE_E_ARG (a NULL array,
  * negative counts, ld too small, an entry outside -1 .. n_pages - 1, a page
@@ -251,7 +252,8 @@ MOE_API moe_status attn_paged_init(const attn_paged_config *cfg, void *cache, vo
  * caller orders them.
  * A graph captured over append and attend calls replays on the batch that is
  * set when it is replayed, which must have as many sequences and the same
- * n_new as the one set at its capture (positions and pages may differ). */
+ * n_new as the one set at its capture (positions and pages may differ);
+ * on a batch with another number of tokens it does nothing. */
 MOE_API moe_status attn_paged_set_batch(attn_paged_ctx *ctx, int32_t n_seqs, const int32_t *n_new,
                                         const int32_t *pos0, const int32_t *table, int32_t ld,
                                         moe_stream_t stream);

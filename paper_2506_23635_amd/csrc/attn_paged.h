@@ -54,7 +54,9 @@ struct Merge {
 };
 
 // Counts that the kernels read on the device, so that a captured launch
-// follows a batch set after the capture.
+// follows a batch set after the capture.  A launch's q, qkv and out have as many
+// rows as the batch that it was made for has tokens (Args::T): on a batch of
+// another T the kernels do nothing.
 struct Header {
     int32_t T, n_pages, n_few, n_tile[2];
     int32_t n_merge[2];        // few()'s entries, tile()'s
@@ -75,6 +77,7 @@ struct Args {
     float* tile_part;          // [slot][128][hd + kPartPad]
     uint8_t *k, *v;            // the layer's pages [page][kv head][slot][hd]
     float *k_scale, *v_scale;  // the layer's scales [page][kv head] (e4m3)
+    int T;                     // the tokens of the batch that the launch is made for
     int H, G, hd, shift;       // page_size = 1 << shift
     int e4m3;
 };

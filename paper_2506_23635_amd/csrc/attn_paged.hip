@@ -77,6 +77,12 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
+// of the batch on the device, 0 where a launch is not made for as many tokens
+__device__ __forceinline__ int count(const Args& a, const int32_t* n)
+{
+    return uniform_load(&a.hdr->T) == a.T ? uniform_load(n) : 0;
+}
+
 // ------------------------------------------------------------------ batch --
 
 // All arrays in one pass over the host memory: the link's latency once, 4 to 7
@@ -193,7 +199,7 @@ __device__ __forceinline__ void append_rows(const Args& a, const Source& x, uint
     Piece v{};
     if (live) v = load_piece<kPacked>(x, t, head, f, hd, n_rotated, turn);
     __syncthreads();
-    if (!live) return;
+    if (!live || uniform_load(&a.hdr->T) != a.T) return;
     if (turn) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) turn_pair(v.lo[i], v.hi[i], s_cs[f + i]);
@@ -259,7 +265,7 @@ __device__ __forceinline__ void append_codes(const Args& a, const Source& x, int
     const int G = a.G, hd = a.hd, P = hd / 8;
     const int per_pass = 256 / P;
     const int tj = threadIdx.x / P, pc = threadIdx.x % P;
-    const int n_tasks = uniform_load(&a.hdr->n_pages) * G * 2;
+    const int n_tasks = count(a, &a.hdr->n_pages) * G * 2;
     for (int task = blockIdx.x; task < n_tasks; task += n_blocks) {
         const PageWork w = uniform_struct(a.pages + task / (2 * G));
         const int g = task / 2 % G;
@@ -468,7 +474,7 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
     // (the first share is read along with the count, not after it: the list
     // has room for every workgroup of the grid)
     Item im = uniform_struct(a.few + b);
-    const int n_first = uniform_load(&a.hdr->n_few);
+    const int n_first = count(a, &a.hdr->n_few);
     for (int it = b, first = b; it < n_first || it != first;) {
         if (it != b) im = uniform_struct(a.few + it);
         const int32_t* table = a.table + im.table;
@@ -799,7 +805,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
     const int pg = w / kRowWaves;                        // the wave's position group
     const Item* items = a.tile[kPG - 1];
     Item im = uniform_struct(items + wg);
-    const int n_items = uniform_load(&a.hdr->n_tile[kPG - 1]);
+    const int n_items = count(a, &a.hdr->n_tile[kPG - 1]);
     const u32x4_t zero = {0u, 0u, 0u, 0u};
     // chunk of row r is at chunk ^ k_key(r) of K, ^ v_key(r) of V (rows of 64
     // dims: two share the 256 bytes of all banks)
@@ -1226,7 +1232,7 @@ __global__ __launch_bounds__(256) void merge_kernel(Args a, uint16_t* __restrict
     const float* part = tiles ? a.tile_part : a.few_part;
     const int stride = (tiles ? 128 : kFewRows) * (HD + kPartPad);
     Merge mg = uniform_struct(list + x / chunks);
-    const int last = uniform_load(&a.hdr->n_merge[tiles]);
+    const int last = count(a, &a.hdr->n_merge[tiles]);
     for (int it = x / chunks; it < last; it += entries) {
         if (it != x / chunks) mg = uniform_struct(list + it);
         const int n = mg.n;

@@ -139,6 +139,7 @@ struct attn_paged_ctx {
     std::vector<int32_t> written;      // per page: the call that last had it written, for set_batch
     int32_t call;
     bool set, unplaced;
+    bool handed;                       // the device has, or may have, a batch with tokens
     int32_t T, n_pages, n_few, n_tile[2], n_merge[2];
     int slots[2];                      // the most of one merge entry
     Stage stage[kStages];
@@ -544,6 +545,7 @@ paged::Args layer_args(attn_paged_ctx* c, int layer)
     a.v = base + L.data_bytes;
     a.k_scale = reinterpret_cast<float*>(base + 2 * L.data_bytes);
     a.v_scale = reinterpret_cast<float*>(base + 2 * L.data_bytes + L.scale_bytes);
+    a.T = c->T;
     a.H = c->cfg.n_heads;
     a.G = c->cfg.n_kv_heads;
     a.hd = c->cfg.head_dim;
@@ -642,7 +644,9 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         b.merge.size() > L.max_merge[0] || b.tile_merge.size() > L.max_merge[1] ||
         (size_t)b.all_slots[0] > L.few_slots || (size_t)b.all_slots[1] > L.tile_slots)
         return fail(ctx, MOE_E_CAPACITY, "the batch has more shares than the workspace holds");
-    if (T > 0) {
+    // (no tokens: nothing is launched, but a graph of an earlier batch that is
+    // replayed all the same must find so)
+    if (T > 0 || ctx->handed) {
         paged::Header h{};
         h.T = (int32_t)T;
         h.n_pages = (int32_t)b.pages.size();
@@ -680,12 +684,14 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
             at += n;
         }
         u.bytes = at;
+        ctx->handed = true;
         e = attn_paged_launch_unpack(&u, s);
         if (e != hipSuccess) return hip_fail(ctx, e, "batch kernel launch");
         e = hipEventRecord(st.done, s);
         if (e != hipSuccess) return hip_fail(ctx, e, "batch event");
         st.busy = true;
         ctx->next_stage = (ctx->next_stage + 1) % kStages;
+        ctx->handed = T > 0;
     }
     ctx->T = (int32_t)T;
     ctx->n_pages = (int32_t)b.pages.size();

@@ -86,6 +86,22 @@ static int overlaps()
     return 0;
 }
 
+// The device knows the tokens of the batch that is set, none included.
+static int tokens_handed_over()
+{
+    n_unpack = 0;
+    CHECK(batch({}) == MOE_OK && batch({0, 0}) == MOE_OK && n_unpack == 0);
+    CHECK(batch({2, 1}) == MOE_OK && n_unpack == 1 && header.T == 3);
+    CHECK(batch({0}) == MOE_OK && n_unpack == 2 && header.T == 0);
+    CHECK(header.n_few == 0 && header.n_pages == 0 && header.n_tile[0] == 0 && header.n_merge[0] == 0);
+    CHECK(batch({0}) == MOE_OK && batch({}) == MOE_OK && n_unpack == 2);
+    CHECK(batch({5}) == MOE_OK && n_unpack == 3 && header.T == 5);
+    is_capturing = true;
+    CHECK(batch({5}) == MOE_E_STATE && batch({0}) == MOE_E_STATE && n_unpack == 3);
+    is_capturing = false;
+    return 0;
+}
+
 int main()
 {
     attn_paged_config c{};
@@ -100,7 +116,7 @@ int main()
     c.max_blocks = 4;
     c.rope_theta = 5e5f;
     CHECK(attn_paged_init(&c, reinterpret_cast<void*>(uintptr_t(1) << 30), reinterpret_cast<void*>(uintptr_t(1) << 40), &ctx) == MOE_OK);
-    if (overlaps()) return 1;
+    if (tokens_handed_over() || overlaps()) return 1;
     attn_paged_destroy(ctx);
     std::printf("ok\n");
     return 0;
