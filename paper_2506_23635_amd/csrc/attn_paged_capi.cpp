@@ -27,6 +27,7 @@ using paged::kXcds;
 using paged::kFewRuns;
 // Dividing positions makes at most twice as many shares (and partial sums) of tile()
 constexpr int64_t kTileItems = 768;
+constexpr int kMostRanges = 16;        // of one row block (the merge's waves take a row of 16 slots)
 constexpr int kFewStep = 4 * paged::kTile;   // positions of a workgroup's step of few()
 constexpr double kStreamRate = 6.3e6;  // bytes/us that few() reads where every CU has its share
 constexpr int kGraphGrid = 512;        // workgroups that a captured launch has at least of a kind,
@@ -86,7 +87,11 @@ Layout make_layout(const attn_paged_config* c)
     const bool tiles = rows > (size_t)paged::kFewRows;
     for (int k = 0; k < 2; ++k)
         L.max_tile[k] = tiles ? (rows / (128 >> k) + tile_seqs) * G + 2 * kTileItems + kXcds : 0;
-    L.tile_slots = tiles ? 2 * kTileItems : 0;
+    // (a row block has at most kMostRanges ranges, and no more than steps; blocks
+    // of 64 rows are the most there are)
+    const size_t tile_steps = ((size_t)c->max_blocks * c->page_size + paged::kStep - 1) / paged::kStep;
+    const size_t most = std::min<size_t>(kMostRanges, tile_steps);
+    L.tile_slots = tiles && most > 1 ? std::min<size_t>(2 * kTileItems, (rows / 64 + tile_seqs) * G * most) : 0;
     L.max_merge[0] = std::max<size_t>(kFewRuns, kGraphMerge);
     L.max_merge[1] = tiles ? kTileItems : 0;
     size_t off = 0;
@@ -267,7 +272,7 @@ double play(const std::vector<double>& times, int cus, double slow)
 // 48, 39.6).
 double divide_blocks(std::vector<Block>& blocks, int G, int head_dim, bool wide, double few_us)
 {
-    constexpr int kCus = 256, kMostRanges = 16;          // (the merge's waves take a row of 16 slots)
+    constexpr int kCus = 256;
     const double step_us = (wide ? 1.25 : 0.9) * (head_dim == 128 ? 1.0 : 0.66), slow = wide ? 1.76 : 1.5, start = wide ? 1.5 : 2.5;
     const int cus = std::max(1, kCus / G);
     int longest = 0;
