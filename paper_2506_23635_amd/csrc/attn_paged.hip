@@ -103,8 +103,10 @@ __global__ __launch_bounds__(256) void unpack_kernel(Unpack u)
 // cos and sin of pos * inv_freq.  The angle is formed and reduced to the
 // nearest multiple k of pi / 2 in fp64 (pi / 2 in two parts; k below 2^25);
 // what is left, r in [-pi / 4, pi / 4], goes through the Taylor series to r^9
-// and r^10 in fp32, which leave out less than 2^-28 and 2^-33: the result is
-// within 2 ulp of fp32.  (With the library's sincosf, and the new values held
+// and r^10 in fp32, which leave out less than 2^-28 and 2^-33.  The result is off
+// by less than 2^-23 and the angle's own error, |angle| 2^-51 (inv_freq and the
+// product rounded to fp64): absolute, as the rotated values need it; near a zero
+// that can be many ulp.  (With the library's sincosf, and the new values held
 // in registers between the scale and the codes, pieces of six prompts of 200 to
 // 900 tokens took 24.3 us into e4m3 pages; so they take 17.7.)
 __device__ inline float2 rotation(int pos, double inv_freq)

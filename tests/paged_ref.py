@@ -44,8 +44,8 @@ def rotate(x, pos, theta):
 
 
 def rotation_error(x):
-    """Bound of the fp32 rotation's error: cos and sin within 2 ulp (their angle, reduced in fp64,
-    enters rounded to fp32: pi 2^-24), two products and a sum."""
+    """Bound of the fp32 rotation's error: cos and sin within 2 2^-24 beside their angle (which,
+    reduced in fp64, enters rounded to fp32: pi 2^-24), two products and a sum."""
     a, b = np.split(np.abs(x), 2, axis=-1)
     e = (np.pi + 2 * 2 + 3) * U32 * (a + b)
     return np.concatenate([e, e], axis=-1)
