@@ -35,11 +35,15 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attn_weights.h"
 #include "moe_common.h"
 
 namespace attn {
 
+using moe::base2;
+using moe::decay;
 using moe::f32x4_t;
+using moe::far_scores;
 using moe::u32x4_t;
 using moe::kTileK;
 using moe::kTileBytes;
@@ -814,7 +818,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a)
 //
 // The position groups' sums are merged through LDS in group order.  With one
 // range the result is written as bf16; with several, each writes its
-// unnormalised sums, maximum (base 2) and sum of weights for merge_kernel: a
+// unnormalised sums, maximum and sum of weights for merge_kernel: a
 // few rows over a long context are split until about two workgroups per CU
 // run (attn_split).
 struct FlashArgs {
@@ -842,15 +846,6 @@ __device__ inline f32x16_t mfma32x32x16(const u32x4_t a, const u32x4_t b, f32x16
 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(moe::bf16x8_t, a),
                                                    __builtin_bit_cast(moe::bf16x8_t, b), c, 0, 0, 0);
-}
-
-// A maximum in base 2, with the product's one rounding everywhere: p, the
-// rescaling and the merges then refer to the same value, and its rounding
-// cancels (contracted into a difference it would not).
-__device__ inline float base2(float m, float scale2)
-{
-#pragma clang fp contract(off)
-    return m * scale2;
 }
 
 constexpr int flash_rows(int pg) { return 128 / pg; }        // query rows per workgroup
@@ -1033,19 +1028,19 @@ __global__ __launch_bounds__(256, 2) void flash_kernel(FlashArgs a)
         const float mn = fmaxf(m, mx);
         // a row with every position masked so far keeps mn = -inf: subtract
         // 0 instead, so its p are 0, not NaN
-        const float ms = base2(mn, a.scale2), msub = mn == -INFINITY ? 0.f : -ms;
+        const float ms = far_scores(sv, mn, mn == -INFINITY ? 0.f : base2(mn, a.scale2));
         float ps = 0.f;
         float pv[NB * 16];
 #pragma unroll
         for (int e = 0; e < NB * 16; ++e) {
-            pv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale2, msub));
+            pv[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], a.scale2, -ms));
             ps += pv[e];
         }
         ps += __shfl_xor(ps, 32, 64);
         // rescale the running sums only where a maximum moved (m == mn gives
         // the factor 1 exactly, so skipping it changes no bit)
         if (__ballot(mn != m)) {
-            const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, a.scale2) - ms);
+            const float alpha = decay(m, mn, a.scale2);
             l *= alpha;
 #pragma unroll
             for (int b = 0; b < DB; ++b) o[b] *= alpha;
@@ -1107,9 +1102,7 @@ __global__ __launch_bounds__(256, 2) void flash_kernel(FlashArgs a)
             const float* src = mg + ((k - 1) * kRowWaves + w) * (DB * 16 + 2) * 64 + lane;
             const float m2 = src[DB * 16 * 64], l2 = src[(DB * 16 + 1) * 64];
             const float mn = fmaxf(m, m2);
-            const float ms = base2(mn, a.scale2);
-            const float f1 = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m, a.scale2) - ms);
-            const float f2 = m2 == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2(m2, a.scale2) - ms);
+            const float f1 = decay(m, mn, a.scale2), f2 = decay(m2, mn, a.scale2);
 #pragma unroll
             for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -1130,7 +1123,7 @@ __global__ __launch_bounds__(256, 2) void flash_kernel(FlashArgs a)
                 *reinterpret_cast<float4*>(dst + b * 32 + 8 * g + 4 * h) =
                     make_float4(o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]);
         if (h == 0) {
-            dst[HD] = base2(m, a.scale2);
+            dst[HD] = m;
             dst[HD + 1] = l;
         }
         return;
@@ -1159,6 +1152,7 @@ struct MergeArgs {
     const float* part;
     uint16_t* out;         // [T][H * hd] bf16
     int n_split;
+    float scale2;
 };
 
 template <int HD>
@@ -1176,7 +1170,7 @@ __global__ __launch_bounds__(256) void merge_kernel(MergeArgs a)
     if (lane == 0) red[0][w] = M;
     __syncthreads();
     M = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-    const float f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
+    const float f = decay(ms, M, a.scale2);
     fs[tid] = f;
     float L = ls * f;
     for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
@@ -1221,7 +1215,7 @@ __global__ __launch_bounds__(256) void merge_few_kernel(MergeArgs a, int n)
     const float ls = lane < S ? base[(int64_t)lane * (HD + kPartPad) + HD + 1] : 0.f;
     float M = ms;
     for (int off = 32; off >= 1; off >>= 1) M = fmaxf(M, __shfl_xor(M, off, 64));
-    const float f = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
+    const float f = decay(ms, M, a.scale2);
     float L = ls * f;
     for (int off = 32; off >= 1; off >>= 1) L += __shfl_xor(L, off, 64);
     float acc[D];
@@ -1433,6 +1427,8 @@ int attn_split(int T, int H, int G, int pos0, int max_seq)
     return best;
 }
 
+static float scale2(int hd) { return (float)(1.4426950408889634 / sqrt((double)hd)); }
+
 hipError_t attn_launch_flash(const uint16_t* q, const uint16_t* kc, const uint16_t* vc, float* part,
                              uint16_t* out, int T, int H, int G, int hd, int max_seq, int pos0,
                              int few, int n_split, hipStream_t s)
@@ -1440,7 +1436,7 @@ hipError_t attn_launch_flash(const uint16_t* q, const uint16_t* kc, const uint16
     const int pg = flash_pg(T, H, G), rows = attn::flash_rows(pg);
     const int nrb = (T * (H / G) + rows - 1) / rows;
     attn::FlashArgs a{q, kc, vc, out, part, T, H, G, max_seq, pos0, nrb, n_split,
-                      (float)(1.4426950408889634 / sqrt((double)hd))};
+                      scale2(hd)};
     const dim3 grid((G * nrb * n_split + attn::kXcds - 1) / attn::kXcds * attn::kXcds), block(256);
 #define ATTN_FLASH(HD, PG) \
     hipLaunchKernelGGL((few ? attn::flash_kernel<HD, PG, 3> : attn::flash_kernel<HD, PG, 2>), grid, block, 0, s, a)
@@ -1479,7 +1475,7 @@ hipError_t attn_launch_short_merge(const float* part, uint16_t* out, int T, int 
 hipError_t attn_launch_merge(const float* part, uint16_t* out, int T, int H, int hd, int n_split,
                              hipStream_t s)
 {
-    attn::MergeArgs a{part, out, n_split};
+    attn::MergeArgs a{part, out, n_split, scale2(hd)};
     const int n = T * H;
     // many rows of few ranges: a wave each (300 tokens of 48 heads, 4 ranges:
     // 15.9 -> 9 us); few rows: a workgroup each (48 rows of 8 ranges: 3.5 us

@@ -11,11 +11,15 @@
 #include <type_traits>
 
 #include "attn_paged.h"
+#include "attn_weights.h"
 #include "moe_common.h"
 
 namespace paged {
 
+using moe::base2;
+using moe::decay;
 using moe::f32x4_t;
+using moe::far_scores;
 using moe::u32x4_t;
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
@@ -335,48 +339,6 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t*
 }
 
 // ----------------------------------------------------------------- attend --
-
-// A weight is 2^(s scale2 - M), M a base-2 maximum of the row, in one fused
-// multiply-add: M is m * scale2 with the product's one rounding, everywhere,
-// so that p, the rescaling and the merges refer to the same value, and what
-// the rounding left out is a factor that all of the row's weights share.  From
-// |M| = 2^31 on that factor alone can leave fp32's range, so from kFar on M is
-// m * scale2 exactly, in two parts (base2, base2_rest), and the weights are
-// 2^((s - m) scale2) (far_scores): the difference first.
-__device__ inline float base2(float m, float scale2)
-{
-#pragma clang fp contract(off)
-    return m * scale2;
-}
-
-constexpr float kFar = 16777216.f;           // 2^24: below, the factor is in [2^-1/2, 2^1/2]
-
-__device__ inline float base2_rest(float m, float scale2)
-{
-    const float b = base2(m, scale2);
-    return fabsf(b) < kFar ? 0.f : fmaf(m, scale2, -b);
-}
-
-// 2^(M' - M) of the maxima m <= mx: what sums that refer to m are multiplied by
-__device__ __forceinline__ float decay(float m, float mx, float scale2)
-{
-    if (m == -INFINITY) return 0.f;
-    return __builtin_amdgcn_exp2f((base2(m, scale2) - base2(mx, scale2)) + (base2_rest(m, scale2) - base2_rest(mx, scale2)));
-}
-
-// Scores of rows whose maximum m is far, less m; and what is to be subtracted
-// from their product with scale2 (ms = base2(m), or 0 where m is -inf).
-template <class Vec, int N>
-__device__ __forceinline__ float far_scores(Vec (&sc)[N], float m, float ms)
-{
-    if (!__ballot(!(fabsf(ms) < kFar))) return ms;
-    const bool far = !(fabsf(ms) < kFar);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int e = 0; e < (int)(sizeof(Vec) / 4); ++e) sc[i][e] -= far ? m : 0.f;
-    return far ? 0.f : ms;
-}
 
 // eight e4m3 codes as eight bf16 of code * scale (exact: a power of two)
 __device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
