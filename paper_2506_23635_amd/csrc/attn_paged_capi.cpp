@@ -693,7 +693,10 @@ moe_status set_batch(attn_paged_ctx* ctx, int32_t n_seqs, const int32_t* n_new, 
         e = attn_paged_launch_unpack(&u, s);
         if (e != hipSuccess) return hip_fail(ctx, e, "batch kernel launch");
         e = hipEventRecord(st.done, s);
-        if (e != hipSuccess) return hip_fail(ctx, e, "batch event");
+        if (e != hipSuccess) {
+            (void)hipStreamSynchronize(s);               // nothing else tells when the stage has been read
+            return hip_fail(ctx, e, "batch event");
+        }
         st.busy = true;
         ctx->next_stage = (ctx->next_stage + 1) % kStages;
         ctx->handed = T > 0;

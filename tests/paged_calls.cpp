@@ -9,7 +9,8 @@
 #include <initializer_list>
 
 static int n_unpack, n_append, n_attend, n_merge;
-static bool is_capturing;
+static int n_sync;
+static bool is_capturing, record_fails;
 static paged::Header header;               // of the last batch handed over
 
 extern "C" {
@@ -26,7 +27,8 @@ hipError_t attn_paged_launch_merge(const paged::Args*, uint16_t*, const int*, co
 hipError_t hipHostMalloc(void** p, size_t n, unsigned) { return (*p = std::malloc(n)) ? hipSuccess : hipErrorOutOfMemory; }
 hipError_t hipHostFree(void* p) { return std::free(p), hipSuccess; }
 hipError_t hipEventCreateWithFlags(hipEvent_t* e, unsigned) { return *e = reinterpret_cast<hipEvent_t>(8), hipSuccess; }
-hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return hipSuccess; }
+hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return record_fails ? hipErrorUnknown : hipSuccess; }
+hipError_t hipStreamSynchronize(hipStream_t) { return ++n_sync, hipSuccess; }
 hipError_t hipEventSynchronize(hipEvent_t) { return hipSuccess; }
 hipError_t hipEventDestroy(hipEvent_t) { return hipSuccess; }
 hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus* s)
@@ -102,6 +104,20 @@ static int tokens_handed_over()
     return 0;
 }
 
+// Where the event that guards a batch's pinned memory is not recorded, the memory may be written
+// or freed again only once the kernel that reads it has ended.
+static int unrecorded_event()
+{
+    record_fails = true;
+    n_unpack = n_sync = 0;
+    CHECK(batch({2}) == MOE_E_HIP && n_unpack == 1 && n_sync == 1);
+    record_fails = false;
+    CHECK(attn_paged_attend(ctx, 0, nullptr, nullptr, nullptr) == MOE_E_STATE);    // no batch is set
+    CHECK(batch({0}) == MOE_OK && header.T == 0 && n_unpack == 2);
+    CHECK(batch({2}) == MOE_OK && header.T == 2 && n_sync == 1);
+    return 0;
+}
+
 int main()
 {
     attn_paged_config c{};
@@ -116,7 +132,7 @@ int main()
     c.max_blocks = 4;
     c.rope_theta = 5e5f;
     CHECK(attn_paged_init(&c, reinterpret_cast<void*>(uintptr_t(1) << 30), reinterpret_cast<void*>(uintptr_t(1) << 40), &ctx) == MOE_OK);
-    if (tokens_handed_over() || overlaps()) return 1;
+    if (tokens_handed_over() || overlaps() || unrecorded_event()) return 1;
     attn_paged_destroy(ctx);
     std::printf("ok\n");
     return 0;
