@@ -291,7 +291,9 @@ MOE_API const char *attn_paged_last_error(const attn_paged_ctx *ctx);
  * with z not NULL also z = norm2(y), as attn_forward_norm.  The contexts must
  * agree in n_heads, n_kv_heads, head_dim and rope_theta (MOE_E_SHAPE) and
  * share one device; T <= max_tokens of ctx, whose own cache is not used.
- * (attn_intermediates then finds no q | k | v in the order it names.)  Errors
+ * (attn_intermediates then finds no q | k | v in the order it names; and a graph
+ * replayed on a batch with another number of tokens leaves the pages alone, but
+ * y and z without meaning.)  Errors
  * as attn_forward and attn_forward_norm; MOE_E_STATE without a batch that
  * append takes. */
 MOE_API moe_status attn_forward_paged(attn_ctx *ctx, int32_t layer, attn_paged_ctx *cache, const uint16_t *x,

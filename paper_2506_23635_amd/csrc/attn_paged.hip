@@ -402,7 +402,9 @@ constexpr uint32_t kOnes = 0x3F803F80u;      // two bf16 ones
 // 32-position steps in turn, each with a maximum and sums of its own, merged
 // through LDS at the end.
 //
-// Everything stays in registers.  Scores transposed, S^T = K Q^T, with
+// Scores, weights and sums stay in registers (at head_dim 128 all 256 of bf16
+// pages' variant, four bytes a lane three times to scratch, and its scalars
+// partly to vector registers).  Scores transposed, S^T = K Q^T, with
 // v_mfma_f32_16x16x32_bf16: lane (r, g) = (lane % 16, lane / 16) supplies K of
 // position r and Q of row r, and ends with the scores of row r at positions
 // 16 s + 4 g + i of sub-block s.  O^T += V^T P^T takes them as they are: its B
@@ -738,7 +740,9 @@ __device__ __forceinline__ void few(const Args& a, const uint16_t* __restrict__ 
 //
 // Bound by what does not run beside the products.  A prompt of 2048 tokens at 48
 // heads of 128 takes 80 to 85 us (610 to 645 TFLOP/s of the 51.6 GFLOP below the
-// diagonal), 500 tokens after 7001 on e4m3 pages 140 to 147 with their merge.
+// diagonal; the matrix cores, which the second term keeps busy half as long
+// again, are busy in 57 % of the cycles), 500 tokens after 7001 on e4m3 pages 140
+// to 147 with their merge, which is some 13 of it.
 constexpr float kLazy = 8.f;
 
 template <int HD>
@@ -1125,7 +1129,7 @@ __device__ __forceinline__ void tile(const Args& a, const uint16_t* __restrict__
 // workgroups that take them come in turn, eight at a time (one per XCD), so
 // that the ones that wait for memory and the ones that multiply share the CUs
 // (24 sequences with one token and two with 150 to 300, after up to 3000
-// positions: 59 to 60 us with the merge; as two calls 36 and 38).
+// positions: 62 to 63 us with the merge; as two calls 36 and 44).
 struct Split {
     int few, tile[2];                        // workgroups / 8 of each kind
 };
@@ -1168,8 +1172,11 @@ __global__ __launch_bounds__(256, 2) void attend_kernel(Args a, const uint16_t* 
 // order.  A slot without weight holds zeros.
 //
 // A workgroup takes four rows of an entry of few()'s, or one where some row has
-// many slots, and eight of tile()'s (sixteen with two slots); `chunks` workgroups an entry of 16 or 128
-// rows.  Bound by its reads, which mostly come from the last-level cache: five
+// many slots, and eight of tile()'s (sixteen with two slots); `chunks` workgroups
+// an entry of 16 or 128 rows.  A wave loads as many slots as its variant has
+// room for, 2, 5, 8 or 16: rows of few slots would otherwise read slot 0 again
+// for the rest (five ranges are what pieces of some hundred tokens behind a long
+// prefix get).  Bound by its reads, which mostly come from the last-level cache: five
 // ranges of 500 tokens' rows, 65 MB, take 13.4 us (one row a wave 15.4); few
 // slots, by latency, 3.7 to 5.
 constexpr int kWaveSlots = 16;

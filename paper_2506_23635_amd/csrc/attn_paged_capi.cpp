@@ -264,12 +264,12 @@ double play(const std::vector<double>& times, int cus, double slow)
 // -> 17.6 us, 16 sequences of 8 tokens 41 -> 46, 20 tokens and a piece 50.8 ->
 // 54.1, and the other 22 batches the same); 1.5 and 2.5 steps more per share, and one for the masks of a block's
 // last; the partial sums written and read at about 9 TB/s, the merge 5 us.  (512
-// tokens after 8000 positions, bf16: 1 range 161 us, 2 140, 5 130.  Cutting all
-// blocks' steps in a row into one equal run per place instead: 5 % slower than
-// the best.)  Beside few()'s shares, which take few_us by themselves, the longest
-// has a neighbour for as long, and the work adds up (24 single tokens and two
-// pieces: 1, 2, 3, 4 ranges 63.4, 58.3, 61.1, 65.3 us; the pieces alone 45, 48,
-// 48, 39.6).
+// tokens after 8000 positions, bf16: 1 range 192 us, 2 165, 3 208, 4 181, 5 168.)
+// Beside few()'s shares, which take few_us by themselves, the longest has a
+// neighbour for as long, and the work adds up (24 single tokens and two pieces:
+// 1, 2, 3, 4 ranges 73.7, 62.1, 66.4, 66.3 us; the pieces alone 59, 46, 45, 44).
+// The factors: 0.66 a step's time at head_dim 64 to 128's; 0.97 keeps the fewer
+// ranges where the estimates are as good as equal.
 double divide_blocks(std::vector<Block>& blocks, int G, int head_dim, bool wide, double few_us)
 {
     constexpr int kCus = 256;
@@ -330,7 +330,9 @@ bool longer(const Item& x, const Item& y) { return x.end - x.begin > y.end - y.b
 // as kStart steps; a sequence that runs share is added up by the merge.
 // Sequences stay whole, a workgroup each, where that is estimated to take no
 // longer: a CU does a step in step_us at least, or all of them stream at
-// kStreamRate; divided, a merge comes after them.  (bf16, from memory: one token after 256,
+// kStreamRate; divided, a merge comes after them (kMergeUs).  1.28 is what two
+// shares on a CU cost beside the mean and a quarter of the longest, fitted to
+// the batches below; 0.9 divides only where the estimates differ.  (bf16, from memory: one token after 256,
 // 511, 1023 and 2047 positions whole 7.9, 10.9, 17.5 and 31 us, divided 11.0,
 // 10.2, 10.4 and 11.0; 32 sequences of 300 to 1000 whole 21.8, 25.9 in equal
 // ranges; 64 of 300 to 3000 whole 87, in equal ranges of each sequence 81, in
@@ -451,10 +453,10 @@ void divide(const attn_paged_config& c, const Layout& L, const int32_t* n_new, c
     // Row blocks of one key/value head: of 128 rows (64 where a sequence has no
     // more), or of 64 all of them where that is estimated to be quicker: twice as
     // many shares, and shorter steps, but a third more work.  (Prompts of 300, 1000
-    // and 2048 tokens: 14.3, 31.2 and 65 us in blocks of 128, 12.4, 29.4 and 80 of
-    // 64; four of 200 to 400 20.3 and 23.7.)  Not beside few()'s shares, where the
-    // CUs are busy anyway (19 single tokens and a piece of 200 to 300: 46.9, and
-    // 52.6 in blocks of 64).
+    // and 2048 tokens: 15.4, 36.9 and 84 us in blocks of 128, 12.9, 34.0 and 98 of
+    // 64; four of 200 to 400 22.0 and 25.9.)  Not beside few()'s shares, which
+    // mostly keep the CUs busy (19 single tokens and a piece of 200 to 300: of one
+    // batch 46.9, and 52.6 in blocks of 64, of another 45.5 and 41.1).
     auto block_rows = [](int64_t R, bool wide) { return wide && R > 64 ? 128 : 64; };
     auto blocks_with = [&](bool wide) {
         std::vector<Block> v;
