@@ -186,11 +186,12 @@ MOE_API const char *attn_last_error(const attn_ctx *ctx);
  * do not see it are untouched by it, and so are all rows by what slots behind a
  * sequence's last token hold.
  *
- * Numbers: scores are sums in fp32 (a row is not finite where the sum of |q_i
- * k_i| passes its range), the weights' maximum and sum are fp32, each weight
- * enters its product with v as two bf16 terms (16 bits), the sums are fp32, and
- * the result is rounded to bf16 once.  The order of the sums, and with it the
- * last bits, depends on how a batch's positions are divided. */
+ * Numbers: scores are sums in fp32 (where the sum of |q_i k_i| passes its range
+ * they may be infinite or NaN, and count as such), the weights' maximum and sum
+ * are fp32, each weight enters its product with v as two bf16 terms (16 bits),
+ * these sums are fp32, and the result is rounded to bf16 once.  The order of the
+ * sums, and with it the last bits, depends on how a batch's positions are
+ * divided. */
 
 typedef struct attn_paged_ctx attn_paged_ctx;
 

@@ -402,9 +402,9 @@ constexpr uint32_t kOnes = 0x3F803F80u;      // two bf16 ones
 // 32-position steps in turn, each with a maximum and sums of its own, merged
 // through LDS at the end.
 //
-// Scores, weights and sums stay in registers (at head_dim 128 all 256 of bf16
-// pages' variant, four bytes a lane three times to scratch, and its scalars
-// partly to vector registers).  Scores transposed, S^T = K Q^T, with
+// Scores, weights and sums stay in registers (the bf16 variant at head_dim 128
+// fills all 256 and spills three to scratch; the scalars spill to vector
+// registers).  Scores transposed, S^T = K Q^T, with
 // v_mfma_f32_16x16x32_bf16: lane (r, g) = (lane % 16, lane / 16) supplies K of
 // position r and Q of row r, and ends with the scores of row r at positions
 // 16 s + 4 g + i of sub-block s.  O^T += V^T P^T takes them as they are: its B
