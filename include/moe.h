@@ -73,6 +73,8 @@ typedef enum {
 #define MOE_PARTIAL_F32 0x1 /* moe_forward writes y as fp32 [T, d], unrounded
                                (an expert-parallel share's partial sum that a
                                cross-device all-reduce adds, Sec. 4.3) */
+#define MOE_E4M3 0x4        /* the experts' products in 8-bit floating point
+                               (see "Products in e4m3" below) */
 
 /* Layer configuration.
  *   d_model, ffn_dim : D_embed and D_ffn (Table tab:vars: 6144 and 10752).
@@ -87,7 +89,8 @@ typedef enum {
  *                      max_tokens * d_model * 2 must stay below 2^31.
  *   d_model * ffn_dim * 4 (one expert's packed gate/up bytes) must stay
  *                      below 2^31.
- *   flags            : 0 or MOE_PARTIAL_F32; any other bit is rejected. */
+ *   flags            : MOE_PARTIAL_F32 and MOE_E4M3, together or apart; any
+ *                      other bit is rejected. */
 typedef struct {
     int32_t d_model, ffn_dim, n_experts, top_k;
     int32_t expert_begin, n_local_experts;
@@ -159,6 +162,50 @@ MOE_API moe_status moe_load_expert(moe_ctx *ctx, int32_t layer, int32_t expert,
 MOE_API moe_status moe_load_router(moe_ctx *ctx, int32_t layer, const float *wr,
                            const float *bias, int32_t src_on_device,
                            moe_stream_t stream);
+
+/* Routing policies: which experts a layer's router chooses and how it weighs
+ * them, where that is not the softmax over the k largest logits.  For a token
+ * with fp32 logits l:
+ *   s_e  = softmax over all experts of l (MOE_SCORE_SOFTMAX), 1 / (1 + exp(-l_e))
+ *          (MOE_SCORE_SIGMOID), or l_e itself (MOE_SCORE_SELECTED);
+ *   c_e  = s_e + balance_e           what the choice goes by (the weights do not);
+ *   the experts form n_groups groups of E / n_groups neighbours; a group's value
+ *   is the sum of its group_best largest c, and only the top_groups groups of
+ *   the largest values (ties: lower group) are open;
+ *   S    = the k experts of open groups with the largest c (ties: larger l, then
+ *          lower id), slots in that order;
+ *   w_e  = scale * s_e, with renormalize scale * s_e / sum over S of s;
+ *          MOE_SCORE_SELECTED: scale * softmax over S of l in both cases.
+ * Scores, choice and sums are fp64 (so that the choice does not hang on the
+ * rounding of an exp), the weights rounded once to fp32.  A c that is NaN counts
+ * as -infinity, and so does a NaN logit among equal c; every slot has an expert of
+ * its own whatever the logits, and weights that a NaN takes part in are NaN.
+ * Scores that are all 0 (or a softmax over nothing but -infinity) give weights 0.
+ *
+ *   score        : moe_score.
+ *   n_groups     : divides n_experts; 1: no groups.
+ *   top_groups   : 1 .. n_groups, with top_k <= top_groups * E / n_groups.
+ *   group_best   : 1 or 2, at most E / n_groups.
+ *   renormalize  : 0 or 1.
+ *   scale        : finite.
+ *   balance      : fp32 [E], device memory of the caller, or NULL (zeros).  It is
+ *                  read by each routing of the layer, so it stays allocated while
+ *                  the policy is set; values written to it are seen by the next
+ *                  routing, a captured graph's replays included. */
+typedef enum { MOE_SCORE_SELECTED = 0, MOE_SCORE_SOFTMAX = 1, MOE_SCORE_SIGMOID = 2 } moe_score;
+typedef struct {
+    int32_t score, n_groups, top_groups, group_best, renormalize;
+    float scale;
+    const float *balance;
+} moe_policy;
+
+/* Sets the policy of one layer's router, for every call that routes the layer
+ * (moe_route, with logits_in too, and all forwards); NULL: the softmax over
+ * the selected logits again, which a new context has.  Host work only.  A
+ * routing returned for this layer before the call is no longer accepted by
+ * moe_forward.  Errors: MOE_E_ARG (layer, a field), MOE_E_SHAPE (groups that do
+ * not divide the experts or hold fewer than top_k), MOE_E_ALIGN. */
+MOE_API moe_status moe_set_policy(moe_ctx *ctx, int32_t layer, const moe_policy *policy);
 
 /* Sec. 2.1 (the router selects 4 of the 16 experts per token), Sec. 3.1
  * (its output decides which experts, and so which nodes, receive a token).
@@ -251,8 +298,8 @@ typedef enum {
     MOE_WS_TILES,              /* int32 [max_tiles][2]: token tiles of 256 rows (expert, first row);
                                   for inspection, no kernel reads them */
     MOE_WS_N_TILES,            /* int32 [1], likewise */
-    MOE_WS_H,                  /* bf16 [rows_max, f] */
-    MOE_WS_O,                  /* fp32 [rows_max, d] */
+    MOE_WS_H,                  /* bf16 [rows_max, f]; MOE_E4M3: then fp32 values on the way */
+    MOE_WS_O,                  /* fp32 [rows_max, d]; MOE_E4M3: x's rounded values before */
     MOE_WS_COUNT
 } moe_ws_region;
 MOE_API int32_t moe_workspace_map(const moe_config *cfg, uint64_t *offset, uint64_t *bytes,
@@ -262,7 +309,8 @@ MOE_API int32_t moe_workspace_map(const moe_config *cfg, uint64_t *offset, uint6
  * forward on ctx, valid until the next forward.  h: bf16 [rows, f], the
  * SiLU-gated activations of each grouped row; o: fp32 [rows, d], each grouped
  * row's expert output before the routing weight.  Rows follow the routing's
- * pair_row / offsets.  Either pointer may be NULL. */
+ * pair_row / offsets.  Either pointer may be NULL.  With MOE_E4M3 h holds the
+ * bf16 values that the activations' codes stand for. */
 MOE_API moe_status moe_intermediates(const moe_ctx *ctx, const uint16_t **h,
                              const float **o);
 
@@ -277,7 +325,8 @@ MOE_API moe_status moe_intermediates(const moe_ctx *ctx, const uint16_t **h,
 typedef enum {
     MOE_K_ROUTER = 0,        /* router logits, fp64 partial sums */
     MOE_K_ROUTE = 1,         /* selection, weights, permutation */
-    MOE_K_DECODE_GATEUP = 2, /* small-T gate/up + SiLU */
+    MOE_K_DECODE_GATEUP = 2, /* small-T gate/up + SiLU (here and below MOE_E4M3:
+                                with the coding of the rows that it reads) */
     MOE_K_DECODE_DOWN = 3,   /* small-T down projection */
     MOE_K_GEMM_GATEUP = 4,   /* grouped GEMM gate/up + SiLU */
     MOE_K_GEMM_DOWN = 5,     /* grouped GEMM down projection */
@@ -304,6 +353,78 @@ MOE_API moe_status moe_profile_read(moe_ctx *ctx, double *total_ms,
  * recording adds one barrier per workgroup. */
 MOE_API moe_status moe_profile_gemm_timeline(moe_ctx *ctx, uint64_t *gateup, uint64_t *down,
                                              int32_t max_wg);
+
+/* ---------------------------------------------------------------------------
+ * Products in e4m3.  A value is a code times a scale: codes of 1 sign, 4
+ * exponent and 3 mantissa bits (bias 7, largest value 448, no infinities), one
+ * scale 2^e for each 128 consecutive elements of a row of activations and for
+ * each 128 x 128 block of a weight matrix (the last ones may be cut off by the
+ * matrix's end).  e is the least integer from -100 on such that 448 * 2^e is no
+ * less than any finite value of the block (at most 119: values past 448 * 2^119
+ * are stored as that); values are divided by 2^e, which is exact, and rounded
+ * once to nearest, ties to even.  What is not finite becomes NaN, and so do the
+ * sums that it enters.  Weights that are e4m3 codes times powers of two already
+ * keep their values exactly when they are passed as bf16.
+ *
+ * A product's terms are exact and are summed in fp32.
+ *
+ * With MOE_E4M3 a layer of moe_init has its experts so: moe_load_expert codes the
+ * three matrices as it repacks them, and per token and chosen expert
+ *   G = Q(x) Q(W1),  U = Q(x) Q(V1),  H = Q(silu(G) * U),  o = H Q(W2),
+ * Q being the rounding above (H's from fp32), G, U and o fp32.  The router takes
+ * x itself.  Every call works on such a layer; the arena needs half of the bytes
+ * (plus the scales'). */
+
+/* Types of elements. */
+typedef enum { MOE_T_F32 = 0, MOE_T_BF16 = 1 } moe_type;
+
+/* Rows to e4m3: x [T] rows of n elements of `type`, ld elements apart (rows
+ * 16-byte aligned); codes [T][n] bytes; scales [T][ceil(n / 128)] bytes, each
+ * e + 127 (the biased exponent of 2^e).  n a positive multiple of 16 (at most
+ * 2^24), T at most 2^24; T == 0 is a no-op.  Enqueued on stream; allocates
+ * nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n), MOE_E_SHAPE (n, T),
+ * MOE_E_ALIGN (x, codes, or a stride that is no multiple of 16 bytes). */
+MOE_API moe_status moe_quantize_e4m3(const void *x, int64_t ld, int32_t type, int32_t T, int32_t n,
+                                     uint8_t *codes, uint8_t *scales, moe_stream_t stream);
+
+/* A product y = Q(x) Q(W) for weights that stay: W [in_dim][out_dim].
+ *   in_dim, out_dim : multiples of 16, at most 2^20, in_dim * out_dim < 2^31 with
+ *                     both rounded up to multiples of 256.
+ *   max_tokens      : most rows of a call, 1 .. 2^20, max_tokens * in_dim < 2^30
+ *                     (in_dim rounded up to a multiple of 128).
+ *   flags           : must be 0. */
+typedef struct moe_linear moe_linear;
+typedef struct { int32_t in_dim, out_dim, max_tokens, flags; } moe_linear_config;
+
+/* Bytes of the caller-allocated weights and workspace; 0 if cfg is invalid. */
+MOE_API size_t moe_linear_weight_bytes(const moe_linear_config *cfg);
+MOE_API size_t moe_linear_workspace_bytes(const moe_linear_config *cfg);
+
+/* Validates cfg and records the two caller-allocated device buffers (256-byte
+ * aligned, kept until moe_linear_destroy).  Allocates only the host-side context.
+ * Errors as moe_init; the message is readable through moe_linear_last_error(NULL). */
+MOE_API moe_status moe_linear_init(const moe_linear_config *cfg, void *weights, void *workspace,
+                                   moe_linear **out);
+
+/* Codes and repacks w bf16 [in_dim][out_dim] row-major, device memory, 16-byte
+ * aligned (kernels enqueued on stream; w may be freed once they have run). */
+MOE_API moe_status moe_linear_load(moe_linear *ctx, const uint16_t *w, moe_stream_t stream);
+
+/* y = Q(x) Q(W) for T rows: x bf16, rows ldx elements apart (16-byte aligned),
+ * y [T][out_dim] of `type` (fp32, or rounded once to bf16), contiguous, 16-byte
+ * aligned, not overlapping x's elements (MOE_E_ARG).  T == 0 is a no-op.  Errors:
+ * MOE_E_ARG, MOE_E_CAPACITY (T > max_tokens), MOE_E_STATE (not loaded),
+ * MOE_E_ALIGN.  Two calls on a context share its workspace: they go to one
+ * stream, or the caller orders them. */
+MOE_API moe_status moe_linear_forward(moe_linear *ctx, const uint16_t *x, int64_t ldx, void *y,
+                                      int32_t type, int32_t T, moe_stream_t stream);
+
+/* Frees the host-side context (never the caller's buffers). */
+MOE_API void moe_linear_destroy(moe_linear *ctx);
+
+/* Message of the last failing call on ctx; with ctx == NULL, of the last
+ * failing moe_linear_init on this thread. */
+MOE_API const char *moe_linear_last_error(const moe_linear *ctx);
 
 /* Frees the host-side context and its profiling events (never the caller's
  * device buffers). */

@@ -18,6 +18,9 @@ LIB_PATH = os.path.join(PKG_DIR, "libmoe.so")
 
 MOE_OK = 0
 MOE_PARTIAL_F32 = 0x1   # moe_config.flags: y of moe_forward is fp32 [T, d]
+MOE_E4M3 = 0x4          # moe_config.flags: the experts' products in e4m3
+SCORE_SELECTED, SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1, 2   # moe_score
+T_F32, T_BF16 = 0, 1       # moe_type
 ATTN_PAGED_E4M3 = 0x1   # attn_paged_config.flags: pages of e4m3 with scales
 QKV_F32, QKV_BF16 = 0, 1   # attn_qkv_type
 DIAG_MAX_WG = 512    # MOE_DIAG_MAX_WG of include/moe.h
@@ -33,6 +36,9 @@ EXPORTED = ["moe_weight_bytes", "moe_workspace_bytes", "moe_workspace_map", "moe
             "moe_intermediates", "moe_profile_enable", "moe_profile_read",
             "moe_profile_gemm_timeline", "moe_destroy",
             "moe_last_error", "moe_status_string", "moe_diag_stream_read", "moe_diag_bf16",
+            "moe_set_policy", "moe_quantize_e4m3", "moe_linear_weight_bytes",
+            "moe_linear_workspace_bytes", "moe_linear_init", "moe_linear_load",
+            "moe_linear_forward", "moe_linear_destroy", "moe_linear_last_error",
             # include/attn.h
             "attn_weight_bytes", "attn_cache_bytes", "attn_workspace_bytes", "attn_init",
             "attn_load_layer", "attn_load_post_norm", "attn_forward", "attn_forward_norm",
@@ -63,6 +69,18 @@ class MoeRouting(ctypes.Structure):
                 ("offsets", ctypes.c_void_p), ("pair_row", ctypes.c_void_p),
                 ("row_token", ctypes.c_void_p), ("T", ctypes.c_int32),
                 ("layer", ctypes.c_int32)]
+
+
+class MoePolicy(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("n_groups", ctypes.c_int32),
+                ("top_groups", ctypes.c_int32), ("group_best", ctypes.c_int32),
+                ("renormalize", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("balance", ctypes.c_void_p)]
+
+
+class LinearConfig(ctypes.Structure):
+    _fields_ = [("in_dim", ctypes.c_int32), ("out_dim", ctypes.c_int32),
+                ("max_tokens", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
 class AttnConfig(ctypes.Structure):
@@ -130,6 +148,19 @@ def lib():
         L.moe_status_string.restype = ctypes.c_char_p
         L.moe_diag_stream_read.argtypes = [P, ctypes.c_uint64, P, P]
         L.moe_diag_bf16.argtypes = [P, P, ctypes.c_uint64, P]
+        L.moe_set_policy.argtypes = [P, I, ctypes.POINTER(MoePolicy)]
+        L.moe_quantize_e4m3.argtypes = [P, ctypes.c_int64, I, I, I, P, P, P]
+        lcfg = ctypes.POINTER(LinearConfig)
+        for fn in ("moe_linear_weight_bytes", "moe_linear_workspace_bytes"):
+            getattr(L, fn).argtypes = [lcfg]
+            getattr(L, fn).restype = ctypes.c_size_t
+        L.moe_linear_init.argtypes = [lcfg, P, P, ctypes.POINTER(P)]
+        L.moe_linear_load.argtypes = [P, P, P]
+        L.moe_linear_forward.argtypes = [P, P, ctypes.c_int64, P, I, I, P]
+        L.moe_linear_destroy.argtypes = [P]
+        L.moe_linear_destroy.restype = None
+        L.moe_linear_last_error.argtypes = [P]
+        L.moe_linear_last_error.restype = ctypes.c_char_p
         acfg = ctypes.POINTER(AttnConfig)
         for fn in ("attn_weight_bytes", "attn_cache_bytes", "attn_workspace_bytes"):
             getattr(L, fn).argtypes = [acfg]
@@ -170,7 +201,8 @@ def lib():
                    "moe_forward_residual",
                    "moe_intermediates", "moe_profile_enable",
                    "moe_profile_read", "moe_profile_gemm_timeline", "moe_diag_stream_read",
-                   "moe_diag_bf16"):
+                   "moe_diag_bf16", "moe_set_policy", "moe_quantize_e4m3", "moe_linear_init",
+                   "moe_linear_load", "moe_linear_forward"):
             getattr(L, fn).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -247,6 +279,22 @@ def moe_forward_layers(ctx, first, n, x_ptr, T, stream=0):
 
 def moe_forward_residual(ctx, layer, x_ptr, r_ptr, T, stream=0):
     _check(ctx, lib().moe_forward_residual(ctx, layer, x_ptr, r_ptr, T, stream))
+
+
+def make_policy(score=SCORE_SELECTED, n_groups=1, top_groups=1, group_best=1, renormalize=True,
+                scale=1.0) -> MoePolicy:
+    """A routing policy (moe_policy of include/moe.h) without a balance."""
+    return MoePolicy(score, n_groups, top_groups, group_best, int(renormalize), scale, None)
+
+
+def moe_set_policy(ctx, layer, policy):
+    _check(ctx, lib().moe_set_policy(ctx, layer, ctypes.byref(policy) if policy is not None else None))
+
+
+def moe_quantize_e4m3(x_ptr, ld, x_type, T, n, codes_ptr, scales_ptr, stream=0):
+    st = lib().moe_quantize_e4m3(x_ptr, ld, x_type, T, n, codes_ptr, scales_ptr, stream)
+    if st != MOE_OK:
+        raise MoeError(st, lib().moe_status_string(st).decode())
 
 
 def moe_diag_stream_read(src_ptr, nbytes, out_ptr, stream=0):
@@ -353,6 +401,7 @@ class MoeLayer:
                           if workspace is None else workspace)
         self.ctx = moe_init(cfg, _tensor_ptr(self.arena, "arena", wb, (torch.uint8,), self.device),
                             _tensor_ptr(self.workspace, "workspace", sb, (torch.uint8,), self.device))
+        self._balance = {}   # layer: the balance that its policy reads
 
     @property
     def stream(self) -> int:
@@ -393,6 +442,20 @@ class MoeLayer:
         moe_load_router(self.ctx, layer, _tensor_ptr(wr, "wr", c.d_model * c.n_experts, f32, dev),
                         _tensor_ptr(bias, "bias", c.n_experts, f32, dev) if bias is not None else None,
                         int(on_dev), self.stream if on_dev else 0)
+
+    def set_policy(self, layer, policy, balance=None):
+        """moe_set_policy: policy from make_policy, or None; balance: fp32 [n_experts] on the
+        layer's device (kept here, and read by every routing of the layer), or None."""
+        if policy is None:
+            if balance is not None:
+                raise MoeError(-1, "a balance needs a policy")
+        else:
+            ptr = (_tensor_ptr(balance, "balance", self.cfg.n_experts, (self.torch.float32,), self.device)
+                   if balance is not None else None)
+            policy = MoePolicy(policy.score, policy.n_groups, policy.top_groups, policy.group_best,
+                               policy.renormalize, policy.scale, ptr)
+        moe_set_policy(self.ctx, layer, policy)
+        self._balance[layer] = balance
 
     def _tokens(self, x, T):
         T = x.shape[0] if T is None else int(T)
@@ -512,6 +575,140 @@ def wall_clock_hz(device: int = 0) -> float:
     if rc != 0:
         raise RuntimeError(f"hipDeviceGetAttribute failed: {rc}")
     return v.value * 1e3
+
+
+# ------------------------------------------------------ products in e4m3 --
+
+def _rows(t, name, T, n, dtypes, device):
+    """(pointer, row stride) of a [>= T, n] tensor whose rows are contiguous."""
+    if t is None:
+        raise MoeError(-1, f"{name} is None")
+    if t.dtype not in dtypes:
+        raise MoeError(-1, f"{name} has dtype {t.dtype}, expected one of {list(dtypes)}")
+    if device is not None and t.device != device:
+        raise MoeError(-1, f"{name} is on {t.device}, expected {device}")
+    if t.dim() != 2 or t.shape[0] < T or t.shape[1] != n:
+        raise MoeError(-2, f"{name} has shape {tuple(t.shape)}, the call uses [{T}, {n}]")
+    if T and n > 1 and t.stride(1) != 1:
+        raise MoeError(-1, f"the rows of {name} must be contiguous")
+    return t.data_ptr(), (t.stride(0) if T > 1 else n)
+
+
+def quantize_e4m3(x, codes, scales):
+    """moe_quantize_e4m3: x [T, n] fp32 or bf16 (bfloat16 or its bits), rows apart by any stride
+    of whole 16 bytes; codes (out) [T, n] float8_e4m3fn or uint8, scales (out) [T, ceil(n / 128)]
+    uint8 (or float8_e8m0fnu), both contiguous."""
+    import torch
+    bf = _bf16_types(torch)
+    if x is None or x.dim() != 2:
+        raise MoeError(-2, "x must be [T, n]")
+    if x.device.type != "cuda":
+        raise MoeError(-1, f"x is on {x.device}, expected a GPU")
+    T, n = x.shape
+    ptr, ld = _rows(x, "x", T, n, bf + (torch.float32,), None)
+    e8m0 = getattr(torch, "float8_e8m0fnu", torch.uint8)
+    with _on_device(torch, x.device):
+        moe_quantize_e4m3(ptr, ld, T_F32 if x.dtype == torch.float32 else T_BF16, T, n,
+                          _tensor_ptr(codes, "codes", T * n, (torch.float8_e4m3fn, torch.uint8), x.device),
+                          _tensor_ptr(scales, "scales", T * ((n + 127) // 128), (torch.uint8, e8m0), x.device),
+                          _raw_stream(torch, x.device))
+
+
+def make_linear_config(in_dim, out_dim, max_tokens=1, flags=0) -> LinearConfig:
+    return LinearConfig(in_dim, out_dim, max_tokens, flags)
+
+
+def moe_linear_weight_bytes(cfg: LinearConfig) -> int:
+    return int(lib().moe_linear_weight_bytes(ctypes.byref(cfg)))
+
+
+def moe_linear_workspace_bytes(cfg: LinearConfig) -> int:
+    return int(lib().moe_linear_workspace_bytes(ctypes.byref(cfg)))
+
+
+def _lcheck(ctx, status: int):
+    if status != MOE_OK:
+        raise MoeError(status, lib().moe_linear_last_error(ctx).decode())
+
+
+def moe_linear_init(cfg: LinearConfig, weights_ptr: int, workspace_ptr: int) -> int:
+    out = ctypes.c_void_p()
+    _lcheck(None, lib().moe_linear_init(ctypes.byref(cfg), weights_ptr, workspace_ptr, ctypes.byref(out)))
+    return out.value
+
+
+def moe_linear_load(ctx, w_ptr, stream=0):
+    _lcheck(ctx, lib().moe_linear_load(ctx, w_ptr, stream))
+
+
+def moe_linear_forward(ctx, x_ptr, ldx, y_ptr, y_type, T, stream=0):
+    _lcheck(ctx, lib().moe_linear_forward(ctx, x_ptr, ldx, y_ptr, y_type, T, stream))
+
+
+class E4m3Linear:
+    """A product with weights in e4m3 (moe_linear of include/moe.h): owns a context plus its
+    torch-allocated weights and workspace on one GPU (argument marshalling only)."""
+
+    def __init__(self, cfg: LinearConfig, device="cuda", weights=None, workspace=None):
+        """weights / workspace: caller-owned uint8 device tensors of at least
+        moe_linear_weight_bytes / moe_linear_workspace_bytes (allocated here if None)."""
+        import torch
+        self.torch = torch
+        self.cfg = cfg
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise MoeError(-1, f"the product runs on a GPU, not on {self.device}")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        wb, sb = moe_linear_weight_bytes(cfg), moe_linear_workspace_bytes(cfg)
+        if not (wb and sb):
+            raise MoeError(-2, "invalid linear config")
+
+        def buf(t, n, name):
+            if t is None:
+                return torch.empty(n, dtype=torch.uint8, device=self.device)
+            _tensor_ptr(t, name, n, (torch.uint8,), self.device)
+            return t
+        self.weights = buf(weights, wb, "weights")
+        self.workspace = buf(workspace, sb, "workspace")
+        self.ctx = moe_linear_init(cfg, self.weights.data_ptr(), self.workspace.data_ptr())
+
+    @property
+    def stream(self) -> int:
+        return _raw_stream(self.torch, self.device)
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            lib().moe_linear_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def load(self, w):
+        """moe_linear_load: w bf16 [in_dim, out_dim], contiguous, on the GPU."""
+        c = self.cfg
+        if w is not None and tuple(w.shape) != (c.in_dim, c.out_dim):
+            raise MoeError(-2, f"w has shape {tuple(w.shape)}, expected [{c.in_dim}, {c.out_dim}]")
+        with _on_device(self.torch, self.device):
+            moe_linear_load(self.ctx, _tensor_ptr(w, "w", c.in_dim * c.out_dim, _bf16_types(self.torch), self.device),
+                            self.stream)
+
+    def forward(self, x, y, T=None):
+        """moe_linear_forward: x bf16 [T, in_dim], rows apart by any stride of whole 16 bytes;
+        y (out) [T, out_dim] float32 or bf16, contiguous."""
+        c, torch = self.cfg, self.torch
+        if x is None or x.dim() != 2:
+            raise MoeError(-2, "x must be [T, in_dim]")
+        T = x.shape[0] if T is None else int(T)
+        bf = _bf16_types(torch)
+        ptr, ldx = _rows(x, "x", T, c.in_dim, bf, self.device)
+        with _on_device(torch, self.device):
+            moe_linear_forward(self.ctx, ptr, ldx, _tensor_ptr(y, "y", T * c.out_dim, bf + (torch.float32,), self.device),
+                               T_F32 if y.dtype == torch.float32 else T_BF16, T, self.stream)
 
 
 # ------------------------------------------------------- attention block --

@@ -15,8 +15,6 @@ constexpr int kFewRuns = 512;      // workgroups that divided positions of few()
 constexpr int kTile = 32;          // positions of a step of one wave of few()
 constexpr int kStep = 64;          // positions of a workgroup's step of tile()
 constexpr int kPartPad = 4;        // maximum, weight and padding behind the hd sums of a partial row
-constexpr int kExpMin = -100;      // exponents of an e4m3 page's scale
-constexpr int kExpMax = 119;        // 448 * 2^119 is the largest such that is a bf16
 
 // A token: its position and its page (the slot is position % page_size), or -1.
 struct Token {

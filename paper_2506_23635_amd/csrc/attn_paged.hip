@@ -11,15 +11,23 @@
 #include <type_traits>
 
 #include "attn_paged.h"
+#include "e4m3.h"
 #include "attn_weights.h"
 #include "moe_common.h"
 
 namespace paged {
 
 using moe::base2;
+using moe::code4;
 using moe::decay;
+using moe::decode8;
+using moe::exp2i;
 using moe::f32x4_t;
 using moe::far_scores;
+using moe::finite;
+using moe::kExpMax;
+using moe::kExpMin;
+using moe::scale_exponent;
 using moe::u32x4_t;
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
@@ -223,30 +231,6 @@ __device__ __forceinline__ void append_rows(const Args& a, const Source& x, uint
     *reinterpret_cast<uint2*>(dst + f + (turn ? half : 4)) = pack_bf16x4(v.hi);
 }
 
-// The least exponent e of kExpMin .. kExpMax with amax <= 448 * 2^e = 1.75 *
-// 2^(e + 8), from the bits of a finite amax >= 0: the carry of the addition is
-// 1 where the mantissa is past 1.75.  (Past kExpMax values end at 448.)
-__device__ inline int scale_exponent(float amax)
-{
-    const int e = (int)((__float_as_uint(amax) + (0x7FFFFFu - 0x600000u)) >> 23) - 127 - 8;
-    return min(max(e, kExpMin), kExpMax);
-}
-
-__device__ inline float exp2i(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
-
-__device__ inline bool finite(float v) { return (__float_as_uint(v) & 0x7F800000u) != 0x7F800000u; }
-
-// four values times 2^-e as e4m3 codes; what is not finite becomes NaN
-__device__ inline uint32_t code4(const float* v, float inv)
-{
-    float w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = finite(v[i]) ? fminf(fmaxf(v[i] * inv, -448.f), 448.f) : NAN;
-    int c = __builtin_amdgcn_cvt_pk_fp8_f32(w[0], w[1], 0, false);
-    c = __builtin_amdgcn_cvt_pk_fp8_f32(w[2], w[3], c, true);
-    return (uint32_t)c;
-}
-
 // codes rounded again for a scale that grew: value * ratio, ratio a power of two
 __device__ inline uint32_t recode4(uint32_t c, float ratio)
 {
@@ -339,15 +323,6 @@ __global__ __launch_bounds__(256) void append_kernel(Args a, Source x, uint16_t*
 }
 
 // ----------------------------------------------------------------- attend --
-
-// eight e4m3 codes as eight bf16 of code * scale (exact: a power of two)
-__device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
-{
-    return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, false)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, true)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, false)),
-                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
-}
 
 // Four rows of 16 dims, 16-bit, transposed on their way from LDS: lane n of
 // each 16 supplies the address of dims 4 (n % 4) .. + 3 of row n / 4 and gets

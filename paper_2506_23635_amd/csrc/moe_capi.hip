@@ -6,6 +6,7 @@
 // once into a persistent array and indexed per layer).
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
@@ -33,6 +34,8 @@ struct Layout {
     // workspace
     size_t dpart_off, logits_off, idx_off, w_off, counts_off, offsets_off, pair_row_off,
         row_token_off, active_off, tiles_off, n_tiles_off, h_off, o_off, ws_bytes;
+    // MOE_E4M3: scales of gate, up and down in an expert; H's fp32 values
+    size_t sg_off, su_off, sd_off, h32_off;
     size_t region_off[MOE_WS_COUNT], region_bytes[MOE_WS_COUNT];   // moe_workspace_map
     int rows_max, max_tiles;
 };
@@ -53,7 +56,7 @@ const char* check_config(const moe_config* c)
         return "max_tokens * d_model * 2 must stay below 2^31 (32-bit gather offsets)";
     if ((int64_t)c->d_model * c->ffn_dim * 4 > INT32_MAX)
         return "d_model * ffn_dim * 4 (one expert's gate/up slab) must stay below 2^31";
-    if (c->flags & ~MOE_PARTIAL_F32) return "flags: only MOE_PARTIAL_F32 is defined";
+    if (c->flags & ~(MOE_PARTIAL_F32 | MOE_E4M3)) return "flags: only MOE_PARTIAL_F32 and MOE_E4M3 are defined";
     return nullptr;
 }
 
@@ -65,9 +68,18 @@ Layout make_layout(const moe_config* c)
     L.router_bytes = align_up(d * E * 4, kAlign);
     L.bias_off = L.router_bytes;
     L.experts_off = L.router_bytes + align_up(E * 4, kAlign);
-    L.gu_bytes = 2 * f * d * 2;
-    L.dn_bytes = d * f * 2;
+    const bool e4m3 = (c->flags & MOE_E4M3) != 0;
+    const size_t size = e4m3 ? 1 : 2;
+    L.gu_bytes = 2 * f * d * size;
+    L.dn_bytes = d * f * size;
     L.expert_bytes = L.gu_bytes + L.dn_bytes;
+    if (e4m3) {
+        const size_t up = f / moe::kBlock * moe::scale_quads((int)d) * 4;
+        L.sg_off = L.expert_bytes;
+        L.su_off = L.sg_off + up;
+        L.sd_off = L.su_off + up;
+        L.expert_bytes = align_up(L.sd_off + d / moe::kBlock * moe::scale_quads((int)f) * 4, kAlign);
+    }
     L.layer_bytes = L.experts_off + nl * L.expert_bytes;
     L.arena_bytes = L.layer_bytes * (size_t)c->n_layers;
 
@@ -94,7 +106,13 @@ Layout make_layout(const moe_config* c)
     L.active_off = take(MOE_WS_ACTIVE, (E + 1) * 4);
     L.tiles_off = take(MOE_WS_TILES, (size_t)L.max_tiles * 2 * 4);
     L.n_tiles_off = take(MOE_WS_N_TILES, 4);
-    L.h_off = take(MOE_WS_H, (size_t)L.rows_max * f * 2);
+    size_t h_bytes = (size_t)L.rows_max * f * 2;
+    if (e4m3) {
+        L.h32_off = align_up(h_bytes, kAlign);
+        h_bytes = L.h32_off + (size_t)L.rows_max * f * 4;
+    }
+    L.h_off = take(MOE_WS_H, h_bytes);
+    L.h32_off += L.h_off;
     L.o_off = take(MOE_WS_O, (size_t)L.rows_max * d * 4);
     L.ws_bytes = off;
     return L;
@@ -106,7 +124,7 @@ thread_local std::string g_init_error;
 // scratch (moe_forward_static).
 struct WsView {
     uint8_t* base;
-    size_t dpart_off, h_off, o_off;
+    size_t dpart_off, h_off, o_off, h32_off;
     moe::RouteView rv;
 };
 
@@ -114,6 +132,7 @@ WsView make_ws_view(uint8_t* w, const Layout& L)
 {
     WsView v{};
     v.base = w;
+    v.h32_off = L.h32_off;
     v.dpart_off = L.dpart_off;
     v.h_off = L.h_off;
     v.o_off = L.o_off;
@@ -140,6 +159,7 @@ struct moe_ctx {
     std::vector<uint8_t> router_loaded;   // [n_layers]
     std::vector<uint8_t> has_bias;        // [n_layers]
     std::vector<uint8_t> expert_loaded;   // [n_layers * n_local]
+    std::vector<moe::Policy> policy;      // [n_layers]
     // per-kernel timing (moe_profile_*): an event pair around each launch
     bool prof_on;
     std::vector<hipEvent_t> prof_events;   // 2 per launch slot
@@ -213,26 +233,27 @@ moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x
     const float* bias = ctx->has_bias[layer] ? reinterpret_cast<const float*>(lb + ctx->L.bias_off)
                                              : nullptr;
     const int tile_rows = moe_prefill_tile_rows();
+    const moe::Policy* policy = &ctx->policy[layer];
     hipError_t e;
     if (!logits_in && moe_route_decode_ok(T, c.n_experts, c.top_k)) {
         double* dpart = reinterpret_cast<double*>(ws.base + ws.dpart_off);
         e = timed(ctx, MOE_K_ROUTE, s, [&] {
             return moe_launch_route_decode(x, wrT, bias, dpart, T, c.d_model, c.n_experts,
                                            c.top_k, c.expert_begin, c.n_local_experts, tile_rows,
-                                           &ws.rv, s);
+                                           policy, &ws.rv, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "route kernel launch");
     } else {
         if (!logits_in) {
             e = timed(ctx, MOE_K_ROUTER, s, [&] {
                 return moe_launch_router_select(x, wrT, bias, T, c.d_model, c.n_experts,
-                                                c.top_k, &ws.rv, s);
+                                                c.top_k, policy, &ws.rv, s);
             });
             if (e != hipSuccess) return hip_fail(ctx, e, "router kernel launch");
         }
         e = timed(ctx, MOE_K_ROUTE, s, [&] {
             return moe_launch_route(logits_in, T, c.n_experts, c.top_k, c.expert_begin,
-                                    c.n_local_experts, tile_rows, &ws.rv, s);
+                                    c.n_local_experts, tile_rows, policy, &ws.rv, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "route kernel launch");
     }
@@ -253,9 +274,59 @@ void fill_routing(moe_ctx* ctx, int layer, int T, moe_routing* out)
     out->layer = layer;
 }
 
+// The experts of a MOE_E4M3 layer: x rounded to the e4m3 grid (into O's space:
+// the down products come after its last reader), gate and up, H rounded, down.
+moe_status run_experts_e4m3(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T, hipStream_t s)
+{
+    const moe_config& c = ctx->cfg;
+    const Layout& L = ctx->L;
+    const int d = c.d_model, f = c.ffn_dim;
+    const uint8_t* experts = layer_base(ctx, layer) + L.experts_off;
+    uint16_t* xq = reinterpret_cast<uint16_t*>(ws.base + ws.o_off);
+    uint16_t* H = reinterpret_cast<uint16_t*>(ws.base + ws.h_off);
+    float* h32 = reinterpret_cast<float*>(ws.base + ws.h32_off);
+    const int max_rows = T * std::min(c.top_k, c.n_local_experts);
+    moe::E4m3Args gu{};
+    gu.w = experts;
+    gu.ws = experts + L.sg_off;
+    gu.ws_up = experts + L.su_off;
+    gu.expert_bytes = L.expert_bytes;
+    gu.x = xq;
+    gu.K = d;
+    gu.N = f;
+    gu.active = ws.rv.active;
+    gu.counts = ws.rv.counts;
+    gu.offsets = ws.rv.offsets;
+    gu.row_token = ws.rv.row_token;
+    gu.e_begin = c.expert_begin;
+    gu.T = T;
+    gu.h32 = h32;
+    moe::E4m3Args dn = gu;
+    dn.w = experts + L.gu_bytes;
+    dn.ws = experts + L.sd_off;
+    dn.x = H;
+    dn.K = f;
+    dn.N = d;
+    dn.y32 = reinterpret_cast<float*>(ws.base + ws.o_off);
+    const int slots = (int)std::min<int64_t>(c.n_local_experts, (int64_t)T * c.top_k);
+    hipError_t e = timed(ctx, MOE_K_DECODE_GATEUP, s, [&] {
+        const hipError_t r = moe_launch_quantize(x, d, 1, T, nullptr, d, d, nullptr, nullptr, xq, s);
+        return r != hipSuccess ? r : moe_launch_e4m3_gateup_few(&gu, slots, s);
+    });
+    if (e != hipSuccess) return hip_fail(ctx, e, "e4m3 gate/up kernel launch");
+    e = timed(ctx, MOE_K_DECODE_DOWN, s, [&] {
+        const hipError_t r =
+            moe_launch_quantize(h32, f, 0, max_rows, ws.rv.offsets + c.n_experts, f, f, nullptr, nullptr, H, s);
+        return r != hipSuccess ? r : moe_launch_e4m3_down_few(&dn, slots, s);
+    });
+    if (e != hipSuccess) return hip_fail(ctx, e, "e4m3 down kernel launch");
+    return MOE_OK;
+}
+
 moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T,
                        hipStream_t s)
 {
+    if (ctx->cfg.flags & MOE_E4M3) return run_experts_e4m3(ctx, ws, layer, x, T, s);
     const moe_config& c = ctx->cfg;
     const uint8_t* experts = layer_base(ctx, layer) + ctx->L.experts_off;
     uint16_t* H = reinterpret_cast<uint16_t*>(ws.base + ws.h_off);
@@ -401,6 +472,7 @@ moe_status moe_init(const moe_config* cfg, void* weight_arena, void* workspace, 
     c->router_loaded.assign(cfg->n_layers, 0);
     c->has_bias.assign(cfg->n_layers, 0);
     c->expert_loaded.assign((size_t)cfg->n_layers * cfg->n_local_experts, 0);
+    c->policy.assign(cfg->n_layers, moe::Policy{});
     c->route_valid = false;
     c->route_layer = -1;
     c->route_T = 0;
@@ -427,16 +499,20 @@ moe_status moe_load_expert(moe_ctx* ctx, int32_t layer, int32_t expert, const ui
                    (size_t)(expert - c.expert_begin) * ctx->L.expert_bytes;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int d = c.d_model, f = c.ffn_dim;
+    const bool e4m3 = (c.flags & MOE_E4M3) != 0;
     if (src_on_device) {
         if (misaligned(gate) || misaligned(up) || misaligned(down))
             return fail(ctx, MOE_E_ALIGN, "device weight pointers must be 16-byte aligned");
         hipError_t e;
-        auto pk = [&](const uint16_t* src, int K, int N, uint8_t* to, int mul, int add) {
-            return timed(ctx, MOE_K_PACK, s, [&] { return moe_launch_pack(src, K, N, to, mul, add, s); });
+        auto pk = [&](const uint16_t* src, int K, int N, uint8_t* to, int mul, int add, size_t scales) {
+            return timed(ctx, MOE_K_PACK, s, [&] {
+                return e4m3 ? moe_launch_pack_e4m3(src, K, N, K, N, to, dst + scales, mul, add, s)
+                            : moe_launch_pack(src, K, N, to, mul, add, s);
+            });
         };
-        if ((e = pk(gate, d, f, dst, 2, 0)) != hipSuccess ||
-            (e = pk(up, d, f, dst, 2, 1)) != hipSuccess ||
-            (e = pk(down, f, d, dst + ctx->L.gu_bytes, 1, 0)) != hipSuccess)
+        if ((e = pk(gate, d, f, dst, 2, 0, ctx->L.sg_off)) != hipSuccess ||
+            (e = pk(up, d, f, dst, 2, 1, ctx->L.su_off)) != hipSuccess ||
+            (e = pk(down, f, d, dst + ctx->L.gu_bytes, 1, 0, ctx->L.sd_off)) != hipSuccess)
             return hip_fail(ctx, e, "pack kernel launch");
     } else {
         std::vector<uint8_t> tmp;
@@ -445,9 +521,15 @@ moe_status moe_load_expert(moe_ctx* ctx, int32_t layer, int32_t expert, const ui
         } catch (...) {
             return fail(ctx, MOE_E_ARG, "out of host memory for the host repack");
         }
-        moe_pack_host(gate, d, f, tmp.data(), 2, 0);
-        moe_pack_host(up, d, f, tmp.data(), 2, 1);
-        moe_pack_host(down, f, d, tmp.data() + ctx->L.gu_bytes, 1, 0);
+        if (e4m3) {
+            moe_pack_e4m3_host(gate, d, f, tmp.data(), tmp.data() + ctx->L.sg_off, 2, 0);
+            moe_pack_e4m3_host(up, d, f, tmp.data(), tmp.data() + ctx->L.su_off, 2, 1);
+            moe_pack_e4m3_host(down, f, d, tmp.data() + ctx->L.gu_bytes, tmp.data() + ctx->L.sd_off, 1, 0);
+        } else {
+            moe_pack_host(gate, d, f, tmp.data(), 2, 0);
+            moe_pack_host(up, d, f, tmp.data(), 2, 1);
+            moe_pack_host(down, f, d, tmp.data() + ctx->L.gu_bytes, 1, 0);
+        }
         hipError_t e = hipMemcpyAsync(dst, tmp.data(), tmp.size(), hipMemcpyHostToDevice, s);
         if (e == hipSuccess) e = hipStreamSynchronize(s);
         if (e != hipSuccess) return hip_fail(ctx, e, "host-to-device copy of packed expert");
@@ -493,6 +575,41 @@ moe_status moe_load_router(moe_ctx* ctx, int32_t layer, const float* wr, const f
     if (ctx->route_layer == layer) ctx->route_valid = false;   // routed with the old router
     ctx->router_loaded[layer] = 1;
     ctx->has_bias[layer] = bias ? 1 : 0;
+    return MOE_OK;
+}
+
+moe_status moe_set_policy(moe_ctx* ctx, int32_t layer, const moe_policy* policy)
+{
+    if (!ctx) return MOE_E_ARG;
+    if (layer < 0 || layer >= ctx->cfg.n_layers) return fail(ctx, MOE_E_ARG, "layer out of range");
+    moe::Policy p{};
+    if (policy) {
+        const int E = ctx->cfg.n_experts, k = ctx->cfg.top_k;
+        if (policy->score < MOE_SCORE_SELECTED || policy->score > MOE_SCORE_SIGMOID)
+            return fail(ctx, MOE_E_ARG, "score is no moe_score");
+        if (policy->n_groups < 1 || policy->n_groups > E || E % policy->n_groups)
+            return fail(ctx, MOE_E_SHAPE, "n_groups must divide n_experts");
+        const int per = E / policy->n_groups;
+        if (policy->top_groups < 1 || policy->top_groups > policy->n_groups)
+            return fail(ctx, MOE_E_ARG, "top_groups must be in [1, n_groups]");
+        if (policy->top_groups * per < k) return fail(ctx, MOE_E_SHAPE, "top_groups groups hold fewer than top_k experts");
+        if (policy->group_best < 1 || policy->group_best > 2 || policy->group_best > per)
+            return fail(ctx, MOE_E_ARG, "group_best must be 1 or 2, and at most a group's experts");
+        if (policy->renormalize != 0 && policy->renormalize != 1)
+            return fail(ctx, MOE_E_ARG, "renormalize must be 0 or 1");
+        if (!std::isfinite(policy->scale)) return fail(ctx, MOE_E_ARG, "scale must be finite");
+        if (misaligned(policy->balance)) return fail(ctx, MOE_E_ALIGN, "balance must be 16-byte aligned");
+        p.on = 1;
+        p.score = policy->score;
+        p.n_groups = policy->n_groups;
+        p.top_groups = policy->top_groups;
+        p.group_best = policy->group_best;
+        p.renormalize = policy->renormalize;
+        p.scale = policy->scale;
+        p.balance = policy->balance;
+    }
+    if (ctx->route_layer == layer) ctx->route_valid = false;   // routed under the old policy
+    ctx->policy[layer] = p;
     return MOE_OK;
 }
 

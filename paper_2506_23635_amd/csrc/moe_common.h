@@ -105,6 +105,13 @@ struct RouteView {
     int32_t* n_tiles;     // [1]
 };
 
+// A layer's routing policy (moe_policy of include/moe.h); on == 0: none is set.
+struct Policy {
+    int on, score, n_groups, top_groups, group_best, renormalize;
+    float scale;
+    const float* balance;     // [E], or NULL
+};
+
 // Arguments of the decode expert kernels (moe_decode.hip).
 struct DecodeArgs {
     const uint8_t* experts;   // arena: first local expert of this layer
@@ -146,6 +153,32 @@ struct GemmArgs {
     int max_stamps;
 };
 
+// Packed weights in e4m3: 16-row x 64-K tiles of 1 KiB.  Granule (g, r) of a tile,
+// at byte 256 g + 16 r (g 0..3), holds K 8 g .. 8 g + 7 and 32 + 8 g .. 32 + 8 g + 7
+// of row r: one 16-byte load brings a lane its operands of two consecutive
+// 16x16x32 instructions, or of two 32x32x16 ones (granule l / 32: K steps 0 and
+// 2, granule 2 + l / 32: 1 and 3).  Row tiles as above (gate and up in turn).
+// Scales of a matrix: one byte e + 127 per 128 x 128 block, [features / 128]
+// [scale_quads(K) * 4].
+constexpr int kBlock = 128;
+constexpr int kTileK8 = 64;
+__host__ __device__ inline int scale_quads(int K) { return (K + 4 * kBlock - 1) / (4 * kBlock); }
+
+// Arguments of the products of few rows in e4m3: of a layer's experts (active
+// set), or of one matrix with rows 0 .. T - 1.
+struct E4m3Args {
+    const uint8_t* w;          // first local expert's packed matrix (gate and up interleaved), ...
+    const uint8_t *ws, *ws_up; // ... its scales, those of up
+    uint64_t expert_bytes;     // from expert to expert, of all three
+    const uint16_t* x;         // rows [..][K], bf16 on the e4m3 grid
+    int K, N;                  // N features (of gate and up: of each)
+    const int32_t *active, *counts, *offsets, *row_token;
+    int e_begin, T;
+    float* h32;                // gate/up: silu(G) U [rows][N]
+    float* y32;                // products [rows][N], or
+    uint16_t* y16;             // ... rounded to bf16
+};
+
 }  // namespace moe
 
 // Launchers (one per kernel family); each returns the launch status.
@@ -161,12 +194,14 @@ int moe_route_decode_ok(int T, int E, int k);
 int moe_route_decode_wgs(int d);
 hipError_t moe_launch_route_decode(const uint16_t* x, const float* wrT, const float* bias,
                                    double* partial, int T, int d, int E, int k, int e_begin,
-                                   int n_local, int tile_rows,
+                                   int n_local, int tile_rows, const moe::Policy* policy,
                                    const moe::RouteView* rv, hipStream_t s);
 hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT, const float* bias, int T,
-                                   int d, int E, int k, const moe::RouteView* rv, hipStream_t s);
+                                   int d, int E, int k, const moe::Policy* policy,
+                                   const moe::RouteView* rv, hipStream_t s);
 hipError_t moe_launch_route(const float* logits_in, int T, int E, int k, int e_begin, int n_local,
-                            int tile_rows, const moe::RouteView* rv, hipStream_t s);
+                            int tile_rows, const moe::Policy* policy, const moe::RouteView* rv,
+                            hipStream_t s);
 hipError_t moe_launch_transpose_router(const float* wr, int d, int E, float* wrT, hipStream_t s);
 hipError_t moe_launch_decode_gateup(const moe::DecodeArgs* a, int n_slots, hipStream_t s);
 hipError_t moe_launch_decode_down(const moe::DecodeArgs* a, int n_slots, hipStream_t s);
@@ -180,6 +215,18 @@ int moe_gemm_plain_split(int T, int M);
 hipError_t moe_launch_combine(const float* O, const int32_t* pair_row, const float* topk_w, int T,
                               int d, int k, uint16_t* y, float* y32, uint16_t* x_residual,
                               hipStream_t s);
+}
+
+// Launchers of the products in e4m3 (moe_e4m3.hip).
+extern "C" {
+hipError_t moe_launch_quantize(const void* x, int64_t ld, int bf16, int64_t T, const int32_t* n_rows, int n,
+                               int n_pad, uint8_t* codes, uint8_t* scales, uint16_t* values, hipStream_t s);
+hipError_t moe_launch_pack_e4m3(const uint16_t* src, int K, int N, int K_pad, int N_pad, uint8_t* dst,
+                                uint8_t* scales, int rt_mul, int rt_add, hipStream_t s);
+void moe_pack_e4m3_host(const uint16_t* src, int K, int N, uint8_t* dst, uint8_t* scales, int rt_mul, int rt_add);
+hipError_t moe_launch_e4m3_gateup_few(const moe::E4m3Args* a, int n_slots, hipStream_t s);
+hipError_t moe_launch_e4m3_down_few(const moe::E4m3Args* a, int n_slots, hipStream_t s);
+hipError_t moe_launch_e4m3_linear_few(const moe::E4m3Args* a, hipStream_t s);
 }
 
 // Launchers of the attention-block kernels (attn.hip).

@@ -1,0 +1,303 @@
+// moe_e4m3.hip -- 8-bit floating point for the experts and for plain products
+// (include/moe.h, "Products in e4m3"): coding rows and weights, and the products
+// of few rows (many rows: moe_prefill.hip).
+//
+// A code times its scale, a power of two, has 4 significant bits, so it is a
+// bf16 exactly, and products of two of them are exact in fp32.  The matrix
+// products therefore run on the bf16 instructions, weights decoded in registers
+// (v_cvt_scalef32_pk_bf16_fp8: two codes and their scale), rows kept as bf16
+// values on the e4m3 grid.  The matrix instructions that take 8-bit operands
+// would do the same work at twice the rate, but their sums are not fp32 sums:
+// within a lane's terms they are aligned to the largest and lose what lies below
+// 2^-13 of it (probed with powers of two; all three forms, 16x16x32 and the
+// scaled 16x16x128 and 32x32x64).  A product of 333 x 1040 x 1488 came out 4.9e-5
+// from its fp64 value so, where fp32 sums leave 1e-7, and it moves silu(G) U
+// across rounding borders before the down product.
+#include <cmath>
+#include <cstring>
+
+#include "e4m3.h"
+#include "moe_common.h"
+
+namespace moe {
+
+// ------------------------------------------------------------------ coding --
+
+// Eight values with scale 2^e as the bf16 values that their codes stand for.
+__device__ __forceinline__ u32x4_t round8(const float* v, int e)
+{
+    const float inv = exp2i(-e), scale = exp2i(e);
+    const uint32_t c0 = code4(v, inv), c1 = code4(v + 4, inv);
+    return decode8(c0, c1, scale);
+}
+
+// Rows to codes and scales, or (codes NULL) to the bf16 values that these stand
+// for: 16 lanes per block of 128, 8 elements each.  The block's maximum is formed
+// across the lanes; rows are read once and written once, so the kernel is bound
+// by memory.  Values from n to n_pad are zeros.  n_rows (device memory): rows that
+// there are, of at most T; or NULL.
+template <bool kBf16>
+__global__ __launch_bounds__(256) void quantize_kernel(const void* __restrict__ x, int64_t ld, int64_t T,
+                                                       const int32_t* __restrict__ n_rows, int n, int n_pad,
+                                                       uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                       uint16_t* __restrict__ values)
+{
+    if (n_rows) T = min(T, (int64_t)*n_rows);
+    const int blocks = (n + kBlock - 1) / kBlock, piece = threadIdx.x % 16;
+    for (int64_t u = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; u < T * blocks; u += (int64_t)gridDim.x * 16) {
+        const int64_t t = u / blocks;
+        const int b = (int)(u - t * blocks), k = b * kBlock + piece * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (k < n) {
+            if constexpr (kBf16) {
+                const u32x4_t p = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(x) + t * ld + k);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[2 * i] = __uint_as_float(p[i] << 16);
+                    v[2 * i + 1] = __uint_as_float(p[i] & 0xFFFF0000u);
+                }
+            } else {
+                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + t * ld + k);
+                const float4 p0 = p[0], p1 = p[1];
+                v[0] = p0.x; v[1] = p0.y; v[2] = p0.z; v[3] = p0.w;
+                v[4] = p1.x; v[5] = p1.y; v[6] = p1.z; v[7] = p1.w;
+            }
+        }
+        float amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (finite(v[i])) amax = fmaxf(amax, fabsf(v[i]));
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 16));
+        const int e = scale_exponent(amax);
+        if (codes) {
+            const float inv = exp2i(-e);
+            if (k < n) *reinterpret_cast<uint2*>(codes + t * n + k) = make_uint2(code4(v, inv), code4(v + 4, inv));
+            if (piece == 0) scales[t * blocks + b] = (uint8_t)(e + 127);
+        } else if (k < n_pad) {
+            *reinterpret_cast<u32x4_t*>(values + t * n_pad + k) = round8(v, e);
+        }
+    }
+}
+
+// Weights src bf16 [K][N] to the packed layout and the scales of their 128 x 128
+// blocks, one block per workgroup: feature n goes to row tile (n / 16) rt_mul +
+// rt_add.  Rows and features past K and N (up to whole blocks) are zeros.
+__global__ __launch_bounds__(256) void pack_e4m3_kernel(const uint16_t* __restrict__ src, int K, int N,
+                                                        uint8_t* __restrict__ dst, uint8_t* __restrict__ scales,
+                                                        int KT, int scale_ld, int rt_mul, int rt_add)
+{
+    __shared__ uint16_t tile[kBlock][kBlock + 2];
+    __shared__ float s_max[4];
+    const int n0 = blockIdx.x * kBlock, kt = blockIdx.y, k0 = kt * kBlock, tid = threadIdx.x;
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = i * 16 + tid / 16, c = tid % 16 * 8;
+        u32x4_t v = {0u, 0u, 0u, 0u};
+        if (k0 + r < K && n0 + c < N) v = *reinterpret_cast<const u32x4_t*>(src + (int64_t)(k0 + r) * N + n0 + c);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            *reinterpret_cast<uint32_t*>(&tile[r][c + 2 * j]) = v[j];
+            const float lo = __uint_as_float(v[j] << 16), hi = __uint_as_float(v[j] & 0xFFFF0000u);
+            if (finite(lo)) amax = fmaxf(amax, fabsf(lo));
+            if (finite(hi)) amax = fmaxf(amax, fabsf(hi));
+        }
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
+    if (tid % 64 == 0) s_max[tid / 64] = amax;
+    __syncthreads();
+    const int e = scale_exponent(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])));
+    // the last block's workgroup also clears the bytes up to the row's end
+    if (tid == 0) scales[(int64_t)blockIdx.x * scale_ld + kt] = (uint8_t)(e + 127);
+    else if (kt + 1 == (int)gridDim.y && kt + tid < scale_ld) scales[(int64_t)blockIdx.x * scale_ld + kt + tid] = 0;
+    const float inv = exp2i(-e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        // granule c % 4 of the block's K tile c / 4: K 8 g .. 8 g + 7 and 32 on
+        const int g = i * 256 + tid, n = g % kBlock, c = g / kBlock;
+        u32x4_t w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = c / 4 * kTileK8 + j / 2 * 32 + c % 4 * 8 + j % 2 * 4;
+            float v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = bf16_to_f32(tile[k + q][n]);
+            w[j] = code4(v, inv);
+        }
+        const int64_t rt = (int64_t)((n0 + n) / kTileRows) * rt_mul + rt_add;
+        *reinterpret_cast<u32x4_t*>(dst + (rt * KT + kt * 2 + c / 4) * kTileBytes + c % 4 * 256 + n % kTileRows * 16) = w;
+    }
+}
+
+// --------------------------------------------------------------- few rows --
+//
+// At most 16 rows per expert (or of a plain product): the weights are streamed
+// once, one 16-feature tile (gate/up: the tiles of both) per workgroup, the K
+// tiles dealt to its waves in turn, as in the bf16 decode kernels.  The weight
+// tile is the A operand, the rows are the B operand.
+
+constexpr int kFewWaves = 8;
+
+enum { kFewGateUp = 0, kFewDown = 1, kFewLinear = 2 };
+
+template <int kMode>
+__global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
+{
+    constexpr int kM = kMode == kFewGateUp ? 2 : 1;      // row tiles per workgroup
+    __shared__ f32x4_t s_red[kM][(kFewWaves - 1) * 64];
+    const int n_tiles = a.N / kTileRows, slot = blockIdx.x / n_tiles, p = blockIdx.x % n_tiles;
+    int e = 0, m = a.T, row0 = 0;
+    if (kMode != kFewLinear) {
+        if (slot >= a.active[0]) return;
+        e = a.active[1 + slot];
+        m = a.counts[e];
+        row0 = a.offsets[e];
+        e -= a.e_begin;
+    }
+    const int lane = threadIdx.x % 64, w = threadIdx.x / 64, j = lane % 16, g = lane / 16;
+    const int KT = a.K / kTileK8, scale_ld = scale_quads(a.K) * 4;
+    const uint64_t at = (uint64_t)e * a.expert_bytes;
+    const uint8_t* pw = a.w + at + (uint64_t)p * kM * KT * kTileBytes + lane * 16;
+    const uint8_t* ps[2] = {a.ws + at + (int64_t)(p * kTileRows / kBlock) * scale_ld,
+                            kM == 2 ? a.ws_up + at + (int64_t)(p * kTileRows / kBlock) * scale_ld : nullptr};
+    for (int j0 = 0; j0 < m; j0 += 16) {
+        const bool live = j0 + j < m;
+        const int64_t row = live ? (kMode == kFewGateUp ? a.row_token[row0 + j0 + j] : row0 + j0 + j) : 0;
+        const uint16_t* px = a.x + row * a.K + g * 8;
+        f32x4_t acc[kM];
+#pragma unroll
+        for (int i = 0; i < kM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int kt = w; kt < KT; kt += kFewWaves) {
+            u32x4_t b0 = {0u, 0u, 0u, 0u}, b1 = b0;
+            if (live) {
+                b0 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8);
+                b1 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8 + 32);
+            }
+#pragma unroll
+            for (int i = 0; i < kM; ++i) {
+                const u32x4_t c = *reinterpret_cast<const u32x4_t*>(pw + ((int64_t)i * KT + kt) * kTileBytes);
+                const float scale = exp2i((int)ps[i][kt / 2] - 127);
+                acc[i] = mfma16x16x32(decode8(c[0], c[1], scale), b0, acc[i]);
+                acc[i] = mfma16x16x32(decode8(c[2], c[3], scale), b1, acc[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kM; ++i)
+            if (w > 0) s_red[i][(w - 1) * 64 + lane] = acc[i];
+        __syncthreads();
+        if (w == 0 && live) {
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+                for (int q = 0; q + 1 < kFewWaves; ++q) acc[i] += s_red[i][q * 64 + lane];
+            const int64_t out = (int64_t)(row0 + j0 + j) * a.N + p * kTileRows + g * 4;
+            if constexpr (kMode == kFewGateUp)
+                *reinterpret_cast<float4*>(a.h32 + out) =
+                    make_float4(silu_mul(acc[0][0], acc[1][0]), silu_mul(acc[0][1], acc[1][1]),
+                                silu_mul(acc[0][2], acc[1][2]), silu_mul(acc[0][3], acc[1][3]));
+            else if (kMode == kFewDown || a.y32)
+                *reinterpret_cast<float4*>(a.y32 + out) = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
+            else
+                *reinterpret_cast<uint2*>(a.y16 + out) =
+                    make_uint2(cvt_pk_bf16(acc[0][0], acc[0][1]), cvt_pk_bf16(acc[0][2], acc[0][3]));
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace moe
+
+extern "C" {
+
+hipError_t moe_launch_quantize(const void* x, int64_t ld, int bf16, int64_t T, const int32_t* n_rows, int n,
+                               int n_pad, uint8_t* codes, uint8_t* scales, uint16_t* values, hipStream_t s)
+{
+    const int64_t units = T * ((n + moe::kBlock - 1) / moe::kBlock);
+    const int grid = (int)((units + 15) / 16 < 65536 ? (units + 15) / 16 : 65536);
+    if (bf16)
+        hipLaunchKernelGGL(moe::quantize_kernel<true>, dim3(grid), dim3(256), 0, s, x, ld, T, n_rows, n, n_pad, codes,
+                           scales, values);
+    else
+        hipLaunchKernelGGL(moe::quantize_kernel<false>, dim3(grid), dim3(256), 0, s, x, ld, T, n_rows, n, n_pad, codes,
+                           scales, values);
+    return hipGetLastError();
+}
+
+hipError_t moe_launch_pack_e4m3(const uint16_t* src, int K, int N, int K_pad, int N_pad, uint8_t* dst,
+                                uint8_t* scales, int rt_mul, int rt_add, hipStream_t s)
+{
+    hipLaunchKernelGGL(moe::pack_e4m3_kernel, dim3(N_pad / moe::kBlock, K_pad / moe::kBlock), dim3(256), 0, s, src, K,
+                       N, dst, scales, K_pad / moe::kTileK8, moe::scale_quads(K_pad) * 4, rt_mul, rt_add);
+    return hipGetLastError();
+}
+
+hipError_t moe_launch_e4m3_gateup_few(const moe::E4m3Args* a, int n_slots, hipStream_t s)
+{
+    hipLaunchKernelGGL(moe::few_kernel<moe::kFewGateUp>, dim3(n_slots * (a->N / moe::kTileRows)),
+                       dim3(64 * moe::kFewWaves), 0, s, *a);
+    return hipGetLastError();
+}
+
+hipError_t moe_launch_e4m3_down_few(const moe::E4m3Args* a, int n_slots, hipStream_t s)
+{
+    hipLaunchKernelGGL(moe::few_kernel<moe::kFewDown>, dim3(n_slots * (a->N / moe::kTileRows)),
+                       dim3(64 * moe::kFewWaves), 0, s, *a);
+    return hipGetLastError();
+}
+
+hipError_t moe_launch_e4m3_linear_few(const moe::E4m3Args* a, hipStream_t s)
+{
+    hipLaunchKernelGGL(moe::few_kernel<moe::kFewLinear>, dim3(a->N / moe::kTileRows), dim3(64 * moe::kFewWaves), 0, s,
+                       *a);
+    return hipGetLastError();
+}
+
+// The same coding and layout on the host, for weights in host memory (K and N
+// multiples of 128).
+void moe_pack_e4m3_host(const uint16_t* src, int K, int N, uint8_t* dst, uint8_t* scales, int rt_mul, int rt_add)
+{
+    const int KT = K / moe::kTileK8, scale_ld = moe::scale_quads(K) * 4;
+    auto value = [](uint16_t b) {
+        const uint32_t u = (uint32_t)b << 16;
+        float f;
+        std::memcpy(&f, &u, 4);
+        return f;
+    };
+    for (int n0 = 0; n0 < N; n0 += moe::kBlock)
+        for (int kb = 0; kb < K / moe::kBlock; ++kb) {
+            const uint16_t* block = src + (size_t)kb * moe::kBlock * N + n0;
+            float amax = 0.f;
+            for (int k = 0; k < moe::kBlock; ++k)
+                for (int n = 0; n < moe::kBlock; ++n) {
+                    const float v = std::fabs(value(block[(size_t)k * N + n]));
+                    if (std::isfinite(v) && v > amax) amax = v;
+                }
+            // the least e with amax <= 448 * 2^e = 1.75 * 2^(e + 8)
+            int e = moe::kExpMin;
+            while (e < moe::kExpMax && amax > std::ldexp(448.0, e)) ++e;
+            scales[(size_t)(n0 / moe::kBlock) * scale_ld + kb] = (uint8_t)(e + 127);
+            for (int n = 0; n < moe::kBlock; ++n)
+                for (int k = 0; k < moe::kBlock; ++k) {
+                    const float x = value(block[(size_t)k * N + n]);
+                    const double v = std::fmin(std::ldexp(std::fabs((double)x), -e), 448.0);
+                    uint8_t c;
+                    if (!std::isfinite(x)) {
+                        c = 0x7F;
+                    } else if (v < 0x1p-6) {
+                        c = (uint8_t)std::nearbyint(std::ldexp(v, 9));       // 8: the least normal code
+                    } else {
+                        int x2;
+                        const double f = std::frexp(v, &x2);                  // f in [1/2, 1)
+                        c = (uint8_t)((x2 + 6) * 8 + (int)std::nearbyint(f * 16) - 8);   // 16 carries
+                    }
+                    if (std::signbit(x)) c |= 0x80;
+                    const size_t rt = (size_t)((n0 + n) / moe::kTileRows) * rt_mul + rt_add;
+                    const int q = k % moe::kTileK8;        // in the K tile: granule, half and byte of it
+                    dst[moe::tile_offset(rt, kb * 2 + k / moe::kTileK8, KT) + q % 32 / 8 * 256 +
+                        n % moe::kTileRows * 16 + q / 32 * 8 + q % 8] = c;
+                }
+        }
+}
+
+}  // extern "C"

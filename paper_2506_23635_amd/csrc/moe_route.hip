@@ -20,6 +20,8 @@
 //       anyway (d <= 512).
 //   select_kernel: selection and weights from caller-supplied fp32 logits.
 //   permute_kernel: the permutation and the list of token tiles (one workgroup).
+// The kernels that select have a second form for a layer with a routing policy
+// (choose below), select_kernel's is policy_select_kernel.
 //
 // Selection: the k largest logits, ties to the lower expert id, slots ordered
 // by (logit desc, id asc); weights = softmax over the selected logits (fp32).
@@ -28,6 +30,7 @@
 // a row, so the order is deterministic.
 #include <algorithm>
 
+#include "../../include/moe.h"
 #include "moe_common.h"
 
 namespace moe {
@@ -83,6 +86,109 @@ __device__ __forceinline__ void select_token_any(const float* l, int t, int E, i
     else select_token<64>(l, E, k, ids, w);
 }
 
+// The value of v in lane q of this lane's W consecutive ones (W 64: q is the same
+// for the wave).
+template <int W>
+__device__ __forceinline__ double from_lane(double v, int q)
+{
+    if constexpr (W == kWave) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, q);
+        const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), q);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    } else {
+        return __shfl(v, q, W);
+    }
+}
+
+template <int W>
+__device__ __forceinline__ float from_lane(float v, int q)
+{
+    if constexpr (W == kWave)
+        return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), q));
+    else
+        return __shfl(v, q, W);
+}
+
+template <int W>
+__device__ __forceinline__ double sum_lanes(double v)
+{
+#pragma unroll
+    for (int o = W / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, W);
+    return v;
+}
+
+template <int W>
+__device__ __forceinline__ double max_lanes(double v)
+{
+#pragma unroll
+    for (int o = W / 2; o >= 1; o >>= 1) v = fmax(v, __shfl_xor(v, o, W));
+    return v;
+}
+
+// Selection and weights of one token under a policy, by W lanes (16 or 64, at
+// least E), lane e holding expert e's logit.  Each lane forms its expert's score
+// and choice value and counts the experts that go before it; the k first write
+// their slots.  All of it in fp64: next to a border the choice would otherwise
+// hang on the last bit of an exp, and scores of far logits would tie.  A whole
+// wave compares its experts through scalar registers.
+template <int W>
+__device__ __forceinline__ void choose(const Policy& p, float logit, int e, int E, int k, int* ids, float* w)
+{
+    const bool live = e < E;
+    const double l = live ? (double)logit : -INFINITY;
+    // exp(l - m) of the lanes that take part; nothing but -inf gives zeros, a NaN stays one
+    auto exp_from = [&](double m, bool in) { return !in || (m == -INFINITY && l == l) ? 0.0 : exp(l - m); };
+    double s = l;
+    if (p.score == MOE_SCORE_SOFTMAX) {
+        const double x = exp_from(max_lanes<W>(l), live);
+        const double z = sum_lanes<W>(x);
+        s = z == 0.0 ? 0.0 : x / z;
+    } else if (p.score == MOE_SCORE_SIGMOID) {
+        s = 1.0 / (1.0 + exp(-l));
+    }
+    double c = s + (live && p.balance ? (double)p.balance[e] : 0.0);
+    if (c != c) c = -INFINITY;
+    const float order = logit == logit ? logit : -INFINITY;   // among equal c
+    bool open = live;
+    if (p.top_groups < p.n_groups) {
+        const int n = E / p.n_groups, g = min(e, E - 1) / n;
+        double b1 = -INFINITY, b2 = -INFINITY;                // the two largest c of the group
+        for (int i = 0; i < n; ++i) {
+            const double v = __shfl(c, g * n + i, W);
+            b2 = v > b1 ? b1 : fmax(b2, v);
+            b1 = fmax(b1, v);
+        }
+        double value = p.group_best == 2 ? b1 + b2 : b1;
+        if (value != value) value = -INFINITY;
+        int before = 0;
+        for (int q = 0; q < p.n_groups; ++q) {
+            const double v = from_lane<W>(value, q * n);
+            before += v > value || (v == value && q < g) ? 1 : 0;
+        }
+        open = live && before < p.top_groups;
+    }
+    const uint64_t opened = __ballot(open) >> (threadIdx.x % kWave / W * W);
+    int rank = 0;
+    for (int q = 0; q < E; ++q) {
+        const double cq = from_lane<W>(c, q);
+        const float lq = from_lane<W>(order, q);
+        const bool first = cq > c || (cq == c && (lq > order || (lq == order && q < e)));
+        rank += first && (opened >> q & 1) ? 1 : 0;
+    }
+    const bool in = open && rank < k;
+    double v = in ? s : 0.0;
+    if (p.score == MOE_SCORE_SELECTED) v = exp_from(max_lanes<W>(in ? l : -INFINITY), in);
+    if (p.renormalize || p.score == MOE_SCORE_SELECTED) {
+        const double z = sum_lanes<W>(v);
+        v = z == 0.0 ? 0.0 : v / z;
+    }
+    if (in) {
+        ids[rank] = e;
+        w[rank] = (float)(v * (double)p.scale);
+    }
+}
+
 // barrier for LDS traffic only: waits for this wave's LDS operations, not for
 // its outstanding global stores (which a __syncthreads() release would)
 __device__ __forceinline__ void lds_barrier()
@@ -127,6 +233,7 @@ struct DecodeRouteArgs {
     const float* bias;
     double* partial;          // [n_wg][kSmallT][kDecE]
     int T, d, E, k, e_begin, n_local, tile_rows, n_wg;
+    Policy policy;
     RouteView rv;
 };
 
@@ -182,12 +289,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_partials_kernel(DecodeRou
     if (tid < a.T * kDecE) a.partial[(int64_t)blockIdx.x * kSmallT * kDecE + tid] = v;
 }
 
+template <bool kPolicy>
 __device__ __forceinline__ void finish_route(const DecodeRouteArgs& a, float (&lg)[kSmallT][kDecE]);
 
 // logits, selection and permutation in LDS, then every routing output
 // written at the end (global stores are not waited for inside the
 // workgroup).  Every step is spread over threads: one (token, expert) pair
 // per thread.
+template <bool kPolicy>
 __global__ __launch_bounds__(kRouteThreads) void route_finish_kernel(DecodeRouteArgs a)
 {
     __shared__ float lg[kSmallT][kDecE];
@@ -215,13 +324,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_finish_kernel(DecodeRoute
             lg[t][ee] = l;
         }
     }
-    finish_route(a, lg);
+    finish_route<kPolicy>(a, lg);
 }
 
 // Both halves in one launch where one workgroup forms the logits anyway
 // (d <= 512): small layer (d 256, f 512, 8 experts, top-2) at 1 token 19.8 ->
 // 16.3 us, at 16 tokens 21.1 -> 18.8.
-template <int kT>
+template <int kT, bool kPolicy>
 __global__ __launch_bounds__(kRouteThreads) void route_one_kernel(DecodeRouteArgs a)
 {
     __shared__ float lg[kSmallT][kDecE];
@@ -232,9 +341,10 @@ __global__ __launch_bounds__(kRouteThreads) void route_one_kernel(DecodeRouteArg
         if (a.bias) l = __fadd_rn(l, a.bias[ee]);
         lg[t][ee] = l;
     }
-    finish_route(a, lg);
+    finish_route<kPolicy>(a, lg);
 }
 
+template <bool kPolicy>
 __device__ __forceinline__ void finish_route(const DecodeRouteArgs& a, float (&lg)[kSmallT][kDecE])
 {
     __shared__ int s_ids[kDecPairs];
@@ -246,41 +356,49 @@ __device__ __forceinline__ void finish_route(const DecodeRouteArgs& a, float (&l
     const int tid = threadIdx.x;
     const int lane = tid & 63, wid = tid >> 6;
     lds_barrier();
-    // rank of expert e in its token's order (logit descending, id ascending):
-    // the experts before e with a logit >= its own and those after it with a
-    // larger one; rank < k selects it at slot rank.  A row holding a NaN
-    // takes the sequential scan instead (its order is scan-dependent).
-    if (tid < T * kDecE) {
-        const int t = tid / kDecE, e = tid % kDecE;
-        if (e < E) {
-            const float le = lg[t][e];
-            int r = 0;
-            bool ordered = true;
-            for (int q = 0; q < E; ++q) {
-                const float lq = lg[t][q];
-                ordered = ordered && lq == lq;
-                r += q < e ? (lq >= le ? 1 : 0) : (lq > le ? 1 : 0);
-            }
-            s_rank[t][e] = ordered ? r : -1;
-            if (ordered && r < k) s_ids[t * k + r] = e;
+    if constexpr (kPolicy) {
+        // 16 lanes per token
+        if (tid < T * kDecE) {
+            const int t = tid / kDecE, e = tid % kDecE;
+            choose<kDecE>(a.policy, lg[t][min(e, E - 1)], e, E, k, &s_ids[t * k], &s_w[t * k]);
         }
-    }
-    lds_barrier();
-    if (tid < T) {
-        const int t = tid;
-        if (s_rank[t][0] < 0) {
-            select_token<kDecE>(&lg[t][0], E, k, &s_ids[t * k], &s_w[t * k]);
-        } else {
-            // weights in slot order, as the sequential selection forms them
-            const float lmax = lg[t][s_ids[t * k]];
-            float z = 0.f;
-            for (int j2 = 0; j2 < k; ++j2) {
-                const float p = expf(lg[t][s_ids[t * k + j2]] - lmax);
-                s_w[t * k + j2] = p;
-                z += p;
+    } else {
+        // rank of expert e in its token's order (logit descending, id ascending):
+        // the experts before e with a logit >= its own and those after it with a
+        // larger one; rank < k selects it at slot rank.  A row holding a NaN
+        // takes the sequential scan instead (its order is scan-dependent).
+        if (tid < T * kDecE) {
+            const int t = tid / kDecE, e = tid % kDecE;
+            if (e < E) {
+                const float le = lg[t][e];
+                int r = 0;
+                bool ordered = true;
+                for (int q = 0; q < E; ++q) {
+                    const float lq = lg[t][q];
+                    ordered = ordered && lq == lq;
+                    r += q < e ? (lq >= le ? 1 : 0) : (lq > le ? 1 : 0);
+                }
+                s_rank[t][e] = ordered ? r : -1;
+                if (ordered && r < k) s_ids[t * k + r] = e;
             }
-            const float inv = 1.0f / z;
-            for (int j2 = 0; j2 < k; ++j2) s_w[t * k + j2] = s_w[t * k + j2] * inv;
+        }
+        lds_barrier();
+        if (tid < T) {
+            const int t = tid;
+            if (s_rank[t][0] < 0) {
+                select_token<kDecE>(&lg[t][0], E, k, &s_ids[t * k], &s_w[t * k]);
+            } else {
+                // weights in slot order, as the sequential selection forms them
+                const float lmax = lg[t][s_ids[t * k]];
+                float z = 0.f;
+                for (int j2 = 0; j2 < k; ++j2) {
+                    const float p = expf(lg[t][s_ids[t * k + j2]] - lmax);
+                    s_w[t * k + j2] = p;
+                    z += p;
+                }
+                const float inv = 1.0f / z;
+                for (int j2 = 0; j2 < k; ++j2) s_w[t * k + j2] = s_w[t * k + j2] * inv;
+            }
         }
     }
     lds_barrier();
@@ -362,11 +480,12 @@ constexpr int kRsExp = 8;
 constexpr int kRsTok = 2 * kRsTokWave;
 constexpr int kRsThreads = 4 * kWave;
 
+template <bool kPolicy>
 __global__ __launch_bounds__(kRsThreads) void router_select_kernel(const uint16_t* __restrict__ x,
                                                                    const float* __restrict__ wrT,
                                                                    const float* __restrict__ bias,
                                                                    int T, int d, int E, int k,
-                                                                   RouteView rv)
+                                                                   Policy policy, RouteView rv)
 {
     __shared__ float lg[kRsTok][64];
     const int wid = threadIdx.x / kWave, lane = threadIdx.x % kWave;
@@ -460,7 +579,14 @@ __global__ __launch_bounds__(kRsThreads) void router_select_kernel(const uint16_
         }
     }
     lds_barrier();
-    if (threadIdx.x < kRsTok) {
+    if constexpr (kPolicy) {
+        for (int i = wid; i < kRsTok; i += kRsThreads / kWave) {
+            const int t = blockIdx.x * kRsTok + i;
+            if (t < T)
+                choose<kWave>(policy, lg[i][min(lane, E - 1)], lane, E, k, rv.topk_idx + (int64_t)t * k,
+                              rv.topk_w + (int64_t)t * k);
+        }
+    } else if (threadIdx.x < kRsTok) {
         const int t = blockIdx.x * kRsTok + threadIdx.x;
         if (t < T) select_token_any(&lg[threadIdx.x][0], t, E, k, rv);
     }
@@ -476,6 +602,17 @@ __global__ __launch_bounds__(256) void select_kernel(const float* __restrict__ l
     const float* l = logits_in + (int64_t)t * E;
     for (int e = 0; e < E; ++e) rv.logits[(int64_t)t * E + e] = l[e];
     select_token_any(l, t, E, k, rv);
+}
+
+// The same under a policy: one wave per token.
+__global__ __launch_bounds__(256) void policy_select_kernel(const float* __restrict__ logits_in, int T, int E, int k,
+                                                            Policy policy, RouteView rv)
+{
+    const int t = blockIdx.x * (256 / kWave) + threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if (t >= T) return;
+    const float l = logits_in[(int64_t)t * E + min(lane, E - 1)];
+    if (lane < E) rv.logits[(int64_t)t * E + lane] = l;
+    choose<kWave>(policy, l, lane, E, k, rv.topk_idx + (int64_t)t * k, rv.topk_w + (int64_t)t * k);
 }
 
 // Expert-grouped permutation of the T*k pairs (one 1024-thread workgroup),
@@ -656,9 +793,11 @@ extern "C" int moe_route_decode_wgs(int d) { return (d / 8 + 63) / 64; }
 extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wrT,
                                               const float* bias, double* partial, int T, int d,
                                               int E, int k, int e_begin, int n_local, int tile_rows,
-                                              const moe::RouteView* rv, hipStream_t s)
+                                              const moe::Policy* policy, const moe::RouteView* rv,
+                                              hipStream_t s)
 {
     moe::DecodeRouteArgs a{};
+    a.policy = *policy;
     a.x = x; a.wrT = wrT; a.bias = bias; a.partial = partial;
     a.T = T; a.d = d; a.E = E; a.k = k;
     a.e_begin = e_begin; a.n_local = n_local; a.tile_rows = tile_rows;
@@ -669,9 +808,13 @@ extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wr
         return T == 1 ? k1 : T == 2 ? k2 : T <= 4 ? k4 : T <= 8 ? k8 : k16;
     };
     if (a.n_wg == 1) {
-        const Kernel one = by_tokens(moe::route_one_kernel<1>, moe::route_one_kernel<2>,
-                                      moe::route_one_kernel<4>, moe::route_one_kernel<8>,
-                                     moe::route_one_kernel<moe::kSmallT>);
+        const Kernel one =
+            policy->on ? by_tokens(moe::route_one_kernel<1, true>, moe::route_one_kernel<2, true>,
+                                   moe::route_one_kernel<4, true>, moe::route_one_kernel<8, true>,
+                                   moe::route_one_kernel<moe::kSmallT, true>)
+                       : by_tokens(moe::route_one_kernel<1, false>, moe::route_one_kernel<2, false>,
+                                   moe::route_one_kernel<4, false>, moe::route_one_kernel<8, false>,
+                                   moe::route_one_kernel<moe::kSmallT, false>);
         hipLaunchKernelGGL(one, dim3(1), dim3(moe::kRouteThreads), 0, s, a);
         return hipGetLastError();
     }
@@ -681,25 +824,33 @@ extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wr
     hipLaunchKernelGGL(partials, dim3(a.n_wg), dim3(moe::kRouteThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(moe::route_finish_kernel, dim3(1), dim3(moe::kRouteThreads), 0, s, a);
+    const Kernel finish = policy->on ? moe::route_finish_kernel<true> : moe::route_finish_kernel<false>;
+    hipLaunchKernelGGL(finish, dim3(1), dim3(moe::kRouteThreads), 0, s, a);
     return hipGetLastError();
 }
 
 extern "C" hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT,
                                                const float* bias, int T, int d, int E, int k,
+                                               const moe::Policy* policy,
                                                const moe::RouteView* rv, hipStream_t s)
 {
     const int grid = (T + moe::kRsTok - 1) / moe::kRsTok;
-    hipLaunchKernelGGL(moe::router_select_kernel, dim3(grid), dim3(moe::kRsThreads), 0, s, x, wrT,
-                       bias, T, d, E, k, *rv);
+    const auto kernel = policy->on ? moe::router_select_kernel<true> : moe::router_select_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(moe::kRsThreads), 0, s, x, wrT, bias, T, d, E, k, *policy,
+                       *rv);
     return hipGetLastError();
 }
 
 extern "C" hipError_t moe_launch_route(const float* logits_in, int T, int E, int k, int e_begin,
-                                       int n_local, int tile_rows, const moe::RouteView* rv,
-                                       hipStream_t s)
+                                       int n_local, int tile_rows, const moe::Policy* policy,
+                                       const moe::RouteView* rv, hipStream_t s)
 {
-    if (logits_in) {
+    if (logits_in && policy->on) {
+        hipLaunchKernelGGL(moe::policy_select_kernel, dim3((T + 3) / 4), dim3(256), 0, s, logits_in, T, E, k,
+                           *policy, *rv);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    } else if (logits_in) {
         hipLaunchKernelGGL(moe::select_kernel, dim3((T + 255) / 256), dim3(256), 0, s, logits_in, T,
                            E, k, *rv);
         const hipError_t e = hipGetLastError();
