@@ -36,6 +36,21 @@ __device__ inline uint32_t code4(const float* v, float inv)
     return (uint32_t)c;
 }
 
+// |v| as bits: ordered like the values, what is not finite from kInfBits on
+constexpr uint32_t kInfBits = 0x7F800000u;
+__device__ inline uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// code4 of finite values
+__device__ inline uint32_t code4_finite(const float* v, float inv)
+{
+    float w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_fmed3f(v[i] * inv, -448.f, 448.f);
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(w[0], w[1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(w[2], w[3], c, true);
+    return (uint32_t)c;
+}
+
 // eight e4m3 codes as eight bf16 of code * scale (exact: a power of two)
 __device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
 {

@@ -34,7 +34,8 @@ struct Layout {
     // workspace
     size_t dpart_off, logits_off, idx_off, w_off, counts_off, offsets_off, pair_row_off,
         row_token_off, active_off, tiles_off, n_tiles_off, h_off, o_off, ws_bytes;
-    // MOE_E4M3: scales of gate, up and down in an expert; H's fp32 values
+    // MOE_E4M3: scales of gate, up and down in an expert; H's fp32 values of
+    // few tokens
     size_t sg_off, su_off, sd_off, h32_off;
     size_t region_off[MOE_WS_COUNT], region_bytes[MOE_WS_COUNT];   // moe_workspace_map
     int rows_max, max_tiles;
@@ -109,7 +110,7 @@ Layout make_layout(const moe_config* c)
     size_t h_bytes = (size_t)L.rows_max * f * 2;
     if (e4m3) {
         L.h32_off = align_up(h_bytes, kAlign);
-        h_bytes = L.h32_off + (size_t)L.rows_max * f * 4;
+        h_bytes = L.h32_off + std::min<size_t>(Tm, kDecodeMaxTokens) * kl * f * 4;
     }
     L.h_off = take(MOE_WS_H, h_bytes);
     L.h32_off += L.h_off;
@@ -274,18 +275,17 @@ void fill_routing(moe_ctx* ctx, int layer, int T, moe_routing* out)
     out->layer = layer;
 }
 
-// The experts of a MOE_E4M3 layer: x rounded to the e4m3 grid (into O's space:
-// the down products come after its last reader), gate and up, H rounded, down.
-moe_status run_experts_e4m3(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T, hipStream_t s)
+// The experts of a MOE_E4M3 layer for few tokens: gate and up, H rounded, down;
+// xq: the rows of x rounded to the e4m3 grid.
+moe_status run_experts_e4m3_few(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* xq, int T, hipStream_t s)
 {
     const moe_config& c = ctx->cfg;
     const Layout& L = ctx->L;
     const int d = c.d_model, f = c.ffn_dim;
     const uint8_t* experts = layer_base(ctx, layer) + L.experts_off;
-    uint16_t* xq = reinterpret_cast<uint16_t*>(ws.base + ws.o_off);
     uint16_t* H = reinterpret_cast<uint16_t*>(ws.base + ws.h_off);
     float* h32 = reinterpret_cast<float*>(ws.base + ws.h32_off);
-    const int max_rows = T * std::min(c.top_k, c.n_local_experts);
+    const int max_rows = T * std::min(c.top_k, c.n_local_experts), slots = std::min(c.n_local_experts, T * c.top_k);
     moe::E4m3Args gu{};
     gu.w = experts;
     gu.ws = experts + L.sg_off;
@@ -299,8 +299,9 @@ moe_status run_experts_e4m3(moe_ctx* ctx, const WsView& ws, int layer, const uin
     gu.offsets = ws.rv.offsets;
     gu.row_token = ws.rv.row_token;
     gu.e_begin = c.expert_begin;
-    gu.T = T;
     gu.h32 = h32;
+    hipError_t e = timed(ctx, MOE_K_DECODE_GATEUP, s, [&] { return moe_launch_e4m3_gateup_few(&gu, slots, s); });
+    if (e != hipSuccess) return hip_fail(ctx, e, "e4m3 gate/up kernel launch");
     moe::E4m3Args dn = gu;
     dn.w = experts + L.gu_bytes;
     dn.ws = experts + L.sd_off;
@@ -308,12 +309,6 @@ moe_status run_experts_e4m3(moe_ctx* ctx, const WsView& ws, int layer, const uin
     dn.K = f;
     dn.N = d;
     dn.y32 = reinterpret_cast<float*>(ws.base + ws.o_off);
-    const int slots = (int)std::min<int64_t>(c.n_local_experts, (int64_t)T * c.top_k);
-    hipError_t e = timed(ctx, MOE_K_DECODE_GATEUP, s, [&] {
-        const hipError_t r = moe_launch_quantize(x, d, 1, T, nullptr, d, d, nullptr, nullptr, xq, s);
-        return r != hipSuccess ? r : moe_launch_e4m3_gateup_few(&gu, slots, s);
-    });
-    if (e != hipSuccess) return hip_fail(ctx, e, "e4m3 gate/up kernel launch");
     e = timed(ctx, MOE_K_DECODE_DOWN, s, [&] {
         const hipError_t r =
             moe_launch_quantize(h32, f, 0, max_rows, ws.rv.offsets + c.n_experts, f, f, nullptr, nullptr, H, s);
@@ -326,12 +321,23 @@ moe_status run_experts_e4m3(moe_ctx* ctx, const WsView& ws, int layer, const uin
 moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T,
                        hipStream_t s)
 {
-    if (ctx->cfg.flags & MOE_E4M3) return run_experts_e4m3(ctx, ws, layer, x, T, s);
     const moe_config& c = ctx->cfg;
     const uint8_t* experts = layer_base(ctx, layer) + ctx->L.experts_off;
     uint16_t* H = reinterpret_cast<uint16_t*>(ws.base + ws.h_off);
     float* O = reinterpret_cast<float*>(ws.base + ws.o_off);
     hipError_t e;
+    const bool e4m3 = (c.flags & MOE_E4M3) != 0;
+    if (e4m3) {
+        // x rounded to the e4m3 grid, into O's space (rows_max >= T): the down
+        // products come after its last reader
+        uint16_t* xq = reinterpret_cast<uint16_t*>(O);
+        e = timed(ctx, T <= kDecodeMaxTokens ? MOE_K_DECODE_GATEUP : MOE_K_GEMM_GATEUP, s, [&] {
+            return moe_launch_quantize(x, c.d_model, 1, T, nullptr, c.d_model, c.d_model, nullptr, nullptr, xq, s);
+        });
+        if (e != hipSuccess) return hip_fail(ctx, e, "quantize kernel launch");
+        x = xq;
+        if (T <= kDecodeMaxTokens) return run_experts_e4m3_few(ctx, ws, layer, x, T, s);
+    }
     if (T <= kDecodeMaxTokens) {
         moe::DecodeArgs a;
         a.experts = experts;
@@ -373,9 +379,11 @@ moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t
         // a timeline is that of the 256 x 256 tiles
         const bool timeline = ctx->tl_gateup || ctx->tl_down;
         a.mid = !timeline && moe_gemm_mid_tiles(T, c.top_k, c.n_experts, c.n_local_experts, 2 * c.ffn_dim);
+        a.scales = e4m3 ? experts + ctx->L.sg_off : nullptr;
         a.stamps = ctx->tl_gateup;
         e = timed(ctx, MOE_K_GEMM_GATEUP, s, [&] { return moe_launch_gemm_gateup(&a, s); });
         if (e != hipSuccess) return hip_fail(ctx, e, "grouped GEMM gate/up kernel launch");
+        a.scales = e4m3 ? experts + ctx->L.sd_off : nullptr;
         a.stamps = ctx->tl_down;
         a.mid = !timeline && moe_gemm_mid_tiles(T, c.top_k, c.n_experts, c.n_local_experts, c.d_model);
         e = timed(ctx, MOE_K_GEMM_DOWN, s, [&] { return moe_launch_gemm_down(&a, s); });

@@ -148,7 +148,9 @@ struct GemmArgs {
     uint16_t *q, *kc, *vc;    // q|k|v: rotated q [T][heads][hd]; the layer's caches
     int heads, kv_heads, hd, max_seq, pos0;
     const uint16_t* res;      // output: x [T, d], and y = bf16(x + o)
-    uint16_t* y16;
+    uint16_t* y16;            // (kLinear: y, or NULL: O)
+    const uint8_t* scales;    // weights in e4m3: first local expert's scales (gate's, then up's), or NULL
+    int n_out;                // kLinear: features of y (d: with the padding)
     uint64_t* stamps;         // per-workgroup timeline [max_stamps][8], or NULL (measurement)
     int max_stamps;
 };
@@ -207,6 +209,7 @@ hipError_t moe_launch_decode_gateup(const moe::DecodeArgs* a, int n_slots, hipSt
 hipError_t moe_launch_decode_down(const moe::DecodeArgs* a, int n_slots, hipStream_t s);
 hipError_t moe_launch_gemm_gateup(const moe::GemmArgs* a, hipStream_t s);
 hipError_t moe_launch_gemm_down(const moe::GemmArgs* a, hipStream_t s);
+hipError_t moe_launch_gemm_linear(const moe::GemmArgs* a, hipStream_t s);
 hipError_t moe_launch_gemm_qkv(const moe::GemmArgs* a, hipStream_t s);
 hipError_t moe_launch_gemm_out(const moe::GemmArgs* a, hipStream_t s);
 int moe_prefill_tile_rows();

@@ -162,48 +162,44 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
     const uint8_t* pw = a.w + at + (uint64_t)p * kM * KT * kTileBytes + lane * 16;
     const uint8_t* ps[2] = {a.ws + at + (int64_t)(p * kTileRows / kBlock) * scale_ld,
                             kM == 2 ? a.ws_up + at + (int64_t)(p * kTileRows / kBlock) * scale_ld : nullptr};
-    for (int j0 = 0; j0 < m; j0 += 16) {
-        const bool live = j0 + j < m;
-        const int64_t row = live ? (kMode == kFewGateUp ? a.row_token[row0 + j0 + j] : row0 + j0 + j) : 0;
-        const uint16_t* px = a.x + row * a.K + g * 8;
-        f32x4_t acc[kM];
+    const bool live = j < m;
+    const int64_t row = live ? (kMode == kFewGateUp ? a.row_token[row0 + j] : row0 + j) : 0;
+    const uint16_t* px = a.x + row * a.K + g * 8;
+    f32x4_t acc[kM];
 #pragma unroll
-        for (int i = 0; i < kM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        for (int kt = w; kt < KT; kt += kFewWaves) {
-            u32x4_t b0 = {0u, 0u, 0u, 0u}, b1 = b0;
-            if (live) {
-                b0 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8);
-                b1 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8 + 32);
-            }
-#pragma unroll
-            for (int i = 0; i < kM; ++i) {
-                const u32x4_t c = *reinterpret_cast<const u32x4_t*>(pw + ((int64_t)i * KT + kt) * kTileBytes);
-                const float scale = exp2i((int)ps[i][kt / 2] - 127);
-                acc[i] = mfma16x16x32(decode8(c[0], c[1], scale), b0, acc[i]);
-                acc[i] = mfma16x16x32(decode8(c[2], c[3], scale), b1, acc[i]);
-            }
+    for (int i = 0; i < kM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int kt = w; kt < KT; kt += kFewWaves) {
+        u32x4_t b0 = {0u, 0u, 0u, 0u}, b1 = b0;
+        if (live) {
+            b0 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8);
+            b1 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8 + 32);
         }
 #pragma unroll
-        for (int i = 0; i < kM; ++i)
-            if (w > 0) s_red[i][(w - 1) * 64 + lane] = acc[i];
-        __syncthreads();
-        if (w == 0 && live) {
-#pragma unroll
-            for (int i = 0; i < kM; ++i)
-                for (int q = 0; q + 1 < kFewWaves; ++q) acc[i] += s_red[i][q * 64 + lane];
-            const int64_t out = (int64_t)(row0 + j0 + j) * a.N + p * kTileRows + g * 4;
-            if constexpr (kMode == kFewGateUp)
-                *reinterpret_cast<float4*>(a.h32 + out) =
-                    make_float4(silu_mul(acc[0][0], acc[1][0]), silu_mul(acc[0][1], acc[1][1]),
-                                silu_mul(acc[0][2], acc[1][2]), silu_mul(acc[0][3], acc[1][3]));
-            else if (kMode == kFewDown || a.y32)
-                *reinterpret_cast<float4*>(a.y32 + out) = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
-            else
-                *reinterpret_cast<uint2*>(a.y16 + out) =
-                    make_uint2(cvt_pk_bf16(acc[0][0], acc[0][1]), cvt_pk_bf16(acc[0][2], acc[0][3]));
+        for (int i = 0; i < kM; ++i) {
+            const u32x4_t c = *reinterpret_cast<const u32x4_t*>(pw + ((int64_t)i * KT + kt) * kTileBytes);
+            const float scale = exp2i((int)ps[i][kt / 2] - 127);
+            acc[i] = mfma16x16x32(decode8(c[0], c[1], scale), b0, acc[i]);
+            acc[i] = mfma16x16x32(decode8(c[2], c[3], scale), b1, acc[i]);
         }
-        __syncthreads();
     }
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+        if (w > 0) s_red[i][(w - 1) * 64 + lane] = acc[i];
+    __syncthreads();
+    if (w > 0 || !live) return;
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+        for (int q = 0; q + 1 < kFewWaves; ++q) acc[i] += s_red[i][q * 64 + lane];
+    const int64_t out = (int64_t)(row0 + j) * a.N + p * kTileRows + g * 4;
+    if constexpr (kMode == kFewGateUp)
+        *reinterpret_cast<float4*>(a.h32 + out) =
+            make_float4(silu_mul(acc[0][0], acc[1][0]), silu_mul(acc[0][1], acc[1][1]),
+                        silu_mul(acc[0][2], acc[1][2]), silu_mul(acc[0][3], acc[1][3]));
+    else if (kMode == kFewDown || a.y32)
+        *reinterpret_cast<float4*>(a.y32 + out) = make_float4(acc[0][0], acc[0][1], acc[0][2], acc[0][3]);
+    else
+        *reinterpret_cast<uint2*>(a.y16 + out) =
+            make_uint2(cvt_pk_bf16(acc[0][0], acc[0][1]), cvt_pk_bf16(acc[0][2], acc[0][3]));
 }
 
 }  // namespace moe

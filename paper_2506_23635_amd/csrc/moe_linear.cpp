@@ -11,6 +11,7 @@
 
 namespace {
 
+constexpr int kFewTokens = 16;          // rows of one MFMA B operand
 constexpr int kFeatures = 256;          // packed features come in multiples of a tile's
 constexpr size_t kAlign = 256;
 
@@ -156,16 +157,36 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
     uint16_t* xq = reinterpret_cast<uint16_t*>(ctx->workspace);
     hipError_t e = moe_launch_quantize(x, ldx, 1, T, nullptr, c.in_dim, ctx->L.K, nullptr, nullptr, xq, s);
     if (e != hipSuccess) return hip_fail(ctx, e, "quantize kernel launch");
-    moe::E4m3Args a{};
-    a.w = ctx->weights;
-    a.ws = ctx->weights + ctx->L.scales_off;
-    a.x = xq;
-    a.K = ctx->L.K;
-    a.N = c.out_dim;
-    a.T = T;
-    if (type == MOE_T_F32) a.y32 = static_cast<float*>(y);
-    else a.y16 = static_cast<uint16_t*>(y);
-    e = moe_launch_e4m3_linear_few(&a, s);
+    float* y32 = type == MOE_T_F32 ? static_cast<float*>(y) : nullptr;
+    uint16_t* y16 = type == MOE_T_F32 ? nullptr : static_cast<uint16_t*>(y);
+    if (T <= kFewTokens) {
+        moe::E4m3Args a{};
+        a.w = ctx->weights;
+        a.ws = ctx->weights + ctx->L.scales_off;
+        a.x = xq;
+        a.K = ctx->L.K;
+        a.N = c.out_dim;
+        a.T = T;
+        a.y32 = y32;
+        a.y16 = y16;
+        e = moe_launch_e4m3_linear_few(&a, s);
+    } else {
+        moe::GemmArgs a{};
+        a.experts = ctx->weights;
+        a.expert_bytes = ctx->L.scales_off;
+        a.scales = ctx->weights + ctx->L.scales_off;
+        a.H = xq;
+        a.O = y32;
+        a.y16 = y16;
+        a.f = ctx->L.K;
+        a.d = ctx->L.N;
+        a.n_out = c.out_dim;
+        a.n_local = 1;
+        a.T = a.max_rows = T;
+        a.mid = moe_gemm_mid_tiles(T, 1, 1, 1, ctx->L.N);
+        a.k_split = 1;
+        e = moe_launch_gemm_linear(&a, s);
+    }
     if (e != hipSuccess) return hip_fail(ctx, e, "product kernel launch");
     return MOE_OK;
 }

@@ -31,12 +31,20 @@
 //   H = bf16(silu(G) * U) (paper Table tab:vars (e): w1 gate, v1 up).
 // gemm<kDown>:   A = DN slab, X = the expert's rows of H; epilogue O fp32.
 //
+// gemm<kLinear>: the plain product of include/moe.h's moe_linear.
+//
+// With weights in e4m3 (kE4m3) the wave loads half of the bytes per stage, decodes
+// a K step's fragments (four v_cvt_scalef32_pk_bf16_fp8 each, the block's scale in
+// them, exact) a step before their MFMAs and goes on as with bf16; the rows are
+// bf16 values on the e4m3 grid, and gate/up rounds H to it (store_tile).
+//
 // Token tiles come from the routing's row offsets; the grid is sized for the
 // worst case and surplus workgroups, all at its end, exit at once.  Few rows
 // per expert take smaller tiles (gemm_mid_kernel below).
 #include <algorithm>
 #include <type_traits>
 
+#include "e4m3.h"
 #include "moe_common.h"
 
 namespace moe {
@@ -72,7 +80,7 @@ __device__ inline f32x16_t mfma32x32x16(const u32x4_t a, const u32x4_t b, f32x16
 
 // What a tile's sums become: kGateUp H, kDown O; the plain products of the
 // attention block are kDown with their own ends (kQkv, kOut).
-enum { kGateUp = 0, kDown = 1, kQkv = 2, kOut = 3 };
+enum { kGateUp = 0, kDown = 1, kQkv = 2, kOut = 3, kLinear = 4 };
 
 // chunk swizzle of B row R in LDS (a function of R mod 16 only, so 32-row
 // token blocks share it): rows 0..7 take eight distinct slots, and rows
@@ -86,9 +94,55 @@ struct TileCtx {
     __amdgpu_buffer_rsrc_t b_rsrc;  // buffer over x (gate/up) or over the tile's rows of H
     uint32_t b_off[B_LOADS];   // byte offsets in b_rsrc of this lane's 16-byte chunk, per load
     uint32_t rd_off[KS];       // LDS byte offsets of this lane's B fragment piece, per K step
+    __amdgpu_buffer_rsrc_t s_rsrc;  // kE4m3: the weights' scales, and ...
+    uint32_t s_off;            // ... this lane's byte offset (its row block; gate or up)
     int n_stages;
     int w, lane;
 };
+
+// The weight operand of a 64-K stage in registers: fragments of the four K steps,
+// or (kE4m3) for each 32-feature block two granules of codes -- granule i holds
+// the lane's codes of K steps i and i + 2 -- and the stage's scale as its biased
+// exponent.
+template <bool kE4m3, int kFB>
+struct AStage {
+    u32x4_t v[kFB * (kE4m3 ? 2 : KS)];
+    uint32_t scale;
+};
+constexpr int kLoadsA8 = 2;    // granules of a stage per feature block
+
+template <bool kE4m3, int kFB>
+__device__ __forceinline__ u32x4_t a_fragment(const AStage<kE4m3, kFB>& A, int fb, int j)
+{
+    if constexpr (kE4m3) {
+        const u32x4_t c = A.v[fb * kLoadsA8 + j % 2];
+        return decode8(c[j / 2 * 2], c[j / 2 * 2 + 1], __uint_as_float(A.scale << 23));
+    } else {
+        return A.v[fb * KS + j];
+    }
+}
+
+// The loads of stage s: piece i of feature block fb (a_off: its first byte), and
+// the scale.
+template <bool kE4m3, int kFB, int kPolicy>
+__device__ __forceinline__ void load_a(AStage<kE4m3, kFB>& A, __amdgpu_buffer_rsrc_t rsrc, uint32_t a_off, int fb, int i,
+                                       uint32_t s)
+{
+    if constexpr (kE4m3)
+        A.v[fb * kLoadsA8 + i] = __builtin_bit_cast(
+            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, a_off + i * (kTileBytes / 2), s * kTileBytes, kPolicy));
+    else
+        // K step i: K tile 2 s + i / 2, its second half (512 bytes on) for odd i
+        A.v[fb * KS + i] = __builtin_bit_cast(
+            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, a_off + (i / 2) * kTileBytes + (i % 2) * (kTileBytes / 2),
+                                                           s * (2 * kTileBytes), kPolicy));
+}
+
+template <bool kE4m3, int kFB>
+__device__ __forceinline__ void load_scale(AStage<kE4m3, kFB>& A, __amdgpu_buffer_rsrc_t rsrc, uint32_t s_off, uint32_t s)
+{
+    A.scale = __builtin_amdgcn_raw_buffer_load_b8(rsrc, s_off, s / (kBlock / BK), 0);
+}
 
 // The K loop of one tile on v_mfma_f32_32x32x16_bf16.  A 32 x 16 operand
 // fragment is 1 KiB in lane order (lane l: row l%32, K 8(l/32)..+7).
@@ -127,12 +181,18 @@ constexpr int a_load_unit(int fb, int j) { return j + 1 < KS ? 8 * (j + 1) + 2 *
 // the compiler would drop them as dead loads anyway.  The stage before a tail
 // stage may be one too, so there only the stage's own B loads before the
 // barrier are certain to follow B(s+1).
-constexpr int vm_after_last_b(bool kTail)
+// With e4m3 weights a stage's codes are decoded a K step ahead, so granule i of
+// block fb is free after unit 8 (i + 1) + 5, the scale after unit 21; all refills
+// of stage s lie between the last B loads of stages s-1 and s.
+constexpr int a_load_unit8(int fb, int i) { return 8 * (i + 1) + 6 + fb; }
+constexpr int kScaleUnit = 24;
+constexpr int vm_after_last_b(bool kTail, bool kE4m3)
 {
     int n = 0;
     for (int q = 0; q < B_LOADS; ++q)
         if (b_load_unit(q) < kBarrierUnit) ++n;
     if (kTail) return n;
+    if (kE4m3) return n + FB * kLoadsA8 + 1;
     for (int fb = 0; fb < FB; ++fb)
         for (int j = 0; j < KS; ++j) {
             const int u = a_load_unit(fb, j);
@@ -142,27 +202,28 @@ constexpr int vm_after_last_b(bool kTail)
     return n;
 }
 static_assert(b_load_unit(B_LOADS - 1) >= kBarrierUnit, "every B(s+1) load precedes the count");
-static_assert(vm_after_last_b(false) < 64, "vmcnt holds 6 bits");
+static_assert(vm_after_last_b(false, false) < 64, "vmcnt holds 6 bits");
+static_assert(a_load_unit8(FB - 1, kLoadsA8 - 1) < kScaleUnit && kScaleUnit < kBarrierUnit, "every refill is counted");
 // s_waitcnt immediate (gfx9 layout: vmcnt[3:0] | expcnt[6:4] | lgkmcnt[11:8] |
 // vmcnt[15:14])
 constexpr int wait_vm(int n) { return (n & 0xF) | ((n >> 4) << 14) | (0x7 << 4) | (0xF << 8); }
-constexpr int kWaitBStage = wait_vm(vm_after_last_b(false));
-constexpr int kWaitBTail = wait_vm(vm_after_last_b(true));
+constexpr int kWaitBStage = wait_vm(vm_after_last_b(false, false));
+constexpr int kWaitBStage8 = wait_vm(vm_after_last_b(false, true));
+constexpr int kWaitBTail = wait_vm(vm_after_last_b(true, false));
 
-template <bool kFull>
+template <bool kFull, bool kE4m3>
 __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t* lds,
                                           f32x16_t (&acc)[FB][TB])
 {
     const int n_stages = c.n_stages;
     const int w = c.w;
-    u32x4_t ra[kRingA][A_FRAGS];
+    using Stage = AStage<kE4m3, FB>;
+    constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
+    Stage ra[kRingA];
     u32x4_t bw[kWin];
-    // A fragment (fb, j) of stage s: K step j lives in K tile 2s + j/2,
-    // second half of the tile for odd j (512 bytes on)
-    auto load_a1 = [&](int s, int fb, int j, u32x4_t& dst) {
-        dst = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                                              c.a_rsrc, c.a_off[fb] + (j / 2) * kTileBytes + (j % 2) * (kTileBytes / 2),
-                                              (uint32_t)s * (2 * kTileBytes), 0));
+    u32x4_t da[2][FB];                       // kE4m3: decoded fragments of two K steps in turn
+    auto load_a1 = [&](int s, int fb, int i, Stage& dst) {
+        load_a<kE4m3, FB, 0>(dst, c.a_rsrc, c.a_off[fb], fb, i, (uint32_t)s);
     };
     // B goes global -> LDS directly through buffer loads: a stage of B is
     // 256 rows x 128 bytes (64 K), row-major in LDS with the eight 16-byte
@@ -186,15 +247,15 @@ __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t
     // would wait for every outstanding LDS DMA (vmcnt 0); the empty asm
     // statements keep the compiler from moving memory operations across it
     auto wait_and_barrier = [&](auto tail) {
-        __builtin_amdgcn_s_waitcnt(decltype(tail)::value ? kWaitBTail : kWaitBStage);
+        __builtin_amdgcn_s_waitcnt(decltype(tail)::value ? kWaitBTail : kE4m3 ? kWaitBStage8 : kWaitBStage);
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    // stage s (A in A, B in LDS buffer s % 4).  B loads past the last stage
+    // stage s (A in A, the next stage's in next, B in LDS buffer s % 4).  B loads past the last stage
     // re-read the last stage into buffers no stage reads; A refills are
     // issued in the main loop only (tail is std::true_type after it).
-    auto stage = [&](int s, u32x4_t (&A)[A_FRAGS], auto tail) {
+    auto stage = [&](int s, Stage& A, const Stage& next, auto tail) {
         constexpr bool kTail = decltype(tail)::value;
         const uint8_t* bcur = lds + (s % kRingB) * B_STAGE_BYTES;
         const uint8_t* bnext = lds + ((s + 1) % kRingB) * B_STAGE_BYTES;
@@ -208,7 +269,15 @@ __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t
             for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
                 for (int j = 0; j < KS; ++j)
-                    if (!kTail && a_load_unit(fb, j) == u) load_a1(sa, fb, j, A[fb * KS + j]);
+                    if (!kE4m3 && !kTail && a_load_unit(fb, j) == u) load_a1(sa, fb, j, A);
+            if constexpr (kE4m3 && !kTail) {
+#pragma unroll
+                for (int fb = 0; fb < FB; ++fb)
+#pragma unroll
+                    for (int i = 0; i < kLoadsA8; ++i)
+                        if (a_load_unit8(fb, i) == u) load_a1(sa, fb, i, A);
+                if (u == kScaleUnit) load_scale(A, c.s_rsrc, c.s_off, (uint32_t)sa);
+            }
             if (u + kLook < kUnits)
                 read_unit(bcur, u + kLook);
             else
@@ -218,15 +287,20 @@ __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t
             if (kFull || t / 2 < n_pairs) {
 #pragma unroll
                 for (int fb = 0; fb < FB; ++fb)
-                    acc[fb][t] = mfma32x32x16(A[fb * KS + j], bw[u % kWin], acc[fb][t]);
+                    acc[fb][t] = mfma32x32x16(kE4m3 ? da[j % 2][fb] : A.v[kE4m3 ? 0 : fb * KS + j], bw[u % kWin], acc[fb][t]);
             }
+            // the next K step's fragments, one block at a time, under the MFMAs
+            if constexpr (kE4m3)
+#pragma unroll
+                for (int fb = 0; fb < FB; ++fb)
+                    if (t == 4 + fb) da[(j + 1) % 2][fb] = j + 1 < KS ? a_fragment(A, fb, j + 1) : a_fragment(next, fb, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
             for (int j = 0; j < KS; ++j)
-                if (!kTail && a_load_unit(fb, j) == kUnits) load_a1(sa, fb, j, A[fb * KS + j]);
+                if (!kE4m3 && !kTail && a_load_unit(fb, j) == kUnits) load_a1(sa, fb, j, A);
     };
 
     // prologue: B(0), B(1) and A(0..2); wait for them, then read the first
@@ -236,26 +310,31 @@ __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t
 #pragma unroll
         for (int q = 0; q < B_LOADS; ++q) load_b1(min(i, n_stages - 1), i, q);
 #pragma unroll
-    for (int i = 0; i < kRingA; ++i)
+    for (int i = 0; i < kRingA; ++i) {
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
-            for (int j = 0; j < KS; ++j) load_a1(min(i, n_stages - 1), fb, j, ra[i][fb * KS + j]);
+            for (int j = 0; j < kLoadsA; ++j) load_a1(min(i, n_stages - 1), fb, j, ra[i]);
+        if constexpr (kE4m3) load_scale(ra[i], c.s_rsrc, c.s_off, (uint32_t)min(i, n_stages - 1));
+    }
     __builtin_amdgcn_s_waitcnt(kWaitAll);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int u = 0; u < kLook; ++u) read_unit(lds, u);
+    if constexpr (kE4m3)
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) da[0][fb] = a_fragment(ra[0], fb, 0);
     // three stages per iteration, so that the A ring is indexed statically
     int s = 0;
     for (; s + kRingA <= n_stages; s += kRingA) {
-        stage(s + 0, ra[0], std::false_type{});
-        stage(s + 1, ra[1], std::false_type{});
-        stage(s + 2, ra[2], std::false_type{});
+        stage(s + 0, ra[0], ra[1], std::false_type{});
+        stage(s + 1, ra[1], ra[2], std::false_type{});
+        stage(s + 2, ra[2], ra[0], std::false_type{});
     }
     if (s < n_stages) {
-        stage(s, ra[0], std::true_type{});
-        if (s + 1 < n_stages) stage(s + 1, ra[1], std::true_type{});
+        stage(s, ra[0], ra[1], std::true_type{});
+        if (s + 1 < n_stages) stage(s + 1, ra[1], ra[2], std::true_type{});
     }
     // the last stages re-issued dummy B loads into LDS: drain them before the
     // workgroup can finish and its LDS be handed to another workgroup
@@ -280,18 +359,21 @@ __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t
 constexpr int kRingH = 6;
 constexpr int kHalfTB = TB / 2;
 
-template <int kTB, bool kOnce>
+// With e4m3 weights a stage's refills are four granules and the scale, those of
+// the first granules before the wait.
+template <int kTB, bool kOnce, bool kE4m3>
 __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16_t (&acc)[FB][kHalfTB])
 {
+    using Stage = AStage<kE4m3, FB>;
+    constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
     constexpr int kStage = kTB * 32 * BK * 2;
-    constexpr int kWait = wait_vm(2 * kTB + 3 * A_FRAGS - FB);
-    static_assert(2 * kTB + 3 * A_FRAGS - FB < 64, "vmcnt holds 6 bits");
+    constexpr int kAfter = 2 * kTB + (kE4m3 ? 2 * (FB * kLoadsA8 + 1) + FB : 3 * A_FRAGS - FB);
+    constexpr int kWait = wait_vm(kAfter);
+    static_assert(kAfter < 64, "vmcnt holds 6 bits");
     const int n_stages = c.n_stages, w = c.w;
-    u32x4_t ra[kRingH][A_FRAGS];
-    auto load_a1 = [&](int s, int fb, int j, u32x4_t& dst) {
-        dst = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                                              c.a_rsrc, c.a_off[fb] + (j / 2) * kTileBytes + (j % 2) * (kTileBytes / 2),
-                                              (uint32_t)s * (2 * kTileBytes), kOnce ? kNonTemporal : 0));
+    Stage ra[kRingH];
+    auto load_a1 = [&](int s, int fb, int i, Stage& dst) {
+        load_a<kE4m3, FB, kOnce ? kNonTemporal : 0>(dst, c.a_rsrc, c.a_off[fb], fb, i, (uint32_t)s);
     };
     // load q of wave w: rows 32 q + 8 w .. + 7, whole 128-byte lines
     auto load_b = [&](int s, int buf) {
@@ -308,9 +390,10 @@ __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16
             dst[t] = *reinterpret_cast<const u32x4_t*>(&lds[buf + c.rd_off[j] + t * 32 * (BK * 2)]);
     };
     int cur = 0, prev = (kRingB - 1) * kStage;   // byte offsets of this and the last stage's buffer
-    auto stage = [&](int s, u32x4_t (&A)[A_FRAGS]) {
+    auto stage = [&](int s, Stage& A) {
         const int next = cur + kStage == kRingB * kStage ? 0 : cur + kStage;
         const int sa = min(s + kRingH, n_stages - 1);
+        u32x4_t a[FB];
         load_b(min(s + kRingB - 1, n_stages - 1), prev);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -325,23 +408,29 @@ __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
+            for (int fb = 0; fb < FB; ++fb) a[fb] = a_fragment(A, fb, j);
+#pragma unroll
             for (int t = 0; t < kTB; ++t)
 #pragma unroll
-                for (int fb = 0; fb < FB; ++fb)
-                    acc[fb][t] = mfma32x32x16(A[fb * KS + j], bw[j & 1][t], acc[fb][t]);
+                for (int fb = 0; fb < FB; ++fb) acc[fb][t] = mfma32x32x16(a[fb], bw[j & 1][t], acc[fb][t]);
+            if (!kE4m3 || j >= 2)
 #pragma unroll
-            for (int fb = 0; fb < FB; ++fb) load_a1(sa, fb, j, A[fb * KS + j]);
+                for (int fb = 0; fb < FB; ++fb) load_a1(sa, fb, kE4m3 ? j - 2 : j, A);
+            if constexpr (kE4m3)
+                if (j + 1 == KS) load_scale(A, c.s_rsrc, c.s_off, (uint32_t)sa);
             __builtin_amdgcn_sched_barrier(0);
         }
         prev = cur;
         cur = next;
     };
 #pragma unroll
-    for (int i = 0; i < kRingH; ++i)
+    for (int i = 0; i < kRingH; ++i) {
 #pragma unroll
         for (int fb = 0; fb < FB; ++fb)
 #pragma unroll
-            for (int j = 0; j < KS; ++j) load_a1(min(i, n_stages - 1), fb, j, ra[i][fb * KS + j]);
+            for (int j = 0; j < kLoadsA; ++j) load_a1(min(i, n_stages - 1), fb, j, ra[i]);
+        if constexpr (kE4m3) load_scale(ra[i], c.s_rsrc, c.s_off, (uint32_t)min(i, n_stages - 1));
+    }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i + 1 < kRingB; ++i) load_b(min(i, n_stages - 1), i * kStage);
@@ -373,7 +462,7 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-// The end of a tile: kBlocks 32-feature blocks per wave (four waves, wave w
+// The end of a tile: kBlocks 32-feature blocks per wave (kW waves, wave w
 // from row tile rt0 + 2 kBlocks w on) of up to kTBs 32-token blocks, token
 // rows row_start .. row_end - 1.  In a block the lane holds token lane % 32
 // and features 8g + 4 (lane / 32) + r in register 4g + r (g, r = 0..3).
@@ -383,7 +472,10 @@ __device__ __forceinline__ void lds_barrier()
 // 32 bytes of each of 32 rows, and with one workgroup per CU nothing hides
 // it (q|k|v of 2048 tokens, rotated here: 197 us from the registers).
 //  kGateUp  the block is 16 gate rows (g = 0, 1) and the 16 up rows of the
-//           same features (g = 2, 3): H = bf16(silu(G) U), all rows at once
+//           same features (g = 2, 3): H = bf16(silu(G) U), all rows at once;
+//           kE4m3: the 256 packed features are one block of 128 of H, so the
+//           workgroup has each token's maximum (over its waves through LDS) and
+//           rounds to the e4m3 grid
 //  kDown    O (fp32), at the K range's offset; here and below 32 token rows
 //           at a time, through two buffers in turn
 //  kQkv     a row tile of a query or key head holds 8 rotation pairs, the
@@ -394,20 +486,68 @@ __device__ __forceinline__ void lds_barrier()
 //           more: 45 us at 2048 tokens.)  Value rows keep their order, so
 //           their "pairs" are 8 features apart and stay unrotated.
 //  kOut     o (fp32) and y = bf16(x + o) (x and y may be the same array)
-template <int kMode, int kBlocks, int kTBs>
+//  kLinear  y fp32 or bf16, features below n_out
+template <int kMode, int kBlocks, int kTBs, int kW, bool kE4m3>
 __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x16_t (&acc)[kBlocks][kTBs],
                                            uint8_t* lds, int rt0, int row_start, int row_end, int w,
                                            int lane, int split)
 {
-    constexpr int kFeat = 4 * kBlocks * 32;   // features of the workgroup
+    constexpr int kThreads = 64 * kW;
+    constexpr int kFeat = kW * kBlocks * 32;  // features of the workgroup
     const int half = lane >> 5, c = lane & 31, tid = w * 64 + lane;
     const int rows = row_end - row_start;
     if constexpr (kMode == kGateUp) {
         constexpr int kRow = kFeat + 16;      // bytes of a token's H features in LDS, padded
         constexpr int kPieces = kFeat / 16;   // 16-byte pieces of them
+        constexpr int kMaxAt = kTBs * 32 * kRow;
+        uint32_t* s_max = reinterpret_cast<uint32_t*>(lds + kMaxAt);   // kE4m3: [waves][tokens]
 #pragma unroll
         for (int t = 0; t < kTBs; ++t) {
             if (t * 32 >= rows) break;
+            if constexpr (kE4m3) {
+                static_assert(kFeat == 2 * kBlock, "one block of H");
+                // the maxima are taken of the bits; a wave that meets a value that
+                // is not finite goes over them again without those
+                float h[kBlocks][8];
+                uint32_t m = 0;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        h[b][i] = silu_mul(acc[b][t][i], acc[b][t][i + 8]);
+                        m = max(m, abs_bits(h[b][i]));
+                    }
+                const bool all_finite = !__ballot(m >= kInfBits);
+                if (!all_finite) {
+                    m = 0;
+#pragma unroll
+                    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) m = max(m, finite(h[b][i]) ? abs_bits(h[b][i]) : 0u);
+                }
+                m = max(m, (uint32_t)__shfl_xor((int)m, 32, 64));
+                if (half == 0) s_max[w * (kTBs * 32) + t * 32 + c] = m;
+                lds_barrier();
+                m = 0;
+#pragma unroll
+                for (int i = 0; i < kW; ++i) m = max(m, s_max[i * (kTBs * 32) + t * 32 + c]);
+                const int e = scale_exponent(__uint_as_float(m));
+                const float inv = exp2i(-e), scale = exp2i(e);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    u32x4_t q;
+                    if (all_finite)
+                        q = decode8(code4_finite(h[b], inv), code4_finite(h[b] + 4, inv), scale);
+                    else
+                        q = decode8(code4(h[b], inv), code4(h[b] + 4, inv), scale);
+#pragma unroll
+                    for (int g = 0; g < 2; ++g)
+                        *reinterpret_cast<uint2*>(
+                            &lds[(t * 32 + c) * kRow + ((w * kBlocks + b) * 16 + 8 * g + 4 * half) * 2]) =
+                            make_uint2(q[2 * g], q[2 * g + 1]);
+                }
+                continue;
+            }
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
                 const f32x16_t v = acc[b][t];
@@ -501,6 +641,17 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x16_t (&a
                     *reinterpret_cast<uint2*>(dst + f0 + gap) =
                         make_uint2(cvt_pk_bf16(y1.x, y1.y), cvt_pk_bf16(y1.z, y1.w));
                 } else {
+                    if constexpr (kMode == kLinear) {
+                        const int n = rt0 * kTileRows + p * 4;
+                        if (n >= a.n_out) continue;
+                        const float4 v = *reinterpret_cast<const float4*>(&buf[r * kRow + p * 16]);
+                        const int64_t at = (int64_t)row * a.n_out + n;
+                        if (a.y16)
+                            *reinterpret_cast<uint2*>(a.y16 + at) = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
+                        else
+                            *reinterpret_cast<float4*>(a.O + at) = v;
+                        continue;
+                    }
                     const int64_t at = (int64_t)row * a.d + rt0 * kTileRows + p * 4;
                     const float4 v = *reinterpret_cast<const float4*>(&buf[r * kRow + p * 16]);
                     *reinterpret_cast<float4*>(a.O + (uint64_t)split * a.split_stride + at) = v;
@@ -518,15 +669,31 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x16_t (&a
     }
 }
 
-// One BM x BN tile (feature tile ft, token tile tt) of the grouped GEMM.
+// A lane's first byte of the weights' scales (its row block, of gate or of up), in
+// a buffer over the expert's, for the wave's features from row tile rt0 on: 64
+// packed features at most, so all in one block of gate and up, or of a plain
+// matrix.
 template <int kMode>
+__device__ __forceinline__ uint32_t scale_offset(const GemmArgs& a, int e, int K, int rt0, int lane,
+                                                 __amdgpu_buffer_rsrc_t& rsrc)
+{
+    const int ld = scale_quads(K) * 4, features = kMode == kGateUp ? a.f : a.d;
+    const int bytes = features / kBlock * ld;         // of one matrix
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.scales + (uint64_t)(e - a.e_begin) * a.expert_bytes), 0,
+                                             kMode == kGateUp ? 2 * bytes : bytes, kBufferFlags);
+    if (kMode == kGateUp) return (uint32_t)(rt0 * kTileRows / (2 * kBlock) * ld + ((lane & 16) ? bytes : 0));
+    return (uint32_t)(rt0 * kTileRows / kBlock * ld);
+}
+
+// One BM x BN tile (feature tile ft, token tile tt) of the grouped GEMM.
+template <int kMode, bool kE4m3>
 __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_start, int row_end, bool once, int ft, uint8_t* lds)
 {
     const int ntb = (row_end - row_start + 31) / 32;   // 32-token blocks with rows
     const bool half = ntb <= kHalfTB;                  // half_loop's tile
 
     const int K = kMode == kGateUp ? a.d : a.f;
-    const uint64_t KT = (uint64_t)K / kTileK;
+    const uint64_t KT = (uint64_t)K / (kE4m3 ? kTileK8 : kTileK);
     const uint8_t* wbase = a.experts + (uint64_t)(e - a.e_begin) * a.expert_bytes +
                            (kMode == kGateUp ? 0 : a.gu_bytes);
 
@@ -549,6 +716,7 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
     for (int fb = 0; fb < FB; ++fb)
         c.a_off[fb] = (uint32_t)tile_offset(rt0 + 2 * fb + ((lane & 31) >> 4), 0, KT) +
                       (uint32_t)(((lane >> 5) * 16) + (lane & 15)) * 16;
+    if constexpr (kE4m3) c.s_off = scale_offset<kMode>(a, e, K, (int)rt0, lane, c.s_rsrc);
     // B: a stage holds, for each of the 256 token rows R of the tile, the
     // 128 bytes of K [64 s, 64 s + 64) as eight 16-byte chunks; chunk c sits
     // in slot c ^ swz(R) so that the MFMA reads (8 consecutive rows at one
@@ -591,10 +759,10 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
 #pragma unroll
             for (int tb = 0; tb < kHalfTB; ++tb) acc[fb][tb] = f32x16_t{};
         if (ntb <= 2)
-            once ? half_loop<2, true>(c, lds, acc) : half_loop<2, false>(c, lds, acc);
+            once ? half_loop<2, true, kE4m3>(c, lds, acc) : half_loop<2, false, kE4m3>(c, lds, acc);
         else
-            once ? half_loop<4, true>(c, lds, acc) : half_loop<4, false>(c, lds, acc);
-        store_tile<kMode, FB, kHalfTB>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
+            once ? half_loop<4, true, kE4m3>(c, lds, acc) : half_loop<4, false, kE4m3>(c, lds, acc);
+        store_tile<kMode, FB, kHalfTB, 4, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
         return;
     }
     f32x16_t acc[FB][TB];
@@ -606,11 +774,11 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
     // full tiles take the branch-free loop; an expert's partial last tile
     // skips the MFMAs of token-block pairs past its last row
     if (ntb == TB)
-        tile_loop<true>(c, TB / 2, lds, acc);
+        tile_loop<true, kE4m3>(c, TB / 2, lds, acc);
     else
-        tile_loop<false>(c, (ntb + 1) / 2, lds, acc);
+        tile_loop<false, kE4m3>(c, (ntb + 1) / 2, lds, acc);
 
-    store_tile<kMode, FB, TB>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
+    store_tile<kMode, FB, TB, 4, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
 }
 
 // Measurement only (a.stamps, set by moe_profile_gemm_timeline): workgroup
@@ -727,7 +895,7 @@ __device__ __forceinline__ TilePos find_tile(const GemmArgs& a, int block, int n
     return t;
 }
 
-template <int kMode>
+template <int kMode, bool kE4m3>
 __global__ __launch_bounds__(kThreads) void gemm_kernel(GemmArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint8_t lds[kRingB * B_STAGE_BYTES];
@@ -743,7 +911,7 @@ __global__ __launch_bounds__(kThreads) void gemm_kernel(GemmArgs a)
         r0 = __builtin_amdgcn_s_memrealtime();
         c0 = __builtin_amdgcn_s_memtime();
     }
-    process_tile<kMode>(a, e, row_start, row_end, tp.n_sub == 1, ft, lds);
+    process_tile<kMode, kE4m3>(a, e, row_start, row_end, tp.n_sub == 1, ft, lds);
     if (stamp) write_stamp(a, r0, c0, ft, tt, row_end - row_start, e);
 }
 
@@ -770,7 +938,8 @@ constexpr int kMidRing = 4;        // A stages in registers
 constexpr int kMidRingB = 4;       // B stages in LDS
 
 struct MidCtx {
-    __amdgpu_buffer_rsrc_t a_rsrc, b_rsrc;
+    __amdgpu_buffer_rsrc_t a_rsrc, b_rsrc, s_rsrc;
+    uint32_t s_off;            // kE4m3: this lane's offset of the weights' scales
     uint32_t a_off;            // this lane's A byte offset at the first stage
     uint32_t b_off[kMidTB];    // byte offsets in b_rsrc of this lane's 16-byte chunk, per load
     uint32_t rd_off[KS];       // LDS byte offsets of this lane's B fragment piece, per K step
@@ -790,25 +959,34 @@ struct MidCtx {
 // there are no A refills (the compiler would drop them as dead), so only the
 // B loads are counted.  B loads past the last stage re-read it into a buffer
 // that no later stage reads.
-template <int kTB, bool kOnce>
+//
+// e4m3 weights are half of the bytes, so eight stages of them are in flight; a
+// stage's refills are two granules and the scale, the first granule's before the
+// wait.  With kW = 8 waves (gate/up in e4m3: 256 packed features, so that the
+// workgroup has whole blocks of H) a load of B takes 64 rows: an odd last block
+// loads rows it has already once more.
+template <int kTB, bool kOnce, bool kE4m3, int kW>
 __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kMidTB])
 {
-    constexpr int kStage = kTB * 32 * BK * 2;
-    constexpr int kWaitMid = wait_vm(2 * kTB + 3 * KS - 1), kWaitMidTail = wait_vm(2 * kTB);
+    using Stage = AStage<kE4m3, 1>;
+    constexpr int kRing = kE4m3 ? 2 * kMidRing : kMidRing;
+    constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
+    constexpr int kLoadsB = (kTB * 4 + kW - 1) / kW;
+    constexpr int kStage = kLoadsB * kW * 8 * BK * 2;
+    constexpr int kAfter = 2 * kLoadsB + (kE4m3 ? 2 * (kLoadsA8 + 1) + 1 : 3 * KS - 1);
+    constexpr int kWaitMid = wait_vm(kAfter), kWaitMidTail = wait_vm(2 * kLoadsB);
     const int n_stages = c.n_stages, w = c.w;
-    u32x4_t ra[kMidRing][KS];
-    auto load_a1 = [&](int s, int j, u32x4_t& dst) {
-        dst = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(
-                                              c.a_rsrc, c.a_off + (j / 2) * kTileBytes + (j % 2) * (kTileBytes / 2),
-                                              (c.s0 + (uint32_t)s) * (2 * kTileBytes), kOnce ? kNonTemporal : 0));
+    Stage ra[kRing];
+    auto load_a1 = [&](int s, int i, Stage& dst) {
+        load_a<kE4m3, 1, kOnce ? kNonTemporal : 0>(dst, c.a_rsrc, c.a_off, 0, i, c.s0 + (uint32_t)s);
     };
-    // load q of wave w: rows 32 q + 8 w .. + 7, whole 128-byte lines
+    // load q of wave w: rows 8 (kW q + w) .. + 7, whole 128-byte lines
     auto load_b = [&](int s, int buf) {
 #pragma unroll
-        for (int q = 0; q < kTB; ++q)
+        for (int q = 0; q < kLoadsB; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 c.b_rsrc,
-                (__attribute__((address_space(3))) void*)(&lds[buf + (q * 4 + w) * kTileBytes]),
+                (__attribute__((address_space(3))) void*)(&lds[buf + (q * kW + w) * kTileBytes]),
                 16, c.b_off[q], (c.s0 + (uint32_t)s) * (BK * 2), 0, 0);
     };
     u32x4_t bw[2][kTB];                        // B fragments of two K steps in turn
@@ -818,10 +996,10 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
             dst[t] = *reinterpret_cast<const u32x4_t*>(&lds[buf + c.rd_off[j] + t * 32 * (BK * 2)]);
     };
     int cur = 0, prev = (kMidRingB - 1) * kStage;   // byte offsets of this and the last stage's buffer
-    auto stage = [&](int s, u32x4_t (&A)[KS], auto tail) {
+    auto stage = [&](int s, Stage& A, auto tail) {
         constexpr bool kTail = decltype(tail)::value;
         const int next = cur + kStage == kMidRingB * kStage ? 0 : cur + kStage;
-        const int sa = min(s + kMidRing, n_stages - 1);
+        const int sa = min(s + kRing, n_stages - 1);
         load_b(min(s + kMidRingB - 1, n_stages - 1), prev);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -836,9 +1014,12 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
                 read_b(cur, j + 1, bw[(j + 1) & 1]);
             }
             __builtin_amdgcn_sched_barrier(0);
+            const u32x4_t a = a_fragment(A, 0, j);
 #pragma unroll
-            for (int t = 0; t < kTB; ++t) acc[t] = mfma32x32x16(A[j], bw[j & 1][t], acc[t]);
-            if (!kTail) load_a1(sa, j, A[j]);
+            for (int t = 0; t < kTB; ++t) acc[t] = mfma32x32x16(a, bw[j & 1][t], acc[t]);
+            if (!kTail && (!kE4m3 || j >= 2)) load_a1(sa, kE4m3 ? j - 2 : j, A);
+            if constexpr (kE4m3 && !kTail)
+                if (j + 1 == KS) load_scale(A, c.s_rsrc, c.s_off, c.s0 + (uint32_t)sa);
             __builtin_amdgcn_sched_barrier(0);
         }
         prev = cur;
@@ -846,9 +1027,11 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     };
     // A first: its addresses do not wait for the row gather
 #pragma unroll
-    for (int i = 0; i < kMidRing; ++i)
+    for (int i = 0; i < kRing; ++i) {
 #pragma unroll
-        for (int j = 0; j < KS; ++j) load_a1(min(i, n_stages - 1), j, ra[i][j]);
+        for (int j = 0; j < kLoadsA; ++j) load_a1(min(i, n_stages - 1), j, ra[i]);
+        if constexpr (kE4m3) load_scale(ra[i], c.s_rsrc, c.s_off, c.s0 + (uint32_t)min(i, n_stages - 1));
+    }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i + 1 < kMidRingB; ++i) load_b(min(i, n_stages - 1), i * kStage);
@@ -857,38 +1040,41 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     asm volatile("" ::: "memory");
     read_b(0, 0, bw[0]);
     int s = 0;
-    for (; s + kMidRing <= n_stages; s += kMidRing) {
-        stage(s + 0, ra[0], std::false_type{});
-        stage(s + 1, ra[1], std::false_type{});
-        stage(s + 2, ra[2], std::false_type{});
-        stage(s + 3, ra[3], std::false_type{});
+    for (; s + kRing <= n_stages; s += kRing) {
+#pragma unroll
+        for (int i = 0; i < kRing; ++i) stage(s + i, ra[i], std::false_type{});
     }
-    if (s < n_stages) stage(s, ra[0], std::true_type{});
-    if (s + 1 < n_stages) stage(s + 1, ra[1], std::true_type{});
-    if (s + 2 < n_stages) stage(s + 2, ra[2], std::true_type{});
+#pragma unroll
+    for (int i = 0; i + 1 < kRing; ++i)
+        if (s + i < n_stages) stage(s + i, ra[i], std::true_type{});
     // drain the dummy B loads before the workgroup's LDS can be handed on
     __builtin_amdgcn_s_waitcnt(kWaitAll);
     __builtin_amdgcn_s_barrier();
 }
 
-template <bool kOnce>
+template <bool kOnce, bool kE4m3, int kW>
 __device__ __forceinline__ void mid_loop_any(int tb, const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kMidTB])
 {
     if (tb == 1)
-        mid_loop<1, kOnce>(c, lds, acc);
+        mid_loop<1, kOnce, kE4m3, kW>(c, lds, acc);
     else if (tb == 2)
-        mid_loop<2, kOnce>(c, lds, acc);
+        mid_loop<2, kOnce, kE4m3, kW>(c, lds, acc);
     else if (tb == 3)
-        mid_loop<3, kOnce>(c, lds, acc);
+        mid_loop<3, kOnce, kE4m3, kW>(c, lds, acc);
     else
-        mid_loop<4, kOnce>(c, lds, acc);
+        mid_loop<4, kOnce, kE4m3, kW>(c, lds, acc);
 }
 
-template <int kMode>
-__global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
+// waves of a workgroup on these tiles, each 32 packed features
+template <int kMode, bool kE4m3>
+constexpr int kMidWaves = kMode == kGateUp && kE4m3 ? 8 : 4;
+
+template <int kMode, bool kE4m3>
+__global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_kernel(GemmArgs a)
 {
+    constexpr int kW = kMidWaves<kMode, kE4m3>;
     __shared__ __attribute__((aligned(16))) uint8_t lds[kMidRingB * MBN * BK * 2];
-    const int n_ftiles = (kMode == kGateUp ? 2 * a.f : a.d) / MBM;
+    const int n_ftiles = (kMode == kGateUp ? 2 * a.f : a.d) / (32 * kW);
     const TilePos tp = find_tile(a, blockIdx.x, n_ftiles * a.k_split, MBN);
     if (tp.el < 0) return;
     const int split = tp.ft / n_ftiles, ft = tp.ft % n_ftiles;
@@ -901,7 +1087,7 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
     const int tb = (row_end - row_start + 31) / 32;   // 32-token blocks with rows
 
     const int K = kMode == kGateUp ? a.d : a.f;
-    const uint64_t KT = (uint64_t)K / kTileK;
+    const uint64_t KT = (uint64_t)K / (kE4m3 ? kTileK8 : kTileK);
     const uint8_t* wbase = a.experts + (uint64_t)(e - a.e_begin) * a.expert_bytes +
                            (kMode == kGateUp ? 0 : a.gu_bytes);
     const int lane = threadIdx.x & 63;
@@ -910,12 +1096,13 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
     const int w = c.w, n_all = K / BK;
     c.s0 = (uint32_t)(n_all * split / a.k_split);
     c.n_stages = n_all * (split + 1) / a.k_split - (int)c.s0;
-    const uint64_t rt = (uint64_t)ft * (MBM / 16) + w * 2;   // the wave's two 16-row weight tiles
+    const uint64_t rt = (uint64_t)ft * (2 * kW) + w * 2;   // the wave's two 16-row weight tiles
     const uint64_t slab_bytes = kMode == kGateUp ? a.gu_bytes : a.expert_bytes - a.gu_bytes;
     c.a_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase), 0, (int)slab_bytes,
                                                  kBufferFlags);
     c.a_off = (uint32_t)tile_offset(rt + ((lane & 31) >> 4), 0, KT) +
               (uint32_t)(((lane >> 5) * 16) + (lane & 15)) * 16;
+    if constexpr (kE4m3) c.s_off = scale_offset<kMode>(a, e, K, (int)rt, lane, c.s_rsrc);
     if (kMode == kGateUp)
         c.b_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x), 0,
                                                      a.T * a.d * 2, kBufferFlags);
@@ -923,8 +1110,8 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
         c.b_rsrc = __builtin_amdgcn_make_buffer_rsrc(a.H + (int64_t)row_start * a.f, 0,
                                                      (row_end - row_start) * a.f * 2, kBufferFlags);
 #pragma unroll
-    for (int q = 0; q < kMidTB; ++q) {
-        const int R = q * 32 + w * 8 + (lane >> 3);
+    for (int q = 0; q < kMidTB * 4 / kW; ++q) {
+        const int R = (q * kW + w) * 8 + (lane >> 3);
         const int row = row_start + R;
         const int rr = row < row_end ? row : row_start;   // rows past the end: any valid row
         const uint32_t chunk = (uint32_t)((lane & 7) ^ b_swizzle(R)) * 16;
@@ -942,11 +1129,11 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
 #pragma unroll
     for (int t = 0; t < kMidTB; ++t) acc[0][t] = f32x16_t{};
     if (tp.n_sub == 1)
-        mid_loop_any<true>(tb, c, lds, acc[0]);
+        mid_loop_any<true, kE4m3, kW>(tb, c, lds, acc[0]);
     else
-        mid_loop_any<false>(tb, c, lds, acc[0]);
+        mid_loop_any<false, kE4m3, kW>(tb, c, lds, acc[0]);
 
-    store_tile<kMode, 1, kMidTB>(a, acc, lds, ft * (MBM / 16), row_start, row_end, w, lane, split);
+    store_tile<kMode, 1, kMidTB, kW, kE4m3>(a, acc, lds, ft * (2 * kW), row_start, row_end, w, lane, split);
 }
 
 }  // namespace moe
@@ -998,46 +1185,42 @@ static dim3 gemm_grid(const moe::GemmArgs* a, int n_ft, int tile_rows)
     return dim3((n + moe::kXcds - 1) / moe::kXcds * moe::kXcds);
 }
 
-template <int kMode>
-static hipError_t launch_gemm(const moe::GemmArgs* a, hipStream_t s)
-{
-    const int M = kMode == moe::kGateUp ? 2 * a->f : a->d;
-    hipLaunchKernelGGL((moe::gemm_kernel<kMode>), gemm_grid(a, M / moe::BM, moe::BN), dim3(moe::kThreads),
-                       0, s, *a);
-    return hipGetLastError();
-}
-
-template <int kMode>
-static hipError_t launch_gemm_mid(const moe::GemmArgs* a, hipStream_t s)
-{
-    const int M = kMode == moe::kGateUp ? 2 * a->f : a->d;
-    hipLaunchKernelGGL((moe::gemm_mid_kernel<kMode>), gemm_grid(a, M / moe::MBM * a->k_split, moe::MBN),
-                       dim3(moe::kThreads), 0, s, *a);
-    return hipGetLastError();
-}
-
-template <int kMode>
+template <int kMode, bool kE4m3>
 static hipError_t launch_any(const moe::GemmArgs* a, hipStream_t s)
 {
-    return a->mid ? launch_gemm_mid<kMode>(a, s) : launch_gemm<kMode>(a, s);
+    const int M = kMode == moe::kGateUp ? 2 * a->f : a->d;
+    if (a->mid) {
+        constexpr int kW = moe::kMidWaves<kMode, kE4m3>;
+        hipLaunchKernelGGL((moe::gemm_mid_kernel<kMode, kE4m3>), gemm_grid(a, M / (32 * kW) * a->k_split, moe::MBN),
+                           dim3(64 * kW), 0, s, *a);
+    } else {
+        hipLaunchKernelGGL((moe::gemm_kernel<kMode, kE4m3>), gemm_grid(a, M / moe::BM, moe::BN), dim3(moe::kThreads), 0, s,
+                           *a);
+    }
+    return hipGetLastError();
 }
 
 extern "C" hipError_t moe_launch_gemm_gateup(const moe::GemmArgs* a, hipStream_t s)
 {
-    return launch_any<moe::kGateUp>(a, s);
+    return a->scales ? launch_any<moe::kGateUp, true>(a, s) : launch_any<moe::kGateUp, false>(a, s);
 }
 
 extern "C" hipError_t moe_launch_gemm_down(const moe::GemmArgs* a, hipStream_t s)
 {
-    return launch_any<moe::kDown>(a, s);
+    return a->scales ? launch_any<moe::kDown, true>(a, s) : launch_any<moe::kDown, false>(a, s);
+}
+
+extern "C" hipError_t moe_launch_gemm_linear(const moe::GemmArgs* a, hipStream_t s)
+{
+    return launch_any<moe::kLinear, true>(a, s);
 }
 
 extern "C" hipError_t moe_launch_gemm_qkv(const moe::GemmArgs* a, hipStream_t s)
 {
-    return launch_any<moe::kQkv>(a, s);
+    return launch_any<moe::kQkv, false>(a, s);
 }
 
 extern "C" hipError_t moe_launch_gemm_out(const moe::GemmArgs* a, hipStream_t s)
 {
-    return launch_any<moe::kOut>(a, s);
+    return launch_any<moe::kOut, false>(a, s);
 }
