@@ -139,6 +139,8 @@ __global__ __launch_bounds__(256) void pack_e4m3_kernel(const uint16_t* __restri
 // tile is the A operand, the rows are the B operand.
 
 constexpr int kFewWaves = 8;
+constexpr int kFewUnrollGU = 6;    // K tiles per wave in flight, of gate and of up
+constexpr int kFewUnroll = 7;
 
 enum { kFewGateUp = 0, kFewDown = 1, kFewLinear = 2 };
 
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
         row0 = a.offsets[e];
         e -= a.e_begin;
     }
-    const int lane = threadIdx.x % 64, w = threadIdx.x / 64, j = lane % 16, g = lane / 16;
+    const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), j = lane % 16, g = lane / 16;
     const int KT = a.K / kTileK8, scale_ld = scale_quads(a.K) * 4;
     const uint64_t at = (uint64_t)e * a.expert_bytes;
     const uint8_t* pw = a.w + at + (uint64_t)p * kM * KT * kTileBytes + lane * 16;
@@ -168,19 +170,38 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
     f32x4_t acc[kM];
 #pragma unroll
     for (int i = 0; i < kM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int kt = w; kt < KT; kt += kFewWaves) {
-        u32x4_t b0 = {0u, 0u, 0u, 0u}, b1 = b0;
-        if (live) {
-            b0 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8);
-            b1 = *reinterpret_cast<const u32x4_t*>(px + kt * kTileK8 + 32);
+    // kUnroll K tiles at a time, w, w + kFewWaves, ...; past the last one they are
+    // the last one again, with rows of zeros.  Lane u loads the scale of tile u.
+    constexpr int kUnroll = kMode == kFewGateUp ? kFewUnrollGU : kFewUnroll;
+    for (int kt = w; kt < KT; kt += kUnroll * kFewWaves) {
+        u32x4_t wt[kM][kUnroll], xb[kUnroll][2];
+        int sc[kM];
+        const int mine = min(kt + lane % kUnroll * kFewWaves, KT - 1);
+#pragma unroll
+        for (int i = 0; i < kM; ++i) sc[i] = ps[i][mine / 2];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+                wt[i][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(
+                    pw + (int64_t)(i * KT + min(kt + u * kFewWaves, KT - 1)) * kTileBytes));
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int t = kt + u * kFewWaves;
+            xb[u][0] = xb[u][1] = u32x4_t{0u, 0u, 0u, 0u};
+            if (live && t < KT) {
+                xb[u][0] = *reinterpret_cast<const u32x4_t*>(px + t * kTileK8);
+                xb[u][1] = *reinterpret_cast<const u32x4_t*>(px + t * kTileK8 + 32);
+            }
         }
 #pragma unroll
-        for (int i = 0; i < kM; ++i) {
-            const u32x4_t c = *reinterpret_cast<const u32x4_t*>(pw + ((int64_t)i * KT + kt) * kTileBytes);
-            const float scale = exp2i((int)ps[i][kt / 2] - 127);
-            acc[i] = mfma16x16x32(decode8(c[0], c[1], scale), b0, acc[i]);
-            acc[i] = mfma16x16x32(decode8(c[2], c[3], scale), b1, acc[i]);
-        }
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < kM; ++i) {
+                const float scale = __int_as_float(__builtin_amdgcn_readlane(sc[i], u) << 23);
+                acc[i] = mfma16x16x32(decode8(wt[i][u][0], wt[i][u][1], scale), xb[u][0], acc[i]);
+                acc[i] = mfma16x16x32(decode8(wt[i][u][2], wt[i][u][3], scale), xb[u][1], acc[i]);
+            }
     }
 #pragma unroll
     for (int i = 0; i < kM; ++i)

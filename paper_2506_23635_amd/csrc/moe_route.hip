@@ -18,8 +18,10 @@
 //       sums them in fixed order, selects and permutes.
 //   route_one_kernel: both in one launch where one workgroup forms the logits
 //       anyway (d <= 512).
-//   select_kernel: selection and weights from caller-supplied fp32 logits.
-//   permute_kernel: the permutation and the list of token tiles (one workgroup).
+//   router_kernel (more than 16 experts): logits on the fp64 matrix cores.
+//   select_kernel: selection and weights from fp32 logits, router_kernel's or the
+//       caller's.
+//   permute_kernel: the permutation and the list of token tiles.
 // The kernels that select have a second form for a layer with a routing policy
 // (choose below), select_kernel's is policy_select_kernel.
 //
@@ -135,6 +137,7 @@ __device__ __forceinline__ double max_lanes(double v)
 template <int W>
 __device__ __forceinline__ void choose(const Policy& p, float logit, int e, int E, int k, int* ids, float* w)
 {
+    constexpr int kAtOnce = 8;            // lanes read at once (those past E are closed)
     const bool live = e < E;
     const double l = live ? (double)logit : -INFINITY;
     // exp(l - m) of the lanes that take part; nothing but -inf gives zeros, a NaN stays one
@@ -154,10 +157,21 @@ __device__ __forceinline__ void choose(const Policy& p, float logit, int e, int 
     if (p.top_groups < p.n_groups) {
         const int n = E / p.n_groups, g = min(e, E - 1) / n;
         double b1 = -INFINITY, b2 = -INFINITY;                // the two largest c of the group
-        for (int i = 0; i < n; ++i) {
-            const double v = __shfl(c, g * n + i, W);
-            b2 = v > b1 ? b1 : fmax(b2, v);
-            b1 = fmax(b1, v);
+        if ((n & (n - 1)) == 0) {
+            b1 = c;
+            for (int o = 1; o < n; o <<= 1) {                 // groups are aligned runs of lanes
+                const double o1 = __shfl_xor(b1, o, W), o2 = __shfl_xor(b2, o, W);
+                b2 = fmax(fmin(b1, o1), fmax(b2, o2));
+                b1 = fmax(b1, o1);
+            }
+        } else {
+            for (int q0 = 0; q0 < E; q0 += kAtOnce)
+#pragma unroll
+                for (int q = q0; q < q0 + kAtOnce; ++q) {
+                    const double v = q >= g * n && q < g * n + n ? from_lane<W>(c, q) : -INFINITY;
+                    b2 = fmax(b2, fmin(b1, v));
+                    b1 = fmax(b1, v);
+                }
         }
         double value = p.group_best == 2 ? b1 + b2 : b1;
         if (value != value) value = -INFINITY;
@@ -168,14 +182,24 @@ __device__ __forceinline__ void choose(const Policy& p, float logit, int e, int 
         }
         open = live && before < p.top_groups;
     }
-    const uint64_t opened = __ballot(open) >> (threadIdx.x % kWave / W * W);
-    int rank = 0;
-    for (int q = 0; q < E; ++q) {
-        const double cq = from_lane<W>(c, q);
-        const float lq = from_lane<W>(order, q);
-        const bool first = cq > c || (cq == c && (lq > order || (lq == order && q < e)));
-        rank += first && (opened >> q & 1) ? 1 : 0;
-    }
+    // how many come before: those of a larger c, and (only where some c are equal)
+    // those of the same c with a larger logit, or the same and a lower id.  A
+    // closed expert's c is NaN here, which no comparison holds for.
+    const double key = open ? c : NAN;
+    int rank = 0, upto = 0;
+    for (int q0 = 0; q0 < E; q0 += kAtOnce)
+#pragma unroll
+        for (int q = q0; q < q0 + kAtOnce; ++q) {
+            const double cq = from_lane<W>(key, q);
+            rank += cq > c ? 1 : 0;
+            upto += cq >= c ? 1 : 0;
+        }
+    if (__ballot(open && upto > rank + 1))
+        for (int q = 0; q < E; ++q) {
+            const double cq = from_lane<W>(key, q);
+            const float lq = from_lane<W>(order, q);
+            rank += cq == c && (lq > order || (lq == order && q < e)) ? 1 : 0;
+        }
     const bool in = open && rank < k;
     double v = in ? s : 0.0;
     if (p.score == MOE_SCORE_SELECTED) v = exp_from(max_lanes<W>(in ? l : -INFINITY), in);
@@ -592,68 +616,169 @@ __global__ __launch_bounds__(kRsThreads) void router_select_kernel(const uint16_
     }
 }
 
-// Selection from caller-supplied fp32 logits (copied into the routing
-// view): one thread per token.
-__global__ __launch_bounds__(256) void select_kernel(const float* __restrict__ logits_in, int T,
+// Logits of more than 16 experts.  A workgroup takes 16 tokens x 16 experts, its
+// 16 waves the 32-element steps of the reduction axis in turn; a wave's step is
+// eight v_mfma_f64_16x16x4_f64, lane l holding eight elements of token l % 16 and of
+// expert l % 16, those from 8 (l / 16) on, and instruction i taking the i-th of
+// all four runs.  The waves' sums meet in LDS and are added in wave order.  Where
+// router_select_kernel spends 96 conversions to fp64 on 256 multiply-adds per lane,
+// this spends 16 on the same; and it has a workgroup for every 16 experts (2048
+// tokens of d 6144, 64 experts: 80 us there, selection included).  A step's loads
+// are issued before the multiplications of the step before.
+constexpr int kRmWaves = 16;
+constexpr int kRmStep = 32;
+constexpr int kRmManyWg = 512;     // workgroups of 16 tokens from which on they take 32
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
+
+template <int kTiles>              // of 16 tokens
+__global__ __launch_bounds__(64 * kRmWaves) void router_kernel(const uint16_t* __restrict__ x,
+                                                               const float* __restrict__ wrT,
+                                                               const float* __restrict__ bias, int T, int d, int E,
+                                                               float* __restrict__ logits)
+{
+    __shared__ double s_part[kRmWaves][4][64];
+    const int tid = threadIdx.x, lane = tid % 64, w = tid / 64;
+    const int t0 = blockIdx.x * (16 * kTiles), e0 = blockIdx.y * 16;
+    // tokens past T and experts past E: the last ones again, their sums dropped
+    const uint16_t* px[kTiles];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) px[n] = x + (int64_t)min(t0 + n * 16 + lane % 16, T - 1) * d + lane / 16 * 8;
+    const float* pw = wrT + (int64_t)min(e0 + lane % 16, E - 1) * d + lane / 16 * 8;
+    struct Step {
+        u32x4_t x[kTiles];
+        float4 w0, w1;
+    };
+    auto fetch = [&](Step& s, int k) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) s.x[n] = *reinterpret_cast<const u32x4_t*>(px[n] + k);
+        s.w0 = *reinterpret_cast<const float4*>(pw + k);
+        s.w1 = *reinterpret_cast<const float4*>(pw + k + 4);
+    };
+    f64x4_t acc[kTiles];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) acc[n] = f64x4_t{0.0, 0.0, 0.0, 0.0};
+    auto multiply = [&](const Step& s) {
+        const float wv[8] = {s.w0.x, s.w0.y, s.w0.z, s.w0.w, s.w1.x, s.w1.y, s.w1.z, s.w1.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+                const float xv = __uint_as_float(i % 2 ? s.x[n][i / 2] & 0xFFFF0000u : s.x[n][i / 2] << 16);
+                acc[n] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)xv, (double)wv[i], acc[n], 0, 0, 0);
+            }
+    };
+    constexpr int kAll = kRmStep * kRmWaves;
+    Step s0, s1;
+    int k = w * kRmStep;
+    if (k < d) fetch(s0, k);
+    for (; k < d; k += 2 * kAll) {
+        fetch(s1, min(k + kAll, d - kRmStep));
+        multiply(s0);
+        if (k + kAll >= d) break;
+        fetch(s0, min(k + 2 * kAll, d - kRmStep));
+        multiply(s1);
+    }
+    // lane l holds tokens l / 16 + 4 i of expert l % 16
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+        if (n > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s_part[w][i][lane] = acc[n][i];
+        __syncthreads();
+        if (tid < 256) {
+            const int i = tid / 64, t = t0 + n * 16 + lane / 16 + 4 * i, e = e0 + lane % 16;
+            double v = 0.0;
+#pragma unroll
+            for (int q = 0; q < kRmWaves; ++q) v += s_part[q][i][lane];
+            if (t < T && e < E) {
+                float l = (float)v;
+                if (bias) l = __fadd_rn(l, bias[e]);
+                logits[(int64_t)t * E + e] = l;
+            }
+        }
+    }
+}
+
+// Selection from fp32 logits (copied into the routing view, where they are not
+// there already): one thread per token.
+__global__ __launch_bounds__(256) void select_kernel(const float* logits_in, int T,
                                                      int E, int k, RouteView rv)
 {
     const int t = blockIdx.x * blockDim.x + threadIdx.x;
     if (t >= T) return;
     const float* l = logits_in + (int64_t)t * E;
-    for (int e = 0; e < E; ++e) rv.logits[(int64_t)t * E + e] = l[e];
+    if (logits_in != rv.logits)
+        for (int e = 0; e < E; ++e) rv.logits[(int64_t)t * E + e] = l[e];
     select_token_any(l, t, E, k, rv);
 }
 
 // The same under a policy: one wave per token.
-__global__ __launch_bounds__(256) void policy_select_kernel(const float* __restrict__ logits_in, int T, int E, int k,
+__global__ __launch_bounds__(256) void policy_select_kernel(const float* logits_in, int T, int E, int k,
                                                             Policy policy, RouteView rv)
 {
     const int t = blockIdx.x * (256 / kWave) + threadIdx.x / kWave, lane = threadIdx.x % kWave;
     if (t >= T) return;
     const float l = logits_in[(int64_t)t * E + min(lane, E - 1)];
-    if (lane < E) rv.logits[(int64_t)t * E + lane] = l;
+    if (lane < E && logits_in != rv.logits) rv.logits[(int64_t)t * E + lane] = l;
     choose<kWave>(policy, l, lane, E, k, rv.topk_idx + (int64_t)t * k, rv.topk_w + (int64_t)t * k);
 }
 
-// Expert-grouped permutation of the T*k pairs (one 1024-thread workgroup),
-// rows grouped by local expert, then by pair (token, slot) order.
-//  1. counts: LDS histogram of the local pairs (order-free); thread 0 then
-//     writes counts, offsets, the active-expert list and the token tiles.
-//  2. rows: pairs in rounds of 1024 x 8; each thread holds 8 consecutive
-//     pairs; per group of 16 experts, one wave scan of packed per-thread
-//     counts plus a scan of the wave totals give each pair its row after the
-//     expert's cursor.
-// Deterministic: no atomic decides a row.
-constexpr int kPermChunk = 8;
-constexpr int kPermGroup = 16;   // experts counted together (packed counters)
+// Expert-grouped permutation of the T*k pairs, rows grouped by local expert, then
+// by pair (token, slot) order.  A workgroup places a chunk of 1024 pairs (or of
+// several rounds of 1024, where there are more than kPermMaxWg chunks).  It
+// counts every pair's expert, those of earlier chunks apart, so that it knows the
+// experts' first rows and how many rows the chunks before it take of each, without
+// a launch or a wait between workgroups; the ids are 4 bytes a pair and lie in the
+// L2.  A pair's place among its round's is the number of equal ids before it: in
+// its wave by ballots over the id's bits, of the waves before by their counts.
+// Deterministic: the counts are sums, and no atomic decides a row.  (One workgroup
+// that placed all pairs, 8192 at a time with packed counters of 16 experts: 18 us
+// for 8192 pairs of 16 experts, 68 for 16384 of 64.)
+constexpr int kPermMaxWg = 1024;
+constexpr int kPermCopies = 4;       // histograms, by lane: fewer lanes meet at one counter
 
 struct PermArgs {
     int T, E, k, e_begin, n_local, tile_rows;
+    int chunk;                       // pairs per workgroup, a multiple of kRouteThreads
     RouteView rv;
 };
 
 __global__ __launch_bounds__(kRouteThreads) void permute_kernel(PermArgs a)
 {
-    constexpr int kWords = kPermGroup / 2;   // two 16-bit counters per word
-    __shared__ int hist[64];
+    __shared__ int hist[2][kPermCopies][64];     // all pairs, pairs of earlier chunks
     __shared__ int cursor[64];
-    __shared__ uint32_t wtot[kRouteWaves][kWords];
-    __shared__ uint32_t wpre[kRouteWaves][kWords];
-    __shared__ uint32_t rtot[kWords];
+    __shared__ int wcount[kRouteWaves][64];
     const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
     const int E = a.E, k = a.k, P = a.T * a.k;
     const int lo = a.e_begin, hi = a.e_begin + a.n_local;
     const RouteView& rv = a.rv;
-    if (tid < 64) hist[tid] = 0;
+    const int c0 = (int)blockIdx.x * a.chunk, c1 = min(c0 + a.chunk, P);
+    if (tid < 2 * kPermCopies * 64) (&hist[0][0][0])[tid] = 0;
     lds_barrier();
-    for (int p = tid; p < P; p += kRouteThreads) {
-        const int e = rv.topk_idx[p];
-        if (e >= lo && e < hi) atomicAdd(&hist[e], 1);
+    constexpr int kLoads = 8;                    // ids in flight per thread
+    for (int p0 = tid; p0 < P; p0 += kRouteThreads * kLoads) {
+        int ids[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) ids[i] = rv.topk_idx[min(p0 + i * kRouteThreads, P - 1)];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int p = p0 + i * kRouteThreads, e = ids[i];
+            if (p < P && e >= lo && e < hi) {
+                atomicAdd(&hist[0][lane % kPermCopies][e], 1);
+                if (p < c0) atomicAdd(&hist[1][lane % kPermCopies][e], 1);
+            }
+        }
     }
     lds_barrier();
-    // offsets, active list and tiles: prefix sums over the experts (wave 0)
+    // the experts' first rows (wave 0); workgroup 0 also writes the counts, the
+    // active list and the tiles
     if (wid == 0) {
-        int c = lane < E ? hist[lane] : 0;
+        int c = 0, earlier = 0;
+#pragma unroll
+        for (int i = 0; i < kPermCopies; ++i) {
+            c += hist[0][i][lane];
+            earlier += hist[1][i][lane];
+        }
         const int nz = c > 0 ? 1 : 0;
         const int tl = (c + a.tile_rows - 1) / a.tile_rows;
         int run = c, na = nz, nt = tl;
@@ -664,10 +789,10 @@ __global__ __launch_bounds__(kRouteThreads) void permute_kernel(PermArgs a)
             if (lane >= off) { run += r1; na += n1; nt += t1; }
         }
         run -= c; na -= nz; nt -= tl;   // exclusive
-        if (lane < E) {
+        cursor[lane] = run + earlier;
+        if (lane < E && blockIdx.x == 0) {
             rv.counts[lane] = c;
             rv.offsets[lane] = run;
-            cursor[lane] = run;
             if (c > 0) {
                 rv.active[1 + na] = lane;
                 for (int r = 0; r < c; r += a.tile_rows) {
@@ -683,87 +808,36 @@ __global__ __launch_bounds__(kRouteThreads) void permute_kernel(PermArgs a)
             }
         }
     }
-    lds_barrier();
-    // rows: rounds of 1024 x 8 pairs; thread t holds pairs 8t .. 8t+7 of the
-    // round.  Per group of 16 experts, each thread packs its per-expert counts
-    // two to a word (a round has at most 8192 pairs, below 2^16), one
-    // wave-level scan and one scan over the wave totals give every thread the
-    // rows of its pairs: cursor[e] + pairs of expert e in earlier threads +
-    // earlier pairs of its own.
-    for (int r0 = 0; r0 < P; r0 += kRouteThreads * kPermChunk) {
-        const int p0 = r0 + tid * kPermChunk;
-        int ids[kPermChunk];
+    for (int r0 = c0; r0 < c1; r0 += kRouteThreads) {
+        const int p = r0 + tid;
+        const int id = p < c1 ? rv.topk_idx[p] : -1;
+        const bool mine = id >= lo && id < hi;
+        uint64_t same = __ballot(mine);          // the wave's pairs of the same expert
 #pragma unroll
-        for (int q = 0; q < kPermChunk; ++q) {
-            ids[q] = p0 + q < P ? rv.topk_idx[p0 + q] : -1;
-            if (p0 + q < P && (ids[q] < lo || ids[q] >= hi)) rv.pair_row[p0 + q] = -1;
+        for (int bit = 0; bit < 6; ++bit) {
+            const uint64_t set = __ballot(id >> bit & 1);
+            same &= id >> bit & 1 ? set : ~set;
         }
-        for (int g0 = lo - lo % kPermGroup; g0 < hi; g0 += kPermGroup) {
-            uint32_t c[kWords];
-#pragma unroll
-            for (int m = 0; m < kWords; ++m) c[m] = 0u;
-#pragma unroll
-            for (int q = 0; q < kPermChunk; ++q) {
-                const int rel = ids[q] - g0;
-                const bool mine = ids[q] >= lo && ids[q] < hi && rel >= 0 && rel < kPermGroup;
-#pragma unroll
-                for (int m = 0; m < kWords; ++m)
-                    if (mine && (rel >> 1) == m) c[m] += 1u << (16 * (rel & 1));
-            }
-            uint32_t inc[kWords];
-#pragma unroll
-            for (int m = 0; m < kWords; ++m) {
-                uint32_t v = c[m];
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) {
-                    const uint32_t o = __shfl_up(v, off, 64);
-                    if (lane >= off) v += o;
-                }
-                inc[m] = v;
-            }
-            if (lane == 63) {
-#pragma unroll
-                for (int m = 0; m < kWords; ++m) wtot[wid][m] = inc[m];
-            }
-            lds_barrier();
-            if (tid < kRouteWaves * kWords) {
-                const int w = tid / kWords, m = tid % kWords;
-                uint32_t pre = 0u;
-                for (int w2 = 0; w2 < w; ++w2) pre += wtot[w2][m];
-                wpre[w][m] = pre;
-                if (w == kRouteWaves - 1) rtot[m] = pre + wtot[w][m];
-            }
-            lds_barrier();
-            // exclusive count of each expert's pairs before this thread's
-            uint32_t ex[kWords];
-#pragma unroll
-            for (int m = 0; m < kWords; ++m) ex[m] = wpre[wid][m] + inc[m] - c[m];
-            uint32_t own[kWords];
-#pragma unroll
-            for (int m = 0; m < kWords; ++m) own[m] = 0u;
-#pragma unroll
-            for (int q = 0; q < kPermChunk; ++q) {
-                const int rel = ids[q] - g0;
-                const bool mine = ids[q] >= lo && ids[q] < hi && rel >= 0 && rel < kPermGroup;
-                if (mine) {
-                    uint32_t before = 0u;
-#pragma unroll
-                    for (int m = 0; m < kWords; ++m)
-                        if ((rel >> 1) == m) {
-                            const int sh = 16 * (rel & 1);
-                            before = ((ex[m] >> sh) & 0xFFFFu) + ((own[m] >> sh) & 0xFFFFu);
-                            own[m] += 1u << sh;
-                        }
-                    const int row = cursor[ids[q]] + (int)before;
-                    rv.pair_row[p0 + q] = row;
-                    rv.row_token[row] = (p0 + q) / k;
-                }
-            }
-            lds_barrier();   // every thread has read cursor and wpre
-            if (tid < kPermGroup && g0 + tid >= lo && g0 + tid < hi)
-                cursor[g0 + tid] += (int)((rtot[tid >> 1] >> (16 * (tid & 1))) & 0xFFFFu);
-            lds_barrier();
+        const int before = __popcll(same & ((1ull << lane) - 1));
+        (&wcount[0][0])[tid] = 0;
+        lds_barrier();                           // (and the cursors are written)
+        if (mine && before == 0) wcount[wid][id] = __popcll(same);
+        lds_barrier();
+        int row = -1;
+        if (mine) {
+            row = cursor[id] + before;
+            for (int w = 0; w < wid; ++w) row += wcount[w][id];
+            rv.row_token[row] = p / k;
         }
+        if (p < c1) rv.pair_row[p] = row;
+        lds_barrier();                           // every thread has read the cursors
+        if (tid < 64) {
+            int n = 0;
+#pragma unroll
+            for (int w = 0; w < kRouteWaves; ++w) n += wcount[w][tid];
+            cursor[tid] += n;
+        }
+        lds_barrier();                           // ... and the waves' counts
     }
 }
 
@@ -829,11 +903,32 @@ extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wr
     return hipGetLastError();
 }
 
+static hipError_t launch_select(const float* logits, int T, int E, int k, const moe::Policy* policy,
+                                const moe::RouteView* rv, hipStream_t s)
+{
+    if (policy->on)
+        hipLaunchKernelGGL(moe::policy_select_kernel, dim3((T + 3) / 4), dim3(256), 0, s, logits, T, E, k, *policy, *rv);
+    else
+        hipLaunchKernelGGL(moe::select_kernel, dim3((T + 255) / 256), dim3(256), 0, s, logits, T, E, k, *rv);
+    return hipGetLastError();
+}
+
 extern "C" hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT,
                                                const float* bias, int T, int d, int E, int k,
                                                const moe::Policy* policy,
                                                const moe::RouteView* rv, hipStream_t s)
 {
+    if (E > 16) {
+        const int n_e = (E + 15) / 16, n_t = (T + 15) / 16;
+        if ((int64_t)n_t * n_e >= moe::kRmManyWg)
+            hipLaunchKernelGGL(moe::router_kernel<2>, dim3((n_t + 1) / 2, n_e), dim3(64 * moe::kRmWaves), 0, s, x, wrT, bias,
+                               T, d, E, rv->logits);
+        else
+            hipLaunchKernelGGL(moe::router_kernel<1>, dim3(n_t, n_e), dim3(64 * moe::kRmWaves), 0, s, x, wrT, bias, T, d, E,
+                               rv->logits);
+        const hipError_t e = hipGetLastError();
+        return e != hipSuccess ? e : launch_select(rv->logits, T, E, k, policy, rv, s);
+    }
     const int grid = (T + moe::kRsTok - 1) / moe::kRsTok;
     const auto kernel = policy->on ? moe::router_select_kernel<true> : moe::router_select_kernel<false>;
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(moe::kRsThreads), 0, s, x, wrT, bias, T, d, E, k, *policy,
@@ -845,22 +940,19 @@ extern "C" hipError_t moe_launch_route(const float* logits_in, int T, int E, int
                                        int n_local, int tile_rows, const moe::Policy* policy,
                                        const moe::RouteView* rv, hipStream_t s)
 {
-    if (logits_in && policy->on) {
-        hipLaunchKernelGGL(moe::policy_select_kernel, dim3((T + 3) / 4), dim3(256), 0, s, logits_in, T, E, k,
-                           *policy, *rv);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    } else if (logits_in) {
-        hipLaunchKernelGGL(moe::select_kernel, dim3((T + 255) / 256), dim3(256), 0, s, logits_in, T,
-                           E, k, *rv);
-        const hipError_t e = hipGetLastError();
+    if (logits_in) {
+        const hipError_t e = launch_select(logits_in, T, E, k, policy, rv, s);
         if (e != hipSuccess) return e;
     }
     moe::PermArgs a{};
     a.T = T; a.E = E; a.k = k;
     a.e_begin = e_begin; a.n_local = n_local; a.tile_rows = tile_rows;
     a.rv = *rv;
-    hipLaunchKernelGGL(moe::permute_kernel, dim3(1), dim3(moe::kRouteThreads), 0, s, a);
+    const int64_t rounds = ((int64_t)T * k + moe::kRouteThreads - 1) / moe::kRouteThreads;
+    const int per_wg = (int)((rounds + moe::kPermMaxWg - 1) / moe::kPermMaxWg);
+    a.chunk = per_wg * moe::kRouteThreads;
+    const int grid = (int)((rounds + per_wg - 1) / per_wg);
+    hipLaunchKernelGGL(moe::permute_kernel, dim3(grid), dim3(moe::kRouteThreads), 0, s, a);
     return hipGetLastError();
 }
 
