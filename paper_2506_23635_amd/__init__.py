@@ -405,7 +405,7 @@ class MoeLayer:
 
     @property
     def stream(self) -> int:
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        return _raw_stream(self.torch, self.device)
 
     def close(self):
         if getattr(self, "ctx", None):
@@ -599,19 +599,27 @@ def quantize_e4m3(x, codes, scales):
     of whole 16 bytes; codes (out) [T, n] float8_e4m3fn or uint8, scales (out) [T, ceil(n / 128)]
     uint8 (or float8_e8m0fnu), both contiguous."""
     import torch
-    bf = _bf16_types(torch)
+    global _e4m3_types
+    if _e4m3_types is None:
+        u8 = torch.uint8
+        _e4m3_types = (_bf16_types(torch) + (torch.float32,), (torch.float8_e4m3fn, u8),
+                       (u8, getattr(torch, "float8_e8m0fnu", u8)))
+    x_types, c_types, s_types = _e4m3_types
     if x is None or x.dim() != 2:
         raise MoeError(-2, "x must be [T, n]")
-    if x.device.type != "cuda":
-        raise MoeError(-1, f"x is on {x.device}, expected a GPU")
+    dev = x.device
+    if dev.type != "cuda":
+        raise MoeError(-1, f"x is on {dev}, expected a GPU")
     T, n = x.shape
-    ptr, ld = _rows(x, "x", T, n, bf + (torch.float32,), None)
-    e8m0 = getattr(torch, "float8_e8m0fnu", torch.uint8)
-    with _on_device(torch, x.device):
+    ptr, ld = _rows(x, "x", T, n, x_types, None)
+    with _on_device(torch, dev):
         moe_quantize_e4m3(ptr, ld, T_F32 if x.dtype == torch.float32 else T_BF16, T, n,
-                          _tensor_ptr(codes, "codes", T * n, (torch.float8_e4m3fn, torch.uint8), x.device),
-                          _tensor_ptr(scales, "scales", T * ((n + 127) // 128), (torch.uint8, e8m0), x.device),
-                          _raw_stream(torch, x.device))
+                          _tensor_ptr(codes, "codes", T * n, c_types, dev),
+                          _tensor_ptr(scales, "scales", T * ((n + 127) // 128), s_types, dev),
+                          _raw_stream(torch, dev))
+
+
+_e4m3_types = None   # types that x, codes and scales may have
 
 
 def make_linear_config(in_dim, out_dim, max_tokens=1, flags=0) -> LinearConfig:
@@ -1052,16 +1060,23 @@ class PagedCache:
 def _raw_stream(torch, device) -> int:
     """The handle of the device's current stream (without a Stream object: 0.1 against 2.1 us,
     of the 4 that a launch takes)."""
-    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return get(device.index) if get else torch.cuda.current_stream(device).cuda_stream
+    global _get_stream
+    if _get_stream is None:
+        _get_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda i: torch.cuda.current_stream(i).cuda_stream)
+    return _get_stream(device.index)
 
 
 _HERE = contextlib.nullcontext()
+_get_stream = _get_device = None
 
 
 def _on_device(torch, device):
     """A context in which the device is current (launches go to the current one)."""
-    return _HERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    global _get_device
+    if _get_device is None:
+        _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _HERE if _get_device() == device.index else torch.cuda.device(device)
 
 
 def _int32(a, name):

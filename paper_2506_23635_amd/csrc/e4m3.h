@@ -60,4 +60,32 @@ __device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
 }
 
+// Eight values with scale 2^e as the bf16 values that their codes stand for.
+__device__ __forceinline__ u32x4_t round8(const float* v, int e)
+{
+    const float inv = exp2i(-e);
+    return decode8(code4(v, inv), code4(v + 4, inv), exp2i(e));
+}
+
+// The exponent of the block of 128 whose elements 16 consecutive lanes hold, 8 each.
+__device__ __forceinline__ int block_exponent(const float* v)
+{
+    float amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (finite(v[i])) amax = fmaxf(amax, fabsf(v[i]));
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 16));
+    return scale_exponent(amax);
+}
+
+__device__ __forceinline__ void unpack8(const u32x4_t p, float* v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(p[i] << 16);
+        v[2 * i + 1] = __uint_as_float(p[i] & 0xFFFF0000u);
+    }
+}
+
 }  // namespace moe

@@ -225,8 +225,18 @@ moe_status check_layer(moe_ctx* ctx, int layer)
     return MOE_OK;
 }
 
+// x rounded to the e4m3 grid, in O's space (rows_max >= T): the down products come
+// after its last reader.
+uint16_t* rounded_x(const WsView& ws) { return reinterpret_cast<uint16_t*>(ws.base + ws.o_off); }
+
+// Whether the routing of T tokens of x rounds x on the way, for a forward.
+bool route_rounds(const moe_ctx* ctx, int T)
+{
+    return (ctx->cfg.flags & MOE_E4M3) && moe_route_decode_ok(T, ctx->cfg.n_experts, ctx->cfg.top_k);
+}
+
 moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T,
-                    const float* logits_in, hipStream_t s)
+                    const float* logits_in, bool forward, hipStream_t s)
 {
     const moe_config& c = ctx->cfg;
     uint8_t* lb = layer_base(ctx, layer);
@@ -241,7 +251,8 @@ moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x
         e = timed(ctx, MOE_K_ROUTE, s, [&] {
             return moe_launch_route_decode(x, wrT, bias, dpart, T, c.d_model, c.n_experts,
                                            c.top_k, c.expert_begin, c.n_local_experts, tile_rows,
-                                           policy, &ws.rv, s);
+                                           policy, forward && route_rounds(ctx, T) ? rounded_x(ws) : nullptr,
+                                           &ws.rv, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "route kernel launch");
     } else {
@@ -318,20 +329,19 @@ moe_status run_experts_e4m3_few(moe_ctx* ctx, const WsView& ws, int layer, const
     return MOE_OK;
 }
 
-moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T,
+// routed: do_route of this forward came before, with the same x
+moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T, bool routed,
                        hipStream_t s)
 {
     const moe_config& c = ctx->cfg;
     const uint8_t* experts = layer_base(ctx, layer) + ctx->L.experts_off;
     uint16_t* H = reinterpret_cast<uint16_t*>(ws.base + ws.h_off);
     float* O = reinterpret_cast<float*>(ws.base + ws.o_off);
-    hipError_t e;
+    hipError_t e = hipSuccess;
     const bool e4m3 = (c.flags & MOE_E4M3) != 0;
     if (e4m3) {
-        // x rounded to the e4m3 grid, into O's space (rows_max >= T): the down
-        // products come after its last reader
-        uint16_t* xq = reinterpret_cast<uint16_t*>(O);
-        e = timed(ctx, T <= kDecodeMaxTokens ? MOE_K_DECODE_GATEUP : MOE_K_GEMM_GATEUP, s, [&] {
+        uint16_t* xq = rounded_x(ws);
+        if (!(routed && route_rounds(ctx, T))) e = timed(ctx, T <= kDecodeMaxTokens ? MOE_K_DECODE_GATEUP : MOE_K_GEMM_GATEUP, s, [&] {
             return moe_launch_quantize(x, c.d_model, 1, T, nullptr, c.d_model, c.d_model, nullptr, nullptr, xq, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "quantize kernel launch");
@@ -641,7 +651,7 @@ moe_status moe_route(moe_ctx* ctx, int32_t layer, const uint16_t* x, int32_t T,
     } else if (misaligned(logits_in)) {
         return fail(ctx, MOE_E_ALIGN, "logits_in must be 16-byte aligned");
     }
-    moe_status st = do_route(ctx, ctx->ws, layer, x, T, logits_in, static_cast<hipStream_t>(stream));
+    moe_status st = do_route(ctx, ctx->ws, layer, x, T, logits_in, false, static_cast<hipStream_t>(stream));
     if (st != MOE_OK) return st;
     ctx->route_valid = true;
     ctx->route_layer = layer;
@@ -672,10 +682,10 @@ moe_status moe_forward(moe_ctx* ctx, int32_t layer, const uint16_t* x, int32_t T
             return fail(ctx, MOE_E_STATE, "routing was computed from a different x");
     } else {
         ctx->route_valid = false;   // the views are about to be overwritten
-        st = do_route(ctx, ctx->ws, layer, x, T, nullptr, s);
+        st = do_route(ctx, ctx->ws, layer, x, T, nullptr, true, s);
         if (st != MOE_OK) return st;
     }
-    st = run_experts(ctx, ctx->ws, layer, x, T, s);
+    st = run_experts(ctx, ctx->ws, layer, x, T, !r, s);
     if (st != MOE_OK) return st;
     const bool f32_out = (ctx->cfg.flags & MOE_PARTIAL_F32) != 0;
     return combine(ctx, ctx->ws, T, f32_out ? nullptr : static_cast<uint16_t*>(y),
@@ -700,9 +710,9 @@ moe_status moe_forward_layers(moe_ctx* ctx, int32_t first, int32_t n, uint16_t* 
     hipStream_t s = static_cast<hipStream_t>(stream);
     ctx->route_valid = false;   // the routing views are overwritten layer by layer
     for (int l = first; l < first + n; ++l) {
-        moe_status st = do_route(ctx, ctx->ws, l, x_inout, T, nullptr, s);
+        moe_status st = do_route(ctx, ctx->ws, l, x_inout, T, nullptr, true, s);
         if (st != MOE_OK) return st;
-        st = run_experts(ctx, ctx->ws, l, x_inout, T, s);
+        st = run_experts(ctx, ctx->ws, l, x_inout, T, true, s);
         if (st != MOE_OK) return st;
         st = combine(ctx, ctx->ws, T, nullptr, nullptr, x_inout, s);
         if (st != MOE_OK) return st;
@@ -724,9 +734,9 @@ moe_status moe_forward_residual(moe_ctx* ctx, int32_t layer, const uint16_t* x, 
     if (misaligned(x) || misaligned(r_inout)) return fail(ctx, MOE_E_ALIGN, "x and r must be 16-byte aligned");
     hipStream_t s = static_cast<hipStream_t>(stream);
     ctx->route_valid = false;   // the routing views are about to be overwritten
-    st = do_route(ctx, ctx->ws, layer, x, T, nullptr, s);
+    st = do_route(ctx, ctx->ws, layer, x, T, nullptr, true, s);
     if (st != MOE_OK) return st;
-    st = run_experts(ctx, ctx->ws, layer, x, T, s);
+    st = run_experts(ctx, ctx->ws, layer, x, T, true, s);
     if (st != MOE_OK) return st;
     return combine(ctx, ctx->ws, T, nullptr, nullptr, r_inout, s);
 }
@@ -761,9 +771,9 @@ moe_status moe_forward_static(moe_ctx* ctx, int32_t layer, const uint16_t* x, in
     if (st != MOE_OK) return st;
     const WsView ws = make_ws_view(base, L);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    st = do_route(ctx, ws, layer, x, T, nullptr, s);
+    st = do_route(ctx, ws, layer, x, T, nullptr, true, s);
     if (st != MOE_OK) return st;
-    st = run_experts(ctx, ws, layer, x, T, s);
+    st = run_experts(ctx, ws, layer, x, T, true, s);
     if (st != MOE_OK) return st;
     const bool f32_out = (ctx->cfg.flags & MOE_PARTIAL_F32) != 0;
     return combine(ctx, ws, T, f32_out ? nullptr : static_cast<uint16_t*>(y),

@@ -159,11 +159,20 @@ struct GemmArgs {
 // at byte 256 g + 16 r (g 0..3), holds K 8 g .. 8 g + 7 and 32 + 8 g .. 32 + 8 g + 7
 // of row r: one 16-byte load brings a lane its operands of two consecutive
 // 16x16x32 instructions, or of two 32x32x16 ones (granule l / 32: K steps 0 and
-// 2, granule 2 + l / 32: 1 and 3).  Row tiles as above (gate and up in turn).
+// 2, granule 2 + l / 32: 1 and 3).  Row tiles as above (gate and up in turn), four
+// of them (a wave's 64 rows of a 256-row tile) side by side, so that a stage reads
+// 4 KiB on end (64 tokens through the layer of d 6144, f 10752: 551 us with one
+// row tile after the other, 543; two or sixteen side by side 547).
 // Scales of a matrix: one byte e + 127 per 128 x 128 block, [features / 128]
 // [scale_quads(K) * 4].
 constexpr int kBlock = 128;
 constexpr int kTileK8 = 64;
+constexpr int kGroup8 = 4;
+// Byte offset of (row tile rt, K tile kt) of a matrix with KT K tiles.
+__host__ __device__ inline uint64_t tile_offset8(uint64_t rt, uint64_t kt, uint64_t KT)
+{
+    return ((rt / kGroup8 * KT + kt) * kGroup8 + rt % kGroup8) * (uint64_t)kTileBytes;
+}
 __host__ __device__ inline int scale_quads(int K) { return (K + 4 * kBlock - 1) / (4 * kBlock); }
 
 // Arguments of the products of few rows in e4m3: of a layer's experts (active
@@ -172,7 +181,9 @@ struct E4m3Args {
     const uint8_t* w;          // first local expert's packed matrix (gate and up interleaved), ...
     const uint8_t *ws, *ws_up; // ... its scales, those of up
     uint64_t expert_bytes;     // from expert to expert, of all three
-    const uint16_t* x;         // rows [..][K], bf16 on the e4m3 grid
+    const uint16_t* x;         // rows [..][K], bf16 on the e4m3 grid; or (raw_K > 0) ...
+    int64_t ldx;               // ... rows of raw_K bf16, ldx apart, which the product rounds itself
+    int raw_K;
     int K, N;                  // N features (of gate and up: of each)
     const int32_t *active, *counts, *offsets, *row_token;
     int e_begin, T;
@@ -196,7 +207,7 @@ int moe_route_decode_ok(int T, int E, int k);
 int moe_route_decode_wgs(int d);
 hipError_t moe_launch_route_decode(const uint16_t* x, const float* wrT, const float* bias,
                                    double* partial, int T, int d, int E, int k, int e_begin,
-                                   int n_local, int tile_rows, const moe::Policy* policy,
+                                   int n_local, int tile_rows, const moe::Policy* policy, uint16_t* xq,
                                    const moe::RouteView* rv, hipStream_t s);
 hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT, const float* bias, int T,
                                    int d, int E, int k, const moe::Policy* policy,
@@ -229,6 +240,7 @@ hipError_t moe_launch_pack_e4m3(const uint16_t* src, int K, int N, int K_pad, in
 void moe_pack_e4m3_host(const uint16_t* src, int K, int N, uint8_t* dst, uint8_t* scales, int rt_mul, int rt_add);
 hipError_t moe_launch_e4m3_gateup_few(const moe::E4m3Args* a, int n_slots, hipStream_t s);
 hipError_t moe_launch_e4m3_down_few(const moe::E4m3Args* a, int n_slots, hipStream_t s);
+int moe_e4m3_linear_raw(int T, int K);
 hipError_t moe_launch_e4m3_linear_few(const moe::E4m3Args* a, hipStream_t s);
 }
 

@@ -23,59 +23,58 @@ namespace moe {
 
 // ------------------------------------------------------------------ coding --
 
-// Eight values with scale 2^e as the bf16 values that their codes stand for.
-__device__ __forceinline__ u32x4_t round8(const float* v, int e)
-{
-    const float inv = exp2i(-e), scale = exp2i(e);
-    const uint32_t c0 = code4(v, inv), c1 = code4(v + 4, inv);
-    return decode8(c0, c1, scale);
-}
-
 // Rows to codes and scales, or (codes NULL) to the bf16 values that these stand
-// for: 16 lanes per block of 128, 8 elements each.  The block's maximum is formed
-// across the lanes; rows are read once and written once, so the kernel is bound
-// by memory.  Values from n to n_pad are zeros.  n_rows (device memory): rows that
-// there are, of at most T; or NULL.
-template <bool kBf16>
-__global__ __launch_bounds__(256) void quantize_kernel(const void* __restrict__ x, int64_t ld, int64_t T,
+// for: 16 lanes per block of 128, 8 elements each, two blocks at a time.  The
+// block's maximum is formed across the lanes; rows are read once and written
+// once, so the kernel is bound by memory.  Values from n to n_pad are zeros.
+// n_rows (device memory): rows that are written, of at most T; or NULL.  Index: the
+// type that counts the blocks (a division in 64 bits per block took half of the
+// time).
+template <bool kBf16, typename Index>
+__global__ __launch_bounds__(256) void quantize_kernel(const void* __restrict__ x, int64_t ld, Index T,
                                                        const int32_t* __restrict__ n_rows, int n, int n_pad,
                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                                        uint16_t* __restrict__ values)
 {
-    if (n_rows) T = min(T, (int64_t)*n_rows);
-    const int blocks = (n + kBlock - 1) / kBlock, piece = threadIdx.x % 16;
-    for (int64_t u = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; u < T * blocks; u += (int64_t)gridDim.x * 16) {
-        const int64_t t = u / blocks;
-        const int b = (int)(u - t * blocks), k = b * kBlock + piece * 8;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (k < n) {
-            if constexpr (kBf16) {
-                const u32x4_t p = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(x) + t * ld + k);
+    constexpr int kAtOnce = 2;
+    const Index blocks = (Index)((n + kBlock - 1) / kBlock), units = T * blocks, step = (Index)gridDim.x * 16;
+    const int piece = threadIdx.x % 16;
+    const int64_t rows = n_rows ? (int64_t)*n_rows : (int64_t)T;
+    for (Index u0 = (Index)blockIdx.x * 16 + threadIdx.x / 16; u0 < units; u0 += kAtOnce * step) {
+        float v[kAtOnce][8];
+        int64_t t[kAtOnce];
+        int b[kAtOnce];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[2 * i] = __uint_as_float(p[i] << 16);
-                    v[2 * i + 1] = __uint_as_float(p[i] & 0xFFFF0000u);
-                }
+        for (int i = 0; i < kAtOnce; ++i) {
+            const Index u = u0 + i * step;
+            const Index row = u / blocks;
+            t[i] = u < units ? (int64_t)row : -1;
+            b[i] = (int)(u - row * blocks);
+            const int k = b[i] * kBlock + piece * 8;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+            if (t[i] < 0 || k >= n) continue;
+            if constexpr (kBf16) {
+                unpack8(*reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(x) + t[i] * ld + k), v[i]);
             } else {
-                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + t * ld + k);
+                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + t[i] * ld + k);
                 const float4 p0 = p[0], p1 = p[1];
-                v[0] = p0.x; v[1] = p0.y; v[2] = p0.z; v[3] = p0.w;
-                v[4] = p1.x; v[5] = p1.y; v[6] = p1.z; v[7] = p1.w;
+                v[i][0] = p0.x; v[i][1] = p0.y; v[i][2] = p0.z; v[i][3] = p0.w;
+                v[i][4] = p1.x; v[i][5] = p1.y; v[i][6] = p1.z; v[i][7] = p1.w;
             }
         }
-        float amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (finite(v[i])) amax = fmaxf(amax, fabsf(v[i]));
-#pragma unroll
-        for (int o = 8; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 16));
-        const int e = scale_exponent(amax);
-        if (codes) {
-            const float inv = exp2i(-e);
-            if (k < n) *reinterpret_cast<uint2*>(codes + t * n + k) = make_uint2(code4(v, inv), code4(v + 4, inv));
-            if (piece == 0) scales[t * blocks + b] = (uint8_t)(e + 127);
-        } else if (k < n_pad) {
-            *reinterpret_cast<u32x4_t*>(values + t * n_pad + k) = round8(v, e);
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int k = b[i] * kBlock + piece * 8, e = block_exponent(v[i]);
+            if (t[i] < 0 || t[i] >= rows) continue;
+            if (codes) {
+                const float inv = exp2i(-e);
+                if (k < n)
+                    *reinterpret_cast<uint2*>(codes + t[i] * n + k) = make_uint2(code4(v[i], inv), code4(v[i] + 4, inv));
+                if (piece == 0) scales[t[i] * (int64_t)blocks + b[i]] = (uint8_t)(e + 127);
+            } else if (k < n_pad) {
+                *reinterpret_cast<u32x4_t*>(values + t[i] * n_pad + k) = round8(v[i], e);
+            }
         }
     }
 }
@@ -127,7 +126,7 @@ __global__ __launch_bounds__(256) void pack_e4m3_kernel(const uint16_t* __restri
             w[j] = code4(v, inv);
         }
         const int64_t rt = (int64_t)((n0 + n) / kTileRows) * rt_mul + rt_add;
-        *reinterpret_cast<u32x4_t*>(dst + (rt * KT + kt * 2 + c / 4) * kTileBytes + c % 4 * 256 + n % kTileRows * 16) = w;
+        *reinterpret_cast<u32x4_t*>(dst + tile_offset8(rt, kt * 2 + c / 4, KT) + c % 4 * 256 + n % kTileRows * 16) = w;
     }
 }
 
@@ -139,43 +138,45 @@ __global__ __launch_bounds__(256) void pack_e4m3_kernel(const uint16_t* __restri
 // tile is the A operand, the rows are the B operand.
 
 constexpr int kFewWaves = 8;
-constexpr int kFewUnrollGU = 6;    // K tiles per wave in flight, of gate and of up
-constexpr int kFewUnroll = 7;
+// K tiles per wave in flight, of each row tile (d 6144, f 10752: a wave has 12 and
+// 21; 3 to 7 within 1 %, 12 at once 20 % slower for the registers)
+constexpr int kFewUnroll = 6;
+constexpr int kFewUnrollDN = 7;
 
-enum { kFewGateUp = 0, kFewDown = 1, kFewLinear = 2 };
+// kFewLinearRaw: rows as they come; every workgroup rounds them itself, into LDS,
+// while its first weights are on their way
+enum { kFewGateUp = 0, kFewDown = 1, kFewLinear = 2, kFewLinearRaw = 3 };
 
 template <int kMode>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
 {
     constexpr int kM = kMode == kFewGateUp ? 2 : 1;      // row tiles per workgroup
-    __shared__ f32x4_t s_red[kM][(kFewWaves - 1) * 64];
+    constexpr bool kExperts = kMode == kFewGateUp || kMode == kFewDown;
+    constexpr bool kRaw = kMode == kFewLinearRaw;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    f32x4_t* s_red = reinterpret_cast<f32x4_t*>(lds);    // [kM][(kFewWaves - 1) * 64]
+    uint16_t* s_x = reinterpret_cast<uint16_t*>(lds + kM * (kFewWaves - 1) * 64 * sizeof(f32x4_t));   // kRaw: [T][K]
     const int n_tiles = a.N / kTileRows, slot = blockIdx.x / n_tiles, p = blockIdx.x % n_tiles;
-    int e = 0, m = a.T, row0 = 0;
-    if (kMode != kFewLinear) {
+    int ge = 0, e = 0;
+    if (kExperts) {
         if (slot >= a.active[0]) return;
-        e = a.active[1 + slot];
-        m = a.counts[e];
-        row0 = a.offsets[e];
-        e -= a.e_begin;
+        ge = a.active[1 + slot];
+        e = ge - a.e_begin;
     }
     const int lane = threadIdx.x % 64, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), j = lane % 16, g = lane / 16;
     const int KT = a.K / kTileK8, scale_ld = scale_quads(a.K) * 4;
     const uint64_t at = (uint64_t)e * a.expert_bytes;
-    const uint8_t* pw = a.w + at + (uint64_t)p * kM * KT * kTileBytes + lane * 16;
+    const uint8_t* pw[kM];
+#pragma unroll
+    for (int i = 0; i < kM; ++i) pw[i] = a.w + at + tile_offset8(p * kM + i, 0, KT) + lane * 16;
     const uint8_t* ps[2] = {a.ws + at + (int64_t)(p * kTileRows / kBlock) * scale_ld,
                             kM == 2 ? a.ws_up + at + (int64_t)(p * kTileRows / kBlock) * scale_ld : nullptr};
-    const bool live = j < m;
-    const int64_t row = live ? (kMode == kFewGateUp ? a.row_token[row0 + j] : row0 + j) : 0;
-    const uint16_t* px = a.x + row * a.K + g * 8;
-    f32x4_t acc[kM];
-#pragma unroll
-    for (int i = 0; i < kM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // kUnroll K tiles at a time, w, w + kFewWaves, ...; past the last one they are
     // the last one again, with rows of zeros.  Lane u loads the scale of tile u.
-    constexpr int kUnroll = kMode == kFewGateUp ? kFewUnrollGU : kFewUnroll;
-    for (int kt = w; kt < KT; kt += kUnroll * kFewWaves) {
-        u32x4_t wt[kM][kUnroll], xb[kUnroll][2];
-        int sc[kM];
+    constexpr int kUnroll = kMode == kFewDown ? kFewUnrollDN : kFewUnroll;
+    u32x4_t wt[kM][kUnroll];
+    int sc[kM];
+    auto fetch = [&](int kt) {
         const int mine = min(kt + lane % kUnroll * kFewWaves, KT - 1);
 #pragma unroll
         for (int i = 0; i < kM; ++i) sc[i] = ps[i][mine / 2];
@@ -184,7 +185,32 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
 #pragma unroll
             for (int i = 0; i < kM; ++i)
                 wt[i][u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(
-                    pw + (int64_t)(i * KT + min(kt + u * kFewWaves, KT - 1)) * kTileBytes));
+                    pw[i] + (int64_t)min(kt + u * kFewWaves, KT - 1) * (kGroup8 * kTileBytes)));
+    };
+    // the weights' addresses are known before the rows'
+    if (w < KT) fetch(w);
+    const int m = kExperts ? a.counts[ge] : a.T, row0 = kExperts ? a.offsets[ge] : 0;
+    const bool live = j < m;
+    const uint16_t* px;
+    if constexpr (kRaw) {
+        const int blocks = a.K / kBlock;
+        for (int u = threadIdx.x / 16; u < m * blocks; u += 64 * kFewWaves / 16) {
+            const int t = u / blocks, k = u % blocks * kBlock + threadIdx.x % 16 * 8;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (k < a.raw_K) unpack8(*reinterpret_cast<const u32x4_t*>(a.x + t * a.ldx + k), v);
+            *reinterpret_cast<u32x4_t*>(&s_x[t * a.K + k]) = round8(v, block_exponent(v));
+        }
+        __syncthreads();
+        px = s_x + (live ? j * a.K : 0) + g * 8;
+    } else {
+        const int64_t row = live ? (kMode == kFewGateUp ? a.row_token[row0 + j] : row0 + j) : 0;
+        px = a.x + row * a.K + g * 8;
+    }
+    f32x4_t acc[kM];
+#pragma unroll
+    for (int i = 0; i < kM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int kt = w; kt < KT; kt += kUnroll * kFewWaves) {
+        u32x4_t xb[kUnroll][2];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             const int t = kt + u * kFewWaves;
@@ -202,15 +228,17 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
                 acc[i] = mfma16x16x32(decode8(wt[i][u][0], wt[i][u][1], scale), xb[u][0], acc[i]);
                 acc[i] = mfma16x16x32(decode8(wt[i][u][2], wt[i][u][3], scale), xb[u][1], acc[i]);
             }
+        if (kt + kUnroll * kFewWaves < KT) fetch(kt + kUnroll * kFewWaves);
     }
+    constexpr int kRed = (kFewWaves - 1) * 64;
 #pragma unroll
     for (int i = 0; i < kM; ++i)
-        if (w > 0) s_red[i][(w - 1) * 64 + lane] = acc[i];
+        if (w > 0) s_red[i * kRed + (w - 1) * 64 + lane] = acc[i];
     __syncthreads();
     if (w > 0 || !live) return;
 #pragma unroll
     for (int i = 0; i < kM; ++i)
-        for (int q = 0; q + 1 < kFewWaves; ++q) acc[i] += s_red[i][q * 64 + lane];
+        for (int q = 0; q + 1 < kFewWaves; ++q) acc[i] += s_red[i * kRed + q * 64 + lane];
     const int64_t out = (int64_t)(row0 + j) * a.N + p * kTileRows + g * 4;
     if constexpr (kMode == kFewGateUp)
         *reinterpret_cast<float4*>(a.h32 + out) =
@@ -230,14 +258,15 @@ extern "C" {
 hipError_t moe_launch_quantize(const void* x, int64_t ld, int bf16, int64_t T, const int32_t* n_rows, int n,
                                int n_pad, uint8_t* codes, uint8_t* scales, uint16_t* values, hipStream_t s)
 {
-    const int64_t units = T * ((n + moe::kBlock - 1) / moe::kBlock);
-    const int grid = (int)((units + 15) / 16 < 65536 ? (units + 15) / 16 : 65536);
-    if (bf16)
-        hipLaunchKernelGGL(moe::quantize_kernel<true>, dim3(grid), dim3(256), 0, s, x, ld, T, n_rows, n, n_pad, codes,
-                           scales, values);
-    else
-        hipLaunchKernelGGL(moe::quantize_kernel<false>, dim3(grid), dim3(256), 0, s, x, ld, T, n_rows, n, n_pad, codes,
-                           scales, values);
+    const int64_t units = T * ((n + moe::kBlock - 1) / moe::kBlock), wgs = (units + 31) / 32;
+    const dim3 grid((unsigned)(wgs < 65536 ? wgs : 65536)), block(256);
+    if (units + (int64_t)grid.x * 32 <= UINT32_MAX) {
+        const auto kernel = bf16 ? moe::quantize_kernel<true, uint32_t> : moe::quantize_kernel<false, uint32_t>;
+        hipLaunchKernelGGL(kernel, grid, block, 0, s, x, ld, (uint32_t)T, n_rows, n, n_pad, codes, scales, values);
+    } else {
+        const auto kernel = bf16 ? moe::quantize_kernel<true, int64_t> : moe::quantize_kernel<false, int64_t>;
+        hipLaunchKernelGGL(kernel, grid, block, 0, s, x, ld, T, n_rows, n, n_pad, codes, scales, values);
+    }
     return hipGetLastError();
 }
 
@@ -249,24 +278,34 @@ hipError_t moe_launch_pack_e4m3(const uint16_t* src, int K, int N, int K_pad, in
     return hipGetLastError();
 }
 
+static size_t few_lds(int row_tiles) { return (size_t)row_tiles * (moe::kFewWaves - 1) * 64 * sizeof(moe::f32x4_t); }
+
 hipError_t moe_launch_e4m3_gateup_few(const moe::E4m3Args* a, int n_slots, hipStream_t s)
 {
     hipLaunchKernelGGL(moe::few_kernel<moe::kFewGateUp>, dim3(n_slots * (a->N / moe::kTileRows)),
-                       dim3(64 * moe::kFewWaves), 0, s, *a);
+                       dim3(64 * moe::kFewWaves), few_lds(2), s, *a);
     return hipGetLastError();
 }
 
 hipError_t moe_launch_e4m3_down_few(const moe::E4m3Args* a, int n_slots, hipStream_t s)
 {
     hipLaunchKernelGGL(moe::few_kernel<moe::kFewDown>, dim3(n_slots * (a->N / moe::kTileRows)),
-                       dim3(64 * moe::kFewWaves), 0, s, *a);
+                       dim3(64 * moe::kFewWaves), few_lds(1), s, *a);
     return hipGetLastError();
 }
 
+// Whether a plain product of T rows rounds them itself: one or two rows that take
+// at most 32 KiB of LDS (so that two workgroups still share a CU), rounded by
+// every workgroup in a round or two of its threads.
+int moe_e4m3_linear_raw(int T, int K) { return T <= 2 && (int64_t)T * K * 2 <= 32768; }
+
 hipError_t moe_launch_e4m3_linear_few(const moe::E4m3Args* a, hipStream_t s)
 {
-    hipLaunchKernelGGL(moe::few_kernel<moe::kFewLinear>, dim3(a->N / moe::kTileRows), dim3(64 * moe::kFewWaves), 0, s,
-                       *a);
+    const dim3 grid(a->N / moe::kTileRows), block(64 * moe::kFewWaves);
+    if (a->raw_K)
+        hipLaunchKernelGGL(moe::few_kernel<moe::kFewLinearRaw>, grid, block, few_lds(1) + (size_t)a->T * a->K * 2, s, *a);
+    else
+        hipLaunchKernelGGL(moe::few_kernel<moe::kFewLinear>, grid, block, few_lds(1), s, *a);
     return hipGetLastError();
 }
 
@@ -311,7 +350,7 @@ void moe_pack_e4m3_host(const uint16_t* src, int K, int N, uint8_t* dst, uint8_t
                     if (std::signbit(x)) c |= 0x80;
                     const size_t rt = (size_t)((n0 + n) / moe::kTileRows) * rt_mul + rt_add;
                     const int q = k % moe::kTileK8;        // in the K tile: granule, half and byte of it
-                    dst[moe::tile_offset(rt, kb * 2 + k / moe::kTileK8, KT) + q % 32 / 8 * 256 +
+                    dst[moe::tile_offset8(rt, kb * 2 + k / moe::kTileK8, KT) + q % 32 / 8 * 256 +
                         n % moe::kTileRows * 16 + q / 32 * 8 + q % 8] = c;
                 }
         }

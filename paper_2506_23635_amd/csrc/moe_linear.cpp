@@ -155,7 +155,9 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
     if (x0 < y1 && y0 < x1) return fail(ctx, MOE_E_ARG, "y overlaps x");
     hipStream_t s = static_cast<hipStream_t>(stream);
     uint16_t* xq = reinterpret_cast<uint16_t*>(ctx->workspace);
-    hipError_t e = moe_launch_quantize(x, ldx, 1, T, nullptr, c.in_dim, ctx->L.K, nullptr, nullptr, xq, s);
+    const bool raw = moe_e4m3_linear_raw(T, ctx->L.K);
+    hipError_t e = hipSuccess;
+    if (!raw) e = moe_launch_quantize(x, ldx, 1, T, nullptr, c.in_dim, ctx->L.K, nullptr, nullptr, xq, s);
     if (e != hipSuccess) return hip_fail(ctx, e, "quantize kernel launch");
     float* y32 = type == MOE_T_F32 ? static_cast<float*>(y) : nullptr;
     uint16_t* y16 = type == MOE_T_F32 ? nullptr : static_cast<uint16_t*>(y);
@@ -163,7 +165,9 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
         moe::E4m3Args a{};
         a.w = ctx->weights;
         a.ws = ctx->weights + ctx->L.scales_off;
-        a.x = xq;
+        a.x = raw ? x : xq;
+        a.ldx = ldx;
+        a.raw_K = raw ? c.in_dim : 0;
         a.K = ctx->L.K;
         a.N = c.out_dim;
         a.T = T;

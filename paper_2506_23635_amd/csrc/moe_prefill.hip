@@ -130,7 +130,8 @@ __device__ __forceinline__ void load_a(AStage<kE4m3, kFB>& A, __amdgpu_buffer_rs
 {
     if constexpr (kE4m3)
         A.v[fb * kLoadsA8 + i] = __builtin_bit_cast(
-            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, a_off + i * (kTileBytes / 2), s * kTileBytes, kPolicy));
+            u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rsrc, a_off + i * (kTileBytes / 2), s * (kGroup8 * kTileBytes),
+                                                           kPolicy));
     else
         // K step i: K tile 2 s + i / 2, its second half (512 bytes on) for odd i
         A.v[fb * KS + i] = __builtin_bit_cast(
@@ -714,7 +715,8 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
                                                  kBufferFlags);
 #pragma unroll
     for (int fb = 0; fb < FB; ++fb)
-        c.a_off[fb] = (uint32_t)tile_offset(rt0 + 2 * fb + ((lane & 31) >> 4), 0, KT) +
+        c.a_off[fb] = (uint32_t)(kE4m3 ? tile_offset8(rt0 + 2 * fb + ((lane & 31) >> 4), 0, KT)
+                                       : tile_offset(rt0 + 2 * fb + ((lane & 31) >> 4), 0, KT)) +
                       (uint32_t)(((lane >> 5) * 16) + (lane & 15)) * 16;
     if constexpr (kE4m3) c.s_off = scale_offset<kMode>(a, e, K, (int)rt0, lane, c.s_rsrc);
     // B: a stage holds, for each of the 256 token rows R of the tile, the
@@ -960,23 +962,22 @@ struct MidCtx {
 // B loads are counted.  B loads past the last stage re-read it into a buffer
 // that no later stage reads.
 //
-// e4m3 weights are half of the bytes, so eight stages of them are in flight; a
-// stage's refills are two granules and the scale, the first granule's before the
-// wait.  With kW = 8 waves (gate/up in e4m3: 256 packed features, so that the
+// e4m3 weights: a stage's refills are two granules and the scale, the first
+// granule's before the wait.  (Eight stages of both operands on their way, where
+// the rows leave room for them, changed nothing.)  With kW = 8 waves (gate/up in e4m3: 256 packed features, so that the
 // workgroup has whole blocks of H) a load of B takes 64 rows: an odd last block
 // loads rows it has already once more.
 template <int kTB, bool kOnce, bool kE4m3, int kW>
 __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kMidTB])
 {
     using Stage = AStage<kE4m3, 1>;
-    constexpr int kRing = kE4m3 ? 2 * kMidRing : kMidRing;
     constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
     constexpr int kLoadsB = (kTB * 4 + kW - 1) / kW;
     constexpr int kStage = kLoadsB * kW * 8 * BK * 2;
     constexpr int kAfter = 2 * kLoadsB + (kE4m3 ? 2 * (kLoadsA8 + 1) + 1 : 3 * KS - 1);
     constexpr int kWaitMid = wait_vm(kAfter), kWaitMidTail = wait_vm(2 * kLoadsB);
     const int n_stages = c.n_stages, w = c.w;
-    Stage ra[kRing];
+    Stage ra[kMidRing];
     auto load_a1 = [&](int s, int i, Stage& dst) {
         load_a<kE4m3, 1, kOnce ? kNonTemporal : 0>(dst, c.a_rsrc, c.a_off, 0, i, c.s0 + (uint32_t)s);
     };
@@ -999,7 +1000,7 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     auto stage = [&](int s, Stage& A, auto tail) {
         constexpr bool kTail = decltype(tail)::value;
         const int next = cur + kStage == kMidRingB * kStage ? 0 : cur + kStage;
-        const int sa = min(s + kRing, n_stages - 1);
+        const int sa = min(s + kMidRing, n_stages - 1);
         load_b(min(s + kMidRingB - 1, n_stages - 1), prev);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -1027,7 +1028,7 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     };
     // A first: its addresses do not wait for the row gather
 #pragma unroll
-    for (int i = 0; i < kRing; ++i) {
+    for (int i = 0; i < kMidRing; ++i) {
 #pragma unroll
         for (int j = 0; j < kLoadsA; ++j) load_a1(min(i, n_stages - 1), j, ra[i]);
         if constexpr (kE4m3) load_scale(ra[i], c.s_rsrc, c.s_off, c.s0 + (uint32_t)min(i, n_stages - 1));
@@ -1040,12 +1041,12 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     asm volatile("" ::: "memory");
     read_b(0, 0, bw[0]);
     int s = 0;
-    for (; s + kRing <= n_stages; s += kRing) {
+    for (; s + kMidRing <= n_stages; s += kMidRing) {
 #pragma unroll
-        for (int i = 0; i < kRing; ++i) stage(s + i, ra[i], std::false_type{});
+        for (int i = 0; i < kMidRing; ++i) stage(s + i, ra[i], std::false_type{});
     }
 #pragma unroll
-    for (int i = 0; i + 1 < kRing; ++i)
+    for (int i = 0; i + 1 < kMidRing; ++i)
         if (s + i < n_stages) stage(s + i, ra[i], std::true_type{});
     // drain the dummy B loads before the workgroup's LDS can be handed on
     __builtin_amdgcn_s_waitcnt(kWaitAll);
@@ -1100,7 +1101,7 @@ __global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_ke
     const uint64_t slab_bytes = kMode == kGateUp ? a.gu_bytes : a.expert_bytes - a.gu_bytes;
     c.a_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase), 0, (int)slab_bytes,
                                                  kBufferFlags);
-    c.a_off = (uint32_t)tile_offset(rt + ((lane & 31) >> 4), 0, KT) +
+    c.a_off = (uint32_t)(kE4m3 ? tile_offset8(rt + ((lane & 31) >> 4), 0, KT) : tile_offset(rt + ((lane & 31) >> 4), 0, KT)) +
               (uint32_t)(((lane >> 5) * 16) + (lane & 15)) * 16;
     if constexpr (kE4m3) c.s_off = scale_offset<kMode>(a, e, K, (int)rt, lane, c.s_rsrc);
     if (kMode == kGateUp)

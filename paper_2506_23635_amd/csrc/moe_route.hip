@@ -33,6 +33,7 @@
 #include <algorithm>
 
 #include "../../include/moe.h"
+#include "e4m3.h"
 #include "moe_common.h"
 
 namespace moe {
@@ -257,6 +258,7 @@ struct DecodeRouteArgs {
     const float* bias;
     double* partial;          // [n_wg][kSmallT][kDecE]
     int T, d, E, k, e_begin, n_local, tile_rows, n_wg;
+    uint16_t* xq;             // x rounded to the e4m3 grid (workgroups from n_wg on), or NULL
     Policy policy;
     RouteView rv;
 };
@@ -305,9 +307,26 @@ __device__ __forceinline__ double partial_logits(const DecodeRouteArgs& a)
     return v;
 }
 
+// x on the e4m3 grid, for experts in that form: the work of the workgroups behind
+// those that form logits, 64 blocks of 128 each (a launch of its own is 4 us).
+constexpr int kRoundBlocks = kRouteThreads / 16;
+__device__ __forceinline__ void round_x(const DecodeRouteArgs& a, int wg)
+{
+    const int blocks = a.d / kBlock, u = wg * kRoundBlocks + threadIdx.x / 16;
+    if (u >= a.T * blocks) return;                       // 16 lanes at once
+    const int64_t at = (int64_t)u * kBlock + threadIdx.x % 16 * 8;
+    float v[8];
+    unpack8(*reinterpret_cast<const u32x4_t*>(a.x + at), v);
+    *reinterpret_cast<u32x4_t*>(a.xq + at) = round8(v, block_exponent(v));
+}
+
 template <int kT>
 __global__ __launch_bounds__(kRouteThreads) void route_partials_kernel(DecodeRouteArgs a)
 {
+    if ((int)blockIdx.x >= a.n_wg) {
+        round_x(a, blockIdx.x - a.n_wg);
+        return;
+    }
     const double v = partial_logits<kT>(a);
     const int tid = threadIdx.x;
     if (tid < a.T * kDecE) a.partial[(int64_t)blockIdx.x * kSmallT * kDecE + tid] = v;
@@ -358,6 +377,10 @@ template <int kT, bool kPolicy>
 __global__ __launch_bounds__(kRouteThreads) void route_one_kernel(DecodeRouteArgs a)
 {
     __shared__ float lg[kSmallT][kDecE];
+    if (blockIdx.x > 0) {
+        round_x(a, blockIdx.x - 1);
+        return;
+    }
     const double v = partial_logits<kT>(a);
     const int tid = threadIdx.x, t = tid / kDecE, ee = tid % kDecE;
     if (t < a.T && ee < a.E) {
@@ -867,11 +890,13 @@ extern "C" int moe_route_decode_wgs(int d) { return (d / 8 + 63) / 64; }
 extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wrT,
                                               const float* bias, double* partial, int T, int d,
                                               int E, int k, int e_begin, int n_local, int tile_rows,
-                                              const moe::Policy* policy, const moe::RouteView* rv,
-                                              hipStream_t s)
+                                              const moe::Policy* policy, uint16_t* xq,
+                                              const moe::RouteView* rv, hipStream_t s)
 {
     moe::DecodeRouteArgs a{};
     a.policy = *policy;
+    a.xq = xq;
+    const int round_wgs = xq ? (T * (d / moe::kBlock) + moe::kRoundBlocks - 1) / moe::kRoundBlocks : 0;
     a.x = x; a.wrT = wrT; a.bias = bias; a.partial = partial;
     a.T = T; a.d = d; a.E = E; a.k = k;
     a.e_begin = e_begin; a.n_local = n_local; a.tile_rows = tile_rows;
@@ -889,13 +914,13 @@ extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wr
                        : by_tokens(moe::route_one_kernel<1, false>, moe::route_one_kernel<2, false>,
                                    moe::route_one_kernel<4, false>, moe::route_one_kernel<8, false>,
                                    moe::route_one_kernel<moe::kSmallT, false>);
-        hipLaunchKernelGGL(one, dim3(1), dim3(moe::kRouteThreads), 0, s, a);
+        hipLaunchKernelGGL(one, dim3(1 + round_wgs), dim3(moe::kRouteThreads), 0, s, a);
         return hipGetLastError();
     }
     const Kernel partials = by_tokens(moe::route_partials_kernel<1>, moe::route_partials_kernel<2>,
                                       moe::route_partials_kernel<4>, moe::route_partials_kernel<8>,
                                       moe::route_partials_kernel<moe::kSmallT>);
-    hipLaunchKernelGGL(partials, dim3(a.n_wg), dim3(moe::kRouteThreads), 0, s, a);
+    hipLaunchKernelGGL(partials, dim3(a.n_wg + round_wgs), dim3(moe::kRouteThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const Kernel finish = policy->on ? moe::route_finish_kernel<true> : moe::route_finish_kernel<false>;
