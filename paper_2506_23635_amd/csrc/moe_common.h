@@ -225,6 +225,8 @@ hipError_t moe_launch_gemm_qkv(const moe::GemmArgs* a, hipStream_t s);
 hipError_t moe_launch_gemm_out(const moe::GemmArgs* a, hipStream_t s);
 int moe_prefill_tile_rows();
 int moe_gemm_mid_tiles(int T, int k, int E, int n_local, int M);
+int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M);
+int moe_gemm_linear_split(int T, int K, int M);
 int moe_gemm_plain_split(int T, int M);
 hipError_t moe_launch_combine(const float* O, const int32_t* pair_row, const float* topk_w, int T,
                               int d, int k, uint16_t* y, float* y32, uint16_t* x_residual,
@@ -241,6 +243,8 @@ void moe_pack_e4m3_host(const uint16_t* src, int K, int N, uint8_t* dst, uint8_t
 hipError_t moe_launch_e4m3_gateup_few(const moe::E4m3Args* a, int n_slots, hipStream_t s);
 hipError_t moe_launch_e4m3_down_few(const moe::E4m3Args* a, int n_slots, hipStream_t s);
 int moe_e4m3_linear_raw(int T, int K);
+hipError_t moe_launch_linear_sum(const float* parts, int n, int64_t stride, int64_t count, float* y32, uint16_t* y16,
+                                 hipStream_t s);
 hipError_t moe_launch_e4m3_linear_few(const moe::E4m3Args* a, hipStream_t s);
 }
 

@@ -130,6 +130,25 @@ __global__ __launch_bounds__(256) void pack_e4m3_kernel(const uint16_t* __restri
     }
 }
 
+// The sums of a plain product's ranges of K, in their order; count is a multiple
+// of 16.
+__global__ __launch_bounds__(256) void linear_sum_kernel(const float* __restrict__ parts, int n, int64_t stride,
+                                                         int64_t count, float* __restrict__ y32,
+                                                         uint16_t* __restrict__ y16)
+{
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= count) return;
+    float4 v = *reinterpret_cast<const float4*>(parts + i);
+    for (int q = 1; q < n; ++q) {
+        const float4 p = *reinterpret_cast<const float4*>(parts + q * stride + i);
+        v = make_float4(v.x + p.x, v.y + p.y, v.z + p.z, v.w + p.w);
+    }
+    if (y32)
+        *reinterpret_cast<float4*>(y32 + i) = v;
+    else
+        *reinterpret_cast<uint2*>(y16 + i) = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
+}
+
 // --------------------------------------------------------------- few rows --
 //
 // At most 16 rows per expert (or of a plain product): the weights are streamed
@@ -306,6 +325,14 @@ hipError_t moe_launch_e4m3_linear_few(const moe::E4m3Args* a, hipStream_t s)
         hipLaunchKernelGGL(moe::few_kernel<moe::kFewLinearRaw>, grid, block, few_lds(1) + (size_t)a->T * a->K * 2, s, *a);
     else
         hipLaunchKernelGGL(moe::few_kernel<moe::kFewLinear>, grid, block, few_lds(1), s, *a);
+    return hipGetLastError();
+}
+
+hipError_t moe_launch_linear_sum(const float* parts, int n, int64_t stride, int64_t count, float* y32, uint16_t* y16,
+                                 hipStream_t s)
+{
+    hipLaunchKernelGGL(moe::linear_sum_kernel, dim3((unsigned)((count / 4 + 255) / 256)), dim3(256), 0, s, parts, n, stride,
+                       count, y32, y16);
     return hipGetLastError();
 }
 

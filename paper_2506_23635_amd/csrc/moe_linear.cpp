@@ -2,6 +2,7 @@
 // (include/moe.h, "Products in e4m3"): checks, the buffers' division, launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <new>
 #include <string>
@@ -12,6 +13,9 @@
 namespace {
 
 constexpr int kFewTokens = 16;          // rows of one MFMA B operand
+constexpr int kRowTile = 128;           // rows of a tile of a product with ranges of K; ...
+constexpr int kSplitRows = 64;          // ... up to these rows there are always such tiles
+constexpr int kMostSplit = 16384;       // ... and beyond these none has ranges (two feature tiles at least)
 constexpr int kFeatures = 256;          // packed features come in multiples of a tile's
 constexpr size_t kAlign = 256;
 
@@ -20,8 +24,14 @@ bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
 struct Layout {
     int K, N;                           // padded
-    size_t scales_off, weight_bytes, ws_bytes;
+    size_t scales_off, weight_bytes, parts_off, ws_bytes;
 };
+
+// Ranges of K of a call with T rows (more than kFewTokens).
+int n_split(const Layout& L, int T)
+{
+    return moe_gemm_mid_tiles(T, 1, 1, 1, L.N) ? moe_gemm_linear_split(T, L.K, L.N) : 1;
+}
 
 const char* check_config(const moe_linear_config* c)
 {
@@ -46,7 +56,16 @@ Layout make_layout(const moe_linear_config* c)
     const size_t quads = moe::scale_quads(L.K);
     L.scales_off = (size_t)L.K * L.N;
     L.weight_bytes = align_up(L.scales_off + (size_t)(L.N / moe::kBlock) * quads * 4, kAlign);
-    L.ws_bytes = align_up((size_t)c->max_tokens * L.K * 2, kAlign);
+    // rows on the e4m3 grid, then the sums of the ranges of K, for the call that
+    // needs the most: calls whose last row tile is the same have as many ranges
+    L.parts_off = align_up((size_t)c->max_tokens * L.K * 2, kAlign);
+    size_t parts = 0;
+    for (int rows = kSplitRows; rows <= kMostSplit; rows += rows < kRowTile ? kRowTile - rows : kRowTile) {
+        const int T = std::min(rows, c->max_tokens), n = T > kFewTokens ? n_split(L, T) : 1;
+        if (n > 1) parts = std::max(parts, (size_t)n * T * c->out_dim * 4);
+        if (T == c->max_tokens) break;
+    }
+    L.ws_bytes = align_up(L.parts_off + parts, kAlign);
     return L;
 }
 
@@ -188,8 +207,14 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
         a.n_local = 1;
         a.T = a.max_rows = T;
         a.mid = moe_gemm_mid_tiles(T, 1, 1, 1, ctx->L.N);
-        a.k_split = 1;
+        a.k_split = n_split(ctx->L, T);
+        if (a.k_split > 1) {
+            a.O = reinterpret_cast<float*>(ctx->workspace + ctx->L.parts_off);
+            a.split_stride = (uint64_t)T * c.out_dim;
+        }
         e = moe_launch_gemm_linear(&a, s);
+        if (e == hipSuccess && a.k_split > 1)
+            e = moe_launch_linear_sum(a.O, a.k_split, (int64_t)a.split_stride, (int64_t)a.split_stride, y32, y16, s);
     }
     if (e != hipSuccess) return hip_fail(ctx, e, "product kernel launch");
     return MOE_OK;

@@ -647,7 +647,9 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x16_t (&a
                         if (n >= a.n_out) continue;
                         const float4 v = *reinterpret_cast<const float4*>(&buf[r * kRow + p * 16]);
                         const int64_t at = (int64_t)row * a.n_out + n;
-                        if (a.y16)
+                        if (a.k_split > 1)
+                            *reinterpret_cast<float4*>(a.O + (uint64_t)split * a.split_stride + at) = v;
+                        else if (a.y16)
                             *reinterpret_cast<uint2*>(a.y16 + at) = make_uint2(cvt_pk_bf16(v.x, v.y), cvt_pk_bf16(v.z, v.w));
                         else
                             *reinterpret_cast<float4*>(a.O + at) = v;
@@ -1163,6 +1165,37 @@ int moe_gemm_mid_tiles(int T, int k, int E, int n_local, int M)
     if (pairs <= (int64_t)64 * E) return 1;
     const int64_t rows = (pairs + E - 1) / E;
     return (int64_t)(M / moe::BM) * n_local * ((rows + moe::BN - 1) / moe::BN) <= 128;
+}
+
+// The same for experts in e4m3.  Half of the weight bytes leave the 256 x 256
+// tiles, one workgroup per CU, more exposed: their partial tiles and uneven last
+// round cost until an expert has 180 rows, or, with few tiles, 400 (whole layer, 256
+// x 256 tiles -> 128 x 128; d 6144, f 10752, 16 experts, top-4: 200 tokens 671 -> 630
+// us, 512 1109 -> 996, 700 (175 rows, 1344 tiles) 1284 -> 1220, 800 1341 -> 1350;
+// 4 of the 16: 700 tokens 446 -> 351, 1400 (350 rows, 672 tiles) 588 -> 540, 2000
+// (500) 658 -> 727; 8 experts, top-2, d 1024, f 2048: 2000 tokens (500 rows, 256
+// tiles) 121 -> 105, 3000 139 -> 138; 16 of d 4096, f 2048, top-4: 1700 tokens 294 ->
+// 263; 32 of d 2048, f 4096, top-4: 2000 tokens (250 rows, 1024 tiles) 496 -> 502).
+int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M)
+{
+    const int64_t rows = ((int64_t)T * k + E - 1) / E;
+    const int64_t tiles = (int64_t)(M / moe::BM) * n_local * ((rows + moe::BN - 1) / moe::BN);
+    return rows <= 176 || tiles <= (rows <= 400 ? 768 : 384);
+}
+
+// Ranges of the reduction of a moe_linear's product on 128 x 128 tiles: as many, up
+// to 4, as leave every range kSplitStages stages and the grid one workgroup per CU
+// (6144 to 8192 features: 64 tokens, 64 tiles, 33.0 -> 23.7 us in four ranges, 200
+// tokens, 128 tiles, 45.8 -> 37.2 in two, 512 tokens, 256 tiles, 53.7 -> 59.2; 2048 to
+// 512: 1024 tokens, 32 tiles of 32 stages, 24.1 -> 20.9 in two; 1040 to 1488: 1024
+// tokens, 96 tiles of 18 stages, 19.0 -> 23.0).
+constexpr int kSplitStages = 16;
+int moe_gemm_linear_split(int T, int K, int M)
+{
+    const int64_t tiles = (int64_t)(M / moe::MBM) * ((T + moe::MBN - 1) / moe::MBN);
+    int n = 1;
+    while (n < 4 && tiles * n * 2 <= 256 && K / moe::BK >= kSplitStages * n * 2) n *= 2;
+    return n;
 }
 
 // Ranges of the reduction of a plain product on 128 x 128 tiles: two where
