@@ -60,23 +60,53 @@ __device__ inline u32x4_t decode8(uint32_t c0, uint32_t c1, float scale)
                          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
 }
 
-// Eight values with scale 2^e as the bf16 values that their codes stand for.
-__device__ __forceinline__ u32x4_t round8(const float* v, int e)
+// The largest of 16 consecutive lanes' values, for all of them: rotations within
+// the row of 16 (row_ror), which the maximum takes as its operand.
+__device__ __forceinline__ uint32_t max16(uint32_t v)
 {
-    const float inv = exp2i(-e);
-    return decode8(code4(v, inv), code4(v + 4, inv), exp2i(e));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x124, 0xF, 0xF, false));
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x122, 0xF, 0xF, false));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x121, 0xF, 0xF, false));
 }
 
-// The exponent of the block of 128 whose elements 16 consecutive lanes hold, 8 each.
-__device__ __forceinline__ int block_exponent(const float* v)
+// The block of 128 whose elements 16 consecutive lanes hold, 8 each: its scale's
+// exponent, and this lane's codes.  The maximum is taken of the bits, so a value
+// that is not finite shows in it, and only then do the lanes look at them one by
+// one (which takes as long as the rest).
+struct Coded {
+    int e;
+    uint32_t lo, hi;
+};
+__device__ __forceinline__ Coded code_block(const float* v)
 {
-    float amax = 0.f;
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (finite(v[i])) amax = fmaxf(amax, fabsf(v[i]));
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(v[i]));
+    m = max16(m);
+    Coded c;
+    if (m < kInfBits) {
+        c.e = scale_exponent(__uint_as_float(m));
+        const float inv = exp2i(-c.e);
+        c.lo = code4_finite(v, inv);
+        c.hi = code4_finite(v + 4, inv);
+        return c;
+    }
+    m = 0;
 #pragma unroll
-    for (int o = 8; o >= 1; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 16));
-    return scale_exponent(amax);
+    for (int i = 0; i < 8; ++i) m = max(m, finite(v[i]) ? abs_bits(v[i]) : 0u);
+    c.e = scale_exponent(__uint_as_float(max16(m)));
+    const float inv = exp2i(-c.e);
+    c.lo = code4(v, inv);
+    c.hi = code4(v + 4, inv);
+    return c;
+}
+
+// The same as the bf16 values that the codes stand for.
+__device__ __forceinline__ u32x4_t round_block(const float* v)
+{
+    const Coded c = code_block(v);
+    return decode8(c.lo, c.hi, exp2i(c.e));
 }
 
 __device__ __forceinline__ void unpack8(const u32x4_t p, float* v)

@@ -229,16 +229,12 @@ moe_status check_layer(moe_ctx* ctx, int layer)
 // after its last reader.
 uint16_t* rounded_x(const WsView& ws) { return reinterpret_cast<uint16_t*>(ws.base + ws.o_off); }
 
-// Whether the routing of T tokens of x rounds x on the way, for a forward.
-bool route_rounds(const moe_ctx* ctx, int T)
-{
-    return (ctx->cfg.flags & MOE_E4M3) && moe_route_decode_ok(T, ctx->cfg.n_experts, ctx->cfg.top_k);
-}
-
 moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x, int T,
                     const float* logits_in, bool forward, hipStream_t s)
 {
     const moe_config& c = ctx->cfg;
+    // for a forward of a MOE_E4M3 layer the routing rounds x on the way
+    uint16_t* xq = forward && (c.flags & MOE_E4M3) ? rounded_x(ws) : nullptr;
     uint8_t* lb = layer_base(ctx, layer);
     const float* wrT = reinterpret_cast<const float*>(lb);
     const float* bias = ctx->has_bias[layer] ? reinterpret_cast<const float*>(lb + ctx->L.bias_off)
@@ -251,8 +247,7 @@ moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x
         e = timed(ctx, MOE_K_ROUTE, s, [&] {
             return moe_launch_route_decode(x, wrT, bias, dpart, T, c.d_model, c.n_experts,
                                            c.top_k, c.expert_begin, c.n_local_experts, tile_rows,
-                                           policy, forward && route_rounds(ctx, T) ? rounded_x(ws) : nullptr,
-                                           &ws.rv, s);
+                                           policy, xq, &ws.rv, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "route kernel launch");
     } else {
@@ -265,7 +260,7 @@ moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x
         }
         e = timed(ctx, MOE_K_ROUTE, s, [&] {
             return moe_launch_route(logits_in, T, c.n_experts, c.top_k, c.expert_begin,
-                                    c.n_local_experts, tile_rows, policy, &ws.rv, s);
+                                    c.n_local_experts, tile_rows, policy, x, c.d_model, xq, &ws.rv, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "route kernel launch");
     }
@@ -341,7 +336,7 @@ moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t
     const bool e4m3 = (c.flags & MOE_E4M3) != 0;
     if (e4m3) {
         uint16_t* xq = rounded_x(ws);
-        if (!(routed && route_rounds(ctx, T))) e = timed(ctx, T <= kDecodeMaxTokens ? MOE_K_DECODE_GATEUP : MOE_K_GEMM_GATEUP, s, [&] {
+        if (!routed) e = timed(ctx, T <= kDecodeMaxTokens ? MOE_K_DECODE_GATEUP : MOE_K_GEMM_GATEUP, s, [&] {
             return moe_launch_quantize(x, c.d_model, 1, T, nullptr, c.d_model, c.d_model, nullptr, nullptr, xq, s);
         });
         if (e != hipSuccess) return hip_fail(ctx, e, "quantize kernel launch");

@@ -213,8 +213,8 @@ hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT, const f
                                    int d, int E, int k, const moe::Policy* policy,
                                    const moe::RouteView* rv, hipStream_t s);
 hipError_t moe_launch_route(const float* logits_in, int T, int E, int k, int e_begin, int n_local,
-                            int tile_rows, const moe::Policy* policy, const moe::RouteView* rv,
-                            hipStream_t s);
+                            int tile_rows, const moe::Policy* policy, const uint16_t* x, int d,
+                            uint16_t* xq, const moe::RouteView* rv, hipStream_t s);
 hipError_t moe_launch_transpose_router(const float* wr, int d, int E, float* wrT, hipStream_t s);
 hipError_t moe_launch_decode_gateup(const moe::DecodeArgs* a, int n_slots, hipStream_t s);
 hipError_t moe_launch_decode_down(const moe::DecodeArgs* a, int n_slots, hipStream_t s);

@@ -24,57 +24,42 @@ namespace moe {
 // ------------------------------------------------------------------ coding --
 
 // Rows to codes and scales, or (codes NULL) to the bf16 values that these stand
-// for: 16 lanes per block of 128, 8 elements each, two blocks at a time.  The
-// block's maximum is formed across the lanes; rows are read once and written
-// once, so the kernel is bound by memory.  Values from n to n_pad are zeros.
-// n_rows (device memory): rows that are written, of at most T; or NULL.  Index: the
-// type that counts the blocks (a division in 64 bits per block took half of the
-// time).
+// for: 16 lanes per block of 128, 8 elements each.  Rows are read once and written
+// once: 2048 x 6144 from bf16 to codes, 38 MB, in 7.5 us, 5.0 TB/s (two blocks per
+// thread at a time 7.5, four 9.0).  Values from n to n_pad are zeros.  n_rows
+// (device memory): rows that are written, of at most T; or NULL.  Index: the type
+// that counts the blocks (a division in 64 bits per block took longer than the
+// rest).
 template <bool kBf16, typename Index>
 __global__ __launch_bounds__(256) void quantize_kernel(const void* __restrict__ x, int64_t ld, Index T,
                                                        const int32_t* __restrict__ n_rows, int n, int n_pad,
                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                                        uint16_t* __restrict__ values)
 {
-    constexpr int kAtOnce = 2;
-    const Index blocks = (Index)((n + kBlock - 1) / kBlock), units = T * blocks, step = (Index)gridDim.x * 16;
+    const Index blocks = (Index)((n + kBlock - 1) / kBlock), units = T * blocks;
     const int piece = threadIdx.x % 16;
     const int64_t rows = n_rows ? (int64_t)*n_rows : (int64_t)T;
-    for (Index u0 = (Index)blockIdx.x * 16 + threadIdx.x / 16; u0 < units; u0 += kAtOnce * step) {
-        float v[kAtOnce][8];
-        int64_t t[kAtOnce];
-        int b[kAtOnce];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const Index u = u0 + i * step;
-            const Index row = u / blocks;
-            t[i] = u < units ? (int64_t)row : -1;
-            b[i] = (int)(u - row * blocks);
-            const int k = b[i] * kBlock + piece * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-            if (t[i] < 0 || k >= n) continue;
+    for (Index u = (Index)blockIdx.x * 16 + threadIdx.x / 16; u < units; u += (Index)gridDim.x * 16) {
+        const int64_t t = (int64_t)(u / blocks);
+        const int b = (int)(u - (Index)t * blocks), k = b * kBlock + piece * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (k < n) {
             if constexpr (kBf16) {
-                unpack8(*reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(x) + t[i] * ld + k), v[i]);
+                unpack8(*reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(x) + t * ld + k), v);
             } else {
-                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + t[i] * ld + k);
+                const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + t * ld + k);
                 const float4 p0 = p[0], p1 = p[1];
-                v[i][0] = p0.x; v[i][1] = p0.y; v[i][2] = p0.z; v[i][3] = p0.w;
-                v[i][4] = p1.x; v[i][5] = p1.y; v[i][6] = p1.z; v[i][7] = p1.w;
+                v[0] = p0.x; v[1] = p0.y; v[2] = p0.z; v[3] = p0.w;
+                v[4] = p1.x; v[5] = p1.y; v[6] = p1.z; v[7] = p1.w;
             }
         }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const int k = b[i] * kBlock + piece * 8, e = block_exponent(v[i]);
-            if (t[i] < 0 || t[i] >= rows) continue;
-            if (codes) {
-                const float inv = exp2i(-e);
-                if (k < n)
-                    *reinterpret_cast<uint2*>(codes + t[i] * n + k) = make_uint2(code4(v[i], inv), code4(v[i] + 4, inv));
-                if (piece == 0) scales[t[i] * (int64_t)blocks + b[i]] = (uint8_t)(e + 127);
-            } else if (k < n_pad) {
-                *reinterpret_cast<u32x4_t*>(values + t[i] * n_pad + k) = round8(v[i], e);
-            }
+        const Coded c = code_block(v);
+        if (t >= rows) continue;
+        if (codes) {
+            if (k < n) *reinterpret_cast<uint2*>(codes + t * n + k) = make_uint2(c.lo, c.hi);
+            if (piece == 0) scales[t * (int64_t)blocks + b] = (uint8_t)(c.e + 127);
+        } else if (k < n_pad) {
+            *reinterpret_cast<u32x4_t*>(values + t * n_pad + k) = decode8(c.lo, c.hi, exp2i(c.e));
         }
     }
 }
@@ -157,14 +142,16 @@ __global__ __launch_bounds__(256) void linear_sum_kernel(const float* __restrict
 // tile is the A operand, the rows are the B operand.
 
 constexpr int kFewWaves = 8;
-// K tiles per wave in flight, of each row tile (d 6144, f 10752: a wave has 12 and
-// 21; 3 to 7 within 1 %, 12 at once 20 % slower for the registers)
-constexpr int kFewUnroll = 6;
-constexpr int kFewUnrollDN = 7;
 
 // kFewLinearRaw: rows as they come; every workgroup rounds them itself, into LDS,
 // while its first weights are on their way
 enum { kFewGateUp = 0, kFewDown = 1, kFewLinear = 2, kFewLinearRaw = 3 };
+
+// K tiles per wave in flight, of each row tile (d 6144, f 10752, one token, where a
+// wave has 12 K tiles of gate and up and 21 of down: gate/up 76.4 us with 3, 78.1
+// with 4, 78.9 with 6; down 45.4 with 4, 43.0 with 7, 52.4 with 11; 6144 to 8192
+// features 7.2 with 4, 7.6 with 6.  4 or 16 waves instead of 8: 2 to 15 % slower.)
+constexpr int few_unroll(int mode) { return mode == kFewGateUp ? 3 : mode == kFewDown ? 7 : 4; }
 
 template <int kMode>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
@@ -192,7 +179,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
                             kM == 2 ? a.ws_up + at + (int64_t)(p * kTileRows / kBlock) * scale_ld : nullptr};
     // kUnroll K tiles at a time, w, w + kFewWaves, ...; past the last one they are
     // the last one again, with rows of zeros.  Lane u loads the scale of tile u.
-    constexpr int kUnroll = kMode == kFewDown ? kFewUnrollDN : kFewUnroll;
+    constexpr int kUnroll = few_unroll(kMode);
     u32x4_t wt[kM][kUnroll];
     int sc[kM];
     auto fetch = [&](int kt) {
@@ -217,7 +204,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
             const int t = u / blocks, k = u % blocks * kBlock + threadIdx.x % 16 * 8;
             float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (k < a.raw_K) unpack8(*reinterpret_cast<const u32x4_t*>(a.x + t * a.ldx + k), v);
-            *reinterpret_cast<u32x4_t*>(&s_x[t * a.K + k]) = round8(v, block_exponent(v));
+            *reinterpret_cast<u32x4_t*>(&s_x[t * a.K + k]) = round_block(v);
         }
         __syncthreads();
         px = s_x + (live ? j * a.K : 0) + g * 8;
@@ -277,9 +264,9 @@ extern "C" {
 hipError_t moe_launch_quantize(const void* x, int64_t ld, int bf16, int64_t T, const int32_t* n_rows, int n,
                                int n_pad, uint8_t* codes, uint8_t* scales, uint16_t* values, hipStream_t s)
 {
-    const int64_t units = T * ((n + moe::kBlock - 1) / moe::kBlock), wgs = (units + 31) / 32;
+    const int64_t units = T * ((n + moe::kBlock - 1) / moe::kBlock), wgs = (units + 15) / 16;
     const dim3 grid((unsigned)(wgs < 65536 ? wgs : 65536)), block(256);
-    if (units + (int64_t)grid.x * 32 <= UINT32_MAX) {
+    if (units + (int64_t)grid.x * 16 <= UINT32_MAX) {
         const auto kernel = bf16 ? moe::quantize_kernel<true, uint32_t> : moe::quantize_kernel<false, uint32_t>;
         hipLaunchKernelGGL(kernel, grid, block, 0, s, x, ld, (uint32_t)T, n_rows, n, n_pad, codes, scales, values);
     } else {

@@ -308,23 +308,24 @@ __device__ __forceinline__ double partial_logits(const DecodeRouteArgs& a)
 }
 
 // x on the e4m3 grid, for experts in that form: the work of the workgroups behind
-// those that form logits, 64 blocks of 128 each (a launch of its own is 4 us).
+// those that form logits or place pairs, 64 blocks of 128 each (a launch of its own
+// is 4 us).
 constexpr int kRoundBlocks = kRouteThreads / 16;
-__device__ __forceinline__ void round_x(const DecodeRouteArgs& a, int wg)
+__device__ __forceinline__ void round_x(const uint16_t* x, uint16_t* xq, int T, int d, int wg)
 {
-    const int blocks = a.d / kBlock, u = wg * kRoundBlocks + threadIdx.x / 16;
-    if (u >= a.T * blocks) return;                       // 16 lanes at once
+    const int u = wg * kRoundBlocks + threadIdx.x / 16;
+    if (u >= T * (d / kBlock)) return;                   // 16 lanes at once
     const int64_t at = (int64_t)u * kBlock + threadIdx.x % 16 * 8;
     float v[8];
-    unpack8(*reinterpret_cast<const u32x4_t*>(a.x + at), v);
-    *reinterpret_cast<u32x4_t*>(a.xq + at) = round8(v, block_exponent(v));
+    unpack8(*reinterpret_cast<const u32x4_t*>(x + at), v);
+    *reinterpret_cast<u32x4_t*>(xq + at) = round_block(v);
 }
 
 template <int kT>
 __global__ __launch_bounds__(kRouteThreads) void route_partials_kernel(DecodeRouteArgs a)
 {
     if ((int)blockIdx.x >= a.n_wg) {
-        round_x(a, blockIdx.x - a.n_wg);
+        round_x(a.x, a.xq, a.T, a.d, blockIdx.x - a.n_wg);
         return;
     }
     const double v = partial_logits<kT>(a);
@@ -378,7 +379,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_one_kernel(DecodeRouteArg
 {
     __shared__ float lg[kSmallT][kDecE];
     if (blockIdx.x > 0) {
-        round_x(a, blockIdx.x - 1);
+        round_x(a.x, a.xq, a.T, a.d, blockIdx.x - 1);
         return;
     }
     const double v = partial_logits<kT>(a);
@@ -763,6 +764,10 @@ constexpr int kPermCopies = 4;       // histograms, by lane: fewer lanes meet at
 struct PermArgs {
     int T, E, k, e_begin, n_local, tile_rows;
     int chunk;                       // pairs per workgroup, a multiple of kRouteThreads
+    int n_wg;                        // workgroups that place pairs; those behind them ...
+    const uint16_t* x;               // ... round x [T, d] to xq, or there are none
+    uint16_t* xq;
+    int d;
     RouteView rv;
 };
 
@@ -775,6 +780,10 @@ __global__ __launch_bounds__(kRouteThreads) void permute_kernel(PermArgs a)
     const int E = a.E, k = a.k, P = a.T * a.k;
     const int lo = a.e_begin, hi = a.e_begin + a.n_local;
     const RouteView& rv = a.rv;
+    if ((int)blockIdx.x >= a.n_wg) {
+        round_x(a.x, a.xq, a.T, a.d, blockIdx.x - a.n_wg);
+        return;
+    }
     const int c0 = (int)blockIdx.x * a.chunk, c1 = min(c0 + a.chunk, P);
     if (tid < 2 * kPermCopies * 64) (&hist[0][0][0])[tid] = 0;
     lds_barrier();
@@ -885,6 +894,9 @@ extern "C" int moe_route_decode_ok(int T, int E, int k)
 
 extern "C" int moe_route_decode_wgs(int d) { return (d / 8 + 63) / 64; }
 
+// workgroups that round x [T, d]
+static int round_wgs(int T, int d) { return (T * (d / moe::kBlock) + moe::kRoundBlocks - 1) / moe::kRoundBlocks; }
+
 
 
 extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wrT,
@@ -896,7 +908,7 @@ extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wr
     moe::DecodeRouteArgs a{};
     a.policy = *policy;
     a.xq = xq;
-    const int round_wgs = xq ? (T * (d / moe::kBlock) + moe::kRoundBlocks - 1) / moe::kRoundBlocks : 0;
+    const int n_round = xq ? round_wgs(T, d) : 0;
     a.x = x; a.wrT = wrT; a.bias = bias; a.partial = partial;
     a.T = T; a.d = d; a.E = E; a.k = k;
     a.e_begin = e_begin; a.n_local = n_local; a.tile_rows = tile_rows;
@@ -914,13 +926,13 @@ extern "C" hipError_t moe_launch_route_decode(const uint16_t* x, const float* wr
                        : by_tokens(moe::route_one_kernel<1, false>, moe::route_one_kernel<2, false>,
                                    moe::route_one_kernel<4, false>, moe::route_one_kernel<8, false>,
                                    moe::route_one_kernel<moe::kSmallT, false>);
-        hipLaunchKernelGGL(one, dim3(1 + round_wgs), dim3(moe::kRouteThreads), 0, s, a);
+        hipLaunchKernelGGL(one, dim3(1 + n_round), dim3(moe::kRouteThreads), 0, s, a);
         return hipGetLastError();
     }
     const Kernel partials = by_tokens(moe::route_partials_kernel<1>, moe::route_partials_kernel<2>,
                                       moe::route_partials_kernel<4>, moe::route_partials_kernel<8>,
                                       moe::route_partials_kernel<moe::kSmallT>);
-    hipLaunchKernelGGL(partials, dim3(a.n_wg + round_wgs), dim3(moe::kRouteThreads), 0, s, a);
+    hipLaunchKernelGGL(partials, dim3(a.n_wg + n_round), dim3(moe::kRouteThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const Kernel finish = policy->on ? moe::route_finish_kernel<true> : moe::route_finish_kernel<false>;
@@ -963,7 +975,8 @@ extern "C" hipError_t moe_launch_router_select(const uint16_t* x, const float* w
 
 extern "C" hipError_t moe_launch_route(const float* logits_in, int T, int E, int k, int e_begin,
                                        int n_local, int tile_rows, const moe::Policy* policy,
-                                       const moe::RouteView* rv, hipStream_t s)
+                                       const uint16_t* x, int d, uint16_t* xq, const moe::RouteView* rv,
+                                       hipStream_t s)
 {
     if (logits_in) {
         const hipError_t e = launch_select(logits_in, T, E, k, policy, rv, s);
@@ -976,8 +989,11 @@ extern "C" hipError_t moe_launch_route(const float* logits_in, int T, int E, int
     const int64_t rounds = ((int64_t)T * k + moe::kRouteThreads - 1) / moe::kRouteThreads;
     const int per_wg = (int)((rounds + moe::kPermMaxWg - 1) / moe::kPermMaxWg);
     a.chunk = per_wg * moe::kRouteThreads;
-    const int grid = (int)((rounds + per_wg - 1) / per_wg);
-    hipLaunchKernelGGL(moe::permute_kernel, dim3(grid), dim3(moe::kRouteThreads), 0, s, a);
+    a.n_wg = (int)((rounds + per_wg - 1) / per_wg);
+    a.x = x;
+    a.xq = xq;
+    a.d = d;
+    hipLaunchKernelGGL(moe::permute_kernel, dim3(a.n_wg + (xq ? round_wgs(T, d) : 0)), dim3(moe::kRouteThreads), 0, s, a);
     return hipGetLastError();
 }
 
