@@ -1078,7 +1078,7 @@ __global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_ke
     constexpr int kW = kMidWaves<kMode, kE4m3>;
     __shared__ __attribute__((aligned(16))) uint8_t lds[kMidRingB * MBN * BK * 2];
     const int n_ftiles = (kMode == kGateUp ? 2 * a.f : a.d) / (32 * kW);
-    const TilePos tp = find_tile(a, blockIdx.x, n_ftiles * a.k_split, MBN);
+    const TilePos tp = find_tile(a, blockIdx.x, n_ftiles * a.k_split, kE4m3 ? a.mid_rows : MBN);
     if (tp.el < 0) return;
     const int split = tp.ft / n_ftiles, ft = tp.ft % n_ftiles;
     const int e = a.e_begin + tp.el;
@@ -1183,6 +1183,24 @@ int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M)
     return rows <= 176 || tiles <= (rows <= 400 ? 768 : 384);
 }
 
+// Token rows of these tiles on e4m3 weights of M packed features per expert, n_split
+// ranges of K: 32 where that leaves one workgroup per CU at most, 64 up to as many as
+// run at once (gate/up's have twice the waves: one per CU, the others two).  The
+// shorter tiles' stages take less time each, where there are too few tiles for the
+// CUs to hide it (a plain product, 32 / 64 / 128 rows: 1040 to 1488 features, 12
+// tiles, 333 tokens 10.2 / 11.8 / 15.8 us, 1024 tokens 14.3 / 14.3 / 18.1, 2048 22.3 /
+// 20.3 / 21.2; 4096 to 4096, two ranges, 200 tokens 24.4 / 21.3 / 22.6; 512 to 2048,
+// 2048 tokens 16.9 / 14.7 / 15.6).
+// (Whole layer, 128 rows -> these, 8 experts, top-2, d 1024, f 2048: 300 tokens 51.6 ->
+// 40.4 us; with 64 rows for gate/up at 1000 tokens, 512 workgroups, 66.4 -> 71.4.)
+int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int gateup)
+{
+    const int waves = gateup ? moe::kMidWaves<moe::kGateUp, true> : moe::kMidWaves<moe::kDown, true>;
+    const int64_t rows = ((int64_t)T * k + E - 1) / E, per_row_tile = (int64_t)n_local * (M / (32 * waves)) * n_split;
+    if (per_row_tile * ((rows + 31) / 32) <= 256) return 32;
+    return per_row_tile * ((rows + 63) / 64) <= 2048 / waves ? 64 : moe::MBN;
+}
+
 // Ranges of the reduction of a moe_linear's product on 128 x 128 tiles: as many, up
 // to 4, as leave every range kSplitStages stages and the grid one workgroup per CU
 // (6144 to 8192 features: 64 tokens, 64 tiles, 33.0 -> 23.7 us in four ranges, 200
@@ -1225,7 +1243,7 @@ static hipError_t launch_any(const moe::GemmArgs* a, hipStream_t s)
     const int M = kMode == moe::kGateUp ? 2 * a->f : a->d;
     if (a->mid) {
         constexpr int kW = moe::kMidWaves<kMode, kE4m3>;
-        hipLaunchKernelGGL((moe::gemm_mid_kernel<kMode, kE4m3>), gemm_grid(a, M / (32 * kW) * a->k_split, moe::MBN),
+        hipLaunchKernelGGL((moe::gemm_mid_kernel<kMode, kE4m3>), gemm_grid(a, M / (32 * kW) * a->k_split, kE4m3 ? a->mid_rows : moe::MBN),
                            dim3(64 * kW), 0, s, *a);
     } else {
         hipLaunchKernelGGL((moe::gemm_kernel<kMode, kE4m3>), gemm_grid(a, M / moe::BM, moe::BN), dim3(moe::kThreads), 0, s,
