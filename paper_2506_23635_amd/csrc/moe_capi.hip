@@ -96,7 +96,7 @@ Layout make_layout(const moe_config* c)
         L.region_bytes[region] = bytes;
         return o;
     };
-    L.dpart_off = take(MOE_WS_ROUTE_PARTIALS, (size_t)moe_route_decode_wgs(c->d_model) * 16 * 16 * 8);
+    L.dpart_off = take(MOE_WS_ROUTE_PARTIALS, moe_route_partial_bytes(c->max_tokens, c->d_model, c->n_experts));
     L.logits_off = take(MOE_WS_LOGITS, Tm * E * 4);
     L.idx_off = take(MOE_WS_TOPK_IDX, Tm * k * 4);
     L.w_off = take(MOE_WS_TOPK_W, Tm * k * 4);
@@ -241,9 +241,9 @@ moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x
                                              : nullptr;
     const int tile_rows = moe_prefill_tile_rows();
     const moe::Policy* policy = &ctx->policy[layer];
+    double* dpart = reinterpret_cast<double*>(ws.base + ws.dpart_off);
     hipError_t e;
     if (!logits_in && moe_route_decode_ok(T, c.n_experts, c.top_k)) {
-        double* dpart = reinterpret_cast<double*>(ws.base + ws.dpart_off);
         e = timed(ctx, MOE_K_ROUTE, s, [&] {
             return moe_launch_route_decode(x, wrT, bias, dpart, T, c.d_model, c.n_experts,
                                            c.top_k, c.expert_begin, c.n_local_experts, tile_rows,
@@ -253,7 +253,7 @@ moe_status do_route(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t* x
     } else {
         if (!logits_in) {
             e = timed(ctx, MOE_K_ROUTER, s, [&] {
-                return moe_launch_router_select(x, wrT, bias, T, c.d_model, c.n_experts,
+                return moe_launch_router_select(x, wrT, bias, dpart, T, c.d_model, c.n_experts,
                                                 c.top_k, policy, &ws.rv, s);
             });
             if (e != hipSuccess) return hip_fail(ctx, e, "router kernel launch");

@@ -210,8 +210,9 @@ hipError_t moe_launch_route_decode(const uint16_t* x, const float* wrT, const fl
                                    double* partial, int T, int d, int E, int k, int e_begin,
                                    int n_local, int tile_rows, const moe::Policy* policy, uint16_t* xq,
                                    const moe::RouteView* rv, hipStream_t s);
-hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT, const float* bias, int T,
-                                   int d, int E, int k, const moe::Policy* policy,
+size_t moe_route_partial_bytes(int max_tokens, int d, int E);
+hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT, const float* bias,
+                                   double* partial, int T, int d, int E, int k, const moe::Policy* policy,
                                    const moe::RouteView* rv, hipStream_t s);
 hipError_t moe_launch_route(const float* logits_in, int T, int E, int k, int e_begin, int n_local,
                             int tile_rows, const moe::Policy* policy, const uint16_t* x, int d,

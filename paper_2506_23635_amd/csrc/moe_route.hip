@@ -10,15 +10,13 @@
 // that every load is 16 bytes.
 //
 // Kernels
-//   router_select_kernel: 8 tokens per workgroup, a wave takes 4 tokens x 8
-//       experts, each dot product split over the 64 lanes and summed by a
-//       fixed transpose-reduce; then each token's selection.
+//   router_kernel (+ sum_select_kernel): logits of many tokens on the fp64 matrix
+//       cores.
 //   route_partials_kernel + route_finish_kernel (T <= 16, E <= 16,
 //       T*k <= 64): partial logits over a few workgroups, then one workgroup
 //       sums them in fixed order, selects and permutes.
 //   route_one_kernel: both in one launch where one workgroup forms the logits
 //       anyway (d <= 512).
-//   router_kernel (more than 16 experts): logits on the fp64 matrix cores.
 //   select_kernel: selection and weights from fp32 logits, router_kernel's or the
 //       caller's.
 //   permute_kernel: the permutation and the list of token tiles.
@@ -513,144 +511,22 @@ __device__ __forceinline__ void finish_route(const DecodeRouteArgs& a, float (&l
     }
 }
 
-// Router and selection for many tokens: 8 tokens per 256-thread workgroup;
-// wave w takes tokens 4(w/2) .. +3 and experts 8(w%2) .. +7 (then +16, ...).
-// Lane l accumulates, in fp64, the 8-element groups l, l + 64, ... of the
-// reduction axis for its 4 tokens x 8 experts, so each router value it
-// loads serves 4 tokens and each x value 8 experts, and a wave reads 512
-// consecutive elements of every row per step (two steps in flight).  A
-// fixed transpose-reduce over the 64 lanes sums the lane partials (32
-// shuffles for the 32 sums); each sum is rounded once to fp32 and the bias
-// added in fp32; then one thread per token selects its experts from the
-// logits in LDS.
-constexpr int kRsTokWave = 4;
-constexpr int kRsExp = 8;
-constexpr int kRsTok = 2 * kRsTokWave;
-constexpr int kRsThreads = 4 * kWave;
-
-template <bool kPolicy>
-__global__ __launch_bounds__(kRsThreads) void router_select_kernel(const uint16_t* __restrict__ x,
-                                                                   const float* __restrict__ wrT,
-                                                                   const float* __restrict__ bias,
-                                                                   int T, int d, int E, int k,
-                                                                   Policy policy, RouteView rv)
-{
-    __shared__ float lg[kRsTok][64];
-    const int wid = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int tg = wid / 2, eh = wid % 2;
-    const int t0 = blockIdx.x * kRsTok + tg * kRsTokWave;
-    for (int e0 = eh * kRsExp; e0 < E; e0 += 2 * kRsExp) {
-        double acc[kRsTokWave][kRsExp];
-#pragma unroll
-        for (int i = 0; i < kRsTokWave; ++i)
-#pragma unroll
-            for (int j = 0; j < kRsExp; ++j) acc[i][j] = 0.0;
-        // tokens past T and experts past E (partial last groups) recompute
-        // token T-1 / expert E-1 so that the loop has no branch; their sums
-        // are dropped
-        const uint16_t* xr[kRsTokWave];
-        const float* wr[kRsExp];
-#pragma unroll
-        for (int i = 0; i < kRsTokWave; ++i) xr[i] = x + (int64_t)min(t0 + i, T - 1) * d;
-#pragma unroll
-        for (int j = 0; j < kRsExp; ++j) wr[j] = wrT + (int64_t)min(e0 + j, E - 1) * d;
-        // two steps of loads in flight: step g + 512 is fetched while step g
-        // computes (a prefetch past d re-reads the lane's current step)
-        struct Step {
-            u32x4_t xv[kRsTokWave];
-            float4 w0[kRsExp], w1[kRsExp];
-        };
-        auto fetch = [&](Step& st, int g) {
-#pragma unroll
-            for (int i = 0; i < kRsTokWave; ++i) st.xv[i] = *reinterpret_cast<const u32x4_t*>(xr[i] + g);
-#pragma unroll
-            for (int j = 0; j < kRsExp; ++j) {
-                st.w0[j] = *reinterpret_cast<const float4*>(wr[j] + g);
-                st.w1[j] = *reinterpret_cast<const float4*>(wr[j] + g + 4);
-            }
-        };
-        auto fma_step = [&](const Step& st) {
-#pragma unroll
-            for (int j = 0; j < kRsExp; ++j)
-#pragma unroll
-                for (int i = 0; i < kRsTokWave; ++i) fma8(acc[i][j], st.xv[i], st.w0[j], st.w1[j]);
-        };
-        constexpr int kStep = kWave * 8;
-        Step s0, s1;
-        int g = lane * 8;
-        if (g < d) fetch(s0, g);
-        for (; g < d; g += 2 * kStep) {
-            const bool more = g + kStep < d;
-            fetch(s1, more ? g + kStep : g);
-            fma_step(s0);
-            if (!more) break;
-            const bool more2 = g + 2 * kStep < d;
-            fetch(s0, more2 ? g + 2 * kStep : g);
-            fma_step(s1);
-        }
-        // transpose-reduce over the 64 lanes: at the step with lane offset o
-        // a lane keeps half of its n values (the upper half if its o bit is
-        // set), sends the other half to lane ^ o and adds what it receives;
-        // after offsets 32..2 each lane holds one value summed over 32 lanes,
-        // and offset 1 completes it.  Value q = 8 i + j ends on the lanes whose
-        // bits 5..1 spell q (bit 5 most significant).  Fixed order.
-        constexpr int kVals = kRsTokWave * kRsExp;   // 32
-        double v[kVals];
-#pragma unroll
-        for (int i = 0; i < kRsTokWave; ++i)
-#pragma unroll
-            for (int j = 0; j < kRsExp; ++j) v[i * kRsExp + j] = acc[i][j];
-#pragma unroll
-        for (int o = kWave / 2, n = kVals; o >= 2; o >>= 1, n >>= 1) {
-            const bool up = (lane & o) != 0;
-#pragma unroll
-            for (int m = 0; m < kVals / 2; ++m) {
-                if (m < n / 2) {
-                    const double send = up ? v[m] : v[m + n / 2];
-                    const double keep = up ? v[m + n / 2] : v[m];
-                    v[m] = keep + __shfl_xor(send, o, kWave);
-                }
-            }
-        }
-        const double total = v[0] + __shfl_xor(v[0], 1, kWave);
-        const int q = ((lane >> 5) & 1) * 16 + ((lane >> 4) & 1) * 8 + ((lane >> 3) & 1) * 4 +
-                      ((lane >> 2) & 1) * 2 + ((lane >> 1) & 1);
-        if ((lane & 1) == 0) {
-            const int i = q / kRsExp, j = q % kRsExp;
-            const int t = t0 + i, e = e0 + j;
-            if (t < T && e < E) {
-                float lv = (float)total;
-                if (bias) lv = __fadd_rn(lv, bias[e]);
-                lg[tg * kRsTokWave + i][e] = lv;
-                rv.logits[(int64_t)t * E + e] = lv;
-            }
-        }
-    }
-    lds_barrier();
-    if constexpr (kPolicy) {
-        for (int i = wid; i < kRsTok; i += kRsThreads / kWave) {
-            const int t = blockIdx.x * kRsTok + i;
-            if (t < T)
-                choose<kWave>(policy, lg[i][min(lane, E - 1)], lane, E, k, rv.topk_idx + (int64_t)t * k,
-                              rv.topk_w + (int64_t)t * k);
-        }
-    } else if (threadIdx.x < kRsTok) {
-        const int t = blockIdx.x * kRsTok + threadIdx.x;
-        if (t < T) select_token_any(&lg[threadIdx.x][0], t, E, k, rv);
-    }
-}
-
-// Logits of more than 16 experts.  A workgroup takes 16 tokens x 16 experts, its
-// 16 waves the 32-element steps of the reduction axis in turn; a wave's step is
-// eight v_mfma_f64_16x16x4_f64, lane l holding eight elements of token l % 16 and of
-// expert l % 16, those from 8 (l / 16) on, and instruction i taking the i-th of
-// all four runs.  The waves' sums meet in LDS and are added in wave order.  Where
-// router_select_kernel spends 96 conversions to fp64 on 256 multiply-adds per lane,
-// this spends 16 on the same; and it has a workgroup for every 16 experts (2048
-// tokens of d 6144, 64 experts: 80 us there, selection included).  A step's loads
-// are issued before the multiplications of the step before.
+// Logits of many tokens, on the fp64 matrix cores.  A workgroup takes 16 tokens
+// (kTiles times) x 16 experts and every n_split-th 512 elements of the reduction
+// axis, its 16 waves 32 of them each; a wave's step is eight v_mfma_f64_16x16x4_f64,
+// lane l holding eight elements of token l % 16 and of expert l % 16, those from 8 (l
+// / 16) on, and instruction i taking the i-th of all four runs.  A step's loads are
+// issued before the multiplications of the step before.  The waves' sums meet in
+// LDS and are added in wave order; with several ranges (few tokens: one workgroup
+// alone multiplies 10 us long at d 6144) they go to the workspace, and
+// sum_select_kernel adds them in order.  Every conversion to fp64 serves 16
+// products; four tokens x eight experts per wave on the vector unit, 64 lanes along
+// the axis and a transpose-reduce at the end, took 17 us for 17 to 500 tokens of d
+// 6144 and 16 experts, 26 for 2048, 92 for 8000, 81 for 2048 and 64 experts.
 constexpr int kRmWaves = 16;
 constexpr int kRmStep = 32;
+constexpr int kRmAxis = kRmWaves * kRmStep;
+constexpr int kRmWg = 256;         // workgroups that n_split aims at: one per CU
 constexpr int kRmManyWg = 512;     // workgroups of 16 tokens from which on they take 32
 typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
@@ -658,7 +534,7 @@ template <int kTiles>              // of 16 tokens
 __global__ __launch_bounds__(64 * kRmWaves) void router_kernel(const uint16_t* __restrict__ x,
                                                                const float* __restrict__ wrT,
                                                                const float* __restrict__ bias, int T, int d, int E,
-                                                               float* __restrict__ logits)
+                                                               float* __restrict__ logits, double* __restrict__ part)
 {
     __shared__ double s_part[kRmWaves][4][64];
     const int tid = threadIdx.x, lane = tid % 64, w = tid / 64;
@@ -691,15 +567,15 @@ __global__ __launch_bounds__(64 * kRmWaves) void router_kernel(const uint16_t* _
                 acc[n] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)xv, (double)wv[i], acc[n], 0, 0, 0);
             }
     };
-    constexpr int kAll = kRmStep * kRmWaves;
+    const int all = kRmAxis * gridDim.z;
     Step s0, s1;
-    int k = w * kRmStep;
+    int k = blockIdx.z * kRmAxis + w * kRmStep;
     if (k < d) fetch(s0, k);
-    for (; k < d; k += 2 * kAll) {
-        fetch(s1, min(k + kAll, d - kRmStep));
+    for (; k < d; k += 2 * all) {
+        fetch(s1, min(k + all, d - kRmStep));
         multiply(s0);
-        if (k + kAll >= d) break;
-        fetch(s0, min(k + 2 * kAll, d - kRmStep));
+        if (k + all >= d) break;
+        fetch(s0, min(k + 2 * all, d - kRmStep));
         multiply(s1);
     }
     // lane l holds tokens l / 16 + 4 i of expert l % 16
@@ -714,12 +590,47 @@ __global__ __launch_bounds__(64 * kRmWaves) void router_kernel(const uint16_t* _
             double v = 0.0;
 #pragma unroll
             for (int q = 0; q < kRmWaves; ++q) v += s_part[q][i][lane];
-            if (t < T && e < E) {
+            if (part) {
+                const int64_t rows = (int64_t)gridDim.x * (16 * kTiles);
+                part[(blockIdx.z * rows + t) * (gridDim.y * 16) + e] = v;
+            } else if (t < T && e < E) {
                 float l = (float)v;
                 if (bias) l = __fadd_rn(l, bias[e]);
                 logits[(int64_t)t * E + e] = l;
             }
         }
+    }
+}
+
+// The logits of router_kernel's ranges (n of them, rows x ld apart), and the
+// selection: one wave per token, lane e its expert e.
+template <bool kPolicy>
+__global__ __launch_bounds__(256) void sum_select_kernel(const double* __restrict__ part, int n, int64_t rows, int ld,
+                                                         const float* __restrict__ bias, int T, int E, int k,
+                                                         Policy policy, RouteView rv)
+{
+    __shared__ float lg[256 / kWave][kWave];
+    const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave, t = blockIdx.x * (256 / kWave) + w;
+    if (t >= T) return;
+    constexpr int kAtOnce = 8;                           // ranges' sums in flight
+    double v = 0.0;
+    for (int z0 = 0; z0 < n; z0 += kAtOnce) {
+        double p[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) p[i] = part[(min(z0 + i, n - 1) * rows + t) * ld + min(lane, E - 1)];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+            if (z0 + i < n) v += p[i];
+    }
+    float l = (float)v;
+    if (bias) l = __fadd_rn(l, bias[min(lane, E - 1)]);
+    if (lane < E) rv.logits[(int64_t)t * E + lane] = l;
+    if constexpr (kPolicy) {
+        choose<kWave>(policy, l, lane, E, k, rv.topk_idx + (int64_t)t * k, rv.topk_w + (int64_t)t * k);
+    } else {
+        lg[w][lane] = l;                                 // (read by the wave that wrote it)
+        __builtin_amdgcn_wave_barrier();
+        if (lane == 0) select_token_any(&lg[w][0], t, E, k, rv);
     }
 }
 
@@ -950,26 +861,41 @@ static hipError_t launch_select(const float* logits, int T, int E, int k, const 
     return hipGetLastError();
 }
 
+// Ranges of the reduction axis that router_kernel takes for T tokens.
+static int router_split(int T, int d, int E)
+{
+    const int64_t wgs = (int64_t)((T + 15) / 16) * ((E + 15) / 16);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(moe::kRmWg / wgs, d / moe::kRmAxis));
+}
+
+// Workspace of the partial logits of up to max_tokens tokens: the decode routing's,
+// and router_kernel's, whose ranges are as many as fit kRmWg workgroups.
+extern "C" size_t moe_route_partial_bytes(int max_tokens, int d, int E)
+{
+    const size_t tiles = (size_t)((max_tokens + 15) / 16) * ((E + 15) / 16) * std::max(1, d / moe::kRmAxis);
+    const size_t few = (size_t)moe_route_decode_wgs(d) * moe::kSmallT * moe::kDecE;
+    return std::max(few, std::min<size_t>(tiles, moe::kRmWg) * 16 * 16) * sizeof(double);
+}
+
 extern "C" hipError_t moe_launch_router_select(const uint16_t* x, const float* wrT,
-                                               const float* bias, int T, int d, int E, int k,
+                                               const float* bias, double* partial, int T, int d, int E, int k,
                                                const moe::Policy* policy,
                                                const moe::RouteView* rv, hipStream_t s)
 {
-    if (E > 16) {
-        const int n_e = (E + 15) / 16, n_t = (T + 15) / 16;
-        if ((int64_t)n_t * n_e >= moe::kRmManyWg)
-            hipLaunchKernelGGL(moe::router_kernel<2>, dim3((n_t + 1) / 2, n_e), dim3(64 * moe::kRmWaves), 0, s, x, wrT, bias,
-                               T, d, E, rv->logits);
-        else
-            hipLaunchKernelGGL(moe::router_kernel<1>, dim3(n_t, n_e), dim3(64 * moe::kRmWaves), 0, s, x, wrT, bias, T, d, E,
-                               rv->logits);
-        const hipError_t e = hipGetLastError();
-        return e != hipSuccess ? e : launch_select(rv->logits, T, E, k, policy, rv, s);
-    }
-    const int grid = (T + moe::kRsTok - 1) / moe::kRsTok;
-    const auto kernel = policy->on ? moe::router_select_kernel<true> : moe::router_select_kernel<false>;
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(moe::kRsThreads), 0, s, x, wrT, bias, T, d, E, k, *policy,
-                       *rv);
+    const int n_e = (E + 15) / 16, n_t = (T + 15) / 16, n = router_split(T, d, E);
+    double* part = n > 1 ? partial : nullptr;
+    if ((int64_t)n_t * n_e >= moe::kRmManyWg)
+        hipLaunchKernelGGL(moe::router_kernel<2>, dim3((n_t + 1) / 2, n_e), dim3(64 * moe::kRmWaves), 0, s, x, wrT, bias, T, d,
+                           E, rv->logits, part);
+    else
+        hipLaunchKernelGGL(moe::router_kernel<1>, dim3(n_t, n_e, n), dim3(64 * moe::kRmWaves), 0, s, x, wrT, bias, T, d, E,
+                           rv->logits, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (!part) return launch_select(rv->logits, T, E, k, policy, rv, s);
+    const auto kernel = policy->on ? moe::sum_select_kernel<true> : moe::sum_select_kernel<false>;
+    hipLaunchKernelGGL(kernel, dim3((T + 3) / 4), dim3(256), 0, s, part, n, (int64_t)n_t * 16, n_e * 16, bias, T, E, k,
+                       *policy, *rv);
     return hipGetLastError();
 }
 
