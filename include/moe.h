@@ -382,7 +382,7 @@ typedef enum { MOE_T_F32 = 0, MOE_T_BF16 = 1 } moe_type;
  * 16-byte aligned); codes [T][n] bytes; scales [T][ceil(n / 128)] bytes, each
  * e + 127 (the biased exponent of 2^e).  n a positive multiple of 16 (at most
  * 2^24), T at most 2^24; T == 0 is a no-op.  Enqueued on stream; allocates
- * nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n), MOE_E_SHAPE (n, T),
+ * nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n or > 2^32), MOE_E_SHAPE (n, T),
  * MOE_E_ALIGN (x, codes, or a stride that is no multiple of 16 bytes). */
 MOE_API moe_status moe_quantize_e4m3(const void *x, int64_t ld, int32_t type, int32_t T, int32_t n,
                                      uint8_t *codes, uint8_t *scales, moe_stream_t stream);
@@ -412,7 +412,8 @@ MOE_API moe_status moe_linear_load(moe_linear *ctx, const uint16_t *w, moe_strea
 
 /* y = Q(x) Q(W) for T rows: x bf16, rows ldx elements apart (16-byte aligned),
  * y [T][out_dim] of `type` (fp32, or rounded once to bf16), contiguous, 16-byte
- * aligned, not overlapping x's elements (MOE_E_ARG).  T == 0 is a no-op.  Errors:
+ * aligned, not overlapping what lies between x's first element and its last
+ * (MOE_E_ARG); ldx from in_dim to 2^32.  T == 0 is a no-op.  Errors:
  * MOE_E_ARG, MOE_E_CAPACITY (T > max_tokens), MOE_E_STATE (not loaded),
  * MOE_E_ALIGN.  Two calls on a context share its workspace: they go to one
  * stream, or the caller orders them. */

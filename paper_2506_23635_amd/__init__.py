@@ -432,16 +432,18 @@ class MoeLayer:
         c, bf = self.cfg, _bf16_types(self.torch)
         on_dev, dev = self._src_device(gate, up, down)
         n = c.d_model * c.ffn_dim
-        moe_load_expert(self.ctx, layer, expert, _tensor_ptr(gate, "gate", n, bf, dev),
-                        _tensor_ptr(up, "up", n, bf, dev), _tensor_ptr(down, "down", n, bf, dev),
-                        int(on_dev), self.stream if on_dev else 0)
+        with _on_device(self.torch, self.device):
+            moe_load_expert(self.ctx, layer, expert, _tensor_ptr(gate, "gate", n, bf, dev),
+                            _tensor_ptr(up, "up", n, bf, dev), _tensor_ptr(down, "down", n, bf, dev),
+                            int(on_dev), self.stream if on_dev else 0)
 
     def load_router(self, layer, wr, bias=None):
         c, f32 = self.cfg, (self.torch.float32,)
         on_dev, dev = self._src_device(wr, bias)
-        moe_load_router(self.ctx, layer, _tensor_ptr(wr, "wr", c.d_model * c.n_experts, f32, dev),
-                        _tensor_ptr(bias, "bias", c.n_experts, f32, dev) if bias is not None else None,
-                        int(on_dev), self.stream if on_dev else 0)
+        with _on_device(self.torch, self.device):
+            moe_load_router(self.ctx, layer, _tensor_ptr(wr, "wr", c.d_model * c.n_experts, f32, dev),
+                            _tensor_ptr(bias, "bias", c.n_experts, f32, dev) if bias is not None else None,
+                            int(on_dev), self.stream if on_dev else 0)
 
     def set_policy(self, layer, policy, balance=None):
         """moe_set_policy: policy from make_policy, or None; balance: fp32 [n_experts] on the
@@ -471,15 +473,17 @@ class MoeLayer:
         xp = _tensor_ptr(x, "x", T * d, _bf16_types(self.torch), self.device) if x is not None else None
         lp = (_tensor_ptr(logits_in, "logits_in", T * E, (self.torch.float32,), self.device)
               if logits_in is not None else None)
-        return moe_route(self.ctx, layer, xp, T, lp, self.stream)
+        with _on_device(self.torch, self.device):
+            return moe_route(self.ctx, layer, xp, T, lp, self.stream)
 
     def forward(self, layer, x, y, routing=None, T=None):
         """y: bf16 [T, d], or fp32 [T, d] when the config has MOE_PARTIAL_F32."""
         T = self._tokens(x, T)
         n, bf = T * self.cfg.d_model, _bf16_types(self.torch)
         ytypes = (self.torch.float32,) if self.cfg.flags & MOE_PARTIAL_F32 else bf
-        moe_forward(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device), T, routing,
-                    _tensor_ptr(y, "y", n, ytypes, self.device), self.stream)
+        with _on_device(self.torch, self.device):
+            moe_forward(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device), T, routing,
+                        _tensor_ptr(y, "y", n, ytypes, self.device), self.stream)
 
     def forward_static(self, layer, x, y, T=None):
         """moe_forward_static: the layer with internal routing on the
@@ -487,27 +491,31 @@ class MoeLayer:
         T = self._tokens(x, T)
         n, bf = T * self.cfg.d_model, _bf16_types(self.torch)
         ytypes = (self.torch.float32,) if self.cfg.flags & MOE_PARTIAL_F32 else bf
-        moe_forward_static(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device), T,
-                           _tensor_ptr(y, "y", n, ytypes, self.device), self.stream)
+        with _on_device(self.torch, self.device):
+            moe_forward_static(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device), T,
+                               _tensor_ptr(y, "y", n, ytypes, self.device), self.stream)
 
     def forward_stack(self, x, T=None):
         T = self._tokens(x, T)
-        moe_forward_stack(self.ctx, _tensor_ptr(x, "x", T * self.cfg.d_model, _bf16_types(self.torch),
-                                                self.device), T, self.stream)
+        with _on_device(self.torch, self.device):
+            moe_forward_stack(self.ctx, _tensor_ptr(x, "x", T * self.cfg.d_model, _bf16_types(self.torch),
+                                                    self.device), T, self.stream)
 
     def forward_residual(self, layer, x, r, T=None):
         """moe_forward_residual: r = bf16(r + bf16(layer(x))) in place."""
         T = self._tokens(x, T)
         n, bf = T * self.cfg.d_model, _bf16_types(self.torch)
-        moe_forward_residual(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device),
-                             _tensor_ptr(r, "r", n, bf, self.device), T, self.stream)
+        with _on_device(self.torch, self.device):
+            moe_forward_residual(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device),
+                                 _tensor_ptr(r, "r", n, bf, self.device), T, self.stream)
 
     def forward_layers(self, first, n, x, T=None):
         """moe_forward_layers: layers first .. first+n-1, x = bf16(x + y) in place."""
         T = self._tokens(x, T)
-        moe_forward_layers(self.ctx, first, n,
-                           _tensor_ptr(x, "x", T * self.cfg.d_model, _bf16_types(self.torch),
-                                       self.device), T, self.stream)
+        with _on_device(self.torch, self.device):
+            moe_forward_layers(self.ctx, first, n,
+                               _tensor_ptr(x, "x", T * self.cfg.d_model, _bf16_types(self.torch),
+                                           self.device), T, self.stream)
 
     def routing_tensors(self, r: MoeRouting):
         """Copies the routing views (device) to host numpy arrays."""

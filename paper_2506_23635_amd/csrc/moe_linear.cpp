@@ -17,6 +17,7 @@ constexpr int kRowTile = 128;           // rows of a tile of a product with rang
 constexpr int kSplitRows = 64;          // ... up to these rows there are always such tiles
 constexpr int kMostSplit = 16384;       // ... and beyond these none has ranges (two feature tiles at least)
 constexpr int kFeatures = 256;          // packed features come in multiples of a tile's
+constexpr int64_t kMostStride = 1ll << 32;   // elements between rows (offsets stay below 2^63)
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -106,7 +107,7 @@ moe_status moe_quantize_e4m3(const void* x, int64_t ld, int32_t type, int32_t T,
     if (T < 0) return MOE_E_ARG;
     if (n < 16 || n % 16 || n > 1 << 24 || T > 1 << 24) return MOE_E_SHAPE;
     if (T == 0) return MOE_OK;
-    if (!x || !codes || !scales || ld < n) return MOE_E_ARG;
+    if (!x || !codes || !scales || ld < n || ld > kMostStride) return MOE_E_ARG;
     const int size = type == MOE_T_F32 ? 4 : 2;
     if (misaligned(x) || misaligned(codes) || (T > 1 && ld % (16 / size))) return MOE_E_ALIGN;
     const hipError_t e = moe_launch_quantize(x, ld, type == MOE_T_BF16, T, nullptr, n, n, codes, scales, nullptr,
@@ -165,7 +166,7 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
     if (!ctx->loaded) return fail(ctx, MOE_E_STATE, "no weights loaded");
     if (T == 0) return MOE_OK;
     if (!x || !y) return fail(ctx, MOE_E_ARG, "x or y is NULL");
-    if (ldx < c.in_dim) return fail(ctx, MOE_E_ARG, "ldx is below in_dim");
+    if (ldx < c.in_dim || ldx > kMostStride) return fail(ctx, MOE_E_ARG, "ldx is below in_dim or above 2^32");
     if (misaligned(x) || misaligned(y) || (T > 1 && ldx % 8))
         return fail(ctx, MOE_E_ALIGN, "x, its rows and y must be 16-byte aligned");
     const uintptr_t x0 = (uintptr_t)x, y0 = (uintptr_t)y;

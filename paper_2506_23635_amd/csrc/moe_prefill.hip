@@ -360,15 +360,16 @@ __device__ __forceinline__ void tile_loop(const TileCtx& c, int n_pairs, uint8_t
 constexpr int kRingH = 6;
 constexpr int kHalfTB = TB / 2;
 
-// With e4m3 weights a stage's refills are four granules and the scale, those of
-// the first granules before the wait.
+// With e4m3 weights a K step's fragments are decoded between the MFMAs of the step
+// before, so a stage's refills, four granules and the scale, all lie before the
+// wait.
 template <int kTB, bool kOnce, bool kE4m3>
 __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16_t (&acc)[FB][kHalfTB])
 {
     using Stage = AStage<kE4m3, FB>;
     constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
     constexpr int kStage = kTB * 32 * BK * 2;
-    constexpr int kAfter = 2 * kTB + (kE4m3 ? 2 * (FB * kLoadsA8 + 1) + FB : 3 * A_FRAGS - FB);
+    constexpr int kAfter = 2 * kTB + (kE4m3 ? 3 * (FB * kLoadsA8 + 1) : 3 * A_FRAGS - FB);
     constexpr int kWait = wait_vm(kAfter);
     static_assert(kAfter < 64, "vmcnt holds 6 bits");
     const int n_stages = c.n_stages, w = c.w;
@@ -391,10 +392,10 @@ __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16
             dst[t] = *reinterpret_cast<const u32x4_t*>(&lds[buf + c.rd_off[j] + t * 32 * (BK * 2)]);
     };
     int cur = 0, prev = (kRingB - 1) * kStage;   // byte offsets of this and the last stage's buffer
-    auto stage = [&](int s, Stage& A) {
+    u32x4_t da[2][FB];                         // kE4m3: decoded fragments of two K steps in turn
+    auto stage = [&](int s, Stage& A, const Stage& after) {
         const int next = cur + kStage == kRingB * kStage ? 0 : cur + kStage;
         const int sa = min(s + kRingH, n_stages - 1);
-        u32x4_t a[FB];
         load_b(min(s + kRingB - 1, n_stages - 1), prev);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -409,16 +410,21 @@ __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16
             }
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int fb = 0; fb < FB; ++fb) a[fb] = a_fragment(A, fb, j);
+            for (int t = 0; t < kTB; ++t) {
 #pragma unroll
-            for (int t = 0; t < kTB; ++t)
+                for (int fb = 0; fb < FB; ++fb)
+                    acc[fb][t] = mfma32x32x16(kE4m3 ? da[j & 1][fb] : A.v[kE4m3 ? 0 : fb * KS + j], bw[j & 1][t], acc[fb][t]);
+                if constexpr (kE4m3) {
+                    if (t < FB) da[(j + 1) & 1][t] = j + 1 < KS ? a_fragment(A, t, j + 1) : a_fragment(after, t, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            // (kE4m3: granule i was decoded last for K step i + 2, a step ago)
+            if (!kE4m3 || j == 1 || j == 2)
 #pragma unroll
-                for (int fb = 0; fb < FB; ++fb) acc[fb][t] = mfma32x32x16(a[fb], bw[j & 1][t], acc[fb][t]);
-            if (!kE4m3 || j >= 2)
-#pragma unroll
-                for (int fb = 0; fb < FB; ++fb) load_a1(sa, fb, kE4m3 ? j - 2 : j, A);
+                for (int fb = 0; fb < FB; ++fb) load_a1(sa, fb, kE4m3 ? j - 1 : j, A);
             if constexpr (kE4m3)
-                if (j + 1 == KS) load_scale(A, c.s_rsrc, c.s_off, (uint32_t)sa);
+                if (j == 2) load_scale(A, c.s_rsrc, c.s_off, (uint32_t)sa);
             __builtin_amdgcn_sched_barrier(0);
         }
         prev = cur;
@@ -439,13 +445,16 @@ __device__ __forceinline__ void half_loop(const TileCtx& c, uint8_t* lds, f32x16
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     read_b(0, 0, bw[0]);
+    if constexpr (kE4m3)
+#pragma unroll
+        for (int fb = 0; fb < FB; ++fb) da[0][fb] = a_fragment(ra[0], fb, 0);
     for (int s = 0; s < n_stages; s += kRingH) {
-        stage(s, ra[0]);
-        if (s + 1 < n_stages) stage(s + 1, ra[1]);
-        if (s + 2 < n_stages) stage(s + 2, ra[2]);
-        if (s + 3 < n_stages) stage(s + 3, ra[3]);
-        if (s + 4 < n_stages) stage(s + 4, ra[4]);
-        if (s + 5 < n_stages) stage(s + 5, ra[5]);
+        stage(s, ra[0], ra[1]);
+        if (s + 1 < n_stages) stage(s + 1, ra[1], ra[2]);
+        if (s + 2 < n_stages) stage(s + 2, ra[2], ra[3]);
+        if (s + 3 < n_stages) stage(s + 3, ra[3], ra[4]);
+        if (s + 4 < n_stages) stage(s + 4, ra[4], ra[5]);
+        if (s + 5 < n_stages) stage(s + 5, ra[5], ra[0]);
     }
     // drain the dummy loads before the epilogue takes the LDS
     __builtin_amdgcn_s_waitcnt(kWaitAll);
@@ -776,10 +785,13 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
         for (int tb = 0; tb < TB; ++tb) acc[fb][tb] = f32x16_t{};
 
     // full tiles take the branch-free loop; an expert's partial last tile
-    // skips the MFMAs of token-block pairs past its last row
-    if (ntb == TB)
+    // skips the MFMAs of token-block pairs past its last row.  (With e4m3 weights
+    // the branches cost more than the MFMAs: 2048 tokens, d 6144, f 10752, gate/up, a
+    // tile of 129 to 192 rows 135 us, of 193 to 255 144, a full one 129; down 230, 248
+    // and 215.)
+    if (kE4m3 || ntb == TB)
         tile_loop<true, kE4m3>(c, TB / 2, lds, acc);
-    else
+    else if constexpr (!kE4m3)
         tile_loop<false, kE4m3>(c, (ntb + 1) / 2, lds, acc);
 
     store_tile<kMode, FB, TB, 4, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
@@ -964,8 +976,8 @@ struct MidCtx {
 // B loads are counted.  B loads past the last stage re-read it into a buffer
 // that no later stage reads.
 //
-// e4m3 weights: a stage's refills are two granules and the scale, the first
-// granule's before the wait.  (Eight stages of both operands on their way, where
+// e4m3 weights: a K step's fragment is decoded between the MFMAs of the step before,
+// so a stage's refills, two granules and the scale, all lie before the wait.  (Eight stages of both operands on their way, where
 // the rows leave room for them, changed nothing.)  With kW = 8 waves (gate/up in e4m3: 256 packed features, so that the
 // workgroup has whole blocks of H) a load of B takes 64 rows: an odd last block
 // loads rows it has already once more.
@@ -976,7 +988,7 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
     constexpr int kLoadsB = (kTB * 4 + kW - 1) / kW;
     constexpr int kStage = kLoadsB * kW * 8 * BK * 2;
-    constexpr int kAfter = 2 * kLoadsB + (kE4m3 ? 2 * (kLoadsA8 + 1) + 1 : 3 * KS - 1);
+    constexpr int kAfter = 2 * kLoadsB + (kE4m3 ? 3 * (kLoadsA8 + 1) : 3 * KS - 1);
     constexpr int kWaitMid = wait_vm(kAfter), kWaitMidTail = wait_vm(2 * kLoadsB);
     const int n_stages = c.n_stages, w = c.w;
     Stage ra[kMidRing];
@@ -999,7 +1011,8 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
             dst[t] = *reinterpret_cast<const u32x4_t*>(&lds[buf + c.rd_off[j] + t * 32 * (BK * 2)]);
     };
     int cur = 0, prev = (kMidRingB - 1) * kStage;   // byte offsets of this and the last stage's buffer
-    auto stage = [&](int s, Stage& A, auto tail) {
+    u32x4_t da[2];                             // kE4m3: decoded fragments of two K steps in turn
+    auto stage = [&](int s, Stage& A, const Stage& after, auto tail) {
         constexpr bool kTail = decltype(tail)::value;
         const int next = cur + kStage == kMidRingB * kStage ? 0 : cur + kStage;
         const int sa = min(s + kMidRing, n_stages - 1);
@@ -1017,12 +1030,18 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
                 read_b(cur, j + 1, bw[(j + 1) & 1]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            const u32x4_t a = a_fragment(A, 0, j);
 #pragma unroll
-            for (int t = 0; t < kTB; ++t) acc[t] = mfma32x32x16(a, bw[j & 1][t], acc[t]);
-            if (!kTail && (!kE4m3 || j >= 2)) load_a1(sa, kE4m3 ? j - 2 : j, A);
+            for (int t = 0; t < kTB; ++t) {
+                acc[t] = mfma32x32x16(kE4m3 ? da[j & 1] : A.v[kE4m3 ? 0 : j], bw[j & 1][t], acc[t]);
+                if constexpr (kE4m3)
+                    if (t == 0) {
+                        da[(j + 1) & 1] = j + 1 < KS ? a_fragment(A, 0, j + 1) : a_fragment(after, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+            if (!kTail && (!kE4m3 || j == 1 || j == 2)) load_a1(sa, kE4m3 ? j - 1 : j, A);
             if constexpr (kE4m3 && !kTail)
-                if (j + 1 == KS) load_scale(A, c.s_rsrc, c.s_off, c.s0 + (uint32_t)sa);
+                if (j == 2) load_scale(A, c.s_rsrc, c.s_off, c.s0 + (uint32_t)sa);
             __builtin_amdgcn_sched_barrier(0);
         }
         prev = cur;
@@ -1042,14 +1061,15 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     read_b(0, 0, bw[0]);
+    if constexpr (kE4m3) da[0] = a_fragment(ra[0], 0, 0);
     int s = 0;
     for (; s + kMidRing <= n_stages; s += kMidRing) {
 #pragma unroll
-        for (int i = 0; i < kMidRing; ++i) stage(s + i, ra[i], std::false_type{});
+        for (int i = 0; i < kMidRing; ++i) stage(s + i, ra[i], ra[(i + 1) % kMidRing], std::false_type{});
     }
 #pragma unroll
     for (int i = 0; i + 1 < kMidRing; ++i)
-        if (s + i < n_stages) stage(s + i, ra[i], std::true_type{});
+        if (s + i < n_stages) stage(s + i, ra[i], ra[i + 1], std::true_type{});
     // drain the dummy B loads before the workgroup's LDS can be handed on
     __builtin_amdgcn_s_waitcnt(kWaitAll);
     __builtin_amdgcn_s_barrier();

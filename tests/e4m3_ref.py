@@ -22,7 +22,8 @@ def bf16_bits(v):
 
 
 def f64(bits):
-    return mi.bf16_bits_to_f32(np.asarray(bits, np.uint16)).astype(np.float64)
+    with np.errstate(invalid="ignore"):          # (NaN of all kinds among the bits)
+        return mi.bf16_bits_to_f32(np.asarray(bits, np.uint16)).astype(np.float64)
 
 
 def exponent(amax):
@@ -126,15 +127,11 @@ def choose(logits, k, score, balance=None, n_groups=1, top_groups=1, best=1, ren
 def permute(ids, first, n_local, E):
     """offsets [E + 1], pair_row [T, k], row_token: rows grouped by local expert, then token."""
     T, k = ids.shape
-    offsets, pair_row, tokens, at = np.zeros(E + 1, np.int64), np.full((T, k), -1), [], 0
-    for e in range(E):
-        offsets[e] = at
-        if first <= e < first + n_local:
-            for t in range(T):
-                for j in range(k):
-                    if ids[t, j] == e:
-                        pair_row[t, j] = at
-                        tokens.append(t)
-                        at += 1
-    offsets[E] = at
-    return offsets, pair_row, np.array(tokens, np.int64)
+    flat = ids.reshape(-1)
+    local = (flat >= first) & (flat < first + n_local)
+    pairs = np.flatnonzero(local)
+    order = pairs[np.argsort(flat[pairs], kind="stable")]
+    pair_row = np.full(T * k, -1)
+    pair_row[order] = np.arange(order.size)
+    counts = np.bincount(flat[pairs], minlength=E)
+    return np.concatenate([[0], np.cumsum(counts)]), pair_row.reshape(T, k), order // k

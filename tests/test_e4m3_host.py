@@ -116,6 +116,7 @@ def test_other_flags_stay_refused(flags):
     ((4096, 64, 0, -1, 64, 8192, 16384), E_ARG), ((None, 64, 0, 4, 64, 8192, 16384), E_ARG),
     ((4096, 64, 0, 4, 64, None, 16384), E_ARG), ((4096, 64, 0, 4, 64, 8192, None), E_ARG),
     ((4096, 63, 0, 4, 64, 8192, 16384), E_ARG),                                                  # ld below n
+    ((4096, 2 ** 32 + 8, 0, 4, 64, 8192, 16384), E_ARG), ((4096, 2 ** 63 - 8, 0, 4, 64, 8192, 16384), E_ARG),
     ((4096, 64, 0, 4, 0, 8192, 16384), E_SHAPE), ((4096, 64, 0, 4, 24, 8192, 16384), E_SHAPE),
     ((4096, 64, 0, 4, (1 << 24) + 16, 8192, 16384), E_SHAPE), ((4096, 64, 0, (1 << 24) + 1, 64, 8192, 16384), E_SHAPE),
     ((4100, 64, 0, 4, 64, 8192, 16384), E_ALIGN), ((4096, 64, 0, 4, 64, 8196, 16384), E_ALIGN),
@@ -167,6 +168,24 @@ def test_linear_calls_refused():
     finally:
         L.moe_linear_destroy(ctx)
     L.moe_linear_destroy(None)
+
+
+@pytest.mark.parametrize("n_in,n_out", [(16, 16), (6144, 8192), (1040, 1488), (6144, 256), (128, 1 << 20), (1 << 20, 256),
+                                        (2048, 33024)])
+def test_linear_workspace_holds_the_ranges_sums(n_in, n_out):
+    """A context for more rows has space for what one for fewer rows has: the sums of the ranges of K
+    are those of the largest such call, not of max_tokens."""
+    K = -(-n_in // 128) * 128
+    need = 0
+    for T in sorted({1, 16, 17, 40, 63, 64, 65, 127, 128, 129, 200, 256, 257, 500, 1000, 1025, 4000, 16384, 16385}):
+        ws = moe.moe_linear_workspace_bytes(moe.make_linear_config(n_in, n_out, max_tokens=T))
+        if ws == 0:                                    # beyond the limit on rows
+            assert T * K * 2 > 2 ** 31 - 1
+            continue
+        rows = (T * K * 2 + 255) // 256 * 256
+        assert ws >= rows
+        need = max(need, ws - rows)
+        assert ws - rows >= need
 
 
 def test_bindings_match_the_header():

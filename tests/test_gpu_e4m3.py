@@ -131,6 +131,8 @@ def check_product(y, x, w, terms, bf16):
 
 SHAPES = [(1, 16, 16), (1, 128, 256), (1, 1040, 1488), (2, 6144, 8192), (3, 144, 272), (15, 512, 48), (16, 2048, 512), (17, 128, 128),
           (31, 784, 1024), (33, 208, 272), (64, 3200, 512), (65, 1040, 1488), (128, 256, 16), (129, 640, 2064), (200, 6144, 1024),
+          # 256 x 256 tiles: two stages of K, whole and partial tiles, an odd number of stages
+          (2100, 16, 4096), (2304, 200 - 8, 4112), (1537, 320, 6000), (2050, 704, 4096), (40, 128, 32784), (300, 256, 32784),
           (255, 272, 784), (256, 512, 256), (257, 128, 1040), (300, 1152, 2304), (513, 144, 528), (700, 2048, 4096), (1025, 6144, 256)]
 
 
@@ -244,6 +246,45 @@ def test_linear_captured(torch, T):
         assert torch.equal(y, eager)
         check_product(y.double().cpu().numpy(), ref.rows(x.double().cpu().numpy())[0], w, 640, False)
     lin.close()
+
+
+@pytest.mark.parametrize("n_in,n_out,T", [(6144, 256, 100), (2048, 512, 300), (4096, 1040, 64), (8192, 48, 17)])
+def test_linear_in_ranges_stays_in_its_workspace(torch, n_in, n_out, T):
+    """Products whose reduction is cut in ranges: the sums' space ends the workspace, rows past T and
+    bytes past the workspace stay as they were, for the largest call and for smaller ones."""
+    cfg = moe.make_linear_config(n_in, n_out, max_tokens=T)
+    n = moe.moe_linear_workspace_bytes(cfg)
+    ws = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    lin = moe.E4m3Linear(cfg, workspace=ws)
+    w = ref.bf16_bits(np.random.default_rng(3).standard_normal((n_in, n_out)) / np.sqrt(n_in))
+    lin.load(dev16(torch, w))
+    bits = ref.bf16_bits(activations(T, n_in))
+    x, _, _ = ref.rows(ref.f64(bits))
+    for rows in (T, T - 3, 17):
+        y = torch.full((rows + 1, n_out), 7.0, dtype=torch.bfloat16, device="cuda")
+        lin.forward(dev16(torch, bits[:rows]), y[:-1])
+        check_product(y[:-1].double().cpu().numpy(), x[:rows], ref.weights(ref.f64(w)), n_in + 4, True)
+        assert bool((y[-1] == 7).all())
+    assert bool((ws[n:] == 0x5A).all())
+    lin.close()
+
+
+def test_layer_stays_in_its_workspace(torch):
+    for T, share in ((16, (0, 4)), (40, (1, 2)), (300, (0, 4))):
+        cfg = moe.make_config(512, 384, 4, 2, expert_begin=share[0], n_local_experts=share[1], max_tokens=T, flags=moe.MOE_E4M3)
+        n, m = moe.moe_workspace_bytes(cfg), moe.moe_weight_bytes(cfg)
+        ws = torch.full((n + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        arena = torch.full((m + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        layer = moe.MoeLayer(cfg, arena=arena, workspace=ws)
+        layer.load_router(0, torch.randn((512, 4)))
+        for e in range(share[0], share[0] + share[1]):
+            layer.load_expert(0, e, *(torch.randn(s, device="cuda").to(torch.bfloat16) for s in ((512, 384), (512, 384), (384, 512))))
+        for rows in (T, min(T, 17), 3, 1):
+            x = torch.randn((rows, 512), device="cuda").to(torch.bfloat16)
+            layer.forward(0, x, torch.empty_like(x))
+        torch.cuda.synchronize()
+        assert bool((ws[n:] == 0x5A).all()) and bool((arena[m:] == 0x5A).all())
+        layer.close()
 
 
 def test_linear_on_another_stream(torch):
@@ -378,6 +419,31 @@ class Layer:
 def test_layer(torch, T, d, f, E, k):
     L = Layer(torch, d, f, E, k, T, seed=T)
     L.run(ref.bf16_bits(activations(T, d, seed=T)))
+    L.layer.close()
+
+
+@pytest.mark.parametrize("T", [17, 70, 130, 260, 400, 900])
+@pytest.mark.parametrize("d,f,E,k", [(256, 128, 4, 2), (512, 384, 8, 2), (768, 640, 3, 1), (256, 896, 2, 2)])
+def test_layer_on_the_large_tiles(torch, T, d, f, E, k):
+    """The 256 x 256 tiles, which smaller calls take while a timeline is recorded: tiles of few, half
+    of and all rows, one to many rounds of their rings, and the same bits as the small tiles."""
+    L = Layer(torch, d, f, E, k, T, seed=T)
+    bits = ref.bf16_bits(activations(T, d, seed=T))
+    small = L.run(bits).clone()
+    stamps = torch.zeros((4, 8), dtype=torch.int64, device="cuda")
+    moe.moe_profile_gemm_timeline(L.layer.ctx, stamps.data_ptr(), None, 4)
+    large = L.run(bits).clone()
+    torch.cuda.synchronize()
+    assert int(stamps.abs().sum()) > 0
+    moe.moe_profile_gemm_timeline(L.layer.ctx, None, None, 0)
+    assert torch.equal(small, large)
+    L.layer.close()
+
+
+def test_layer_that_takes_the_large_tiles(torch):
+    """Enough rows and tiles that the layer chooses them itself."""
+    L = Layer(torch, 256, 2048, 8, 2, 3300, seed=5)
+    L.run(ref.bf16_bits(activations(3300, 256, seed=5)))
     L.layer.close()
 
 

@@ -51,14 +51,15 @@ def set_policy(layer, balance=None, best=1, **kw):
 
 
 # (d, T): one workgroup, partial logits, many tokens
-@pytest.mark.parametrize("d,T", [(256, 1), (256, 3), (512, 16), (768, 1), (1024, 7), (1024, 16), (256, 17), (768, 130)])
-@pytest.mark.parametrize("E,k", [(8, 2), (16, 4), (16, 8)])
+@pytest.mark.parametrize("d,T", [(256, 1), (256, 3), (512, 16), (768, 1), (1024, 7), (1024, 16), (256, 17), (768, 130), (6144, 33),
+                                 (3840, 300)])
+@pytest.mark.parametrize("E,k", [(8, 2), (16, 4), (16, 8), (12, 4), (24, 6), (64, 8)])
 @pytest.mark.parametrize("balanced", [False, True])
 def test_from_x(torch, d, T, E, k, balanced):
     layer, x = make(torch, d, E, k, T, seed=T + E)
     balance = torch.randn(E, generator=torch.Generator().manual_seed(E)).cuda() * 0.2 if balanced else None
     for p in POLICIES:
-        if p.get("top_groups", 1) * E // p.get("n_groups", 1) < k:
+        if E % p.get("n_groups", 1) or p.get("top_groups", 1) * E // p.get("n_groups", 1) < k:
             continue
         set_policy(layer, balance, **p)
         rt = layer.routing_tensors(layer.route(0, x))
@@ -68,7 +69,8 @@ def test_from_x(torch, d, T, E, k, balanced):
 
 @pytest.mark.parametrize("T", [1, 5, 64, 333])
 @pytest.mark.parametrize("E,k,groups,top,best", [(1, 1, 1, 1, 1), (3, 2, 3, 2, 1), (48, 6, 6, 3, 2), (64, 8, 8, 4, 2),
-                                                 (64, 64, 1, 1, 1), (60, 9, 15, 5, 1), (16, 4, 16, 4, 1)])
+                                                 (64, 64, 1, 1, 1), (60, 9, 15, 5, 1), (16, 4, 16, 4, 1),
+                                                 (60, 8, 4, 2, 2), (12, 4, 4, 2, 2), (63, 5, 7, 3, 2)])
 @pytest.mark.parametrize("score", [0, 1, 2])
 def test_given_logits(torch, T, E, k, groups, top, best, score):
     layer, _ = make(torch, 256, E, k, T)
@@ -128,6 +130,37 @@ def test_edges_from_x(torch):
             set_policy(layer, **p)
             check(layer.routing_tensors(layer.route(0, x)), 4, 16, 0, 16, **p)
         layer.close()
+
+
+@pytest.mark.parametrize("T,E,k", [(1100, 64, 8), (3000, 16, 4), (9000, 20, 2)])
+def test_many_tokens(torch, T, E, k):
+    """Several workgroups of the permutation and of every range of the reduction axis, or one range."""
+    layer, x = make(torch, 1536, E, k, T, first=E // 4, local=E // 2)
+    p = dict(score=2, n_groups=4, top_groups=2, best=2, scale=2.5)
+    set_policy(layer, **p)
+    rt = layer.routing_tensors(layer.route(0, x))
+    ids, w = ref.choose(rt["logits"], k, **p)
+    assert np.array_equal(rt["idx"], ids)
+    assert np.all(np.abs(rt["w"] - w) <= np.abs(w) * (2.0 ** -24 + 2.0 ** -40))
+    offsets, pair_row, tokens = ref.permute(ids, E // 4, E // 2, E)
+    assert np.array_equal(rt["offsets"], offsets) and np.array_equal(rt["pair_row"], pair_row)
+    assert np.array_equal(rt["row_token"], tokens) and np.array_equal(rt["counts"], np.diff(offsets))
+    layer.close()
+
+
+@pytest.mark.parametrize("d,T,E", [(256, 1, 64), (6144, 5, 16), (6144, 40, 16), (6144, 40, 64), (4096, 700, 17)])
+def test_logits_are_the_exact_sums_rounded(torch, d, T, E):
+    """fp32 of the exact sum: the fp64 sums' own error, d 2^-53 of the sum of magnitudes, may move one
+    that lies at a border by a step."""
+    layer, x = make(torch, d, E, 1, T, bias=False, seed=7)
+    wr = np.random.default_rng(7).standard_normal((d, E)).astype(np.float32) * 0.1
+    rt = layer.routing_tensors(layer.route(0, x))
+    v = ref.f64(x.cpu().numpy().view(np.uint16))
+    exact = v @ wr.astype(np.float64)
+    slack = 2 * d * 2.0 ** -53 * (np.abs(v) @ np.abs(wr.astype(np.float64)))
+    assert np.all(np.abs(rt["logits"] - exact) <= np.abs(exact) * 2.0 ** -24 + slack)
+    assert np.mean(rt["logits"] == exact.astype(np.float32)) > 0.999
+    layer.close()
 
 
 @pytest.mark.parametrize("T", [4, 40])
