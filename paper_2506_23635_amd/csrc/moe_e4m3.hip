@@ -347,19 +347,20 @@ void moe_pack_e4m3_host(const uint16_t* src, int K, int N, uint8_t* dst, uint8_t
             int e = moe::kExpMin;
             while (e < moe::kExpMax && amax > std::ldexp(448.0, e)) ++e;
             scales[(size_t)(n0 / moe::kBlock) * scale_ld + kb] = (uint8_t)(e + 127);
+            const float inv = std::ldexp(1.f, -e);
             for (int n = 0; n < moe::kBlock; ++n)
                 for (int k = 0; k < moe::kBlock; ++k) {
                     const float x = value(block[(size_t)k * N + n]);
-                    const double v = std::fmin(std::ldexp(std::fabs((double)x), -e), 448.0);
+                    const float v = std::fmin(std::fabs(x) * inv, 448.f);
                     uint8_t c;
                     if (!std::isfinite(x)) {
                         c = 0x7F;
-                    } else if (v < 0x1p-6) {
-                        c = (uint8_t)std::nearbyint(std::ldexp(v, 9));       // 8: the least normal code
+                    } else if (v < 0x1p-6f) {
+                        c = (uint8_t)(v * 512.f + 0x1.8p23f - 0x1.8p23f);    // to nearest even; 8: the least normal code
                     } else {
-                        int x2;
-                        const double f = std::frexp(v, &x2);                  // f in [1/2, 1)
-                        c = (uint8_t)((x2 + 6) * 8 + (int)std::nearbyint(f * 16) - 8);   // 16 carries
+                        uint32_t u;                                          // 20 bits rounded off the mantissa
+                        std::memcpy(&u, &v, 4);
+                        c = (uint8_t)(((u + 0x7FFFFu + (u >> 20 & 1)) >> 20) - ((127 - 7) << 3));
                     }
                     if (std::signbit(x)) c |= 0x80;
                     const size_t rt = (size_t)((n0 + n) / moe::kTileRows) * rt_mul + rt_add;

@@ -23,6 +23,12 @@ constexpr size_t kAlign = 256;
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
+bool overlap(const void* a, size_t na, const void* b, size_t nb)
+{
+    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+    return p < q + nb && q < p + na;
+}
+
 struct Layout {
     int K, N;                           // padded
     size_t scales_off, weight_bytes, parts_off, ws_bytes;
@@ -108,8 +114,12 @@ moe_status moe_quantize_e4m3(const void* x, int64_t ld, int32_t type, int32_t T,
     if (n < 16 || n % 16 || n > 1 << 24 || T > 1 << 24) return MOE_E_SHAPE;
     if (T == 0) return MOE_OK;
     if (!x || !codes || !scales || ld < n || ld > kMostStride) return MOE_E_ARG;
-    const int size = type == MOE_T_F32 ? 4 : 2;
+    const int size = type == MOE_T_F32 ? 4 : 2, blocks = (n + moe::kBlock - 1) / moe::kBlock;
     if (misaligned(x) || misaligned(codes) || (T > 1 && ld % (16 / size))) return MOE_E_ALIGN;
+    const size_t x_bytes = ((size_t)(T - 1) * (size_t)ld + n) * size, c_bytes = (size_t)T * n, s_bytes = (size_t)T * blocks;
+    if (overlap(x, x_bytes, codes, c_bytes) || overlap(x, x_bytes, scales, s_bytes) ||
+        overlap(codes, c_bytes, scales, s_bytes))
+        return MOE_E_ARG;
     const hipError_t e = moe_launch_quantize(x, ld, type == MOE_T_BF16, T, nullptr, n, n, codes, scales, nullptr,
                                              static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MOE_OK : MOE_E_HIP;
@@ -169,10 +179,8 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
     if (ldx < c.in_dim || ldx > kMostStride) return fail(ctx, MOE_E_ARG, "ldx is below in_dim or above 2^32");
     if (misaligned(x) || misaligned(y) || (T > 1 && ldx % 8))
         return fail(ctx, MOE_E_ALIGN, "x, its rows and y must be 16-byte aligned");
-    const uintptr_t x0 = (uintptr_t)x, y0 = (uintptr_t)y;
-    const uintptr_t x1 = x0 + ((uintptr_t)(T - 1) * (uintptr_t)ldx + c.in_dim) * 2;
-    const uintptr_t y1 = y0 + (uintptr_t)T * c.out_dim * (type == MOE_T_F32 ? 4 : 2);
-    if (x0 < y1 && y0 < x1) return fail(ctx, MOE_E_ARG, "y overlaps x");
+    if (overlap(x, ((size_t)(T - 1) * (size_t)ldx + c.in_dim) * 2, y, (size_t)T * c.out_dim * (type == MOE_T_F32 ? 4 : 2)))
+        return fail(ctx, MOE_E_ARG, "y overlaps x");
     hipStream_t s = static_cast<hipStream_t>(stream);
     uint16_t* xq = reinterpret_cast<uint16_t*>(ctx->workspace);
     const bool raw = moe_e4m3_linear_raw(T, ctx->L.K);

@@ -167,7 +167,8 @@ __device__ __forceinline__ void choose(const Policy& p, float logit, int e, int 
             for (int q0 = 0; q0 < E; q0 += kAtOnce)
 #pragma unroll
                 for (int q = q0; q < q0 + kAtOnce; ++q) {
-                    const double v = q >= g * n && q < g * n + n ? from_lane<W>(c, q) : -INFINITY;
+                    const double cq = from_lane<W>(c, q);
+                    const double v = q >= g * n && q < g * n + n ? cq : -INFINITY;
                     b2 = fmax(b2, fmin(b1, v));
                     b1 = fmax(b1, v);
                 }

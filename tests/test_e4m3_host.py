@@ -121,6 +121,9 @@ def test_other_flags_stay_refused(flags):
     ((4096, 64, 0, 4, (1 << 24) + 16, 8192, 16384), E_SHAPE), ((4096, 64, 0, (1 << 24) + 1, 64, 8192, 16384), E_SHAPE),
     ((4100, 64, 0, 4, 64, 8192, 16384), E_ALIGN), ((4096, 64, 0, 4, 64, 8196, 16384), E_ALIGN),
     ((4096, 66, 0, 4, 64, 8192, 16384), E_ALIGN), ((4096, 68, 1, 4, 64, 8192, 16384), E_ALIGN),  # rows
+    ((4096, 64, 0, 4, 64, 4096 + 1008, 16384), E_ARG), ((8192, 64, 0, 4, 64, 8192 - 16, 16384), E_ARG),   # overlaps
+    ((4096, 64, 0, 4, 64, 8192, 4100), E_ARG), ((4096, 64, 0, 4, 64, 8192, 8192 + 255), E_ARG),
+    ((4096, 96, 0, 4, 64, 4096 + 256, 16384), E_ARG),                                            # between x's rows
     ((None, 0, 1, 0, 64, None, None), 0),                                                        # nothing to do
 ], ids=str)
 def test_quantize_arguments(args, status):
