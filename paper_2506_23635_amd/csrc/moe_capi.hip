@@ -385,7 +385,7 @@ moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t
         const bool timeline = ctx->tl_gateup || ctx->tl_down;
         const auto mid_tiles = e4m3 ? moe_gemm_mid_tiles_e4m3 : moe_gemm_mid_tiles;
         a.mid = !timeline && mid_tiles(T, c.top_k, c.n_experts, c.n_local_experts, 2 * c.ffn_dim);
-        a.mid_rows = moe_gemm_mid_rows(T, c.top_k, c.n_experts, c.n_local_experts, 2 * c.ffn_dim, 1, 1);
+        a.mid_rows = moe_gemm_mid_rows(T, c.top_k, c.n_experts, c.n_local_experts, 2 * c.ffn_dim, 1, 2);
         a.scales = e4m3 ? experts + ctx->L.sg_off : nullptr;
         a.stamps = ctx->tl_gateup;
         e = timed(ctx, MOE_K_GEMM_GATEUP, s, [&] { return moe_launch_gemm_gateup(&a, s); });
@@ -393,7 +393,8 @@ moe_status run_experts(moe_ctx* ctx, const WsView& ws, int layer, const uint16_t
         a.scales = e4m3 ? experts + ctx->L.sd_off : nullptr;
         a.stamps = ctx->tl_down;
         a.mid = !timeline && mid_tiles(T, c.top_k, c.n_experts, c.n_local_experts, c.d_model);
-        a.mid_rows = moe_gemm_mid_rows(T, c.top_k, c.n_experts, c.n_local_experts, c.d_model, 1, 0);
+        a.mid_blocks = moe_gemm_mid_blocks(T, c.top_k, c.n_experts, c.n_local_experts, c.d_model);
+        a.mid_rows = moe_gemm_mid_rows(T, c.top_k, c.n_experts, c.n_local_experts, c.d_model, 1, a.mid_blocks);
         e = timed(ctx, MOE_K_GEMM_DOWN, s, [&] { return moe_launch_gemm_down(&a, s); });
         if (e != hipSuccess) return hip_fail(ctx, e, "grouped GEMM down kernel launch");
     }

@@ -141,7 +141,8 @@ struct GemmArgs {
     int T;                    // tokens of the call (rows of x)
     int max_rows;             // most rows the call can have
     int mid;                  // take the 128 x 128 tiles, where
-    int mid_rows;             // ... (e4m3) with 32, 64 or 128 token rows, and ...
+    int mid_rows;             // ... (e4m3) with 32, 64 or 128 token rows, ...
+    int mid_blocks;           // ... (kDown, e4m3) with 1 or 2 times 128 features, and ...
     int k_split;              // ... the reduction of a kDown is cut in k_split ranges, ...
     uint64_t split_stride;    // ... range i's sums at O + i * split_stride
     // the attention block's products (O: their fp32 values)
@@ -229,7 +230,8 @@ int moe_prefill_tile_rows();
 int moe_gemm_mid_tiles(int T, int k, int E, int n_local, int M);
 int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M);
 int moe_gemm_linear_split(int T, int K, int M);
-int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int gateup);
+int moe_gemm_mid_blocks(int T, int k, int E, int n_local, int M);
+int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int n_blocks);
 int moe_gemm_plain_split(int T, int M);
 hipError_t moe_launch_combine(const float* O, const int32_t* pair_row, const float* topk_w, int T,
                               int d, int k, uint16_t* y, float* y32, uint16_t* x_residual,

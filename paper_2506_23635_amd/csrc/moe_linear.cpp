@@ -217,7 +217,7 @@ moe_status moe_linear_forward(moe_linear* ctx, const uint16_t* x, int64_t ldx, v
         a.T = a.max_rows = T;
         a.mid = moe_gemm_mid_tiles(T, 1, 1, 1, ctx->L.N);
         a.k_split = n_split(ctx->L, T);
-        a.mid_rows = moe_gemm_mid_rows(T, 1, 1, 1, ctx->L.N, a.k_split, 0);
+        a.mid_rows = moe_gemm_mid_rows(T, 1, 1, 1, ctx->L.N, a.k_split, 1);
         if (a.k_split > 1) {
             a.O = reinterpret_cast<float*>(ctx->workspace + ctx->L.parts_off);
             a.split_stride = (uint64_t)T * c.out_dim;

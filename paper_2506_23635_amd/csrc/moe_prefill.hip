@@ -472,7 +472,7 @@ __device__ __forceinline__ void lds_barrier()
     asm volatile("" ::: "memory");
 }
 
-// The end of a tile: kBlocks 32-feature blocks per wave (kW waves, wave w
+// The end of a tile: kBlocks 32-feature blocks per wave (four waves, wave w
 // from row tile rt0 + 2 kBlocks w on) of up to kTBs 32-token blocks, token
 // rows row_start .. row_end - 1.  In a block the lane holds token lane % 32
 // and features 8g + 4 (lane / 32) + r in register 4g + r (g, r = 0..3).
@@ -497,13 +497,12 @@ __device__ __forceinline__ void lds_barrier()
 //           their "pairs" are 8 features apart and stay unrotated.
 //  kOut     o (fp32) and y = bf16(x + o) (x and y may be the same array)
 //  kLinear  y fp32 or bf16, features below n_out
-template <int kMode, int kBlocks, int kTBs, int kW, bool kE4m3>
+template <int kMode, int kBlocks, int kTBs, bool kE4m3>
 __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x16_t (&acc)[kBlocks][kTBs],
                                            uint8_t* lds, int rt0, int row_start, int row_end, int w,
                                            int lane, int split)
 {
-    constexpr int kThreads = 64 * kW;
-    constexpr int kFeat = kW * kBlocks * 32;  // features of the workgroup
+    constexpr int kFeat = 4 * kBlocks * 32;   // features of the workgroup
     const int half = lane >> 5, c = lane & 31, tid = w * 64 + lane;
     const int rows = row_end - row_start;
     if constexpr (kMode == kGateUp) {
@@ -540,7 +539,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x16_t (&a
                 lds_barrier();
                 m = 0;
 #pragma unroll
-                for (int i = 0; i < kW; ++i) m = max(m, s_max[i * (kTBs * 32) + t * 32 + c]);
+                for (int i = 0; i < 4; ++i) m = max(m, s_max[i * (kTBs * 32) + t * 32 + c]);
                 const int e = scale_exponent(__uint_as_float(m));
                 const float inv = exp2i(-e), scale = exp2i(e);
 #pragma unroll
@@ -775,7 +774,7 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
             once ? half_loop<2, true, kE4m3>(c, lds, acc) : half_loop<2, false, kE4m3>(c, lds, acc);
         else
             once ? half_loop<4, true, kE4m3>(c, lds, acc) : half_loop<4, false, kE4m3>(c, lds, acc);
-        store_tile<kMode, FB, kHalfTB, 4, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
+        store_tile<kMode, FB, kHalfTB, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
         return;
     }
     f32x16_t acc[FB][TB];
@@ -794,7 +793,7 @@ __device__ __forceinline__ void process_tile(const GemmArgs& a, int e, int row_s
     else if constexpr (!kE4m3)
         tile_loop<false, kE4m3>(c, (ntb + 1) / 2, lds, acc);
 
-    store_tile<kMode, FB, TB, 4, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
+    store_tile<kMode, FB, TB, kE4m3>(a, acc, lds, ft * (BM / 16), row_start, row_end, w, lane, 0);
 }
 
 // Measurement only (a.stamps, set by moe_profile_gemm_timeline): workgroup
@@ -956,7 +955,7 @@ constexpr int kMidRingB = 4;       // B stages in LDS
 struct MidCtx {
     __amdgpu_buffer_rsrc_t a_rsrc, b_rsrc, s_rsrc;
     uint32_t s_off;            // kE4m3: this lane's offset of the weights' scales
-    uint32_t a_off;            // this lane's A byte offset at the first stage
+    uint32_t a_off[FB];        // this lane's A byte offset per feature block at the first stage
     uint32_t b_off[kMidTB];    // byte offsets in b_rsrc of this lane's 16-byte chunk, per load
     uint32_t rd_off[KS];       // LDS byte offsets of this lane's B fragment piece, per K step
     int n_stages, w;
@@ -977,31 +976,32 @@ struct MidCtx {
 // that no later stage reads.
 //
 // e4m3 weights: a K step's fragment is decoded between the MFMAs of the step before,
-// so a stage's refills, two granules and the scale, all lie before the wait.  (Eight stages of both operands on their way, where
-// the rows leave room for them, changed nothing.)  With kW = 8 waves (gate/up in e4m3: 256 packed features, so that the
-// workgroup has whole blocks of H) a load of B takes 64 rows: an odd last block
-// loads rows it has already once more.
-template <int kTB, bool kOnce, bool kE4m3, int kW>
-__device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kMidTB])
+// so a stage's refills, two granules and the scale per feature block, all lie before
+// the wait.  (Eight stages of both operands on their way, where the rows leave room
+// for them, changed nothing.)
+template <int kTB, bool kOnce, bool kE4m3, int kFB, int kMax>
+__device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kFB][kMax])
 {
-    using Stage = AStage<kE4m3, 1>;
+    static_assert(kE4m3 || kFB == 1, "bf16 tiles have one feature block per wave");
+    using Stage = AStage<kE4m3, kFB>;
     constexpr int kLoadsA = kE4m3 ? kLoadsA8 : KS;
-    constexpr int kLoadsB = (kTB * 4 + kW - 1) / kW;
-    constexpr int kStage = kLoadsB * kW * 8 * BK * 2;
-    constexpr int kAfter = 2 * kLoadsB + (kE4m3 ? 3 * (kLoadsA8 + 1) : 3 * KS - 1);
-    constexpr int kWaitMid = wait_vm(kAfter), kWaitMidTail = wait_vm(2 * kLoadsB);
+    constexpr int kStage = kTB * 32 * BK * 2;
+    constexpr int kAfter = 2 * kTB + (kE4m3 ? 3 * (kFB * kLoadsA8 + 1) : 3 * KS - 1);
+    constexpr int kWaitMid = wait_vm(kAfter), kWaitMidTail = wait_vm(2 * kTB);
     const int n_stages = c.n_stages, w = c.w;
     Stage ra[kMidRing];
     auto load_a1 = [&](int s, int i, Stage& dst) {
-        load_a<kE4m3, 1, kOnce ? kNonTemporal : 0>(dst, c.a_rsrc, c.a_off, 0, i, c.s0 + (uint32_t)s);
+#pragma unroll
+        for (int fb = 0; fb < kFB; ++fb)
+            load_a<kE4m3, kFB, kOnce ? kNonTemporal : 0>(dst, c.a_rsrc, c.a_off[fb], fb, i, c.s0 + (uint32_t)s);
     };
-    // load q of wave w: rows 8 (kW q + w) .. + 7, whole 128-byte lines
+    // load q of wave w: rows 32 q + 8 w .. + 7, whole 128-byte lines
     auto load_b = [&](int s, int buf) {
 #pragma unroll
-        for (int q = 0; q < kLoadsB; ++q)
+        for (int q = 0; q < kTB; ++q)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 c.b_rsrc,
-                (__attribute__((address_space(3))) void*)(&lds[buf + (q * kW + w) * kTileBytes]),
+                (__attribute__((address_space(3))) void*)(&lds[buf + (q * 4 + w) * kTileBytes]),
                 16, c.b_off[q], (c.s0 + (uint32_t)s) * (BK * 2), 0, 0);
     };
     u32x4_t bw[2][kTB];                        // B fragments of two K steps in turn
@@ -1011,7 +1011,7 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
             dst[t] = *reinterpret_cast<const u32x4_t*>(&lds[buf + c.rd_off[j] + t * 32 * (BK * 2)]);
     };
     int cur = 0, prev = (kMidRingB - 1) * kStage;   // byte offsets of this and the last stage's buffer
-    u32x4_t da[2];                             // kE4m3: decoded fragments of two K steps in turn
+    u32x4_t da[2][kFB];                        // kE4m3: decoded fragments of two K steps in turn
     auto stage = [&](int s, Stage& A, const Stage& after, auto tail) {
         constexpr bool kTail = decltype(tail)::value;
         const int next = cur + kStage == kMidRingB * kStage ? 0 : cur + kStage;
@@ -1032,12 +1032,16 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < kTB; ++t) {
-                acc[t] = mfma32x32x16(kE4m3 ? da[j & 1] : A.v[kE4m3 ? 0 : j], bw[j & 1][t], acc[t]);
-                if constexpr (kE4m3)
-                    if (t == 0) {
-                        da[(j + 1) & 1] = j + 1 < KS ? a_fragment(A, 0, j + 1) : a_fragment(after, 0, 0);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+#pragma unroll
+                for (int fb = 0; fb < kFB; ++fb)
+                    acc[fb][t] = mfma32x32x16(kE4m3 ? da[j & 1][fb] : A.v[kE4m3 ? 0 : j], bw[j & 1][t], acc[fb][t]);
+                if constexpr (kE4m3) {
+#pragma unroll
+                    for (int fb = 0; fb < kFB; ++fb)
+                        if (t == min(fb, kTB - 1))
+                            da[(j + 1) & 1][fb] = j + 1 < KS ? a_fragment(A, fb, j + 1) : a_fragment(after, fb, 0);
+                    if (t < kFB) __builtin_amdgcn_sched_barrier(0);
+                }
             }
             if (!kTail && (!kE4m3 || j == 1 || j == 2)) load_a1(sa, kE4m3 ? j - 1 : j, A);
             if constexpr (kE4m3 && !kTail)
@@ -1061,7 +1065,9 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     read_b(0, 0, bw[0]);
-    if constexpr (kE4m3) da[0] = a_fragment(ra[0], 0, 0);
+    if constexpr (kE4m3)
+#pragma unroll
+        for (int fb = 0; fb < kFB; ++fb) da[0][fb] = a_fragment(ra[0], fb, 0);
     int s = 0;
     for (; s + kMidRing <= n_stages; s += kMidRing) {
 #pragma unroll
@@ -1075,29 +1081,36 @@ __device__ __forceinline__ void mid_loop(const MidCtx& c, uint8_t* lds, f32x16_t
     __builtin_amdgcn_s_barrier();
 }
 
-template <bool kOnce, bool kE4m3, int kW>
-__device__ __forceinline__ void mid_loop_any(int tb, const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kMidTB])
+template <bool kOnce, bool kE4m3, int kFB, int kMax>
+__device__ __forceinline__ void mid_loop_any(int tb, const MidCtx& c, uint8_t* lds, f32x16_t (&acc)[kFB][kMax])
 {
     if (tb == 1)
-        mid_loop<1, kOnce, kE4m3, kW>(c, lds, acc);
-    else if (tb == 2)
-        mid_loop<2, kOnce, kE4m3, kW>(c, lds, acc);
-    else if (tb == 3)
-        mid_loop<3, kOnce, kE4m3, kW>(c, lds, acc);
-    else
-        mid_loop<4, kOnce, kE4m3, kW>(c, lds, acc);
+        mid_loop<1, kOnce, kE4m3, kFB>(c, lds, acc);
+    else if (tb == 2 || kMax == 2)
+        mid_loop<2, kOnce, kE4m3, kFB>(c, lds, acc);
+    else if constexpr (kMax > 2) {
+        if (tb == 3)
+            mid_loop<3, kOnce, kE4m3, kFB>(c, lds, acc);
+        else
+            mid_loop<4, kOnce, kE4m3, kFB>(c, lds, acc);
+    }
 }
 
-// waves of a workgroup on these tiles, each 32 packed features
-template <int kMode, bool kE4m3>
-constexpr int kMidWaves = kMode == kGateUp && kE4m3 ? 8 : 4;
-
-template <int kMode, bool kE4m3>
-__global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_kernel(GemmArgs a)
+// kFB: 32-feature blocks per wave.  Two, and 64 token rows at most, only for e4m3: for
+// gate/up, whose workgroup then has whole blocks of H (eight waves of one block and 128
+// rows, one workgroup per CU, need the barrier of all eight in every stage; whole
+// layer, those -> these: 8 experts of d 1024, f 2048, top-2, 2000 tokens 97.1 -> 88.5
+// us; 32 of d 2048, f 4096, top-4, 300 tokens 191 -> 179; 16 of d 6144, f 10752, top-4,
+// 64 tokens 532 -> 527, but 350 tokens, where 64 rows read some experts'
+// weights twice, 753 -> 797), and for down where moe_gemm_mid_blocks says so.
+template <int kMode, bool kE4m3, int kFB>
+__global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
 {
-    constexpr int kW = kMidWaves<kMode, kE4m3>;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[kMidRingB * MBN * BK * 2];
-    const int n_ftiles = (kMode == kGateUp ? 2 * a.f : a.d) / (32 * kW);
+    constexpr int kFeat = kFB * MBM, kMax = kMidTB / kFB, MBN = 32 * kMax;
+    constexpr int kStore = kMode == kGateUp ? MBN * (kFeat + 16) + (kE4m3 ? 4 * MBN * 4 : 0) : 2 * 32 * (kFeat * 4 + 16);
+    constexpr int kRings = kMidRingB * MBN * BK * 2;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[kRings > kStore ? kRings : kStore];
+    const int n_ftiles = (kMode == kGateUp ? 2 * a.f : a.d) / kFeat;
     const TilePos tp = find_tile(a, blockIdx.x, n_ftiles * a.k_split, kE4m3 ? a.mid_rows : MBN);
     if (tp.el < 0) return;
     const int split = tp.ft / n_ftiles, ft = tp.ft % n_ftiles;
@@ -1119,12 +1132,16 @@ __global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_ke
     const int w = c.w, n_all = K / BK;
     c.s0 = (uint32_t)(n_all * split / a.k_split);
     c.n_stages = n_all * (split + 1) / a.k_split - (int)c.s0;
-    const uint64_t rt = (uint64_t)ft * (2 * kW) + w * 2;   // the wave's two 16-row weight tiles
+    const uint64_t rt = (uint64_t)ft * (kFeat / 16) + w * (2 * kFB);   // the wave's first 16-row weight tile
     const uint64_t slab_bytes = kMode == kGateUp ? a.gu_bytes : a.expert_bytes - a.gu_bytes;
     c.a_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(wbase), 0, (int)slab_bytes,
                                                  kBufferFlags);
-    c.a_off = (uint32_t)(kE4m3 ? tile_offset8(rt + ((lane & 31) >> 4), 0, KT) : tile_offset(rt + ((lane & 31) >> 4), 0, KT)) +
-              (uint32_t)(((lane >> 5) * 16) + (lane & 15)) * 16;
+#pragma unroll
+    for (int fb = 0; fb < kFB; ++fb) {
+        const uint64_t r = rt + 2 * fb + ((lane & 31) >> 4);
+        c.a_off[fb] = (uint32_t)(kE4m3 ? tile_offset8(r, 0, KT) : tile_offset(r, 0, KT)) +
+                      (uint32_t)(((lane >> 5) * 16) + (lane & 15)) * 16;
+    }
     if constexpr (kE4m3) c.s_off = scale_offset<kMode>(a, e, K, (int)rt, lane, c.s_rsrc);
     if (kMode == kGateUp)
         c.b_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x), 0,
@@ -1133,8 +1150,8 @@ __global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_ke
         c.b_rsrc = __builtin_amdgcn_make_buffer_rsrc(a.H + (int64_t)row_start * a.f, 0,
                                                      (row_end - row_start) * a.f * 2, kBufferFlags);
 #pragma unroll
-    for (int q = 0; q < kMidTB * 4 / kW; ++q) {
-        const int R = (q * kW + w) * 8 + (lane >> 3);
+    for (int q = 0; q < kMax; ++q) {
+        const int R = q * 32 + w * 8 + (lane >> 3);
         const int row = row_start + R;
         const int rr = row < row_end ? row : row_start;   // rows past the end: any valid row
         const uint32_t chunk = (uint32_t)((lane & 7) ^ b_swizzle(R)) * 16;
@@ -1148,15 +1165,17 @@ __global__ __launch_bounds__((64 * kMidWaves<kMode, kE4m3>), 2) void gemm_mid_ke
         const int R = lane & 31;
         c.rd_off[j] = (uint32_t)R * (BK * 2) + (uint32_t)(((2 * j + (lane >> 5)) ^ b_swizzle(R)) * 16);
     }
-    f32x16_t acc[1][kMidTB];
+    f32x16_t acc[kFB][kMax];
 #pragma unroll
-    for (int t = 0; t < kMidTB; ++t) acc[0][t] = f32x16_t{};
+    for (int fb = 0; fb < kFB; ++fb)
+#pragma unroll
+        for (int t = 0; t < kMax; ++t) acc[fb][t] = f32x16_t{};
     if (tp.n_sub == 1)
-        mid_loop_any<true, kE4m3, kW>(tb, c, lds, acc[0]);
+        mid_loop_any<true, kE4m3, kFB>(tb, c, lds, acc);
     else
-        mid_loop_any<false, kE4m3, kW>(tb, c, lds, acc[0]);
+        mid_loop_any<false, kE4m3, kFB>(tb, c, lds, acc);
 
-    store_tile<kMode, 1, kMidTB, kW, kE4m3>(a, acc, lds, ft * (2 * kW), row_start, row_end, w, lane, split);
+    store_tile<kMode, kFB, kMax, kE4m3>(a, acc, lds, ft * (kFeat / 16), row_start, row_end, w, lane, split);
 }
 
 }  // namespace moe
@@ -1187,38 +1206,52 @@ int moe_gemm_mid_tiles(int T, int k, int E, int n_local, int M)
     return (int64_t)(M / moe::BM) * n_local * ((rows + moe::BN - 1) / moe::BN) <= 128;
 }
 
-// The same for experts in e4m3.  Half of the weight bytes leave the 256 x 256
-// tiles, one workgroup per CU, more exposed: their partial tiles and uneven last
-// round cost until an expert has 180 rows, or, with few tiles, 400 (whole layer, 256
-// x 256 tiles -> 128 x 128; d 6144, f 10752, 16 experts, top-4: 200 tokens 671 -> 630
-// us, 512 1109 -> 996, 700 (175 rows, 1344 tiles) 1284 -> 1220, 800 1341 -> 1350;
-// 4 of the 16: 700 tokens 446 -> 351, 1400 (350 rows, 672 tiles) 588 -> 540, 2000
-// (500) 658 -> 727; 8 experts, top-2, d 1024, f 2048: 2000 tokens (500 rows, 256
-// tiles) 121 -> 105, 3000 139 -> 138; 16 of d 4096, f 2048, top-4: 1700 tokens 294 ->
-// 263; 32 of d 2048, f 4096, top-4: 2000 tokens (250 rows, 1024 tiles) 496 -> 502).
+// The same for experts in e4m3.  Half of the weight bytes leave the 256 x 256 tiles,
+// one workgroup per CU, more exposed: their partial tiles and uneven last round cost
+// until an expert has 180 rows, or, with few tiles, 400, or, with two per CU, at all
+// (whole layer, 256 x 256 tiles -> the small ones for both products; d 6144, f 10752,
+// 16 experts, top-4: 512 tokens 1037 -> 969 us, 700 (175 rows, 1344 tiles) 1240 ->
+// 1171, 800 1257 -> 1312; 4 of the 16: 700 tokens 446 -> 322, 1400 (350 rows, 672
+// tiles) 568 -> 476, 2000 (500) 636 -> 652; 8 experts, top-2, d 1024, f 2048: 2000
+// tokens (500 rows, 256 tiles) 117 -> 88, 4000 (1000, 512) 152 -> 140; 16 of d 4096, f
+// 2048, top-2: 1700 tokens 277 -> 220; 32 of d 2048, f 4096, top-4: 2000 tokens (250
+// rows, 1024 tiles) 480 -> 447, 3000 (375, 2048) 618 -> 625).
 int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M)
 {
     const int64_t rows = ((int64_t)T * k + E - 1) / E;
     const int64_t tiles = (int64_t)(M / moe::BM) * n_local * ((rows + moe::BN - 1) / moe::BN);
-    return rows <= 176 || tiles <= (rows <= 400 ? 768 : 384);
+    return rows <= 176 || tiles <= (rows <= 400 ? 1024 : 512);
 }
 
-// Token rows of these tiles on e4m3 weights of M packed features per expert, n_split
-// ranges of K: 32 where that leaves one workgroup per CU at most, 64 up to as many as
-// run at once (gate/up's have twice the waves: one per CU, the others two).  The
-// shorter tiles' stages take less time each, where there are too few tiles for the
-// CUs to hide it (a plain product, 32 / 64 / 128 rows: 1040 to 1488 features, 12
-// tiles, 333 tokens 10.2 / 11.8 / 15.8 us, 1024 tokens 14.3 / 14.3 / 18.1, 2048 22.3 /
-// 20.3 / 21.2; 4096 to 4096, two ranges, 200 tokens 24.4 / 21.3 / 22.6; 512 to 2048,
-// 2048 tokens 16.9 / 14.7 / 15.6).
-// (Whole layer, 128 rows -> these, 8 experts, top-2, d 1024, f 2048: 300 tokens 51.6 ->
-// 40.4 us; with 64 rows for gate/up at 1000 tokens, 512 workgroups, 66.4 -> 71.4.)
-int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int gateup)
+// 128-feature halves of these tiles for the down product of experts in e4m3: two
+// (256 features of 64 token rows) where three quarters of the CUs' workgroups have one
+// and the rows fill them, else one (128 of up to 128).  A B fragment is read from LDS
+// once for two MFMAs (whole layer, one -> two: d 6144, f 10752, 16 experts, top-4, 384
+// tiles of 64 rows and more: 200 tokens 629 -> 613 us, 512 1038 -> 987, 1000 1705 ->
+// 1582; 64 tokens, 16 rows per expert, 527 -> 533; 4 of the 16: 700 tokens, 288 tiles,
+// 322 -> 335, 1000, 384 tiles, 394 -> 405, 1400, 576 tiles, 506 -> 472; 32 of d 1536,
+// 1025 tokens, 384 tiles, 92.7 -> 80.3; 8 of d 1024, 100 tokens, 32 tiles, 37.0 ->
+// 41.5).
+int moe_gemm_mid_blocks(int T, int k, int E, int n_local, int M)
 {
-    const int waves = gateup ? moe::kMidWaves<moe::kGateUp, true> : moe::kMidWaves<moe::kDown, true>;
-    const int64_t rows = ((int64_t)T * k + E - 1) / E, per_row_tile = (int64_t)n_local * (M / (32 * waves)) * n_split;
+    const int64_t rows = ((int64_t)T * k + E - 1) / E;
+    const int64_t tiles = (int64_t)n_local * (M / (2 * moe::MBM)) * ((rows + 63) / 64);
+    return rows > 32 && tiles >= 384 ? 2 : 1;
+}
+
+// Token rows of these tiles, n_blocks x 128 features, on e4m3 weights of M packed
+// features per expert, n_split ranges of K: 32 where that leaves one workgroup per CU
+// at most, 64 up to as many as run at once, two per CU.  The shorter tiles' stages take
+// less time each, where there are too few tiles for the CUs to hide it (a plain
+// product, 32 / 64 / 128 rows: 1040 to 1488 features, 12 tiles, 333 tokens 10.2 / 11.8
+// / 15.8 us, 1024 tokens 14.3 / 14.3 / 18.1, 2048 22.3 / 20.3 / 21.2; 4096 to 4096, two
+// ranges, 200 tokens 24.4 / 21.3 / 22.6; 512 to 2048, 2048 tokens 16.9 / 14.7 / 15.6).
+int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int n_blocks)
+{
+    const int64_t rows = ((int64_t)T * k + E - 1) / E;
+    const int64_t per_row_tile = (int64_t)n_local * (M / (moe::MBM * n_blocks)) * n_split;
     if (per_row_tile * ((rows + 31) / 32) <= 256) return 32;
-    return per_row_tile * ((rows + 63) / 64) <= 2048 / waves ? 64 : moe::MBN;
+    return n_blocks == 2 || per_row_tile * ((rows + 63) / 64) <= 512 ? 64 : moe::MBN;
 }
 
 // Ranges of the reduction of a moe_linear's product on 128 x 128 tiles: as many, up
@@ -1262,9 +1295,18 @@ static hipError_t launch_any(const moe::GemmArgs* a, hipStream_t s)
 {
     const int M = kMode == moe::kGateUp ? 2 * a->f : a->d;
     if (a->mid) {
-        constexpr int kW = moe::kMidWaves<kMode, kE4m3>;
-        hipLaunchKernelGGL((moe::gemm_mid_kernel<kMode, kE4m3>), gemm_grid(a, M / (32 * kW) * a->k_split, kE4m3 ? a->mid_rows : moe::MBN),
-                           dim3(64 * kW), 0, s, *a);
+        const int rows = kE4m3 ? a->mid_rows : moe::MBN;
+        const auto launch = [&](auto blocks) {
+            constexpr int kFB = decltype(blocks)::value;
+            hipLaunchKernelGGL((moe::gemm_mid_kernel<kMode, kE4m3, kFB>),
+                               gemm_grid(a, M / (kFB * moe::MBM) * a->k_split, rows), dim3(moe::kThreads), 0, s, *a);
+        };
+        if constexpr (kE4m3 && kMode == moe::kGateUp)
+            launch(std::integral_constant<int, 2>{});
+        else if constexpr (kE4m3 && kMode == moe::kDown)
+            a->mid_blocks == 2 ? launch(std::integral_constant<int, 2>{}) : launch(std::integral_constant<int, 1>{});
+        else
+            launch(std::integral_constant<int, 1>{});
     } else {
         hipLaunchKernelGGL((moe::gemm_kernel<kMode, kE4m3>), gemm_grid(a, M / moe::BM, moe::BN), dim3(moe::kThreads), 0, s,
                            *a);

@@ -447,6 +447,31 @@ def test_layer_that_takes_the_large_tiles(torch):
     L.layer.close()
 
 
+def test_layer_of_more_rows_than_the_small_tiles_take(torch):
+    """640 tiles of 256 x 256 for gate/up, 1050 rows to an expert."""
+    L = Layer(torch, 256, 2048, 8, 2, 4200, seed=6)
+    L.run(ref.bf16_bits(activations(4200, 256, seed=6)))
+    L.layer.close()
+
+
+@pytest.mark.parametrize("T,d,f,E,k", [(1600, 2048, 128, 8, 2), (601, 1536, 384, 32, 4), (3000, 512, 256, 16, 4),
+                                       (2501, 1024, 128, 16, 2)])
+def test_down_on_tiles_of_two_feature_blocks(torch, T, d, f, E, k):
+    """384 and more tiles of 256 features and 64 rows, full and partial ones, two and more stages of
+    K: against the oracle, and the same bits as the 256 x 256 tiles."""
+    L = Layer(torch, d, f, E, k, T, seed=T)
+    bits = ref.bf16_bits(activations(T, d, seed=T))
+    small = L.run(bits).clone()
+    stamps = torch.zeros((4, 8), dtype=torch.int64, device="cuda")
+    moe.moe_profile_gemm_timeline(L.layer.ctx, None, stamps.data_ptr(), 4)
+    large = L.run(bits).clone()
+    torch.cuda.synchronize()
+    assert int(stamps.abs().sum()) > 0
+    moe.moe_profile_gemm_timeline(L.layer.ctx, None, None, 0)
+    assert torch.equal(small, large)
+    L.layer.close()
+
+
 @pytest.mark.parametrize("T", [3, 16, 50, 600])
 @pytest.mark.parametrize("first,local", [(0, 2), (5, 3), (7, 1)])
 def test_a_share(torch, T, first, local):
