@@ -191,7 +191,9 @@ MOE_API moe_status moe_load_router(moe_ctx *ctx, int32_t layer, const float *wr,
  *   balance      : fp32 [E], device memory of the caller, or NULL (zeros).  It is
  *                  read by each routing of the layer, so it stays allocated while
  *                  the policy is set; values written to it are seen by the next
- *                  routing, a captured graph's replays included. */
+ *                  routing, a captured graph's replays included.  A graph keeps the
+ *                  policy that its routings were captured under, and reads that
+ *                  one's balance as long as it is replayed. */
 typedef enum { MOE_SCORE_SELECTED = 0, MOE_SCORE_SOFTMAX = 1, MOE_SCORE_SIGMOID = 2 } moe_score;
 typedef struct {
     int32_t score, n_groups, top_groups, group_best, renormalize;
@@ -382,8 +384,8 @@ typedef enum { MOE_T_F32 = 0, MOE_T_BF16 = 1 } moe_type;
  * 16-byte aligned); codes [T][n] bytes; scales [T][ceil(n / 128)] bytes, each
  * e + 127 (the biased exponent of 2^e).  n a positive multiple of 16 (at most
  * 2^24), T at most 2^24; T == 0 is a no-op.  Enqueued on stream; allocates
- * nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n or > 2^32, arrays that overlap,
- * x's from its first element to its last), MOE_E_SHAPE (n, T),
+ * nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n or > 2^32, arrays
+ * that overlap, x's from its first element to its last), MOE_E_SHAPE (n, T),
  * MOE_E_ALIGN (x, codes, or a stride that is no multiple of 16 bytes). */
 MOE_API moe_status moe_quantize_e4m3(const void *x, int64_t ld, int32_t type, int32_t T, int32_t n,
                                      uint8_t *codes, uint8_t *scales, moe_stream_t stream);

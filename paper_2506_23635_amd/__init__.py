@@ -447,7 +447,8 @@ class MoeLayer:
 
     def set_policy(self, layer, policy, balance=None):
         """moe_set_policy: policy from make_policy, or None; balance: fp32 [n_experts] on the
-        layer's device (kept here, and read by every routing of the layer), or None."""
+        layer's device (kept here until the next call, and read by every routing of the layer),
+        or None.  A graph captured under a policy goes on reading that policy's balance."""
         if policy is None:
             if balance is not None:
                 raise MoeError(-1, "a balance needs a policy")
