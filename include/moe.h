@@ -247,10 +247,12 @@ MOE_API moe_status moe_forward(moe_ctx *ctx, int32_t layer, const uint16_t *x,
  * of MOE_STATIC_SCRATCH_BYTES that the library holds on each GPU it runs on
  * until the process ends, not in the context's workspace.  The call leaves
  * the workspace untouched (a routing from moe_route stays valid) and calls no
- * allocating routine.  T is limited by max_tokens and by the scratch: the
- * workspace that moe_workspace_bytes reports for max_tokens = T must fit in
- * MOE_STATIC_SCRATCH_BYTES (T <= 40 at d 6144, f 10752, 16 experts, top-4);
- * beyond either, MOE_E_CAPACITY and nothing is enqueued.  The context's
+ * allocating routine.  T is limited by max_tokens and by the scratch.  Every T
+ * is taken for which the workspace that moe_workspace_bytes reports for
+ * max_tokens = T fits in MOE_STATIC_SCRATCH_BYTES, and some more, since here
+ * the routing's partial sums share O's space (T <= 45 at d 6144, f 10752, 16
+ * experts, top-4, with MOE_E4M3 T <= 30; T <= 2015 at d 256, f 512, 8 experts,
+ * top-2); beyond either, MOE_E_CAPACITY and nothing is enqueued.  The context's
  * device must be current.  Every call on a GPU shares that GPU's array and
  * leaves its contents behind: calls that overlap on one GPU (two streams, two
  * host threads) race and must be ordered by the caller.  The first call on a

@@ -61,7 +61,11 @@ const char* check_config(const moe_config* c)
     return nullptr;
 }
 
-Layout make_layout(const moe_config* c)
+// The arena and the workspace.  one_call (the static scratch): of a single forward of
+// max_tokens tokens, whose routing's partial sums lie in O's space behind x's rounded
+// values (O is written when both have been read; with a region of their own, up to 512
+// KiB, d 256, f 512, 8 experts, top-2 had room for 1955 tokens, now 2015).
+Layout make_layout(const moe_config* c, bool one_call = false)
 {
     Layout L{};
     const size_t d = c->d_model, f = c->ffn_dim, E = c->n_experts, k = c->top_k;
@@ -96,7 +100,8 @@ Layout make_layout(const moe_config* c)
         L.region_bytes[region] = bytes;
         return o;
     };
-    L.dpart_off = take(MOE_WS_ROUTE_PARTIALS, moe_route_partial_bytes(c->max_tokens, c->d_model, c->n_experts));
+    const size_t dpart_bytes = moe_route_partial_bytes(c->max_tokens, c->d_model, c->n_experts);
+    if (!one_call) L.dpart_off = take(MOE_WS_ROUTE_PARTIALS, dpart_bytes);
     L.logits_off = take(MOE_WS_LOGITS, Tm * E * 4);
     L.idx_off = take(MOE_WS_TOPK_IDX, Tm * k * 4);
     L.w_off = take(MOE_WS_TOPK_W, Tm * k * 4);
@@ -114,7 +119,13 @@ Layout make_layout(const moe_config* c)
     }
     L.h_off = take(MOE_WS_H, h_bytes);
     L.h32_off += L.h_off;
-    L.o_off = take(MOE_WS_O, (size_t)L.rows_max * d * 4);
+    size_t o_bytes = (size_t)L.rows_max * d * 4;
+    if (one_call) {
+        L.dpart_off = e4m3 ? align_up(Tm * d * 2, kAlign) : 0;
+        o_bytes = std::max(o_bytes, L.dpart_off + dpart_bytes);
+    }
+    L.o_off = take(MOE_WS_O, o_bytes);
+    if (one_call) L.dpart_off += L.o_off;
     L.ws_bytes = off;
     return L;
 }
@@ -757,10 +768,10 @@ moe_status moe_forward_static(moe_ctx* ctx, int32_t layer, const uint16_t* x, in
     if (T == 0) return MOE_OK;
     if (!x || !y) return fail(ctx, MOE_E_ARG, "x or y is NULL");
     if (misaligned(x) || misaligned(y)) return fail(ctx, MOE_E_ALIGN, "x and y must be 16-byte aligned");
-    // the workspace layout of this T, carved from the static scratch
+    // the layout of this T, carved from the static scratch
     moe_config c = ctx->cfg;
     c.max_tokens = T;
-    const Layout L = make_layout(&c);
+    const Layout L = make_layout(&c, true);
     if (L.ws_bytes > MOE_STATIC_SCRATCH_BYTES)
         return fail(ctx, MOE_E_CAPACITY,
                     "T needs " + std::to_string(L.ws_bytes) + " bytes of scratch; the static scratch holds " +
