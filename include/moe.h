@@ -251,8 +251,8 @@ MOE_API moe_status moe_forward(moe_ctx *ctx, int32_t layer, const uint16_t *x,
  * is taken for which the workspace that moe_workspace_bytes reports for
  * max_tokens = T fits in MOE_STATIC_SCRATCH_BYTES, and some more, since here
  * the routing's partial sums share O's space (T <= 45 at d 6144, f 10752, 16
- * experts, top-4, with MOE_E4M3 T <= 30; T <= 2015 at d 256, f 512, 8 experts,
- * top-2); beyond either, MOE_E_CAPACITY and nothing is enqueued.  The context's
+ * experts, top-4, with MOE_E4M3 or without; T <= 2015 at d 256, f 512, 8
+ * experts, top-2); beyond either, MOE_E_CAPACITY and nothing is enqueued.  The context's
  * device must be current.  Every call on a GPU shares that GPU's array and
  * leaves its contents behind: calls that overlap on one GPU (two streams, two
  * host threads) race and must be ordered by the caller.  The first call on a
@@ -302,7 +302,7 @@ typedef enum {
     MOE_WS_TILES,              /* int32 [max_tiles][2]: token tiles of 256 rows (expert, first row);
                                   for inspection, no kernel reads them */
     MOE_WS_N_TILES,            /* int32 [1], likewise */
-    MOE_WS_H,                  /* bf16 [rows_max, f]; MOE_E4M3: then fp32 values on the way */
+    MOE_WS_H,                  /* bf16 [rows_max, f]; MOE_E4M3: of up to 16 tokens, then fp32 values on the way */
     MOE_WS_O,                  /* fp32 [rows_max, d]; MOE_E4M3: x's rounded values before */
     MOE_WS_COUNT
 } moe_ws_region;

@@ -113,9 +113,12 @@ Layout make_layout(const moe_config* c, bool one_call = false)
     L.tiles_off = take(MOE_WS_TILES, (size_t)L.max_tiles * 2 * 4);
     L.n_tiles_off = take(MOE_WS_N_TILES, 4);
     size_t h_bytes = (size_t)L.rows_max * f * 2;
-    if (e4m3) {
-        L.h32_off = align_up(h_bytes, kAlign);
-        h_bytes = L.h32_off + std::min<size_t>(Tm, kDecodeMaxTokens) * kl * f * 4;
+    if (e4m3 && !(one_call && Tm > kDecodeMaxTokens)) {
+        // a call of few tokens has its fp32 values behind its own rows of H, in space
+        // that the rows of larger calls take
+        const size_t few = std::min<size_t>(Tm, kDecodeMaxTokens) * kl;
+        L.h32_off = align_up(few * f * 2, kAlign);
+        h_bytes = std::max(h_bytes, L.h32_off + few * f * 4);
     }
     L.h_off = take(MOE_WS_H, h_bytes);
     L.h32_off += L.h_off;

@@ -60,3 +60,14 @@ def test_partial_sums_beside_the_rounded_rows(torch, d, E, k, first, local, flag
     for T in (1, 2, 5, 16, 17, 18, 33, 100, 400):
         check_equal(torch, layer, x[:T])
     layer.close()
+
+
+@pytest.mark.parametrize("d,f,E,k,T", [(256, 512, 8, 2, 2015), (1024, 2048, 8, 2, 509), (4096, 2048, 32, 2, 203),
+                                       (256, 10752, 16, 4, 92)])
+def test_as_many_tokens_with_experts_in_e4m3(torch, d, f, E, k, T):
+    """The fp32 values of H of few tokens take no space from a call of more; calls of few tokens beside
+    them stay right in a context for many."""
+    layer, x = make(torch, d, f, E, k, T, moe.MOE_E4M3)
+    for n in (T, 16, 3, T, 1):
+        check_equal(torch, layer, x[:n])
+    layer.close()
