@@ -46,6 +46,7 @@
 
 #include "e4m3.h"
 #include "moe_common.h"
+#include "tile_order.h"
 
 namespace moe {
 
@@ -838,15 +839,8 @@ __device__ __forceinline__ void write_stamp(const GemmArgs& a, uint64_t r0, uint
 // and down 215 + 143 us, so 174 + 120; on DBRX's gate/up, 84 tiles, a share of 4
 // experts with skewed loads, 1300 tokens, whole layer 587 -> 550 us.)
 //
-// Narrow matrices (below 2048 features) are one list of the experts' tiles, an
-// eighth of it for each XCD, so that most experts' weights and token rows are
-// read through one L2 (dealt as above every XCD reads every expert's: 32 experts
-// of d 512, f 4096, 4000 tokens, down 149 us against 103; 16 of d 1024, f 4096,
-// 1900 tokens, 112 against 98).  At 2048 features and more the XCDs stay with one
-// expert at a time (8 experts of d 2048, f 8192, 4000 tokens, down 304 us
-// against 354 from a list).  Whole layer, 8 experts, top-2, d 256, f 512, 32768
-// tokens: 505 us with tile ft on XCD ft % 8, now 335.
-constexpr int kNarrow = 2048;      // features
+// Narrow matrices are one list of the experts' tiles, an eighth of it for each XCD
+// (tile_order.h).
 
 struct TilePos {
     int el;            // local expert, or -1 past the last tile
@@ -856,10 +850,13 @@ struct TilePos {
     int ft;            // feature tile
 };
 
-__device__ __forceinline__ TilePos find_tile(const GemmArgs& a, int block, int n_ftiles, int tile_rows)
+// features: the matrix's (n_ftiles counts its tiles in every range of K); small_e4m3:
+// gemm_mid_kernel's tiles on e4m3 weights
+__device__ __forceinline__ TilePos find_tile(const GemmArgs& a, int block, int features, int n_ftiles, int tile_rows,
+                                             bool small_e4m3)
 {
     // groups of eight, and the rest
-    const int n_fg = n_ftiles * tile_rows < kNarrow ? 0 : n_ftiles / kXcds, n_left = n_ftiles - n_fg * kXcds;
+    const int n_fg = one_list(features, small_e4m3) ? 0 : n_ftiles / kXcds, n_left = n_ftiles - n_fg * kXcds;
     const int pos = block / kXcds, xcd = block % kXcds;
     const int lane = threadIdx.x & 63;
     int first = 0, rows = 0;
@@ -916,7 +913,7 @@ __global__ __launch_bounds__(kThreads) void gemm_kernel(GemmArgs a)
     __shared__ __attribute__((aligned(16))) uint8_t lds[kRingB * B_STAGE_BYTES];
     const int M = kMode == kGateUp ? 2 * a.f : a.d;   // a multiple of BM
     const int n_ftiles = M / BM;
-    const TilePos tp = find_tile(a, blockIdx.x, n_ftiles, BN);
+    const TilePos tp = find_tile(a, blockIdx.x, M, n_ftiles, BN, false);
     if (tp.el < 0) return;
     const int ft = tp.ft, tt = tp.before + tp.sub, e = a.e_begin + tp.el;
     const int row_start = tp.first + tp.sub * BN, row_end = min(row_start + BN, tp.first + tp.rows);
@@ -1110,8 +1107,8 @@ __global__ __launch_bounds__(kThreads, 2) void gemm_mid_kernel(GemmArgs a)
     constexpr int kStore = kMode == kGateUp ? MBN * (kFeat + 16) + (kE4m3 ? 4 * MBN * 4 : 0) : 2 * 32 * (kFeat * 4 + 16);
     constexpr int kRings = kMidRingB * MBN * BK * 2;
     __shared__ __attribute__((aligned(16))) uint8_t lds[kRings > kStore ? kRings : kStore];
-    const int n_ftiles = (kMode == kGateUp ? 2 * a.f : a.d) / kFeat;
-    const TilePos tp = find_tile(a, blockIdx.x, n_ftiles * a.k_split, kE4m3 ? a.mid_rows : MBN);
+    const int M = kMode == kGateUp ? 2 * a.f : a.d, n_ftiles = M / kFeat;
+    const TilePos tp = find_tile(a, blockIdx.x, M, n_ftiles * a.k_split, kE4m3 ? a.mid_rows : MBN, kE4m3);
     if (tp.el < 0) return;
     const int split = tp.ft / n_ftiles, ft = tp.ft % n_ftiles;
     const int e = a.e_begin + tp.el;
