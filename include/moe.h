@@ -190,7 +190,8 @@ MOE_API moe_status moe_load_router(moe_ctx *ctx, int32_t layer, const float *wr,
  *   scale        : finite.
  *   balance      : fp32 [E], device memory of the caller, or NULL (zeros).  It is
  *                  read by each routing of the layer, so it stays allocated while
- *                  the policy is set; values written to it are seen by the next
+ *                  the policy is set and until the routings enqueued under it, on
+ *                  any stream, have run; values written to it are seen by the next
  *                  routing, a captured graph's replays included.  A graph keeps the
  *                  policy that its routings were captured under, and reads that
  *                  one's balance as long as it is replayed. */

@@ -401,7 +401,8 @@ class MoeLayer:
                           if workspace is None else workspace)
         self.ctx = moe_init(cfg, _tensor_ptr(self.arena, "arena", wb, (torch.uint8,), self.device),
                             _tensor_ptr(self.workspace, "workspace", sb, (torch.uint8,), self.device))
-        self._balance = {}   # layer: the balance that its policy reads
+        self._balance = {}   # layer: (the balance that its policy reads, the streams recorded on it)
+        self._captured = []  # balances that captured graphs read
 
     @property
     def stream(self) -> int:
@@ -447,8 +448,9 @@ class MoeLayer:
 
     def set_policy(self, layer, policy, balance=None):
         """moe_set_policy: policy from make_policy, or None; balance: fp32 [n_experts] on the
-        layer's device (kept here until the next call, and read by every routing of the layer),
-        or None.  A graph captured under a policy goes on reading that policy's balance."""
+        layer's device, or None.  It is read by every routing of the layer until the next call,
+        and its memory stays its own until those have run, on whatever streams; a graph captured
+        under a policy goes on reading that policy's balance, which is kept until close()."""
         if policy is None:
             if balance is not None:
                 raise MoeError(-1, "a balance needs a policy")
@@ -458,7 +460,29 @@ class MoeLayer:
             policy = MoePolicy(policy.score, policy.n_groups, policy.top_groups, policy.group_best,
                                policy.renormalize, policy.scale, ptr)
         moe_set_policy(self.ctx, layer, policy)
-        self._balance[layer] = balance
+        if balance is not None:
+            self._balance[layer] = (balance, set())
+        else:
+            self._balance.pop(layer, None)
+
+    def _reader(self, first, n=1) -> int:
+        """The current stream, for a call that routes layers first .. first + n - 1.  The balances
+        that it will read are recorded on it, so that their memory is not given out again, once a
+        policy without them is set, before the call has run; under capture they are kept."""
+        stream = self.stream
+        if self._balance:
+            capturing = self.torch.cuda.is_current_stream_capturing()
+            for layer in (first,) if n == 1 else [i for i in self._balance if first <= i < first + n]:
+                balance, streams = self._balance.get(layer, (None, ()))
+                if balance is None:
+                    continue
+                if capturing:
+                    if not any(b is balance for b in self._captured):
+                        self._captured.append(balance)
+                elif stream not in streams:
+                    balance.record_stream(self.torch.cuda.current_stream(self.device))
+                    streams.add(stream)
+        return stream
 
     def _tokens(self, x, T):
         T = x.shape[0] if T is None else int(T)
@@ -475,7 +499,7 @@ class MoeLayer:
         lp = (_tensor_ptr(logits_in, "logits_in", T * E, (self.torch.float32,), self.device)
               if logits_in is not None else None)
         with _on_device(self.torch, self.device):
-            return moe_route(self.ctx, layer, xp, T, lp, self.stream)
+            return moe_route(self.ctx, layer, xp, T, lp, self._reader(layer))
 
     def forward(self, layer, x, y, routing=None, T=None):
         """y: bf16 [T, d], or fp32 [T, d] when the config has MOE_PARTIAL_F32."""
@@ -484,7 +508,7 @@ class MoeLayer:
         ytypes = (self.torch.float32,) if self.cfg.flags & MOE_PARTIAL_F32 else bf
         with _on_device(self.torch, self.device):
             moe_forward(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device), T, routing,
-                        _tensor_ptr(y, "y", n, ytypes, self.device), self.stream)
+                        _tensor_ptr(y, "y", n, ytypes, self.device), self._reader(layer))
 
     def forward_static(self, layer, x, y, T=None):
         """moe_forward_static: the layer with internal routing on the
@@ -494,13 +518,13 @@ class MoeLayer:
         ytypes = (self.torch.float32,) if self.cfg.flags & MOE_PARTIAL_F32 else bf
         with _on_device(self.torch, self.device):
             moe_forward_static(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device), T,
-                               _tensor_ptr(y, "y", n, ytypes, self.device), self.stream)
+                               _tensor_ptr(y, "y", n, ytypes, self.device), self._reader(layer))
 
     def forward_stack(self, x, T=None):
         T = self._tokens(x, T)
         with _on_device(self.torch, self.device):
             moe_forward_stack(self.ctx, _tensor_ptr(x, "x", T * self.cfg.d_model, _bf16_types(self.torch),
-                                                    self.device), T, self.stream)
+                                                    self.device), T, self._reader(0, self.cfg.n_layers))
 
     def forward_residual(self, layer, x, r, T=None):
         """moe_forward_residual: r = bf16(r + bf16(layer(x))) in place."""
@@ -508,7 +532,7 @@ class MoeLayer:
         n, bf = T * self.cfg.d_model, _bf16_types(self.torch)
         with _on_device(self.torch, self.device):
             moe_forward_residual(self.ctx, layer, _tensor_ptr(x, "x", n, bf, self.device),
-                                 _tensor_ptr(r, "r", n, bf, self.device), T, self.stream)
+                                 _tensor_ptr(r, "r", n, bf, self.device), T, self._reader(layer))
 
     def forward_layers(self, first, n, x, T=None):
         """moe_forward_layers: layers first .. first+n-1, x = bf16(x + y) in place."""
@@ -516,7 +540,7 @@ class MoeLayer:
         with _on_device(self.torch, self.device):
             moe_forward_layers(self.ctx, first, n,
                                _tensor_ptr(x, "x", T * self.cfg.d_model, _bf16_types(self.torch),
-                                           self.device), T, self.stream)
+                                           self.device), T, self._reader(first, n))
 
     def routing_tensors(self, r: MoeRouting):
         """Copies the routing views (device) to host numpy arrays."""
