@@ -386,8 +386,8 @@ typedef enum { MOE_T_F32 = 0, MOE_T_BF16 = 1 } moe_type;
 /* Rows to e4m3: x [T] rows of n elements of `type`, ld elements apart (rows
  * 16-byte aligned); codes [T][n] bytes; scales [T][ceil(n / 128)] bytes, each
  * e + 127 (the biased exponent of 2^e).  n a positive multiple of 16 (at most
- * 2^24), T at most 2^24; T == 0 is a no-op.  Enqueued on stream; allocates
- * nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n or > 2^32, arrays
+ * 2^24), T at most 2^24, T * ceil(n / 128) at most 2^31 (256 GiB of codes);
+ * T == 0 is a no-op.  Enqueued on stream; allocates nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n or > 2^32, arrays
  * that overlap, x's from its first element to its last), MOE_E_SHAPE (n, T),
  * MOE_E_ALIGN (x, codes, or a stride that is no multiple of 16 bytes). */
 MOE_API moe_status moe_quantize_e4m3(const void *x, int64_t ld, int32_t type, int32_t T, int32_t n,

@@ -27,21 +27,20 @@ namespace moe {
 // for: 16 lanes per block of 128, 8 elements each.  Rows are read once and written
 // once: 2048 x 6144 from bf16 to codes, 38 MB, in 7.5 us, 5.0 TB/s (two blocks per
 // thread at a time 7.5, four 9.0).  Values from n to n_pad are zeros.  n_rows
-// (device memory): rows that are written, of at most T; or NULL.  Index: the type
-// that counts the blocks (a division in 64 bits per block took longer than the
-// rest).
-template <bool kBf16, typename Index>
-__global__ __launch_bounds__(256) void quantize_kernel(const void* __restrict__ x, int64_t ld, Index T,
+// (device memory): rows that are written, of at most T; or NULL.  Blocks are counted
+// in 32 bits (a division in 64 per block took longer than the rest).
+template <bool kBf16>
+__global__ __launch_bounds__(256) void quantize_kernel(const void* __restrict__ x, int64_t ld, uint32_t T,
                                                        const int32_t* __restrict__ n_rows, int n, int n_pad,
                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                                        uint16_t* __restrict__ values)
 {
-    const Index blocks = (Index)((n + kBlock - 1) / kBlock), units = T * blocks;
+    const uint32_t blocks = (uint32_t)((n + kBlock - 1) / kBlock), units = T * blocks;
     const int piece = threadIdx.x % 16;
     const int64_t rows = n_rows ? (int64_t)*n_rows : (int64_t)T;
-    for (Index u = (Index)blockIdx.x * 16 + threadIdx.x / 16; u < units; u += (Index)gridDim.x * 16) {
+    for (uint32_t u = blockIdx.x * 16 + threadIdx.x / 16; u < units; u += gridDim.x * 16) {
         const int64_t t = (int64_t)(u / blocks);
-        const int b = (int)(u - (Index)t * blocks), k = b * kBlock + piece * 8;
+        const int b = (int)(u - (uint32_t)t * blocks), k = b * kBlock + piece * 8;
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (k < n) {
             if constexpr (kBf16) {
@@ -261,18 +260,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(E4m3Args a)
 
 extern "C" {
 
+// At most 2^31 blocks in all (and 16 of each of up to 65536 workgroups past them).
 hipError_t moe_launch_quantize(const void* x, int64_t ld, int bf16, int64_t T, const int32_t* n_rows, int n,
                                int n_pad, uint8_t* codes, uint8_t* scales, uint16_t* values, hipStream_t s)
 {
     const int64_t units = T * ((n + moe::kBlock - 1) / moe::kBlock), wgs = (units + 15) / 16;
     const dim3 grid((unsigned)(wgs < 65536 ? wgs : 65536)), block(256);
-    if (units + (int64_t)grid.x * 16 <= UINT32_MAX) {
-        const auto kernel = bf16 ? moe::quantize_kernel<true, uint32_t> : moe::quantize_kernel<false, uint32_t>;
-        hipLaunchKernelGGL(kernel, grid, block, 0, s, x, ld, (uint32_t)T, n_rows, n, n_pad, codes, scales, values);
-    } else {
-        const auto kernel = bf16 ? moe::quantize_kernel<true, int64_t> : moe::quantize_kernel<false, int64_t>;
-        hipLaunchKernelGGL(kernel, grid, block, 0, s, x, ld, T, n_rows, n, n_pad, codes, scales, values);
-    }
+    const auto kernel = bf16 ? moe::quantize_kernel<true> : moe::quantize_kernel<false>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, x, ld, (uint32_t)T, n_rows, n, n_pad, codes, scales, values);
     return hipGetLastError();
 }
 

@@ -18,6 +18,7 @@ constexpr int kSplitRows = 64;          // ... up to these rows there are always
 constexpr int kMostSplit = 16384;       // ... and beyond these none has ranges (two feature tiles at least)
 constexpr int kFeatures = 256;          // packed features come in multiples of a tile's
 constexpr int64_t kMostStride = 1ll << 32;   // elements between rows (offsets stay below 2^63)
+constexpr int64_t kMostBlocks = 1ll << 31;   // that moe_quantize_e4m3 codes in a call
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -112,6 +113,7 @@ moe_status moe_quantize_e4m3(const void* x, int64_t ld, int32_t type, int32_t T,
     if (type != MOE_T_F32 && type != MOE_T_BF16) return MOE_E_ARG;
     if (T < 0) return MOE_E_ARG;
     if (n < 16 || n % 16 || n > 1 << 24 || T > 1 << 24) return MOE_E_SHAPE;
+    if ((int64_t)T * ((n + moe::kBlock - 1) / moe::kBlock) > kMostBlocks) return MOE_E_SHAPE;
     if (T == 0) return MOE_OK;
     if (!x || !codes || !scales || ld < n || ld > kMostStride) return MOE_E_ARG;
     const int size = type == MOE_T_F32 ? 4 : 2, blocks = (n + moe::kBlock - 1) / moe::kBlock;
