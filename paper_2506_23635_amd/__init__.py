@@ -287,12 +287,19 @@ def make_policy(score=SCORE_SELECTED, n_groups=1, top_groups=1, group_best=1, re
     return MoePolicy(score, n_groups, top_groups, group_best, int(renormalize), scale, None)
 
 
+def _int32_or_refused(v) -> int:
+    """v as the library's int32, or the end of its range that it refuses (ctypes takes 2^32 for 0)."""
+    return max(-1, min(v, 2 ** 31 - 1))
+
+
 def moe_set_policy(ctx, layer, policy):
-    _check(ctx, lib().moe_set_policy(ctx, layer, ctypes.byref(policy) if policy is not None else None))
+    _check(ctx, lib().moe_set_policy(ctx, _int32_or_refused(layer),
+                                     ctypes.byref(policy) if policy is not None else None))
 
 
 def moe_quantize_e4m3(x_ptr, ld, x_type, T, n, codes_ptr, scales_ptr, stream=0):
-    st = lib().moe_quantize_e4m3(x_ptr, ld, x_type, T, n, codes_ptr, scales_ptr, stream)
+    st = lib().moe_quantize_e4m3(x_ptr, ld, x_type, _int32_or_refused(T), _int32_or_refused(n), codes_ptr,
+                                 scales_ptr, stream)
     if st != MOE_OK:
         raise MoeError(st, lib().moe_status_string(st).decode())
 
@@ -683,7 +690,7 @@ def moe_linear_load(ctx, w_ptr, stream=0):
 
 
 def moe_linear_forward(ctx, x_ptr, ldx, y_ptr, y_type, T, stream=0):
-    _lcheck(ctx, lib().moe_linear_forward(ctx, x_ptr, ldx, y_ptr, y_type, T, stream))
+    _lcheck(ctx, lib().moe_linear_forward(ctx, x_ptr, ldx, y_ptr, y_type, _int32_or_refused(T), stream))
 
 
 class E4m3Linear:
