@@ -371,14 +371,19 @@ MOE_API moe_status moe_profile_gemm_timeline(moe_ctx *ctx, uint64_t *gateup, uin
  * sums that it enters.  Weights that are e4m3 codes times powers of two already
  * keep their values exactly when they are passed as bf16.
  *
- * A product's terms are exact and are summed in fp32.
+ * A product's terms are exact (as far as fp32's range goes) and are summed in fp32.
  *
  * With MOE_E4M3 a layer of moe_init has its experts so: moe_load_expert codes the
  * three matrices as it repacks them, and per token and chosen expert
  *   G = Q(x) Q(W1),  U = Q(x) Q(V1),  H = Q(silu(G) * U),  o = H Q(W2),
- * Q being the rounding above (H's from fp32), G, U and o fp32.  The router takes
- * x itself.  Every call works on such a layer; the arena needs half of the bytes
- * (plus the scales'). */
+ * Q being the rounding above (H's from fp32), G, U and o fp32.  An element of H
+ * whose exact value lies next to a border of the grid is rounded to the side that
+ * the fp32 sums end on, so that another order of sums gives outputs that differ
+ * by shares of such an element's step (2^-3 of it) rather than by fp32 rounding (64
+ * tokens of d 6144, f 10752: 2e-4 of the outputs' norm, whose own rounding to bf16 is
+ * 1.7e-3); a call repeats itself bit for bit.  The router takes x itself.  Every
+ * call works on such a layer; the arena needs half of the bytes (plus the
+ * scales'). */
 
 /* Types of elements. */
 typedef enum { MOE_T_F32 = 0, MOE_T_BF16 = 1 } moe_type;

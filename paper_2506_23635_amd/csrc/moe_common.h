@@ -79,7 +79,11 @@ __device__ inline uint32_t cvt_pk_bf16(float lo, float hi)
 
 // silu(g) * u with an overflow-free logistic: for g << 0, exp(-g) -> inf,
 // 1 / inf -> 0 and g * 0 -> -0, which is the limit.  The reciprocal is the
-// hardware one (1 ulp): the result is rounded to bf16 next.
+// hardware one (1 ulp): the result is rounded to bf16 next, or to the e4m3 grid,
+// where it decides fewer roundings than the order of the sums in g and u does (d
+// 6144, f 10752, 16 experts, 8192 rows of H: 8e-7 of the elements lie elsewhere than
+// the exact value's rounding if only this is in fp32, 7e-7 with an exp and a
+// division of the full precision, 7.5e-6 with fp32 sums).
 __device__ inline float silu_mul(float g, float u)
 {
     return g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * u;

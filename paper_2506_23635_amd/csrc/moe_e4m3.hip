@@ -9,9 +9,9 @@
 // values on the e4m3 grid.  The matrix instructions that take 8-bit operands
 // would do the same work at twice the rate, but their sums are not fp32 sums:
 // within a lane's terms they are aligned to the largest and lose what lies below
-// 2^-13 of it (probed with powers of two; all three forms, 16x16x32 and the
-// scaled 16x16x128 and 32x32x64).  A product of 333 x 1040 x 1488 came out 4.9e-5
-// from its fp64 value so, where fp32 sums leave 1e-7, and it moves silu(G) U
+// 2^-13 of it (profiles/e4m3_mfma_sums.txt: 16x16x32 and the scaled 16x16x128 and
+// 32x32x64, beside bf16's, which keep 2^-24).  A product of 333 x 1040 x 1488 came
+// out 4.9e-5 from its fp64 value so, where fp32 sums leave 1e-7, and it moves silu(G) U
 // across rounding borders before the down product.
 #include <cmath>
 #include <cstring>
