@@ -25,8 +25,8 @@ namespace moe {
 
 // Rows to codes and scales, or (codes NULL) to the bf16 values that these stand
 // for: 16 lanes per block of 128, 8 elements each.  Rows are read once and written
-// once: 2048 x 6144 from bf16 to codes, 38 MB, in 7.5 us, 5.0 TB/s (two blocks per
-// thread at a time 7.5, four 9.0).  Values from n to n_pad are zeros.  n_rows
+// once: 2048 x 6144 from bf16 to codes, 38 MB, in 7.5 to 8.1 us, 4.7 to 5.0 TB/s (two
+// blocks per thread at a time 7.5, four 9.0).  Values from n to n_pad are zeros.  n_rows
 // (device memory): rows that are written, of at most T; or NULL.  Blocks are counted
 // in 32 bits (a division in 64 per block took longer than the rest).
 template <bool kBf16>

@@ -1206,13 +1206,16 @@ int moe_gemm_mid_tiles(int T, int k, int E, int n_local, int M)
 // The same for experts in e4m3.  Half of the weight bytes leave the 256 x 256 tiles,
 // one workgroup per CU, more exposed: their partial tiles and uneven last round cost
 // until an expert has 180 rows, or, with few tiles, 400, or, with two per CU, at all
-// (whole layer, 256 x 256 tiles -> the small ones for both products; d 6144, f 10752,
-// 16 experts, top-4: 512 tokens 1037 -> 969 us, 700 (175 rows, 1344 tiles) 1240 ->
-// 1171, 800 1257 -> 1312; 4 of the 16: 700 tokens 446 -> 322, 1400 (350 rows, 672
-// tiles) 568 -> 476, 2000 (500) 636 -> 652; 8 experts, top-2, d 1024, f 2048: 2000
-// tokens (500 rows, 256 tiles) 117 -> 88, 4000 (1000, 512) 152 -> 140; 16 of d 4096, f
-// 2048, top-2: 1700 tokens 277 -> 220; 32 of d 2048, f 4096, top-4: 2000 tokens (250
-// rows, 1024 tiles) 480 -> 447, 3000 (375, 2048) 618 -> 625).
+// (whole layer, 256 x 256 tiles -> the small ones for both products, loads as even
+// as random logits make them, and in brackets with a bias of 0.3 on those; d 6144, f
+// 10752, 16 experts, top-4: 512 tokens 1048 -> 978 us (1053 -> 978), 700 (175 rows, 1344
+// tiles) 1296 -> 1149 (1243 -> 1211), 800 1313 -> 1318 (1458 -> 1348); 4 of the 16: 700
+// tokens 452 -> 360 (448 -> 377), 1400 (350 rows, 672 tiles) 600 -> 569 (638 -> 612), 2000
+// (500) 669 -> 704 (832 -> 826); 8 experts, top-2, d 1024, f 2048: 2000 tokens (500 rows,
+// 256 tiles) 109 -> 94 (122 -> 93), 4000 (1000, 512) 150 -> 143 (162 -> 135); 16 of d 4096,
+// f 2048, top-2: 1700 tokens 200 -> 222 (288 -> 225); 32 of d 2048, f 4096, top-4: 2000
+// tokens (250 rows, 1024 tiles) 515 -> 469 (509 -> 459), 3000 (375, 2048) 662 -> 643 (693 ->
+// 642)).
 int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M)
 {
     const int64_t rows = ((int64_t)T * k + E - 1) / E;
@@ -1223,12 +1226,13 @@ int moe_gemm_mid_tiles_e4m3(int T, int k, int E, int n_local, int M)
 // 128-feature halves of these tiles for the down product of experts in e4m3: two
 // (256 features of 64 token rows) where three quarters of the CUs' workgroups have one
 // and the rows fill them, else one (128 of up to 128).  A B fragment is read from LDS
-// once for two MFMAs (whole layer, one -> two: d 6144, f 10752, 16 experts, top-4, 384
-// tiles of 64 rows and more: 200 tokens 629 -> 613 us, 512 1038 -> 987, 1000 1705 ->
-// 1582; 64 tokens, 16 rows per expert, 527 -> 533; 4 of the 16: 700 tokens, 288 tiles,
-// 322 -> 335, 1000, 384 tiles, 394 -> 405, 1400, 576 tiles, 506 -> 472; 32 of d 1536,
-// 1025 tokens, 384 tiles, 92.7 -> 80.3; 8 of d 1024, 100 tokens, 32 tiles, 37.0 ->
-// 41.5).
+// once for two MFMAs (whole layer, one -> two, loads as above; d 6144, f 10752, 16
+// experts, top-4, 384 tiles of 64 rows and more: 200 tokens 609 -> 607 us (626 -> 620),
+// 350 798 -> 816, 512 1035 -> 1009 (979 -> 972), 1000 1567 -> 1576 (1615 -> 1611); 64 tokens,
+// 16 rows per expert, 525 -> 535 (530 -> 537); 4 of the 16: 700 tokens, 288 tiles, 354 ->
+// 374 (375 -> 380), 1000, 384 tiles, 487 -> 448 (511 -> 465), 1400, 576 tiles, 591 -> 589 (637
+// -> 630); 32 of d 1536, 1025 tokens, 384 tiles, 104 -> 98; 8 of d 1024, 100 tokens, 32 tiles,
+// 41 -> 45).
 int moe_gemm_mid_blocks(int T, int k, int E, int n_local, int M)
 {
     const int64_t rows = ((int64_t)T * k + E - 1) / E;
@@ -1240,9 +1244,9 @@ int moe_gemm_mid_blocks(int T, int k, int E, int n_local, int M)
 // features per expert, n_split ranges of K: 32 where that leaves one workgroup per CU
 // at most, 64 up to as many as run at once, two per CU.  The shorter tiles' stages take
 // less time each, where there are too few tiles for the CUs to hide it (a plain
-// product, 32 / 64 / 128 rows: 1040 to 1488 features, 12 tiles, 333 tokens 10.2 / 11.8
-// / 15.8 us, 1024 tokens 14.3 / 14.3 / 18.1, 2048 22.3 / 20.3 / 21.2; 4096 to 4096, two
-// ranges, 200 tokens 24.4 / 21.3 / 22.6; 512 to 2048, 2048 tokens 16.9 / 14.7 / 15.6).
+// product, 32 / 64 / 128 rows: 1040 to 1488 features, 12 tiles, 333 tokens 10.7 / 12.0
+// / 15.3 us, 1024 tokens 13.2 / 13.0 / 15.9, 2048 19.3 / 18.3 / 18.0; 4096 to 4096, two
+// ranges, 200 tokens 23.3 / 21.6 / 24.7; 512 to 2048, 2048 tokens 15.9 / 14.0 / 14.2).
 int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int n_blocks)
 {
     const int64_t rows = ((int64_t)T * k + E - 1) / E;
@@ -1253,10 +1257,12 @@ int moe_gemm_mid_rows(int T, int k, int E, int n_local, int M, int n_split, int 
 
 // Ranges of the reduction of a moe_linear's product on 128 x 128 tiles: as many, up
 // to 4, as leave every range kSplitStages stages and the grid one workgroup per CU
-// (6144 to 8192 features: 64 tokens, 64 tiles, 33.0 -> 23.7 us in four ranges, 200
-// tokens, 128 tiles, 45.8 -> 37.2 in two, 512 tokens, 256 tiles, 53.7 -> 59.2; 2048 to
-// 512: 1024 tokens, 32 tiles of 32 stages, 24.1 -> 20.9 in two; 1040 to 1488: 1024
-// tokens, 96 tiles of 18 stages, 19.0 -> 23.0).
+// (6144 to 8192 features: 64 tokens, 64 tiles, one / two / four ranges 28.0 / 24.0 /
+// 21.9 us; 512 tokens, 256 tiles, 59.7 / 63.6 / 76.1; 1040 to 1488: 1024 tokens, 96 tiles
+// of 18 stages, one 13.6, two 19.2).  The rule counts tiles of 128 rows; where
+// moe_gemm_mid_rows then takes shorter ones, one range is quicker in places: 6144 to
+// 8192, 200 tokens, 31.7 / 35.1 / 37.3; 2048 to 512, 1024 tokens, 13.2 against 14.6 in
+// two.
 constexpr int kSplitStages = 16;
 int moe_gemm_linear_split(int T, int K, int M)
 {
