@@ -253,8 +253,8 @@ MOE_API moe_status moe_forward(moe_ctx *ctx, int32_t layer, const uint16_t *x,
  * max_tokens = T fits in MOE_STATIC_SCRATCH_BYTES, and some more, since here
  * the routing's partial sums share O's space (T <= 45 at d 6144, f 10752, 16
  * experts, top-4, with MOE_E4M3 or without; T <= 2015 at d 256, f 512, 8
- * experts, top-2); beyond either, MOE_E_CAPACITY and nothing is enqueued.  The context's
- * device must be current.  Every call on a GPU shares that GPU's array and
+ * experts, top-2); beyond either, MOE_E_CAPACITY and nothing is enqueued.  The
+ * context's device must be current.  Every call on a GPU shares that GPU's array and
  * leaves its contents behind: calls that overlap on one GPU (two streams, two
  * host threads) race and must be ordered by the caller.  The first call on a
  * device looks up the array's device address (a runtime query, no
@@ -392,9 +392,10 @@ typedef enum { MOE_T_F32 = 0, MOE_T_BF16 = 1 } moe_type;
  * 16-byte aligned); codes [T][n] bytes; scales [T][ceil(n / 128)] bytes, each
  * e + 127 (the biased exponent of 2^e).  n a positive multiple of 16 (at most
  * 2^24), T at most 2^24, T * ceil(n / 128) at most 2^31 (256 GiB of codes);
- * T == 0 is a no-op.  Enqueued on stream; allocates nothing.  Errors: MOE_E_ARG (NULL, negative T, type, ld < n or > 2^32, arrays
- * that overlap, x's from its first element to its last), MOE_E_SHAPE (n, T),
- * MOE_E_ALIGN (x, codes, or a stride that is no multiple of 16 bytes). */
+ * T == 0 is a no-op.  Enqueued on stream; allocates nothing.  Errors: MOE_E_ARG
+ * (NULL, negative T, type, ld < n or > 2^32, arrays that overlap, x's from its
+ * first element to its last), MOE_E_SHAPE (n, T), MOE_E_ALIGN (x, codes, or a
+ * stride that is no multiple of 16 bytes). */
 MOE_API moe_status moe_quantize_e4m3(const void *x, int64_t ld, int32_t type, int32_t T, int32_t n,
                                      uint8_t *codes, uint8_t *scales, moe_stream_t stream);
 
